@@ -361,14 +361,114 @@ int augtree_prompt_grad_reduce(int32_t n_tensors, int64_t rows, int32_t heads, i
                                int64_t part_stride, const float* parts, const int32_t* row_map,
                                uint16_t* out, float* out_f32, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * Linear attention over replay trees
+ *
+ * The mixing layer of models whose layers keep a decayed state instead of a KV
+ * cache, on the same packed batches of replay trees. With gamma the decay of a
+ * KV head, s = softmax_scale and rows numbered through a prompt and on through
+ * a branch (the first row of a branch follows the last one of its prompt):
+ *   o_t = s sum_{j <= t} gamma^(t-j) (q_t . k_j) v_j  +  s gamma^(t+1) q_t S_0
+ *   S_t = gamma S_(t-1) + k_t v_t^T                     [d_k, d_v], fp32
+ * over the rows j of t's prompt and of its own branch. The prompt's state is
+ * computed once and every branch goes on from it; in the backward the branches'
+ * gradients of that state are added, in branch order, to what the prompt's own
+ * rows receive (the linear form of Eq. 2).
+ *
+ * decay: HOST array [num_kv_heads], 0 < decay <= 1, at most 256 KV heads. It is a
+ * constant of the layer: no gradient is formed for it.
+ * The rows of a chunk (64 rows) of a sequence pass through common matrix
+ * products, so a NaN or infinity in one row may reach earlier rows of its
+ * chunk too; it never reaches another tree, or from a branch any other branch.
+ * Every call enqueues kernels only and may be captured into a graph; calls that
+ * share a workspace must not overlap (as for all entry points).
+ * Results are bitwise reproducible and a tree's do not depend on the batch.
+ * ------------------------------------------------------------------------- */
+
+/* Bytes of workspace of augtree_linear_fwd (backward = 0) or
+ * augtree_linear_bwd (backward != 0). 0 on invalid arguments. */
+size_t augtree_linear_workspace_size(const augtree_groups* grp, int backward);
+
+/*
+ * Forward. In:  q_p [T_P,Hq,d], k_p, v_p [T_P,Hkv,d], q_r [T_R,Hq,d], k_r, v_r
+ *      [T_R,Hkv,d] bf16; state [num_groups,Hkv,d,d] fp32: what each prompt begins
+ *      from (nullable: zero).
+ * Out: o_p [T_P,Hq,d], o_r [T_R,Hq,d] bf16; state_p [num_groups,Hkv,d,d], state_r
+ *      [num_branches,Hkv,d,d] fp32: the states after each prompt and each branch
+ *      (nullable), for augtree_linear_step or the next piece of a sequence.
+ * num_branches = 0 is a batch of plain sequences: cu_branch and cu_resp are not
+ * read and the response pointers may be NULL. softmax_scale is s.
+ */
+int augtree_linear_fwd(const augtree_groups* grp, const float* decay, const uint16_t* q_p,
+                       const uint16_t* k_p, const uint16_t* v_p, const uint16_t* q_r, const uint16_t* k_r,
+                       const uint16_t* v_r, const float* state, uint16_t* o_p, uint16_t* o_r, float* state_p,
+                       float* state_r, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Backward: gradients of the outputs' loss for q, k and v (none for `state`
+ * or through state_p / state_r). In: as forward, do_p, do_r bf16 like o_p, o_r;
+ * the outputs are not read. Out: dq like q, dk, dv like k, bf16.
+ */
+int augtree_linear_bwd(const augtree_groups* grp, const float* decay, const uint16_t* q_p,
+                       const uint16_t* k_p, const uint16_t* v_p, const uint16_t* do_p, const uint16_t* q_r,
+                       const uint16_t* k_r, const uint16_t* v_r, const uint16_t* do_r, const float* state,
+                       uint16_t* dq_p, uint16_t* dk_p, uint16_t* dv_p, uint16_t* dq_r, uint16_t* dk_r,
+                       uint16_t* dv_r, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * One token of each of `rows` sequences:
+ *   state_out[r] = decay state_in[src[r]] + k_r v_r^T,  o_r = scale q_r state_out[r].
+ * In:  q [rows,Hq,d], k, v [rows,Hkv,d] bf16, state_in [n_states,Hkv,d,d] fp32,
+ *      src [rows] DEVICE int32 or NULL (src[r] = r). Several rows may read one
+ *      state (the branches of a prompt); a src outside [0, n_states) begins from a
+ *      zero state. decay: HOST array [Hkv].
+ * Out: state_out [rows,Hkv,d,d] fp32, o [rows,Hq,d] bf16.
+ * state_out may be state_in without src (in place); any other overlap of the
+ * two is refused. No workspace.
+ */
+int augtree_linear_step(int32_t rows, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+                        float scale, const float* decay, const uint16_t* q, const uint16_t* k,
+                        const uint16_t* v, int32_t n_states, const float* state_in, const int32_t* src,
+                        float* state_out, uint16_t* o, void* stream);
+
+typedef enum augtree_activation { AUGTREE_ACT_NONE = 0, AUGTREE_ACT_SILU = 1 } augtree_activation;
+
+/*
+ * Norm of each head of each row, with an activation (a group norm over
+ * [rows, heads * head_dim], one group per head), as it follows linear
+ * attention: n = (x - mean) / sqrt(var + eps) over the head_dim channels (var
+ * with the divisor head_dim), a = n * weight + bias, and
+ *   y = act(a),  or with a gate  y = a * act(gate);  act(u) = u / (1 + exp(-u)) (SILU) or u (NONE).
+ * In:  x, gate (nullable) [rows,heads,head_dim] bf16; weight, bias (each
+ *      nullable: 1 and 0) [heads,head_dim] fp32. head_dim a multiple of 8, at most 1024.
+ * Out: y like x. rows = 0 is a no-op.
+ */
+int augtree_head_norm_fwd(int64_t rows, int32_t heads, int32_t head_dim, int activation, float eps,
+                          const uint16_t* x, const uint16_t* gate, const float* weight, const float* bias,
+                          uint16_t* y, void* stream);
+
+/*
+ * Its backward. In: as forward, dy like y. Out: dx, dgate (with a gate) bf16;
+ * dweight, dbias [heads,head_dim] fp32 (each nullable), summed over the rows in a
+ * fixed order. The workspace (augtree_head_norm_workspace_size bytes) is needed
+ * for dweight or dbias only. rows = 0 writes zeros to them.
+ */
+int augtree_head_norm_bwd(int64_t rows, int32_t heads, int32_t head_dim, int activation, float eps,
+                          const uint16_t* x, const uint16_t* gate, const float* weight, const float* bias,
+                          const uint16_t* dy, uint16_t* dx, uint16_t* dgate, float* dweight, float* dbias,
+                          void* ws, size_t ws_bytes, void* stream);
+size_t augtree_head_norm_workspace_size(int64_t rows, int32_t heads, int32_t head_dim);
+
 /*
  * Launch hook (instrumentation; not part of the method). When set, `hook` is
  * called on the calling thread immediately before (phase 0) and after
  * (phase 1) every kernel launch the library enqueues from that thread, with a
  * static role name ("fwd_prefill", "fwd_replay", "fwd_tree", "fwd_replay_split",
  * "lse_merge", "dq_prefill", "dkv_prefill", "dq_replay", "dkv_replay", "dq_tree",
- * "dkv_tree", "grad_reduce", "reduce_tree") and the stream the
- * kernel is enqueued on, so that a caller can record HIP events around single
+ * "dkv_tree", "grad_reduce", "reduce_tree", "linear_table", "linear_state",
+ * "linear_state_rev", "linear_scan", "linear_scan_rev", "linear_out", "linear_dq",
+ * "linear_dv", "linear_dk", "linear_step", "head_norm", "head_norm_bwd") and the
+ * stream the kernel is enqueued on, so that a caller can record HIP events around single
  * kernels. The hook must not call back into the library. NULL removes it.
  * Per thread; the library keeps no other state.
  */

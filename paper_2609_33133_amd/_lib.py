@@ -32,12 +32,17 @@ OP_REPLAY_BWD = 3
 OP_TREE_FWD = 4
 OP_TREE_BWD = 5
 
+ACT_NONE = 0
+ACT_SILU = 1
+
 EXPORTS = (
     "augtree_workspace_size", "augtree_prefill_fwd", "augtree_replay_fwd", "augtree_lse_merge",
     "augtree_replay_bwd", "augtree_prefill_bwd", "augtree_prompt_grad_reduce", "augtree_status_string",
     "augtree_last_error", "augtree_check_device", "augtree_version", "augtree_set_launch_hook",
     "augtree_replay_split_groups", "augtree_tree_fwd", "augtree_tree_bwd", "augtree_tree_bwd_noalloc",
     "augtree_noalloc_scratch_bytes", "augtree_set_tree_chunk_blocks", "augtree_tree_chunk_blocks",
+    "augtree_linear_workspace_size", "augtree_linear_fwd", "augtree_linear_bwd", "augtree_linear_step",
+    "augtree_head_norm_fwd", "augtree_head_norm_bwd", "augtree_head_norm_workspace_size",
 )
 
 LAUNCH_HOOK = ctypes.CFUNCTYPE(None, ctypes.c_char_p, ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p)
@@ -69,6 +74,7 @@ _lib = None
 _P = ctypes.c_void_p
 _I32 = ctypes.c_int32
 _I64 = ctypes.c_int64
+_F32 = ctypes.c_float
 _SZ = ctypes.c_size_t
 _GP = ctypes.POINTER(Groups)
 
@@ -94,6 +100,13 @@ def _sig(lib):
         "augtree_noalloc_scratch_bytes": (_SZ, []),
         "augtree_set_tree_chunk_blocks": (ctypes.c_int, [_I32]),
         "augtree_tree_chunk_blocks": (_I32, []),
+        "augtree_linear_workspace_size": (_SZ, [_GP, ctypes.c_int]),
+        "augtree_linear_fwd": (ctypes.c_int, [_GP] + [_P] * 12 + [_P, _SZ, _P]),
+        "augtree_linear_bwd": (ctypes.c_int, [_GP] + [_P] * 16 + [_P, _SZ, _P]),
+        "augtree_linear_step": (ctypes.c_int, [_I32, _I32, _I32, _I32, _F32, _P, _P, _P, _P, _I32] + [_P] * 5),
+        "augtree_head_norm_fwd": (ctypes.c_int, [_I64, _I32, _I32, ctypes.c_int, _F32] + [_P] * 6),
+        "augtree_head_norm_bwd": (ctypes.c_int, [_I64, _I32, _I32, ctypes.c_int, _F32] + [_P] * 9 + [_P, _SZ, _P]),
+        "augtree_head_norm_workspace_size": (_SZ, [_I64, _I32, _I32]),
     }
     for name, (res, args) in sigs.items():
         fn = getattr(lib, name)

@@ -17,7 +17,7 @@ import torch
 
 from . import _lib
 from ._lib import (REPLAY_FUSED, REPLAY_SPLIT, REPLAY_AUTO, OP_PREFILL_FWD, OP_REPLAY_FWD,  # noqa: F401
-                   OP_PREFILL_BWD, OP_REPLAY_BWD, OP_TREE_FWD, OP_TREE_BWD)
+                   OP_PREFILL_BWD, OP_REPLAY_BWD, OP_TREE_FWD, OP_TREE_BWD, ACT_NONE, ACT_SILU)
 
 
 def _ptr(t: Optional[torch.Tensor]):
@@ -294,3 +294,207 @@ def tree_bwd(b: GroupBatch, q_p, k_p, v_p, o_p, lse_p, do_p, q_r, k_r, v_r, o_r,
                                             _ptr(dq_r), _ptr(dk_r), _ptr(dv_r), _ptr(ws), nws, _stream(stream)),
                "tree_bwd")
     return dq_p, dk_p, dv_p, dq_r, dk_r, dv_r, dkv_p_f32
+
+
+# ---------------------------------------------------------------------------- linear attention layer
+
+class _On:
+    """The device of a call's tensors made current, with the stream it runs on there. Every tensor has to be on that
+    device (a stream given by the caller too)."""
+
+    def __init__(self, tensors, stream=None):
+        dev = None
+        for name, t in tensors:
+            if t is None:
+                continue
+            if t.device.type != "cuda":
+                raise ValueError(f"{name} must be a GPU tensor (the op has no CPU path)")
+            if dev is None:
+                dev = t.device
+            elif t.device != dev:
+                raise ValueError(f"{name} is on {t.device}, other tensors on {dev}")
+        if stream is not None and stream.device != dev:
+            raise ValueError(f"the stream is on {stream.device}, the tensors on {dev}")
+        self.device, self.stream, self.guard = dev, stream, torch.cuda.device(dev)
+
+    def __enter__(self):
+        self.guard.__enter__()
+        s = self.stream if self.stream is not None else torch.cuda.current_stream()
+        return ctypes.c_void_p(s.cuda_stream)
+
+    def __exit__(self, *exc):
+        self.guard.__exit__(*exc)
+
+
+def _decay(decay, heads: int) -> np.ndarray:
+    """Host array [heads] of fp32 decays (a sequence, a numpy array or a CPU tensor; one number for all heads)."""
+    if isinstance(decay, torch.Tensor):
+        if decay.device.type != "cpu":
+            raise ValueError("decay must be on the host")
+        if decay.requires_grad:
+            raise ValueError("decay is a constant of the layer: no gradient is formed for it")
+        decay = decay.numpy()
+    a = np.asarray(decay, dtype=np.float32)
+    a = np.ascontiguousarray(np.broadcast_to(a, (heads,)) if a.ndim == 0 else a)
+    if a.shape != (heads,):
+        raise ValueError(f"decay: shape {a.shape}, expected {(heads,)}")
+    return a
+
+
+def _out(t, name, dtype, shape, device):
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    _need(t, name, dtype, shape)
+    return t
+
+
+def linear_workspace_size(b: GroupBatch, backward: bool = False) -> int:
+    lib = _lib.load()
+    n = lib.augtree_linear_workspace_size(b.ref, int(backward))
+    if n == 0:
+        raise _lib.AugtreeError(_lib.AUGTREE_ERR_INVALID_ARGUMENT, "linear_workspace_size",
+                                lib.augtree_last_error().decode())
+    return int(n)
+
+
+def _linear_ws(b, backward, ws, device):
+    if ws is None:
+        ws = torch.empty(linear_workspace_size(b, backward), dtype=torch.uint8, device=device)
+    return ws
+
+
+def _linear_inputs(b: GroupBatch, named):
+    for n, t in named:
+        rows = b.tp if n.endswith("_p") else b.tr
+        _need(t, n, torch.bfloat16, (rows, b.hkv if n[0] in "kv" else b.hq, b.d))
+
+
+def linear_fwd(b: GroupBatch, decay, q_p, k_p, v_p, q_r, k_r, v_r, state=None, o_p=None, o_r=None, state_p=None,
+               state_r=None, want_states: bool = False, ws=None, stream=None):
+    """Linear attention of every tree (augtree_linear_fwd). `decay`: host values, one per KV head. A batch without
+    branches (cu_branch all 0, cu_resp [0]) takes response tensors of no rows. Returns (o_p, o_r, state_p, state_r);
+    the states are None unless asked for."""
+    dec = _decay(decay, b.hkv)
+    named = (("q_p", q_p), ("k_p", k_p), ("v_p", v_p), ("q_r", q_r), ("k_r", k_r), ("v_r", v_r))
+    on = _On(named + (("state", state), ("o_p", o_p), ("o_r", o_r), ("state_p", state_p), ("state_r", state_r),
+                      ("ws", ws)), stream)
+    _linear_inputs(b, named)
+    dev, f32 = on.device, torch.float32
+    if state is not None:
+        _need(state, "state", f32, (b.num_groups, b.hkv, b.d, b.d))
+    with on as st:
+        o_p = _out(o_p, "o_p", torch.bfloat16, q_p.shape, dev)
+        o_r = _out(o_r, "o_r", torch.bfloat16, q_r.shape, dev)
+        if want_states or state_p is not None:
+            state_p = _out(state_p, "state_p", f32, (b.num_groups, b.hkv, b.d, b.d), dev)
+        if want_states or state_r is not None:
+            state_r = _out(state_r, "state_r", f32, (b.num_branches, b.hkv, b.d, b.d), dev)
+        ws = _linear_ws(b, False, ws, dev)
+        _lib.check(_lib.load().augtree_linear_fwd(
+            b.ref, dec.ctypes.data_as(ctypes.c_void_p), _ptr(q_p), _ptr(k_p), _ptr(v_p), _ptr(q_r), _ptr(k_r),
+            _ptr(v_r), _ptr(state), _ptr(o_p), _ptr(o_r), _ptr(state_p), _ptr(state_r) if b.num_branches else None,
+            _ptr(ws), ctypes.c_size_t(ws.numel()), st), "linear_fwd")
+    return o_p, o_r, state_p, state_r
+
+
+def linear_bwd(b: GroupBatch, decay, q_p, k_p, v_p, do_p, q_r, k_r, v_r, do_r, state=None, dq_p=None, dk_p=None,
+               dv_p=None, dq_r=None, dk_r=None, dv_r=None, ws=None, stream=None):
+    """Gradients of linear_fwd's outputs (augtree_linear_bwd). Returns (dq_p, dk_p, dv_p, dq_r, dk_r, dv_r)."""
+    dec = _decay(decay, b.hkv)
+    named = (("q_p", q_p), ("k_p", k_p), ("v_p", v_p), ("do_p", do_p), ("q_r", q_r), ("k_r", k_r), ("v_r", v_r),
+             ("do_r", do_r))
+    on = _On(named + (("state", state), ("dq_p", dq_p), ("dk_p", dk_p), ("dv_p", dv_p), ("dq_r", dq_r),
+                      ("dk_r", dk_r), ("dv_r", dv_r), ("ws", ws)), stream)
+    _linear_inputs(b, named)
+    dev = on.device
+    if state is not None:
+        _need(state, "state", torch.float32, (b.num_groups, b.hkv, b.d, b.d))
+    with on as st:
+        outs = [_out(t, n, torch.bfloat16, like.shape, dev)
+                for t, n, like in ((dq_p, "dq_p", q_p), (dk_p, "dk_p", k_p), (dv_p, "dv_p", v_p),
+                                   (dq_r, "dq_r", q_r), (dk_r, "dk_r", k_r), (dv_r, "dv_r", v_r))]
+        ws = _linear_ws(b, True, ws, dev)
+        _lib.check(_lib.load().augtree_linear_bwd(
+            b.ref, dec.ctypes.data_as(ctypes.c_void_p), _ptr(q_p), _ptr(k_p), _ptr(v_p), _ptr(do_p), _ptr(q_r),
+            _ptr(k_r), _ptr(v_r), _ptr(do_r), _ptr(state), *(_ptr(t) for t in outs), _ptr(ws),
+            ctypes.c_size_t(ws.numel()), st), "linear_bwd")
+    return tuple(outs)
+
+
+def linear_step(q, k, v, decay, state, src=None, state_out=None, o=None, scale: Optional[float] = None, stream=None):
+    """One token of linear attention for every row (augtree_linear_step): q [rows, Hq, d], k, v [rows, Hkv, d] bf16,
+    state [n, Hkv, d, d] fp32. `src` [rows] int32 on the GPU names the state each row goes on from (the branches of a
+    prompt share one; outside [0, n): from zero). Writes the new states to `state_out` (a new tensor if None; `state`
+    itself only without src) and returns (o, state_out)."""
+    on = _On((("q", q), ("k", k), ("v", v), ("state", state), ("src", src), ("state_out", state_out), ("o", o)), stream)
+    if q.dim() != 3 or k.dim() != 3:
+        raise ValueError("q and k must be [rows, heads, head_dim]")
+    rows, hq, d = q.shape
+    hkv, n = k.shape[1], state.shape[0]
+    _need(q, "q", torch.bfloat16, (rows, hq, d))
+    _need(k, "k", torch.bfloat16, (rows, hkv, d))
+    _need(v, "v", torch.bfloat16, (rows, hkv, d))
+    _need(state, "state", torch.float32, (n, hkv, d, d))
+    if src is not None:
+        _need(src, "src", torch.int32, (rows,))
+    dec = _decay(decay, hkv)
+    with on as st:
+        state_out = _out(state_out, "state_out", torch.float32, (rows, hkv, d, d), on.device)
+        o = _out(o, "o", torch.bfloat16, q.shape, on.device)
+        _lib.check(_lib.load().augtree_linear_step(
+            rows, hq, hkv, d, 1.0 / math.sqrt(d) if scale is None else float(scale),
+            dec.ctypes.data_as(ctypes.c_void_p), _ptr(q), _ptr(k), _ptr(v), n, _ptr(state), _ptr(src),
+            _ptr(state_out), _ptr(o), st), "linear_step")
+    return o, state_out
+
+
+def _norm_inputs(x, gate, weight, bias):
+    if x.dim() != 3:
+        raise ValueError("x must be [rows, heads, head_dim]")
+    _need(x, "x", torch.bfloat16, x.shape)
+    if gate is not None:
+        _need(gate, "gate", torch.bfloat16, x.shape)
+    for n, t in (("weight", weight), ("bias", bias)):
+        if t is not None:
+            _need(t, n, torch.float32, x.shape[1:])
+
+
+def head_norm_fwd(x, weight=None, bias=None, gate=None, activation: int = ACT_NONE, eps: float = 1e-5, y=None,
+                  stream=None):
+    """Norm over each head with an activation or a gate (augtree_head_norm_fwd)."""
+    on = _On((("x", x), ("weight", weight), ("bias", bias), ("gate", gate), ("y", y)), stream)
+    _norm_inputs(x, gate, weight, bias)
+    rows, heads, d = x.shape
+    with on as st:
+        y = _out(y, "y", torch.bfloat16, x.shape, on.device)
+        _lib.check(_lib.load().augtree_head_norm_fwd(rows, heads, d, int(activation), float(eps), _ptr(x), _ptr(gate),
+                                                     _ptr(weight), _ptr(bias), _ptr(y), st), "head_norm_fwd")
+    return y
+
+
+def head_norm_bwd(x, dy, weight=None, bias=None, gate=None, activation: int = ACT_NONE, eps: float = 1e-5, dx=None,
+                  dgate=None, dweight=None, dbias=None, want_dweight: bool = False, want_dbias: bool = False, ws=None,
+                  stream=None):
+    """Its gradients (augtree_head_norm_bwd). Returns (dx, dgate, dweight, dbias); dgate is None without a gate, the
+    last two unless asked for."""
+    on = _On((("x", x), ("dy", dy), ("weight", weight), ("bias", bias), ("gate", gate), ("dx", dx), ("dgate", dgate),
+              ("dweight", dweight), ("dbias", dbias), ("ws", ws)), stream)
+    _norm_inputs(x, gate, weight, bias)
+    _need(dy, "dy", torch.bfloat16, x.shape)
+    rows, heads, d = x.shape
+    dev, f32, lib = on.device, torch.float32, _lib.load()
+    with on as st:
+        dx = _out(dx, "dx", torch.bfloat16, x.shape, dev)
+        if gate is not None:
+            dgate = _out(dgate, "dgate", torch.bfloat16, x.shape, dev)
+        if want_dweight or dweight is not None:
+            dweight = _out(dweight, "dweight", f32, (heads, d), dev)
+        if want_dbias or dbias is not None:
+            dbias = _out(dbias, "dbias", f32, (heads, d), dev)
+        if ws is None and (dweight is not None or dbias is not None):
+            ws = torch.empty(int(lib.augtree_head_norm_workspace_size(rows, heads, d)), dtype=torch.uint8, device=dev)
+        _lib.check(lib.augtree_head_norm_bwd(rows, heads, d, int(activation), float(eps), _ptr(x), _ptr(gate),
+                                             _ptr(weight), _ptr(bias), _ptr(dy), _ptr(dx), _ptr(dgate), _ptr(dweight),
+                                             _ptr(dbias), _ptr(ws), ctypes.c_size_t(0 if ws is None else ws.numel()),
+                                             st), "head_norm_bwd")
+    return dx, dgate, dweight, dbias

@@ -11,10 +11,21 @@ gradient of every branch plus the prompt queries' own contribution summed on
 the prompt KV in a fixed order, Eq. 2). Every step runs in the library's
 kernels on the current stream; autograd only routes tensors. There is no CPU
 path.
+
+The layers of a model that keep a decayed state instead of a KV cache take the
+same batches:
+
+    o_p, o_r = group_linear_attention(q_p, k_p, v_p, q_r, k_r, v_r, batch, decay)
+    y = head_norm(o_r, weight, bias, gate=gate, activation="silu")
+
+The first computes a prompt's state once and goes on from it in every branch
+(augtree_linear_fwd/bwd); the second is the norm over each head that follows
+such a layer (augtree_head_norm_fwd/bwd). At decode, api.linear_step takes one
+token of every sequence at a time.
 """
 from __future__ import annotations
 
-from typing import Tuple
+from typing import Optional, Tuple
 
 import torch
 
@@ -62,3 +73,78 @@ def group_attention(q_p: torch.Tensor, k_p: torch.Tensor, v_p: torch.Tensor, q_r
                     mode: int = REPLAY_FUSED) -> Tuple[torch.Tensor, torch.Tensor]:
     """(O_P, O_R) of shared-prompt group attention; differentiable in all six inputs."""
     return _GroupAttention.apply(q_p, k_p, v_p, q_r, k_r, v_r, batch, int(mode))
+
+
+class _GroupLinearAttention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q_p, k_p, v_p, q_r, k_r, v_r, batch: GroupBatch, decay, state, return_state: bool):
+        b = batch
+        for t, n, rows, h in ((q_p, "q_p", b.tp, b.hq), (k_p, "k_p", b.tp, b.hkv), (v_p, "v_p", b.tp, b.hkv),
+                              (q_r, "q_r", b.tr, b.hq), (k_r, "k_r", b.tr, b.hkv), (v_r, "v_r", b.tr, b.hkv)):
+            _check(t, n, rows, h, b.d)
+        q_p, k_p, v_p, q_r, k_r, v_r = (t.contiguous() for t in (q_p, k_p, v_p, q_r, k_r, v_r))
+        o_p, o_r, state_p, state_r = api.linear_fwd(b, decay, q_p, k_p, v_p, q_r, k_r, v_r, state=state,
+                                                    want_states=return_state)
+        ctx.save_for_backward(q_p, k_p, v_p, q_r, k_r, v_r, state)
+        ctx.batch, ctx.decay = b, decay
+        if not return_state:
+            return o_p, o_r
+        ctx.mark_non_differentiable(state_p, state_r)
+        return o_p, o_r, state_p, state_r
+
+    @staticmethod
+    def backward(ctx, do_p, do_r, *_):
+        q_p, k_p, v_p, q_r, k_r, v_r, state = ctx.saved_tensors
+        # an output that did not reach the loss has a zero gradient
+        do_p = torch.zeros_like(q_p) if do_p is None else do_p.to(torch.bfloat16).contiguous()
+        do_r = torch.zeros_like(q_r) if do_r is None else do_r.to(torch.bfloat16).contiguous()
+        grads = api.linear_bwd(ctx.batch, ctx.decay, q_p, k_p, v_p, do_p, q_r, k_r, v_r, do_r, state=state)
+        return (*grads, None, None, None, None)
+
+
+def group_linear_attention(q_p: torch.Tensor, k_p: torch.Tensor, v_p: torch.Tensor, q_r: torch.Tensor,
+                           k_r: torch.Tensor, v_r: torch.Tensor, batch: GroupBatch, decay,
+                           state: Optional[torch.Tensor] = None, return_state: bool = False):
+    """(O_P, O_R) of linear attention over replay trees with a decay per KV head (host values in (0, 1]);
+    differentiable in the six tensors. `state` [num_groups, Hkv, d, d] fp32 is what the prompts begin from; with
+    `return_state` the states after every prompt and every branch follow the outputs (no gradient flows through
+    either)."""
+    if state is not None and state.requires_grad:
+        raise ValueError("state is a constant of the op: no gradient is formed for it")
+    decay = api._decay(decay, batch.hkv).copy()
+    return _GroupLinearAttention.apply(q_p, k_p, v_p, q_r, k_r, v_r, batch, decay, state, bool(return_state))
+
+
+ACTIVATIONS = {"none": api.ACT_NONE, "silu": api.ACT_SILU}
+
+
+class _HeadNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, gate, activation: int, eps: float):
+        x = x.contiguous()
+        gate = None if gate is None else gate.contiguous()
+        weight = None if weight is None else weight.contiguous()
+        bias = None if bias is None else bias.contiguous()
+        y = api.head_norm_fwd(x, weight, bias, gate, activation, eps)
+        ctx.save_for_backward(x, weight, bias, gate)
+        ctx.activation, ctx.eps = activation, eps
+        return y
+
+    @staticmethod
+    def backward(ctx, dy):
+        x, weight, bias, gate = ctx.saved_tensors
+        dx, dgate, dweight, dbias = api.head_norm_bwd(
+            x, dy.to(torch.bfloat16).contiguous(), weight, bias, gate, ctx.activation, ctx.eps,
+            want_dweight=weight is not None and ctx.needs_input_grad[1],
+            want_dbias=bias is not None and ctx.needs_input_grad[2])
+        return dx, dweight, dbias, dgate, None, None
+
+
+def head_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
+              gate: Optional[torch.Tensor] = None, activation: str = "none", eps: float = 1e-5) -> torch.Tensor:
+    """Norm over each head of packed rows [rows, heads, head_dim] (bf16), n = (x - mean) / sqrt(var + eps), then
+    a = n * weight + bias ([heads, head_dim] fp32, each optional) and y = act(a), or with a gate y = a * act(gate).
+    `activation`: "none" or "silu". Differentiable in every tensor."""
+    if activation not in ACTIVATIONS:
+        raise ValueError(f"activation {activation!r} not in {tuple(ACTIVATIONS)}")
+    return _HeadNorm.apply(x, weight, bias, gate, ACTIVATIONS[activation], float(eps))

@@ -1104,6 +1104,10 @@ namespace augtree {
 
 int fail_status(int status, const char* msg) { return fail(status, "%s", msg); }
 
+void launch_hook(const char* role, int phase, void* stream) {
+  if (g_hook) g_hook(role, phase, stream, g_hook_user);
+}
+
 int tree_chunk_count(int64_t nr, int group) {
   const int64_t blocks = (nr + kDkvBlockQ - 1) / kDkvBlockQ * group;
   const int64_t per = g_tree_chunk_blocks.load(std::memory_order_relaxed);

@@ -1,0 +1,499 @@
+// Host side of the linear-attention layer: argument validation, segment
+// tables, workspace layout and launches.
+//
+// The segment table travels in the kernel arguments; a batch of more than
+// kLinInlineSegs segments has it written into the workspace by small kernels
+// that carry it in theirs. So every call enqueues kernels only.
+#include "linear.h"
+
+#include <algorithm>
+#include <cmath>
+#include <cstdio>
+#include <cstring>
+#include <exception>
+#include <vector>
+
+#include "../../include/augtree.h"
+#include "internal.h"
+
+using namespace augtree;
+
+namespace {
+
+template <class... A>
+int fail(int status, const char* fmt, A... a) {
+  char buf[512];
+  std::snprintf(buf, sizeof(buf), fmt, a...);
+  return fail_status(status, buf);
+}
+
+int hip_ok(hipError_t e, const char* what) {
+  return e == hipSuccess ? AUGTREE_OK : fail(AUGTREE_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
+}
+
+// Calls the launch hook around one kernel launch.
+struct Hook {
+  const char* role;
+  hipStream_t stream;
+  Hook(const char* r, hipStream_t s) : role(r), stream(s) { launch_hook(role, 0, stream); }
+  ~Hook() { launch_hook(role, 1, stream); }
+};
+
+// No C++ exception crosses the ABI (the tables are vectors).
+template <class F>
+int guarded(F f) {
+  try {
+    return f();
+  } catch (const std::exception& e) {
+    return fail(AUGTREE_ERR_INVALID_ARGUMENT, "host allocation failed: %s", e.what());
+  }
+}
+
+int check_ptr(const void* p, const char* name, bool required, size_t align = 16) {
+  if (!p) return required ? fail(AUGTREE_ERR_INVALID_ARGUMENT, "null pointer: %s", name) : AUGTREE_OK;
+  if (reinterpret_cast<uintptr_t>(p) % align)
+    return fail(AUGTREE_ERR_MISALIGNED, "pointer %s is not %d-byte aligned", name, (int)align);
+  return AUGTREE_OK;
+}
+
+int check_heads(int hq, int hkv, int d, float scale, const float* decay) {
+  if (hq < 1 || hkv < 1) return fail(AUGTREE_ERR_INVALID_ARGUMENT, "head counts must be >= 1");
+  if (hq % hkv) return fail(AUGTREE_ERR_UNSUPPORTED, "num_q_heads %d not a multiple of num_kv_heads %d", hq, hkv);
+  if (hkv > kLinMaxHeads) return fail(AUGTREE_ERR_UNSUPPORTED, "num_kv_heads %d > %d", hkv, kLinMaxHeads);
+  if (d != 64 && d != 128) return fail(AUGTREE_ERR_UNSUPPORTED, "head_dim %d not in {64,128}", d);
+  if (!(scale > 0.f) || !std::isfinite(scale))
+    return fail(AUGTREE_ERR_INVALID_ARGUMENT, "softmax_scale must be finite and > 0");
+  if (!decay) return fail(AUGTREE_ERR_INVALID_ARGUMENT, "null pointer: decay");
+  for (int h = 0; h < hkv; ++h)
+    if (!(decay[h] > 0.f && decay[h] <= 1.f))
+      return fail(AUGTREE_ERR_INVALID_ARGUMENT, "decay[%d] = %g not in (0, 1]", h, (double)decay[h]);
+  return AUGTREE_OK;
+}
+
+int check_offsets(const int32_t* cu, int n, const char* name) {
+  if (!cu) return fail(AUGTREE_ERR_INVALID_ARGUMENT, "null offset array: %s", name);
+  if (cu[0] != 0) return fail(AUGTREE_ERR_INVALID_ARGUMENT, "%s must start at 0", name);
+  for (int i = 0; i < n; ++i)
+    if (cu[i + 1] <= cu[i])
+      return fail(AUGTREE_ERR_INVALID_ARGUMENT, "%s: length %d is not positive or offsets decrease", name, i);
+  return AUGTREE_OK;
+}
+
+// num_branches == 0: prompts only, cu_branch and cu_resp are not read
+int check_batch(const augtree_groups* g, const float* decay) {
+  if (!g) return fail(AUGTREE_ERR_INVALID_ARGUMENT, "null descriptor");
+  if (g->num_groups < 1 || g->num_branches < 0)
+    return fail(AUGTREE_ERR_INVALID_ARGUMENT, "num_groups=%d must be >= 1, num_branches=%d >= 0", g->num_groups,
+                g->num_branches);
+  int st = check_offsets(g->cu_prompt, g->num_groups, "cu_prompt");
+  if (!st && g->num_branches > 0) {
+    st = check_offsets(g->cu_branch, g->num_groups, "cu_branch");
+    if (!st && g->cu_branch[g->num_groups] != g->num_branches)
+      return fail(AUGTREE_ERR_INVALID_ARGUMENT, "cu_branch[num_groups]=%d != num_branches=%d",
+                  g->cu_branch[g->num_groups], g->num_branches);
+    if (!st) st = check_offsets(g->cu_resp, g->num_branches, "cu_resp");
+  }
+  return st ? st : check_heads(g->num_q_heads, g->num_kv_heads, g->head_dim, g->softmax_scale, decay);
+}
+
+// Rows of a block. A block is one workgroup a KV head in the state and output
+// kernels, and costs its state's way through the workspace: written, read and
+// written by the scan, read (16 d^2 bytes a KV head). Cuts follow from a tree's
+// own size, so that its results do not depend on the batch: enough blocks for
+// two workgroups on every CU from the tree alone, and never fewer than 128 rows
+// (two chunks) or more than 1024 (the state's traffic is below a tenth then).
+int block_rows(int64_t tokens, int hkv) {
+  int rows = 128;
+  while (rows < 1024 && tokens * hkv > (int64_t)512 * rows) rows *= 2;
+  return rows;
+}
+
+struct Layout {
+  std::vector<LinSeg> segs;
+  int64_t blocks = 0;
+  size_t states = 0, tree = 0;  // bytes: states of all blocks; one state per tree
+};
+
+size_t align_up(size_t n) { return (n + 255) / 256 * 256; }
+
+int make_layout(const augtree_groups* g, Layout* L) {
+  const int ng = g->num_groups, nb = g->num_branches;
+  L->segs.resize((size_t)ng + nb);
+  int64_t blocks = 0;
+  auto add = [&](int i, int row0, int len, int link, int rows) {
+    LinSeg& s = L->segs[i];
+    s.row0 = row0;
+    s.len = len;
+    s.link = link;
+    s.rows = rows;
+    s.block0 = (int32_t)std::min<int64_t>(blocks, INT32_MAX);
+    blocks += (len + (int64_t)rows - 1) / rows;
+  };
+  std::vector<int> rows(ng);
+  for (int t = 0; t < ng; ++t) {
+    int64_t tokens = g->cu_prompt[t + 1] - g->cu_prompt[t];
+    if (nb) tokens += g->cu_resp[g->cu_branch[t + 1]] - g->cu_resp[g->cu_branch[t]];
+    rows[t] = block_rows(tokens, g->num_kv_heads);
+    add(t, g->cu_prompt[t], g->cu_prompt[t + 1] - g->cu_prompt[t], nb ? g->cu_branch[t] : 0, rows[t]);
+  }
+  for (int t = 0; nb && t < ng; ++t)
+    for (int b = g->cu_branch[t]; b < g->cu_branch[t + 1]; ++b)
+      add(ng + b, g->cu_resp[b], g->cu_resp[b + 1] - g->cu_resp[b], t, rows[t]);
+  const int64_t slices = (int64_t)g->head_dim * g->head_dim / 1024;
+  if (blocks * g->num_kv_heads > INT32_MAX || (ng + (int64_t)nb) * g->num_kv_heads * slices > INT32_MAX)
+    return fail(AUGTREE_ERR_UNSUPPORTED, "%lld blocks of %d KV heads exceed a launch", (long long)blocks,
+                g->num_kv_heads);
+  L->blocks = blocks;
+  const size_t state = (size_t)g->num_kv_heads * g->head_dim * g->head_dim * sizeof(float);
+  L->states = align_up(state * (size_t)blocks);
+  L->tree = state;
+  return AUGTREE_OK;
+}
+
+size_t workspace_bytes(const augtree_groups* g, const Layout& L, bool backward) {
+  size_t n = align_up(L.segs.size() * sizeof(LinSeg)) + L.states + align_up(L.tree * g->num_groups);
+  if (backward) n += L.states + align_up(L.tree * (size_t)std::max(1, g->num_branches));
+  return n;
+}
+
+// A call: the batch in kernel form, the workspace handed out piece by piece.
+struct Call {
+  const augtree_groups* g;
+  Layout L;
+  LinBatch b;
+  char* ws;
+  hipStream_t stream;
+
+  template <class T>
+  T* take(size_t bytes) {
+    T* p = reinterpret_cast<T*>(ws);
+    ws += align_up(bytes);
+    return p;
+  }
+
+  // after validation: segment table, inline or through the workspace
+  int begin(const float* decay) {
+    std::memset(&b, 0, sizeof(b));
+    const size_t n = L.segs.size();
+    b.num_trees = g->num_groups;
+    b.num_branches = g->num_branches;
+    b.num_blocks = (int32_t)L.blocks;
+    b.heads_kv = g->num_kv_heads;
+    b.group = g->num_q_heads / g->num_kv_heads;
+    for (int h = 0; h < b.heads_kv; ++h) b.log2_decay[h] = (float)std::log2((double)decay[h]);
+    LinSeg* table = take<LinSeg>(n * sizeof(LinSeg));
+    if (n <= (size_t)kLinInlineSegs) {
+      std::copy(L.segs.begin(), L.segs.end(), b.inl);
+      return AUGTREE_OK;
+    }
+    b.segs = table;
+    const size_t words = n * (sizeof(LinSeg) / 4);
+    const int32_t* src = reinterpret_cast<const int32_t*>(L.segs.data());
+    for (size_t at = 0; at < words; at += kLinTableWords) {
+      LinTable t;
+      t.dst = reinterpret_cast<int32_t*>(table) + at;
+      t.n = (int32_t)std::min<size_t>(kLinTableWords, words - at);
+      std::memcpy(t.words, src + at, (size_t)t.n * 4);
+      Hook h("linear_table", stream);
+      if (int st = hip_ok(launch_lin_table(t, stream), "segment table launch")) return st;
+    }
+    return AUGTREE_OK;
+  }
+
+  // states[block] <- what reaches the block. exact: as fp32 sums would have it; the forward's states always are, so that
+  // its outputs do not depend on whether they are handed out.
+  int states(bool reverse, const uint16_t* const y[2], const uint16_t* const z[2], const float* init, float* states,
+             float* tree, float* out_p, float* out_r, bool exact) {
+    const bool branches = g->num_branches > 0;
+    LinStateParams s;
+    std::memset(&s, 0, sizeof(s));
+    for (int i = 0; i < 2; ++i) s.y[i] = y[i], s.z[i] = z[i];
+    s.heads_y = reverse ? g->num_q_heads : g->num_kv_heads;
+    s.states = states;
+    // nobody reads a prompt's own end without branches (a start in reverse), nor a branch's unless it is handed out
+    s.skip_prompt = reverse || (!branches && !out_p);
+    s.skip_branch = !reverse && !out_r;
+    s.b = b;
+    {
+      Hook h(reverse ? "linear_state_rev" : "linear_state", stream);
+      if (int st = hip_ok(launch_lin_state(s, g->head_dim, reverse, exact, stream), "state launch")) return st;
+    }
+    LinScanParams c;
+    std::memset(&c, 0, sizeof(c));
+    c.states = states;
+    c.init = init;
+    c.tree = tree;
+    c.out_p = out_p;
+    c.out_r = out_r;
+    c.skip_prompt = s.skip_prompt;
+    c.skip_branch = s.skip_branch;
+    c.b = b;
+    for (int k = 0; k < 2; ++k) {
+      const bool prompts = reverse ? k == 1 : k == 0;
+      if (!prompts && !branches) continue;
+      Hook h(reverse ? "linear_scan_rev" : "linear_scan", stream);
+      if (int st = hip_ok(launch_lin_scan(c, g->head_dim, reverse, prompts, stream), "scan launch")) return st;
+    }
+    return AUGTREE_OK;
+  }
+
+  int out(const char* role, bool reverse, bool transposed, const uint16_t* const x[2], const uint16_t* const y[2],
+          const uint16_t* const z[2], uint16_t* const o[2], const float* states) {
+    LinOutParams p;
+    std::memset(&p, 0, sizeof(p));
+    for (int i = 0; i < 2; ++i) p.x[i] = x[i], p.y[i] = y[i], p.z[i] = z[i], p.out[i] = o[i];
+    p.states = states;
+    p.scale = g->softmax_scale;
+    p.b = b;
+    Hook h(role, stream);
+    return hip_ok(launch_lin_out(p, g->head_dim, reverse, transposed, stream), role);
+  }
+};
+
+int check_ws(const void* ws, size_t have, size_t need) {
+  if (!ws || have < need)
+    return fail(AUGTREE_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed", ws ? have : (size_t)0, need);
+  return check_ptr(ws, "ws", true, 256);
+}
+
+struct Named {
+  const void* p;
+  const char* name;
+};
+
+int check_all(const Named* v, int n, bool required) {
+  for (int i = 0; i < n; ++i)
+    if (int st = check_ptr(v[i].p, v[i].name, required)) return st;
+  return AUGTREE_OK;
+}
+
+bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return x < y + nb && y < x + na;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t augtree_linear_workspace_size(const augtree_groups* grp, int backward) {
+  size_t n = 0;
+  guarded([&]() -> int {
+    static const std::vector<float> ones(kLinMaxHeads, 1.f);
+    if (int st = check_batch(grp, ones.data())) return st;
+    Layout L;
+    if (int st = make_layout(grp, &L)) return st;
+    n = workspace_bytes(grp, L, backward != 0);
+    return fail_status(AUGTREE_OK, "");
+  });
+  return n;
+}
+
+int augtree_linear_fwd(const augtree_groups* grp, const float* decay, const uint16_t* q_p, const uint16_t* k_p,
+                       const uint16_t* v_p, const uint16_t* q_r, const uint16_t* k_r, const uint16_t* v_r,
+                       const float* state, uint16_t* o_p, uint16_t* o_r, float* state_p, float* state_r, void* ws,
+                       size_t ws_bytes, void* stream) {
+  return guarded([&]() -> int {
+    int st = check_batch(grp, decay);
+    if (st) return st;
+    const bool br = grp->num_branches > 0;
+    const Named prompt[] = {{q_p, "q_p"}, {k_p, "k_p"}, {v_p, "v_p"}, {o_p, "o_p"}};
+    const Named resp[] = {{q_r, "q_r"}, {k_r, "k_r"}, {v_r, "v_r"}, {o_r, "o_r"}};
+    const Named opt[] = {{state, "state"}, {state_p, "state_p"}, {state_r, "state_r"}};
+    if ((st = check_all(prompt, 4, true)) || (br && (st = check_all(resp, 4, true))) || (st = check_all(opt, 3, false)))
+      return st;
+    if (!br && state_r) return fail(AUGTREE_ERR_INVALID_ARGUMENT, "state_r without branches");
+    Call c;
+    c.g = grp;
+    if ((st = make_layout(grp, &c.L)) || (st = check_ws(ws, ws_bytes, workspace_bytes(grp, c.L, false))) ||
+        (st = augtree_check_device()))
+      return st;
+    c.ws = static_cast<char*>(ws);
+    c.stream = static_cast<hipStream_t>(stream);
+    if ((st = c.begin(decay))) return st;
+    float* const states = c.take<float>(c.L.states);
+    float* const tree = c.take<float>(c.L.tree * grp->num_groups);
+    const uint16_t *const q[2] = {q_p, q_r}, *const k[2] = {k_p, k_r}, *const v[2] = {v_p, v_r};
+    uint16_t* const o[2] = {o_p, o_r};
+    if ((st = c.states(false, k, v, state, states, tree, state_p, state_r, true)) ||
+        (st = c.out("linear_out", false, false, q, k, v, o, states)))
+      return st;
+    return fail_status(AUGTREE_OK, "");
+  });
+}
+
+int augtree_linear_bwd(const augtree_groups* grp, const float* decay, const uint16_t* q_p, const uint16_t* k_p,
+                       const uint16_t* v_p, const uint16_t* do_p, const uint16_t* q_r, const uint16_t* k_r,
+                       const uint16_t* v_r, const uint16_t* do_r, const float* state, uint16_t* dq_p, uint16_t* dk_p,
+                       uint16_t* dv_p, uint16_t* dq_r, uint16_t* dk_r, uint16_t* dv_r, void* ws, size_t ws_bytes,
+                       void* stream) {
+  return guarded([&]() -> int {
+    int st = check_batch(grp, decay);
+    if (st) return st;
+    const bool br = grp->num_branches > 0;
+    const Named prompt[] = {{q_p, "q_p"}, {k_p, "k_p"}, {v_p, "v_p"}, {do_p, "do_p"}, {dq_p, "dq_p"}, {dk_p, "dk_p"},
+                            {dv_p, "dv_p"}};
+    const Named resp[] = {{q_r, "q_r"}, {k_r, "k_r"}, {v_r, "v_r"}, {do_r, "do_r"}, {dq_r, "dq_r"}, {dk_r, "dk_r"},
+                          {dv_r, "dv_r"}};
+    if ((st = check_all(prompt, 7, true)) || (br && (st = check_all(resp, 7, true))) ||
+        (st = check_ptr(state, "state", false)))
+      return st;
+    Call c;
+    c.g = grp;
+    if ((st = make_layout(grp, &c.L)) || (st = check_ws(ws, ws_bytes, workspace_bytes(grp, c.L, true))) ||
+        (st = augtree_check_device()))
+      return st;
+    c.ws = static_cast<char*>(ws);
+    c.stream = static_cast<hipStream_t>(stream);
+    if ((st = c.begin(decay))) return st;
+    float* const fwd = c.take<float>(c.L.states);
+    float* const tree = c.take<float>(c.L.tree * grp->num_groups);
+    float* const rev = c.take<float>(c.L.states);
+    float* const ends = c.take<float>(c.L.tree * std::max(1, grp->num_branches));
+    const uint16_t *const q[2] = {q_p, q_r}, *const k[2] = {k_p, k_r}, *const v[2] = {v_p, v_r},
+                   *const g[2] = {do_p, do_r};
+    uint16_t *const dq[2] = {dq_p, dq_r}, *const dk[2] = {dk_p, dk_r}, *const dv[2] = {dv_p, dv_r};
+    if ((st = c.states(false, k, v, state, fwd, tree, nullptr, nullptr, false)) ||
+        (st = c.out("linear_dq", false, true, g, v, k, dq, fwd)) ||
+        (st = c.states(true, q, g, nullptr, rev, ends, nullptr, nullptr, false)) ||
+        (st = c.out("linear_dv", true, false, k, q, g, dv, rev)) ||
+        (st = c.out("linear_dk", true, true, v, g, q, dk, rev)))
+      return st;
+    return fail_status(AUGTREE_OK, "");
+  });
+}
+
+int augtree_linear_step(int32_t rows, int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, float scale,
+                        const float* decay, const uint16_t* q, const uint16_t* k, const uint16_t* v, int32_t n_states,
+                        const float* state_in, const int32_t* src, float* state_out, uint16_t* o, void* stream) {
+  int st = check_heads(num_q_heads, num_kv_heads, head_dim, scale, decay);
+  if (st) return st;
+  if (rows < 0 || n_states < 0)
+    return fail(AUGTREE_ERR_INVALID_ARGUMENT, "rows=%d n_states=%d must be >= 0", rows, n_states);
+  if (!src && n_states < rows)
+    return fail(AUGTREE_ERR_INVALID_ARGUMENT, "%d states for %d rows without src", n_states, rows);
+  if (rows == 0) return fail_status(AUGTREE_OK, "");
+  const Named need[] = {{q, "q"}, {k, "k"}, {v, "v"}, {state_out, "state_out"}, {o, "o"}};
+  if ((st = check_all(need, 5, true)) || (st = check_ptr(state_in, "state_in", n_states > 0)) ||
+      (st = check_ptr(src, "src", false, 4)))
+    return st;
+  const size_t state = (size_t)num_kv_heads * head_dim * head_dim * sizeof(float);
+  if ((src || state_in != state_out) && overlap(state_in, state * n_states, state_out, state * rows))
+    return fail(AUGTREE_ERR_INVALID_ARGUMENT,
+                "state_out overlaps state_in (in place only without src, and at the same address)");
+  if ((int64_t)rows * num_kv_heads * (head_dim / 64) > INT32_MAX)
+    return fail(AUGTREE_ERR_UNSUPPORTED, "%d rows of %d KV heads exceed a launch", rows, num_kv_heads);
+  if ((st = augtree_check_device())) return st;
+  LinStepParams p;
+  std::memset(&p, 0, sizeof(p));
+  p.q = q;
+  p.k = k;
+  p.v = v;
+  p.state_in = state_in;
+  p.src = src;
+  p.state_out = state_out;
+  p.o = o;
+  p.rows = rows;
+  p.n_states = n_states;
+  p.heads_kv = num_kv_heads;
+  p.group = num_q_heads / num_kv_heads;
+  p.scale = scale;
+  std::copy(decay, decay + num_kv_heads, p.decay);
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  Hook h("linear_step", s);
+  if ((st = hip_ok(launch_lin_step(p, head_dim, s), "step launch"))) return st;
+  return fail_status(AUGTREE_OK, "");
+}
+
+}  // extern "C"
+
+namespace {
+
+int check_norm(int64_t rows, int heads, int d, int activation, float eps) {
+  if (rows < 0) return fail(AUGTREE_ERR_INVALID_ARGUMENT, "rows=%lld must be >= 0", (long long)rows);
+  if (heads < 1 || heads > 65535) return fail(AUGTREE_ERR_UNSUPPORTED, "heads %d not in [1, 65535]", heads);
+  if (d < 8 || d % 8 || d > kHeadNormMaxDim)
+    return fail(AUGTREE_ERR_UNSUPPORTED, "head_dim %d not a multiple of 8 in [8, %d]", d, kHeadNormMaxDim);
+  if (activation != AUGTREE_ACT_NONE && activation != AUGTREE_ACT_SILU)
+    return fail(AUGTREE_ERR_INVALID_ARGUMENT, "unknown activation %d", activation);
+  if (!(eps > 0.f) || !std::isfinite(eps)) return fail(AUGTREE_ERR_INVALID_ARGUMENT, "eps must be finite and > 0");
+  if (rows > ((int64_t)1 << 47) / ((int64_t)heads * d))
+    return fail(AUGTREE_ERR_UNSUPPORTED, "%lld rows of %d x %d", (long long)rows, heads, d);
+  return AUGTREE_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t augtree_head_norm_workspace_size(int64_t rows, int32_t heads, int32_t head_dim) {
+  if (check_norm(rows, heads, head_dim, AUGTREE_ACT_NONE, 1.f)) return 0;
+  fail_status(AUGTREE_OK, "");
+  return align_up((size_t)head_norm_grid(rows, heads, head_dim).parts * 2 * heads * head_dim * sizeof(float));
+}
+
+int augtree_head_norm_fwd(int64_t rows, int32_t heads, int32_t head_dim, int activation, float eps, const uint16_t* x,
+                          const uint16_t* gate, const float* weight, const float* bias, uint16_t* y, void* stream) {
+  int st = check_norm(rows, heads, head_dim, activation, eps);
+  if (st) return st;
+  if (rows == 0) return fail_status(AUGTREE_OK, "");
+  const Named need[] = {{x, "x"}, {y, "y"}}, opt[] = {{gate, "gate"}, {weight, "weight"}, {bias, "bias"}};
+  if ((st = check_all(need, 2, true)) || (st = check_all(opt, 3, false)) || (st = augtree_check_device())) return st;
+  HeadNormParams p;
+  std::memset(&p, 0, sizeof(p));
+  p.x = x;
+  p.gate = gate;
+  p.weight = weight;
+  p.bias = bias;
+  p.y = y;
+  p.rows = rows;
+  p.heads = heads;
+  p.d = head_dim;
+  p.silu = activation == AUGTREE_ACT_SILU;
+  p.eps = eps;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  Hook h("head_norm", s);
+  if ((st = hip_ok(launch_head_norm_fwd(p, s), "head norm launch"))) return st;
+  return fail_status(AUGTREE_OK, "");
+}
+
+int augtree_head_norm_bwd(int64_t rows, int32_t heads, int32_t head_dim, int activation, float eps, const uint16_t* x,
+                          const uint16_t* gate, const float* weight, const float* bias, const uint16_t* dy,
+                          uint16_t* dx, uint16_t* dgate, float* dweight, float* dbias, void* ws, size_t ws_bytes,
+                          void* stream) {
+  int st = check_norm(rows, heads, head_dim, activation, eps);
+  if (st) return st;
+  const Named need[] = {{x, "x"}, {dy, "dy"}, {dx, "dx"}};
+  const Named opt[] = {{gate, "gate"}, {weight, "weight"}, {bias, "bias"}, {dgate, "dgate"}, {dweight, "dweight"},
+                       {dbias, "dbias"}};
+  if (rows > 0 && (st = check_all(need, 3, true))) return st;
+  if ((st = check_all(opt, 6, false))) return st;
+  if (rows > 0 && !gate != !dgate) return fail(AUGTREE_ERR_INVALID_ARGUMENT, "gate and dgate go together");
+  const bool sums = dweight || dbias;
+  if (rows == 0 && !sums) return fail_status(AUGTREE_OK, "");
+  if (sums && (st = check_ws(ws, ws_bytes, augtree_head_norm_workspace_size(rows, heads, head_dim)))) return st;
+  if ((st = augtree_check_device())) return st;
+  HeadNormParams p;
+  std::memset(&p, 0, sizeof(p));
+  p.x = x;
+  p.gate = gate;
+  p.dy = dy;
+  p.weight = weight;
+  p.bias = bias;
+  p.dx = dx;
+  p.dgate = dgate;
+  p.dweight = dweight;
+  p.dbias = dbias;
+  p.part = sums ? static_cast<float*>(ws) : nullptr;
+  p.rows = rows;
+  p.heads = heads;
+  p.d = head_dim;
+  p.silu = activation == AUGTREE_ACT_SILU;
+  p.eps = eps;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  Hook h("head_norm_bwd", s);
+  if ((st = hip_ok(launch_head_norm_bwd(p, s), "head norm backward launch"))) return st;
+  return fail_status(AUGTREE_OK, "");
+}
+
+}  // extern "C"

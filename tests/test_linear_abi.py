@@ -1,0 +1,181 @@
+"""Refusals of the linear-attention layer's entry points (no GPU: every call fails before anything is enqueued)."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2609_33133_amd import _lib, api
+from paper_2609_33133_amd.api import GroupBatch
+from paper_2609_33133_amd.autograd import group_linear_attention, head_norm
+
+OK, INVALID, UNSUPPORTED, MISALIGNED, WORKSPACE, DEVICE = range(6)
+
+
+@pytest.fixture(scope="module")
+def C():
+    return _lib.load()
+
+
+def fake(n=1 << 20):
+    """A 256-byte-aligned address that is never dereferenced."""
+    return ctypes.c_void_p(n * 256)
+
+
+ODD = ctypes.c_void_p((1 << 28) + 2)
+BIG = 1 << 40
+
+
+def dec(*v):
+    return np.array(v, np.float32)
+
+
+def fwd(C, b, decay, p=None, resp=None, ws=None, n=BIG, **kw):
+    p = fake() if p is None else p
+    r = p if resp is None else resp
+    q_p = kw.get("q_p", p)
+    return C.augtree_linear_fwd(b.ref, decay.ctypes.data_as(ctypes.c_void_p), q_p, p, p, r, r, r, kw.get("state"), p, r,
+                                kw.get("state_p"), kw.get("state_r"), fake() if ws is None else ws, n, None)
+
+
+def bwd(C, b, decay, **kw):
+    p = fake()
+    return C.augtree_linear_bwd(b.ref, decay.ctypes.data_as(ctypes.c_void_p), p, p, p, kw.get("do_p", p), p, p, p, p, None,
+                                p, p, p, p, p, kw.get("dv_r", p), kw.get("ws", p), kw.get("n", BIG), None)
+
+
+GOOD = ([0, 10, 25], [0, 2, 3], [0, 5, 12, 20])
+
+
+def test_valid_calls_reach_the_device_check(C):
+    if torch.cuda.is_available():
+        pytest.skip("a GPU is present")
+    b = GroupBatch(*GOOD, 4, 2, 64)
+    assert fwd(C, b, dec(0.9, 1.0)) == DEVICE and bwd(C, b, dec(0.9, 1.0)) == DEVICE
+    plain = GroupBatch([0, 10, 25], [0, 0, 0], [0], 4, 2, 64)
+    assert C.augtree_linear_fwd(plain.ref, dec(1, 1).ctypes.data_as(ctypes.c_void_p), *[fake()] * 3, None, None, None, None,
+                                fake(), None, None, None, fake(), BIG, None) == DEVICE
+
+
+@pytest.mark.parametrize("args,code", [
+    (([0, 10, 10], [0, 2, 3], [0, 5, 12, 20], 4, 2, 64), INVALID),    # empty prompt
+    (([0, 10, 25], [0, 2, 2], [0, 5, 12, 20], 4, 2, 64), INVALID),    # group without branch
+    (([0, 10, 25], [0, 2, 3], [0, 5, 5, 20], 4, 2, 64), INVALID),     # empty branch
+    (([1, 10, 25], [0, 2, 3], [0, 5, 12, 20], 4, 2, 64), INVALID),    # offsets not from 0
+    (([0, 10, 25], [0, 1, 2], [0, 5, 12, 20], 4, 2, 64), INVALID),    # branches that no group has
+    (([0, 10, 25], [0, 2, 3], [0, 5, 12, 20], 4, 3, 64), UNSUPPORTED),
+    (([0, 10, 25], [0, 2, 3], [0, 5, 12, 20], 4, 2, 96), UNSUPPORTED),
+    (([0, 10, 25], [0, 2, 3], [0, 5, 12, 20], 514, 257, 64), UNSUPPORTED),
+])
+def test_bad_batches(C, args, code):
+    b = GroupBatch(*args)
+    d = np.ones(b.hkv, np.float32)
+    assert fwd(C, b, d) == code and bwd(C, b, d) == code
+    assert C.augtree_linear_workspace_size(b.ref, 0) == 0 and C.augtree_last_error() != b""
+    with pytest.raises(_lib.AugtreeError):
+        api.linear_workspace_size(b)
+
+
+@pytest.mark.parametrize("bad", [0.0, -0.5, 1.0001, float("nan"), float("inf")])
+def test_bad_decays(C, bad):
+    b = GroupBatch(*GOOD, 4, 2, 64)
+    assert fwd(C, b, dec(0.9, bad)) == INVALID and bwd(C, b, dec(bad, 0.9)) == INVALID
+    p = fake()
+    assert C.augtree_linear_step(2, 4, 2, 64, 0.1, dec(0.9, bad).ctypes.data_as(ctypes.c_void_p), p, p, p, 2, p, None,
+                                 fake(1 << 21), p, None) == INVALID
+
+
+def test_bad_pointers_and_workspaces(C):
+    b, d = GroupBatch(*GOOD, 4, 2, 64), dec(0.9, 0.9)
+    assert C.augtree_linear_fwd(None, None, *[None] * 11, None, 0, None) == INVALID
+    assert C.augtree_linear_fwd(b.ref, None, *[fake()] * 6, None, fake(), fake(), None, None, fake(), BIG, None) == INVALID
+    assert fwd(C, b, d, q_p=ctypes.c_void_p(None)) == INVALID
+    assert fwd(C, b, d, resp=ctypes.c_void_p(None)) == INVALID
+    assert fwd(C, b, d, q_p=ODD) == MISALIGNED and fwd(C, b, d, state=ODD) == MISALIGNED
+    assert fwd(C, b, d, state_r=ODD) == MISALIGNED
+    need = [C.augtree_linear_workspace_size(b.ref, k) for k in (0, 1)]
+    assert 0 < need[0] < need[1] and need[0] % 256 == 0
+    assert fwd(C, b, d, n=need[0] - 1) == WORKSPACE and fwd(C, b, d, ws=ctypes.c_void_p(None)) == WORKSPACE
+    assert fwd(C, b, d, ws=ctypes.c_void_p((1 << 28) + 16)) == MISALIGNED
+    assert bwd(C, b, d, n=need[1] - 1) == WORKSPACE and bwd(C, b, d, dv_r=ctypes.c_void_p(None)) == INVALID
+    assert bwd(C, b, d, do_p=ODD) == MISALIGNED
+    plain = GroupBatch([0, 10], [0, 0], [0], 4, 2, 64)
+    assert fwd(C, plain, d, state_r=fake()) == INVALID
+    scale = GroupBatch(*GOOD, 4, 2, 64, softmax_scale=float("inf"))
+    assert fwd(C, scale, d) == INVALID
+
+
+def test_step_refusals(C):
+    p, far = fake(), fake(1 << 24)
+
+    def step(rows=4, hq=4, hkv=2, d=64, scale=0.1, n=4, s_in=p, src=None, s_out=far, q=p):
+        return C.augtree_linear_step(rows, hq, hkv, d, scale, np.ones(300, np.float32).ctypes.data_as(ctypes.c_void_p), q, p,
+                                     p, n, s_in, src, s_out, p, None)
+    assert step(rows=0) == OK and step(rows=-1) == INVALID and step(n=-1) == INVALID
+    assert step(n=3) == INVALID and step(d=32) == UNSUPPORTED and step(hq=3) == UNSUPPORTED
+    assert step(hq=257, hkv=257) == UNSUPPORTED and step(scale=0.0) == INVALID
+    assert step(q=None) == INVALID and step(q=ODD) == MISALIGNED and step(src=ODD.value + 1) == MISALIGNED
+    # overlaps: in place needs the same address and no src
+    assert step(src=p, s_out=p) == INVALID
+    assert step(s_out=ctypes.c_void_p(p.value + 2 * 64 * 64 * 4)) == INVALID
+    assert step(rows=2 ** 31 - 1, n=2 ** 31 - 1, hq=256, hkv=256, s_out=ctypes.c_void_p(1 << 60)) == UNSUPPORTED
+    if not torch.cuda.is_available():
+        assert step() == DEVICE and step(s_out=p) == DEVICE and step(src=p, n=1) == DEVICE
+
+
+def test_norm_refusals(C):
+    p = fake()
+
+    def fwd_(rows=4, heads=2, d=64, act=1, eps=1e-5, x=p, y=p):
+        return C.augtree_head_norm_fwd(rows, heads, d, act, eps, x, None, None, None, y, None)
+    assert fwd_(rows=0, x=None) == OK and fwd_(rows=-1) == INVALID
+    for d in (0, 4, 12, 1032):
+        assert fwd_(d=d) == UNSUPPORTED and C.augtree_head_norm_workspace_size(4, 2, d) == 0
+    assert fwd_(heads=0) == UNSUPPORTED and fwd_(heads=65536) == UNSUPPORTED and fwd_(act=2) == INVALID
+    assert fwd_(eps=0.0) == INVALID and fwd_(eps=float("nan")) == INVALID and fwd_(x=None) == INVALID
+    assert fwd_(y=ODD) == MISALIGNED and fwd_(rows=2 ** 47) == UNSUPPORTED
+
+    def bwd_(rows=4, gate=None, dgate=None, dw=None, ws=None, n=0):
+        return C.augtree_head_norm_bwd(rows, 2, 64, 1, 1e-5, p, gate, None, None, p, p, dgate, dw, None, ws, n, None)
+    assert bwd_(gate=p) == INVALID and bwd_(dgate=p) == INVALID
+    need = C.augtree_head_norm_workspace_size(4, 2, 64)
+    assert need > 0 and bwd_(dw=p) == WORKSPACE and bwd_(dw=p, ws=p, n=need - 1) == WORKSPACE
+    assert bwd_(dw=p, ws=ctypes.c_void_p((1 << 28) + 16), n=need) == MISALIGNED
+    assert bwd_(rows=0) == OK
+
+
+def test_python_refusals():
+    b = GroupBatch(*GOOD, 4, 2, 64)
+    z = lambda t, h: torch.zeros(t, h, 64, dtype=torch.bfloat16)
+    x = (z(25, 4), z(25, 2), z(25, 2), z(20, 4), z(20, 2), z(20, 2))
+    with pytest.raises(ValueError, match="no CPU path"):
+        group_linear_attention(*x, b, [0.9, 0.9])
+    with pytest.raises(ValueError, match="no CPU path"):
+        api.linear_fwd(b, [0.9, 0.9], *x)
+    with pytest.raises(ValueError, match="no CPU path"):
+        api.linear_step(*x[:3], [0.9, 0.9], torch.zeros(25, 2, 64, 64))
+    with pytest.raises(ValueError, match="no CPU path"):
+        head_norm(x[0])
+    with pytest.raises(ValueError, match="shape"):
+        group_linear_attention(*x, b, [0.9])
+    with pytest.raises(ValueError, match="constant"):
+        group_linear_attention(*x, b, torch.tensor([0.9, 0.9], requires_grad=True))
+    with pytest.raises(ValueError, match="constant"):
+        group_linear_attention(*x, b, 0.9, state=torch.zeros(2, 2, 64, 64, requires_grad=True))
+    with pytest.raises(ValueError, match="activation"):
+        head_norm(x[0], activation="relu")
+
+
+def test_block_cuts_follow_from_the_tree():
+    """Workspaces grow with the batch, and a batch of two trees needs what its trees need on their own (its states are
+    the sum of theirs)."""
+    def states(trees, backward):
+        cu = lambda v: np.concatenate([[0], np.cumsum(v)])
+        b = GroupBatch(cu([p for p, _ in trees]), cu([len(r) for _, r in trees]), cu([x for _, r in trees for x in r]), 8,
+                       8, 128)
+        return api.linear_workspace_size(b, backward)
+    a, c = [(5000, [700, 3])], [(40, [9000])]
+    state = 8 * 128 * 128 * 4
+    for backward in (False, True):
+        both, one, two = states(a + c, backward), states(a, backward), states(c, backward)
+        assert both > max(one, two) and abs(both - one - two) < state  # the tables differ by alignment only
