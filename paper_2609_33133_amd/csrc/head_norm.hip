@@ -9,8 +9,11 @@
 // are formed again in the backward. Arithmetic in fp32, one rounding at the end.
 //
 // A head is taken by T lanes (the power of two from d / 8 on, at most 64), each
-// holding NC pieces of 8 channels, so its sums stay inside a wavefront.
-#include <algorithm>
+// holding NC pieces of 8 channels, so its sums stay inside a wavefront: exchanges
+// by DPP, no LDS. A lane stays with its channels and goes down the rows, so that
+// weight and bias are read once and their gradients are summed in registers.
+// What else costs here is the vector ALU: the exact expf and division of the
+// activation alone kept the forward at 3.2 of the 4.9 TB/s that a copy reaches.
 #include <type_traits>
 
 #include "common.h"
@@ -19,10 +22,23 @@
 namespace augtree {
 namespace {
 
+template <int CTRL>
+__device__ __forceinline__ float dpp_add(float x) {
+  return x + __uint_as_float(__builtin_amdgcn_mov_dpp((int)__float_as_uint(x), CTRL, 0xf, 0xf, true));
+}
+
+// the sum over T neighbouring lanes, in each of them
 template <int T>
 __device__ __forceinline__ float lane_sum(float x) {
-#pragma unroll
-  for (int k = 1; k < T; k <<= 1) x += __shfl_xor(x, k);
+  if constexpr (T >= 2) x = dpp_add<0xB1>(x);   // quad_perm 1, 0, 3, 2
+  if constexpr (T >= 4) x = dpp_add<0x4E>(x);   // quad_perm 2, 3, 0, 1
+  if constexpr (T >= 8) x = dpp_add<0x141>(x);  // row_half_mirror: the other four of eight
+  if constexpr (T >= 16) x = dpp_add<0x140>(x); // row_mirror: the other eight of sixteen
+  if constexpr (T >= 32) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  }
+  if constexpr (T >= 64) x = pair_sum(x);
   return x;
 }
 
@@ -79,27 +95,51 @@ __device__ __forceinline__ float normalise(float* x, int l, int pieces, float in
       sq += x[i] * x[i];
     }
   }
-  const float rstd = 1.f / sqrtf(lane_sum<T>(sq) * inv_d + eps);
+  const float rstd = __builtin_amdgcn_rsqf(lane_sum<T>(sq) * inv_d + eps);  // 1 ulp
 #pragma unroll
   for (int i = 0; i < 8 * NC; ++i) x[i] *= rstd;
   return rstd;
 }
 
-__device__ __forceinline__ float sigmoid(float u) { return 1.f / (1.f + expf(-u)); }
+// 1 / (1 + e^-u) by the hardware's exp2 and reciprocal, 1 ulp each. The product
+// u log2(e) is rounded once, which is off by 2^-24 |u| in the exponent.
+__device__ __forceinline__ float sigmoid(float u) {
+  return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(u * -1.442695041f));
+}
+
+// The lanes' place: a workgroup takes a run of hpw heads and one of row_parts
+// parts of the rows, which the 256 / T / hpw groups of lanes of a head share.
+template <int T>
+struct Place {
+  int l, head, sub, sharing;
+  bool idle;
+  int64_t r0, r1;
+  __device__ __forceinline__ Place(const HeadNormParams& p, int hpw, int row_parts) {
+    const int grp = threadIdx.x / T;
+    l = threadIdx.x & (T - 1);
+    sharing = 256 / T / hpw;
+    sub = grp / hpw;
+    head = blockIdx.y * hpw + grp - sub * hpw;
+    idle = head >= p.heads || sub >= sharing;
+    r0 = p.rows * blockIdx.x / row_parts;
+    r1 = p.rows * (blockIdx.x + 1) / row_parts;
+  }
+};
 
 template <int T, int NC, bool GATE, bool SILU>
-__global__ __launch_bounds__(256) void head_norm_fwd_kernel(HeadNormParams p) {
-  const int l = threadIdx.x & (T - 1), pieces = p.d / 8;
+__global__ __launch_bounds__(256) void head_norm_fwd_kernel(HeadNormParams p, int hpw, int row_parts) {
+  const Place<T> at(p, hpw, row_parts);
+  if (at.idle) return;
+  const int l = at.l, pieces = p.d / 8;
   const float inv_d = 1.f / (float)p.d;
-  const int64_t units = p.rows * p.heads, step = (int64_t)gridDim.x * (256 / T);
-  for (int64_t u = (int64_t)blockIdx.x * (256 / T) + threadIdx.x / T; u < units; u += step) {
-    const int64_t at = u * p.d;
-    const int head = (int)(u % p.heads);
-    float x[8 * NC], w[8 * NC], b[8 * NC], gt[8 * NC];
-    load16<T, NC>(x, p.x + at, l, pieces);
-    if (GATE) load16<T, NC>(gt, p.gate + at, l, pieces);
-    load32<T, NC>(w, p.weight ? p.weight + head * p.d : nullptr, l, pieces, 1.f);
-    load32<T, NC>(b, p.bias ? p.bias + head * p.d : nullptr, l, pieces, 0.f);
+  float w[8 * NC], b[8 * NC];
+  load32<T, NC>(w, p.weight ? p.weight + at.head * p.d : nullptr, l, pieces, 1.f);
+  load32<T, NC>(b, p.bias ? p.bias + at.head * p.d : nullptr, l, pieces, 0.f);
+  for (int64_t r = at.r0 + at.sub; r < at.r1; r += at.sharing) {
+    const int64_t o = (r * p.heads + at.head) * p.d;
+    float x[8 * NC], gt[8 * NC];
+    load16<T, NC>(x, p.x + o, l, pieces);
+    if (GATE) load16<T, NC>(gt, p.gate + o, l, pieces);
     normalise<T, NC>(x, l, pieces, inv_d, p.eps);
 #pragma unroll
     for (int i = 0; i < 8 * NC; ++i) {
@@ -107,27 +147,23 @@ __global__ __launch_bounds__(256) void head_norm_fwd_kernel(HeadNormParams p) {
       const float act = SILU ? t * sigmoid(t) : t;
       x[i] = GATE ? a * act : act;
     }
-    store16<T, NC>(p.y + at, x, l, pieces);
+    store16<T, NC>(p.y + o, x, l, pieces);
   }
 }
 
-// A workgroup takes the rows of one of `row_parts` parts and a run of `hpw`
-// heads; 256 / T / hpw groups of lanes share the rows of a head. Each group
-// leaves its sums of dweight and dbias as one of p.parts partial sums.
+// Every group of lanes leaves its sums of dweight and dbias as a partial sum.
 template <int T, int NC, bool GATE, bool SILU>
 __global__ __launch_bounds__(256) void head_norm_bwd_kernel(HeadNormParams p, int hpw, int row_parts) {
-  const int l = threadIdx.x & (T - 1), grp = threadIdx.x / T, pieces = p.d / 8;
-  const int rl = 256 / T / hpw;  // groups that share a head
-  const int head = blockIdx.y * hpw + grp % hpw, sub = grp / hpw;
-  if (head >= p.heads || sub >= rl) return;
+  const Place<T> place(p, hpw, row_parts);
+  if (place.idle) return;
+  const int l = place.l, head = place.head, pieces = p.d / 8;
   const float inv_d = 1.f / (float)p.d;
-  const int64_t r0 = p.rows * blockIdx.x / row_parts, r1 = p.rows * (blockIdx.x + 1) / row_parts;
   float w[8 * NC], b[8 * NC], dw[8 * NC], db[8 * NC];
   load32<T, NC>(w, p.weight ? p.weight + head * p.d : nullptr, l, pieces, 1.f);
   load32<T, NC>(b, p.bias ? p.bias + head * p.d : nullptr, l, pieces, 0.f);
 #pragma unroll
   for (int i = 0; i < 8 * NC; ++i) dw[i] = db[i] = 0.f;
-  for (int64_t r = r0 + sub; r < r1; r += rl) {
+  for (int64_t r = place.r0 + place.sub; r < place.r1; r += place.sharing) {
     const int64_t at = (r * p.heads + head) * p.d;
     float n[8 * NC], gt[8 * NC], dy[8 * NC];
     load16<T, NC>(n, p.x + at, l, pieces);
@@ -156,7 +192,7 @@ __global__ __launch_bounds__(256) void head_norm_bwd_kernel(HeadNormParams p, in
     if (GATE) store16<T, NC>(p.dgate + at, gt, l, pieces);
   }
   if (!p.part) return;
-  float* const out = p.part + ((int64_t)blockIdx.x * rl + sub) * 2 * p.heads * p.d + (int64_t)head * p.d;
+  float* const out = p.part + ((int64_t)blockIdx.x * place.sharing + place.sub) * 2 * p.heads * p.d + (int64_t)head * p.d;
 #pragma unroll
   for (int c = 0; c < NC; ++c) {
     const int k = l + c * T;
@@ -169,20 +205,25 @@ __global__ __launch_bounds__(256) void head_norm_bwd_kernel(HeadNormParams p, in
   }
 }
 
-// dweight, dbias: the partial sums in order. 64 channels a workgroup, four
-// wavefronts with every fourth part each.
-__global__ __launch_bounds__(256) void head_norm_sum_kernel(const float* part, int parts, int width, float* dweight,
-                                                            float* dbias) {
-  __shared__ float s[4][64];
+// dweight, dbias: the partial sums. 64 channels a workgroup, 16 wavefronts with
+// every 16th part each (one wavefront of 4 took 54 us for 512 parts of 2 x 4096
+// where this takes SUM_US), then the 16 in order.
+__global__ __launch_bounds__(1024) void head_norm_sum_kernel(const float* part, int parts, int width, float* dweight,
+                                                             float* dbias) {
+  __shared__ float s[16][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int i = blockIdx.x * 64 + lane;  // of 2 * width
+  const int64_t i = (int64_t)blockIdx.x * 64 + lane, row = 2 * (int64_t)width;
   float a = 0.f;
-  if (i < 2 * width)
-    for (int k = wave; k < parts; k += 4) a += part[(int64_t)k * 2 * width + i];
+  if (i < row) {
+#pragma unroll 8
+    for (int k = wave; k < parts; k += 16) a += part[k * row + i];
+  }
   s[wave][lane] = a;
   __syncthreads();
-  if (wave == 0 && i < 2 * width) {
-    a = (s[0][lane] + s[1][lane]) + (s[2][lane] + s[3][lane]);
+  if (wave == 0 && i < row) {
+    a = 0.f;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) a += s[k][lane];
     if (i < width) {
       if (dweight) dweight[i] = a;
     } else if (dbias) {
@@ -209,12 +250,12 @@ hipError_t with_shape(int d, F f) {
 hipError_t launch_head_norm_fwd(const HeadNormParams& p, hipStream_t stream) {
   return with_shape(p.d, [&](auto t, auto nc) {
     constexpr int T = decltype(t)::value, NC = decltype(nc)::value;
-    const int64_t units = p.rows * p.heads, per = 256 / T;
-    const dim3 grid((unsigned)std::min<int64_t>((units + per - 1) / per, 8192));
-    if (p.gate && p.silu) head_norm_fwd_kernel<T, NC, true, true><<<grid, 256, 0, stream>>>(p);
-    else if (p.gate) head_norm_fwd_kernel<T, NC, true, false><<<grid, 256, 0, stream>>>(p);
-    else if (p.silu) head_norm_fwd_kernel<T, NC, false, true><<<grid, 256, 0, stream>>>(p);
-    else head_norm_fwd_kernel<T, NC, false, false><<<grid, 256, 0, stream>>>(p);
+    const HeadNormGrid g = head_norm_grid(p.rows, p.heads, p.d, 4096);
+    const dim3 grid(g.row_parts, g.head_blocks);
+    if (p.gate && p.silu) head_norm_fwd_kernel<T, NC, true, true><<<grid, 256, 0, stream>>>(p, g.heads, g.row_parts);
+    else if (p.gate) head_norm_fwd_kernel<T, NC, true, false><<<grid, 256, 0, stream>>>(p, g.heads, g.row_parts);
+    else if (p.silu) head_norm_fwd_kernel<T, NC, false, true><<<grid, 256, 0, stream>>>(p, g.heads, g.row_parts);
+    else head_norm_fwd_kernel<T, NC, false, false><<<grid, 256, 0, stream>>>(p, g.heads, g.row_parts);
     return hipGetLastError();
   });
 }
@@ -222,7 +263,7 @@ hipError_t launch_head_norm_fwd(const HeadNormParams& p, hipStream_t stream) {
 hipError_t launch_head_norm_bwd(const HeadNormParams& p, hipStream_t stream) {
   const hipError_t e = with_shape(p.d, [&](auto t, auto nc) {
     constexpr int T = decltype(t)::value, NC = decltype(nc)::value;
-    const HeadNormGrid g = head_norm_grid(p.rows, p.heads, p.d);
+    const HeadNormGrid g = head_norm_bwd_grid(p.rows, p.heads, p.d);
     const dim3 grid(g.row_parts, g.head_blocks);
     if (p.gate && p.silu) head_norm_bwd_kernel<T, NC, true, true><<<grid, 256, 0, stream>>>(p, g.heads, g.row_parts);
     else if (p.gate) head_norm_bwd_kernel<T, NC, true, false><<<grid, 256, 0, stream>>>(p, g.heads, g.row_parts);
@@ -232,7 +273,7 @@ hipError_t launch_head_norm_bwd(const HeadNormParams& p, hipStream_t stream) {
   });
   if (e != hipSuccess || !p.part) return e;
   const int width = p.heads * p.d;
-  head_norm_sum_kernel<<<(2 * width + 63) / 64, 256, 0, stream>>>(p.part, head_norm_grid(p.rows, p.heads, p.d).parts,
+  head_norm_sum_kernel<<<(2 * width + 63) / 64, 1024, 0, stream>>>(p.part, head_norm_bwd_grid(p.rows, p.heads, p.d).parts,
                                                                   width, p.dweight, p.dbias);
   return hipGetLastError();
 }

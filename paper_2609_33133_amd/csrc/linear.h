@@ -55,19 +55,26 @@ struct LinScanParams {
   LinBatch b;
 };
 
-// out_t = scale * (sum over the block's rows before (reverse: after) and at t of
-// decay^distance (x_t . y_j) z_j + decay^(distance to the block's edge) x_t . state)
+// o from q, k, v and the states that reach the blocks.
 struct LinOutParams {
-  const uint16_t* x[2];
-  const uint16_t* y[2];
-  const uint16_t* z[2];
-  uint16_t* out[2];
+  const uint16_t *q[2], *k[2], *v[2];
+  uint16_t* o[2];
   const float* states;
   float scale;
   LinBatch b;
 };
 
-static_assert(sizeof(LinStateParams) <= 4096 && sizeof(LinScanParams) <= 4096 && sizeof(LinOutParams) <= 4096,
+// dq, dk, dv from q, k, v, do and the states in both directions.
+struct LinGradParams {
+  const uint16_t *q[2], *k[2], *v[2], *dout[2];
+  uint16_t *dq[2], *dk[2], *dv[2];
+  const float *states, *states_rev;
+  float scale;
+  LinBatch b;
+};
+
+static_assert(sizeof(LinStateParams) <= 4096 && sizeof(LinScanParams) <= 4096 && sizeof(LinOutParams) <= 4096 &&
+                  sizeof(LinGradParams) <= 4096,
               "kernel arguments");
 
 // writes n words (at most kLinTableWords) to dst
@@ -83,8 +90,8 @@ hipError_t launch_lin_table(const LinTable& t, hipStream_t stream);
 // exact: sums to fp32 accuracy (states that are handed out)
 hipError_t launch_lin_state(const LinStateParams& p, int head_dim, bool reverse, bool exact, hipStream_t stream);
 hipError_t launch_lin_scan(const LinScanParams& p, int head_dim, bool reverse, bool prompts, hipStream_t stream);
-// transposed: the states hold [z][y] instead of [y][z]
-hipError_t launch_lin_out(const LinOutParams& p, int head_dim, bool reverse, bool transposed, hipStream_t stream);
+hipError_t launch_lin_out(const LinOutParams& p, int head_dim, hipStream_t stream);
+hipError_t launch_lin_grad(const LinGradParams& p, int head_dim, hipStream_t stream);
 
 struct LinStepParams {
   const uint16_t *q, *k, *v;
@@ -109,13 +116,13 @@ struct HeadNormParams {
   int32_t silu;
   float eps;
 };
-// The backward's workgroups: row_parts x head_blocks of `heads` heads, leaving
-// `parts` partial sums of the weight and bias gradients.
+// Workgroups: row_parts x head_blocks (about `want` at most) of `heads` heads. In
+// the backward they leave `parts` partial sums of the weight and bias gradients.
 struct HeadNormGrid {
   int heads, head_blocks, row_parts, parts;
 };
 constexpr int kHeadNormMaxDim = 1024;
-inline HeadNormGrid head_norm_grid(int64_t rows, int heads, int d) {
+inline HeadNormGrid head_norm_grid(int64_t rows, int heads, int d, int want) {
   int lanes = 1;
   while (lanes < d / 8 && lanes < 64) lanes *= 2;
   const int groups = 256 / lanes;
@@ -123,12 +130,13 @@ inline HeadNormGrid head_norm_grid(int64_t rows, int heads, int d) {
   g.heads = heads < groups ? heads : groups;
   g.head_blocks = (heads + g.heads - 1) / g.heads;
   const int sharing = groups / g.heads;  // groups of lanes that share a head's rows
-  int64_t parts = 1024 / g.head_blocks;
+  int64_t parts = want / g.head_blocks;
   if (parts * sharing > rows) parts = (rows + sharing - 1) / sharing;
   g.row_parts = parts < 1 ? 1 : (int)parts;
   g.parts = g.row_parts * sharing;
   return g;
 }
+inline HeadNormGrid head_norm_bwd_grid(int64_t rows, int heads, int d) { return head_norm_grid(rows, heads, d, 1024); }
 hipError_t launch_head_norm_fwd(const HeadNormParams& p, hipStream_t stream);
 hipError_t launch_head_norm_bwd(const HeadNormParams& p, hipStream_t stream);
 
