@@ -59,6 +59,7 @@ int check_ptr(const void* p, const char* name, bool required, size_t align = 16)
 int check_heads(int hq, int hkv, int d, float scale, const float* decay) {
   if (hq < 1 || hkv < 1) return fail(AUGTREE_ERR_INVALID_ARGUMENT, "head counts must be >= 1");
   if (hq % hkv) return fail(AUGTREE_ERR_UNSUPPORTED, "num_q_heads %d not a multiple of num_kv_heads %d", hq, hkv);
+  if (hq > 65536) return fail(AUGTREE_ERR_UNSUPPORTED, "num_q_heads %d > 65536", hq);  // 64 rows within 2^31 bytes
   if (hkv > kLinMaxHeads) return fail(AUGTREE_ERR_UNSUPPORTED, "num_kv_heads %d > %d", hkv, kLinMaxHeads);
   if (d != 64 && d != 128) return fail(AUGTREE_ERR_UNSUPPORTED, "head_dim %d not in {64,128}", d);
   if (!(scale > 0.f) || !std::isfinite(scale))
@@ -140,7 +141,7 @@ int make_layout(const augtree_groups* g, Layout* L) {
     for (int b = g->cu_branch[t]; b < g->cu_branch[t + 1]; ++b)
       add(ng + b, g->cu_resp[b], g->cu_resp[b + 1] - g->cu_resp[b], t, rows[t]);
   const int64_t slices = (int64_t)g->head_dim * g->head_dim / 1024;
-  if (blocks * g->num_kv_heads > INT32_MAX || (ng + (int64_t)nb) * g->num_kv_heads * slices > INT32_MAX)
+  if (blocks * g->num_kv_heads > INT32_MAX / 3 - 8 || (ng + (int64_t)nb) * g->num_kv_heads * slices > INT32_MAX)
     return fail(AUGTREE_ERR_UNSUPPORTED, "%lld blocks of %d KV heads exceed a launch", (long long)blocks,
                 g->num_kv_heads);
   L->blocks = blocks;
@@ -236,18 +237,6 @@ struct Call {
     }
     return AUGTREE_OK;
   }
-
-  int out(const char* role, bool reverse, bool transposed, const uint16_t* const x[2], const uint16_t* const y[2],
-          const uint16_t* const z[2], uint16_t* const o[2], const float* states) {
-    LinOutParams p;
-    std::memset(&p, 0, sizeof(p));
-    for (int i = 0; i < 2; ++i) p.x[i] = x[i], p.y[i] = y[i], p.z[i] = z[i], p.out[i] = o[i];
-    p.states = states;
-    p.scale = g->softmax_scale;
-    p.b = b;
-    Hook h(role, stream);
-    return hip_ok(launch_lin_out(p, g->head_dim, reverse, transposed, stream), role);
-  }
 };
 
 int check_ws(const void* ws, size_t have, size_t need) {
@@ -315,9 +304,15 @@ int augtree_linear_fwd(const augtree_groups* grp, const float* decay, const uint
     float* const tree = c.take<float>(c.L.tree * grp->num_groups);
     const uint16_t *const q[2] = {q_p, q_r}, *const k[2] = {k_p, k_r}, *const v[2] = {v_p, v_r};
     uint16_t* const o[2] = {o_p, o_r};
-    if ((st = c.states(false, k, v, state, states, tree, state_p, state_r, true)) ||
-        (st = c.out("linear_out", false, false, q, k, v, o, states)))
-      return st;
+    if ((st = c.states(false, k, v, state, states, tree, state_p, state_r, true))) return st;
+    LinOutParams p;
+    std::memset(&p, 0, sizeof(p));
+    for (int i = 0; i < 2; ++i) p.q[i] = q[i], p.k[i] = k[i], p.v[i] = v[i], p.o[i] = o[i];
+    p.states = states;
+    p.scale = grp->softmax_scale;
+    p.b = c.b;
+    Hook h("linear_out", c.stream);
+    if ((st = hip_ok(launch_lin_out(p, grp->head_dim, c.stream), "output launch"))) return st;
     return fail_status(AUGTREE_OK, "");
   });
 }
@@ -354,11 +349,20 @@ int augtree_linear_bwd(const augtree_groups* grp, const float* decay, const uint
                    *const g[2] = {do_p, do_r};
     uint16_t *const dq[2] = {dq_p, dq_r}, *const dk[2] = {dk_p, dk_r}, *const dv[2] = {dv_p, dv_r};
     if ((st = c.states(false, k, v, state, fwd, tree, nullptr, nullptr, false)) ||
-        (st = c.out("linear_dq", false, true, g, v, k, dq, fwd)) ||
-        (st = c.states(true, q, g, nullptr, rev, ends, nullptr, nullptr, false)) ||
-        (st = c.out("linear_dv", true, false, k, q, g, dv, rev)) ||
-        (st = c.out("linear_dk", true, true, v, g, q, dk, rev)))
+        (st = c.states(true, q, g, nullptr, rev, ends, nullptr, nullptr, false)))
       return st;
+    LinGradParams p;
+    std::memset(&p, 0, sizeof(p));
+    for (int i = 0; i < 2; ++i) {
+      p.q[i] = q[i], p.k[i] = k[i], p.v[i] = v[i], p.dout[i] = g[i];
+      p.dq[i] = dq[i], p.dk[i] = dk[i], p.dv[i] = dv[i];
+    }
+    p.states = fwd;
+    p.states_rev = rev;
+    p.scale = grp->softmax_scale;
+    p.b = c.b;
+    Hook h("linear_grad", c.stream);
+    if ((st = hip_ok(launch_lin_grad(p, grp->head_dim, c.stream), "gradient launch"))) return st;
     return fail_status(AUGTREE_OK, "");
   });
 }
@@ -429,7 +433,7 @@ extern "C" {
 size_t augtree_head_norm_workspace_size(int64_t rows, int32_t heads, int32_t head_dim) {
   if (check_norm(rows, heads, head_dim, AUGTREE_ACT_NONE, 1.f)) return 0;
   fail_status(AUGTREE_OK, "");
-  return align_up((size_t)head_norm_grid(rows, heads, head_dim).parts * 2 * heads * head_dim * sizeof(float));
+  return align_up((size_t)head_norm_bwd_grid(rows, heads, head_dim).parts * 2 * heads * head_dim * sizeof(float));
 }
 
 int augtree_head_norm_fwd(int64_t rows, int32_t heads, int32_t head_dim, int activation, float eps, const uint16_t* x,

@@ -14,16 +14,19 @@
 // or from the branches back onto the prompt (lin_scan_kernel), and the outputs,
 // every block from the state that reaches it (lin_out_kernel).
 //
-// A workgroup has one wavefront for every 32 columns of z. The state's columns
-// stay in that wavefront's accumulators (rows: y, column of the lane: z) and
-// serve from there as an operand of the next product, whose k index runs over
-// y: the row order of `perm` below makes registers 8s .. 8s+7 of a lane hold 8
-// consecutive rows of y, so that x is read from LDS in its plain order.
+// A workgroup has one wavefront for every 16 columns of z (8 for d = 128). The
+// state's columns stay in that wavefront's accumulators (rows: y, column of the
+// lane: z) and serve from there as an operand of the next product, whose k index
+// runs over y. Small tiles (16x16x32 products) keep a wavefront below 128
+// registers: with 16 wavefronts on a CU the LDS reads in front of the matrix
+// instructions are covered; 4 wavefronts of 32 columns each (32x32x16, 244
+// registers, 8 on a CU) took 305 us where these take OUT_US (49152 rows, 32 / 8
+// heads, d = 128, forward).
 //
-// Roundings to bf16, all of them operands of matrix products: P (2^-9 of an
-// element); the decayed z of the state's update and the state itself as an
-// operand are each split into two bf16 terms (2^-17), or z into three (2^-25)
-// where the state is handed out in fp32.
+// Roundings to bf16, all of them operands of matrix products: P, the decayed z of
+// the state's update and the state itself as an operand are each split into two
+// bf16 terms (2^-17 of an element), or z into three (2^-25) where the state is
+// handed out in fp32.
 #include "common.h"
 #include "linear.h"
 
@@ -31,80 +34,150 @@ namespace augtree {
 namespace {
 
 constexpr int C = kLinChunk;
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2), may_alias));
 
 // ---------------------------------------------------------------------------- the batch
 
 struct Block {
-  int seg, row0, len;
-  int index, count;  // of its segment's blocks
-  bool prompt;
+  int row0, len;
+  bool prompt, first, last;  // of a prompt; the first, the last block of its segment
 };
 
-__device__ __forceinline__ const LinSeg* segments(const LinBatch& b) { return b.segs ? b.segs : b.inl; }
+// Segment i. From the kernel arguments or the device copy, each by an access of
+// its own kind, and made uniform (scalar registers).
+__device__ __forceinline__ LinSeg load_segment(const LinBatch& b, int i) {
+  const LinSeg s = b.segs ? b.segs[i] : b.inl[i];
+  return {__builtin_amdgcn_readfirstlane(s.row0), __builtin_amdgcn_readfirstlane(s.len),
+          __builtin_amdgcn_readfirstlane(s.block0), __builtin_amdgcn_readfirstlane(s.link),
+          __builtin_amdgcn_readfirstlane(s.rows)};
+}
 
 __device__ __forceinline__ Block find_block(const LinBatch& b, int block) {
-  const LinSeg* s = segments(b);
   int lo = 0, hi = b.num_trees + b.num_branches;
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
-    if (s[mid].block0 <= block) lo = mid;
+    const int first = __builtin_amdgcn_readfirstlane(b.segs ? b.segs[mid].block0 : b.inl[mid].block0);
+    if (first <= block) lo = mid;
     else hi = mid;
   }
+  const LinSeg s = load_segment(b, lo);
   Block r;
-  const int at = (block - s[lo].block0) * s[lo].rows;
-  r.seg = lo;
-  r.row0 = s[lo].row0 + at;
-  r.len = min(s[lo].rows, s[lo].len - at);
-  r.index = block - s[lo].block0;
-  r.count = (s[lo].len + s[lo].rows - 1) / s[lo].rows;
+  const int at = (block - s.block0) * s.rows;
+  r.row0 = s.row0 + at;
+  r.len = min(s.rows, s.len - at);
+  r.first = at == 0;
+  r.last = s.len - at <= s.rows;
   r.prompt = lo < b.num_trees;
   return r;
 }
 
 // ---------------------------------------------------------------------------- operands
+//
+// 16x16x32 products: lane l holds row (column) l % 16 of the first (second)
+// operand, k indices 8 (l / 16) .. + 7; of the result column l % 16, rows
+// 4 (l / 16) + 0..3.
 
-// Transpose reads of a swizzled [64, D] tile (TrOffsets of common.h), of the
-// 32 columns from c0 on. PERM exchanges the second and third group of four
-// columns in every 16, which gives accumulator register i of half-wave hf the
-// column 16 (i / 8) + 8 hf + i % 8 of the 32.
-template <int D, bool PERM>
-struct ColumnReader {
-  int o[2];
-  __device__ __forceinline__ void init(int c0, int lane) {
-    const int grp = lane >> 4, j = lane & 15;
-    const int row = 4 * (grp >> 1) + (j >> 2);
-    const int q = j & 3, qp = PERM ? ((q & 1) << 1) | (q >> 1) : q;
-    const int col = c0 + 16 * (grp & 1) + 4 * qp;
-    o[0] = 2 * toff<D>(row, col);
-    o[1] = 2 * toff<D>(row + 8, col);
-  }
-  // rows 16 m .. 16 m + 15: elements 0..3 are rows 16 m + 4 hf + 0..3, 4..7 are 8 further on
-  __device__ __forceinline__ bf16x8 read(const __bf16* tile, int m) const {
-    const char* t = reinterpret_cast<const char*>(tile) + m * 16 * D * 2;
-    const s16x4 a = lds_tr16(reinterpret_cast<const __bf16*>(t + o[0]));
-    const s16x4 b = lds_tr16(reinterpret_cast<const __bf16*>(t + o[1]));
-    bf16x8 r;
-    __builtin_memcpy(&r, &a, 8);
-    __builtin_memcpy(reinterpret_cast<char*>(&r) + 8, &b, 8);
-    return r;
-  }
-};
+__device__ __forceinline__ f32x4 mfma16(const bf16x8& a, const bf16x8& b, const f32x4& c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
 
-// v = hi + lo up to 2^-17 of v
-__device__ __forceinline__ void split2(const float* v, bf16x8& hi, bf16x8& lo) {
+// LDS tiles: row-major, the 16-byte pieces of a row exchanged by an exclusive or
+// with swz16(row). The LDS serves a 16-byte read in groups of 16 lanes that take
+// rows 0-3 and 12-15 from one quarter of the wavefront and rows 4-11 from the
+// next one, whose piece differs in bit 0; and a transpose read in groups of 32,
+// four rows and two neighbouring pieces from one quarter and the rows 8 further
+// on from the next. The order 0, 2, 3, 1 of the middle bits keeps both free of
+// bank conflicts. (With the order 0, 1, 2, 3, made for 32x32 products, 45 % of
+// the LDS cycles here were conflicts.)
+template <int D>
+__device__ __forceinline__ int swz16(int row) {
+  const int g = (0x78 >> ((row >> 1) & 6)) & 3;  // 0, 2, 3, 1 for rows 0-3, 4-7, 8-11, 12-15
+  if constexpr (D == 128) return ((row & 3) << 2) | g;
+  else return (((row >> 1) & 1) << 2) | g;
+}
+
+// element offset of (row, col); col % 4 == 0 keeps 8-byte accesses inside one piece
+template <int D>
+__device__ __forceinline__ int loff(int row, int col) {
+  return row * D + (((col >> 3) ^ swz16<D>(row)) << 3) + (col & 7);
+}
+
+// An operand whose k index runs down the rows of a swizzled [64, D] tile: 16
+// columns, of which lane j of 16 names the four from `col` on in row j / 4 and
+// receives one in four rows (transpose reads). Rows 32 m + 8 (lane / 16) + 0..7
+// are read in two pieces of four, which lie 4 rows apart: row bit 2 and, in the
+// swizzle, piece bit 1.
+template <int D>
+__device__ __forceinline__ int column_base(int col, int lane) {
+  return 2 * loff<D>(8 * (lane >> 4) + ((lane & 15) >> 2), col);
+}
+// `base`: byte offset of the named columns; FLIP: bytes by which the columns wanted differ from them (bits of the
+// swizzled piece, so an exclusive or)
+template <int D>
+__device__ __forceinline__ bf16x8 read_columns(const __bf16* tile, int base, int flip, int m) {
+  const char* t = reinterpret_cast<const char*>(tile) + m * 32 * D * 2;
+  constexpr int kFourRows = D == 128 ? 4 * 256 + 32 : 4 * 128 + 32;
+  const s16x4 a = lds_tr16(reinterpret_cast<const __bf16*>(t + (base ^ flip)));
+  const s16x4 b = lds_tr16(reinterpret_cast<const __bf16*>(t + (base ^ flip ^ kFourRows)));
+  bf16x8 r;
+  __builtin_memcpy(&r, &a, 8);
+  __builtin_memcpy(reinterpret_cast<char*>(&r) + 8, &b, 8);
+  return r;
+}
+
+// The compiler keeps such sums of a base and a constant over a loop, a register
+// each; behind this it forms them where they are used.
+__device__ __forceinline__ int here(int base) {
+  asm volatile("" : "+v"(base));
+  return base;
+}
+
+// Rows of the state (columns of y) in the accumulators: register i of tile t in
+// lane quarter q. Tiles 2s and 2s + 1 are k step s of the product with x, whose
+// lanes need the same 8 columns of x. Plain: 16 t + 4 q + i, so x is read in two
+// pieces of four columns. PAIRED: the two tiles take every other four columns,
+// and x is read in pieces of eight; but then the transpose reads of y touch every
+// other 8 bytes, two lanes a bank. Paired pays where x is read once a head and y
+// once a chunk (forward), plain in reverse.
+template <bool PAIRED>
+__device__ __forceinline__ int state_row(int t, int q, int i) {
+  return PAIRED ? 32 * (t >> 1) + 8 * q + 4 * (t & 1) + i : 16 * t + 4 * q + i;
+}
+
+// a and b as bf16, a in the low half. (Two conversions in one instruction, which
+// the compiler does not always find.)
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
+  uint32_t r;
+  asm("v_cvt_pk_bf16_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+  return r;
+}
+
+// v = hi + lo up to 2^-17 of v (NEXT: what is left of v stays in it)
+template <bool NEXT = false>
+__device__ __forceinline__ void split2(float* v, bf16x8& hi, bf16x8& lo) {
+  uint32_t h[4], l[4];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    hi[e] = (__bf16)v[e];
-    lo[e] = (__bf16)(v[e] - (float)hi[e]);
+  for (int e = 0; e < 4; ++e) {
+    float &a = v[2 * e], &b = v[2 * e + 1];
+    h[e] = bf16_pair(a, b);
+    a -= __uint_as_float(h[e] << 16);
+    b -= __uint_as_float(h[e] & 0xffff0000u);
+    l[e] = bf16_pair(a, b);
+    if (NEXT) {
+      a -= __uint_as_float(l[e] << 16);
+      b -= __uint_as_float(l[e] & 0xffff0000u);
+    }
   }
+  __builtin_memcpy(&hi, h, 16);
+  __builtin_memcpy(&lo, l, 16);
 }
 
 // The decays of a workgroup in LDS. row[r]: from row r of a chunk of n rows to
 // its end (reverse: to its start), the weights of the state's update; rows from
-// n on weigh nothing. pair[32 + k]: over a distance of k rows, 0 for k < 0.
+// n on weigh nothing. pair[16 + k]: over a distance of k rows, 0 for k < 0.
 struct Decays {
   float row[C];
-  float pair[32 + C];
+  float pair[16 + C];
 };
 
 template <bool REV>
@@ -114,97 +187,139 @@ __device__ __forceinline__ void set_row_decays(Decays& t, float lg, int n) {
 }
 __device__ __forceinline__ void set_pair_decays(Decays& t, float lg) {
   const int i = threadIdx.x;
-  if (i < 32 + C) t.pair[i] = i < 32 ? 0.f : exp2f(lg * (float)(i - 32));
+  if (i < 16 + C) t.pair[i] = i < 16 ? 0.f : exp2f(lg * (float)(i - 16));
 }
 
-// s += Y^T (w Z) of one chunk: rows y (of all of Y's D columns, permuted),
-// columns z (32 of this wavefront). TERMS bf16 terms of the weighted z.
-template <int D, int TERMS>
-__device__ __forceinline__ void update_state(f32x16* s, const __bf16* yt, const __bf16* zt,
-                                             const ColumnReader<D, true>* yr, const ColumnReader<D, false>& zr,
-                                             const float* w, int hf) {
+// s += Y^T (w Z) of one chunk: rows y (of all of Y's D columns), columns z (16 of
+// this wavefront, in zf). TERMS bf16 terms of the weighted z.
+template <int D, bool PAIRED, int TERMS>
+__device__ __forceinline__ void update_state(f32x4* s, const __bf16* yt, const bf16x8* zf, int ybase, const float* w,
+                                             int q) {
+  const int yb = here(ybase);
 #pragma unroll
-  for (int m = 0; m < 4; ++m) {
-    const bf16x8 z = zr.read(zt, m);
-    const f32x4 w0 = *reinterpret_cast<const f32x4*>(w + 16 * m + 4 * hf);
-    const f32x4 w1 = *reinterpret_cast<const f32x4*>(w + 16 * m + 8 + 4 * hf);
+  for (int m = 0; m < 2; ++m) {
+    const f32x4 w0 = *reinterpret_cast<const f32x4*>(w + 32 * m + 8 * q);
+    const f32x4 w1 = *reinterpret_cast<const f32x4*>(w + 32 * m + 8 * q + 4);
     float f[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) f[e] = (float)z[e] * (e < 4 ? w0[e] : w1[e - 4]);
+    for (int e = 0; e < 8; ++e) f[e] = (float)zf[m][e] * (e < 4 ? w0[e] : w1[e - 4]);
     bf16x8 b[3];
-    split2(f, b[0], b[1]);
+    split2<TERMS == 3>(f, b[0], b[1]);
     if constexpr (TERMS == 3) {
+      uint32_t r[4];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) b[2][e] = (__bf16)(f[e] - (float)b[0][e] - (float)b[1][e]);
+      for (int e = 0; e < 4; ++e) r[e] = bf16_pair(f[2 * e], f[2 * e + 1]);
+      __builtin_memcpy(&b[2], r, 16);
     }
 #pragma unroll
-    for (int t = 0; t < D / 32; ++t) {
-      const bf16x8 a = yr[t].read(yt, m);
+    for (int t = 0; t < D / 16; ++t) {
+      const bf16x8 a = read_columns<D>(yt, yb, PAIRED ? 64 * (t >> 1) + 8 * (t & 1) : 32 * t, m);
 #pragma unroll
-      for (int k = 0; k < TERMS; ++k) s[t] = mfma32(a, b[k], s[t]);
+      for (int k = 0; k < TERMS; ++k) s[t] = mfma16(a, b[k], s[t]);
     }
   }
 }
 
-// row of the state (y column) that register i of tile t holds
-__device__ __forceinline__ int state_row(int t, int i, int hf) { return 32 * t + 16 * (i >> 3) + 8 * hf + (i & 7); }
+template <int NT>
+__device__ __forceinline__ void scale_state(f32x4* s, float f) {
+#pragma unroll
+  for (int t = 0; t < NT; ++t) s[t] *= f;
+}
+
+// A [64, D] tile on its way from memory to LDS through registers: fetch()
+// issues the loads, put() waits for them and writes the swizzled tile. The loads
+// of the next tiles are in flight while a chunk is worked on, and LDS holds one
+// tile of each operand, so that two workgroups fit a CU. Rows from n on are zeros.
+template <int D, int NW>
+struct TileStage {
+  static constexpr int CH = D / 8, RPI = 64 / CH, NI = C / (RPI * NW);
+  static_assert(NW * RPI == 32, "rows of one pass: a multiple of the swizzle's period");
+  raw16 r[NI];
+  __device__ __forceinline__ static int row() {
+    return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * RPI + (threadIdx.x & 63) / CH;
+  }
+  // byte offset of this lane's first piece in the tensor's rows (of `stride` elements)
+  __device__ __forceinline__ static uint32_t source(int64_t stride) {
+    return (uint32_t)(2 * row() * stride) + 16 * ((threadIdx.x & 63) % CH);
+  }
+  __device__ __forceinline__ static int target() {
+    return 2 * row() * D + ((((threadIdx.x & 63) % CH) ^ swz16<D>(row())) << 4);
+  }
+  __device__ __forceinline__ void fetch(const uint16_t* base, uint32_t src, int n, int64_t stride) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    const __amdgpu_buffer_rsrc_t rsrc =
+        __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, (int)(2 * n * stride), 0x00020000);
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const auto v = __builtin_amdgcn_raw_buffer_load_b128(rsrc, src + i * (uint32_t)(64 * stride), 0, 0);
+      __builtin_memcpy(&r[i], &v, 16);
+    }
+#endif
+  }
+  __device__ __forceinline__ void put(__bf16* tile, int dst) const {
+    char* t = reinterpret_cast<char*>(tile) + dst;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) *reinterpret_cast<raw16*>(t + i * 64 * D) = r[i];
+  }
+};
 
 // ---------------------------------------------------------------------------- blocks' own states
 
 template <int D, bool REV, int TERMS>
-__global__ __launch_bounds__(2 * D, 2) void lin_state_kernel(LinStateParams p) {
-  constexpr int NW = D / 32;
+__global__ __launch_bounds__(4 * D, 4) void lin_state_kernel(LinStateParams p) {
+  constexpr int NT = D / 16;  // tiles of the state's rows, and wavefronts
   __shared__ __attribute__((aligned(1024))) __bf16 yt[C * D];
   __shared__ __attribute__((aligned(1024))) __bf16 zt[C * D];
   __shared__ __attribute__((aligned(16))) Decays decays;
   const int block = blockIdx.x / p.b.heads_kv, kvh = blockIdx.x - block * p.b.heads_kv;
   const Block bl = find_block(p.b, block);
-  const bool edge = REV ? bl.index == 0 : bl.index == bl.count - 1;
+  const bool edge = REV ? bl.first : bl.last;
   if (edge && (bl.prompt ? p.skip_prompt : p.skip_branch)) return;
 
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hf = lane >> 5;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), q = lane >> 4;
   const float lg = p.b.log2_decay[kvh];
   const int side = bl.prompt ? 0 : 1, gy = p.heads_y / p.b.heads_kv;
   const int64_t stride = (int64_t)p.heads_y * D;
   const uint16_t* y = p.y[side] + bl.row0 * stride + (int64_t)kvh * gy * D;
   const uint16_t* z = p.z[side] + bl.row0 * stride + (int64_t)kvh * gy * D;
-  TileCopy<C, D, NW> copy;
-  copy.init(stride);
-  ColumnReader<D, true> yr[NW];
-  ColumnReader<D, false> zr;
+  typedef TileStage<D, NT> Stage;
+  Stage sy, sz;
+  const uint32_t src = Stage::source(stride);
+  const int dst = Stage::target();
+  const int ybase = column_base<D>(4 * (lane & 3), lane), zbase = column_base<D>(16 * wave + 4 * (lane & 3), lane);
+  f32x4 s[NT];
 #pragma unroll
-  for (int t = 0; t < NW; ++t) yr[t].init(32 * t, lane);
-  zr.init(32 * wave, lane);
-  f32x16 s[NW];
-#pragma unroll
-  for (int t = 0; t < NW; ++t)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) s[t][i] = 0.f;
+  for (int t = 0; t < NT; ++t) s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  int row_n = -1;
   const int chunks = (bl.len + C - 1) / C;
+  auto fetch = [&](int ci, int h) {
+    const int c = REV ? chunks - 1 - ci : ci, n = min(C, bl.len - c * C);
+    const int64_t at = c * C * stride + h * D;
+    sy.fetch(y + at, src, n, stride);
+    sz.fetch(z + at, src, n, stride);
+  };
+  fetch(0, 0);
+  int row_n = -1;
   for (int ci = 0; ci < chunks; ++ci) {
     const int c = REV ? chunks - 1 - ci : ci, n = min(C, bl.len - c * C);
-    const float fade = exp2f(lg * (float)n);
-#pragma unroll
-    for (int t = 0; t < NW; ++t)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[t][i] *= fade;
+    scale_state<NT>(s, exp2f(lg * (float)n));
     for (int h = 0; h < gy; ++h) {
       __syncthreads();
+      sy.put(yt, dst);
+      sz.put(zt, dst);
       if (n != row_n) set_row_decays<REV>(decays, lg, n), row_n = n;
-      copy.issue_at(yt, y + c * C * stride + h * D, n, stride);
-      copy.issue_at(zt, z + c * C * stride + h * D, n, stride);
-      wait_vmem();
       __syncthreads();
-      update_state<D, TERMS>(s, yt, zt, yr, zr, decays.row, hf);
+      if (h + 1 < gy) fetch(ci, h + 1);
+      else if (ci + 1 < chunks) fetch(ci + 1, 0);
+      const bf16x8 zf[2] = {read_columns<D>(zt, zbase, 0, 0), read_columns<D>(zt, zbase, 0, 1)};
+      update_state<D, false, TERMS>(s, yt, zf, ybase, decays.row, q);
     }
   }
-  float* out = p.states + ((int64_t)block * p.b.heads_kv + kvh) * D * D + 32 * wave + (lane & 31);
+  float* out = p.states + ((int64_t)block * p.b.heads_kv + kvh) * D * D + 16 * wave + (lane & 15);
 #pragma unroll
-  for (int t = 0; t < NW; ++t)
+  for (int t = 0; t < NT; ++t)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) out[state_row(t, i, hf) * D] = s[t][i];
+    for (int i = 0; i < 4; ++i) out[state_row<false>(t, q, i) * D] = s[t][i];
 }
 
 // ---------------------------------------------------------------------------- scan
@@ -215,8 +330,7 @@ __global__ __launch_bounds__(256) void lin_scan_kernel(LinScanParams p, int prom
   const int slices = elems / 1024;
   const int unit = blockIdx.x / slices, slice = blockIdx.x - unit * slices;
   const int seg_i = unit / p.b.heads_kv, kvh = unit - seg_i * p.b.heads_kv;
-  const LinSeg* segs = segments(p.b);
-  const LinSeg sg = segs[prompts ? seg_i : p.b.num_trees + seg_i];
+  const LinSeg sg = load_segment(p.b, prompts ? seg_i : p.b.num_trees + seg_i);
   const float lg = p.b.log2_decay[kvh];
   const int64_t per = (int64_t)p.b.heads_kv * elems;                        // one block's (tree's) states
   const int64_t at = (int64_t)kvh * elems + slice * 1024 + threadIdx.x * 4;  // this thread's four elements of them
@@ -228,7 +342,7 @@ __global__ __launch_bounds__(256) void lin_scan_kernel(LinScanParams p, int prom
     if (!prompts) carry = ld(p.tree, sg.link);
     else if (p.init) carry = ld(p.init, seg_i);
   } else if (prompts) {
-    const int b1 = seg_i + 1 < p.b.num_trees ? segs[seg_i + 1].link : p.b.num_branches;
+    const int b1 = seg_i + 1 < p.b.num_trees ? load_segment(p.b, seg_i + 1).link : p.b.num_branches;
     for (int b = sg.link; b < b1; ++b) carry += ld(p.tree, b);
   }
   const int count = (sg.len + sg.rows - 1) / sg.rows;
@@ -260,194 +374,288 @@ __global__ __launch_bounds__(256) void lin_scan_kernel(LinScanParams p, int prom
 
 // ---------------------------------------------------------------------------- outputs
 
-// Forward: x and out have `group` heads for each head of y and z. Reverse: y
-// and z have, and their terms are summed.
+// The product of one block and KV head (see the top of the file). Forward: x
+// and out have `group` heads for each head of y and z. Reverse: y and z have,
+// and their terms are summed.
+struct Product {
+  const uint16_t *x, *y, *z;
+  uint16_t* out;
+  const float* state;  // of the block and KV head
+};
+
+template <int D>
+struct OutShared {
+  __attribute__((aligned(1024))) __bf16 xt[C * D];
+  __attribute__((aligned(1024))) __bf16 yt[C * D];
+  __attribute__((aligned(1024))) __bf16 zt[C * D];
+  __attribute__((aligned(1024))) __bf16 pt[2][C * C];  // P as two bf16 terms, rows x, columns y, swizzled
+  Decays decays;
+};
+
+// Rows 16 tx + l16 (< n) of a chunk, 4 columns from 4 q on, from `out` on. The
+// buffer's range ends behind row n - 1, so later rows are not written.
+template <int D>
+__device__ __forceinline__ void store_rows(uint16_t* out, const f32x4* acc, float scale, int n, int64_t stride, int l16,
+                                           int q) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)out, 0, (int)(2 * n * stride), 0x00020000);
+  const uint32_t at = 2 * (uint32_t)(l16 * stride) + 8 * q;
+#pragma unroll
+  for (int tx = 0; tx < 4; ++tx) {
+    const u32x2 w = {bf16_pair(acc[tx][0] * scale, acc[tx][1] * scale),
+                     bf16_pair(acc[tx][2] * scale, acc[tx][3] * scale)};
+    __builtin_amdgcn_raw_buffer_store_b64(w, rsrc, at + tx * (uint32_t)(32 * stride), 0, 0);
+  }
+#endif
+}
+
 template <int D, bool REV, bool TS>
-__global__ __launch_bounds__(2 * D, 2) void lin_out_kernel(LinOutParams p) {
-  constexpr int NW = D / 32;
-  __shared__ __attribute__((aligned(1024))) __bf16 xt[C * D];
-  __shared__ __attribute__((aligned(1024))) __bf16 yt[C * D];
-  __shared__ __attribute__((aligned(1024))) __bf16 zt[C * D];
-  __shared__ __attribute__((aligned(1024))) __bf16 pt[C * C];
-  __shared__ __attribute__((aligned(16))) Decays decays;
-  const int block = blockIdx.x / p.b.heads_kv, kvh = blockIdx.x - block * p.b.heads_kv;
-  const Block bl = find_block(p.b, block);
+__device__ __forceinline__ void lin_out(OutShared<D>& sh, const LinBatch& batch, float scale, const Block& bl, int kvh,
+                                        const Product& pr) {
+  constexpr int NT = D / 16;  // tiles of the state's rows, and wavefronts
+  constexpr bool PAIRED = !REV;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int hf = lane >> 5, l32 = lane & 31;
-  const float lg = p.b.log2_decay[kvh];
-  const int side = bl.prompt ? 0 : 1, g = p.b.group;
-  const int64_t stride_q = (int64_t)p.b.heads_kv * g * D, stride_kv = (int64_t)p.b.heads_kv * D;
+  const int q = lane >> 4, l16 = lane & 15;
+  const float lg = batch.log2_decay[kvh];
+  const int g = batch.group;
+  const int64_t stride_q = (int64_t)batch.heads_kv * g * D, stride_kv = (int64_t)batch.heads_kv * D;
   const int64_t stride_x = REV ? stride_kv : stride_q, stride_y = REV ? stride_q : stride_kv;
   const int64_t off_x = bl.row0 * stride_x + (int64_t)kvh * (REV ? 1 : g) * D;
   const int64_t off_y = bl.row0 * stride_y + (int64_t)kvh * (REV ? g : 1) * D;
-  const uint16_t* x = p.x[side] + off_x;
-  const uint16_t* y = p.y[side] + off_y;
-  const uint16_t* z = p.z[side] + off_y;
-  uint16_t* out = p.out[side] + off_x;
-  TileCopy<C, D, NW> copy_x, copy_y;
-  copy_x.init(stride_x);
-  copy_y.init(stride_y);
-  ColumnReader<D, true> yr[NW];
-  ColumnReader<D, false> zr;
-#pragma unroll
-  for (int t = 0; t < NW; ++t) yr[t].init(32 * t, lane);
-  zr.init(32 * wave, lane);
-  RowOffsets<D> rows;  // of the chunk's first 32 rows; the other 32 lie 64 D bytes further on (same swizzle)
-  rows.init(l32, hf);
-  auto row8 = [&](const __bf16* tile, int half, int ks) { return lds_row8_at<D>(tile + half * 32 * D, rows.o[ks]); };
-  set_pair_decays(decays, lg);
+  const uint16_t* const x = pr.x + off_x;
+  const uint16_t* const y = pr.y + off_y;
+  const uint16_t* const z = pr.z + off_y;
+  uint16_t* const out = pr.out + off_x;
+  typedef TileStage<D, NT> Stage;
+  Stage s0, s1;  // forward: x; reverse: y and z
+  const uint32_t src_x = Stage::source(stride_x), src_y = Stage::source(stride_y);
+  const int dst = Stage::target();
+
+  const int chunks = (bl.len + C - 1) / C;
+  auto chunk_of = [&](int ci) { return REV ? chunks - 1 - ci : ci; };
+  auto rows_of = [&](int c) { return min(C, bl.len - c * C); };
+  auto fetch_x = [&](Stage& a, int ci, int h) {
+    const int c = chunk_of(ci);
+    a.fetch(x + c * C * stride_x + h * D, src_x, rows_of(c), stride_x);
+  };
+  auto fetch_yz = [&](Stage& a, Stage& b, int ci, int h) {
+    const int c = chunk_of(ci);
+    a.fetch(y + c * C * stride_y + h * D, src_y, rows_of(c), stride_y);
+    b.fetch(z + c * C * stride_y + h * D, src_y, rows_of(c), stride_y);
+  };
+  if (REV) fetch_yz(s0, s1, 0, 0);
+  else fetch_x(s0, 0, 0);
+
+  const int ybase = column_base<D>(state_row<PAIRED>(0, lane & 3, 0), lane);
+  const int zbase = column_base<D>(16 * wave + 4 * (lane & 3), lane);
+  set_pair_decays(sh.decays, lg);
+  // P is written where it is not masked; the 16 x 16 tiles beside the diagonal that are read with it stay zero
+  for (int i = threadIdx.x; i < 2 * C * C / 8; i += 4 * D) reinterpret_cast<raw16*>(sh.pt)[i] = raw16{0u, 0u, 0u, 0u};
 
   // the state that reaches the block
-  f32x16 s[NW];
+  f32x4 s[NT];
   {
-    const float* st = p.states + ((int64_t)block * p.b.heads_kv + kvh) * D * D;
-    const int col = 32 * wave + l32;
+    const int col = 16 * wave + l16;
 #pragma unroll
-    for (int t = 0; t < NW; ++t)
+    for (int t = 0; t < NT; ++t) {
+      if (TS) {
+        s[t] = *reinterpret_cast<const f32x4*>(pr.state + col * D + state_row<PAIRED>(t, q, 0));
+      } else {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int r = state_row(t, i, hf);
-        s[t][i] = TS ? st[col * D + r] : st[r * D + col];
+        for (int i = 0; i < 4; ++i) s[t][i] = pr.state[state_row<PAIRED>(t, q, i) * D + col];
       }
+    }
   }
 
-  // Tiles of P^T, [32 y] x [32 x]: the diagonal ones and the one off it. With
-  // four wavefronts 0, 1 and 2 take one each, with two wavefront 0 both
-  // diagonal ones.
-  const bool diag = NW == 4 ? wave != 1 : wave == 0;
-  const float* const pw = decays.pair + 32 + (REV ? 4 * hf - l32 : l32 - 4 * hf) + (diag ? 0 : 32);
+  // Byte offsets of this lane's row among a tile's first 16 (16 rows further on: + 32 D, the swizzle's period), from
+  // column 8 q on; k step ks flips 64 ks.
+  const int rbase = 2 * loff<D>(l16, 8 * q);
+  auto read8 = [&](const __bf16* tile, int base, int rt, int ks) {
+    return *reinterpret_cast<const bf16x8*>(reinterpret_cast<const char*>(tile) + rt * 32 * D + (base ^ (64 * ks)));
+  };
+  // x in the order of the state's rows
+  const int xbase = PAIRED ? rbase : 2 * loff<D>(l16, 4 * q);
+  auto read_x = [&](int base, int rt, int ks) {
+    if (PAIRED) return read8(sh.xt, base, rt, ks);
+    const char* t = reinterpret_cast<const char*>(sh.xt) + rt * 32 * D;
+    bf16x8 r;
+    __builtin_memcpy(&r, t + (base ^ (64 * ks)), 8);
+    __builtin_memcpy(reinterpret_cast<char*>(&r) + 8, t + (base ^ (64 * ks + 32)), 8);
+    return r;
+  };
+
+  // Tile (ty, tx) of P^T, [16 y] x [16 x], a lane having one x and four y.
   auto p_tile = [&](int ty, int tx) {
-    f32x16 acc;
+    f32x4 a = {0.f, 0.f, 0.f, 0.f};
+    const int rb = here(rbase);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) acc[i] = 0.f;
+    for (int ks = 0; ks < D / 32; ++ks) a = mfma16(read8(sh.yt, rb, ty, ks), read8(sh.xt, rb, tx, ks), a);
+    const float* const pw = sh.decays.pair + 16 + (REV ? 16 * (ty - tx) + 4 * q - l16 : 16 * (tx - ty) + l16 - 4 * q);
+    u32x2 v, u;
 #pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks)
-      acc = mfma32(row8(yt, ty, ks), row8(xt, tx, ks), acc);
-#pragma unroll
-    for (int qd = 0; qd < 4; ++qd) {
-      typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-      bf16x4 v;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = (__bf16)(acc[4 * qd + e] * pw[REV ? 8 * qd + e : -8 * qd - e]);
-      // k step 2 ty + qd / 2, in the order of the transposed z: chunk 2 m + hf, half qd % 2
-      *reinterpret_cast<bf16x4*>(pt + toff<64>(32 * tx + l32, 8 * (2 * (2 * ty + (qd >> 1)) + hf)) + 4 * (qd & 1)) = v;
+    for (int e = 0; e < 2; ++e) {
+      const float f0 = a[2 * e] * pw[REV ? 2 * e : -2 * e], f1 = a[2 * e + 1] * pw[REV ? 2 * e + 1 : -2 * e - 1];
+      v[e] = bf16_pair(f0, f1);
+      u[e] = bf16_pair(f0 - __uint_as_float(v[e] << 16), f1 - __uint_as_float(v[e] & 0xffff0000u));
+    }
+    const int o = loff<C>(16 * tx + l16, 16 * ty + 4 * q);
+    *reinterpret_cast<u32x2*>(sh.pt[0] + o) = v;
+    *reinterpret_cast<u32x2*>(sh.pt[1] + o) = u;
+  };
+  // the 10 tiles on and beside the diagonal, dealt to the wavefronts: tile k is
+  // (i, j), j <= i, with i (i + 1) / 2 + j = k
+  auto p_tiles = [&]() {
+    for (int k = wave; k < 10; k += NT) {
+      const int i = (k >= 1) + (k >= 3) + (k >= 6), j = k - i * (i + 1) / 2;
+      if (REV) p_tile(i, j);
+      else p_tile(j, i);
     }
   };
-  int prow[2];
-#pragma unroll
-  for (int tx = 0; tx < 2; ++tx) prow[tx] = 32 * tx + l32;
 
-  int row_n = -1;
-  f32x16 acc[2];
-  const int chunks = (bl.len + C - 1) / C;
-  for (int ci = 0; ci < chunks; ++ci) {
-    const int c = REV ? chunks - 1 - ci : ci, n = min(C, bl.len - c * C);
-    const float fade = exp2f(lg * (float)n);
-    // the state as an operand (forward: of all heads; reverse: once, where it is used)
-    bf16x8 hi[NW][2], lo[NW][2];
-    auto split_state = [&](int t, int k) {
+  const int pbase = 2 * loff<C>(l16, 8 * q);
+
+  f32x4 acc[4];
+  // acc = out^T [z, x] of what reaches the chunk: S^T X^T, the state as two bf16 terms, and its decay to each row
+  auto from_state = [&](int n) {
+    const int xb = here(xbase);
+#pragma unroll
+    for (int tx = 0; tx < 4; ++tx) acc[tx] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int ks = 0; ks < D / 32; ++ks) {
       float f[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) f[e] = s[t][8 * k + e];
-      split2(f, hi[t][k], lo[t][k]);
-    };
-    if (!REV) {
+      for (int e = 0; e < 8; ++e) f[e] = s[2 * ks + (e >> 2)][e & 3];
+      bf16x8 hi, lo, xv[4];
+      split2(f, hi, lo);
 #pragma unroll
-      for (int t = 0; t < NW; ++t)
+      for (int tx = 0; tx < 4; ++tx) xv[tx] = read_x(xb, tx, ks);
 #pragma unroll
-        for (int k = 0; k < 2; ++k) split_state(t, k);
+      for (int tx = 0; tx < 4; ++tx) acc[tx] = mfma16(hi, xv[tx], acc[tx]);
+#pragma unroll
+      for (int tx = 0; tx < 4; ++tx) acc[tx] = mfma16(lo, xv[tx], acc[tx]);
+      __builtin_amdgcn_sched_barrier(0);
     }
-    for (int h = 0; h < g; ++h) {
-      __syncthreads();
-      if (n != row_n) set_row_decays<REV>(decays, lg, n), row_n = n;
-      if (!REV || h == 0) copy_x.issue_at(xt, x + c * C * stride_x + (REV ? 0 : h) * D, n, stride_x);
-      if (REV || h == 0) {
-        copy_y.issue_at(yt, y + c * C * stride_y + (REV ? h : 0) * D, n, stride_y);
-        copy_y.issue_at(zt, z + c * C * stride_y + (REV ? h : 0) * D, n, stride_y);
-      }
-      wait_vmem();
-      __syncthreads();
-      if constexpr (NW == 4) {
-        if (wave == 0) p_tile(0, 0);
-        else if (wave == 1) p_tile(REV ? 1 : 0, REV ? 0 : 1);
-        else if (wave == 2) p_tile(1, 1);
-      } else {
-        if (wave == 0) p_tile(0, 0), p_tile(1, 1);
-        else p_tile(REV ? 1 : 0, REV ? 0 : 1);
-      }
-      if (!REV || h == 0) {
-        // out^T [z, x] = S^T X^T
 #pragma unroll
-        for (int tx = 0; tx < 2; ++tx)
+    for (int tx = 0; tx < 4; ++tx) {
+      const int r = 16 * tx + l16;
+      acc[tx] *= exp2f(lg * (float)(REV ? max(n - r, 0) : r + 1));
+    }
+  };
+  // acc += Z^T P^T
+  auto from_chunk = [&](const bf16x8* zf) {
+    const int pb = here(pbase);
 #pragma unroll
-          for (int i = 0; i < 16; ++i) acc[tx][i] = 0.f;
+    for (int k = 0; k < 2; ++k)
 #pragma unroll
-        for (int t = 0; t < NW; ++t)
+      for (int m = 0; m < 2; ++m)
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            if (REV) split_state(t, k);
-#pragma unroll
-            for (int tx = 0; tx < 2; ++tx) {
-              const bf16x8 xv = row8(xt, tx, 2 * t + k);
-              acc[tx] = mfma32(hi[t][k], xv, acc[tx]);
-              acc[tx] = mfma32(lo[t][k], xv, acc[tx]);
-            }
-          }
-#pragma unroll
-        for (int tx = 0; tx < 2; ++tx) {
-          const int r = 32 * tx + l32;
-          const float lead = exp2f(lg * (float)(REV ? max(n - r, 0) : r + 1));
-#pragma unroll
-          for (int i = 0; i < 16; ++i) acc[tx][i] *= lead;
+        for (int tx = 0; tx < 4; ++tx) {
+          if (REV ? m < (tx >> 1) : m > (tx >> 1)) continue;  // masked
+          const char* t = reinterpret_cast<const char*>(sh.pt[k]) + tx * 32 * C;
+          acc[tx] = mfma16(zf[m], *reinterpret_cast<const bf16x8*>(t + (pb ^ (64 * m))), acc[tx]);
         }
-      }
-      if (REV && h == 0) {
-#pragma unroll
-        for (int t = 0; t < NW; ++t)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) s[t][i] *= fade;
-      }
+  };
+  auto store = [&](int c, int h, int n) {
+    store_rows<D>(out + c * C * stride_x + h * D + 16 * wave, acc, scale, n, stride_x, l16, q);
+  };
+
+  int row_n = -1;
+  for (int ci = 0; ci < chunks; ++ci) {
+    const int c = chunk_of(ci), n = rows_of(c);
+    const bool more = ci + 1 < chunks;
+    const float fade = exp2f(lg * (float)n);
+    // x of the first head (reverse: y and z) is on its way already; what only a chunk's first head brings is not fetched
+    // ahead, that would take too many registers
+    if constexpr (REV) {
+      Stage a;
+      fetch_x(a, ci, 0);
       __syncthreads();
-      // out^T += Z^T P^T
-#pragma unroll
-      for (int m = 0; m < 4; ++m) {
-        const bf16x8 zv = zr.read(zt, m);
-#pragma unroll
-        for (int tx = 0; tx < 2; ++tx)
-          if (REV ? (tx == 0 || m >= 2) : (tx == 1 || m < 2))
-            acc[tx] = mfma32(zv, *reinterpret_cast<const bf16x8*>(pt + toff<64>(prow[tx], 8 * (2 * m + hf))), acc[tx]);
+      a.put(sh.xt, dst);
+      if (n != row_n) set_row_decays<REV>(sh.decays, lg, n), row_n = n;
+      __syncthreads();
+      from_state(n);
+      scale_state<NT>(s, fade);
+      for (int h = 0; h < g; ++h) {
+        if (h > 0) __syncthreads();  // the tiles of the head before have been read
+        s0.put(sh.yt, dst);
+        s1.put(sh.zt, dst);
+        __syncthreads();
+        if (h + 1 < g) fetch_yz(s0, s1, ci, h + 1);
+        else if (more) fetch_yz(s0, s1, ci + 1, 0);
+        const bf16x8 zf[2] = {read_columns<D>(sh.zt, zbase, 0, 0), read_columns<D>(sh.zt, zbase, 0, 1)};
+        p_tiles();
+        __syncthreads();
+        from_chunk(zf);
+        update_state<D, PAIRED, 2>(s, sh.yt, zf, ybase, sh.decays.row, q);
       }
-      if (REV) update_state<D, 2>(s, yt, zt, yr, zr, decays.row, hf);
-      if (!REV || h == g - 1) {
-        uint16_t* const o = out + c * C * stride_x + (REV ? 0 : h) * D + 32 * wave + 8 * hf;
+      store(c, 0, n);
+    } else {
+      {
+        Stage a, b;
+        fetch_yz(a, b, ci, 0);
+        __syncthreads();
+        a.put(sh.yt, dst);
+        b.put(sh.zt, dst);
+        if (n != row_n) set_row_decays<REV>(sh.decays, lg, n), row_n = n;
+      }
+      bf16x8 zf[2];
+      for (int h = 0; h < g; ++h) {
+        if (h > 0) __syncthreads();
+        s0.put(sh.xt, dst);
+        __syncthreads();
+        if (h + 1 < g) fetch_x(s0, ci, h + 1);
+        else if (more) fetch_x(s0, ci + 1, 0);
+        if (h == 0) zf[0] = read_columns<D>(sh.zt, zbase, 0, 0), zf[1] = read_columns<D>(sh.zt, zbase, 0, 1);
+        p_tiles();
+        // (the state's two terms are formed again for every head: kept over the loop they take registers, which then
+        // spill. The empty asm keeps the compiler from doing that.)
 #pragma unroll
-        for (int tx = 0; tx < 2; ++tx) {
-          uint32_t d[8];  // registers 2i, 2i + 1 as bf16
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-            const bf16x2 v = {(__bf16)(acc[tx][2 * i] * p.scale), (__bf16)(acc[tx][2 * i + 1] * p.scale)};
-            __builtin_memcpy(&d[i], &v, 4);
-          }
-          const int r = 32 * tx + l32;
-#pragma unroll
-          for (int pr = 0; pr < 2; ++pr) {
-            // the half-waves exchange four columns: each then has eight consecutive ones
-            const auto e0 = __builtin_amdgcn_permlane32_swap(d[4 * pr], d[4 * pr + 2], false, false);
-            const auto e1 = __builtin_amdgcn_permlane32_swap(d[4 * pr + 1], d[4 * pr + 3], false, false);
-            const raw16 v = {e0[0], e1[0], e0[1], e1[1]};
-            if (r < n) *reinterpret_cast<raw16*>(o + r * stride_x + 16 * pr) = v;
-          }
-        }
+        for (int t = 0; t < NT; ++t) asm volatile("" : "+v"(s[t]));
+        from_state(n);
+        __syncthreads();
+        from_chunk(zf);
+        store(c, h, n);
+      }
+      if (more) {
+        scale_state<NT>(s, fade);
+        update_state<D, PAIRED, 2>(s, sh.yt, zf, ybase, sh.decays.row, q);
       }
     }
-    if (!REV && ci + 1 < chunks) {
-#pragma unroll
-      for (int t = 0; t < NW; ++t)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[t][i] *= fade;
-      update_state<D, 2>(s, yt, zt, yr, zr, decays.row, hf);
-    }
+  }
+}
+
+template <int D>
+__global__ __launch_bounds__(4 * D, 4) void lin_out_kernel(LinOutParams p) {
+  __shared__ OutShared<D> sh;
+  const int block = blockIdx.x / p.b.heads_kv, kvh = blockIdx.x - block * p.b.heads_kv;
+  const Block bl = find_block(p.b, block);
+  const int side = bl.prompt ? 0 : 1;
+  const float* state = p.states + ((int64_t)block * p.b.heads_kv + kvh) * D * D;
+  const Product pr = {p.q[side], p.k[side], p.v[side], p.o[side], state};
+  lin_out<D, false, false>(sh, p.b, p.scale, bl, kvh, pr);
+}
+
+// dq, dv and dk: three workgroups a block and KV head, one after the other on
+// one XCD (workgroups go to the 8 XCDs in turn), so that what they share of q,
+// k, v and do comes from memory once.
+template <int D>
+__global__ __launch_bounds__(4 * D, 4) void lin_grad_kernel(LinGradParams p) {
+  __shared__ OutShared<D> sh;
+  const int j = blockIdx.x >> 3, unit = (j / 3) * 8 + (blockIdx.x & 7), role = j % 3;
+  if (unit >= p.b.num_blocks * p.b.heads_kv) return;
+  const int block = unit / p.b.heads_kv, kvh = unit - block * p.b.heads_kv;
+  const Block bl = find_block(p.b, block);
+  const int side = bl.prompt ? 0 : 1;
+  const int64_t at = ((int64_t)block * p.b.heads_kv + kvh) * D * D;
+  if (role == 0) {
+    const Product pr = {p.dout[side], p.v[side], p.k[side], p.dq[side], p.states + at};
+    lin_out<D, false, true>(sh, p.b, p.scale, bl, kvh, pr);
+  } else if (role == 1) {
+    const Product pr = {p.k[side], p.q[side], p.dout[side], p.dv[side], p.states_rev + at};
+    lin_out<D, true, false>(sh, p.b, p.scale, bl, kvh, pr);
+  } else {
+    const Product pr = {p.v[side], p.dout[side], p.q[side], p.dk[side], p.states_rev + at};
+    lin_out<D, true, true>(sh, p.b, p.scale, bl, kvh, pr);
   }
 }
 
@@ -465,13 +673,13 @@ hipError_t launch_lin_table(const LinTable& t, hipStream_t stream) {
 hipError_t launch_lin_state(const LinStateParams& p, int head_dim, bool reverse, bool exact, hipStream_t stream) {
   const dim3 grid(p.b.num_blocks * p.b.heads_kv);
   if (head_dim == 128) {
-    if (reverse) lin_state_kernel<128, true, 2><<<grid, 256, 0, stream>>>(p);
-    else if (exact) lin_state_kernel<128, false, 3><<<grid, 256, 0, stream>>>(p);
-    else lin_state_kernel<128, false, 2><<<grid, 256, 0, stream>>>(p);
+    if (reverse) lin_state_kernel<128, true, 2><<<grid, 512, 0, stream>>>(p);
+    else if (exact) lin_state_kernel<128, false, 3><<<grid, 512, 0, stream>>>(p);
+    else lin_state_kernel<128, false, 2><<<grid, 512, 0, stream>>>(p);
   } else {
-    if (reverse) lin_state_kernel<64, true, 2><<<grid, 128, 0, stream>>>(p);
-    else if (exact) lin_state_kernel<64, false, 3><<<grid, 128, 0, stream>>>(p);
-    else lin_state_kernel<64, false, 2><<<grid, 128, 0, stream>>>(p);
+    if (reverse) lin_state_kernel<64, true, 2><<<grid, 256, 0, stream>>>(p);
+    else if (exact) lin_state_kernel<64, false, 3><<<grid, 256, 0, stream>>>(p);
+    else lin_state_kernel<64, false, 2><<<grid, 256, 0, stream>>>(p);
   }
   return hipGetLastError();
 }
@@ -484,19 +692,17 @@ hipError_t launch_lin_scan(const LinScanParams& p, int head_dim, bool reverse, b
   return hipGetLastError();
 }
 
-hipError_t launch_lin_out(const LinOutParams& p, int head_dim, bool reverse, bool transposed, hipStream_t stream) {
+hipError_t launch_lin_out(const LinOutParams& p, int head_dim, hipStream_t stream) {
   const dim3 grid(p.b.num_blocks * p.b.heads_kv);
-  if (head_dim == 128) {
-    if (!reverse && !transposed) lin_out_kernel<128, false, false><<<grid, 256, 0, stream>>>(p);
-    else if (!reverse) lin_out_kernel<128, false, true><<<grid, 256, 0, stream>>>(p);
-    else if (!transposed) lin_out_kernel<128, true, false><<<grid, 256, 0, stream>>>(p);
-    else lin_out_kernel<128, true, true><<<grid, 256, 0, stream>>>(p);
-  } else {
-    if (!reverse && !transposed) lin_out_kernel<64, false, false><<<grid, 128, 0, stream>>>(p);
-    else if (!reverse) lin_out_kernel<64, false, true><<<grid, 128, 0, stream>>>(p);
-    else if (!transposed) lin_out_kernel<64, true, false><<<grid, 128, 0, stream>>>(p);
-    else lin_out_kernel<64, true, true><<<grid, 128, 0, stream>>>(p);
-  }
+  if (head_dim == 128) lin_out_kernel<128><<<grid, 512, 0, stream>>>(p);
+  else lin_out_kernel<64><<<grid, 256, 0, stream>>>(p);
+  return hipGetLastError();
+}
+
+hipError_t launch_lin_grad(const LinGradParams& p, int head_dim, hipStream_t stream) {
+  const dim3 grid((p.b.num_blocks * p.b.heads_kv + 7) / 8 * 24);
+  if (head_dim == 128) lin_grad_kernel<128><<<grid, 512, 0, stream>>>(p);
+  else lin_grad_kernel<64><<<grid, 256, 0, stream>>>(p);
   return hipGetLastError();
 }
 
