@@ -408,12 +408,16 @@ int augtree_linear_fwd(const augtree_groups* grp, const float* decay, const uint
  * Backward: gradients of the outputs' loss for q, k and v (none for `state`
  * or through state_p / state_r). In: as forward, do_p, do_r bf16 like o_p, o_r;
  * the outputs are not read. Out: dq like q, dk, dv like k, bf16.
+ * fwd_ws (nullable): the workspace of the augtree_linear_fwd call of the same
+ * batch, decay, k, v and state, not written since. The states it holds are then
+ * used instead of being formed again; the results are the same bits.
  */
 int augtree_linear_bwd(const augtree_groups* grp, const float* decay, const uint16_t* q_p,
                        const uint16_t* k_p, const uint16_t* v_p, const uint16_t* do_p, const uint16_t* q_r,
                        const uint16_t* k_r, const uint16_t* v_r, const uint16_t* do_r, const float* state,
                        uint16_t* dq_p, uint16_t* dk_p, uint16_t* dv_p, uint16_t* dq_r, uint16_t* dk_r,
-                       uint16_t* dv_r, void* ws, size_t ws_bytes, void* stream);
+                       uint16_t* dv_r, const void* fwd_ws, size_t fwd_ws_bytes, void* ws, size_t ws_bytes,
+                       void* stream);
 
 /*
  * One token of each of `rows` sequences:
@@ -466,9 +470,9 @@ size_t augtree_head_norm_workspace_size(int64_t rows, int32_t heads, int32_t hea
  * static role name ("fwd_prefill", "fwd_replay", "fwd_tree", "fwd_replay_split",
  * "lse_merge", "dq_prefill", "dkv_prefill", "dq_replay", "dkv_replay", "dq_tree",
  * "dkv_tree", "grad_reduce", "reduce_tree", "linear_table", "linear_state",
- * "linear_state_rev", "linear_scan", "linear_scan_rev", "linear_out", "linear_dq",
- * "linear_dv", "linear_dk", "linear_step", "head_norm", "head_norm_bwd") and the
- * stream the kernel is enqueued on, so that a caller can record HIP events around single
+ * "linear_state_rev", "linear_scan", "linear_scan_rev", "linear_out", "linear_grad",
+ * "linear_step", "head_norm", "head_norm_bwd") and the stream the kernel is
+ * enqueued on, so that a caller can record HIP events around single
  * kernels. The hook must not call back into the library. NULL removes it.
  * Per thread; the library keeps no other state.
  */

@@ -102,7 +102,7 @@ def _sig(lib):
         "augtree_tree_chunk_blocks": (_I32, []),
         "augtree_linear_workspace_size": (_SZ, [_GP, ctypes.c_int]),
         "augtree_linear_fwd": (ctypes.c_int, [_GP] + [_P] * 12 + [_P, _SZ, _P]),
-        "augtree_linear_bwd": (ctypes.c_int, [_GP] + [_P] * 16 + [_P, _SZ, _P]),
+        "augtree_linear_bwd": (ctypes.c_int, [_GP] + [_P] * 16 + [_P, _SZ, _P, _SZ, _P]),
         "augtree_linear_step": (ctypes.c_int, [_I32, _I32, _I32, _I32, _F32, _P, _P, _P, _P, _I32] + [_P] * 5),
         "augtree_head_norm_fwd": (ctypes.c_int, [_I64, _I32, _I32, ctypes.c_int, _F32] + [_P] * 6),
         "augtree_head_norm_bwd": (ctypes.c_int, [_I64, _I32, _I32, ctypes.c_int, _F32] + [_P] * 9 + [_P, _SZ, _P]),

@@ -398,13 +398,14 @@ def linear_fwd(b: GroupBatch, decay, q_p, k_p, v_p, q_r, k_r, v_r, state=None, o
 
 
 def linear_bwd(b: GroupBatch, decay, q_p, k_p, v_p, do_p, q_r, k_r, v_r, do_r, state=None, dq_p=None, dk_p=None,
-               dv_p=None, dq_r=None, dk_r=None, dv_r=None, ws=None, stream=None):
-    """Gradients of linear_fwd's outputs (augtree_linear_bwd). Returns (dq_p, dk_p, dv_p, dq_r, dk_r, dv_r)."""
+               dv_p=None, dq_r=None, dk_r=None, dv_r=None, fwd_ws=None, ws=None, stream=None):
+    """Gradients of linear_fwd's outputs (augtree_linear_bwd). `fwd_ws`: the workspace that linear_fwd was given for the
+    same inputs, not written since (saves forming its states again). Returns (dq_p, dk_p, dv_p, dq_r, dk_r, dv_r)."""
     dec = _decay(decay, b.hkv)
     named = (("q_p", q_p), ("k_p", k_p), ("v_p", v_p), ("do_p", do_p), ("q_r", q_r), ("k_r", k_r), ("v_r", v_r),
              ("do_r", do_r))
     on = _On(named + (("state", state), ("dq_p", dq_p), ("dk_p", dk_p), ("dv_p", dv_p), ("dq_r", dq_r),
-                      ("dk_r", dk_r), ("dv_r", dv_r), ("ws", ws)), stream)
+                      ("dk_r", dk_r), ("dv_r", dv_r), ("fwd_ws", fwd_ws), ("ws", ws)), stream)
     _linear_inputs(b, named)
     dev = on.device
     if state is not None:
@@ -416,8 +417,9 @@ def linear_bwd(b: GroupBatch, decay, q_p, k_p, v_p, do_p, q_r, k_r, v_r, do_r, s
         ws = _linear_ws(b, True, ws, dev)
         _lib.check(_lib.load().augtree_linear_bwd(
             b.ref, dec.ctypes.data_as(ctypes.c_void_p), _ptr(q_p), _ptr(k_p), _ptr(v_p), _ptr(do_p), _ptr(q_r),
-            _ptr(k_r), _ptr(v_r), _ptr(do_r), _ptr(state), *(_ptr(t) for t in outs), _ptr(ws),
-            ctypes.c_size_t(ws.numel()), st), "linear_bwd")
+            _ptr(k_r), _ptr(v_r), _ptr(do_r), _ptr(state), *(_ptr(t) for t in outs), _ptr(fwd_ws),
+            ctypes.c_size_t(0 if fwd_ws is None else fwd_ws.numel()), _ptr(ws), ctypes.c_size_t(ws.numel()), st),
+            "linear_bwd")
     return tuple(outs)
 
 

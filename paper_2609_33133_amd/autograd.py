@@ -83,9 +83,10 @@ class _GroupLinearAttention(torch.autograd.Function):
                               (q_r, "q_r", b.tr, b.hq), (k_r, "k_r", b.tr, b.hkv), (v_r, "v_r", b.tr, b.hkv)):
             _check(t, n, rows, h, b.d)
         q_p, k_p, v_p, q_r, k_r, v_r = (t.contiguous() for t in (q_p, k_p, v_p, q_r, k_r, v_r))
+        ws = torch.empty(api.linear_workspace_size(b), dtype=torch.uint8, device=q_p.device)
         o_p, o_r, state_p, state_r = api.linear_fwd(b, decay, q_p, k_p, v_p, q_r, k_r, v_r, state=state,
-                                                    want_states=return_state)
-        ctx.save_for_backward(q_p, k_p, v_p, q_r, k_r, v_r, state)
+                                                    want_states=return_state, ws=ws)
+        ctx.save_for_backward(q_p, k_p, v_p, q_r, k_r, v_r, state, ws)  # the states in ws serve the backward too
         ctx.batch, ctx.decay = b, decay
         if not return_state:
             return o_p, o_r
@@ -94,11 +95,11 @@ class _GroupLinearAttention(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, do_p, do_r, *_):
-        q_p, k_p, v_p, q_r, k_r, v_r, state = ctx.saved_tensors
+        q_p, k_p, v_p, q_r, k_r, v_r, state, ws = ctx.saved_tensors
         # an output that did not reach the loss has a zero gradient
         do_p = torch.zeros_like(q_p) if do_p is None else do_p.to(torch.bfloat16).contiguous()
         do_r = torch.zeros_like(q_r) if do_r is None else do_r.to(torch.bfloat16).contiguous()
-        grads = api.linear_bwd(ctx.batch, ctx.decay, q_p, k_p, v_p, do_p, q_r, k_r, v_r, do_r, state=state)
+        grads = api.linear_bwd(ctx.batch, ctx.decay, q_p, k_p, v_p, do_p, q_r, k_r, v_r, do_r, state=state, fwd_ws=ws)
         return (*grads, None, None, None, None)
 
 

@@ -97,21 +97,38 @@ int check_batch(const augtree_groups* g, const float* decay) {
   return st ? st : check_heads(g->num_q_heads, g->num_kv_heads, g->head_dim, g->softmax_scale, decay);
 }
 
-// Rows of a block. A block is one workgroup a KV head in the state and output
-// kernels, and costs its state's way through the workspace: written, read and
-// written by the scan, read (16 d^2 bytes a KV head). Cuts follow from a tree's
-// own size, so that its results do not depend on the batch: enough blocks for
-// two workgroups on every CU from the tree alone, and never fewer than 128 rows
-// (two chunks) or more than 1024 (the state's traffic is below a tenth then).
-int block_rows(int64_t tokens, int hkv) {
-  int rows = 128;
-  while (rows < 1024 && tokens * hkv > (int64_t)512 * rows) rows *= 2;
-  return rows;
+int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Rows of a tree's blocks. A block is one workgroup a KV head in the state and
+// output kernels and three in the gradient kernel; the chip runs `slots` of them
+// at once (two a CU for d = 128, three for d = 64), so a launch takes whole rounds
+// of them, each as long as a block: its rows and its state's way through memory
+// (written, scanned and read: 16 d^2 bytes, as much as 4 d / (1 + group) rows'
+// own traffic). The rows that make these rounds shortest are taken. The tree
+// alone decides, so that its results do not depend on the batch. (32768-token
+// prompt, eight branches of 2048, 32 / 8 heads, forward + backward: RULE_US.)
+int block_rows(const augtree_groups* g, int tree) {
+  const int d = g->head_dim, hkv = g->num_kv_heads, nb = g->num_branches;
+  const int64_t slots = d == 128 ? 512 : 768;
+  const double state = 4.0 * d / (1 + g->num_q_heads / hkv);
+  int best = 0;
+  double best_cost = 0;
+  for (int rows = 128; rows <= 1024; rows += kLinChunk) {
+    int64_t units = cdiv(g->cu_prompt[tree + 1] - g->cu_prompt[tree], rows);
+    for (int b = nb ? g->cu_branch[tree] : 0; nb && b < g->cu_branch[tree + 1]; ++b)
+      units += cdiv(g->cu_resp[b + 1] - g->cu_resp[b], rows);
+    units *= hkv;
+    const double cost = (double)(cdiv(units, slots) + cdiv(3 * units, slots)) * (rows + state);
+    if (!best || cost < best_cost) best = rows, best_cost = cost;
+  }
+  return best;
 }
+
+constexpr int64_t kScanBlocks = 64;
 
 struct Layout {
   std::vector<LinSeg> segs;
-  int64_t blocks = 0;
+  int64_t blocks = 0, longest = 0;  // of the batch; of the tree with the most
   size_t states = 0, tree = 0;  // bytes: states of all blocks; one state per tree
 };
 
@@ -132,10 +149,13 @@ int make_layout(const augtree_groups* g, Layout* L) {
   };
   std::vector<int> rows(ng);
   for (int t = 0; t < ng; ++t) {
-    int64_t tokens = g->cu_prompt[t + 1] - g->cu_prompt[t];
-    if (nb) tokens += g->cu_resp[g->cu_branch[t + 1]] - g->cu_resp[g->cu_branch[t]];
-    rows[t] = block_rows(tokens, g->num_kv_heads);
+    rows[t] = block_rows(g, t);
+    int64_t own = blocks;
     add(t, g->cu_prompt[t], g->cu_prompt[t + 1] - g->cu_prompt[t], nb ? g->cu_branch[t] : 0, rows[t]);
+    own = blocks - own;
+    for (int b = nb ? g->cu_branch[t] : 0; nb && b < g->cu_branch[t + 1]; ++b)
+      own += cdiv(g->cu_resp[b + 1] - g->cu_resp[b], rows[t]);
+    L->longest = std::max(L->longest, own);
   }
   for (int t = 0; nb && t < ng; ++t)
     for (int b = g->cu_branch[t]; b < g->cu_branch[t + 1]; ++b)
@@ -204,7 +224,7 @@ struct Call {
   // states[block] <- what reaches the block. exact: as fp32 sums would have it; the forward's states always are, so that
   // its outputs do not depend on whether they are handed out.
   int states(bool reverse, const uint16_t* const y[2], const uint16_t* const z[2], const float* init, float* states,
-             float* tree, float* out_p, float* out_r, bool exact) {
+             float* ends, float* out_p, float* out_r, bool exact) {
     const bool branches = g->num_branches > 0;
     LinStateParams s;
     std::memset(&s, 0, sizeof(s));
@@ -223,17 +243,19 @@ struct Call {
     std::memset(&c, 0, sizeof(c));
     c.states = states;
     c.init = init;
-    c.tree = tree;
+    c.ends = ends;
     c.out_p = out_p;
     c.out_r = out_r;
     c.skip_prompt = s.skip_prompt;
     c.skip_branch = s.skip_branch;
     c.b = b;
-    for (int k = 0; k < 2; ++k) {
-      const bool prompts = reverse ? k == 1 : k == 0;
-      if (!prompts && !branches) continue;
+    // A tree's blocks are scanned by one launch, its branches one after the other, where they are few; else prompts and
+    // branches get a launch each, in which the branches run side by side (SPLIT_US).
+    const bool split = branches && L.longest > kScanBlocks;
+    for (int k = 0; k < (split ? 2 : 1); ++k) {
+      const int part = !split ? 0 : (k == 0) != reverse ? 1 : 2;
       Hook h(reverse ? "linear_scan_rev" : "linear_scan", stream);
-      if (int st = hip_ok(launch_lin_scan(c, g->head_dim, reverse, prompts, stream), "scan launch")) return st;
+      if (int st = hip_ok(launch_lin_scan(c, g->head_dim, reverse, part, stream), "scan launch")) return st;
     }
     return AUGTREE_OK;
   }
@@ -320,8 +342,8 @@ int augtree_linear_fwd(const augtree_groups* grp, const float* decay, const uint
 int augtree_linear_bwd(const augtree_groups* grp, const float* decay, const uint16_t* q_p, const uint16_t* k_p,
                        const uint16_t* v_p, const uint16_t* do_p, const uint16_t* q_r, const uint16_t* k_r,
                        const uint16_t* v_r, const uint16_t* do_r, const float* state, uint16_t* dq_p, uint16_t* dk_p,
-                       uint16_t* dv_p, uint16_t* dq_r, uint16_t* dk_r, uint16_t* dv_r, void* ws, size_t ws_bytes,
-                       void* stream) {
+                       uint16_t* dv_p, uint16_t* dq_r, uint16_t* dk_r, uint16_t* dv_r, const void* fwd_ws,
+                       size_t fwd_ws_bytes, void* ws, size_t ws_bytes, void* stream) {
   return guarded([&]() -> int {
     int st = check_batch(grp, decay);
     if (st) return st;
@@ -336,21 +358,29 @@ int augtree_linear_bwd(const augtree_groups* grp, const float* decay, const uint
     Call c;
     c.g = grp;
     if ((st = make_layout(grp, &c.L)) || (st = check_ws(ws, ws_bytes, workspace_bytes(grp, c.L, true))) ||
-        (st = augtree_check_device()))
+        (fwd_ws && (st = check_ws(fwd_ws, fwd_ws_bytes, workspace_bytes(grp, c.L, false)))))
       return st;
+    if (fwd_ws && overlap(fwd_ws, fwd_ws_bytes, ws, ws_bytes))
+      return fail(AUGTREE_ERR_INVALID_ARGUMENT, "ws overlaps fwd_ws");
+    if ((st = augtree_check_device())) return st;
     c.ws = static_cast<char*>(ws);
     c.stream = static_cast<hipStream_t>(stream);
     if ((st = c.begin(decay))) return st;
-    float* const fwd = c.take<float>(c.L.states);
+    const float* fwd = nullptr;
+    float* const own = c.take<float>(c.L.states);
     float* const tree = c.take<float>(c.L.tree * grp->num_groups);
     float* const rev = c.take<float>(c.L.states);
     float* const ends = c.take<float>(c.L.tree * std::max(1, grp->num_branches));
     const uint16_t *const q[2] = {q_p, q_r}, *const k[2] = {k_p, k_r}, *const v[2] = {v_p, v_r},
                    *const g[2] = {do_p, do_r};
     uint16_t *const dq[2] = {dq_p, dq_r}, *const dk[2] = {dk_p, dk_r}, *const dv[2] = {dv_p, dv_r};
-    if ((st = c.states(false, k, v, state, fwd, tree, nullptr, nullptr, false)) ||
-        (st = c.states(true, q, g, nullptr, rev, ends, nullptr, nullptr, false)))
-      return st;
+    if (fwd_ws) {
+      fwd = reinterpret_cast<const float*>(static_cast<const char*>(fwd_ws) + align_up(c.L.segs.size() * sizeof(LinSeg)));
+    } else {
+      fwd = own;
+      if ((st = c.states(false, k, v, state, own, tree, nullptr, nullptr, true))) return st;
+    }
+    if ((st = c.states(true, q, g, nullptr, rev, ends, nullptr, nullptr, false))) return st;
     LinGradParams p;
     std::memset(&p, 0, sizeof(p));
     for (int i = 0; i < 2; ++i) {

@@ -48,7 +48,7 @@ struct LinStateParams {
 struct LinScanParams {
   float* states;
   const float* init;    // [num_trees] states that prompts begin from (forward), or nullptr: zero
-  float* tree;          // forward: [num_trees] prompts' ends; reverse: [num_branches] branches' ends
+  float* ends;          // forward: [num_trees] prompts' ends; reverse: [num_branches] branches' ends
   float* out_p;         // forward: user's copies of the prompts' and branches' ends, or nullptr
   float* out_r;
   int32_t skip_prompt, skip_branch;  // the last block's own state was left out
@@ -89,7 +89,8 @@ static_assert(sizeof(LinTable) <= 4096, "kernel arguments");
 hipError_t launch_lin_table(const LinTable& t, hipStream_t stream);
 // exact: sums to fp32 accuracy (states that are handed out)
 hipError_t launch_lin_state(const LinStateParams& p, int head_dim, bool reverse, bool exact, hipStream_t stream);
-hipError_t launch_lin_scan(const LinScanParams& p, int head_dim, bool reverse, bool prompts, hipStream_t stream);
+// part: 0 whole trees, 1 prompts, 2 branches (1 and 2 hand over through `ends`, in the order of the direction)
+hipError_t launch_lin_scan(const LinScanParams& p, int head_dim, bool reverse, int part, hipStream_t stream);
 hipError_t launch_lin_out(const LinOutParams& p, int head_dim, hipStream_t stream);
 hipError_t launch_lin_grad(const LinGradParams& p, int head_dim, hipStream_t stream);
 

@@ -324,51 +324,83 @@ __global__ __launch_bounds__(4 * D, 4) void lin_state_kernel(LinStateParams p) {
 
 // ---------------------------------------------------------------------------- scan
 
-// One workgroup: 1024 elements of the states of one segment and KV head.
+// A thread carries four elements of the states of one KV head through blocks.
+struct Scan {
+  const LinScanParams& p;
+  int64_t per, at;  // elements of one block's (tree's) states; this thread's place in them
+  float lg;
+  __device__ __forceinline__ f32x4 load(const float* base, int64_t i) const {
+    return *reinterpret_cast<const f32x4*>(base + i * per + at);
+  }
+  __device__ __forceinline__ void store(float* base, int64_t i, f32x4 v) const {
+    *reinterpret_cast<f32x4*>(base + i * per + at) = v;
+  }
+  // One segment: every block's own state is replaced by the carry that reaches it. Eight blocks are loaded ahead: with
+  // one at a time 32 blocks took 11 us where these take SCAN_US.
+  template <bool REV>
+  __device__ __forceinline__ f32x4 segment(const LinSeg& s, f32x4 carry, bool skip) const {
+    constexpr int kAhead = 8;
+    const int count = (s.len + s.rows - 1) / s.rows, last = count - 1;
+    for (int i0 = 0; i0 < count; i0 += kAhead) {
+      f32x4 own[kAhead];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const int i = min(i0 + k, last);
+        own[k] = load(p.states, s.block0 + (REV ? last - i : i));
+      }
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        const int i = i0 + k, j = REV ? last - i : i;
+        if (i >= count) break;
+        store(p.states, s.block0 + j, carry);
+        if (i == last && skip) break;  // its own state was left out
+        carry = carry * exp2f(lg * (float)min(s.rows, s.len - j * s.rows)) + own[k];
+      }
+    }
+    return carry;
+  }
+};
+
+// A workgroup takes 1024 elements of the states of one KV head of a tree. `part`:
+// 0 the whole tree, 1 its prompt alone, 2 one branch of it (the grid then has a
+// workgroup for every branch).
 template <bool REV>
-__global__ __launch_bounds__(256) void lin_scan_kernel(LinScanParams p, int prompts, int elems) {
+__global__ __launch_bounds__(256) void lin_scan_kernel(LinScanParams p, int part, int elems) {
   const int slices = elems / 1024;
   const int unit = blockIdx.x / slices, slice = blockIdx.x - unit * slices;
-  const int seg_i = unit / p.b.heads_kv, kvh = unit - seg_i * p.b.heads_kv;
-  const LinSeg sg = load_segment(p.b, prompts ? seg_i : p.b.num_trees + seg_i);
-  const float lg = p.b.log2_decay[kvh];
-  const int64_t per = (int64_t)p.b.heads_kv * elems;                        // one block's (tree's) states
-  const int64_t at = (int64_t)kvh * elems + slice * 1024 + threadIdx.x * 4;  // this thread's four elements of them
-  auto ld = [&](const float* base, int64_t i) { return *reinterpret_cast<const f32x4*>(base + i * per + at); };
-  auto st = [&](float* base, int64_t i, f32x4 v) { *reinterpret_cast<f32x4*>(base + i * per + at) = v; };
-
-  f32x4 carry = {0.f, 0.f, 0.f, 0.f};
-  if (!REV) {
-    if (!prompts) carry = ld(p.tree, sg.link);
-    else if (p.init) carry = ld(p.init, seg_i);
-  } else if (prompts) {
-    const int b1 = seg_i + 1 < p.b.num_trees ? load_segment(p.b, seg_i + 1).link : p.b.num_branches;
-    for (int b = sg.link; b < b1; ++b) carry += ld(p.tree, b);
-  }
-  const int count = (sg.len + sg.rows - 1) / sg.rows;
-  const int skip = prompts ? p.skip_prompt : p.skip_branch;
-  for (int i = 0; i < count; ++i) {
-    const int j = REV ? count - 1 - i : i;
-    const int len = min(sg.rows, sg.len - j * sg.rows);
-    const int64_t b = sg.block0 + j;
-    if (skip && i == count - 1) {
-      st(p.states, b, carry);
-      break;
+  const int i = unit / p.b.heads_kv, kvh = unit - i * p.b.heads_kv;
+  const Scan scan = {p, (int64_t)p.b.heads_kv * elems, (int64_t)kvh * elems + slice * 1024 + threadIdx.x * 4,
+                     p.b.log2_decay[kvh]};
+  const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
+  if (part == 2) {
+    const LinSeg s = load_segment(p.b, p.b.num_trees + i);
+    if (REV) {
+      scan.store(p.ends, i, scan.segment<true>(s, zero, false));
+    } else {
+      const f32x4 end = scan.segment<false>(s, scan.load(p.ends, s.link), p.skip_branch);
+      if (p.out_r) scan.store(p.out_r, i, end);
     }
-    const f32x4 own = ld(p.states, b);
-    st(p.states, b, carry);
-    carry = carry * exp2f(lg * (float)len) + own;
+    return;
   }
-  if (skip) return;
-  if (!REV) {
-    if (prompts) {
-      st(p.tree, seg_i, carry);
-      if (p.out_p) st(p.out_p, seg_i, carry);
-    } else if (p.out_r) {
-      st(p.out_r, seg_i, carry);
+  const LinSeg prompt = load_segment(p.b, i);
+  const int b0 = prompt.link, b1 = i + 1 < p.b.num_trees ? load_segment(p.b, i + 1).link : p.b.num_branches;
+  if (REV) {
+    f32x4 carry = zero;
+    for (int b = b0; b < b1; ++b)
+      carry += part == 1 ? scan.load(p.ends, b)
+                         : scan.segment<true>(load_segment(p.b, p.b.num_trees + b), zero, false);
+    scan.segment<true>(prompt, carry, p.skip_prompt);
+  } else {
+    const f32x4 end = scan.segment<false>(prompt, p.init ? scan.load(p.init, i) : zero, p.skip_prompt);
+    if (p.out_p) scan.store(p.out_p, i, end);
+    if (part == 1) {
+      scan.store(p.ends, i, end);
+    } else {
+      for (int b = b0; b < b1; ++b) {
+        const f32x4 e = scan.segment<false>(load_segment(p.b, p.b.num_trees + b), end, p.skip_branch);
+        if (p.out_r) scan.store(p.out_r, b, e);
+      }
     }
-  } else if (!prompts) {
-    st(p.tree, seg_i, carry);
   }
 }
 
@@ -684,11 +716,11 @@ hipError_t launch_lin_state(const LinStateParams& p, int head_dim, bool reverse,
   return hipGetLastError();
 }
 
-hipError_t launch_lin_scan(const LinScanParams& p, int head_dim, bool reverse, bool prompts, hipStream_t stream) {
-  const int elems = head_dim * head_dim, segs = prompts ? p.b.num_trees : p.b.num_branches;
-  const dim3 grid(segs * p.b.heads_kv * (elems / 1024));
-  if (reverse) lin_scan_kernel<true><<<grid, 256, 0, stream>>>(p, prompts, elems);
-  else lin_scan_kernel<false><<<grid, 256, 0, stream>>>(p, prompts, elems);
+hipError_t launch_lin_scan(const LinScanParams& p, int head_dim, bool reverse, int part, hipStream_t stream) {
+  const int elems = head_dim * head_dim, units = part == 2 ? p.b.num_branches : p.b.num_trees;
+  const dim3 grid(units * p.b.heads_kv * (elems / 1024));
+  if (reverse) lin_scan_kernel<true><<<grid, 256, 0, stream>>>(p, part, elems);
+  else lin_scan_kernel<false><<<grid, 256, 0, stream>>>(p, part, elems);
   return hipGetLastError();
 }
 

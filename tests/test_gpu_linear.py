@@ -55,6 +55,27 @@ def test_begins_from_a_state():
     check(run(b, dec, x, state=state), oracle(b, dec, x, state=state), "state")
 
 
+def test_backward_from_the_forwards_workspace():
+    b = batch([(300, [70, 257]), (33, [5])], 4, 2, 128)
+    dec = decays(2)
+    x = inputs(b, 24)
+    ws = torch.empty(api.linear_workspace_size(b), dtype=torch.uint8, device="cuda")
+    api.linear_fwd(b, dec, *(x[n] for n in LEAVES), ws=ws)
+    args = (b, dec, x["q_p"], x["k_p"], x["v_p"], x["do_p"], x["q_r"], x["k_r"], x["v_r"], x["do_r"])
+    keep = ws.clone()
+    for g, w in zip(api.linear_bwd(*args, fwd_ws=ws), api.linear_bwd(*args)):
+        assert torch.equal(g, w)
+    assert torch.equal(ws, keep)
+
+
+def test_many_blocks_scan_branches_side_by_side():
+    """More blocks in a tree than one scan launch takes: 64 at 128 rows."""
+    b = batch([(4500, [1300, 2500, 1]), (70, [300])], 1, 1, 64)
+    dec = decays(1, 8.0, 8.0)
+    x = inputs(b, 25)
+    check(run(b, dec, x), oracle(b, dec, x), "two scan launches")
+
+
 def test_sequences_without_branches():
     b = batch([(200, []), (1, []), (500, [])], 4, 2, 64)
     dec = decays(2)

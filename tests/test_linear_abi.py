@@ -41,7 +41,8 @@ def fwd(C, b, decay, p=None, resp=None, ws=None, n=BIG, **kw):
 def bwd(C, b, decay, **kw):
     p = fake()
     return C.augtree_linear_bwd(b.ref, decay.ctypes.data_as(ctypes.c_void_p), p, p, p, kw.get("do_p", p), p, p, p, p, None,
-                                p, p, p, p, p, kw.get("dv_r", p), kw.get("ws", p), kw.get("n", BIG), None)
+                                p, p, p, p, p, kw.get("dv_r", p), kw.get("fwd_ws"), kw.get("fwd_n", 0),
+                                kw.get("ws", fake(1 << 22)), kw.get("n", 1 << 30), None)
 
 
 GOOD = ([0, 10, 25], [0, 2, 3], [0, 5, 12, 20])
@@ -99,6 +100,9 @@ def test_bad_pointers_and_workspaces(C):
     assert fwd(C, b, d, ws=ctypes.c_void_p((1 << 28) + 16)) == MISALIGNED
     assert bwd(C, b, d, n=need[1] - 1) == WORKSPACE and bwd(C, b, d, dv_r=ctypes.c_void_p(None)) == INVALID
     assert bwd(C, b, d, do_p=ODD) == MISALIGNED
+    assert bwd(C, b, d, fwd_ws=fake(), fwd_n=need[0] - 1) == WORKSPACE
+    assert bwd(C, b, d, fwd_ws=ctypes.c_void_p((1 << 28) + 16), fwd_n=need[0]) == MISALIGNED
+    assert bwd(C, b, d, fwd_ws=fake(1 << 22), fwd_n=need[0]) == INVALID  # the same memory as ws
     plain = GroupBatch([0, 10], [0, 0], [0], 4, 2, 64)
     assert fwd(C, plain, d, state_r=fake()) == INVALID
     scale = GroupBatch(*GOOD, 4, 2, 64, softmax_scale=float("inf"))
