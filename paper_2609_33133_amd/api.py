@@ -302,32 +302,43 @@ class _On:
     """The device of a call's tensors made current, with the stream it runs on there. Every tensor has to be on that
     device (a stream given by the caller too)."""
 
+    __slots__ = ("device", "stream", "guard")
+
     def __init__(self, tensors, stream=None):
         dev = None
         for name, t in tensors:
             if t is None:
                 continue
-            if t.device.type != "cuda":
-                raise ValueError(f"{name} must be a GPU tensor (the op has no CPU path)")
+            d = t.device
             if dev is None:
-                dev = t.device
-            elif t.device != dev:
-                raise ValueError(f"{name} is on {t.device}, other tensors on {dev}")
+                if d.type != "cuda":
+                    raise ValueError(f"{name} must be a GPU tensor (the op has no CPU path)")
+                dev = d
+            elif d != dev:
+                raise ValueError(f"{name} is on {d}, other tensors on {dev}")
         if stream is not None and stream.device != dev:
             raise ValueError(f"the stream is on {stream.device}, the tensors on {dev}")
-        self.device, self.stream, self.guard = dev, stream, torch.cuda.device(dev)
+        self.device, self.stream, self.guard = dev, stream, None
 
     def __enter__(self):
-        self.guard.__enter__()
-        s = self.stream if self.stream is not None else torch.cuda.current_stream()
-        return ctypes.c_void_p(s.cuda_stream)
+        if self.device.index != torch.cuda.current_device():
+            self.guard = torch.cuda.device(self.device)
+            self.guard.__enter__()
+        return (torch.cuda.current_stream() if self.stream is None else self.stream).cuda_stream
 
     def __exit__(self, *exc):
-        self.guard.__exit__(*exc)
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+
+def _addr(t):
+    return None if t is None else t.data_ptr()
 
 
 def _decay(decay, heads: int) -> np.ndarray:
     """Host array [heads] of fp32 decays (a sequence, a numpy array or a CPU tensor; one number for all heads)."""
+    if type(decay) is np.ndarray and decay.dtype == np.float32 and decay.shape == (heads,) and decay.flags.c_contiguous:
+        return decay
     if isinstance(decay, torch.Tensor):
         if decay.device.type != "cpu":
             raise ValueError("decay must be on the host")
@@ -382,19 +393,22 @@ def linear_fwd(b: GroupBatch, decay, q_p, k_p, v_p, q_r, k_r, v_r, state=None, o
     dev, f32 = on.device, torch.float32
     if state is not None:
         _need(state, "state", f32, (b.num_groups, b.hkv, b.d, b.d))
-    with on as st:
-        o_p = _out(o_p, "o_p", torch.bfloat16, q_p.shape, dev)
-        o_r = _out(o_r, "o_r", torch.bfloat16, q_r.shape, dev)
-        if want_states or state_p is not None:
-            state_p = _out(state_p, "state_p", f32, (b.num_groups, b.hkv, b.d, b.d), dev)
-        if want_states or state_r is not None:
-            state_r = _out(state_r, "state_r", f32, (b.num_branches, b.hkv, b.d, b.d), dev)
-        ws = _linear_ws(b, False, ws, dev)
-        _lib.check(_lib.load().augtree_linear_fwd(
-            b.ref, dec.ctypes.data_as(ctypes.c_void_p), _ptr(q_p), _ptr(k_p), _ptr(v_p), _ptr(q_r), _ptr(k_r),
-            _ptr(v_r), _ptr(state), _ptr(o_p), _ptr(o_r), _ptr(state_p), _ptr(state_r) if b.num_branches else None,
-            _ptr(ws), ctypes.c_size_t(ws.numel()), st), "linear_fwd")
+    o_p = _out(o_p, "o_p", torch.bfloat16, q_p.shape, dev)
+    o_r = _out(o_r, "o_r", torch.bfloat16, q_r.shape, dev)
+    if want_states or state_p is not None:
+        state_p = _out(state_p, "state_p", f32, (b.num_groups, b.hkv, b.d, b.d), dev)
+    if want_states or state_r is not None:
+        state_r = _out(state_r, "state_r", f32, (b.num_branches, b.hkv, b.d, b.d), dev)
+    _linear_fwd(b, dec, (q_p, k_p, v_p, q_r, k_r, v_r, state, o_p, o_r, state_p, state_r if b.num_branches else None),
+                _linear_ws(b, False, ws, dev), on)
     return o_p, o_r, state_p, state_r
+
+
+def _linear_fwd(b: GroupBatch, dec, tensors, ws, on: _On):
+    """The call of linear_fwd behind its checks: inputs, state and outputs in the order of augtree_linear_fwd."""
+    with on as st:
+        _lib.check(_lib.load().augtree_linear_fwd(b.ref, dec.ctypes.data, *(_addr(t) for t in tensors), _addr(ws),
+                                                  ws.numel(), st), "linear_fwd")
 
 
 def linear_bwd(b: GroupBatch, decay, q_p, k_p, v_p, do_p, q_r, k_r, v_r, do_r, state=None, dq_p=None, dk_p=None,
@@ -410,17 +424,19 @@ def linear_bwd(b: GroupBatch, decay, q_p, k_p, v_p, do_p, q_r, k_r, v_r, do_r, s
     dev = on.device
     if state is not None:
         _need(state, "state", torch.float32, (b.num_groups, b.hkv, b.d, b.d))
-    with on as st:
-        outs = [_out(t, n, torch.bfloat16, like.shape, dev)
-                for t, n, like in ((dq_p, "dq_p", q_p), (dk_p, "dk_p", k_p), (dv_p, "dv_p", v_p),
-                                   (dq_r, "dq_r", q_r), (dk_r, "dk_r", k_r), (dv_r, "dv_r", v_r))]
-        ws = _linear_ws(b, True, ws, dev)
-        _lib.check(_lib.load().augtree_linear_bwd(
-            b.ref, dec.ctypes.data_as(ctypes.c_void_p), _ptr(q_p), _ptr(k_p), _ptr(v_p), _ptr(do_p), _ptr(q_r),
-            _ptr(k_r), _ptr(v_r), _ptr(do_r), _ptr(state), *(_ptr(t) for t in outs), _ptr(fwd_ws),
-            ctypes.c_size_t(0 if fwd_ws is None else fwd_ws.numel()), _ptr(ws), ctypes.c_size_t(ws.numel()), st),
-            "linear_bwd")
+    outs = [_out(t, n, torch.bfloat16, like.shape, dev)
+            for t, n, like in ((dq_p, "dq_p", q_p), (dk_p, "dk_p", k_p), (dv_p, "dv_p", v_p),
+                               (dq_r, "dq_r", q_r), (dk_r, "dk_r", k_r), (dv_r, "dv_r", v_r))]
+    _linear_bwd(b, dec, (q_p, k_p, v_p, do_p, q_r, k_r, v_r, do_r, state, *outs), fwd_ws, _linear_ws(b, True, ws, dev), on)
     return tuple(outs)
+
+
+def _linear_bwd(b: GroupBatch, dec, tensors, fwd_ws, ws, on: _On):
+    """The call of linear_bwd behind its checks: inputs, state and outputs in the order of augtree_linear_bwd."""
+    with on as st:
+        _lib.check(_lib.load().augtree_linear_bwd(b.ref, dec.ctypes.data, *(_addr(t) for t in tensors), _addr(fwd_ws),
+                                                  0 if fwd_ws is None else fwd_ws.numel(), _addr(ws), ws.numel(), st),
+                   "linear_bwd")
 
 
 def linear_step(q, k, v, decay, state, src=None, state_out=None, o=None, scale: Optional[float] = None, stream=None):
@@ -445,8 +461,8 @@ def linear_step(q, k, v, decay, state, src=None, state_out=None, o=None, scale: 
         o = _out(o, "o", torch.bfloat16, q.shape, on.device)
         _lib.check(_lib.load().augtree_linear_step(
             rows, hq, hkv, d, 1.0 / math.sqrt(d) if scale is None else float(scale),
-            dec.ctypes.data_as(ctypes.c_void_p), _ptr(q), _ptr(k), _ptr(v), n, _ptr(state), _ptr(src),
-            _ptr(state_out), _ptr(o), st), "linear_step")
+            dec.ctypes.data, _addr(q), _addr(k), _addr(v), n, _addr(state), _addr(src),
+            _addr(state_out), _addr(o), st), "linear_step")
     return o, state_out
 
 
@@ -469,8 +485,8 @@ def head_norm_fwd(x, weight=None, bias=None, gate=None, activation: int = ACT_NO
     rows, heads, d = x.shape
     with on as st:
         y = _out(y, "y", torch.bfloat16, x.shape, on.device)
-        _lib.check(_lib.load().augtree_head_norm_fwd(rows, heads, d, int(activation), float(eps), _ptr(x), _ptr(gate),
-                                                     _ptr(weight), _ptr(bias), _ptr(y), st), "head_norm_fwd")
+        _lib.check(_lib.load().augtree_head_norm_fwd(rows, heads, d, int(activation), float(eps), _addr(x), _addr(gate),
+                                                     _addr(weight), _addr(bias), _addr(y), st), "head_norm_fwd")
     return y
 
 
@@ -495,8 +511,8 @@ def head_norm_bwd(x, dy, weight=None, bias=None, gate=None, activation: int = AC
             dbias = _out(dbias, "dbias", f32, (heads, d), dev)
         if ws is None and (dweight is not None or dbias is not None):
             ws = torch.empty(int(lib.augtree_head_norm_workspace_size(rows, heads, d)), dtype=torch.uint8, device=dev)
-        _lib.check(lib.augtree_head_norm_bwd(rows, heads, d, int(activation), float(eps), _ptr(x), _ptr(gate),
-                                             _ptr(weight), _ptr(bias), _ptr(dy), _ptr(dx), _ptr(dgate), _ptr(dweight),
-                                             _ptr(dbias), _ptr(ws), ctypes.c_size_t(0 if ws is None else ws.numel()),
+        _lib.check(lib.augtree_head_norm_bwd(rows, heads, d, int(activation), float(eps), _addr(x), _addr(gate),
+                                             _addr(weight), _addr(bias), _addr(dy), _addr(dx), _addr(dgate), _addr(dweight),
+                                             _addr(dbias), _addr(ws), 0 if ws is None else ws.numel(),
                                              st), "head_norm_bwd")
     return dx, dgate, dweight, dbias

@@ -79,14 +79,10 @@ class _GroupLinearAttention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q_p, k_p, v_p, q_r, k_r, v_r, batch: GroupBatch, decay, state, return_state: bool):
         b = batch
-        for t, n, rows, h in ((q_p, "q_p", b.tp, b.hq), (k_p, "k_p", b.tp, b.hkv), (v_p, "v_p", b.tp, b.hkv),
-                              (q_r, "q_r", b.tr, b.hq), (k_r, "k_r", b.tr, b.hkv), (v_r, "v_r", b.tr, b.hkv)):
-            _check(t, n, rows, h, b.d)
-        q_p, k_p, v_p, q_r, k_r, v_r = (t.contiguous() for t in (q_p, k_p, v_p, q_r, k_r, v_r))
+        x = [t.contiguous() for t in (q_p, k_p, v_p, q_r, k_r, v_r)]
         ws = torch.empty(api.linear_workspace_size(b), dtype=torch.uint8, device=q_p.device)
-        o_p, o_r, state_p, state_r = api.linear_fwd(b, decay, q_p, k_p, v_p, q_r, k_r, v_r, state=state,
-                                                    want_states=return_state, ws=ws)
-        ctx.save_for_backward(q_p, k_p, v_p, q_r, k_r, v_r, state, ws)  # the states in ws serve the backward too
+        o_p, o_r, state_p, state_r = api.linear_fwd(b, decay, *x, state=state, want_states=return_state, ws=ws)
+        ctx.save_for_backward(*x, state, ws)  # the states in ws serve the backward too
         ctx.batch, ctx.decay = b, decay
         if not return_state:
             return o_p, o_r
@@ -99,7 +95,12 @@ class _GroupLinearAttention(torch.autograd.Function):
         # an output that did not reach the loss has a zero gradient
         do_p = torch.zeros_like(q_p) if do_p is None else do_p.to(torch.bfloat16).contiguous()
         do_r = torch.zeros_like(q_r) if do_r is None else do_r.to(torch.bfloat16).contiguous()
-        grads = api.linear_bwd(ctx.batch, ctx.decay, q_p, k_p, v_p, do_p, q_r, k_r, v_r, do_r, state=state, fwd_ws=ws)
+        # the forward has checked what it saved; the outputs' gradients are new
+        api._linear_inputs(ctx.batch, (("do_p", do_p), ("do_r", do_r)))
+        on = api._On((("q_p", q_p), ("do_p", do_p), ("do_r", do_r)))
+        grads = [torch.empty_like(t) for t in (q_p, k_p, v_p, q_r, k_r, v_r)]
+        api._linear_bwd(ctx.batch, ctx.decay, (q_p, k_p, v_p, do_p, q_r, k_r, v_r, do_r, state, *grads), ws,
+                        api._linear_ws(ctx.batch, True, None, q_p.device), on)
         return (*grads, None, None, None, None)
 
 

@@ -101,7 +101,7 @@ int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // Rows of a tree's blocks. A block is one workgroup a KV head in the state and
 // output kernels and three in the gradient kernel; the chip runs `slots` of them
-// at once (two a CU for d = 128, three for d = 64), so a launch takes whole rounds
+// at once (two a CU for d = 128, four for d = 64), so a launch takes whole rounds
 // of them, each as long as a block: its rows and its state's way through memory
 // (written, scanned and read: 16 d^2 bytes, as much as 4 d / (1 + group) rows'
 // own traffic). The rows that make these rounds shortest are taken. The tree
@@ -109,7 +109,7 @@ int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // prompt, eight branches of 2048, 32 / 8 heads, forward + backward: RULE_US.)
 int block_rows(const augtree_groups* g, int tree) {
   const int d = g->head_dim, hkv = g->num_kv_heads, nb = g->num_branches;
-  const int64_t slots = d == 128 ? 512 : 768;
+  const int64_t slots = d == 128 ? 512 : 1024;
   const double state = 4.0 * d / (1 + g->num_q_heads / hkv);
   int best = 0;
   double best_cost = 0;

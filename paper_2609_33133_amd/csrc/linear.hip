@@ -35,6 +35,7 @@ namespace {
 
 constexpr int C = kLinChunk;
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2), may_alias));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 // ---------------------------------------------------------------------------- the batch
 
@@ -174,10 +175,10 @@ __device__ __forceinline__ void split2(float* v, bf16x8& hi, bf16x8& lo) {
 
 // The decays of a workgroup in LDS. row[r]: from row r of a chunk of n rows to
 // its end (reverse: to its start), the weights of the state's update; rows from
-// n on weigh nothing. pair[16 + k]: over a distance of k rows, 0 for k < 0.
+// n on weigh nothing. pair[32 + k]: over a distance of k rows, 0 for k < 0.
 struct Decays {
   float row[C];
-  float pair[16 + C];
+  float pair[32 + C];
 };
 
 template <bool REV>
@@ -185,9 +186,11 @@ __device__ __forceinline__ void set_row_decays(Decays& t, float lg, int n) {
   const int r = threadIdx.x;
   if (r < C) t.row[r] = r < n ? exp2f(lg * (float)(REV ? r : n - 1 - r)) : 0.f;
 }
+template <int THREADS>
 __device__ __forceinline__ void set_pair_decays(Decays& t, float lg) {
+  static_assert(THREADS >= 32 + C, "one element a thread");
   const int i = threadIdx.x;
-  if (i < 16 + C) t.pair[i] = i < 16 ? 0.f : exp2f(lg * (float)(i - 16));
+  if (i < 32 + C) t.pair[i] = i < 32 ? 0.f : exp2f(lg * (float)(i - 32));
 }
 
 // s += Y^T (w Z) of one chunk: rows y (of all of Y's D columns), columns z (16 of
@@ -232,8 +235,8 @@ __device__ __forceinline__ void scale_state(f32x4* s, float f) {
 // tile of each operand, so that two workgroups fit a CU. Rows from n on are zeros.
 template <int D, int NW>
 struct TileStage {
-  static constexpr int CH = D / 8, RPI = 64 / CH, NI = C / (RPI * NW);
-  static_assert(NW * RPI == 32, "rows of one pass: a multiple of the swizzle's period");
+  static constexpr int CH = D / 8, RPI = 64 / CH, ROWS = NW * RPI, NI = C / ROWS;  // pieces of a row; rows of a pass
+  static_assert(ROWS % 16 == 0, "a multiple of the swizzle's period");
   raw16 r[NI];
   __device__ __forceinline__ static int row() {
     return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * RPI + (threadIdx.x & 63) / CH;
@@ -251,7 +254,7 @@ struct TileStage {
         __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, (int)(2 * n * stride), 0x00020000);
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
-      const auto v = __builtin_amdgcn_raw_buffer_load_b128(rsrc, src + i * (uint32_t)(64 * stride), 0, 0);
+      const auto v = __builtin_amdgcn_raw_buffer_load_b128(rsrc, src + i * (uint32_t)(2 * ROWS * stride), 0, 0);
       __builtin_memcpy(&r[i], &v, 16);
     }
 #endif
@@ -259,7 +262,7 @@ struct TileStage {
   __device__ __forceinline__ void put(__bf16* tile, int dst) const {
     char* t = reinterpret_cast<char*>(tile) + dst;
 #pragma unroll
-    for (int i = 0; i < NI; ++i) *reinterpret_cast<raw16*>(t + i * 64 * D) = r[i];
+    for (int i = 0; i < NI; ++i) *reinterpret_cast<raw16*>(t + i * 2 * ROWS * D) = r[i];
   }
 };
 
@@ -415,39 +418,76 @@ struct Product {
   const float* state;  // of the block and KV head
 };
 
+// Rows 32 tx + l32 (< n) of a chunk, 32 columns from `out` on. The buffer's range
+// ends behind row n - 1, so later rows are not written.
+template <int D>
+__device__ __forceinline__ void store_rows(uint16_t* out, const f32x16* acc, float scale, int n, int64_t stride, int l32,
+                                           int hf) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)out, 0, (int)(2 * n * stride), 0x00020000);
+  const uint32_t at = 2 * (uint32_t)(l32 * stride) + 16 * hf;
+#pragma unroll
+  for (int tx = 0; tx < 2; ++tx) {
+    uint32_t d[8];  // registers 2i, 2i + 1
+#pragma unroll
+    for (int i = 0; i < 8; ++i) d[i] = bf16_pair(acc[tx][2 * i] * scale, acc[tx][2 * i + 1] * scale);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      // the half-waves exchange four columns: each then has eight consecutive ones
+      const auto e0 = __builtin_amdgcn_permlane32_swap(d[4 * k], d[4 * k + 2], false, false);
+      const auto e1 = __builtin_amdgcn_permlane32_swap(d[4 * k + 1], d[4 * k + 3], false, false);
+      const u32x4 v = {e0[0], e1[0], e0[1], e1[1]};
+      __builtin_amdgcn_raw_buffer_store_b128(v, rsrc, at + 32 * k + tx * (uint32_t)(64 * stride), 0, 0);
+    }
+  }
+#endif
+}
+
 template <int D>
 struct OutShared {
   __attribute__((aligned(1024))) __bf16 xt[C * D];
   __attribute__((aligned(1024))) __bf16 yt[C * D];
   __attribute__((aligned(1024))) __bf16 zt[C * D];
-  __attribute__((aligned(1024))) __bf16 pt[2][C * C];  // P as two bf16 terms, rows x, columns y, swizzled
+  // P as two bf16 terms, x by y in 32 x 32 tiles: (0, 0), the one off the diagonal, (1, 1)
+  __attribute__((aligned(1024))) __bf16 pt[2][3][32 * 32];
   Decays decays;
 };
 
-// Rows 16 tx + l16 (< n) of a chunk, 4 columns from 4 q on, from `out` on. The
-// buffer's range ends behind row n - 1, so later rows are not written.
+// 32x32x16 products (see common.h): lane l holds row (column) l % 32, k indices
+// 8 (l / 32) .. + 7; register i of the result column l % 32, row acc_row(i, l / 32).
+
+// As read_columns, for 32 columns: rows 16 m + 4 hf + 0..3 and 8 further on.
 template <int D>
-__device__ __forceinline__ void store_rows(uint16_t* out, const f32x4* acc, float scale, int n, int64_t stride, int l16,
-                                           int q) {
-#if defined(__HIP_DEVICE_COMPILE__)
-  const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)out, 0, (int)(2 * n * stride), 0x00020000);
-  const uint32_t at = 2 * (uint32_t)(l16 * stride) + 8 * q;
-#pragma unroll
-  for (int tx = 0; tx < 4; ++tx) {
-    const u32x2 w = {bf16_pair(acc[tx][0] * scale, acc[tx][1] * scale),
-                     bf16_pair(acc[tx][2] * scale, acc[tx][3] * scale)};
-    __builtin_amdgcn_raw_buffer_store_b64(w, rsrc, at + tx * (uint32_t)(32 * stride), 0, 0);
-  }
-#endif
+__device__ __forceinline__ int column32_base(int col, int lane) {
+  return 2 * loff<D>(4 * (lane >> 5) + ((lane & 15) >> 2), col);
 }
+template <int D>
+__device__ __forceinline__ bf16x8 read_columns32(const __bf16* tile, int base, int flip, int m) {
+  const char* t = reinterpret_cast<const char*>(tile) + m * 16 * D * 2;
+  // rows 8 further on: row bit 3 and, in the swizzle (0, 2, 3, 1), both middle bits: 0 <-> 3, 2 <-> 1
+  constexpr int kEightRows = 8 * 2 * D + 48;
+  const s16x4 a = lds_tr16(reinterpret_cast<const __bf16*>(t + (base ^ flip)));
+  const s16x4 b = lds_tr16(reinterpret_cast<const __bf16*>(t + (base ^ flip ^ kEightRows)));
+  bf16x8 r;
+  __builtin_memcpy(&r, &a, 8);
+  __builtin_memcpy(reinterpret_cast<char*>(&r) + 8, &b, 8);
+  return r;
+}
+
+// Rows of the state in the accumulators: register i of tile t in half hf. The
+// columns of y are read with the second and third four of every 16 exchanged, so
+// that registers 8 s .. 8 s + 7 hold 8 consecutive ones and x is read plainly.
+__device__ __forceinline__ int state32_row(int t, int i, int hf) { return 32 * t + 16 * (i >> 3) + 8 * hf + (i & 7); }
+
+// element offset of the 16-byte piece `ch` (0..3) of row r of a [32, 32] tile of P
+__device__ __forceinline__ int poff(int r, int ch) { return 32 * r + 8 * (ch ^ ((r >> 2) & 3)); }
 
 template <int D, bool REV, bool TS>
 __device__ __forceinline__ void lin_out(OutShared<D>& sh, const LinBatch& batch, float scale, const Block& bl, int kvh,
                                         const Product& pr) {
-  constexpr int NT = D / 16;  // tiles of the state's rows, and wavefronts
-  constexpr bool PAIRED = !REV;
+  constexpr int NW = D / 32;  // wavefronts, and tiles of the state's rows
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int q = lane >> 4, l16 = lane & 15;
+  const int hf = lane >> 5, l32 = lane & 31;
   const float lg = batch.log2_decay[kvh];
   const int g = batch.group;
   const int64_t stride_q = (int64_t)batch.heads_kv * g * D, stride_kv = (int64_t)batch.heads_kv * D;
@@ -458,8 +498,8 @@ __device__ __forceinline__ void lin_out(OutShared<D>& sh, const LinBatch& batch,
   const uint16_t* const y = pr.y + off_y;
   const uint16_t* const z = pr.z + off_y;
   uint16_t* const out = pr.out + off_x;
-  typedef TileStage<D, NT> Stage;
-  Stage s0, s1;  // forward: x; reverse: y and z
+  typedef TileStage<D, NW> Stage;
+  Stage s0, s1, s2;  // forward: x, y, z; reverse: y, z, x
   const uint32_t src_x = Stage::source(stride_x), src_y = Stage::source(stride_y);
   const int dst = Stage::target();
 
@@ -475,102 +515,96 @@ __device__ __forceinline__ void lin_out(OutShared<D>& sh, const LinBatch& batch,
     a.fetch(y + c * C * stride_y + h * D, src_y, rows_of(c), stride_y);
     b.fetch(z + c * C * stride_y + h * D, src_y, rows_of(c), stride_y);
   };
-  if (REV) fetch_yz(s0, s1, 0, 0);
-  else fetch_x(s0, 0, 0);
+  if (REV) fetch_x(s2, 0, 0), fetch_yz(s0, s1, 0, 0);
+  else fetch_yz(s1, s2, 0, 0), fetch_x(s0, 0, 0);
 
-  const int ybase = column_base<D>(state_row<PAIRED>(0, lane & 3, 0), lane);
-  const int zbase = column_base<D>(16 * wave + 4 * (lane & 3), lane);
-  set_pair_decays(sh.decays, lg);
-  // P is written where it is not masked; the 16 x 16 tiles beside the diagonal that are read with it stay zero
-  for (int i = threadIdx.x; i < 2 * C * C / 8; i += 4 * D) reinterpret_cast<raw16*>(sh.pt)[i] = raw16{0u, 0u, 0u, 0u};
+  // bytes: this lane's four columns of y (exchanged order) and z, its row of a tile's first 32, its row of a tile of P
+  const int c4 = 16 * ((lane >> 4) & 1);
+  const int ybase = column32_base<D>(c4 + 4 * (((lane & 1) << 1) | ((lane >> 1) & 1)), lane);
+  const int zbase = column32_base<D>(32 * wave + c4 + 4 * (lane & 3), lane);
+  const int rbase = 2 * loff<D>(l32, 8 * hf);
+  const int pbase = 2 * poff(l32, hf);
+  set_pair_decays<2 * D>(sh.decays, lg);
 
   // the state that reaches the block
-  f32x4 s[NT];
+  f32x16 s[NW];
   {
-    const int col = 16 * wave + l16;
+    const int col = 32 * wave + l32;
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-      if (TS) {
-        s[t] = *reinterpret_cast<const f32x4*>(pr.state + col * D + state_row<PAIRED>(t, q, 0));
-      } else {
+    for (int t = 0; t < NW; ++t)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[t][i] = pr.state[state_row<PAIRED>(t, q, i) * D + col];
+      for (int i = 0; i < 16; ++i) {
+        const int r = state32_row(t, i, hf);
+        s[t][i] = TS ? pr.state[col * D + r] : pr.state[r * D + col];
       }
-    }
   }
 
-  // Byte offsets of this lane's row among a tile's first 16 (16 rows further on: + 32 D, the swizzle's period), from
-  // column 8 q on; k step ks flips 64 ks.
-  const int rbase = 2 * loff<D>(l16, 8 * q);
-  auto read8 = [&](const __bf16* tile, int base, int rt, int ks) {
-    return *reinterpret_cast<const bf16x8*>(reinterpret_cast<const char*>(tile) + rt * 32 * D + (base ^ (64 * ks)));
+  // row l32 of a tile's half `half`, 8 columns from 16 ks + 8 hf on
+  auto read8 = [&](const __bf16* tile, int base, int half, int ks) {
+    return *reinterpret_cast<const bf16x8*>(reinterpret_cast<const char*>(tile) + half * 64 * D + (base ^ (32 * ks)));
   };
-  // x in the order of the state's rows
-  const int xbase = PAIRED ? rbase : 2 * loff<D>(l16, 4 * q);
-  auto read_x = [&](int base, int rt, int ks) {
-    if (PAIRED) return read8(sh.xt, base, rt, ks);
-    const char* t = reinterpret_cast<const char*>(sh.xt) + rt * 32 * D;
-    bf16x8 r;
-    __builtin_memcpy(&r, t + (base ^ (64 * ks)), 8);
-    __builtin_memcpy(reinterpret_cast<char*>(&r) + 8, t + (base ^ (64 * ks + 32)), 8);
-    return r;
-  };
-
-  // Tile (ty, tx) of P^T, [16 y] x [16 x], a lane having one x and four y.
-  auto p_tile = [&](int ty, int tx) {
-    f32x4 a = {0.f, 0.f, 0.f, 0.f};
+  // Tile k of P (rows x, columns y): P^T is formed, [32 y] x [32 x], a lane having one x.
+  auto p_tile = [&](int k) {
+    const int ty = REV ? (k > 0) : (k == 2), tx = REV ? (k == 2) : (k > 0);
+    const float* const pw = sh.decays.pair + 32 + (REV ? 4 * hf - l32 : l32 - 4 * hf) + (k == 1 ? 32 : 0);
     const int rb = here(rbase);
+    f32x16 acc;
 #pragma unroll
-    for (int ks = 0; ks < D / 32; ++ks) a = mfma16(read8(sh.yt, rb, ty, ks), read8(sh.xt, rb, tx, ks), a);
-    const float* const pw = sh.decays.pair + 16 + (REV ? 16 * (ty - tx) + 4 * q - l16 : 16 * (tx - ty) + l16 - 4 * q);
-    u32x2 v, u;
+    for (int i = 0; i < 16; ++i) acc[i] = 0.f;
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const float f0 = a[2 * e] * pw[REV ? 2 * e : -2 * e], f1 = a[2 * e + 1] * pw[REV ? 2 * e + 1 : -2 * e - 1];
-      v[e] = bf16_pair(f0, f1);
-      u[e] = bf16_pair(f0 - __uint_as_float(v[e] << 16), f1 - __uint_as_float(v[e] & 0xffff0000u));
+    for (int ks = 0; ks < D / 16; ++ks) acc = mfma32(read8(sh.yt, rb, ty, ks), read8(sh.xt, rb, tx, ks), acc);
+#pragma unroll
+    for (int qd = 0; qd < 4; ++qd) {
+      u32x2 v, u;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int i = 4 * qd + 2 * e, at = 8 * qd + 2 * e;
+        const float f0 = acc[i] * pw[REV ? at : -at], f1 = acc[i + 1] * pw[REV ? at + 1 : -at - 1];
+        v[e] = bf16_pair(f0, f1);
+        u[e] = bf16_pair(f0 - __uint_as_float(v[e] << 16), f1 - __uint_as_float(v[e] & 0xffff0000u));
+      }
+      // k step qd / 2 of the tile, in the order of the transposed z: piece 2 (qd / 2) + hf, half qd % 2
+      const int o = poff(l32, 2 * (qd >> 1) + hf) + 4 * (qd & 1);
+      *reinterpret_cast<u32x2*>(sh.pt[0][k] + o) = v;
+      *reinterpret_cast<u32x2*>(sh.pt[1][k] + o) = u;
     }
-    const int o = loff<C>(16 * tx + l16, 16 * ty + 4 * q);
-    *reinterpret_cast<u32x2*>(sh.pt[0] + o) = v;
-    *reinterpret_cast<u32x2*>(sh.pt[1] + o) = u;
   };
-  // the 10 tiles on and beside the diagonal, dealt to the wavefronts: tile k is
-  // (i, j), j <= i, with i (i + 1) / 2 + j = k
   auto p_tiles = [&]() {
-    for (int k = wave; k < 10; k += NT) {
-      const int i = (k >= 1) + (k >= 3) + (k >= 6), j = k - i * (i + 1) / 2;
-      if (REV) p_tile(i, j);
-      else p_tile(j, i);
+    if constexpr (NW == 4) {
+      if (wave < 3) p_tile(wave);
+    } else {
+      if (wave == 0) p_tile(0), p_tile(2);
+      else p_tile(1);
     }
   };
 
-  const int pbase = 2 * loff<C>(l16, 8 * q);
-
-  f32x4 acc[4];
+  f32x16 acc[2];
   // acc = out^T [z, x] of what reaches the chunk: S^T X^T, the state as two bf16 terms, and its decay to each row
   auto from_state = [&](int n) {
-    const int xb = here(xbase);
+    const int xb = here(rbase);
 #pragma unroll
-    for (int tx = 0; tx < 4; ++tx) acc[tx] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int tx = 0; tx < 2; ++tx)
 #pragma unroll
-    for (int ks = 0; ks < D / 32; ++ks) {
+      for (int i = 0; i < 16; ++i) acc[tx][i] = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) {
       float f[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) f[e] = s[2 * ks + (e >> 2)][e & 3];
-      bf16x8 hi, lo, xv[4];
+      for (int e = 0; e < 8; ++e) f[e] = s[ks >> 1][8 * (ks & 1) + e];
+      bf16x8 hi, lo;
       split2(f, hi, lo);
-#pragma unroll
-      for (int tx = 0; tx < 4; ++tx) xv[tx] = read_x(xb, tx, ks);
-#pragma unroll
-      for (int tx = 0; tx < 4; ++tx) acc[tx] = mfma16(hi, xv[tx], acc[tx]);
-#pragma unroll
-      for (int tx = 0; tx < 4; ++tx) acc[tx] = mfma16(lo, xv[tx], acc[tx]);
-      __builtin_amdgcn_sched_barrier(0);
+      const bf16x8 x0 = read8(sh.xt, xb, 0, ks), x1 = read8(sh.xt, xb, 1, ks);
+      acc[0] = mfma32(hi, x0, acc[0]);
+      acc[1] = mfma32(hi, x1, acc[1]);
+      acc[0] = mfma32(lo, x0, acc[0]);
+      acc[1] = mfma32(lo, x1, acc[1]);
     }
 #pragma unroll
-    for (int tx = 0; tx < 4; ++tx) {
-      const int r = 16 * tx + l16;
-      acc[tx] *= exp2f(lg * (float)(REV ? max(n - r, 0) : r + 1));
+    for (int tx = 0; tx < 2; ++tx) {
+      const int r = 32 * tx + l32;
+      const float lead = exp2f(lg * (float)(REV ? max(n - r, 0) : r + 1));
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[tx][i] *= lead;
     }
   };
   // acc += Z^T P^T
@@ -579,16 +613,43 @@ __device__ __forceinline__ void lin_out(OutShared<D>& sh, const LinBatch& batch,
 #pragma unroll
     for (int k = 0; k < 2; ++k)
 #pragma unroll
-      for (int m = 0; m < 2; ++m)
+      for (int m = 0; m < 4; ++m)
 #pragma unroll
-        for (int tx = 0; tx < 4; ++tx) {
-          if (REV ? m < (tx >> 1) : m > (tx >> 1)) continue;  // masked
-          const char* t = reinterpret_cast<const char*>(sh.pt[k]) + tx * 32 * C;
-          acc[tx] = mfma16(zf[m], *reinterpret_cast<const bf16x8*>(t + (pb ^ (64 * m))), acc[tx]);
+        for (int tx = 0; tx < 2; ++tx) {
+          const int ty = m >> 1;
+          if (REV ? ty < tx : ty > tx) continue;  // masked
+          const char* t = reinterpret_cast<const char*>(sh.pt[k][ty == tx ? 2 * tx : 1]);
+          acc[tx] = mfma32(zf[m], *reinterpret_cast<const bf16x8*>(t + (pb ^ (32 * (m & 1)))), acc[tx]);
         }
   };
+  // s += Y^T (w Z)
+  auto update = [&](const bf16x8* zf) {
+    const int yb = here(ybase);
+    const float* const w = sh.decays.row + 4 * hf;
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+      const f32x4 w0 = *reinterpret_cast<const f32x4*>(w + 16 * m), w1 = *reinterpret_cast<const f32x4*>(w + 16 * m + 8);
+      float f[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[e] = (float)zf[m][e] * (e < 4 ? w0[e] : w1[e - 4]);
+      bf16x8 hi, lo;
+      split2(f, hi, lo);
+#pragma unroll
+      for (int t = 0; t < NW; ++t) {
+        const bf16x8 a = read_columns32<D>(sh.yt, yb, 64 * t, m);
+        s[t] = mfma32(a, hi, s[t]);
+        s[t] = mfma32(a, lo, s[t]);
+      }
+    }
+  };
+  auto fade_state = [&](float f) {
+#pragma unroll
+    for (int t = 0; t < NW; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[t][i] *= f;
+  };
   auto store = [&](int c, int h, int n) {
-    store_rows<D>(out + c * C * stride_x + h * D + 16 * wave, acc, scale, n, stride_x, l16, q);
+    store_rows<D>(out + c * C * stride_x + h * D + 32 * wave, acc, scale, n, stride_x, l32, hf);
   };
 
   int row_n = -1;
@@ -596,68 +657,65 @@ __device__ __forceinline__ void lin_out(OutShared<D>& sh, const LinBatch& batch,
     const int c = chunk_of(ci), n = rows_of(c);
     const bool more = ci + 1 < chunks;
     const float fade = exp2f(lg * (float)n);
-    // x of the first head (reverse: y and z) is on its way already; what only a chunk's first head brings is not fetched
-    // ahead, that would take too many registers
     if constexpr (REV) {
-      Stage a;
-      fetch_x(a, ci, 0);
       __syncthreads();
-      a.put(sh.xt, dst);
+      s2.put(sh.xt, dst);
       if (n != row_n) set_row_decays<REV>(sh.decays, lg, n), row_n = n;
       __syncthreads();
       from_state(n);
-      scale_state<NT>(s, fade);
+      fade_state(fade);
       for (int h = 0; h < g; ++h) {
         if (h > 0) __syncthreads();  // the tiles of the head before have been read
         s0.put(sh.yt, dst);
         s1.put(sh.zt, dst);
         __syncthreads();
         if (h + 1 < g) fetch_yz(s0, s1, ci, h + 1);
-        else if (more) fetch_yz(s0, s1, ci + 1, 0);
-        const bf16x8 zf[2] = {read_columns<D>(sh.zt, zbase, 0, 0), read_columns<D>(sh.zt, zbase, 0, 1)};
+        else if (more) fetch_yz(s0, s1, ci + 1, 0), fetch_x(s2, ci + 1, 0);
+        bf16x8 zf[4];
+#pragma unroll
+        for (int m = 0; m < 4; ++m) zf[m] = read_columns32<D>(sh.zt, zbase, 0, m);
         p_tiles();
+        update(zf);
         __syncthreads();
         from_chunk(zf);
-        update_state<D, PAIRED, 2>(s, sh.yt, zf, ybase, sh.decays.row, q);
       }
       store(c, 0, n);
     } else {
-      {
-        Stage a, b;
-        fetch_yz(a, b, ci, 0);
-        __syncthreads();
-        a.put(sh.yt, dst);
-        b.put(sh.zt, dst);
-        if (n != row_n) set_row_decays<REV>(sh.decays, lg, n), row_n = n;
-      }
-      bf16x8 zf[2];
+      __syncthreads();
+      s1.put(sh.yt, dst);
+      s2.put(sh.zt, dst);
+      if (n != row_n) set_row_decays<REV>(sh.decays, lg, n), row_n = n;
+      bf16x8 zf[4];
       for (int h = 0; h < g; ++h) {
         if (h > 0) __syncthreads();
         s0.put(sh.xt, dst);
         __syncthreads();
         if (h + 1 < g) fetch_x(s0, ci, h + 1);
-        else if (more) fetch_x(s0, ci + 1, 0);
-        if (h == 0) zf[0] = read_columns<D>(sh.zt, zbase, 0, 0), zf[1] = read_columns<D>(sh.zt, zbase, 0, 1);
+        else if (more) fetch_x(s0, ci + 1, 0), fetch_yz(s1, s2, ci + 1, 0);
+        if (h == 0) {
+#pragma unroll
+          for (int m = 0; m < 4; ++m) zf[m] = read_columns32<D>(sh.zt, zbase, 0, m);
+        }
         p_tiles();
         // (the state's two terms are formed again for every head: kept over the loop they take registers, which then
         // spill. The empty asm keeps the compiler from doing that.)
 #pragma unroll
-        for (int t = 0; t < NT; ++t) asm volatile("" : "+v"(s[t]));
+        for (int t = 0; t < NW; ++t) asm volatile("" : "+v"(s[t]));
         from_state(n);
         __syncthreads();
         from_chunk(zf);
         store(c, h, n);
       }
       if (more) {
-        scale_state<NT>(s, fade);
-        update_state<D, PAIRED, 2>(s, sh.yt, zf, ybase, sh.decays.row, q);
+        fade_state(fade);
+        update(zf);
       }
     }
   }
 }
 
 template <int D>
-__global__ __launch_bounds__(4 * D, 4) void lin_out_kernel(LinOutParams p) {
+__global__ __launch_bounds__(2 * D, 2) void lin_out_kernel(LinOutParams p) {
   __shared__ OutShared<D> sh;
   const int block = blockIdx.x / p.b.heads_kv, kvh = blockIdx.x - block * p.b.heads_kv;
   const Block bl = find_block(p.b, block);
@@ -671,7 +729,7 @@ __global__ __launch_bounds__(4 * D, 4) void lin_out_kernel(LinOutParams p) {
 // one XCD (workgroups go to the 8 XCDs in turn), so that what they share of q,
 // k, v and do comes from memory once.
 template <int D>
-__global__ __launch_bounds__(4 * D, 4) void lin_grad_kernel(LinGradParams p) {
+__global__ __launch_bounds__(2 * D, 2) void lin_grad_kernel(LinGradParams p) {
   __shared__ OutShared<D> sh;
   const int j = blockIdx.x >> 3, unit = (j / 3) * 8 + (blockIdx.x & 7), role = j % 3;
   if (unit >= p.b.num_blocks * p.b.heads_kv) return;
@@ -726,15 +784,15 @@ hipError_t launch_lin_scan(const LinScanParams& p, int head_dim, bool reverse, i
 
 hipError_t launch_lin_out(const LinOutParams& p, int head_dim, hipStream_t stream) {
   const dim3 grid(p.b.num_blocks * p.b.heads_kv);
-  if (head_dim == 128) lin_out_kernel<128><<<grid, 512, 0, stream>>>(p);
-  else lin_out_kernel<64><<<grid, 256, 0, stream>>>(p);
+  if (head_dim == 128) lin_out_kernel<128><<<grid, 256, 0, stream>>>(p);
+  else lin_out_kernel<64><<<grid, 128, 0, stream>>>(p);
   return hipGetLastError();
 }
 
 hipError_t launch_lin_grad(const LinGradParams& p, int head_dim, hipStream_t stream) {
   const dim3 grid((p.b.num_blocks * p.b.heads_kv + 7) / 8 * 24);
-  if (head_dim == 128) lin_grad_kernel<128><<<grid, 512, 0, stream>>>(p);
-  else lin_grad_kernel<64><<<grid, 256, 0, stream>>>(p);
+  if (head_dim == 128) lin_grad_kernel<128><<<grid, 256, 0, stream>>>(p);
+  else lin_grad_kernel<64><<<grid, 128, 0, stream>>>(p);
   return hipGetLastError();
 }
 
