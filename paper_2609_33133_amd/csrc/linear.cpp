@@ -106,17 +106,19 @@ int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // (written, scanned and read: 16 d^2 bytes, as much as 4 d / (1 + group) rows'
 // own traffic). The rows that make these rounds shortest are taken. The tree
 // alone decides, so that its results do not depend on the batch. (32768-token
-// prompt, eight branches of 2048, 32 / 8 heads, forward + backward: RULE_US.)
+// prompt, eight branches of 2048, 32 / 8 heads, forward + backward: 1376 us with blocks
+// of 512 or 1024 rows, 1260 with the 832 rows that fill one round exactly.)
 int block_rows(const augtree_groups* g, int tree) {
   const int d = g->head_dim, hkv = g->num_kv_heads, nb = g->num_branches;
   const int64_t slots = d == 128 ? 512 : 1024;
+  auto blocks = [](int32_t len, uint32_t rows) { return ((uint32_t)len + rows - 1) / rows; };
   const double state = 4.0 * d / (1 + g->num_q_heads / hkv);
   int best = 0;
   double best_cost = 0;
   for (int rows = 128; rows <= 1024; rows += kLinChunk) {
-    int64_t units = cdiv(g->cu_prompt[tree + 1] - g->cu_prompt[tree], rows);
+    int64_t units = blocks(g->cu_prompt[tree + 1] - g->cu_prompt[tree], rows);
     for (int b = nb ? g->cu_branch[tree] : 0; nb && b < g->cu_branch[tree + 1]; ++b)
-      units += cdiv(g->cu_resp[b + 1] - g->cu_resp[b], rows);
+      units += blocks(g->cu_resp[b + 1] - g->cu_resp[b], rows);
     units *= hkv;
     const double cost = (double)(cdiv(units, slots) + cdiv(3 * units, slots)) * (rows + state);
     if (!best || cost < best_cost) best = rows, best_cost = cost;
@@ -221,10 +223,9 @@ struct Call {
     return AUGTREE_OK;
   }
 
-  // states[block] <- what reaches the block. exact: as fp32 sums would have it; the forward's states always are, so that
-  // its outputs do not depend on whether they are handed out.
+  // states[block] <- what reaches the block
   int states(bool reverse, const uint16_t* const y[2], const uint16_t* const z[2], const float* init, float* states,
-             float* ends, float* out_p, float* out_r, bool exact) {
+             float* ends, float* out_p, float* out_r) {
     const bool branches = g->num_branches > 0;
     LinStateParams s;
     std::memset(&s, 0, sizeof(s));
@@ -237,7 +238,7 @@ struct Call {
     s.b = b;
     {
       Hook h(reverse ? "linear_state_rev" : "linear_state", stream);
-      if (int st = hip_ok(launch_lin_state(s, g->head_dim, reverse, exact, stream), "state launch")) return st;
+      if (int st = hip_ok(launch_lin_state(s, g->head_dim, reverse, stream), "state launch")) return st;
     }
     LinScanParams c;
     std::memset(&c, 0, sizeof(c));
@@ -250,7 +251,8 @@ struct Call {
     c.skip_branch = s.skip_branch;
     c.b = b;
     // A tree's blocks are scanned by one launch, its branches one after the other, where they are few; else prompts and
-    // branches get a launch each, in which the branches run side by side (SPLIT_US).
+    // branches get a launch each, in which the branches run side by side. (49152 rows in 64 blocks: 12 us against 22;
+    // 264192 rows in 258 blocks, 16 branches: 30 us in two launches.)
     const bool split = branches && L.longest > kScanBlocks;
     for (int k = 0; k < (split ? 2 : 1); ++k) {
       const int part = !split ? 0 : (k == 0) != reverse ? 1 : 2;
@@ -326,7 +328,7 @@ int augtree_linear_fwd(const augtree_groups* grp, const float* decay, const uint
     float* const tree = c.take<float>(c.L.tree * grp->num_groups);
     const uint16_t *const q[2] = {q_p, q_r}, *const k[2] = {k_p, k_r}, *const v[2] = {v_p, v_r};
     uint16_t* const o[2] = {o_p, o_r};
-    if ((st = c.states(false, k, v, state, states, tree, state_p, state_r, true))) return st;
+    if ((st = c.states(false, k, v, state, states, tree, state_p, state_r))) return st;
     LinOutParams p;
     std::memset(&p, 0, sizeof(p));
     for (int i = 0; i < 2; ++i) p.q[i] = q[i], p.k[i] = k[i], p.v[i] = v[i], p.o[i] = o[i];
@@ -378,9 +380,9 @@ int augtree_linear_bwd(const augtree_groups* grp, const float* decay, const uint
       fwd = reinterpret_cast<const float*>(static_cast<const char*>(fwd_ws) + align_up(c.L.segs.size() * sizeof(LinSeg)));
     } else {
       fwd = own;
-      if ((st = c.states(false, k, v, state, own, tree, nullptr, nullptr, true))) return st;
+      if ((st = c.states(false, k, v, state, own, tree, nullptr, nullptr))) return st;
     }
-    if ((st = c.states(true, q, g, nullptr, rev, ends, nullptr, nullptr, false))) return st;
+    if ((st = c.states(true, q, g, nullptr, rev, ends, nullptr, nullptr))) return st;
     LinGradParams p;
     std::memset(&p, 0, sizeof(p));
     for (int i = 0; i < 2; ++i) {

@@ -87,8 +87,7 @@ struct LinTable {
 static_assert(sizeof(LinTable) <= 4096, "kernel arguments");
 
 hipError_t launch_lin_table(const LinTable& t, hipStream_t stream);
-// exact: sums to fp32 accuracy (states that are handed out)
-hipError_t launch_lin_state(const LinStateParams& p, int head_dim, bool reverse, bool exact, hipStream_t stream);
+hipError_t launch_lin_state(const LinStateParams& p, int head_dim, bool reverse, hipStream_t stream);
 // part: 0 whole trees, 1 prompts, 2 branches (1 and 2 hand over through `ends`, in the order of the direction)
 hipError_t launch_lin_scan(const LinScanParams& p, int head_dim, bool reverse, int part, hipStream_t stream);
 hipError_t launch_lin_out(const LinOutParams& p, int head_dim, hipStream_t stream);

@@ -12,21 +12,29 @@
 // [d, d] in fp32. Three steps: each block's own state (lin_state_kernel), a scan
 // of the blocks' states along a segment and from the prompt into its branches,
 // or from the branches back onto the prompt (lin_scan_kernel), and the outputs,
-// every block from the state that reaches it (lin_out_kernel).
+// every block from the state that reaches it (lin_out_kernel, lin_grad_kernel).
 //
-// A workgroup has one wavefront for every 16 columns of z (8 for d = 128). The
-// state's columns stay in that wavefront's accumulators (rows: y, column of the
-// lane: z) and serve from there as an operand of the next product, whose k index
-// runs over y. Small tiles (16x16x32 products) keep a wavefront below 128
-// registers: with 16 wavefronts on a CU the LDS reads in front of the matrix
-// instructions are covered; 4 wavefronts of 32 columns each (32x32x16, 244
-// registers, 8 on a CU) took 305 us where these take OUT_US (49152 rows, 32 / 8
-// heads, d = 128, forward).
+// Each wavefront owns columns of z (16 in the state kernel, 32 in the others).
+// The state's columns stay in its accumulators (rows: y, column of the lane: z)
+// and serve from there as an operand of the next product, whose k index runs
+// over y.
 //
 // Roundings to bf16, all of them operands of matrix products: P, the decayed z of
 // the state's update and the state itself as an operand are each split into two
-// bf16 terms (2^-17 of an element), or z into three (2^-25) where the state is
-// handed out in fp32.
+// bf16 terms (2^-17 of an element), or z into three (2^-25) in the forward's
+// states, which are handed out in fp32. So results are as exact as their own
+// rounding; the low terms are 45 % of the matrix instructions and cost about a
+// sixth of the time.
+//
+// What bounds it (49152 rows, 32 / 8 heads, d = 128; a copy reaches 4.9 TB/s
+// here): the forward's output kernel moves 1.1 GB in 250 us, 4.4 TB/s, and the
+// state kernels 3.5 TB/s forward and 6.4 in reverse (partly from the Infinity
+// Cache). The gradient kernel moves 1.5 GB of HBM in 700 us and is bound by its
+// work on the CU: per 64 rows of a head and role about 5400 cycles, 59 % of them
+// matrix instructions, at the clock that the chip's power leaves. Other shapes of
+// it took the same time within 3 %: 8 wavefronts of 16 columns (four on a SIMD
+// instead of two, but 2.4 times the LDS reads), P in 32 x 32 tiles, wavefront
+// priorities.
 #include "common.h"
 #include "linear.h"
 
@@ -77,7 +85,6 @@ __device__ __forceinline__ Block find_block(const LinBatch& b, int block) {
 // 16x16x32 products: lane l holds row (column) l % 16 of the first (second)
 // operand, k indices 8 (l / 16) .. + 7; of the result column l % 16, rows
 // 4 (l / 16) + 0..3.
-
 __device__ __forceinline__ f32x4 mfma16(const bf16x8& a, const bf16x8& b, const f32x4& c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
@@ -112,7 +119,7 @@ template <int D>
 __device__ __forceinline__ int column_base(int col, int lane) {
   return 2 * loff<D>(8 * (lane >> 4) + ((lane & 15) >> 2), col);
 }
-// `base`: byte offset of the named columns; FLIP: bytes by which the columns wanted differ from them (bits of the
+// `base`: byte offset of the named columns; `flip`: bytes by which the columns wanted differ from them (bits of the
 // swizzled piece, so an exclusive or)
 template <int D>
 __device__ __forceinline__ bf16x8 read_columns(const __bf16* tile, int base, int flip, int m) {
@@ -133,23 +140,15 @@ __device__ __forceinline__ int here(int base) {
   return base;
 }
 
-// Rows of the state (columns of y) in the accumulators: register i of tile t in
-// lane quarter q. Tiles 2s and 2s + 1 are k step s of the product with x, whose
-// lanes need the same 8 columns of x. Plain: 16 t + 4 q + i, so x is read in two
-// pieces of four columns. PAIRED: the two tiles take every other four columns,
-// and x is read in pieces of eight; but then the transpose reads of y touch every
-// other 8 bytes, two lanes a bank. Paired pays where x is read once a head and y
-// once a chunk (forward), plain in reverse.
-template <bool PAIRED>
-__device__ __forceinline__ int state_row(int t, int q, int i) {
-  return PAIRED ? 32 * (t >> 1) + 8 * q + 4 * (t & 1) + i : 16 * t + 4 * q + i;
-}
-
-// a and b as bf16, a in the low half. (Two conversions in one instruction, which
-// the compiler does not always find.)
+// a and b as bf16, a in the low half: one instruction. (An inline asm of it would
+// hide from the compiler that a matrix instruction reading the result has to wait.)
 __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  const f32x2 v = {a, b};
+  const bf16x2 w = __builtin_convertvector(v, bf16x2);
   uint32_t r;
-  asm("v_cvt_pk_bf16_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+  __builtin_memcpy(&r, &w, 4);
   return r;
 }
 
@@ -195,7 +194,7 @@ __device__ __forceinline__ void set_pair_decays(Decays& t, float lg) {
 
 // s += Y^T (w Z) of one chunk: rows y (of all of Y's D columns), columns z (16 of
 // this wavefront, in zf). TERMS bf16 terms of the weighted z.
-template <int D, bool PAIRED, int TERMS>
+template <int D, int TERMS>
 __device__ __forceinline__ void update_state(f32x4* s, const __bf16* yt, const bf16x8* zf, int ybase, const float* w,
                                              int q) {
   const int yb = here(ybase);
@@ -216,7 +215,7 @@ __device__ __forceinline__ void update_state(f32x4* s, const __bf16* yt, const b
     }
 #pragma unroll
     for (int t = 0; t < D / 16; ++t) {
-      const bf16x8 a = read_columns<D>(yt, yb, PAIRED ? 64 * (t >> 1) + 8 * (t & 1) : 32 * t, m);
+      const bf16x8 a = read_columns<D>(yt, yb, 32 * t, m);
 #pragma unroll
       for (int k = 0; k < TERMS; ++k) s[t] = mfma16(a, b[k], s[t]);
     }
@@ -231,8 +230,9 @@ __device__ __forceinline__ void scale_state(f32x4* s, float f) {
 
 // A [64, D] tile on its way from memory to LDS through registers: fetch()
 // issues the loads, put() waits for them and writes the swizzled tile. The loads
-// of the next tiles are in flight while a chunk is worked on, and LDS holds one
-// tile of each operand, so that two workgroups fit a CU. Rows from n on are zeros.
+// of the next tiles are in flight while a chunk is worked on (they arrive before
+// they are waited for: 110 cycles of a 5400-cycle step), and LDS holds one tile of
+// each operand, so that two workgroups fit a CU. Rows from n on are zeros.
 template <int D, int NW>
 struct TileStage {
   static constexpr int CH = D / 8, RPI = 64 / CH, ROWS = NW * RPI, NI = C / ROWS;  // pieces of a row; rows of a pass
@@ -268,9 +268,10 @@ struct TileStage {
 
 // ---------------------------------------------------------------------------- blocks' own states
 
-template <int D, bool REV, int TERMS>
+template <int D, bool REV>
 __global__ __launch_bounds__(4 * D, 4) void lin_state_kernel(LinStateParams p) {
-  constexpr int NT = D / 16;  // tiles of the state's rows, and wavefronts
+  constexpr int NT = D / 16;            // tiles of the state's rows, and wavefronts
+  constexpr int TERMS = REV ? 2 : 3;    // forward states may be handed out
   __shared__ __attribute__((aligned(1024))) __bf16 yt[C * D];
   __shared__ __attribute__((aligned(1024))) __bf16 zt[C * D];
   __shared__ __attribute__((aligned(16))) Decays decays;
@@ -315,14 +316,14 @@ __global__ __launch_bounds__(4 * D, 4) void lin_state_kernel(LinStateParams p) {
       if (h + 1 < gy) fetch(ci, h + 1);
       else if (ci + 1 < chunks) fetch(ci + 1, 0);
       const bf16x8 zf[2] = {read_columns<D>(zt, zbase, 0, 0), read_columns<D>(zt, zbase, 0, 1)};
-      update_state<D, false, TERMS>(s, yt, zf, ybase, decays.row, q);
+      update_state<D, TERMS>(s, yt, zf, ybase, decays.row, q);
     }
   }
   float* out = p.states + ((int64_t)block * p.b.heads_kv + kvh) * D * D + 16 * wave + (lane & 15);
 #pragma unroll
   for (int t = 0; t < NT; ++t)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) out[state_row<false>(t, q, i) * D] = s[t][i];
+    for (int i = 0; i < 4; ++i) out[(16 * t + 4 * q + i) * D] = s[t][i];
 }
 
 // ---------------------------------------------------------------------------- scan
@@ -338,8 +339,9 @@ struct Scan {
   __device__ __forceinline__ void store(float* base, int64_t i, f32x4 v) const {
     *reinterpret_cast<f32x4*>(base + i * per + at) = v;
   }
-  // One segment: every block's own state is replaced by the carry that reaches it. Eight blocks are loaded ahead: with
-  // one at a time 32 blocks took 11 us where these take SCAN_US.
+  // One segment: every block's own state is replaced by the carry that reaches it. Eight blocks are loaded ahead: a scan
+  // of 48 MB of states then takes 12 us, which is the time of reading and writing them (one at a time, prompts and
+  // branches in a launch each: 22 us).
   template <bool REV>
   __device__ __forceinline__ f32x4 segment(const LinSeg& s, f32x4 carry, bool skip) const {
     constexpr int kAhead = 8;
@@ -348,8 +350,8 @@ struct Scan {
       f32x4 own[kAhead];
 #pragma unroll
       for (int k = 0; k < kAhead; ++k) {
-        const int i = min(i0 + k, last);
-        own[k] = load(p.states, s.block0 + (REV ? last - i : i));
+        const int i = i0 + k;
+        if (i < count) own[k] = load(p.states, s.block0 + (REV ? last - i : i));
       }
 #pragma unroll
       for (int k = 0; k < kAhead; ++k) {
@@ -525,6 +527,8 @@ __device__ __forceinline__ void lin_out(OutShared<D>& sh, const LinBatch& batch,
   const int rbase = 2 * loff<D>(l32, 8 * hf);
   const int pbase = 2 * poff(l32, hf);
   set_pair_decays<2 * D>(sh.decays, lg);
+  // the 16 x 16 tiles of P beside the diagonal that are masked stay zero
+  for (int i = threadIdx.x; i < 2 * 3 * 32 * 32 / 8; i += 2 * D) reinterpret_cast<raw16*>(sh.pt)[i] = raw16{0u, 0u, 0u, 0u};
 
   // the state that reaches the block
   f32x16 s[NW];
@@ -543,38 +547,42 @@ __device__ __forceinline__ void lin_out(OutShared<D>& sh, const LinBatch& batch,
   auto read8 = [&](const __bf16* tile, int base, int half, int ks) {
     return *reinterpret_cast<const bf16x8*>(reinterpret_cast<const char*>(tile) + half * 64 * D + (base ^ (32 * ks)));
   };
-  // Tile k of P (rows x, columns y): P^T is formed, [32 y] x [32 x], a lane having one x.
-  auto p_tile = [&](int k) {
-    const int ty = REV ? (k > 0) : (k == 2), tx = REV ? (k == 2) : (k > 0);
-    const float* const pw = sh.decays.pair + 32 + (REV ? 4 * hf - l32 : l32 - 4 * hf) + (k == 1 ? 32 : 0);
-    const int rb = here(rbase);
-    f32x16 acc;
+  // P^T in 16 x 16 tiles (16x16x32 products, a lane having one x and four y), of which the 10 on and beside the diagonal
+  // are dealt to the wavefronts: tile k is (i, j), j <= i, with i (i + 1) / 2 + j = k. (The three 32 x 32 tiles they make
+  // up leave one of four wavefronts without one.)
+  const int q = lane >> 4, l16 = lane & 15;
+  const int rbase16 = 2 * loff<D>(l16, 8 * q);
+  auto p_tile = [&](int ty, int tx) {
+    const int rb = here(rbase16);
+    const char* const yt = reinterpret_cast<const char*>(sh.yt) + ty * 32 * D;
+    const char* const xt = reinterpret_cast<const char*>(sh.xt) + tx * 32 * D;
+    f32x4 a = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < 16; ++i) acc[i] = 0.f;
+    for (int ks = 0; ks < D / 32; ++ks)
+      a = mfma16(*reinterpret_cast<const bf16x8*>(yt + (rb ^ (64 * ks))),
+                 *reinterpret_cast<const bf16x8*>(xt + (rb ^ (64 * ks))), a);
+    const float* const pw = sh.decays.pair + 32 + (REV ? 16 * (ty - tx) + 4 * q - l16 : 16 * (tx - ty) + l16 - 4 * q);
+    u32x2 v, u;
 #pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks) acc = mfma32(read8(sh.yt, rb, ty, ks), read8(sh.xt, rb, tx, ks), acc);
-#pragma unroll
-    for (int qd = 0; qd < 4; ++qd) {
-      u32x2 v, u;
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int i = 4 * qd + 2 * e, at = 8 * qd + 2 * e;
-        const float f0 = acc[i] * pw[REV ? at : -at], f1 = acc[i + 1] * pw[REV ? at + 1 : -at - 1];
-        v[e] = bf16_pair(f0, f1);
-        u[e] = bf16_pair(f0 - __uint_as_float(v[e] << 16), f1 - __uint_as_float(v[e] & 0xffff0000u));
-      }
-      // k step qd / 2 of the tile, in the order of the transposed z: piece 2 (qd / 2) + hf, half qd % 2
-      const int o = poff(l32, 2 * (qd >> 1) + hf) + 4 * (qd & 1);
-      *reinterpret_cast<u32x2*>(sh.pt[0][k] + o) = v;
-      *reinterpret_cast<u32x2*>(sh.pt[1][k] + o) = u;
+    for (int e = 0; e < 2; ++e) {
+      const float f0 = a[2 * e] * pw[REV ? 2 * e : -2 * e], f1 = a[2 * e + 1] * pw[REV ? 2 * e + 1 : -2 * e - 1];
+      v[e] = bf16_pair(f0, f1);
+      u[e] = bf16_pair(f0 - __uint_as_float(v[e] << 16), f1 - __uint_as_float(v[e] & 0xffff0000u));
     }
+    // in the order of the transposed z: y = 4 q of k step ty % 2 is piece 2 (ty % 2) + q % 2, half q / 2
+    const int k = (ty >> 1) == (tx >> 1) ? 2 * (tx >> 1) : 1;
+    const int o = poff(16 * (tx & 1) + l16, 2 * (ty & 1) + (q & 1)) + 4 * (q >> 1);
+    *reinterpret_cast<u32x2*>(sh.pt[0][k] + o) = v;
+    *reinterpret_cast<u32x2*>(sh.pt[1][k] + o) = u;
   };
   auto p_tiles = [&]() {
-    if constexpr (NW == 4) {
-      if (wave < 3) p_tile(wave);
-    } else {
-      if (wave == 0) p_tile(0), p_tile(2);
-      else p_tile(1);
+#pragma unroll
+    for (int r = 0; r < (10 + NW - 1) / NW; ++r) {
+      const int k = r * NW + wave;
+      if (k >= 10) break;
+      const int i = (k >= 1) + (k >= 3) + (k >= 6), j = k - i * (i + 1) / 2;
+      if (REV) p_tile(i, j);
+      else p_tile(j, i);
     }
   };
 
@@ -760,16 +768,14 @@ hipError_t launch_lin_table(const LinTable& t, hipStream_t stream) {
   return hipGetLastError();
 }
 
-hipError_t launch_lin_state(const LinStateParams& p, int head_dim, bool reverse, bool exact, hipStream_t stream) {
+hipError_t launch_lin_state(const LinStateParams& p, int head_dim, bool reverse, hipStream_t stream) {
   const dim3 grid(p.b.num_blocks * p.b.heads_kv);
   if (head_dim == 128) {
-    if (reverse) lin_state_kernel<128, true, 2><<<grid, 512, 0, stream>>>(p);
-    else if (exact) lin_state_kernel<128, false, 3><<<grid, 512, 0, stream>>>(p);
-    else lin_state_kernel<128, false, 2><<<grid, 512, 0, stream>>>(p);
+    if (reverse) lin_state_kernel<128, true><<<grid, 512, 0, stream>>>(p);
+    else lin_state_kernel<128, false><<<grid, 512, 0, stream>>>(p);
   } else {
-    if (reverse) lin_state_kernel<64, true, 2><<<grid, 256, 0, stream>>>(p);
-    else if (exact) lin_state_kernel<64, false, 3><<<grid, 256, 0, stream>>>(p);
-    else lin_state_kernel<64, false, 2><<<grid, 256, 0, stream>>>(p);
+    if (reverse) lin_state_kernel<64, true><<<grid, 256, 0, stream>>>(p);
+    else lin_state_kernel<64, false><<<grid, 256, 0, stream>>>(p);
   }
   return hipGetLastError();
 }
