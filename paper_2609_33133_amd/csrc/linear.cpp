@@ -115,7 +115,7 @@ int block_rows(const augtree_groups* g, int tree) {
   const double state = 4.0 * d / (1 + g->num_q_heads / hkv);
   int best = 0;
   double best_cost = 0;
-  for (int rows = 128; rows <= 1024; rows += kLinChunk) {
+  for (int rows = kLinChunk; rows <= 1024; rows += kLinChunk) {
     int64_t units = blocks(g->cu_prompt[tree + 1] - g->cu_prompt[tree], rows);
     for (int b = nb ? g->cu_branch[tree] : 0; nb && b < g->cu_branch[tree + 1]; ++b)
       units += blocks(g->cu_resp[b + 1] - g->cu_resp[b], rows);

@@ -29,10 +29,11 @@
 // What bounds it (49152 rows, 32 / 8 heads, d = 128; a copy reaches 4.9 TB/s
 // here): the forward's output kernel moves 1.1 GB in 250 us, 4.4 TB/s, and the
 // state kernels 3.5 TB/s forward and 6.4 in reverse (partly from the Infinity
-// Cache). The gradient kernel moves 1.5 GB of HBM in 700 us and is bound by its
-// work on the CU: per 64 rows of a head and role about 5400 cycles, 59 % of them
-// matrix instructions, at the clock that the chip's power leaves. Other shapes of
-// it took the same time within 3 %: 8 wavefronts of 16 columns (four on a SIMD
+// Cache). The gradient kernel moves 2.3 GB past the L2s (1.7 read: dv and dk share
+// theirs, dq runs the other way through time) in 700 us, 3.3 TB/s, and has about
+// as much work on the CU: per 64 rows of a head and role about 5400 cycles of a CU
+// that two workgroups share, 59 % of them matrix instructions, at the 1.9 GHz that
+// the chip's power leaves of 2.4. Other shapes of it took the same time within 3 %: 8 wavefronts of 16 columns (four on a SIMD
 // instead of two, but 2.4 times the LDS reads), P in 32 x 32 tiles, wavefront
 // priorities.
 #include "common.h"

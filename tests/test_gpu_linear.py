@@ -69,7 +69,7 @@ def test_backward_from_the_forwards_workspace():
 
 
 def test_many_blocks_scan_branches_side_by_side():
-    """More blocks in a tree than one scan launch takes: 64 at 128 rows."""
+    """More blocks in a tree than one scan launch takes (64)."""
     b = batch([(4500, [1300, 2500, 1]), (70, [300])], 1, 1, 64)
     dec = decays(1, 8.0, 8.0)
     x = inputs(b, 25)
