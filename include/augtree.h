@@ -381,7 +381,8 @@ int augtree_prompt_grad_reduce(int32_t n_tensors, int64_t rows, int32_t heads, i
  * products, so a NaN or infinity in one row may reach earlier rows of its
  * chunk too; it never reaches another tree, or from a branch any other branch.
  * Every call enqueues kernels only and may be captured into a graph; calls that
- * share a workspace must not overlap (as for all entry points).
+ * share a workspace must not overlap (as for all entry points). Outputs must lie
+ * apart from the inputs and from one another, but for what is named below.
  * Results are bitwise reproducible and a tree's do not depend on the batch.
  * ------------------------------------------------------------------------- */
 
@@ -396,6 +397,7 @@ size_t augtree_linear_workspace_size(const augtree_groups* grp, int backward);
  * Out: o_p [T_P,Hq,d], o_r [T_R,Hq,d] bf16; state_p [num_groups,Hkv,d,d], state_r
  *      [num_branches,Hkv,d,d] fp32: the states after each prompt and each branch
  *      (nullable), for augtree_linear_step or the next piece of a sequence.
+ *      state_p may be state.
  * num_branches = 0 is a batch of plain sequences: cu_branch and cu_resp are not
  * read and the response pointers may be NULL. softmax_scale is s.
  */
@@ -445,14 +447,15 @@ typedef enum augtree_activation { AUGTREE_ACT_NONE = 0, AUGTREE_ACT_SILU = 1 } a
  *   y = act(a),  or with a gate  y = a * act(gate);  act(u) = u / (1 + exp(-u)) (SILU) or u (NONE).
  * In:  x, gate (nullable) [rows,heads,head_dim] bf16; weight, bias (each
  *      nullable: 1 and 0) [heads,head_dim] fp32. head_dim a multiple of 8, at most 1024.
- * Out: y like x. rows = 0 is a no-op.
+ * Out: y like x (it may be x or gate itself). rows = 0 is a no-op.
  */
 int augtree_head_norm_fwd(int64_t rows, int32_t heads, int32_t head_dim, int activation, float eps,
                           const uint16_t* x, const uint16_t* gate, const float* weight, const float* bias,
                           uint16_t* y, void* stream);
 
 /*
- * Its backward. In: as forward, dy like y. Out: dx, dgate (with a gate) bf16;
+ * Its backward. In: as forward, dy like y. Out: dx, dgate (with a gate) bf16
+ * (each may be x, gate or dy itself, not both the same);
  * dweight, dbias [heads,head_dim] fp32 (each nullable), summed over the rows in a
  * fixed order. The workspace (augtree_head_norm_workspace_size bytes) is needed
  * for dweight or dbias only. rows = 0 writes zeros to them.

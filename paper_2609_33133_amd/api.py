@@ -321,10 +321,13 @@ class _On:
         self.device, self.stream, self.guard = dev, stream, None
 
     def __enter__(self):
-        if self.device.index != torch.cuda.current_device():
+        if self.stream is not None:  # what is allocated inside belongs to that stream
+            self.guard = torch.cuda.stream(self.stream)
+        elif self.device.index != torch.cuda.current_device():
             self.guard = torch.cuda.device(self.device)
+        if self.guard is not None:
             self.guard.__enter__()
-        return (torch.cuda.current_stream() if self.stream is None else self.stream).cuda_stream
+        return torch.cuda.current_stream().cuda_stream
 
     def __exit__(self, *exc):
         if self.guard is not None:
@@ -333,6 +336,12 @@ class _On:
 
 def _addr(t):
     return None if t is None else t.data_ptr()
+
+
+def _want(t: torch.Tensor, name: str, dtype, shape):
+    """_need for tensors that _On has seen, quick where there is nothing to say."""
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
+        _need(t, name, dtype, shape)
 
 
 def _decay(decay, heads: int) -> np.ndarray:
@@ -355,7 +364,7 @@ def _decay(decay, heads: int) -> np.ndarray:
 def _out(t, name, dtype, shape, device):
     if t is None:
         return torch.empty(shape, dtype=dtype, device=device)
-    _need(t, name, dtype, shape)
+    _want(t, name, dtype, shape)
     return t
 
 
@@ -377,7 +386,7 @@ def _linear_ws(b, backward, ws, device):
 def _linear_inputs(b: GroupBatch, named):
     for n, t in named:
         rows = b.tp if n.endswith("_p") else b.tr
-        _need(t, n, torch.bfloat16, (rows, b.hkv if n[0] in "kv" else b.hq, b.d))
+        _want(t, n, torch.bfloat16, (rows, b.hkv if n[0] in "kv" else b.hq, b.d))
 
 
 def linear_fwd(b: GroupBatch, decay, q_p, k_p, v_p, q_r, k_r, v_r, state=None, o_p=None, o_r=None, state_p=None,
@@ -392,23 +401,20 @@ def linear_fwd(b: GroupBatch, decay, q_p, k_p, v_p, q_r, k_r, v_r, state=None, o
     _linear_inputs(b, named)
     dev, f32 = on.device, torch.float32
     if state is not None:
-        _need(state, "state", f32, (b.num_groups, b.hkv, b.d, b.d))
-    o_p = _out(o_p, "o_p", torch.bfloat16, q_p.shape, dev)
-    o_r = _out(o_r, "o_r", torch.bfloat16, q_r.shape, dev)
-    if want_states or state_p is not None:
-        state_p = _out(state_p, "state_p", f32, (b.num_groups, b.hkv, b.d, b.d), dev)
-    if want_states or state_r is not None:
-        state_r = _out(state_r, "state_r", f32, (b.num_branches, b.hkv, b.d, b.d), dev)
-    _linear_fwd(b, dec, (q_p, k_p, v_p, q_r, k_r, v_r, state, o_p, o_r, state_p, state_r if b.num_branches else None),
-                _linear_ws(b, False, ws, dev), on)
-    return o_p, o_r, state_p, state_r
-
-
-def _linear_fwd(b: GroupBatch, dec, tensors, ws, on: _On):
-    """The call of linear_fwd behind its checks: inputs, state and outputs in the order of augtree_linear_fwd."""
+        _want(state, "state", f32, (b.num_groups, b.hkv, b.d, b.d))
     with on as st:
-        _lib.check(_lib.load().augtree_linear_fwd(b.ref, dec.ctypes.data, *(_addr(t) for t in tensors), _addr(ws),
-                                                  ws.numel(), st), "linear_fwd")
+        o_p = _out(o_p, "o_p", torch.bfloat16, q_p.shape, dev)
+        o_r = _out(o_r, "o_r", torch.bfloat16, q_r.shape, dev)
+        if want_states or state_p is not None:
+            state_p = _out(state_p, "state_p", f32, (b.num_groups, b.hkv, b.d, b.d), dev)
+        if want_states or state_r is not None:
+            state_r = _out(state_r, "state_r", f32, (b.num_branches, b.hkv, b.d, b.d), dev)
+        ws = _linear_ws(b, False, ws, dev)
+        _lib.check(_lib.load().augtree_linear_fwd(
+            b.ref, dec.ctypes.data, _addr(q_p), _addr(k_p), _addr(v_p), _addr(q_r), _addr(k_r), _addr(v_r), _addr(state),
+            _addr(o_p), _addr(o_r), _addr(state_p), _addr(state_r) if b.num_branches else None, _addr(ws), ws.numel(),
+            st), "linear_fwd")
+    return o_p, o_r, state_p, state_r
 
 
 def linear_bwd(b: GroupBatch, decay, q_p, k_p, v_p, do_p, q_r, k_r, v_r, do_r, state=None, dq_p=None, dk_p=None,
@@ -423,20 +429,21 @@ def linear_bwd(b: GroupBatch, decay, q_p, k_p, v_p, do_p, q_r, k_r, v_r, do_r, s
     _linear_inputs(b, named)
     dev = on.device
     if state is not None:
-        _need(state, "state", torch.float32, (b.num_groups, b.hkv, b.d, b.d))
-    outs = [_out(t, n, torch.bfloat16, like.shape, dev)
-            for t, n, like in ((dq_p, "dq_p", q_p), (dk_p, "dk_p", k_p), (dv_p, "dv_p", v_p),
-                               (dq_r, "dq_r", q_r), (dk_r, "dk_r", k_r), (dv_r, "dv_r", v_r))]
-    _linear_bwd(b, dec, (q_p, k_p, v_p, do_p, q_r, k_r, v_r, do_r, state, *outs), fwd_ws, _linear_ws(b, True, ws, dev), on)
+        _want(state, "state", torch.float32, (b.num_groups, b.hkv, b.d, b.d))
+    with on as st:
+        outs = [_out(t, n, torch.bfloat16, like.shape, dev)
+                for t, n, like in ((dq_p, "dq_p", q_p), (dk_p, "dk_p", k_p), (dv_p, "dv_p", v_p),
+                                   (dq_r, "dq_r", q_r), (dk_r, "dk_r", k_r), (dv_r, "dv_r", v_r))]
+        _linear_bwd(b, dec, (q_p, k_p, v_p, do_p, q_r, k_r, v_r, do_r, state, *outs), fwd_ws,
+                    _linear_ws(b, True, ws, dev), st)
     return tuple(outs)
 
 
-def _linear_bwd(b: GroupBatch, dec, tensors, fwd_ws, ws, on: _On):
+def _linear_bwd(b: GroupBatch, dec, tensors, fwd_ws, ws, stream):
     """The call of linear_bwd behind its checks: inputs, state and outputs in the order of augtree_linear_bwd."""
-    with on as st:
-        _lib.check(_lib.load().augtree_linear_bwd(b.ref, dec.ctypes.data, *(_addr(t) for t in tensors), _addr(fwd_ws),
-                                                  0 if fwd_ws is None else fwd_ws.numel(), _addr(ws), ws.numel(), st),
-                   "linear_bwd")
+    _lib.check(_lib.load().augtree_linear_bwd(b.ref, dec.ctypes.data, *(_addr(t) for t in tensors), _addr(fwd_ws),
+                                              0 if fwd_ws is None else fwd_ws.numel(), _addr(ws), ws.numel(), stream),
+               "linear_bwd")
 
 
 def linear_step(q, k, v, decay, state, src=None, state_out=None, o=None, scale: Optional[float] = None, stream=None):
@@ -449,12 +456,12 @@ def linear_step(q, k, v, decay, state, src=None, state_out=None, o=None, scale: 
         raise ValueError("q and k must be [rows, heads, head_dim]")
     rows, hq, d = q.shape
     hkv, n = k.shape[1], state.shape[0]
-    _need(q, "q", torch.bfloat16, (rows, hq, d))
-    _need(k, "k", torch.bfloat16, (rows, hkv, d))
-    _need(v, "v", torch.bfloat16, (rows, hkv, d))
-    _need(state, "state", torch.float32, (n, hkv, d, d))
+    _want(q, "q", torch.bfloat16, (rows, hq, d))
+    _want(k, "k", torch.bfloat16, (rows, hkv, d))
+    _want(v, "v", torch.bfloat16, (rows, hkv, d))
+    _want(state, "state", torch.float32, (n, hkv, d, d))
     if src is not None:
-        _need(src, "src", torch.int32, (rows,))
+        _want(src, "src", torch.int32, (rows,))
     dec = _decay(decay, hkv)
     with on as st:
         state_out = _out(state_out, "state_out", torch.float32, (rows, hkv, d, d), on.device)
@@ -469,12 +476,12 @@ def linear_step(q, k, v, decay, state, src=None, state_out=None, o=None, scale: 
 def _norm_inputs(x, gate, weight, bias):
     if x.dim() != 3:
         raise ValueError("x must be [rows, heads, head_dim]")
-    _need(x, "x", torch.bfloat16, x.shape)
+    _want(x, "x", torch.bfloat16, x.shape)
     if gate is not None:
-        _need(gate, "gate", torch.bfloat16, x.shape)
+        _want(gate, "gate", torch.bfloat16, x.shape)
     for n, t in (("weight", weight), ("bias", bias)):
         if t is not None:
-            _need(t, n, torch.float32, x.shape[1:])
+            _want(t, n, torch.float32, x.shape[1:])
 
 
 def head_norm_fwd(x, weight=None, bias=None, gate=None, activation: int = ACT_NONE, eps: float = 1e-5, y=None,
@@ -498,7 +505,7 @@ def head_norm_bwd(x, dy, weight=None, bias=None, gate=None, activation: int = AC
     on = _On((("x", x), ("dy", dy), ("weight", weight), ("bias", bias), ("gate", gate), ("dx", dx), ("dgate", dgate),
               ("dweight", dweight), ("dbias", dbias), ("ws", ws)), stream)
     _norm_inputs(x, gate, weight, bias)
-    _need(dy, "dy", torch.bfloat16, x.shape)
+    _want(dy, "dy", torch.bfloat16, x.shape)
     rows, heads, d = x.shape
     dev, f32, lib = on.device, torch.float32, _lib.load()
     with on as st:

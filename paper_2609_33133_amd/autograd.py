@@ -28,6 +28,7 @@ from __future__ import annotations
 from typing import Optional, Tuple
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import api
 from .api import REPLAY_FUSED, GroupBatch
@@ -75,6 +76,11 @@ def group_attention(q_p: torch.Tensor, k_p: torch.Tensor, v_p: torch.Tensor, q_r
     return _GroupAttention.apply(q_p, k_p, v_p, q_r, k_r, v_r, batch, int(mode))
 
 
+def _trains(tensors) -> bool:
+    """Whether a gradient may be asked for: otherwise autograd is left out, and its time."""
+    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
+
+
 class _GroupLinearAttention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q_p, k_p, v_p, q_r, k_r, v_r, batch: GroupBatch, decay, state, return_state: bool):
@@ -90,6 +96,7 @@ class _GroupLinearAttention(torch.autograd.Function):
         return o_p, o_r, state_p, state_r
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, do_p, do_r, *_):
         q_p, k_p, v_p, q_r, k_r, v_r, state, ws = ctx.saved_tensors
         # an output that did not reach the loss has a zero gradient
@@ -97,10 +104,10 @@ class _GroupLinearAttention(torch.autograd.Function):
         do_r = torch.zeros_like(q_r) if do_r is None else do_r.to(torch.bfloat16).contiguous()
         # the forward has checked what it saved; the outputs' gradients are new
         api._linear_inputs(ctx.batch, (("do_p", do_p), ("do_r", do_r)))
-        on = api._On((("q_p", q_p), ("do_p", do_p), ("do_r", do_r)))
-        grads = [torch.empty_like(t) for t in (q_p, k_p, v_p, q_r, k_r, v_r)]
-        api._linear_bwd(ctx.batch, ctx.decay, (q_p, k_p, v_p, do_p, q_r, k_r, v_r, do_r, state, *grads), ws,
-                        api._linear_ws(ctx.batch, True, None, q_p.device), on)
+        with api._On((("q_p", q_p), ("do_p", do_p), ("do_r", do_r))) as stream:
+            grads = [torch.empty_like(t) for t in (q_p, k_p, v_p, q_r, k_r, v_r)]
+            api._linear_bwd(ctx.batch, ctx.decay, (q_p, k_p, v_p, do_p, q_r, k_r, v_r, do_r, state, *grads), ws,
+                            api._linear_ws(ctx.batch, True, None, q_p.device), stream)
         return (*grads, None, None, None, None)
 
 
@@ -113,8 +120,12 @@ def group_linear_attention(q_p: torch.Tensor, k_p: torch.Tensor, v_p: torch.Tens
     either)."""
     if state is not None and state.requires_grad:
         raise ValueError("state is a constant of the op: no gradient is formed for it")
-    decay = api._decay(decay, batch.hkv).copy()
-    return _GroupLinearAttention.apply(q_p, k_p, v_p, q_r, k_r, v_r, batch, decay, state, bool(return_state))
+    decay = api._decay(decay, batch.hkv)
+    x = (q_p, k_p, v_p, q_r, k_r, v_r)
+    if not _trains(x):
+        out = api.linear_fwd(batch, decay, *(t.contiguous() for t in x), state=state, want_states=return_state)
+        return out if return_state else out[:2]
+    return _GroupLinearAttention.apply(*x, batch, decay.copy(), state, bool(return_state))
 
 
 ACTIVATIONS = {"none": api.ACT_NONE, "silu": api.ACT_SILU}
@@ -123,22 +134,18 @@ ACTIVATIONS = {"none": api.ACT_NONE, "silu": api.ACT_SILU}
 class _HeadNorm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, bias, gate, activation: int, eps: float):
-        x = x.contiguous()
-        gate = None if gate is None else gate.contiguous()
-        weight = None if weight is None else weight.contiguous()
-        bias = None if bias is None else bias.contiguous()
         y = api.head_norm_fwd(x, weight, bias, gate, activation, eps)
         ctx.save_for_backward(x, weight, bias, gate)
         ctx.activation, ctx.eps = activation, eps
         return y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         x, weight, bias, gate = ctx.saved_tensors
         dx, dgate, dweight, dbias = api.head_norm_bwd(
             x, dy.to(torch.bfloat16).contiguous(), weight, bias, gate, ctx.activation, ctx.eps,
-            want_dweight=weight is not None and ctx.needs_input_grad[1],
-            want_dbias=bias is not None and ctx.needs_input_grad[2])
+            want_dweight=ctx.needs_input_grad[1], want_dbias=ctx.needs_input_grad[2])
         return dx, dweight, dbias, dgate, None, None
 
 
@@ -147,6 +154,10 @@ def head_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Opti
     """Norm over each head of packed rows [rows, heads, head_dim] (bf16), n = (x - mean) / sqrt(var + eps), then
     a = n * weight + bias ([heads, head_dim] fp32, each optional) and y = act(a), or with a gate y = a * act(gate).
     `activation`: "none" or "silu". Differentiable in every tensor."""
-    if activation not in ACTIVATIONS:
+    act = ACTIVATIONS.get(activation)
+    if act is None:
         raise ValueError(f"activation {activation!r} not in {tuple(ACTIVATIONS)}")
-    return _HeadNorm.apply(x, weight, bias, gate, ACTIVATIONS[activation], float(eps))
+    t = [None if v is None else v.contiguous() for v in (x, weight, bias, gate)]
+    if not _trains(t):
+        return api.head_norm_fwd(*t, act, eps)
+    return _HeadNorm.apply(*t, act, float(eps))

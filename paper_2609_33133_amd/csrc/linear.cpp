@@ -282,8 +282,43 @@ int check_all(const Named* v, int n, bool required) {
 
 bool overlap(const void* a, size_t na, const void* b, size_t nb) {
   const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return x < y + nb && y < x + na;
+  return a && b && x < y + nb && y < x + na;
 }
+
+// A tensor of a call, for the check that outputs are apart from all else.
+struct Span {
+  const void* p;
+  size_t bytes;
+  const char* name;
+};
+
+int check_apart(const Span* in, int n_in, const Span* out, int n_out) {
+  for (int i = 0; i < n_out; ++i) {
+    for (int j = 0; j < n_in; ++j)
+      if (overlap(out[i].p, out[i].bytes, in[j].p, in[j].bytes))
+        return fail(AUGTREE_ERR_INVALID_ARGUMENT, "%s overlaps %s", out[i].name, in[j].name);
+    for (int j = 0; j < i; ++j)
+      if (overlap(out[i].p, out[i].bytes, out[j].p, out[j].bytes))
+        return fail(AUGTREE_ERR_INVALID_ARGUMENT, "%s overlaps %s", out[i].name, out[j].name);
+  }
+  return AUGTREE_OK;
+}
+
+// bytes of a batch's tensors: q and k rows of prompts and responses, states of trees and branches
+struct Sizes {
+  size_t qp, kp, qr, kr, sp, sr;
+  explicit Sizes(const augtree_groups* g) {
+    const size_t row = 2 * (size_t)g->head_dim, tp = g->cu_prompt[g->num_groups],
+                 tr = g->num_branches ? g->cu_resp[g->num_branches] : 0;
+    const size_t state = (size_t)g->num_kv_heads * g->head_dim * g->head_dim * sizeof(float);
+    qp = tp * row * g->num_q_heads;
+    kp = tp * row * g->num_kv_heads;
+    qr = tr * row * g->num_q_heads;
+    kr = tr * row * g->num_kv_heads;
+    sp = state * g->num_groups;
+    sr = state * g->num_branches;
+  }
+};
 
 }  // namespace
 
@@ -316,6 +351,12 @@ int augtree_linear_fwd(const augtree_groups* grp, const float* decay, const uint
     if ((st = check_all(prompt, 4, true)) || (br && (st = check_all(resp, 4, true))) || (st = check_all(opt, 3, false)))
       return st;
     if (!br && state_r) return fail(AUGTREE_ERR_INVALID_ARGUMENT, "state_r without branches");
+    const Sizes z(grp);
+    const Span ins[] = {{q_p, z.qp, "q_p"}, {k_p, z.kp, "k_p"}, {v_p, z.kp, "v_p"}, {q_r, z.qr, "q_r"},
+                        {k_r, z.kr, "k_r"}, {v_r, z.kr, "v_r"}, {state != state_p ? state : nullptr, z.sp, "state"}};
+    const Span outs[] = {{o_p, z.qp, "o_p"}, {o_r, z.qr, "o_r"}, {state_p, z.sp, "state_p"}, {state_r, z.sr, "state_r"},
+                         {ws, ws_bytes, "ws"}};
+    if ((st = check_apart(ins, 7, outs, 5))) return st;
     Call c;
     c.g = grp;
     if ((st = make_layout(grp, &c.L)) || (st = check_ws(ws, ws_bytes, workspace_bytes(grp, c.L, false))) ||
@@ -357,13 +398,18 @@ int augtree_linear_bwd(const augtree_groups* grp, const float* decay, const uint
     if ((st = check_all(prompt, 7, true)) || (br && (st = check_all(resp, 7, true))) ||
         (st = check_ptr(state, "state", false)))
       return st;
+    const Sizes z(grp);
+    const Span ins[] = {{q_p, z.qp, "q_p"},   {k_p, z.kp, "k_p"}, {v_p, z.kp, "v_p"}, {do_p, z.qp, "do_p"}, {q_r, z.qr, "q_r"},
+                        {k_r, z.kr, "k_r"},   {v_r, z.kr, "v_r"}, {do_r, z.qr, "do_r"}, {state, z.sp, "state"},
+                        {fwd_ws, fwd_ws_bytes, "fwd_ws"}};
+    const Span outs[] = {{dq_p, z.qp, "dq_p"}, {dk_p, z.kp, "dk_p"}, {dv_p, z.kp, "dv_p"}, {dq_r, z.qr, "dq_r"},
+                         {dk_r, z.kr, "dk_r"}, {dv_r, z.kr, "dv_r"}, {ws, ws_bytes, "ws"}};
+    if ((st = check_apart(ins, 10, outs, 7))) return st;
     Call c;
     c.g = grp;
     if ((st = make_layout(grp, &c.L)) || (st = check_ws(ws, ws_bytes, workspace_bytes(grp, c.L, true))) ||
         (fwd_ws && (st = check_ws(fwd_ws, fwd_ws_bytes, workspace_bytes(grp, c.L, false)))))
       return st;
-    if (fwd_ws && overlap(fwd_ws, fwd_ws_bytes, ws, ws_bytes))
-      return fail(AUGTREE_ERR_INVALID_ARGUMENT, "ws overlaps fwd_ws");
     if ((st = augtree_check_device())) return st;
     c.ws = static_cast<char*>(ws);
     c.stream = static_cast<hipStream_t>(stream);
@@ -408,17 +454,20 @@ int augtree_linear_step(int32_t rows, int32_t num_q_heads, int32_t num_kv_heads,
     return fail(AUGTREE_ERR_INVALID_ARGUMENT, "rows=%d n_states=%d must be >= 0", rows, n_states);
   if (!src && n_states < rows)
     return fail(AUGTREE_ERR_INVALID_ARGUMENT, "%d states for %d rows without src", n_states, rows);
+  if ((int64_t)rows * num_kv_heads * (head_dim / 64) > INT32_MAX)
+    return fail(AUGTREE_ERR_UNSUPPORTED, "%d rows of %d KV heads exceed a launch", rows, num_kv_heads);
   if (rows == 0) return fail_status(AUGTREE_OK, "");
   const Named need[] = {{q, "q"}, {k, "k"}, {v, "v"}, {state_out, "state_out"}, {o, "o"}};
   if ((st = check_all(need, 5, true)) || (st = check_ptr(state_in, "state_in", n_states > 0)) ||
       (st = check_ptr(src, "src", false, 4)))
     return st;
   const size_t state = (size_t)num_kv_heads * head_dim * head_dim * sizeof(float);
-  if ((src || state_in != state_out) && overlap(state_in, state * n_states, state_out, state * rows))
-    return fail(AUGTREE_ERR_INVALID_ARGUMENT,
-                "state_out overlaps state_in (in place only without src, and at the same address)");
-  if ((int64_t)rows * num_kv_heads * (head_dim / 64) > INT32_MAX)
-    return fail(AUGTREE_ERR_UNSUPPORTED, "%d rows of %d KV heads exceed a launch", rows, num_kv_heads);
+  const size_t nq = 2 * (size_t)rows * num_q_heads * head_dim, nk = 2 * (size_t)rows * num_kv_heads * head_dim;
+  const bool in_place = !src && state_in == state_out;  // otherwise a row could read what another one wrote
+  const Span ins[] = {{q, nq, "q"}, {k, nk, "k"}, {v, nk, "v"}, {in_place ? nullptr : state_in, state * n_states, "state_in"},
+                      {src, 4 * (size_t)rows, "src"}};
+  const Span outs[] = {{state_out, state * rows, "state_out"}, {o, nq, "o"}};
+  if ((st = check_apart(ins, 5, outs, 2))) return st;
   if ((st = augtree_check_device())) return st;
   LinStepParams p;
   std::memset(&p, 0, sizeof(p));

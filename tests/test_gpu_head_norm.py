@@ -94,6 +94,19 @@ def test_constant_rows_and_large_gates():
     check(t, True)
 
 
+def test_in_place():
+    t = make(300, 4, 128, True, True)
+    args = dict(weight=t["weight"], bias=t["bias"], activation=api.ACT_SILU)
+    y = api.head_norm_fwd(t["x"], gate=t["gate"], **args)
+    dx, dgate, _, _ = api.head_norm_bwd(t["x"], t["dy"], gate=t["gate"], **args)
+    for n in ("x", "gate"):
+        c = {k: v.clone() for k, v in t.items()}
+        assert torch.equal(api.head_norm_fwd(c["x"], gate=c["gate"], y=c[n], **args), y)
+    c = {k: v.clone() for k, v in t.items()}
+    api.head_norm_bwd(c["x"], c["dy"], gate=c["gate"], dx=c["dy"], dgate=c["gate"], **args)
+    assert torch.equal(c["dy"], dx) and torch.equal(c["gate"], dgate)
+
+
 def test_no_rows():
     t = make(0, 3, 64, True, True)
     y = api.head_norm_fwd(t["x"], t["weight"], t["bias"], t["gate"])

@@ -76,6 +76,41 @@ def test_many_blocks_scan_branches_side_by_side():
     check(run(b, dec, x), oracle(b, dec, x), "two scan launches")
 
 
+def test_pieces_of_a_sequence_in_place():
+    """A prompt taken in pieces, its state updated in place, is the prompt taken at once."""
+    whole = batch([(300, [])], 4, 2, 64)
+    dec = decays(2)
+    x = inputs(whole, 26)
+    ref = oracle(whole, dec, x, grads=False)
+    state = torch.zeros(1, 2, 64, 64, device="cuda")
+    outs, a = [], 0
+    for n in (130, 1, 169):
+        b = batch([(n, [])], 4, 2, 64)
+        part = [x[m + "_p"][a:a + n].contiguous() for m in "qkv"]
+        o, _, s, _ = api.linear_fwd(b, dec, *part, *(x[m][:0] for m in ("q_r", "k_r", "v_r")), state=state, state_p=state)
+        assert s is state
+        outs.append(o)
+        a += n
+    check({"o_p": torch.cat(outs), "state_p": state}, {n: ref[n] for n in ("o_p", "state_p")}, "pieces")
+
+
+def test_a_given_stream():
+    """Memory that a call allocates belongs to the stream it is given."""
+    b = batch([(2000, [700] * 4)], 4, 2, 128)
+    dec = decays(2)
+    x = inputs(b, 27)
+    want = run(b, dec, x)
+    s = torch.cuda.Stream()
+    for _ in range(3):
+        s.wait_stream(torch.cuda.current_stream())
+        got = run(b, dec, x, stream=s)
+        noise = [torch.full((1 << 20,), float("nan"), device="cuda") for _ in range(8)]  # reuses what the calls freed
+        torch.cuda.current_stream().wait_stream(s)
+        for n in want:
+            assert torch.equal(want[n], got[n]), n
+        del noise
+
+
 def test_sequences_without_branches():
     b = batch([(200, []), (1, []), (500, [])], 4, 2, 64)
     dec = decays(2)
@@ -171,6 +206,16 @@ def test_autograd_and_differences():
         diff = loss(moved) - loss(x)
         along = (ref["d" + n][0] * to64(step)).sum()
         assert abs(diff - along) <= 1e-9 * (abs(ref["d" + n][0]) * abs(to64(step))).sum(), n
+
+
+def test_no_second_derivatives():
+    b = batch([(20, [4])], 2, 2, 64)
+    x = inputs(b, 28)
+    leaf = [x[n].requires_grad_(True) for n in LEAVES]
+    o = group_linear_attention(*leaf, b, 0.9)
+    g, = torch.autograd.grad(o[0].float().sum(), leaf[:1], create_graph=True)
+    with pytest.raises(RuntimeError):
+        g.float().sum().backward()
 
 
 def test_strided_inputs_and_unused_outputs():

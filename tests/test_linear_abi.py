@@ -30,19 +30,26 @@ def dec(*v):
     return np.array(v, np.float32)
 
 
-def fwd(C, b, decay, p=None, resp=None, ws=None, n=BIG, **kw):
-    p = fake() if p is None else p
-    r = p if resp is None else resp
-    q_p = kw.get("q_p", p)
-    return C.augtree_linear_fwd(b.ref, decay.ctypes.data_as(ctypes.c_void_p), q_p, p, p, r, r, r, kw.get("state"), p, r,
-                                kw.get("state_p"), kw.get("state_r"), fake() if ws is None else ws, n, None)
+def at(i):
+    """Address i of tensors that lie apart."""
+    return ctypes.c_void_p((1 << 50) + (i << 44))
 
 
-def bwd(C, b, decay, **kw):
-    p = fake()
-    return C.augtree_linear_bwd(b.ref, decay.ctypes.data_as(ctypes.c_void_p), p, p, p, kw.get("do_p", p), p, p, p, p, None,
-                                p, p, p, p, p, kw.get("dv_r", p), kw.get("fwd_ws"), kw.get("fwd_n", 0),
-                                kw.get("ws", fake(1 << 22)), kw.get("n", 1 << 30), None)
+FWD = ("q_p", "k_p", "v_p", "q_r", "k_r", "v_r", "state", "o_p", "o_r", "state_p", "state_r")
+BWD = ("q_p", "k_p", "v_p", "do_p", "q_r", "k_r", "v_r", "do_r", "state", "dq_p", "dk_p", "dv_p", "dq_r", "dk_r", "dv_r")
+
+
+def tensors(names, kw):
+    optional = {"state": None, "state_p": None, "state_r": None}
+    return [kw[n] if n in kw else optional.get(n, at(i)) for i, n in enumerate(names)]
+
+
+def fwd(C, b, decay, ws=at(30), n=1 << 40, **kw):
+    return C.augtree_linear_fwd(b.ref, decay.ctypes.data_as(ctypes.c_void_p), *tensors(FWD, kw), ws, n, None)
+
+
+def bwd(C, b, decay, ws=at(30), n=1 << 40, fwd_ws=None, fwd_n=0, **kw):
+    return C.augtree_linear_bwd(b.ref, decay.ctypes.data_as(ctypes.c_void_p), *tensors(BWD, kw), fwd_ws, fwd_n, ws, n, None)
 
 
 GOOD = ([0, 10, 25], [0, 2, 3], [0, 5, 12, 20])
@@ -54,8 +61,9 @@ def test_valid_calls_reach_the_device_check(C):
     b = GroupBatch(*GOOD, 4, 2, 64)
     assert fwd(C, b, dec(0.9, 1.0)) == DEVICE and bwd(C, b, dec(0.9, 1.0)) == DEVICE
     plain = GroupBatch([0, 10, 25], [0, 0, 0], [0], 4, 2, 64)
-    assert C.augtree_linear_fwd(plain.ref, dec(1, 1).ctypes.data_as(ctypes.c_void_p), *[fake()] * 3, None, None, None, None,
-                                fake(), None, None, None, fake(), BIG, None) == DEVICE
+    none = {n: None for n in ("q_r", "k_r", "v_r", "o_r")}
+    assert fwd(C, plain, dec(1, 1), **none) == DEVICE
+    assert fwd(C, plain, dec(1, 1), state=at(25), state_p=at(25), **none) == DEVICE
 
 
 @pytest.mark.parametrize("args,code", [
@@ -81,50 +89,66 @@ def test_bad_batches(C, args, code):
 def test_bad_decays(C, bad):
     b = GroupBatch(*GOOD, 4, 2, 64)
     assert fwd(C, b, dec(0.9, bad)) == INVALID and bwd(C, b, dec(bad, 0.9)) == INVALID
-    p = fake()
-    assert C.augtree_linear_step(2, 4, 2, 64, 0.1, dec(0.9, bad).ctypes.data_as(ctypes.c_void_p), p, p, p, 2, p, None,
-                                 fake(1 << 21), p, None) == INVALID
+    assert C.augtree_linear_step(2, 4, 2, 64, 0.1, dec(0.9, bad).ctypes.data_as(ctypes.c_void_p), at(0), at(1), at(2), 2,
+                                 at(3), None, at(4), at(5), None) == INVALID
 
 
 def test_bad_pointers_and_workspaces(C):
     b, d = GroupBatch(*GOOD, 4, 2, 64), dec(0.9, 0.9)
     assert C.augtree_linear_fwd(None, None, *[None] * 11, None, 0, None) == INVALID
-    assert C.augtree_linear_fwd(b.ref, None, *[fake()] * 6, None, fake(), fake(), None, None, fake(), BIG, None) == INVALID
-    assert fwd(C, b, d, q_p=ctypes.c_void_p(None)) == INVALID
-    assert fwd(C, b, d, resp=ctypes.c_void_p(None)) == INVALID
-    assert fwd(C, b, d, q_p=ODD) == MISALIGNED and fwd(C, b, d, state=ODD) == MISALIGNED
-    assert fwd(C, b, d, state_r=ODD) == MISALIGNED
+    assert C.augtree_linear_fwd(b.ref, None, *tensors(FWD, {}), at(30), BIG, None) == INVALID
+    for n in FWD:
+        assert fwd(C, b, d, **{n: ODD}) == MISALIGNED, n
+        if n[:5] != "state":
+            assert fwd(C, b, d, **{n: None}) == INVALID, n
+    for n in BWD:
+        assert bwd(C, b, d, **{n: ODD}) == MISALIGNED, n
+        if n != "state":
+            assert bwd(C, b, d, **{n: None}) == INVALID, n
     need = [C.augtree_linear_workspace_size(b.ref, k) for k in (0, 1)]
     assert 0 < need[0] < need[1] and need[0] % 256 == 0
-    assert fwd(C, b, d, n=need[0] - 1) == WORKSPACE and fwd(C, b, d, ws=ctypes.c_void_p(None)) == WORKSPACE
-    assert fwd(C, b, d, ws=ctypes.c_void_p((1 << 28) + 16)) == MISALIGNED
-    assert bwd(C, b, d, n=need[1] - 1) == WORKSPACE and bwd(C, b, d, dv_r=ctypes.c_void_p(None)) == INVALID
-    assert bwd(C, b, d, do_p=ODD) == MISALIGNED
-    assert bwd(C, b, d, fwd_ws=fake(), fwd_n=need[0] - 1) == WORKSPACE
-    assert bwd(C, b, d, fwd_ws=ctypes.c_void_p((1 << 28) + 16), fwd_n=need[0]) == MISALIGNED
-    assert bwd(C, b, d, fwd_ws=fake(1 << 22), fwd_n=need[0]) == INVALID  # the same memory as ws
+    off = ctypes.c_void_p(at(30).value + 16)
+    assert fwd(C, b, d, n=need[0] - 1) == WORKSPACE and fwd(C, b, d, ws=None) == WORKSPACE
+    assert fwd(C, b, d, ws=off) == MISALIGNED
+    assert bwd(C, b, d, n=need[1] - 1) == WORKSPACE and bwd(C, b, d, ws=None) == WORKSPACE
+    assert bwd(C, b, d, fwd_ws=at(31), fwd_n=need[0] - 1) == WORKSPACE
+    assert bwd(C, b, d, fwd_ws=off, fwd_n=need[0], ws=at(31)) == MISALIGNED
     plain = GroupBatch([0, 10], [0, 0], [0], 4, 2, 64)
-    assert fwd(C, plain, d, state_r=fake()) == INVALID
+    assert fwd(C, plain, d, state_r=at(29)) == INVALID
     scale = GroupBatch(*GOOD, 4, 2, 64, softmax_scale=float("inf"))
     assert fwd(C, scale, d) == INVALID
 
 
-def test_step_refusals(C):
-    p, far = fake(), fake(1 << 24)
+def test_outputs_lie_apart(C):
+    b, d = GroupBatch(*GOOD, 4, 2, 64), dec(0.9, 0.9)
+    last = ctypes.c_void_p(at(0).value + 25 * 4 * 64 * 2 - 16)  # inside q_p
+    for n in ("o_p", "o_r", "state_p", "state_r"):
+        assert fwd(C, b, d, **{n: at(0)}) == INVALID and fwd(C, b, d, **{n: last}) == INVALID, n
+        assert b"overlaps" in C.augtree_last_error()
+    assert fwd(C, b, d, o_r=at(7)) == INVALID and fwd(C, b, d, ws=at(7)) == INVALID
+    assert fwd(C, b, d, state=at(25), state_r=at(25)) == INVALID
+    for n in BWD[9:]:
+        assert bwd(C, b, d, **{n: at(3)}) == INVALID, n
+    assert bwd(C, b, d, dk_p=at(11)) == INVALID and bwd(C, b, d, ws=at(4)) == INVALID
+    assert bwd(C, b, d, fwd_ws=at(30), fwd_n=1 << 30) == INVALID  # the same memory as ws
 
-    def step(rows=4, hq=4, hkv=2, d=64, scale=0.1, n=4, s_in=p, src=None, s_out=far, q=p):
-        return C.augtree_linear_step(rows, hq, hkv, d, scale, np.ones(300, np.float32).ctypes.data_as(ctypes.c_void_p), q, p,
-                                     p, n, s_in, src, s_out, p, None)
+
+def test_step_refusals(C):
+    p, far = at(0), at(1)
+
+    def step(rows=4, hq=4, hkv=2, d=64, scale=0.1, n=4, s_in=p, src=None, s_out=far, q=at(2), o=at(5)):
+        return C.augtree_linear_step(rows, hq, hkv, d, scale, np.ones(300, np.float32).ctypes.data_as(ctypes.c_void_p), q,
+                                     at(3), at(4), n, s_in, src, s_out, o, None)
     assert step(rows=0) == OK and step(rows=-1) == INVALID and step(n=-1) == INVALID
     assert step(n=3) == INVALID and step(d=32) == UNSUPPORTED and step(hq=3) == UNSUPPORTED
     assert step(hq=257, hkv=257) == UNSUPPORTED and step(scale=0.0) == INVALID
     assert step(q=None) == INVALID and step(q=ODD) == MISALIGNED and step(src=ODD.value + 1) == MISALIGNED
     # overlaps: in place needs the same address and no src
-    assert step(src=p, s_out=p) == INVALID
+    assert step(src=at(6), s_out=p) == INVALID and step(o=at(2)) == INVALID and step(s_out=at(5)) == INVALID
     assert step(s_out=ctypes.c_void_p(p.value + 2 * 64 * 64 * 4)) == INVALID
-    assert step(rows=2 ** 31 - 1, n=2 ** 31 - 1, hq=256, hkv=256, s_out=ctypes.c_void_p(1 << 60)) == UNSUPPORTED
+    assert step(rows=2 ** 31 - 1, n=2 ** 31 - 1, hq=256, hkv=256, s_in=ctypes.c_void_p(1 << 60), s_out=ctypes.c_void_p(1 << 61)) == UNSUPPORTED
     if not torch.cuda.is_available():
-        assert step() == DEVICE and step(s_out=p) == DEVICE and step(src=p, n=1) == DEVICE
+        assert step() == DEVICE and step(s_out=p) == DEVICE and step(src=at(6), n=1) == DEVICE
 
 
 def test_norm_refusals(C):
