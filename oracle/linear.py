@@ -20,7 +20,7 @@ def segments(cu_prompt, cu_branch, cu_resp):
 
 def attention(cu_prompt, cu_branch, cu_resp, decay, scale, x, state=None, grads=True):
     """x: q_p, k_p, v_p, q_r, k_r, v_r (and do_p, do_r) fp64 [rows, heads, d]. Returns {name: (value, sum over the rows
-    of |P| |z|, sum of |x| |y| |z|)} for o, dq, dk, dv of both sides, and {state_p, state_r: (value, sum of |k| |v|)}."""
+    of |x| |y| |z|)} for o, dq, dk, dv of both sides, and {state_p, state_r: (value, sum of |k| |v|)}."""
     hq, hkv, d = x["q_p"].shape[1], x["k_p"].shape[1], x["q_p"].shape[2]
     g = hq // hkv
     out = {}
@@ -28,7 +28,7 @@ def attention(cu_prompt, cu_branch, cu_resp, decay, scale, x, state=None, grads=
     for n in names:
         for s in "pr":
             like = x[("q_" if n in ("o", "dq") else "k_") + s]
-            out[n + "_" + s] = tuple(np.zeros(like.shape) for _ in range(3))
+            out[n + "_" + s] = tuple(np.zeros(like.shape) for _ in range(2))
     trees, branches = len(cu_prompt) - 1, len(cu_resp) - 1
     out["state_p"] = tuple(np.zeros((trees, hkv, d, d)) for _ in range(2))
     out["state_r"] = tuple(np.zeros((branches, hkv, d, d)) for _ in range(2))
@@ -48,30 +48,30 @@ def attention(cu_prompt, cu_branch, cu_resp, decay, scale, x, state=None, grads=
             for hh in range(h * g, h * g + g):
                 q = x["q_" + side][at.start:at.stop, hh]
 
-                def add(name, rows_of, value, a, b):
+                def add(name, rows_of, value, mag):
                     arr = out[name + "_" + rows_of[0]]
-                    for t, u in zip(arr, (value, a, b)):
+                    for t, u in zip(arr, (value, mag)):
                         t[rows_of[1]:rows_of[2], hh if name in ("o", "dq") else h] += scale * u
 
                 me = (side, at.start, at.stop)
                 pm, pa = w * (q @ kh.T), w * (abs(q) @ abs(kh).T)
-                o, oa, ob = pm @ vh, abs(pm) @ abs(vh), pa @ abs(vh)
+                o, oa = pm @ vh, pa @ abs(vh)
                 if s0 is not None:
-                    o, ob = o + lead * (q @ s0), ob + lead * (abs(q) @ abs(s0))
-                add("o", me, o, oa, ob)
+                    o, oa = o + lead * (q @ s0), oa + lead * (abs(q) @ abs(s0))
+                add("o", me, o, oa)
                 if not grads:
                     continue
                 do = x["do_" + side][at.start:at.stop, hh]
                 bm, ba = w * (do @ vh.T), w * (abs(do) @ abs(vh).T)
-                dq, qa, qb = bm @ kh, abs(bm) @ abs(kh), ba @ abs(kh)
+                dq, qa = bm @ kh, ba @ abs(kh)
                 if s0 is not None:
-                    dq, qb = dq + lead * (do @ s0.T), qb + lead * (abs(do) @ abs(s0).T)
-                add("dq", me, dq, qa, qb)
+                    dq, qa = dq + lead * (do @ s0.T), qa + lead * (abs(do) @ abs(s0).T)
+                add("dq", me, dq, qa)
                 for name, m, ma, z in (("dk", bm, ba, q), ("dv", pm, pa, do)):
-                    value, a, b = m.T @ z, abs(m).T @ abs(z), ma.T @ abs(z)
-                    add(name, ("p", p.start, p.stop), value[:len(p)], a[:len(p)], b[:len(p)])
+                    value, mag = m.T @ z, ma.T @ abs(z)
+                    add(name, ("p", p.start, p.stop), value[:len(p)], mag[:len(p)])
                     if branch is not None:
-                        add(name, me, value[before:], a[before:], b[before:])
+                        add(name, me, value[before:], mag[before:])
             end = np.exp(np.log(float(decay[h])) * np.arange(total - 1, -1, -1.0))[:, None]
             s, sa = (end * kh).T @ vh, (end * abs(kh)).T @ abs(vh)
             if s0 is not None:

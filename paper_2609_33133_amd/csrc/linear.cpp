@@ -126,7 +126,7 @@ int block_rows(const augtree_groups* g, int tree) {
   return best;
 }
 
-constexpr int64_t kScanBlocks = 64;
+constexpr int64_t kScanBlocks = 16;
 
 struct Layout {
   std::vector<LinSeg> segs;
@@ -251,8 +251,9 @@ struct Call {
     c.skip_branch = s.skip_branch;
     c.b = b;
     // A tree's blocks are scanned by one launch, its branches one after the other, where they are few; else prompts and
-    // branches get a launch each, in which the branches run side by side. (49152 rows in 64 blocks: 12 us against 22;
-    // 264192 rows in 258 blocks, 16 branches: 30 us in two launches.)
+    // branches get a launch each, in which the branches run side by side. A launch costs 5 us and each block of the chain
+    // about 0.3 (32 / 8 heads, d = 128, one launch against two: 64 blocks, 8 branches, 24 us against 19; 258 blocks, 16
+    // branches, 122 us against 57).
     const bool split = branches && L.longest > kScanBlocks;
     for (int k = 0; k < (split ? 2 : 1); ++k) {
       const int part = !split ? 0 : (k == 0) != reverse ? 1 : 2;

@@ -27,15 +27,15 @@
 // sixth of the time.
 //
 // What bounds it (49152 rows, 32 / 8 heads, d = 128; a copy reaches 4.9 TB/s
-// here): the forward's output kernel moves 1.1 GB in 250 us, 4.4 TB/s, and the
-// state kernels 3.5 TB/s forward and 6.4 in reverse (partly from the Infinity
-// Cache). The gradient kernel moves 2.3 GB past the L2s (1.7 read: dv and dk share
+// here): the forward's output kernel moves 1.0 GB in 250 us, 4.2 TB/s, the state
+// kernels 0.2 GB in 55 us forward and 0.8 GB in 167 us in reverse, 3.6 and 4.8
+// TB/s. The gradient kernel moves 2.3 GB past the L2s (1.7 read: dv and dk share
 // theirs, dq runs the other way through time) in 700 us, 3.3 TB/s, and has about
 // as much work on the CU: per 64 rows of a head and role about 5400 cycles of a CU
 // that two workgroups share, 59 % of them matrix instructions, at the 1.9 GHz that
-// the chip's power leaves of 2.4. Other shapes of it took the same time within 3 %: 8 wavefronts of 16 columns (four on a SIMD
-// instead of two, but 2.4 times the LDS reads), P in 32 x 32 tiles, wavefront
-// priorities.
+// the chip's power leaves of 2.4. Other shapes of it took the same time within
+// 3 %: 8 wavefronts of 16 columns (four on a SIMD instead of two, but 2.4 times
+// the LDS reads), P in 32 x 32 tiles, wavefront priorities.
 #include "common.h"
 #include "linear.h"
 
@@ -340,9 +340,9 @@ struct Scan {
   __device__ __forceinline__ void store(float* base, int64_t i, f32x4 v) const {
     *reinterpret_cast<f32x4*>(base + i * per + at) = v;
   }
-  // One segment: every block's own state is replaced by the carry that reaches it. Eight blocks are loaded ahead: a scan
-  // of 48 MB of states then takes 12 us, which is the time of reading and writing them (one at a time, prompts and
-  // branches in a launch each: 22 us).
+  // One segment: every block's own state is replaced by the carry that reaches it. Eight blocks are loaded ahead, which
+  // hides most of the way to memory: 64 blocks of 0.5 MB, read and written in a chain, take 25 us. Workgroups of one
+  // wavefront instead of four (more CUs with work) took the same.
   template <bool REV>
   __device__ __forceinline__ f32x4 segment(const LinSeg& s, f32x4 carry, bool skip) const {
     constexpr int kAhead = 8;

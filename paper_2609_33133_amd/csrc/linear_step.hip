@@ -1,7 +1,10 @@
 // One token of linear attention for every row: S' = gamma S + k v^T,
 // o_h = scale q_h S'. The states are read and written once, 8 d^2 bytes per row
 // and KV head against 2 d^2 (1 + group) multiply-adds, so the kernel is bound
-// by HBM. All arithmetic is fp32.
+// by HBM. All arithmetic is fp32. A state is held in registers between its read
+// and its write, so nothing waits in LDS but k, q and the heads' partial sums.
+// Measured at 32 / 8 heads, d = 128: 512 rows, 0.55 GB, in 102 us, 5.4 TB/s (a
+// copy of 2 GiB: 4.9); 8 rows 5.6 us, the time of a launch.
 #include "common.h"
 #include "linear.h"
 

@@ -169,7 +169,7 @@ def test_prefill_then_steps_equal_one_longer_sequence():
         o, state = api.linear_step(q, k, v, dec, state, src=src if t == 0 else None,
                                    state_out=None if t == 0 else state)
         at = rows.cpu().numpy() + t
-        want, mag = ref["o_r"][0][at], ref["o_r"][2][at]
+        want, mag = ref["o_r"][0][at], ref["o_r"][1][at]
         assert (abs(to64(o) - want) <= 2.0 ** -8 * abs(want) + 2.0 ** -17 * mag).all(), t
     assert (abs(to64(state) - ref["state_r"][0]) <= 2.0 ** -18 * ref["state_r"][1]).all()
 
