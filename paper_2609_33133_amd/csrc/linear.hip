@@ -30,12 +30,14 @@
 // here): the forward's output kernel moves 1.0 GB in 250 us, 4.2 TB/s, the state
 // kernels 0.2 GB in 55 us forward and 0.8 GB in 167 us in reverse, 3.6 and 4.8
 // TB/s. The gradient kernel moves 2.3 GB past the L2s (1.7 read: dv and dk share
-// theirs, dq runs the other way through time) in 700 us, 3.3 TB/s, and has about
-// as much work on the CU: per 64 rows of a head and role about 5400 cycles of a CU
-// that two workgroups share, 59 % of them matrix instructions, at the 1.9 GHz that
-// the chip's power leaves of 2.4. Other shapes of it took the same time within
-// 3 %: 8 wavefronts of 16 columns (four on a SIMD instead of two, but 2.4 times
-// the LDS reads), P in 32 x 32 tiles, wavefront priorities.
+// theirs, dq runs the other way through time) in 660 us, 3.6 TB/s, and has about
+// as much work on the CU: a wavefront needs 6900 cycles for 64 rows of a head,
+// beside one of another workgroup on its SIMD. Of these, two such wavefronts keep
+// the matrix cores busy for 3600, the LDS for 3000 and the vector unit for about
+// as many. The clock is what the chip's power leaves, 1.4 to 1.9 GHz of 2.4. Other
+// shapes of it took the same time within 3 %: 8 wavefronts of 16 columns (four on
+// a SIMD instead of two, but 2.4 times the LDS reads), P in 32 x 32 tiles,
+// wavefront priorities, three barriers a head instead of two.
 #include "common.h"
 #include "linear.h"
 
@@ -232,8 +234,9 @@ __device__ __forceinline__ void scale_state(f32x4* s, float f) {
 // A [64, D] tile on its way from memory to LDS through registers: fetch()
 // issues the loads, put() waits for them and writes the swizzled tile. The loads
 // of the next tiles are in flight while a chunk is worked on (they arrive before
-// they are waited for: 110 cycles of a 5400-cycle step), and LDS holds one tile of
-// each operand, so that two workgroups fit a CU. Rows from n on are zeros.
+// they are waited for: 150 cycles of a step of 6900 go to that and the barrier),
+// and LDS holds one tile of each operand, so that two workgroups fit a CU. Rows
+// from n on are zeros.
 template <int D, int NW>
 struct TileStage {
   static constexpr int CH = D / 8, RPI = 64 / CH, ROWS = NW * RPI, NI = C / ROWS;  // pieces of a row; rows of a pass
@@ -661,42 +664,42 @@ __device__ __forceinline__ void lin_out(OutShared<D>& sh, const LinBatch& batch,
     store_rows<D>(out + c * C * stride_x + h * D + 32 * wave, acc, scale, n, stride_x, l32, hf);
   };
 
+  // Two barriers a head: behind the first its tiles are in LDS, behind the second P is, and all that reads the tiles has
+  // read them (forward: but for y and z, once a chunk), so that the next ones may be written beside the product with P.
   int row_n = -1;
   for (int ci = 0; ci < chunks; ++ci) {
     const int c = chunk_of(ci), n = rows_of(c);
     const bool more = ci + 1 < chunks;
     const float fade = exp2f(lg * (float)n);
     if constexpr (REV) {
-      __syncthreads();
       s2.put(sh.xt, dst);
       if (n != row_n) set_row_decays<REV>(sh.decays, lg, n), row_n = n;
-      __syncthreads();
-      from_state(n);
-      fade_state(fade);
+      if (ci == 0) s0.put(sh.yt, dst), s1.put(sh.zt, dst);
       for (int h = 0; h < g; ++h) {
-        if (h > 0) __syncthreads();  // the tiles of the head before have been read
-        s0.put(sh.yt, dst);
-        s1.put(sh.zt, dst);
         __syncthreads();
         if (h + 1 < g) fetch_yz(s0, s1, ci, h + 1);
         else if (more) fetch_yz(s0, s1, ci + 1, 0), fetch_x(s2, ci + 1, 0);
+        if (h == 0) {
+          from_state(n);
+          fade_state(fade);
+        }
         bf16x8 zf[4];
 #pragma unroll
         for (int m = 0; m < 4; ++m) zf[m] = read_columns32<D>(sh.zt, zbase, 0, m);
         p_tiles();
         update(zf);
         __syncthreads();
+        if (more || h + 1 < g) s0.put(sh.yt, dst), s1.put(sh.zt, dst);
         from_chunk(zf);
       }
       store(c, 0, n);
     } else {
-      __syncthreads();
+      if (ci > 0) __syncthreads();  // y has been read by the state's update
       s1.put(sh.yt, dst);
       s2.put(sh.zt, dst);
       if (n != row_n) set_row_decays<REV>(sh.decays, lg, n), row_n = n;
       bf16x8 zf[4];
       for (int h = 0; h < g; ++h) {
-        if (h > 0) __syncthreads();
         s0.put(sh.xt, dst);
         __syncthreads();
         if (h + 1 < g) fetch_x(s0, ci, h + 1);

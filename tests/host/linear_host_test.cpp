@@ -69,13 +69,14 @@ void check_batch(const LinBatch& b) {
     check(s[i].row0 == cu[j] && s[i].len == cu[j + 1] - cu[j], "rows of a segment");
     check(s[i].block0 == block, "block numbers");
     check(s[i].rows % kLinChunk == 0 && s[i].rows >= kLinChunk, "rows of a block");
-    block += (s[i].len + s[i].rows - 1) / s[i].rows;
+    const int n = (s[i].len + s[i].rows - 1) / s[i].rows;
+    check(s[i].rows == kLinChunk || (int64_t)n * (s[i].rows - kLinChunk) < s[i].len, "even blocks");
+    block += n;
     if (prompt) {
       check(nb == 0 ? s[i].link == 0 : s[i].link == g.cu_branch[j], "first branch");
     } else {
       const int t = s[i].link;
       check(t >= 0 && t < ng && j >= g.cu_branch[t] && j < g.cu_branch[t + 1], "tree of a branch");
-      check(s[i].rows == s[t].rows, "one block length a tree");
     }
   }
   check(block == b.num_blocks, "number of blocks");
