@@ -447,7 +447,7 @@ typedef enum augtree_activation { AUGTREE_ACT_NONE = 0, AUGTREE_ACT_SILU = 1 } a
  *   y = act(a),  or with a gate  y = a * act(gate);  act(u) = u / (1 + exp(-u)) (SILU) or u (NONE).
  * In:  x, gate (nullable) [rows,heads,head_dim] bf16; weight, bias (each
  *      nullable: 1 and 0) [heads,head_dim] fp32. head_dim a multiple of 8, at most 1024.
- * Out: y like x (it may be x or gate itself). rows = 0 is a no-op.
+ * Out: y like x (it may be x or gate itself; other overlaps are refused). rows = 0 is a no-op.
  */
 int augtree_head_norm_fwd(int64_t rows, int32_t heads, int32_t head_dim, int activation, float eps,
                           const uint16_t* x, const uint16_t* gate, const float* weight, const float* bias,
@@ -455,7 +455,7 @@ int augtree_head_norm_fwd(int64_t rows, int32_t heads, int32_t head_dim, int act
 
 /*
  * Its backward. In: as forward, dy like y. Out: dx, dgate (with a gate) bf16
- * (each may be x, gate or dy itself, not both the same);
+ * (each may be x, gate or dy itself, not both the same; other overlaps are refused);
  * dweight, dbias [heads,head_dim] fp32 (each nullable), summed over the rows in a
  * fixed order. The workspace (augtree_head_norm_workspace_size bytes) is needed
  * for dweight or dbias only. rows = 0 writes zeros to them.

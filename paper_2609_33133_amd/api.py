@@ -368,8 +368,15 @@ def _out(t, name, dtype, shape, device):
     return t
 
 
+def _check_batch(b: GroupBatch):
+    """The offsets' counts, which the library takes from the batch's struct."""
+    if b.num_branches and len(b.cu_branch) != b.num_groups + 1:
+        raise ValueError(f"cu_branch: {len(b.cu_branch)} offsets for {b.num_groups} prompts")
+
+
 def linear_workspace_size(b: GroupBatch, backward: bool = False) -> int:
     lib = _lib.load()
+    _check_batch(b)
     n = lib.augtree_linear_workspace_size(b.ref, int(backward))
     if n == 0:
         raise _lib.AugtreeError(_lib.AUGTREE_ERR_INVALID_ARGUMENT, "linear_workspace_size",
@@ -377,13 +384,20 @@ def linear_workspace_size(b: GroupBatch, backward: bool = False) -> int:
     return int(n)
 
 
+def _want_ws(ws, name: str):
+    if ws is not None and (ws.dtype is not torch.uint8 or not ws.is_contiguous()):
+        raise ValueError(f"{name} must be a contiguous uint8 tensor")
+
+
 def _linear_ws(b, backward, ws, device):
     if ws is None:
         ws = torch.empty(linear_workspace_size(b, backward), dtype=torch.uint8, device=device)
+    _want_ws(ws, "ws")
     return ws
 
 
 def _linear_inputs(b: GroupBatch, named):
+    _check_batch(b)
     for n, t in named:
         rows = b.tp if n.endswith("_p") else b.tr
         _want(t, n, torch.bfloat16, (rows, b.hkv if n[0] in "kv" else b.hq, b.d))
@@ -428,6 +442,7 @@ def linear_bwd(b: GroupBatch, decay, q_p, k_p, v_p, do_p, q_r, k_r, v_r, do_r, s
                       ("dk_r", dk_r), ("dv_r", dv_r), ("fwd_ws", fwd_ws), ("ws", ws)), stream)
     _linear_inputs(b, named)
     dev = on.device
+    _want_ws(fwd_ws, "fwd_ws")
     if state is not None:
         _want(state, "state", torch.float32, (b.num_groups, b.hkv, b.d, b.d))
     with on as st:
@@ -452,8 +467,8 @@ def linear_step(q, k, v, decay, state, src=None, state_out=None, o=None, scale: 
     prompt share one; outside [0, n): from zero). Writes the new states to `state_out` (a new tensor if None; `state`
     itself only without src) and returns (o, state_out)."""
     on = _On((("q", q), ("k", k), ("v", v), ("state", state), ("src", src), ("state_out", state_out), ("o", o)), stream)
-    if q.dim() != 3 or k.dim() != 3:
-        raise ValueError("q and k must be [rows, heads, head_dim]")
+    if q.dim() != 3 or k.dim() != 3 or state.dim() != 4:
+        raise ValueError("q and k must be [rows, heads, head_dim], state [n, heads, head_dim, head_dim]")
     rows, hq, d = q.shape
     hkv, n = k.shape[1], state.shape[0]
     _want(q, "q", torch.bfloat16, (rows, hq, d))
@@ -516,6 +531,7 @@ def head_norm_bwd(x, dy, weight=None, bias=None, gate=None, activation: int = AC
             dweight = _out(dweight, "dweight", f32, (heads, d), dev)
         if want_dbias or dbias is not None:
             dbias = _out(dbias, "dbias", f32, (heads, d), dev)
+        _want_ws(ws, "ws")
         if ws is None and (dweight is not None or dbias is not None):
             ws = torch.empty(int(lib.augtree_head_norm_workspace_size(rows, heads, d)), dtype=torch.uint8, device=dev)
         _lib.check(lib.augtree_head_norm_bwd(rows, heads, d, int(activation), float(eps), _addr(x), _addr(gate),

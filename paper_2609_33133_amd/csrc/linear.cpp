@@ -136,6 +136,7 @@ struct Layout {
 
 size_t align_up(size_t n) { return (n + 255) / 256 * 256; }
 
+// (A launch has fewer than 2^32 threads: the gradient and the scan kernels' are the most.)
 int make_layout(const augtree_groups* g, Layout* L) {
   const int ng = g->num_groups, nb = g->num_branches;
   L->segs.resize((size_t)ng + nb);
@@ -164,10 +165,10 @@ int make_layout(const augtree_groups* g, Layout* L) {
     for (int b = g->cu_branch[t]; b < g->cu_branch[t + 1]; ++b)
       own[t] += add(ng + b, g->cu_resp[b], g->cu_resp[b + 1] - g->cu_resp[b], t, rows[t]);
   L->longest = *std::max_element(own.begin(), own.end());
-  const int64_t slices = (int64_t)g->head_dim * g->head_dim / 1024;
-  if (blocks * g->num_kv_heads > INT32_MAX / 3 - 8 || (ng + (int64_t)nb) * g->num_kv_heads * slices > INT32_MAX)
-    return fail(AUGTREE_ERR_UNSUPPORTED, "%lld blocks of %d KV heads exceed a launch", (long long)blocks,
-                g->num_kv_heads);
+  const int64_t hkv = g->num_kv_heads, d = g->head_dim;
+  if (24 * cdiv(blocks * hkv, 8) * 2 * d > UINT32_MAX || (ng + (int64_t)nb) * hkv * (d * d / 1024) * 256 > UINT32_MAX)
+    return fail(AUGTREE_ERR_UNSUPPORTED, "%lld blocks, %lld prompts and branches of %d KV heads exceed a launch",
+                (long long)blocks, (long long)ng + nb, g->num_kv_heads);
   L->blocks = blocks;
   const size_t state = (size_t)g->num_kv_heads * g->head_dim * g->head_dim * sizeof(float);
   L->states = align_up(state * (size_t)blocks);
@@ -285,20 +286,23 @@ int check_all(const Named* v, int n, bool required) {
 
 bool overlap(const void* a, size_t na, const void* b, size_t nb) {
   const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return a && b && x < y + nb && y < x + na;
+  return a && b && na && nb && x < y + nb && y < x + na;
 }
 
-// A tensor of a call, for the check that outputs are apart from all else.
+// A tensor of a call, for the check that outputs are apart from all else. An `in_place` output may be an `in_place`
+// input itself.
 struct Span {
   const void* p;
   size_t bytes;
   const char* name;
+  bool in_place = false;
 };
 
 int check_apart(const Span* in, int n_in, const Span* out, int n_out) {
   for (int i = 0; i < n_out; ++i) {
     for (int j = 0; j < n_in; ++j)
-      if (overlap(out[i].p, out[i].bytes, in[j].p, in[j].bytes))
+      if (overlap(out[i].p, out[i].bytes, in[j].p, in[j].bytes) &&
+          !(out[i].in_place && in[j].in_place && out[i].p == in[j].p))
         return fail(AUGTREE_ERR_INVALID_ARGUMENT, "%s overlaps %s", out[i].name, in[j].name);
     for (int j = 0; j < i; ++j)
       if (overlap(out[i].p, out[i].bytes, out[j].p, out[j].bytes))
@@ -356,9 +360,9 @@ int augtree_linear_fwd(const augtree_groups* grp, const float* decay, const uint
     if (!br && state_r) return fail(AUGTREE_ERR_INVALID_ARGUMENT, "state_r without branches");
     const Sizes z(grp);
     const Span ins[] = {{q_p, z.qp, "q_p"}, {k_p, z.kp, "k_p"}, {v_p, z.kp, "v_p"}, {q_r, z.qr, "q_r"},
-                        {k_r, z.kr, "k_r"}, {v_r, z.kr, "v_r"}, {state != state_p ? state : nullptr, z.sp, "state"}};
-    const Span outs[] = {{o_p, z.qp, "o_p"}, {o_r, z.qr, "o_r"}, {state_p, z.sp, "state_p"}, {state_r, z.sr, "state_r"},
-                         {ws, ws_bytes, "ws"}};
+                        {k_r, z.kr, "k_r"}, {v_r, z.kr, "v_r"}, {state, z.sp, "state", true}};
+    const Span outs[] = {{o_p, z.qp, "o_p"}, {o_r, z.qr, "o_r"}, {state_p, z.sp, "state_p", true},
+                         {state_r, z.sr, "state_r"}, {ws, ws_bytes, "ws"}};
     if ((st = check_apart(ins, 7, outs, 5))) return st;
     Call c;
     c.g = grp;
@@ -457,7 +461,7 @@ int augtree_linear_step(int32_t rows, int32_t num_q_heads, int32_t num_kv_heads,
     return fail(AUGTREE_ERR_INVALID_ARGUMENT, "rows=%d n_states=%d must be >= 0", rows, n_states);
   if (!src && n_states < rows)
     return fail(AUGTREE_ERR_INVALID_ARGUMENT, "%d states for %d rows without src", n_states, rows);
-  if ((int64_t)rows * num_kv_heads * (head_dim / 64) > INT32_MAX)
+  if ((int64_t)rows * num_kv_heads * (head_dim / 64) * 256 > UINT32_MAX)
     return fail(AUGTREE_ERR_UNSUPPORTED, "%d rows of %d KV heads exceed a launch", rows, num_kv_heads);
   if (rows == 0) return fail_status(AUGTREE_OK, "");
   const Named need[] = {{q, "q"}, {k, "k"}, {v, "v"}, {state_out, "state_out"}, {o, "o"}};
@@ -466,10 +470,10 @@ int augtree_linear_step(int32_t rows, int32_t num_q_heads, int32_t num_kv_heads,
     return st;
   const size_t state = (size_t)num_kv_heads * head_dim * head_dim * sizeof(float);
   const size_t nq = 2 * (size_t)rows * num_q_heads * head_dim, nk = 2 * (size_t)rows * num_kv_heads * head_dim;
-  const bool in_place = !src && state_in == state_out;  // otherwise a row could read what another one wrote
-  const Span ins[] = {{q, nq, "q"}, {k, nk, "k"}, {v, nk, "v"}, {in_place ? nullptr : state_in, state * n_states, "state_in"},
+  const bool in_place = !src;  // with src a row could read what another one wrote
+  const Span ins[] = {{q, nq, "q"}, {k, nk, "k"}, {v, nk, "v"}, {state_in, state * n_states, "state_in", in_place},
                       {src, 4 * (size_t)rows, "src"}};
-  const Span outs[] = {{state_out, state * rows, "state_out"}, {o, nq, "o"}};
+  const Span outs[] = {{state_out, state * rows, "state_out", in_place}, {o, nq, "o"}};
   if ((st = check_apart(ins, 5, outs, 2))) return st;
   if ((st = augtree_check_device())) return st;
   LinStepParams p;
@@ -526,7 +530,11 @@ int augtree_head_norm_fwd(int64_t rows, int32_t heads, int32_t head_dim, int act
   if (st) return st;
   if (rows == 0) return fail_status(AUGTREE_OK, "");
   const Named need[] = {{x, "x"}, {y, "y"}}, opt[] = {{gate, "gate"}, {weight, "weight"}, {bias, "bias"}};
-  if ((st = check_all(need, 2, true)) || (st = check_all(opt, 3, false)) || (st = augtree_check_device())) return st;
+  if ((st = check_all(need, 2, true)) || (st = check_all(opt, 3, false))) return st;
+  const size_t row = (size_t)heads * head_dim, all = 2 * row * rows;
+  const Span ins[] = {{x, all, "x", true}, {gate, all, "gate", true}, {weight, 4 * row, "weight"}, {bias, 4 * row, "bias"}};
+  const Span outs[] = {{y, all, "y", true}};
+  if ((st = check_apart(ins, 4, outs, 1)) || (st = augtree_check_device())) return st;
   HeadNormParams p;
   std::memset(&p, 0, sizeof(p));
   p.x = x;
@@ -560,7 +568,12 @@ int augtree_head_norm_bwd(int64_t rows, int32_t heads, int32_t head_dim, int act
   const bool sums = dweight || dbias;
   if (rows == 0 && !sums) return fail_status(AUGTREE_OK, "");
   if (sums && (st = check_ws(ws, ws_bytes, augtree_head_norm_workspace_size(rows, heads, head_dim)))) return st;
-  if ((st = augtree_check_device())) return st;
+  const size_t row = (size_t)heads * head_dim, all = 2 * row * rows;
+  const Span ins[] = {{x, all, "x", true}, {gate, all, "gate", true}, {dy, all, "dy", true}, {weight, 4 * row, "weight"},
+                      {bias, 4 * row, "bias"}};
+  const Span outs[] = {{dx, all, "dx", true}, {dgate, all, "dgate", true}, {dweight, 4 * row, "dweight"},
+                       {dbias, 4 * row, "dbias"}, {sums ? ws : nullptr, ws_bytes, "ws"}};
+  if ((st = check_apart(ins, 5, outs, 5)) || (st = augtree_check_device())) return st;
   HeadNormParams p;
   std::memset(&p, 0, sizeof(p));
   p.x = x;

@@ -128,3 +128,17 @@ def test_runs_repeat_and_replay():
         c = api.head_norm_bwd(*args, want_dweight=True, want_dbias=True)
         for u, v, w in zip(a, b, c):
             assert torch.equal(u, v) and torch.equal(u, w)
+
+
+def test_offsets_past_31_bits():
+    """Rows behind 2^31 elements, as on their own."""
+    rows, tail = 2 ** 31 // (16 * 128) + 50, 40
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    x, dy, gate = (torch.empty(rows, 16, 128, dtype=torch.bfloat16, device="cuda").normal_(generator=gen) for _ in range(3))
+    w, b = (torch.empty(16, 128, device="cuda").normal_(generator=gen) for _ in range(2))
+    last = [t[-tail:].contiguous() for t in (x, dy, gate)]
+    assert torch.equal(api.head_norm_fwd(x, w, b, gate, api.ACT_SILU)[-tail:],
+                       api.head_norm_fwd(last[0], w, b, last[2], api.ACT_SILU))
+    got = api.head_norm_bwd(x, dy, w, b, gate, api.ACT_SILU)
+    want = api.head_norm_bwd(*last[:2], w, b, last[2], api.ACT_SILU)
+    assert torch.equal(got[0][-tail:], want[0]) and torch.equal(got[1][-tail:], want[1])

@@ -320,3 +320,67 @@ def test_a_layer_trains_and_decodes():
     for n in par:
         e = np.linalg.norm(to64(gpu[n].grad) - ref[n].grad.numpy()) / np.linalg.norm(ref[n].grad.numpy())
         assert e <= 10 * 2.0 ** -8, (n, e)
+
+
+def test_a_tree_scanned_beside_a_longer_one():
+    """The longer tree has its branches scanned by a launch of their own, and the short one with it; alone the short
+    one's take one launch with its prompt."""
+    t1, t2 = (1500, [300, 20]), (200, [70, 333])
+    both, alone = batch([t1, t2], 2, 1, 128), batch([t2], 2, 1, 128)
+    dec = decays(1)
+    x = inputs(both, 29)
+    y = {n: t[(1500 if n.endswith("p") else 320):].contiguous() for n, t in x.items()}
+    a, c = run(both, dec, x), run(alone, dec, y)
+    for n in a:
+        at = (1 if n.endswith("p") else 2) if n.startswith("state") else 1500 if n.endswith("p") else 320
+        assert torch.equal(a[n][at:], c[n]), n
+
+
+def test_offsets_past_31_bits():
+    """A small tree behind one whose query rows take 2^31 elements, of prompt and branch: as on its own."""
+    n = 2 ** 31 // (16 * 128) + 65
+    b, alone = batch([(n, [n - 1]), (100, [70])], 16, 1, 128), batch([(100, [70])], 16, 1, 128)
+    dec = decays(1)
+    gen = torch.Generator(device="cuda").manual_seed(31)
+    x = {}
+    for side, t in (("p", b.tp), ("r", b.tr)):
+        for name, h in (("q", 16), ("k", 1), ("v", 1), ("do", 16)):
+            x[f"{name}_{side}"] = torch.empty(t, h, 128, dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    y = {k: t[n if k.endswith("p") else n - 1:].contiguous() for k, t in x.items()}
+    got, want = run(b, dec, x), run(alone, dec, y)
+    for k in want:
+        at = 1 if k.startswith("state") else n if k.endswith("p") else n - 1
+        assert torch.equal(got[k][at:], want[k]), k
+
+
+def test_captured_training_step_replays():
+    """Forward and backward through autograd in one graph. (No eager graph of the leaves is alive at the capture.)"""
+    b = batch([(150, [70, 33])], 4, 2, 64)
+    dec = decays(2)
+    x = inputs(b, 41)
+
+    def grads(leaves):
+        o_p, o_r = group_linear_attention(*leaves, b, dec)
+        return torch.autograd.grad((o_p, o_r), leaves, (x["do_p"], x["do_r"]))
+
+    def leaves():
+        return [x[n].clone().requires_grad_() for n in LEAVES]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        grads(leaves())
+    torch.cuda.synchronize()
+    static = leaves()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        got = grads(static)
+    for k in range(3):
+        y = inputs(b, 42 + k)
+        with torch.no_grad():
+            for n, t in zip(LEAVES, static):
+                x[n].copy_(y[n])
+                t.copy_(y[n])
+        g.replay()
+        torch.cuda.synchronize()
+        for u, v in zip(got, grads(leaves())):
+            assert torch.equal(u, v), k

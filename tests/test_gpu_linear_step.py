@@ -82,3 +82,21 @@ def test_captured_steps_replay():
         torch.cuda.synchronize()
         o2, want = api.linear_step(q, k, v, dec, want)
         assert torch.equal(o, o2) and torch.equal(state, want), i
+
+
+def test_offsets_past_32_bits():
+    """Rows behind 4 GiB of states, as on their own."""
+    rows, tail = 2 ** 32 // (128 * 128 * 4) + 40, 30
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    bf = lambda h: torch.empty(rows, h, 128, dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    q, k, v = bf(2), bf(1), bf(1)
+    s = torch.empty(rows, 1, 128, 128, device="cuda").normal_(generator=gen)
+    dec = decays(1)
+    src = torch.arange(rows - 1, -1, -1, dtype=torch.int32, device="cuda")
+    last = [t[-tail:].contiguous() for t in (q, k, v)]
+    o, new = api.linear_step(q, k, v, dec, s, src=src)
+    want = api.linear_step(*last, dec, s[:tail].flip(0).contiguous())
+    assert torch.equal(o[-tail:], want[0]) and torch.equal(new[-tail:], want[1])
+    want = api.linear_step(*last, dec, s[-tail:].contiguous())
+    o, new = api.linear_step(q, k, v, dec, s, state_out=s)
+    assert torch.equal(o[-tail:], want[0]) and torch.equal(s[-tail:], want[1])

@@ -172,6 +172,55 @@ def test_norm_refusals(C):
     assert bwd_(rows=0) == OK
 
 
+def test_norm_outputs_lie_apart(C):
+    n = 4 * 2 * 64 * 2
+
+    def inside(i):
+        return ctypes.c_void_p(at(i).value + n - 16)
+
+    def fwd_(y, x=at(0), gate=at(1), weight=at(2), bias=at(3)):
+        return C.augtree_head_norm_fwd(4, 2, 64, 1, 1e-5, x, gate, weight, bias, y, None)
+
+    def bwd_(dx=at(5), dgate=at(6), dw=at(7), db=at(8), ws=at(9)):
+        return C.augtree_head_norm_bwd(4, 2, 64, 1, 1e-5, at(0), at(1), at(2), at(3), at(4), dx, dgate, dw, db, ws, 1 << 30,
+                                       None)
+    for i in range(4):
+        assert fwd_(inside(i) if i < 2 else at(i)) == INVALID, i
+        assert b"overlaps" in C.augtree_last_error()
+    for kw in ("dx", "dgate", "dw", "db", "ws"):
+        for i in (0, 1, 4):
+            bad = ctypes.c_void_p(at(i).value + 256) if kw == "ws" else inside(i)
+            assert bwd_(**{kw: bad}) == INVALID, (kw, i)
+        assert bwd_(**{kw: at(2)}) == INVALID, kw
+    assert bwd_(dx=at(6)) == INVALID and bwd_(dx=at(0), dgate=at(0)) == INVALID and bwd_(db=at(7)) == INVALID
+    if not torch.cuda.is_available():
+        assert fwd_(at(0)) == DEVICE and fwd_(at(1)) == DEVICE and bwd_() == DEVICE
+        for i in (0, 1, 4):
+            assert bwd_(dx=at(i)) == DEVICE and bwd_(dgate=at(i)) == DEVICE
+
+
+def test_batches_beyond_a_launch(C):
+    """2^32 threads: the scan has 256 for every 1024 state elements of a segment, a step 256 for 64 columns."""
+    def size(trees, hkv, d):
+        b = GroupBatch(np.arange(trees + 1), np.zeros(trees + 1), [0], hkv, hkv, d)
+        return C.augtree_linear_workspace_size(b.ref, 0)
+    assert size(65535, 16, 128) > 0 and size(65536, 16, 128) == 0
+    assert size(65536 * 4 - 1, 16, 64) > 0 and size(65536 * 4, 16, 64) == 0
+
+    def step(rows):
+        return C.augtree_linear_step(rows, 128, 128, 128, 0.1, np.ones(128, np.float32).ctypes.data_as(ctypes.c_void_p),
+                                     None, at(3), at(4), rows, at(0), None, at(0), at(5), None)
+    assert step(65535) == INVALID and step(65536) == UNSUPPORTED
+
+
+def test_empty_responses_overlap_nothing(C):
+    """A batch without branches may come with response pointers, of no bytes, into other tensors."""
+    plain, d = GroupBatch([0, 10], [0, 0], [0], 4, 2, 64), dec(0.9, 0.9)
+    inner = ctypes.c_void_p(at(0).value + 64)
+    if not torch.cuda.is_available():
+        assert fwd(C, plain, d, o_r=inner) == DEVICE
+
+
 def test_python_refusals():
     b = GroupBatch(*GOOD, 4, 2, 64)
     z = lambda t, h: torch.zeros(t, h, 64, dtype=torch.bfloat16)
@@ -192,6 +241,11 @@ def test_python_refusals():
         group_linear_attention(*x, b, 0.9, state=torch.zeros(2, 2, 64, 64, requires_grad=True))
     with pytest.raises(ValueError, match="activation"):
         head_norm(x[0], activation="relu")
+    with pytest.raises(ValueError, match="cu_branch"):
+        api.linear_workspace_size(GroupBatch([0, 10, 25], [0, 3], [0, 5, 12, 20], 4, 2, 64))
+    for ws in (torch.zeros(64), torch.zeros(64, dtype=torch.uint8)[::2]):
+        with pytest.raises(ValueError, match="uint8"):
+            api._want_ws(ws, "ws")
 
 
 def test_block_cuts_follow_from_the_tree():
