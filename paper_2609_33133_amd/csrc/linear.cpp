@@ -99,15 +99,16 @@ int check_batch(const augtree_groups* g, const float* decay) {
 
 int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// Rows of a tree's blocks. A block is one workgroup a KV head in the state and
-// output kernels and three in the gradient kernel; the chip runs `slots` of them
-// at once (two a CU for d = 128, four for d = 64), so a launch takes whole rounds
-// of them, each as long as a block: its rows and its state's way through memory
-// (written, scanned and read: 16 d^2 bytes, as much as 4 d / (1 + group) rows'
-// own traffic). The rows that make these rounds shortest are taken. The tree
-// alone decides, so that its results do not depend on the batch. (32768-token
-// prompt, eight branches of 2048, 32 / 8 heads, forward + backward: 1320 us with
-// blocks of 512 rows, 1330 with 1024, 1280 with the 832 that fill one round.)
+// Rows of a tree's blocks. A block is a workgroup a KV head in each kernel; the
+// chip runs `slots` of them at once (for d = 128 two a CU, of the one for dk and
+// dv, whose workgroups are as large as two, one a CU; for d = 64 twice as many),
+// so a launch takes whole rounds, each as long as a block: its rows and its
+// state's way through memory (written, scanned and read: 16 d^2 bytes, as much as
+// 4 d / (1 + group) rows' own traffic). The rows that make the rounds of a training
+// step shortest are taken (output, dq, and dk and dv at 0.7 of their time a round).
+// The tree alone decides, so that its results do not depend on the batch.
+// (32768-token prompt, eight branches of 2048, 32 / 8 heads, forward + backward:
+// 1165 us with blocks of 512 rows, 1200 with 1024, 1110 with the 832 that fill a round.)
 int block_rows(const augtree_groups* g, int tree) {
   const int d = g->head_dim, hkv = g->num_kv_heads, nb = g->num_branches;
   const int64_t slots = d == 128 ? 512 : 1024;
@@ -120,8 +121,8 @@ int block_rows(const augtree_groups* g, int tree) {
     for (int b = nb ? g->cu_branch[tree] : 0; nb && b < g->cu_branch[tree + 1]; ++b)
       units += blocks(g->cu_resp[b + 1] - g->cu_resp[b], rows);
     units *= hkv;
-    const double cost = (double)(cdiv(units, slots) + cdiv(3 * units, slots)) * (rows + state);
-    if (!best || cost < best_cost) best = rows, best_cost = cost;
+    const double rounds = 2.0 * cdiv(units, slots) + 0.7 * cdiv(2 * units, slots);
+    if (!best || rounds * (rows + state) < best_cost) best = rows, best_cost = rounds * (rows + state);
   }
   return best;
 }
@@ -136,7 +137,7 @@ struct Layout {
 
 size_t align_up(size_t n) { return (n + 255) / 256 * 256; }
 
-// (A launch has fewer than 2^32 threads: the gradient and the scan kernels' are the most.)
+// (A launch has fewer than 2^32 threads: the state and the scan kernels' are the most.)
 int make_layout(const augtree_groups* g, Layout* L) {
   const int ng = g->num_groups, nb = g->num_branches;
   L->segs.resize((size_t)ng + nb);
@@ -166,7 +167,7 @@ int make_layout(const augtree_groups* g, Layout* L) {
       own[t] += add(ng + b, g->cu_resp[b], g->cu_resp[b + 1] - g->cu_resp[b], t, rows[t]);
   L->longest = *std::max_element(own.begin(), own.end());
   const int64_t hkv = g->num_kv_heads, d = g->head_dim;
-  if (24 * cdiv(blocks * hkv, 8) * 2 * d > UINT32_MAX || (ng + (int64_t)nb) * hkv * (d * d / 1024) * 256 > UINT32_MAX)
+  if (blocks * hkv * 4 * d > UINT32_MAX || (ng + (int64_t)nb) * hkv * (d * d / 1024) * 256 > UINT32_MAX)
     return fail(AUGTREE_ERR_UNSUPPORTED, "%lld blocks, %lld prompts and branches of %d KV heads exceed a launch",
                 (long long)blocks, (long long)ng + nb, g->num_kv_heads);
   L->blocks = blocks;
@@ -446,8 +447,12 @@ int augtree_linear_bwd(const augtree_groups* grp, const float* decay, const uint
     p.states_rev = rev;
     p.scale = grp->softmax_scale;
     p.b = c.b;
-    Hook h("linear_grad", c.stream);
-    if ((st = hip_ok(launch_lin_grad(p, grp->head_dim, c.stream), "gradient launch"))) return st;
+    {
+      Hook h("linear_dq", c.stream);
+      if ((st = hip_ok(launch_lin_dq(p, grp->head_dim, c.stream), "dq launch"))) return st;
+    }
+    Hook h("linear_dkv", c.stream);
+    if ((st = hip_ok(launch_lin_dkv(p, grp->head_dim, c.stream), "dk/dv launch"))) return st;
     return fail_status(AUGTREE_OK, "");
   });
 }

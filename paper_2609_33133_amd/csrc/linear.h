@@ -91,7 +91,8 @@ hipError_t launch_lin_state(const LinStateParams& p, int head_dim, bool reverse,
 // part: 0 whole trees, 1 prompts, 2 branches (1 and 2 hand over through `ends`, in the order of the direction)
 hipError_t launch_lin_scan(const LinScanParams& p, int head_dim, bool reverse, int part, hipStream_t stream);
 hipError_t launch_lin_out(const LinOutParams& p, int head_dim, hipStream_t stream);
-hipError_t launch_lin_grad(const LinGradParams& p, int head_dim, hipStream_t stream);
+hipError_t launch_lin_dq(const LinGradParams& p, int head_dim, hipStream_t stream);
+hipError_t launch_lin_dkv(const LinGradParams& p, int head_dim, hipStream_t stream);
 
 struct LinStepParams {
   const uint16_t *q, *k, *v;

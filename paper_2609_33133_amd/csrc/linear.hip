@@ -12,12 +12,13 @@
 // [d, d] in fp32. Three steps: each block's own state (lin_state_kernel), a scan
 // of the blocks' states along a segment and from the prompt into its branches,
 // or from the branches back onto the prompt (lin_scan_kernel), and the outputs,
-// every block from the state that reaches it (lin_out_kernel, lin_grad_kernel).
+// every block from the state that reaches it (lin_out_kernel, lin_dq_kernel,
+// lin_dkv_kernel).
 //
 // Each wavefront owns columns of z (16 in the state kernel, 32 in the others).
 // The state's columns stay in its accumulators (rows: y, column of the lane: z)
 // and serve from there as an operand of the next product, whose k index runs
-// over y.
+// over y. (The kernel for dk and dv hands it on through LDS: see there.)
 //
 // Roundings to bf16, all of them operands of matrix products: P, the decayed z of
 // the state's update and the state itself as an operand are each split into two
@@ -27,17 +28,16 @@
 // sixth of the time.
 //
 // What bounds it (49152 rows, 32 / 8 heads, d = 128; a copy reaches 4.9 TB/s
-// here): the forward's output kernel moves 1.0 GB in 250 us, 4.2 TB/s, the state
-// kernels 0.2 GB in 55 us forward and 0.8 GB in 167 us in reverse, 3.6 and 4.8
-// TB/s. The gradient kernel moves 2.3 GB past the L2s (1.7 read: dv and dk share
-// theirs, dq runs the other way through time) in 660 us, 3.6 TB/s, and has about
-// as much work on the CU: a wavefront needs 6900 cycles for 64 rows of a head,
-// beside one of another workgroup on its SIMD. Of these, two such wavefronts keep
-// the matrix cores busy for 3600, the LDS for 3000 and the vector unit for about
-// as many. The clock is what the chip's power leaves, 1.4 to 1.9 GHz of 2.4. Other
-// shapes of it took the same time within 3 %: 8 wavefronts of 16 columns (four on
-// a SIMD instead of two, but 2.4 times the LDS reads), P in 32 x 32 tiles,
-// wavefront priorities, three barriers a head instead of two.
+// here): the output and dq kernels move 1.0 GB each in 234 us, 4.4 TB/s, the state
+// kernels 0.2 GB in 57 us forward and 0.8 GB in 168 us in reverse, 3.6 and 4.8
+// TB/s. The kernel for dk and dv moves 1.2 GB in 340 us, 3.6 TB/s; its matrix
+// cores and its LDS are busy for 40 % of that each, in phases that barriers part.
+// The clock is what the chip's power leaves, 1.4 to 2.0 GHz of 2.4. Taken or left
+// within 3 % of the time: P in 32 x 32 tiles, 8 wavefronts of 16 columns, wavefront
+// priorities, tiles fetched half a step earlier, operands of a product with P all
+// read ahead of it.
+#include <type_traits>
+
 #include "common.h"
 #include "linear.h"
 
@@ -234,9 +234,8 @@ __device__ __forceinline__ void scale_state(f32x4* s, float f) {
 // A [64, D] tile on its way from memory to LDS through registers: fetch()
 // issues the loads, put() waits for them and writes the swizzled tile. The loads
 // of the next tiles are in flight while a chunk is worked on (they arrive before
-// they are waited for: 150 cycles of a step of 6900 go to that and the barrier),
-// and LDS holds one tile of each operand, so that two workgroups fit a CU. Rows
-// from n on are zeros.
+// they are waited for: 200 cycles of a step of 5500 go to that and the barrier),
+// and LDS holds one tile of each operand. Rows from n on are zeros.
 template <int D, int NW>
 struct TileStage {
   static constexpr int CH = D / 8, RPI = 64 / CH, ROWS = NW * RPI, NI = C / ROWS;  // pieces of a row; rows of a pass
@@ -415,9 +414,8 @@ __global__ __launch_bounds__(256) void lin_scan_kernel(LinScanParams p, int part
 
 // ---------------------------------------------------------------------------- outputs
 
-// The product of one block and KV head (see the top of the file). Forward: x
-// and out have `group` heads for each head of y and z. Reverse: y and z have,
-// and their terms are summed.
+// The product of one block and KV head, forward in time (see the top of the
+// file): x and out have `group` heads for each head of y and z.
 struct Product {
   const uint16_t *x, *y, *z;
   uint16_t* out;
@@ -427,10 +425,11 @@ struct Product {
 // Rows 32 tx + l32 (< n) of a chunk, 32 columns from `out` on. The buffer's range
 // ends behind row n - 1, so later rows are not written.
 template <int D>
-__device__ __forceinline__ void store_rows(uint16_t* out, const f32x16* acc, float scale, int n, int64_t stride, int l32,
-                                           int hf) {
+__device__ __forceinline__ void store_rows(uint16_t* out, const f32x16* acc, float scale, int n, int64_t stride,
+                                           int l32, int hf) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)out, 0, (int)(2 * n * stride), 0x00020000);
+  const __amdgpu_buffer_rsrc_t rsrc =
+      __builtin_amdgcn_make_buffer_rsrc((void*)out, 0, (int)(2 * n * stride), 0x00020000);
   const uint32_t at = 2 * (uint32_t)(l32 * stride) + 16 * hf;
 #pragma unroll
   for (int tx = 0; tx < 2; ++tx) {
@@ -448,16 +447,6 @@ __device__ __forceinline__ void store_rows(uint16_t* out, const f32x16* acc, flo
   }
 #endif
 }
-
-template <int D>
-struct OutShared {
-  __attribute__((aligned(1024))) __bf16 xt[C * D];
-  __attribute__((aligned(1024))) __bf16 yt[C * D];
-  __attribute__((aligned(1024))) __bf16 zt[C * D];
-  // P as two bf16 terms, x by y in 32 x 32 tiles: (0, 0), the one off the diagonal, (1, 1)
-  __attribute__((aligned(1024))) __bf16 pt[2][3][32 * 32];
-  Decays decays;
-};
 
 // 32x32x16 products (see common.h): lane l holds row (column) l % 32, k indices
 // 8 (l / 32) .. + 7; register i of the result column l % 32, row acc_row(i, l / 32).
@@ -485,10 +474,51 @@ __device__ __forceinline__ bf16x8 read_columns32(const __bf16* tile, int base, i
 // that registers 8 s .. 8 s + 7 hold 8 consecutive ones and x is read plainly.
 __device__ __forceinline__ int state32_row(int t, int i, int hf) { return 32 * t + 16 * (i >> 3) + 8 * hf + (i & 7); }
 
-// element offset of the 16-byte piece `ch` (0..3) of row r of a [32, 32] tile of P
+// 8 elements from byte `at` of a tile
+__device__ __forceinline__ bf16x8 read8(const __bf16* tile, int at) {
+  return *reinterpret_cast<const bf16x8*>(reinterpret_cast<const char*>(tile) + at);
+}
+
+// P as two bf16 terms, x by y in 32 x 32 tiles: (0, 0), the one off the diagonal, (1, 1)
+typedef __bf16 PTiles[2][3][32 * 32];
+// element offset of the 16-byte piece `ch` (0..3) of row r of such a tile
 __device__ __forceinline__ int poff(int r, int ch) { return 32 * r + 8 * (ch ^ ((r >> 2) & 3)); }
 
-template <int D, bool REV, bool TS>
+// This lane's four elements (x l16, y 4 q .. + 3) of the 16 x 16 tile (tx, ty), in the order of the transposed z:
+// y = 4 q of k step ty % 2 is piece 2 (ty % 2) + q % 2, half q / 2.
+// w: their decays.
+__device__ __forceinline__ void put_p(PTiles& pt, int tx, int ty, const f32x4& a, const float* w, int q, int l16) {
+  u32x2 v, u;
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const float f0 = a[2 * e] * w[2 * e], f1 = a[2 * e + 1] * w[2 * e + 1];
+    v[e] = bf16_pair(f0, f1);
+    u[e] = bf16_pair(f0 - __uint_as_float(v[e] << 16), f1 - __uint_as_float(v[e] & 0xffff0000u));
+  }
+  const int k = (ty >> 1) == (tx >> 1) ? 2 * (tx >> 1) : 1;
+  const int o = poff(16 * (tx & 1) + l16, 2 * (ty & 1) + (q & 1)) + 4 * (q >> 1);
+  *reinterpret_cast<u32x2*>(pt[0][k] + o) = v;
+  *reinterpret_cast<u32x2*>(pt[1][k] + o) = u;
+}
+
+template <int THREADS>
+__device__ __forceinline__ void clear(void* p, int bytes) {
+  for (int i = threadIdx.x; i < bytes / 16; i += THREADS) static_cast<raw16*>(p)[i] = raw16{0u, 0u, 0u, 0u};
+}
+
+template <int N>
+using Int = std::integral_constant<int, N>;
+
+template <int D>
+struct OutShared {
+  __attribute__((aligned(1024))) __bf16 xt[C * D];
+  __attribute__((aligned(1024))) __bf16 yt[C * D];
+  __attribute__((aligned(1024))) __bf16 zt[C * D];
+  __attribute__((aligned(1024))) PTiles pt;
+  Decays decays;
+};
+
+template <int D, bool TS>
 __device__ __forceinline__ void lin_out(OutShared<D>& sh, const LinBatch& batch, float scale, const Block& bl, int kvh,
                                         const Product& pr) {
   constexpr int NW = D / 32;  // wavefronts, and tiles of the state's rows
@@ -496,33 +526,32 @@ __device__ __forceinline__ void lin_out(OutShared<D>& sh, const LinBatch& batch,
   const int hf = lane >> 5, l32 = lane & 31;
   const float lg = batch.log2_decay[kvh];
   const int g = batch.group;
-  const int64_t stride_q = (int64_t)batch.heads_kv * g * D, stride_kv = (int64_t)batch.heads_kv * D;
-  const int64_t stride_x = REV ? stride_kv : stride_q, stride_y = REV ? stride_q : stride_kv;
-  const int64_t off_x = bl.row0 * stride_x + (int64_t)kvh * (REV ? 1 : g) * D;
-  const int64_t off_y = bl.row0 * stride_y + (int64_t)kvh * (REV ? g : 1) * D;
+  const int64_t stride_x = (int64_t)batch.heads_kv * g * D, stride_y = (int64_t)batch.heads_kv * D;
+  const int64_t off_x = bl.row0 * stride_x + (int64_t)kvh * g * D, off_y = bl.row0 * stride_y + (int64_t)kvh * D;
   const uint16_t* const x = pr.x + off_x;
   const uint16_t* const y = pr.y + off_y;
   const uint16_t* const z = pr.z + off_y;
   uint16_t* const out = pr.out + off_x;
   typedef TileStage<D, NW> Stage;
-  Stage s0, s1, s2;  // forward: x, y, z; reverse: y, z, x
+  Stage sx, sy, sz;
   const uint32_t src_x = Stage::source(stride_x), src_y = Stage::source(stride_y);
   const int dst = Stage::target();
 
   const int chunks = (bl.len + C - 1) / C;
-  auto chunk_of = [&](int ci) { return REV ? chunks - 1 - ci : ci; };
-  auto rows_of = [&](int c) { return min(C, bl.len - c * C); };
-  auto fetch_x = [&](Stage& a, int ci, int h) {
-    const int c = chunk_of(ci);
-    a.fetch(x + c * C * stride_x + h * D, src_x, rows_of(c), stride_x);
+  auto rows_of = [&](int c) { return c < chunks ? min(C, bl.len - c * C) : 0; };
+  // (Nothing is fetched behind the last head, by a range of no rows: under a branch the registers of both ways would be
+  // copied, and the copies wait for the loads.)
+  int fetched = 0, head = 0;  // chunk and head of the next fetch of x
+  auto fetch_x = [&]() {
+    sx.fetch(x + fetched * C * stride_x + head * D, src_x, rows_of(fetched), stride_x);
+    if (++head == g) head = 0, ++fetched;
   };
-  auto fetch_yz = [&](Stage& a, Stage& b, int ci, int h) {
-    const int c = chunk_of(ci);
-    a.fetch(y + c * C * stride_y + h * D, src_y, rows_of(c), stride_y);
-    b.fetch(z + c * C * stride_y + h * D, src_y, rows_of(c), stride_y);
+  auto fetch_yz = [&](int c) {
+    sy.fetch(y + c * C * stride_y, src_y, rows_of(c), stride_y);
+    sz.fetch(z + c * C * stride_y, src_y, rows_of(c), stride_y);
   };
-  if (REV) fetch_x(s2, 0, 0), fetch_yz(s0, s1, 0, 0);
-  else fetch_yz(s1, s2, 0, 0), fetch_x(s0, 0, 0);
+  fetch_yz(0);
+  fetch_x();
 
   // bytes: this lane's four columns of y (exchanged order) and z, its row of a tile's first 32, its row of a tile of P
   const int c4 = 16 * ((lane >> 4) & 1);
@@ -532,7 +561,7 @@ __device__ __forceinline__ void lin_out(OutShared<D>& sh, const LinBatch& batch,
   const int pbase = 2 * poff(l32, hf);
   set_pair_decays<2 * D>(sh.decays, lg);
   // the 16 x 16 tiles of P beside the diagonal that are masked stay zero
-  for (int i = threadIdx.x; i < 2 * 3 * 32 * 32 / 8; i += 2 * D) reinterpret_cast<raw16*>(sh.pt)[i] = raw16{0u, 0u, 0u, 0u};
+  clear<2 * D>(&sh.pt, sizeof(sh.pt));
 
   // the state that reaches the block
   f32x16 s[NW];
@@ -547,52 +576,39 @@ __device__ __forceinline__ void lin_out(OutShared<D>& sh, const LinBatch& batch,
       }
   }
 
-  // row l32 of a tile's half `half`, 8 columns from 16 ks + 8 hf on
-  auto read8 = [&](const __bf16* tile, int base, int half, int ks) {
-    return *reinterpret_cast<const bf16x8*>(reinterpret_cast<const char*>(tile) + half * 64 * D + (base ^ (32 * ks)));
-  };
   // P^T in 16 x 16 tiles (16x16x32 products, a lane having one x and four y), of which the 10 on and beside the diagonal
-  // are dealt to the wavefronts: tile k is (i, j), j <= i, with i (i + 1) / 2 + j = k. (The three 32 x 32 tiles they make
-  // up leave one of four wavefronts without one.)
+  // are dealt to the wavefronts: tile k is (tx, ty), ty <= tx, with tx (tx + 1) / 2 + ty = k. (The three 32 x 32 tiles
+  // they make up leave one of four wavefronts without one.) A wavefront forms its tiles k0, k0 + NW, ... side by side.
   const int q = lane >> 4, l16 = lane & 15;
   const int rbase16 = 2 * loff<D>(l16, 8 * q);
-  auto p_tile = [&](int ty, int tx) {
+  auto p_tiles = [&](auto count, int k0) {
+    constexpr int N = decltype(count)::value;
     const int rb = here(rbase16);
-    const char* const yt = reinterpret_cast<const char*>(sh.yt) + ty * 32 * D;
-    const char* const xt = reinterpret_cast<const char*>(sh.xt) + tx * 32 * D;
-    f32x4 a = {0.f, 0.f, 0.f, 0.f};
+    int tx[N], ty[N];
+    f32x4 a[N];
+    float w[N][4];
+#pragma unroll
+    for (int r = 0; r < N; ++r) {
+      const int k = k0 + r * NW;
+      tx[r] = (k >= 1) + (k >= 3) + (k >= 6);
+      ty[r] = k - tx[r] * (tx[r] + 1) / 2;
+      a[r] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[r][e] = sh.decays.pair[32 + 16 * (tx[r] - ty[r]) + l16 - 4 * q - e];
+    }
 #pragma unroll
     for (int ks = 0; ks < D / 32; ++ks)
-      a = mfma16(*reinterpret_cast<const bf16x8*>(yt + (rb ^ (64 * ks))),
-                 *reinterpret_cast<const bf16x8*>(xt + (rb ^ (64 * ks))), a);
-    const float* const pw = sh.decays.pair + 32 + (REV ? 16 * (ty - tx) + 4 * q - l16 : 16 * (tx - ty) + l16 - 4 * q);
-    u32x2 v, u;
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const float f0 = a[2 * e] * pw[REV ? 2 * e : -2 * e], f1 = a[2 * e + 1] * pw[REV ? 2 * e + 1 : -2 * e - 1];
-      v[e] = bf16_pair(f0, f1);
-      u[e] = bf16_pair(f0 - __uint_as_float(v[e] << 16), f1 - __uint_as_float(v[e] & 0xffff0000u));
-    }
-    // in the order of the transposed z: y = 4 q of k step ty % 2 is piece 2 (ty % 2) + q % 2, half q / 2
-    const int k = (ty >> 1) == (tx >> 1) ? 2 * (tx >> 1) : 1;
-    const int o = poff(16 * (tx & 1) + l16, 2 * (ty & 1) + (q & 1)) + 4 * (q >> 1);
-    *reinterpret_cast<u32x2*>(sh.pt[0][k] + o) = v;
-    *reinterpret_cast<u32x2*>(sh.pt[1][k] + o) = u;
-  };
-  auto p_tiles = [&]() {
+      for (int r = 0; r < N; ++r)
+        a[r] = mfma16(read8(sh.yt + ty[r] * 16 * D, rb ^ (64 * ks)), read8(sh.xt + tx[r] * 16 * D, rb ^ (64 * ks)),
+                      a[r]);
 #pragma unroll
-    for (int r = 0; r < (10 + NW - 1) / NW; ++r) {
-      const int k = r * NW + wave;
-      if (k >= 10) break;
-      const int i = (k >= 1) + (k >= 3) + (k >= 6), j = k - i * (i + 1) / 2;
-      if (REV) p_tile(i, j);
-      else p_tile(j, i);
-    }
+    for (int r = 0; r < N; ++r) put_p(sh.pt, tx[r], ty[r], a[r], w[r], q, l16);
   };
 
   f32x16 acc[2];
   // acc = out^T [z, x] of what reaches the chunk: S^T X^T, the state as two bf16 terms, and its decay to each row
-  auto from_state = [&](int n) {
+  auto from_state = [&]() {
     const int xb = here(rbase);
 #pragma unroll
     for (int tx = 0; tx < 2; ++tx)
@@ -605,7 +621,7 @@ __device__ __forceinline__ void lin_out(OutShared<D>& sh, const LinBatch& batch,
       for (int e = 0; e < 8; ++e) f[e] = s[ks >> 1][8 * (ks & 1) + e];
       bf16x8 hi, lo;
       split2(f, hi, lo);
-      const bf16x8 x0 = read8(sh.xt, xb, 0, ks), x1 = read8(sh.xt, xb, 1, ks);
+      const bf16x8 x0 = read8(sh.xt, xb ^ (32 * ks)), x1 = read8(sh.xt + 32 * D, xb ^ (32 * ks));
       acc[0] = mfma32(hi, x0, acc[0]);
       acc[1] = mfma32(hi, x1, acc[1]);
       acc[0] = mfma32(lo, x0, acc[0]);
@@ -614,7 +630,7 @@ __device__ __forceinline__ void lin_out(OutShared<D>& sh, const LinBatch& batch,
 #pragma unroll
     for (int tx = 0; tx < 2; ++tx) {
       const int r = 32 * tx + l32;
-      const float lead = exp2f(lg * (float)(REV ? max(n - r, 0) : r + 1));
+      const float lead = exp2f(lg * (float)(r + 1));
 #pragma unroll
       for (int i = 0; i < 16; ++i) acc[tx][i] *= lead;
     }
@@ -629,9 +645,8 @@ __device__ __forceinline__ void lin_out(OutShared<D>& sh, const LinBatch& batch,
 #pragma unroll
         for (int tx = 0; tx < 2; ++tx) {
           const int ty = m >> 1;
-          if (REV ? ty < tx : ty > tx) continue;  // masked
-          const char* t = reinterpret_cast<const char*>(sh.pt[k][ty == tx ? 2 * tx : 1]);
-          acc[tx] = mfma32(zf[m], *reinterpret_cast<const bf16x8*>(t + (pb ^ (32 * (m & 1)))), acc[tx]);
+          if (ty > tx) continue;  // masked
+          acc[tx] = mfma32(zf[m], read8(sh.pt[k][ty == tx ? 2 * tx : 1], pb ^ (32 * (m & 1))), acc[tx]);
         }
   };
   // s += Y^T (w Z)
@@ -660,68 +675,40 @@ __device__ __forceinline__ void lin_out(OutShared<D>& sh, const LinBatch& batch,
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[t][i] *= f;
   };
-  auto store = [&](int c, int h, int n) {
-    store_rows<D>(out + c * C * stride_x + h * D + 32 * wave, acc, scale, n, stride_x, l32, hf);
-  };
-
-  // Two barriers a head: behind the first its tiles are in LDS, behind the second P is, and all that reads the tiles has
-  // read them (forward: but for y and z, once a chunk), so that the next ones may be written beside the product with P.
+  // Two barriers a head: behind the first its tiles are in LDS, behind the second P is, and all that reads x (and, with
+  // the chunk's last head, y) has read it.
   int row_n = -1;
-  for (int ci = 0; ci < chunks; ++ci) {
-    const int c = chunk_of(ci), n = rows_of(c);
-    const bool more = ci + 1 < chunks;
-    const float fade = exp2f(lg * (float)n);
-    if constexpr (REV) {
-      s2.put(sh.xt, dst);
-      if (n != row_n) set_row_decays<REV>(sh.decays, lg, n), row_n = n;
-      if (ci == 0) s0.put(sh.yt, dst), s1.put(sh.zt, dst);
-      for (int h = 0; h < g; ++h) {
-        __syncthreads();
-        if (h + 1 < g) fetch_yz(s0, s1, ci, h + 1);
-        else if (more) fetch_yz(s0, s1, ci + 1, 0), fetch_x(s2, ci + 1, 0);
-        if (h == 0) {
-          from_state(n);
-          fade_state(fade);
-        }
-        bf16x8 zf[4];
+  for (int c = 0; c < chunks; ++c) {
+    const int n = rows_of(c);
+    if (c > 0) __syncthreads();  // y has been read by the state's update
+    sy.put(sh.yt, dst);
+    sz.put(sh.zt, dst);
+    if (c + 1 < chunks) fetch_yz(c + 1);
+    if (n != row_n) set_row_decays<false>(sh.decays, lg, n), row_n = n;
+    bf16x8 zf[4];
+    for (int h = 0; h < g; ++h) {
+      sx.put(sh.xt, dst);
+      __syncthreads();
+      fetch_x();
+      if (h == 0) {
 #pragma unroll
         for (int m = 0; m < 4; ++m) zf[m] = read_columns32<D>(sh.zt, zbase, 0, m);
-        p_tiles();
-        update(zf);
-        __syncthreads();
-        if (more || h + 1 < g) s0.put(sh.yt, dst), s1.put(sh.zt, dst);
-        from_chunk(zf);
       }
-      store(c, 0, n);
-    } else {
-      if (ci > 0) __syncthreads();  // y has been read by the state's update
-      s1.put(sh.yt, dst);
-      s2.put(sh.zt, dst);
-      if (n != row_n) set_row_decays<REV>(sh.decays, lg, n), row_n = n;
-      bf16x8 zf[4];
-      for (int h = 0; h < g; ++h) {
-        s0.put(sh.xt, dst);
-        __syncthreads();
-        if (h + 1 < g) fetch_x(s0, ci, h + 1);
-        else if (more) fetch_x(s0, ci + 1, 0), fetch_yz(s1, s2, ci + 1, 0);
-        if (h == 0) {
+      if (NW == 2) p_tiles(Int<5>{}, wave);
+      else if (wave < 2) p_tiles(Int<3>{}, wave);
+      else p_tiles(Int<2>{}, wave);
+      // (the state's two terms are formed again for every head: kept over the loop they take registers, which then
+      // spill. The empty asm keeps the compiler from doing that.)
 #pragma unroll
-          for (int m = 0; m < 4; ++m) zf[m] = read_columns32<D>(sh.zt, zbase, 0, m);
-        }
-        p_tiles();
-        // (the state's two terms are formed again for every head: kept over the loop they take registers, which then
-        // spill. The empty asm keeps the compiler from doing that.)
-#pragma unroll
-        for (int t = 0; t < NW; ++t) asm volatile("" : "+v"(s[t]));
-        from_state(n);
-        __syncthreads();
-        from_chunk(zf);
-        store(c, h, n);
-      }
-      if (more) {
-        fade_state(fade);
-        update(zf);
-      }
+      for (int t = 0; t < NW; ++t) asm volatile("" : "+v"(s[t]));
+      from_state();
+      __syncthreads();
+      from_chunk(zf);
+      store_rows<D>(out + c * C * stride_x + h * D + 32 * wave, acc, scale, n, stride_x, l32, hf);
+    }
+    if (c + 1 < chunks) {
+      fade_state(exp2f(lg * (float)n));
+      update(zf);
     }
   }
 }
@@ -734,31 +721,255 @@ __global__ __launch_bounds__(2 * D, 2) void lin_out_kernel(LinOutParams p) {
   const int side = bl.prompt ? 0 : 1;
   const float* state = p.states + ((int64_t)block * p.b.heads_kv + kvh) * D * D;
   const Product pr = {p.q[side], p.k[side], p.v[side], p.o[side], state};
-  lin_out<D, false, false>(sh, p.b, p.scale, bl, kvh, pr);
+  lin_out<D, false>(sh, p.b, p.scale, bl, kvh, pr);
 }
 
-// dq, dv and dk: three workgroups a block and KV head, one after the other on
-// one XCD (workgroups go to the 8 XCDs in turn), so that what they share of q,
-// k, v and do comes from memory once.
 template <int D>
-__global__ __launch_bounds__(2 * D, 2) void lin_grad_kernel(LinGradParams p) {
+__global__ __launch_bounds__(2 * D, 2) void lin_dq_kernel(LinGradParams p) {
   __shared__ OutShared<D> sh;
-  const int j = blockIdx.x >> 3, unit = (j / 3) * 8 + (blockIdx.x & 7), role = j % 3;
-  if (unit >= p.b.num_blocks * p.b.heads_kv) return;
-  const int block = unit / p.b.heads_kv, kvh = unit - block * p.b.heads_kv;
+  const int block = blockIdx.x / p.b.heads_kv, kvh = blockIdx.x - block * p.b.heads_kv;
   const Block bl = find_block(p.b, block);
   const int side = bl.prompt ? 0 : 1;
-  const int64_t at = ((int64_t)block * p.b.heads_kv + kvh) * D * D;
-  if (role == 0) {
-    const Product pr = {p.dout[side], p.v[side], p.k[side], p.dq[side], p.states + at};
-    lin_out<D, false, true>(sh, p.b, p.scale, bl, kvh, pr);
-  } else if (role == 1) {
-    const Product pr = {p.k[side], p.q[side], p.dout[side], p.dv[side], p.states_rev + at};
-    lin_out<D, true, false>(sh, p.b, p.scale, bl, kvh, pr);
-  } else {
-    const Product pr = {p.v[side], p.dout[side], p.q[side], p.dk[side], p.states_rev + at};
-    lin_out<D, true, true>(sh, p.b, p.scale, bl, kvh, pr);
+  const float* const state = p.states + ((int64_t)block * p.b.heads_kv + kvh) * D * D;
+  const Product pr = {p.dout[side], p.v[side], p.k[side], p.dq[side], state};
+  lin_out<D, true>(sh, p.b, p.scale, bl, kvh, pr);
+}
+
+// ---------------------------------------------------------------------------- dk and dv
+
+// Both sum over the query heads and run backwards in time, and their states are
+// one and the transpose of it: dv_t = k_t S, dk_t = v_t S^T with S = sum q_j do_j^T.
+// So a workgroup forms both, with two kinds of wavefronts that take 32 columns each:
+// those of dv own columns of S, as the accumulators of its update, and those of dk
+// form P for both. Between chunks S goes through LDS as two bf16 terms, where dv's
+// wavefronts read it by rows and dk's by columns. The two kinds share SIMDs: one is
+// busy with matrix products where the other waits for LDS or converts. (Workgroups
+// of their own for dk and dv, two a CU, each with a state and P: 1160 us for forward
+// and backward of those 49152 rows where this takes 1075.)
+template <int D>
+struct DkvShared {
+  __attribute__((aligned(1024))) __bf16 kt[C * D];
+  __attribute__((aligned(1024))) __bf16 vt[C * D];
+  __attribute__((aligned(1024))) __bf16 qt[C * D];
+  __attribute__((aligned(1024))) __bf16 gt[C * D];     // do
+  __attribute__((aligned(1024))) PTiles pt[2];         // of dv, of dk
+  // S^T as two bf16 terms: a row for each column of do (the second and third four of every 16 exchanged)
+  __attribute__((aligned(1024))) __bf16 st[2][D * D];
+  Decays decays;
+};
+
+template <int D, bool OF_K>
+__device__ __forceinline__ void lin_dkv(DkvShared<D>& sh, const LinGradParams& p, const Block& bl, int block, int kvh,
+                                        int wave) {
+  constexpr int NW = D / 32;  // wavefronts of either kind, and tiles of the state's rows
+  const int side = bl.prompt ? 0 : 1;
+  const int lane = threadIdx.x & 63;
+  const int hf = lane >> 5, l32 = lane & 31, q4 = lane >> 4, l16 = lane & 15;
+  const float lg = p.b.log2_decay[kvh];
+  const int g = p.b.group;
+  const int64_t stride_q = (int64_t)p.b.heads_kv * g * D, stride_k = (int64_t)p.b.heads_kv * D;
+  const int64_t off_q = bl.row0 * stride_q + (int64_t)kvh * g * D, off_k = bl.row0 * stride_k + (int64_t)kvh * D;
+  const uint16_t *const qp = p.q[side] + off_q, *const gp = p.dout[side] + off_q;
+  const uint16_t *const kp = p.k[side] + off_k, *const vp = p.v[side] + off_k;
+  uint16_t* const out = (OF_K ? p.dk[side] : p.dv[side]) + off_k;
+
+  typedef TileStage<D, 2 * NW> Stage;
+  Stage sq, sg, sk, sv;
+  const uint32_t src_q = Stage::source(stride_q), src_k = Stage::source(stride_k);
+  const int dst = Stage::target();
+  const int chunks = (bl.len + C - 1) / C;
+  auto rows_of = [&](int c) { return min(C, bl.len - c * C); };
+  // (Nothing is fetched behind the last head, by a range of no rows: under a branch the registers of both ways would be
+  // copied, and the copies wait for the loads.)
+  int fetched = 0, head = 0;  // chunk and head of the next fetch
+  auto fetch_q = [&]() {
+    const int c = chunks - 1 - fetched, n = fetched < chunks ? rows_of(c) : 0;
+    sq.fetch(qp + c * C * stride_q + head * D, src_q, n, stride_q);
+    sg.fetch(gp + c * C * stride_q + head * D, src_q, n, stride_q);
+    const int next = head + 1 == g;
+    head = __builtin_amdgcn_readfirstlane(next ? 0 : head + 1);
+    fetched = __builtin_amdgcn_readfirstlane(fetched + next);
+  };
+  auto fetch_k = [&](int ci) {
+    const int c = chunks - 1 - ci, n = ci < chunks ? rows_of(c) : 0;
+    sk.fetch(kp + c * C * stride_k, src_k, n, stride_k);
+    sv.fetch(vp + c * C * stride_k, src_k, n, stride_k);
+  };
+  auto put_q = [&]() {
+    sq.put(sh.qt, dst);
+    sg.put(sh.gt, dst);
+    fetch_q();
+  };
+  fetch_k(0);
+  fetch_q();
+
+  const int c4 = 16 * ((lane >> 4) & 1);
+  const int ybase = column32_base<D>(c4 + 4 * (((lane & 1) << 1) | ((lane >> 1) & 1)), lane);
+  const int zbase = column32_base<D>(32 * wave + c4 + 4 * (lane & 3), lane);
+  const int rbase = 2 * loff<D>(l32, 8 * hf), rbase16 = 2 * loff<D>(l16, 8 * q4);
+  const int pbase = 2 * poff(l32, hf);
+  const int g4 = (l32 >> 2) & 3;
+  const int srow = 32 * wave + (l32 & 19) + 4 * (((g4 & 1) << 1) | (g4 >> 1));
+  const int sbase = 2 * loff<D>(srow, 8 * hf);
+  set_pair_decays<4 * D>(sh.decays, lg);
+  clear<4 * D>(&sh.pt, sizeof(sh.pt));
+
+  f32x16 s[NW];  // dv: the state that reaches the chunk
+  auto put_state = [&]() {
+    const int sb = here(sbase);
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) {
+      float f[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) f[e] = s[ks >> 1][8 * (ks & 1) + e];
+      bf16x8 hi, lo;
+      split2(f, hi, lo);
+      *reinterpret_cast<bf16x8*>(reinterpret_cast<char*>(sh.st[0]) + (sb ^ (32 * ks))) = hi;
+      *reinterpret_cast<bf16x8*>(reinterpret_cast<char*>(sh.st[1]) + (sb ^ (32 * ks))) = lo;
+    }
+  };
+  if constexpr (!OF_K) {
+    const float* const in = p.states_rev + ((int64_t)block * p.b.heads_kv + kvh) * D * D;
+#pragma unroll
+    for (int t = 0; t < NW; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[t][i] = in[state32_row(t, i, hf) * D + 32 * wave + l32];
+    put_state();
   }
+
+  // P^T of two rows of 16 x 16 tiles (y) against those of x before them and at their own place
+  auto p_rows = [&](auto r0, auto r1, int which) {
+    constexpr int R0 = decltype(r0)::value, R1 = decltype(r1)::value;
+    static_assert(R0 > R1, "the longer row first");
+    const __bf16 *const yt = which ? sh.gt : sh.qt, *const xt = which ? sh.vt : sh.kt;
+    const int rb = here(rbase16);
+    f32x4 a[R0 + R1 + 2];
+#pragma unroll
+    for (int t = 0; t < R0 + R1 + 2; ++t) a[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int ks = 0; ks < D / 32; ++ks) {
+      const int at = rb ^ (64 * ks);
+      const bf16x8 y0 = read8(yt + R0 * 16 * D, at), y1 = read8(yt + R1 * 16 * D, at);
+#pragma unroll
+      for (int t = 0; t <= R0; ++t) {
+        const bf16x8 x = read8(xt + t * 16 * D, at);
+        a[t] = mfma16(y0, x, a[t]);
+        if (t <= R1) a[R0 + 1 + t] = mfma16(y1, x, a[R0 + 1 + t]);
+      }
+    }
+    const float* const pw = sh.decays.pair + 32 + 4 * q4 - l16;
+    float w[R0 + 1][4];
+#pragma unroll
+    for (int t = 0; t <= R0; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[t][e] = pw[16 * t + e];
+#pragma unroll
+    for (int t = 0; t < R0 + R1 + 2; ++t) {
+      const int ty = t <= R0 ? R0 : R1, tx = t <= R0 ? t : t - R0 - 1;
+      put_p(sh.pt[which], tx, ty, a[t], w[ty - tx], q4, l16);
+    }
+  };
+
+  put_q();
+  f32x16 acc[2];  // out^T [column, row]
+  // Two barriers a head, as in lin_out: behind the first its tiles and S are in LDS, behind the second P is, and tiles and
+  // S have been read.
+  int row_n = -1;
+  for (int ci = 0; ci < chunks; ++ci) {
+    const int c = chunks - 1 - ci, n = rows_of(c);
+    const bool more = ci + 1 < chunks;
+    sk.put(sh.kt, dst);
+    sv.put(sh.vt, dst);
+    if (more) fetch_k(ci + 1);
+    if (n != row_n) set_row_decays<true>(sh.decays, lg, n), row_n = n;
+    for (int h = 0; h < g; ++h) {
+      __syncthreads();
+      if (h == 0) {
+#pragma unroll
+        for (int tx = 0; tx < 2; ++tx)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[tx][i] = 0.f;
+        const int xb = here(rbase), sb = here(OF_K ? zbase : sbase);
+        const __bf16* const xt = OF_K ? sh.vt : sh.kt;
+#pragma unroll
+        for (int ks = 0; ks < D / 16; ++ks) {
+          bf16x8 hi, lo;
+          if constexpr (OF_K) hi = read_columns32<D>(sh.st[0], sb, 0, ks), lo = read_columns32<D>(sh.st[1], sb, 0, ks);
+          else hi = read8(sh.st[0], sb ^ (32 * ks)), lo = read8(sh.st[1], sb ^ (32 * ks));
+          const bf16x8 x0 = read8(xt, xb ^ (32 * ks)), x1 = read8(xt + 32 * D, xb ^ (32 * ks));
+          acc[0] = mfma32(hi, x0, acc[0]);
+          acc[1] = mfma32(hi, x1, acc[1]);
+          acc[0] = mfma32(lo, x0, acc[0]);
+          acc[1] = mfma32(lo, x1, acc[1]);
+        }
+#pragma unroll
+        for (int tx = 0; tx < 2; ++tx) {
+          const float lead = exp2f(lg * (float)max(n - 32 * tx - l32, 0));
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[tx][i] *= lead;
+        }
+      }
+      bf16x8 zf[4];
+#pragma unroll
+      for (int m = 0; m < 4; ++m) zf[m] = read_columns32<D>(OF_K ? sh.qt : sh.gt, zbase, 0, m);
+      if constexpr (OF_K) {
+        if (NW == 2 || wave < 2) p_rows(Int<3>{}, Int<0>{}, wave & 1);
+        if (NW == 2 || wave >= 2) p_rows(Int<2>{}, Int<1>{}, wave & 1);
+      } else {
+        if (h == 0) {
+          const float fade = exp2f(lg * (float)n);
+#pragma unroll
+          for (int t = 0; t < NW; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[t][i] *= fade;
+        }
+        const int yb = here(ybase);
+        const float* const w = sh.decays.row + 4 * hf;
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+          const f32x4 w0 = *reinterpret_cast<const f32x4*>(w + 16 * m);
+          const f32x4 w1 = *reinterpret_cast<const f32x4*>(w + 16 * m + 8);
+          float f[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) f[e] = (float)zf[m][e] * (e < 4 ? w0[e] : w1[e - 4]);
+          bf16x8 hi, lo;
+          split2(f, hi, lo);
+#pragma unroll
+          for (int t = 0; t < NW; ++t) {
+            const bf16x8 a = read_columns32<D>(sh.qt, yb, 64 * t, m);
+            s[t] = mfma32(a, hi, s[t]);
+            s[t] = mfma32(a, lo, s[t]);
+          }
+        }
+      }
+      __syncthreads();
+      put_q();
+      const int pb = here(pbase);
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
+#pragma unroll
+          for (int tx = 0; tx < 2; ++tx) {
+            const int ty = m >> 1;
+            if (ty < tx) continue;  // masked
+            acc[tx] = mfma32(zf[m], read8(sh.pt[OF_K][k][ty == tx ? 2 * tx : 1], pb ^ (32 * (m & 1))), acc[tx]);
+          }
+    }
+    if constexpr (!OF_K)
+      if (more) put_state();
+    store_rows<D>(out + c * C * stride_k + 32 * wave, acc, p.scale, n, stride_k, l32, hf);
+  }
+}
+
+template <int D>
+__global__ __launch_bounds__(4 * D, 2) void lin_dkv_kernel(LinGradParams p) {
+  __shared__ DkvShared<D> sh;
+  const int block = blockIdx.x / p.b.heads_kv, kvh = blockIdx.x - block * p.b.heads_kv;
+  const Block bl = find_block(p.b, block);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (wave < D / 32) lin_dkv<D, false>(sh, p, bl, block, kvh, wave);
+  else lin_dkv<D, true>(sh, p, bl, block, kvh, wave - D / 32);
 }
 
 __global__ __launch_bounds__(256) void lin_table_kernel(LinTable t) {
@@ -799,10 +1010,17 @@ hipError_t launch_lin_out(const LinOutParams& p, int head_dim, hipStream_t strea
   return hipGetLastError();
 }
 
-hipError_t launch_lin_grad(const LinGradParams& p, int head_dim, hipStream_t stream) {
-  const dim3 grid((p.b.num_blocks * p.b.heads_kv + 7) / 8 * 24);
-  if (head_dim == 128) lin_grad_kernel<128><<<grid, 256, 0, stream>>>(p);
-  else lin_grad_kernel<64><<<grid, 128, 0, stream>>>(p);
+hipError_t launch_lin_dq(const LinGradParams& p, int head_dim, hipStream_t stream) {
+  const dim3 grid(p.b.num_blocks * p.b.heads_kv);
+  if (head_dim == 128) lin_dq_kernel<128><<<grid, 256, 0, stream>>>(p);
+  else lin_dq_kernel<64><<<grid, 128, 0, stream>>>(p);
+  return hipGetLastError();
+}
+
+hipError_t launch_lin_dkv(const LinGradParams& p, int head_dim, hipStream_t stream) {
+  const dim3 grid(p.b.num_blocks * p.b.heads_kv);
+  if (head_dim == 128) lin_dkv_kernel<128><<<grid, 512, 0, stream>>>(p);
+  else lin_dkv_kernel<64><<<grid, 256, 0, stream>>>(p);
   return hipGetLastError();
 }
 

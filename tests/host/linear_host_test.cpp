@@ -112,10 +112,14 @@ hipError_t launch_lin_out(const LinOutParams& p, int, hipStream_t) {
   inside(p.states, state_bytes() * p.b.num_blocks, "states");
   return launched("out");
 }
-hipError_t launch_lin_grad(const LinGradParams& p, int, hipStream_t) {
+hipError_t launch_lin_dq(const LinGradParams& p, int, hipStream_t) {
+  check_batch(p.b);
+  return launched("dq");
+}
+hipError_t launch_lin_dkv(const LinGradParams& p, int, hipStream_t) {
   check_batch(p.b);
   inside(p.states_rev, state_bytes() * p.b.num_blocks, "reverse states");
-  return launched("grad");
+  return launched("dkv");
 }
 hipError_t launch_lin_step(const LinStepParams&, int, hipStream_t) { return launched("step"); }
 hipError_t launch_head_norm_fwd(const HeadNormParams&, hipStream_t) { return launched("norm"); }
@@ -187,7 +191,7 @@ int main() {
         splits += split;
         std::string want;
         if (!kept) want += split ? "state scan_p scan_r " : "state scan ";
-        if (backward) want += split ? "state_rev scan_rev_r scan_rev_p grad " : "state_rev scan_rev grad ";
+        if (backward) want += split ? "state_rev scan_rev_r scan_rev_p dq dkv " : "state_rev scan_rev dq dkv ";
         else want += "out ";
         check(order == want, order.c_str());
       }
