@@ -30,7 +30,7 @@
 // What bounds it (49152 rows, 32 / 8 heads, d = 128; a copy reaches 4.9 TB/s
 // here): the output and dq kernels move 1.0 GB each in 234 us, 4.4 TB/s, the state
 // kernels 0.2 GB in 57 us forward and 0.8 GB in 168 us in reverse, 3.6 and 4.8
-// TB/s. The kernel for dk and dv moves 1.2 GB in 340 us, 3.6 TB/s; its matrix
+// TB/s. The kernel for dk and dv moves 1.2 GB in 330 us, 3.7 TB/s; its matrix
 // cores and its LDS are busy for 40 % of that each, in phases that barriers part.
 // The clock is what the chip's power leaves, 1.4 to 2.0 GHz of 2.4. Taken or left
 // within 3 % of the time: P in 32 x 32 tiles, 8 wavefronts of 16 columns, wavefront
@@ -745,7 +745,7 @@ __global__ __launch_bounds__(2 * D, 2) void lin_dq_kernel(LinGradParams p) {
 // wavefronts read it by rows and dk's by columns. The two kinds share SIMDs: one is
 // busy with matrix products where the other waits for LDS or converts. (Workgroups
 // of their own for dk and dv, two a CU, each with a state and P: 1160 us for forward
-// and backward of those 49152 rows where this takes 1075.)
+// and backward of those 49152 rows where this takes 1065.)
 template <int D>
 struct DkvShared {
   __attribute__((aligned(1024))) __bf16 kt[C * D];
@@ -837,11 +837,12 @@ __device__ __forceinline__ void lin_dkv(DkvShared<D>& sh, const LinGradParams& p
     put_state();
   }
 
+  bf16x8 xr[4][D / 32];  // dk: x of the chunk's tiles of P, the same for all heads
   // P^T of two rows of 16 x 16 tiles (y) against those of x before them and at their own place
   auto p_rows = [&](auto r0, auto r1, int which) {
     constexpr int R0 = decltype(r0)::value, R1 = decltype(r1)::value;
     static_assert(R0 > R1, "the longer row first");
-    const __bf16 *const yt = which ? sh.gt : sh.qt, *const xt = which ? sh.vt : sh.kt;
+    const __bf16* const yt = which ? sh.gt : sh.qt;
     const int rb = here(rbase16);
     f32x4 a[R0 + R1 + 2];
 #pragma unroll
@@ -852,9 +853,8 @@ __device__ __forceinline__ void lin_dkv(DkvShared<D>& sh, const LinGradParams& p
       const bf16x8 y0 = read8(yt + R0 * 16 * D, at), y1 = read8(yt + R1 * 16 * D, at);
 #pragma unroll
       for (int t = 0; t <= R0; ++t) {
-        const bf16x8 x = read8(xt + t * 16 * D, at);
-        a[t] = mfma16(y0, x, a[t]);
-        if (t <= R1) a[R0 + 1 + t] = mfma16(y1, x, a[R0 + 1 + t]);
+        a[t] = mfma16(y0, xr[t][ks], a[t]);
+        if (t <= R1) a[R0 + 1 + t] = mfma16(y1, xr[t][ks], a[R0 + 1 + t]);
       }
     }
     const float* const pw = sh.decays.pair + 32 + 4 * q4 - l16;
@@ -913,6 +913,14 @@ __device__ __forceinline__ void lin_dkv(DkvShared<D>& sh, const LinGradParams& p
 #pragma unroll
       for (int m = 0; m < 4; ++m) zf[m] = read_columns32<D>(OF_K ? sh.qt : sh.gt, zbase, 0, m);
       if constexpr (OF_K) {
+        if (h == 0) {
+          const __bf16* const xt = wave & 1 ? sh.vt : sh.kt;
+          const int rb = here(rbase16);
+#pragma unroll
+          for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int ks = 0; ks < D / 32; ++ks) xr[t][ks] = read8(xt + t * 16 * D, rb ^ (64 * ks));
+        }
         if (NW == 2 || wave < 2) p_rows(Int<3>{}, Int<0>{}, wave & 1);
         if (NW == 2 || wave >= 2) p_rows(Int<2>{}, Int<1>{}, wave & 1);
       } else {
@@ -925,21 +933,31 @@ __device__ __forceinline__ void lin_dkv(DkvShared<D>& sh, const LinGradParams& p
         }
         const int yb = here(ybase);
         const float* const w = sh.decays.row + 4 * hf;
+        // (operands of the next 16 rows are read, and their z weighed, beside the products of these)
+        bf16x8 a[2][NW], hi[2], lo[2];
+        auto operands = [&](int m) {
 #pragma unroll
-        for (int m = 0; m < 4; ++m) {
+          for (int t = 0; t < NW; ++t) a[m & 1][t] = read_columns32<D>(sh.qt, yb, 64 * t, m);
+        };
+        auto weigh = [&](int m) {
           const f32x4 w0 = *reinterpret_cast<const f32x4*>(w + 16 * m);
           const f32x4 w1 = *reinterpret_cast<const f32x4*>(w + 16 * m + 8);
           float f[8];
 #pragma unroll
           for (int e = 0; e < 8; ++e) f[e] = (float)zf[m][e] * (e < 4 ? w0[e] : w1[e - 4]);
-          bf16x8 hi, lo;
-          split2(f, hi, lo);
+          split2(f, hi[m & 1], lo[m & 1]);
+        };
+        operands(0);
+        weigh(0);
 #pragma unroll
-          for (int t = 0; t < NW; ++t) {
-            const bf16x8 a = read_columns32<D>(sh.qt, yb, 64 * t, m);
-            s[t] = mfma32(a, hi, s[t]);
-            s[t] = mfma32(a, lo, s[t]);
-          }
+        for (int m = 0; m < 4; ++m) {
+          if (m < 3) operands(m + 1);
+          __builtin_amdgcn_sched_barrier(0);
+          if (m < 3) weigh(m + 1);
+#pragma unroll
+          for (int t = 0; t < NW; ++t) s[t] = mfma32(a[m & 1][t], hi[m & 1], s[t]);
+#pragma unroll
+          for (int t = 0; t < NW; ++t) s[t] = mfma32(a[m & 1][t], lo[m & 1], s[t]);
         }
       }
       __syncthreads();
