@@ -522,7 +522,7 @@ def head_norm_bwd(x, dy, weight=None, bias=None, gate=None, activation: int = AC
     _norm_inputs(x, gate, weight, bias)
     _want(dy, "dy", torch.bfloat16, x.shape)
     rows, heads, d = x.shape
-    dev, f32, lib = on.device, torch.float32, _lib.load()
+    dev, f32 = on.device, torch.float32
     with on as st:
         dx = _out(dx, "dx", torch.bfloat16, x.shape, dev)
         if gate is not None:
@@ -532,10 +532,18 @@ def head_norm_bwd(x, dy, weight=None, bias=None, gate=None, activation: int = AC
         if want_dbias or dbias is not None:
             dbias = _out(dbias, "dbias", f32, (heads, d), dev)
         _want_ws(ws, "ws")
-        if ws is None and (dweight is not None or dbias is not None):
-            ws = torch.empty(int(lib.augtree_head_norm_workspace_size(rows, heads, d)), dtype=torch.uint8, device=dev)
-        _lib.check(lib.augtree_head_norm_bwd(rows, heads, d, int(activation), float(eps), _addr(x), _addr(gate),
-                                             _addr(weight), _addr(bias), _addr(dy), _addr(dx), _addr(dgate), _addr(dweight),
-                                             _addr(dbias), _addr(ws), 0 if ws is None else ws.numel(),
-                                             st), "head_norm_bwd")
+        _head_norm_bwd(x, dy, weight, bias, gate, int(activation), float(eps), dx, dgate, dweight, dbias, ws, st)
     return dx, dgate, dweight, dbias
+
+
+def _head_norm_bwd(x, dy, weight, bias, gate, activation, eps, dx, dgate, dweight, dbias, ws, stream):
+    """The call of head_norm_bwd behind its checks."""
+    rows, heads, d = x.shape
+    lib, n = _lib.load(), 0
+    if dweight is not None or dbias is not None:
+        if ws is None:
+            ws = torch.empty(lib.augtree_head_norm_workspace_size(rows, heads, d), dtype=torch.uint8, device=x.device)
+        n = ws.numel()
+    _lib.check(lib.augtree_head_norm_bwd(rows, heads, d, activation, eps, _addr(x), _addr(gate), _addr(weight),
+                                         _addr(bias), _addr(dy), _addr(dx), _addr(dgate), _addr(dweight), _addr(dbias),
+                                         _addr(ws), n, stream), "head_norm_bwd")

@@ -89,7 +89,7 @@ class _GroupLinearAttention(torch.autograd.Function):
         ws = torch.empty(api.linear_workspace_size(b), dtype=torch.uint8, device=q_p.device)
         o_p, o_r, state_p, state_r = api.linear_fwd(b, decay, *x, state=state, want_states=return_state, ws=ws)
         ctx.save_for_backward(*x, state, ws)  # the states in ws serve the backward too
-        ctx.batch, ctx.decay = b, decay
+        ctx.batch, ctx.decay, ctx.ws_bytes = b, decay, api.linear_workspace_size(b, True)
         if not return_state:
             return o_p, o_r
         ctx.mark_non_differentiable(state_p, state_r)
@@ -99,15 +99,13 @@ class _GroupLinearAttention(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, do_p, do_r, *_):
         q_p, k_p, v_p, q_r, k_r, v_r, state, ws = ctx.saved_tensors
-        # an output that did not reach the loss has a zero gradient
-        do_p = torch.zeros_like(q_p) if do_p is None else do_p.to(torch.bfloat16).contiguous()
-        do_r = torch.zeros_like(q_r) if do_r is None else do_r.to(torch.bfloat16).contiguous()
-        # the forward has checked what it saved; the outputs' gradients are new
-        api._linear_inputs(ctx.batch, (("do_p", do_p), ("do_r", do_r)))
-        with api._On((("q_p", q_p), ("do_p", do_p), ("do_r", do_r))) as stream:
+        # the forward has checked what it saved, autograd the gradients' shapes and device (zeros for an unused output)
+        do_p, do_r = do_p.to(torch.bfloat16).contiguous(), do_r.to(torch.bfloat16).contiguous()
+        with api._On((("q_p", q_p),)) as stream:
             grads = [torch.empty_like(t) for t in (q_p, k_p, v_p, q_r, k_r, v_r)]
-            api._linear_bwd(ctx.batch, ctx.decay, (q_p, k_p, v_p, do_p, q_r, k_r, v_r, do_r, state, *grads), ws,
-                            api._linear_ws(ctx.batch, True, None, q_p.device), stream)
+            bwd_ws = torch.empty(ctx.ws_bytes, dtype=torch.uint8, device=q_p.device)
+            api._linear_bwd(ctx.batch, ctx.decay, (q_p, k_p, v_p, do_p, q_r, k_r, v_r, do_r, state, *grads), ws, bwd_ws,
+                            stream)
         return (*grads, None, None, None, None)
 
 
@@ -143,9 +141,15 @@ class _HeadNorm(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, dy):
         x, weight, bias, gate = ctx.saved_tensors
-        dx, dgate, dweight, dbias = api.head_norm_bwd(
-            x, dy.to(torch.bfloat16).contiguous(), weight, bias, gate, ctx.activation, ctx.eps,
-            want_dweight=ctx.needs_input_grad[1], want_dbias=ctx.needs_input_grad[2])
+        # the forward has checked what it saved, autograd the gradient's shape and device
+        dy = dy.to(torch.bfloat16).contiguous()
+        with api._On((("x", x),)) as stream:
+            dx = torch.empty_like(x)
+            dgate = None if gate is None else torch.empty_like(gate)
+            dweight = torch.empty_like(weight) if ctx.needs_input_grad[1] else None
+            dbias = torch.empty_like(bias) if ctx.needs_input_grad[2] else None
+            api._head_norm_bwd(x, dy, weight, bias, gate, ctx.activation, ctx.eps, dx, dgate, dweight, dbias, None,
+                               stream)
         return dx, dweight, dbias, dgate, None, None
 
 
