@@ -99,30 +99,41 @@ int check_batch(const augtree_groups* g, const float* decay) {
 
 int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// Rows of a tree's blocks. A block is a workgroup a KV head in each kernel; the
-// chip runs `slots` of them at once (for d = 128 two a CU, of the one for dk and
-// dv, whose workgroups are as large as two, one a CU; for d = 64 twice as many),
-// so a launch takes whole rounds, each as long as a block: its rows and its
-// state's way through memory (written, scanned and read: 16 d^2 bytes, as much as
-// 4 d / (1 + group) rows' own traffic). The rows that make the rounds of a training
-// step shortest are taken (output, dq, and dk and dv at 0.7 of their time a round).
-// The tree alone decides, so that its results do not depend on the batch.
-// (32768-token prompt, eight branches of 2048, 32 / 8 heads, forward + backward:
-// 1165 us with blocks of 512 rows, 1200 with 1024, 1110 with the 832 that fill a round.)
+// Rounds of `units` workgroups with at most `per_cu` on each of 256 CUs; w of them on a CU take sqrt(w) times
+// as long as one (measured: 1.42 for two, 2.0 for four).
+double rounds(int64_t units, int per_cu) {
+  const int64_t rest = units % (256 * per_cu);
+  return (double)(units / (256 * per_cu)) * std::sqrt((double)per_cu) + std::sqrt((double)cdiv(rest, 256));
+}
+
+// Rows of a tree's blocks: those for which this model of a training step's kernels gives the shortest time. A
+// workgroup of the output kernel takes `row` us a row and 2 d / (1 + group) rows' time for its state; dq and
+// the state kernels come to 1.75 of that; dk and dv take 0.9 a row and twice the state, with workgroups that
+// fill twice the room; each of the two scans moves the states once in and out at 4.7 TB/s, but takes 0.23 us
+// for every block of its longest chain. Measured against it (sums of the kernels, us, 32 / 8 heads, d = 128,
+// blocks of 64, 128, 192 and 256 rows): prompt of 417 rows with six branches of 64 to 977 132, 123, 152, 181
+// (model 121, 104, 132, 161); 4096 rows with eight of 1024 447, 361, 401, 342 (382, 282, 349, 264). 32768
+// rows with eight of 2048, forward + backward: 1110 us with the 832 rows chosen, 1165 with 512, 1200 with
+// 1024. The tree alone decides, so that its results do not depend on the batch.
 int block_rows(const augtree_groups* g, int tree) {
-  const int d = g->head_dim, hkv = g->num_kv_heads, nb = g->num_branches;
-  const int64_t slots = d == 128 ? 512 : 1024;
+  const int d = g->head_dim, hkv = g->num_kv_heads, nb = g->num_branches, group = g->num_q_heads / hkv;
+  const double row = group * (d == 128 ? 0.033 : 0.025), state = 2.0 * d / (1 + group);
   auto blocks = [](int32_t len, uint32_t rows) { return ((uint32_t)len + rows - 1) / rows; };
-  const double state = 4.0 * d / (1 + g->num_q_heads / hkv);
   int best = 0;
   double best_cost = 0;
   for (int rows = kLinChunk; rows <= 1024; rows += kLinChunk) {
-    int64_t units = blocks(g->cu_prompt[tree + 1] - g->cu_prompt[tree], rows);
-    for (int b = nb ? g->cu_branch[tree] : 0; nb && b < g->cu_branch[tree + 1]; ++b)
-      units += blocks(g->cu_resp[b + 1] - g->cu_resp[b], rows);
+    const int64_t prompt = blocks(g->cu_prompt[tree + 1] - g->cu_prompt[tree], rows);
+    int64_t units = prompt, longest = 0;
+    for (int b = nb ? g->cu_branch[tree] : 0; nb && b < g->cu_branch[tree + 1]; ++b) {
+      const int64_t n = blocks(g->cu_resp[b + 1] - g->cu_resp[b], rows);
+      units += n;
+      longest = std::max(longest, n);
+    }
     units *= hkv;
-    const double rounds = 2.0 * cdiv(units, slots) + 0.7 * cdiv(2 * units, slots);
-    if (!best || rounds * (rows + state) < best_cost) best = rows, best_cost = rounds * (rows + state);
+    const double cost = 2.75 * row * (rows + state) * rounds(units, d == 128 ? 2 : 4) +
+                        0.9 * row * (rows + 2 * state) * rounds(units, d == 128 ? 1 : 2) +
+                        2 * std::max((double)units * d * d * 8 / 4.7e6, 0.23 * (double)(prompt + longest));
+    if (!best || cost < best_cost) best = rows, best_cost = cost;
   }
   return best;
 }
