@@ -109,7 +109,7 @@ double rounds(int64_t units, int per_cu) {
 // Rows of a tree's blocks: those for which this model of a training step's kernels gives the shortest time. A
 // workgroup of the output kernel takes `row` us a row and 2 d / (1 + group) rows' time for its state; dq and
 // the state kernels come to 1.75 of that; dk and dv take 0.9 a row and twice the state, with workgroups that
-// fill twice the room; each of the two scans moves the states once in and out at 4.7 TB/s, but takes 0.23 us
+// fill twice the room; each of the two scans moves the states once in and out at 4.7 TB/s, but takes 0.12 us
 // for every block of its longest chain. Measured against it (sums of the kernels, us, 32 / 8 heads, d = 128,
 // blocks of 64, 128, 192 and 256 rows): prompt of 417 rows with six branches of 64 to 977 132, 123, 152, 181
 // (model 121, 104, 132, 161); 4096 rows with eight of 1024 447, 361, 401, 342 (382, 282, 349, 264). 32768
@@ -132,7 +132,7 @@ int block_rows(const augtree_groups* g, int tree) {
     units *= hkv;
     const double cost = 2.75 * row * (rows + state) * rounds(units, d == 128 ? 2 : 4) +
                         0.9 * row * (rows + 2 * state) * rounds(units, d == 128 ? 1 : 2) +
-                        2 * std::max((double)units * d * d * 8 / 4.7e6, 0.23 * (double)(prompt + longest));
+                        2 * std::max((double)units * d * d * 8 / 4.7e6, 0.12 * (double)(prompt + longest));
     if (!best || cost < best_cost) best = rows, best_cost = cost;
   }
   return best;
@@ -262,13 +262,10 @@ struct Call {
     c.ends = ends;
     c.out_p = out_p;
     c.out_r = out_r;
-    c.skip_prompt = s.skip_prompt;
-    c.skip_branch = s.skip_branch;
     c.b = b;
     // A tree's blocks are scanned by one launch, its branches one after the other, where they are few; else prompts and
-    // branches get a launch each, in which the branches run side by side. A launch costs 5 us and each block of the chain
-    // about 0.3 (32 / 8 heads, d = 128, one launch against two: 64 blocks, 8 branches, 24 us against 19; 258 blocks, 16
-    // branches, 122 us against 57).
+    // branches get a launch each, in which the branches run side by side (32 / 8 heads, d = 128, one launch against two:
+    // 64 blocks, 8 branches, 24 us against 19; 258 blocks, 16 branches, 122 us against 57).
     const bool split = branches && L.longest > kScanBlocks;
     for (int k = 0; k < (split ? 2 : 1); ++k) {
       const int part = !split ? 0 : (k == 0) != reverse ? 1 : 2;

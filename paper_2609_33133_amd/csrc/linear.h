@@ -51,7 +51,6 @@ struct LinScanParams {
   float* ends;          // forward: [num_trees] prompts' ends; reverse: [num_branches] branches' ends
   float* out_p;         // forward: user's copies of the prompts' and branches' ends, or nullptr
   float* out_r;
-  int32_t skip_prompt, skip_branch;  // the last block's own state was left out
   LinBatch b;
 };
 

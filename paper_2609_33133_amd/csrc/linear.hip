@@ -342,33 +342,50 @@ struct Scan {
   __device__ __forceinline__ void store(float* base, int64_t i, f32x4 v) const {
     *reinterpret_cast<f32x4*>(base + i * per + at) = v;
   }
-  // One segment: every block's own state is replaced by the carry that reaches it. Eight blocks are loaded ahead, which
-  // hides most of the way to memory: 64 blocks of 0.5 MB, read and written in a chain, take 25 us. Workgroups of one
-  // wavefront instead of four (more CUs with work) took the same.
+  // One segment: every block's own state is replaced by the carry that reaches it. While a group of eight blocks is
+  // worked on the next one is on its way: from sixteen blocks on without a branch, behind which the wait for a load would
+  // take in all that are on their way.
   template <bool REV>
-  __device__ __forceinline__ f32x4 segment(const LinSeg& s, f32x4 carry, bool skip) const {
+  __device__ __forceinline__ f32x4 segment(const LinSeg& s, f32x4 carry) const {
     constexpr int kAhead = 8;
     const int count = (s.len + s.rows - 1) / s.rows, last = count - 1;
-    for (int i0 = 0; i0 < count; i0 += kAhead) {
-      f32x4 own[kAhead];
+    const float fade = exp2f(lg * (float)s.rows), short_fade = exp2f(lg * (float)(s.len - last * s.rows));
+    auto block = [&](int i) { return REV ? last - i : i; };
+    auto pass = [&](f32x4 own, int i) {
+      store(p.states, s.block0 + block(i), carry);
+      carry = carry * (block(i) == last ? short_fade : fade) + own;
+    };
+    f32x4 a[kAhead], b[kAhead];
+    int i0 = 0;
+    if (count >= 2 * kAhead) {
+      auto fetch = [&](f32x4* own, int i) {
 #pragma unroll
-      for (int k = 0; k < kAhead; ++k) {
-        const int i = i0 + k;
-        if (i < count) own[k] = load(p.states, s.block0 + (REV ? last - i : i));
-      }
+        for (int k = 0; k < kAhead; ++k) own[k] = load(p.states, s.block0 + block(min(i + k, last)));
+      };
+      fetch(a, 0);
+      for (; i0 + 2 * kAhead <= count; i0 += 2 * kAhead) {
+        fetch(b, i0 + kAhead);
 #pragma unroll
-      for (int k = 0; k < kAhead; ++k) {
-        const int i = i0 + k, j = REV ? last - i : i;
-        if (i >= count) break;
-        store(p.states, s.block0 + j, carry);
-        if (i == last && skip) break;  // its own state was left out
-        carry = carry * exp2f(lg * (float)min(s.rows, s.len - j * s.rows)) + own[k];
+        for (int k = 0; k < kAhead; ++k) pass(a[k], i0 + k);
+        fetch(a, i0 + 2 * kAhead);
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) pass(b[k], i0 + kAhead + k);
       }
+    }
+    for (; i0 < count; i0 += kAhead) {
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k)
+        if (i0 + k < count) a[k] = load(p.states, s.block0 + block(i0 + k));
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k)
+        if (i0 + k < count) pass(a[k], i0 + k);
     }
     return carry;
   }
 };
 
+// Where the state kernel left a segment's last block out, what is found there ends in a carry that nobody reads.
+//
 // A workgroup takes 1024 elements of the states of one KV head of a tree. `part`:
 // 0 the whole tree, 1 its prompt alone, 2 one branch of it (the grid then has a
 // workgroup for every branch).
@@ -383,9 +400,9 @@ __global__ __launch_bounds__(256) void lin_scan_kernel(LinScanParams p, int part
   if (part == 2) {
     const LinSeg s = load_segment(p.b, p.b.num_trees + i);
     if (REV) {
-      scan.store(p.ends, i, scan.segment<true>(s, zero, false));
+      scan.store(p.ends, i, scan.segment<true>(s, zero));
     } else {
-      const f32x4 end = scan.segment<false>(s, scan.load(p.ends, s.link), p.skip_branch);
+      const f32x4 end = scan.segment<false>(s, scan.load(p.ends, s.link));
       if (p.out_r) scan.store(p.out_r, i, end);
     }
     return;
@@ -394,18 +411,28 @@ __global__ __launch_bounds__(256) void lin_scan_kernel(LinScanParams p, int part
   const int b0 = prompt.link, b1 = i + 1 < p.b.num_trees ? load_segment(p.b, i + 1).link : p.b.num_branches;
   if (REV) {
     f32x4 carry = zero;
-    for (int b = b0; b < b1; ++b)
-      carry += part == 1 ? scan.load(p.ends, b)
-                         : scan.segment<true>(load_segment(p.b, p.b.num_trees + b), zero, false);
-    scan.segment<true>(prompt, carry, p.skip_prompt);
+    if (part == 0) {
+      for (int b = b0; b < b1; ++b) carry += scan.segment<true>(load_segment(p.b, p.b.num_trees + b), zero);
+    } else {
+      for (int b = b0; b < b1; b += 8) {
+        f32x4 e[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if (b + k < b1) e[k] = scan.load(p.ends, b + k);
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if (b + k < b1) carry += e[k];
+      }
+    }
+    scan.segment<true>(prompt, carry);
   } else {
-    const f32x4 end = scan.segment<false>(prompt, p.init ? scan.load(p.init, i) : zero, p.skip_prompt);
+    const f32x4 end = scan.segment<false>(prompt, p.init ? scan.load(p.init, i) : zero);
     if (p.out_p) scan.store(p.out_p, i, end);
     if (part == 1) {
       scan.store(p.ends, i, end);
     } else {
       for (int b = b0; b < b1; ++b) {
-        const f32x4 e = scan.segment<false>(load_segment(p.b, p.b.num_trees + b), end, p.skip_branch);
+        const f32x4 e = scan.segment<false>(load_segment(p.b, p.b.num_trees + b), end);
         if (p.out_r) scan.store(p.out_r, b, e);
       }
     }
