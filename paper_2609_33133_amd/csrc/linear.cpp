@@ -138,7 +138,7 @@ int block_rows(const augtree_groups* g, int tree) {
   return best;
 }
 
-constexpr int64_t kScanBlocks = 16;
+constexpr int64_t kScanBlocks = 32;
 
 struct Layout {
   std::vector<LinSeg> segs;
@@ -264,8 +264,8 @@ struct Call {
     c.out_r = out_r;
     c.b = b;
     // A tree's blocks are scanned by one launch, its branches one after the other, where they are few; else prompts and
-    // branches get a launch each, in which the branches run side by side (32 / 8 heads, d = 128, one launch against two:
-    // 64 blocks, 8 branches, 24 us against 19; 258 blocks, 16 branches, 122 us against 57).
+    // branches get a launch each, in which the branches run side by side (32 / 8 heads, d = 128, both scans of a step,
+    // one launch against two: two trees of 27 and 29 blocks 28 us against 32; 64 blocks, 8 branches, 41 against 36).
     const bool split = branches && L.longest > kScanBlocks;
     for (int k = 0; k < (split ? 2 : 1); ++k) {
       const int part = !split ? 0 : (k == 0) != reverse ? 1 : 2;

@@ -199,6 +199,7 @@ int main() {
     }
   }
   if (g_errors) return 1;
+  check(tables > 0 && splits > 0, "both forms of the segments and of the scan were met");
   std::printf("ok, %d calls, %d tables, %d split scans\n", calls, tables, splits);
   return 0;
 }

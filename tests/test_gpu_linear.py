@@ -26,6 +26,7 @@ CASES = {
     "grouped_heads": ([(200, [70, 131]), (33, [5])], 14, 2, 128),
     "one_kv_head": ([(150, [90])], 8, 1, 64),
     "d64_blocks": ([(700, [260, 3])], 4, 4, 64),
+    "scan_groups": ([(1024, [512, 1088]), (1040, [1000])], 1, 1, 64),
     "long_blocks": ([(2100, [1500])], 64, 32, 64),
 }
 
@@ -69,7 +70,7 @@ def test_backward_from_the_forwards_workspace():
 
 
 def test_many_blocks_scan_branches_side_by_side():
-    """More blocks in a tree than one scan launch takes (64)."""
+    """More blocks in a tree than one scan launch takes (32)."""
     b = batch([(4500, [1300, 2500, 1]), (70, [300])], 1, 1, 64)
     dec = decays(1, 8.0, 8.0)
     x = inputs(b, 25)
@@ -325,14 +326,14 @@ def test_a_layer_trains_and_decodes():
 def test_a_tree_scanned_beside_a_longer_one():
     """The longer tree has its branches scanned by a launch of their own, and the short one with it; alone the short
     one's take one launch with its prompt."""
-    t1, t2 = (1500, [300, 20]), (200, [70, 333])
+    t1, t2 = (2500, [300, 20]), (200, [70, 333])
     both, alone = batch([t1, t2], 2, 1, 128), batch([t2], 2, 1, 128)
     dec = decays(1)
     x = inputs(both, 29)
-    y = {n: t[(1500 if n.endswith("p") else 320):].contiguous() for n, t in x.items()}
+    y = {n: t[(2500 if n.endswith("p") else 320):].contiguous() for n, t in x.items()}
     a, c = run(both, dec, x), run(alone, dec, y)
     for n in a:
-        at = (1 if n.endswith("p") else 2) if n.startswith("state") else 1500 if n.endswith("p") else 320
+        at = (1 if n.endswith("p") else 2) if n.startswith("state") else 2500 if n.endswith("p") else 320
         assert torch.equal(a[n][at:], c[n]), n
 
 
