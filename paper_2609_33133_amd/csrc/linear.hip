@@ -772,7 +772,7 @@ __global__ __launch_bounds__(2 * D, 2) void lin_dq_kernel(LinGradParams p) {
 // wavefronts read it by rows and dk's by columns. The two kinds share SIMDs: one is
 // busy with matrix products where the other waits for LDS or converts. (Workgroups
 // of their own for dk and dv, two a CU, each with a state and P: 1160 us for forward
-// and backward of those 49152 rows where this takes 1065.)
+// and backward of those 49152 rows where this took 1065.)
 template <int D>
 struct DkvShared {
   __attribute__((aligned(1024))) __bf16 kt[C * D];
