@@ -899,8 +899,8 @@ __device__ __forceinline__ void lin_dkv(DkvShared<D>& sh, const LinGradParams& p
 
   put_q();
   f32x16 acc[2];  // out^T [column, row]
-  // Two barriers a head, as in lin_out: behind the first its tiles and S are in LDS, behind the second P is, and tiles and
-  // S have been read.
+  // Two barriers a head, the same for both kinds of wavefronts: behind the first its tiles and S are in LDS, behind the
+  // second P is, and tiles and S have been read.
   int row_n = -1;
   for (int ci = 0; ci < chunks; ++ci) {
     const int c = chunks - 1 - ci, n = rows_of(c);
