@@ -41,14 +41,19 @@ def _need(t: torch.Tensor, name: str, dtype, shape):
         raise ValueError(f"{name} must be a device tensor")
 
 
+def _offsets(cu) -> np.ndarray:
+    """A batch's own copy: a caller may refill its arrays for the next batch before the backward of this one reads them."""
+    a = np.array(cu, dtype=np.int32, order="C")
+    a.flags.writeable = False
+    return a
+
+
 class GroupBatch:
-    """A batch of replay trees (struct augtree_groups) with its host offsets."""
+    """A batch of replay trees (struct augtree_groups) with its host offsets, which are copied and stay as they are."""
 
     def __init__(self, cu_prompt, cu_branch, cu_resp, num_q_heads: int, num_kv_heads: int, head_dim: int,
                  softmax_scale: Optional[float] = None):
-        self.cu_prompt = np.ascontiguousarray(cu_prompt, dtype=np.int32)
-        self.cu_branch = np.ascontiguousarray(cu_branch, dtype=np.int32)
-        self.cu_resp = np.ascontiguousarray(cu_resp, dtype=np.int32)
+        self.cu_prompt, self.cu_branch, self.cu_resp = _offsets(cu_prompt), _offsets(cu_branch), _offsets(cu_resp)
         self.num_groups = len(self.cu_prompt) - 1
         self.num_branches = len(self.cu_resp) - 1
         self.hq, self.hkv, self.d = int(num_q_heads), int(num_kv_heads), int(head_dim)
