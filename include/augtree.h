@@ -377,9 +377,11 @@ int augtree_prompt_grad_reduce(int32_t n_tensors, int64_t rows, int32_t heads, i
  *
  * decay: HOST array [num_kv_heads], 0 < decay <= 1, at most 256 KV heads. It is a
  * constant of the layer: no gradient is formed for it.
- * The rows of a chunk (64 rows) of a sequence pass through common matrix
- * products, so a NaN or infinity in one row may reach earlier rows of its
- * chunk too; it never reaches another tree, or from a branch any other branch.
+ * A NaN or infinity in one row reaches the rows that the formulas name, an
+ * infinity perhaps as NaN (operands are split into two terms). The rows of a
+ * chunk (64 rows) of a sequence pass through common matrix products, so it may
+ * reach the other rows of its chunk too; never another KV head or another tree,
+ * nor from a branch any other branch.
  * Every call enqueues kernels only and may be captured into a graph; calls that
  * share a workspace must not overlap (as for all entry points). Outputs must lie
  * apart from the inputs and from one another, but for what is named below.
