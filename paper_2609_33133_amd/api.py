@@ -14,6 +14,7 @@ from typing import Optional, Sequence
 
 import numpy as np
 import torch
+from torch.autograd import forward_ad
 
 from . import _lib
 from ._lib import (REPLAY_FUSED, REPLAY_SPLIT, REPLAY_AUTO, OP_PREFILL_FWD, OP_REPLAY_FWD,  # noqa: F401
@@ -349,6 +350,13 @@ def _want(t: torch.Tensor, name: str, dtype, shape):
         _need(t, name, dtype, shape)
 
 
+def _tangent(tensors) -> bool:
+    """Whether one of them is a dual tensor: forward-mode derivatives are taken of nothing here. (Outside a dual level,
+    where the ops are called, that is one comparison.)"""
+    return (getattr(forward_ad, "_current_level", 0) >= 0
+            and any(t is not None and forward_ad.unpack_dual(t).tangent is not None for t in tensors))
+
+
 def _decay(decay, heads: int) -> np.ndarray:
     """Host array [heads] of fp32 decays (a sequence, a numpy array or a CPU tensor; one number for all heads)."""
     if type(decay) is np.ndarray and decay.dtype == np.float32 and decay.shape == (heads,) and decay.flags.c_contiguous:
@@ -356,7 +364,7 @@ def _decay(decay, heads: int) -> np.ndarray:
     if isinstance(decay, torch.Tensor):
         if decay.device.type != "cpu":
             raise ValueError("decay must be on the host")
-        if decay.requires_grad:
+        if decay.requires_grad or _tangent((decay,)):
             raise ValueError("decay is a constant of the layer: no gradient is formed for it")
         decay = decay.numpy()
     a = np.asarray(decay, dtype=np.float32)

@@ -77,8 +77,9 @@ def group_attention(q_p: torch.Tensor, k_p: torch.Tensor, v_p: torch.Tensor, q_r
 
 
 def _trains(tensors) -> bool:
-    """Whether a gradient may be asked for: otherwise autograd is left out, and its time."""
-    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
+    """Whether a derivative may be asked for: otherwise autograd is left out, and its time. (A tangent counts, which the
+    Functions refuse: it would get lost.)"""
+    return (torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)) or api._tangent(tensors)
 
 
 class _GroupLinearAttention(torch.autograd.Function):
@@ -120,7 +121,7 @@ def group_linear_attention(q_p: torch.Tensor, k_p: torch.Tensor, v_p: torch.Tens
         raise ValueError("state is a constant of the op: no gradient is formed for it")
     decay = api._decay(decay, batch.hkv)
     x = (q_p, k_p, v_p, q_r, k_r, v_r)
-    if not _trains(x):
+    if not _trains(x + (state,)):
         out = api.linear_fwd(batch, decay, *(t.contiguous() for t in x), state=state, want_states=return_state)
         return out if return_state else out[:2]
     return _GroupLinearAttention.apply(*x, batch, decay.copy(), state, bool(return_state))
