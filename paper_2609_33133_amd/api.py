@@ -478,8 +478,14 @@ def linear_step(q, k, v, decay, state, src=None, state_out=None, o=None, scale: 
     """One token of linear attention for every row (augtree_linear_step): q [rows, Hq, d], k, v [rows, Hkv, d] bf16,
     state [n, Hkv, d, d] fp32. `src` [rows] int32 on the GPU names the state each row goes on from (the branches of a
     prompt share one; outside [0, n): from zero). Writes the new states to `state_out` (a new tensor if None; `state`
-    itself only without src) and returns (o, state_out)."""
+    itself only without src) and returns (o, state_out). Decode only: tensors that ask for a gradient are refused while
+    gradients are enabled."""
     on = _On((("q", q), ("k", k), ("v", v), ("state", state), ("src", src), ("state_out", state_out), ("o", o)), stream)
+    floats = (q, k, v, state, state_out, o)
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in floats):
+        raise ValueError("linear_step forms no gradient: call it under torch.no_grad(), or with detached tensors")
+    if _tangent(floats):
+        raise ValueError("linear_step takes no dual tensors: a tangent would get lost")
     if q.dim() != 3 or k.dim() != 3 or state.dim() != 4:
         raise ValueError("q and k must be [rows, heads, head_dim], state [n, heads, head_dim, head_dim]")
     rows, hq, d = q.shape

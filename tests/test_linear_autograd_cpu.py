@@ -56,3 +56,51 @@ def test_a_decay_has_no_forward_derivative(stand_ins):
     b, x = GroupBatch(*CU, 4, 2, 64), leaves()
     with forward_ad.dual_level(), pytest.raises(ValueError, match="constant"):
         autograd.group_linear_attention(*x, b, dual(torch.tensor([0.9, 0.9])))
+
+
+class Reached(Exception):
+    """A call went past the checks of its arguments."""
+
+
+class FakeOn:
+    """api._On for host tensors: the library is not reached."""
+
+    def __init__(self, tensors, stream=None):
+        pass
+
+    def __enter__(self):
+        raise Reached
+
+    def __exit__(self, *exc):
+        pass
+
+
+def step_args():
+    z = lambda *s: torch.zeros(3, *s, 64, dtype=torch.bfloat16)
+    return dict(q=z(4), k=z(2), v=z(2), state=torch.zeros(3, 2, 64, 64), state_out=torch.zeros(3, 2, 64, 64), o=z(4))
+
+
+def step(a):
+    return api.linear_step(a["q"], a["k"], a["v"], 0.9, a["state"], state_out=a["state_out"], o=a["o"])
+
+
+@pytest.mark.parametrize("name", ["q", "k", "v", "state", "state_out", "o"])
+def test_a_step_forms_no_gradient_and_says_so(monkeypatch, name):
+    monkeypatch.setattr(api, "_On", FakeOn)
+    monkeypatch.setattr(api, "_need", lambda *a: None)  # (it asks for device tensors)
+    a = step_args()
+    with pytest.raises(Reached):
+        step(a)
+    a[name].requires_grad_(True)
+    with pytest.raises(ValueError, match="no_grad"):
+        step(a)
+    with torch.no_grad(), pytest.raises(Reached):
+        step(a)
+    with torch.inference_mode(), pytest.raises(Reached):
+        step(a)
+    for grad in (True, False):
+        a = step_args()
+        with forward_ad.dual_level(), torch.set_grad_enabled(grad):
+            a[name] = dual(a[name])
+            with pytest.raises(ValueError, match="tangent"):
+                step(a)
