@@ -381,6 +381,14 @@ def _out(t, name, dtype, shape, device):
     return t
 
 
+def _written(given):
+    """Counts a call's writes to the caller's own tensors as torch's in-place operations count theirs, so that a backward
+    which saved one of them notices."""
+    given = [t for t in given if t is not None]
+    if given:
+        torch.autograd.graph.increment_version(given)
+
+
 def _check_batch(b: GroupBatch):
     """The offsets' counts, which the library takes from the batch's struct."""
     if b.num_branches and len(b.cu_branch) != b.num_groups + 1:
@@ -426,7 +434,7 @@ def linear_fwd(b: GroupBatch, decay, q_p, k_p, v_p, q_r, k_r, v_r, state=None, o
     on = _On(named + (("state", state), ("o_p", o_p), ("o_r", o_r), ("state_p", state_p), ("state_r", state_r),
                       ("ws", ws)), stream)
     _linear_inputs(b, named)
-    dev, f32 = on.device, torch.float32
+    dev, f32, given = on.device, torch.float32, (o_p, o_r, state_p, state_r, ws)
     if state is not None:
         _want(state, "state", f32, (b.num_groups, b.hkv, b.d, b.d))
     with on as st:
@@ -441,6 +449,7 @@ def linear_fwd(b: GroupBatch, decay, q_p, k_p, v_p, q_r, k_r, v_r, state=None, o
             b.ref, dec.ctypes.data, _addr(q_p), _addr(k_p), _addr(v_p), _addr(q_r), _addr(k_r), _addr(v_r), _addr(state),
             _addr(o_p), _addr(o_r), _addr(state_p), _addr(state_r) if b.num_branches else None, _addr(ws), ws.numel(),
             st), "linear_fwd")
+    _written(given)
     return o_p, o_r, state_p, state_r
 
 
@@ -454,7 +463,7 @@ def linear_bwd(b: GroupBatch, decay, q_p, k_p, v_p, do_p, q_r, k_r, v_r, do_r, s
     on = _On(named + (("state", state), ("dq_p", dq_p), ("dk_p", dk_p), ("dv_p", dv_p), ("dq_r", dq_r),
                       ("dk_r", dk_r), ("dv_r", dv_r), ("fwd_ws", fwd_ws), ("ws", ws)), stream)
     _linear_inputs(b, named)
-    dev = on.device
+    dev, given = on.device, (dq_p, dk_p, dv_p, dq_r, dk_r, dv_r, ws)
     _want_ws(fwd_ws, "fwd_ws")
     if state is not None:
         _want(state, "state", torch.float32, (b.num_groups, b.hkv, b.d, b.d))
@@ -464,6 +473,7 @@ def linear_bwd(b: GroupBatch, decay, q_p, k_p, v_p, do_p, q_r, k_r, v_r, do_r, s
                                    (dq_r, "dq_r", q_r), (dk_r, "dk_r", k_r), (dv_r, "dv_r", v_r))]
         _linear_bwd(b, dec, (q_p, k_p, v_p, do_p, q_r, k_r, v_r, do_r, state, *outs), fwd_ws,
                     _linear_ws(b, True, ws, dev), st)
+    _written(given)
     return tuple(outs)
 
 
@@ -496,7 +506,7 @@ def linear_step(q, k, v, decay, state, src=None, state_out=None, o=None, scale: 
     _want(state, "state", torch.float32, (n, hkv, d, d))
     if src is not None:
         _want(src, "src", torch.int32, (rows,))
-    dec = _decay(decay, hkv)
+    dec, given = _decay(decay, hkv), (state_out, o)
     with on as st:
         state_out = _out(state_out, "state_out", torch.float32, (rows, hkv, d, d), on.device)
         o = _out(o, "o", torch.bfloat16, q.shape, on.device)
@@ -504,6 +514,7 @@ def linear_step(q, k, v, decay, state, src=None, state_out=None, o=None, scale: 
             rows, hq, hkv, d, 1.0 / math.sqrt(d) if scale is None else float(scale),
             dec.ctypes.data, _addr(q), _addr(k), _addr(v), n, _addr(state), _addr(src),
             _addr(state_out), _addr(o), st), "linear_step")
+    _written(given)
     return o, state_out
 
 
@@ -524,10 +535,12 @@ def head_norm_fwd(x, weight=None, bias=None, gate=None, activation: int = ACT_NO
     on = _On((("x", x), ("weight", weight), ("bias", bias), ("gate", gate), ("y", y)), stream)
     _norm_inputs(x, gate, weight, bias)
     rows, heads, d = x.shape
+    given = (y,)
     with on as st:
         y = _out(y, "y", torch.bfloat16, x.shape, on.device)
         _lib.check(_lib.load().augtree_head_norm_fwd(rows, heads, d, int(activation), float(eps), _addr(x), _addr(gate),
                                                      _addr(weight), _addr(bias), _addr(y), st), "head_norm_fwd")
+    _written(given)
     return y
 
 
@@ -541,7 +554,7 @@ def head_norm_bwd(x, dy, weight=None, bias=None, gate=None, activation: int = AC
     _norm_inputs(x, gate, weight, bias)
     _want(dy, "dy", torch.bfloat16, x.shape)
     rows, heads, d = x.shape
-    dev, f32 = on.device, torch.float32
+    dev, f32, given = on.device, torch.float32, (dx, dgate, dweight, dbias, ws)
     with on as st:
         dx = _out(dx, "dx", torch.bfloat16, x.shape, dev)
         if gate is not None:
@@ -552,6 +565,7 @@ def head_norm_bwd(x, dy, weight=None, bias=None, gate=None, activation: int = AC
             dbias = _out(dbias, "dbias", f32, (heads, d), dev)
         _want_ws(ws, "ws")
         _head_norm_bwd(x, dy, weight, bias, gate, int(activation), float(eps), dx, dgate, dweight, dbias, ws, st)
+    _written(given)
     return dx, dgate, dweight, dbias
 
 

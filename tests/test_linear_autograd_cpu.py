@@ -104,3 +104,70 @@ def test_a_step_forms_no_gradient_and_says_so(monkeypatch, name):
             a[name] = dual(a[name])
             with pytest.raises(ValueError, match="tangent"):
                 step(a)
+
+
+@pytest.fixture
+def library(monkeypatch):
+    """Calls that pass the checks of their arguments and write nothing."""
+    class On:
+        def __init__(self, tensors, stream=None):
+            self.device = torch.device("cpu")
+
+        def __enter__(self):
+            return 0
+
+        def __exit__(self, *exc):
+            pass
+
+    class Lib:
+        def __getattr__(self, name):
+            return lambda *a: 1024 if name.endswith("workspace_size") else 0
+    monkeypatch.setattr(api, "_On", On)
+    monkeypatch.setattr(api._lib, "load", lambda: Lib())
+
+
+def written(call, given, *unwritten):
+    """Every tensor in `given` counts as written by the call, none of the others does."""
+    for t in given.values():
+        assert t._version == 0
+    before = [t._version for t in unwritten]
+    call(**given)
+    assert not [n for n, t in given.items() if t._version == 0]
+    assert [t._version for t in unwritten] == before
+
+
+def test_what_a_call_writes_counts_as_written(library):
+    """A tensor that another op has saved for its backward is not replaced unnoticed."""
+    b, x = GroupBatch(*CU, 4, 2, 64), leaves()
+    do = [x[0].clone(), x[3].clone()]
+    like = lambda *names: {n: x[{"q": 0, "k": 1, "v": 2, "o": 0}[n.lstrip("d")[0]] + 3 * n.endswith("_r")].clone() for n in names}
+    ws = lambda: torch.zeros(1024, dtype=torch.uint8)
+    states = dict(state_p=torch.zeros(2, 2, 64, 64), state_r=torch.zeros(3, 2, 64, 64))
+    written(lambda **k: api.linear_fwd(b, 0.9, *x, **k), dict(like("o_p", "o_r"), ws=ws(), **states), *x)
+    kept = ws()
+    written(lambda **k: api.linear_bwd(b, 0.9, *x[:3], do[0], *x[3:], do[1], fwd_ws=kept, **k),
+            dict(like("dq_p", "dk_p", "dv_p", "dq_r", "dk_r", "dv_r"), ws=ws()), *x, *do, kept)
+    a = step_args()
+    written(lambda **k: api.linear_step(a["q"], a["k"], a["v"], 0.9, a["state"], **k),
+            {n: a[n] for n in ("state_out", "o")}, a["q"], a["k"], a["v"], a["state"])
+    w = lambda: torch.zeros(4, 64)
+    written(lambda **k: api.head_norm_fwd(x[0], **k), {"y": x[0].clone()}, x[0])
+    written(lambda **k: api.head_norm_bwd(x[0], do[0], w(), w(), x[0].clone(), **k),
+            {"dx": x[0].clone(), "dgate": x[0].clone(), "dweight": w(), "dbias": w(), "ws": ws()}, x[0], do[0])
+
+
+def test_a_state_saved_for_a_backward_is_not_updated_in_place_unnoticed(library):
+    a = step_args()
+    weight = torch.ones(1, requires_grad=True)
+    loss = (a["state"] * weight).sum()  # saves the state
+    with torch.no_grad():
+        api.linear_step(a["q"], a["k"], a["v"], 0.9, a["state"], state_out=a["state"])
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
+
+
+def test_what_a_refused_call_would_have_written_does_not(library):
+    a = step_args()
+    with pytest.raises((ValueError, TypeError)):
+        api.linear_step(a["q"], a["k"], a["v"].float(), 0.9, a["state"], state_out=a["state_out"])
+    assert a["state_out"]._version == 0
