@@ -364,9 +364,9 @@ def _decay(decay, heads: int) -> np.ndarray:
     if isinstance(decay, torch.Tensor):
         if decay.device.type != "cpu":
             raise ValueError("decay must be on the host")
-        if decay.requires_grad or _tangent((decay,)):
+        if (decay.requires_grad and torch.is_grad_enabled()) or _tangent((decay,)):
             raise ValueError("decay is a constant of the layer: no gradient is formed for it")
-        decay = decay.numpy()
+        decay = decay.detach().numpy()
     a = np.asarray(decay, dtype=np.float32)
     a = np.ascontiguousarray(np.broadcast_to(a, (heads,)) if a.ndim == 0 else a)
     if a.shape != (heads,):

@@ -116,8 +116,8 @@ def group_linear_attention(q_p: torch.Tensor, k_p: torch.Tensor, v_p: torch.Tens
     """(O_P, O_R) of linear attention over replay trees with a decay per KV head (host values in (0, 1]);
     differentiable in the six tensors. `state` [num_groups, Hkv, d, d] fp32 is what the prompts begin from; with
     `return_state` the states after every prompt and every branch follow the outputs (no gradient flows through
-    either)."""
-    if state is not None and state.requires_grad:
+    either: a state, or a decay tensor, that asks for one is refused while gradients are enabled)."""
+    if state is not None and state.requires_grad and torch.is_grad_enabled():
         raise ValueError("state is a constant of the op: no gradient is formed for it")
     decay = api._decay(decay, batch.hkv)
     x = (q_p, k_p, v_p, q_r, k_r, v_r)

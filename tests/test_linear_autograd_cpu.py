@@ -171,3 +171,18 @@ def test_what_a_refused_call_would_have_written_does_not(library):
     with pytest.raises((ValueError, TypeError)):
         api.linear_step(a["q"], a["k"], a["v"].float(), 0.9, a["state"], state_out=a["state_out"])
     assert a["state_out"]._version == 0
+
+
+def test_a_learned_state_and_decay_serve_inference(stand_ins):
+    """Refused where a gradient could be asked for, constants as any other where it cannot."""
+    b, x = GroupBatch(*CU, 4, 2, 64), leaves()
+    state = torch.nn.Parameter(torch.zeros(2, 2, 64, 64))
+    decay = torch.nn.Parameter(torch.tensor([0.9, 0.8]))
+    for kw in (dict(decay=0.9, state=state), dict(decay=decay)):
+        with pytest.raises(ValueError, match="constant"):
+            autograd.group_linear_attention(*x, b, **kw)
+    for off in (torch.no_grad, torch.inference_mode):
+        with off():
+            o_p, o_r = autograd.group_linear_attention(*x, b, decay, state=state)
+            assert o_p.shape == x[0].shape and o_r.shape == x[3].shape
+            assert api._decay(decay, 2).tolist() == [np.float32(0.9), np.float32(0.8)]
