@@ -414,7 +414,8 @@ int augtree_linear_fwd(const augtree_groups* grp, const float* decay, const uint
  * the outputs are not read. Out: dq like q, dk, dv like k, bf16.
  * fwd_ws (nullable): the workspace of the augtree_linear_fwd call of the same
  * batch, decay, k, v and state, not written since. The states it holds are then
- * used instead of being formed again; the results are the same bits.
+ * used instead of being formed again, and `state` is not read; the results are
+ * the same bits.
  */
 int augtree_linear_bwd(const augtree_groups* grp, const float* decay, const uint16_t* q_p,
                        const uint16_t* k_p, const uint16_t* v_p, const uint16_t* do_p, const uint16_t* q_r,

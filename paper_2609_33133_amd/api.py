@@ -456,7 +456,8 @@ def linear_fwd(b: GroupBatch, decay, q_p, k_p, v_p, q_r, k_r, v_r, state=None, o
 def linear_bwd(b: GroupBatch, decay, q_p, k_p, v_p, do_p, q_r, k_r, v_r, do_r, state=None, dq_p=None, dk_p=None,
                dv_p=None, dq_r=None, dk_r=None, dv_r=None, fwd_ws=None, ws=None, stream=None):
     """Gradients of linear_fwd's outputs (augtree_linear_bwd). `fwd_ws`: the workspace that linear_fwd was given for the
-    same inputs, not written since (saves forming its states again). Returns (dq_p, dk_p, dv_p, dq_r, dk_r, dv_r)."""
+    same inputs, not written since (saves forming its states again; `state` is not read then). Returns
+    (dq_p, dk_p, dv_p, dq_r, dk_r, dv_r)."""
     dec = _decay(decay, b.hkv)
     named = (("q_p", q_p), ("k_p", k_p), ("v_p", v_p), ("do_p", do_p), ("q_r", q_r), ("k_r", k_r), ("v_r", v_r),
              ("do_r", do_r))

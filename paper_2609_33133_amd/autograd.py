@@ -89,7 +89,7 @@ class _GroupLinearAttention(torch.autograd.Function):
         x = [t.contiguous() for t in (q_p, k_p, v_p, q_r, k_r, v_r)]
         ws = torch.empty(api.linear_workspace_size(b), dtype=torch.uint8, device=q_p.device)
         o_p, o_r, state_p, state_r = api.linear_fwd(b, decay, *x, state=state, want_states=return_state, ws=ws)
-        ctx.save_for_backward(*x, state, ws)  # the states in ws serve the backward too
+        ctx.save_for_backward(*x, ws)  # the backward takes its states from ws: the caller may go on with `state`
         ctx.batch, ctx.decay, ctx.ws_bytes = b, decay, api.linear_workspace_size(b, True)
         if not return_state:
             return o_p, o_r
@@ -99,13 +99,13 @@ class _GroupLinearAttention(torch.autograd.Function):
     @staticmethod
     @once_differentiable
     def backward(ctx, do_p, do_r, *_):
-        q_p, k_p, v_p, q_r, k_r, v_r, state, ws = ctx.saved_tensors
+        q_p, k_p, v_p, q_r, k_r, v_r, ws = ctx.saved_tensors
         # the forward has checked what it saved, autograd the gradients' shapes and device (zeros for an unused output)
         do_p, do_r = do_p.to(torch.bfloat16).contiguous(), do_r.to(torch.bfloat16).contiguous()
         with api._On((("q_p", q_p),)) as stream:
             grads = [torch.empty_like(t) for t in (q_p, k_p, v_p, q_r, k_r, v_r)]
             bwd_ws = torch.empty(ctx.ws_bytes, dtype=torch.uint8, device=q_p.device)
-            api._linear_bwd(ctx.batch, ctx.decay, (q_p, k_p, v_p, do_p, q_r, k_r, v_r, do_r, state, *grads), ws, bwd_ws,
+            api._linear_bwd(ctx.batch, ctx.decay, (q_p, k_p, v_p, do_p, q_r, k_r, v_r, do_r, None, *grads), ws, bwd_ws,
                             stream)
         return (*grads, None, None, None, None)
 

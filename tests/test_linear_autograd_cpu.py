@@ -186,3 +186,35 @@ def test_a_learned_state_and_decay_serve_inference(stand_ins):
             o_p, o_r = autograd.group_linear_attention(*x, b, decay, state=state)
             assert o_p.shape == x[0].shape and o_r.shape == x[3].shape
             assert api._decay(decay, 2).tolist() == [np.float32(0.9), np.float32(0.8)]
+
+
+def train(monkeypatch, state, return_state=False):
+    """A step of group_linear_attention on stand-ins; what _linear_bwd was handed is kept."""
+    b, x = GroupBatch(*CU, 4, 2, 64), [t.requires_grad_(True) for t in leaves()]
+    states = (torch.zeros(2, 2, 64, 64), torch.zeros(3, 2, 64, 64)) if return_state else (None, None)
+    handed = []
+
+    class On:
+        def __init__(self, tensors, stream=None):
+            pass
+
+        def __enter__(self):
+            return 0
+
+        def __exit__(self, *exc):
+            pass
+    monkeypatch.setattr(api, "linear_fwd", lambda b, dec, q_p, k_p, v_p, q_r, *a, **k:
+                        (q_p.detach().clone(), q_r.detach().clone(), *states))
+    monkeypatch.setattr(api, "_On", On)
+    monkeypatch.setattr(api, "_linear_bwd", lambda *a: handed.append(a))
+    return x, autograd.group_linear_attention(*x, b, 0.9, state=state, return_state=return_state), handed
+
+
+def test_a_state_may_be_updated_between_forward_and_backward(monkeypatch):
+    """The backward reads the states that the forward left in its workspace, not the one it began from."""
+    state = torch.zeros(2, 2, 64, 64)
+    x, (o_p, o_r), handed = train(monkeypatch, state)
+    state.add_(1)
+    torch.autograd.grad((o_p, o_r), x, (torch.zeros_like(o_p), torch.zeros_like(o_r)))
+    (_, _, tensors, fwd_ws, _, _), = handed
+    assert tensors[8] is None and fwd_ws is not None
