@@ -91,6 +91,7 @@ class _GroupLinearAttention(torch.autograd.Function):
         o_p, o_r, state_p, state_r = api.linear_fwd(b, decay, *x, state=state, want_states=return_state, ws=ws)
         ctx.save_for_backward(*x, ws)  # the backward takes its states from ws: the caller may go on with `state`
         ctx.batch, ctx.decay, ctx.ws_bytes = b, decay, api.linear_workspace_size(b, True)
+        ctx.set_materialize_grads(False)  # no zeros for the states' gradients, which nobody reads
         if not return_state:
             return o_p, o_r
         ctx.mark_non_differentiable(state_p, state_r)
@@ -100,8 +101,9 @@ class _GroupLinearAttention(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, do_p, do_r, *_):
         q_p, k_p, v_p, q_r, k_r, v_r, ws = ctx.saved_tensors
-        # the forward has checked what it saved, autograd the gradients' shapes and device (zeros for an unused output)
-        do_p, do_r = do_p.to(torch.bfloat16).contiguous(), do_r.to(torch.bfloat16).contiguous()
+        # the forward has checked what it saved, autograd the gradients' shapes and device (None for an unused output)
+        do_p, do_r = (torch.zeros_like(q) if g is None else g.to(torch.bfloat16).contiguous()
+                      for g, q in ((do_p, q_p), (do_r, q_r)))
         with api._On((("q_p", q_p),)) as stream:
             grads = [torch.empty_like(t) for t in (q_p, k_p, v_p, q_r, k_r, v_r)]
             bwd_ws = torch.empty(ctx.ws_bytes, dtype=torch.uint8, device=q_p.device)

@@ -3,6 +3,7 @@ import numpy as np
 import pytest
 import torch
 from torch.autograd import forward_ad
+from torch.utils._python_dispatch import TorchDispatchMode
 
 from paper_2609_33133_amd import api, autograd
 from paper_2609_33133_amd.api import GroupBatch
@@ -218,3 +219,24 @@ def test_a_state_may_be_updated_between_forward_and_backward(monkeypatch):
     torch.autograd.grad((o_p, o_r), x, (torch.zeros_like(o_p), torch.zeros_like(o_r)))
     (_, _, tensors, fwd_ws, _, _), = handed
     assert tensors[8] is None and fwd_ws is not None
+
+
+def test_states_returned_in_training_get_no_gradients_made_of_zeros(monkeypatch):
+    """A state is [d, d] per head, tree and branch in fp32: nothing of that size is filled with zeros for the backward. An
+    output outside the loss still has a gradient of zeros."""
+    x, (o_p, o_r, state_p, state_r), handed = train(monkeypatch, None, return_state=True)
+    assert not state_p.requires_grad and not state_r.requires_grad
+    made = []
+
+    class Sizes(TorchDispatchMode):
+        def __torch_dispatch__(self, func, types, args=(), kwargs=None):
+            r = func(*args, **(kwargs or {}))
+            if isinstance(r, torch.Tensor):
+                made.append(r.shape)
+            return r
+    with Sizes(), torch.autograd.set_multithreading_enabled(False):
+        torch.autograd.grad(o_r, x, torch.ones_like(o_r))
+    assert made and not [s for s in made if len(s) == 4]
+    (_, _, tensors, _, _, _), = handed
+    do_p, do_r = tensors[3], tensors[7]
+    assert do_p.shape == o_p.shape and not do_p.any() and do_p.dtype == torch.bfloat16 and (do_r == 1).all()
