@@ -388,8 +388,9 @@ int augtree_prompt_grad_reduce(int32_t n_tensors, int64_t rows, int32_t heads, i
  * Results are bitwise reproducible and a tree's do not depend on the batch.
  * ------------------------------------------------------------------------- */
 
-/* Bytes of workspace of augtree_linear_fwd (backward = 0) or
- * augtree_linear_bwd (backward != 0). 0 on invalid arguments. */
+/* Bytes of workspace of augtree_linear_fwd (backward = 0), of augtree_linear_bwd
+ * (1) and of an augtree_linear_bwd that is given fwd_ws (2: about half of that).
+ * 0 on invalid arguments. */
 size_t augtree_linear_workspace_size(const augtree_groups* grp, int backward);
 
 /*

@@ -395,10 +395,11 @@ def _check_batch(b: GroupBatch):
         raise ValueError(f"cu_branch: {len(b.cu_branch)} offsets for {b.num_groups} prompts")
 
 
-def linear_workspace_size(b: GroupBatch, backward: bool = False) -> int:
+def linear_workspace_size(b: GroupBatch, backward: bool = False, from_fwd_ws: bool = False) -> int:
+    """Bytes of workspace of linear_fwd, or of linear_bwd, which needs less where it is given the forward's."""
     lib = _lib.load()
     _check_batch(b)
-    n = lib.augtree_linear_workspace_size(b.ref, int(backward))
+    n = lib.augtree_linear_workspace_size(b.ref, 0 if not backward else 2 if from_fwd_ws else 1)
     if n == 0:
         raise _lib.AugtreeError(_lib.AUGTREE_ERR_INVALID_ARGUMENT, "linear_workspace_size",
                                 lib.augtree_last_error().decode())
@@ -410,9 +411,9 @@ def _want_ws(ws, name: str):
         raise ValueError(f"{name} must be a contiguous uint8 tensor")
 
 
-def _linear_ws(b, backward, ws, device):
+def _linear_ws(b, backward, ws, device, from_fwd_ws=False):
     if ws is None:
-        ws = torch.empty(linear_workspace_size(b, backward), dtype=torch.uint8, device=device)
+        ws = torch.empty(linear_workspace_size(b, backward, from_fwd_ws), dtype=torch.uint8, device=device)
     _want_ws(ws, "ws")
     return ws
 
@@ -473,7 +474,7 @@ def linear_bwd(b: GroupBatch, decay, q_p, k_p, v_p, do_p, q_r, k_r, v_r, do_r, s
                 for t, n, like in ((dq_p, "dq_p", q_p), (dk_p, "dk_p", k_p), (dv_p, "dv_p", v_p),
                                    (dq_r, "dq_r", q_r), (dk_r, "dk_r", k_r), (dv_r, "dv_r", v_r))]
         _linear_bwd(b, dec, (q_p, k_p, v_p, do_p, q_r, k_r, v_r, do_r, state, *outs), fwd_ws,
-                    _linear_ws(b, True, ws, dev), st)
+                    _linear_ws(b, True, ws, dev, fwd_ws is not None), st)
     _written(given)
     return tuple(outs)
 

@@ -90,7 +90,7 @@ class _GroupLinearAttention(torch.autograd.Function):
         ws = torch.empty(api.linear_workspace_size(b), dtype=torch.uint8, device=q_p.device)
         o_p, o_r, state_p, state_r = api.linear_fwd(b, decay, *x, state=state, want_states=return_state, ws=ws)
         ctx.save_for_backward(*x, ws)  # the backward takes its states from ws: the caller may go on with `state`
-        ctx.batch, ctx.decay, ctx.ws_bytes = b, decay, api.linear_workspace_size(b, True)
+        ctx.batch, ctx.decay, ctx.ws_bytes = b, decay, api.linear_workspace_size(b, True, from_fwd_ws=True)
         ctx.set_materialize_grads(False)  # no zeros for the states' gradients, which nobody reads
         if not return_state:
             return o_p, o_r

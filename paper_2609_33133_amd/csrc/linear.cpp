@@ -187,9 +187,14 @@ int make_layout(const augtree_groups* g, Layout* L) {
   return AUGTREE_OK;
 }
 
-size_t workspace_bytes(const augtree_groups* g, const Layout& L, bool backward) {
-  size_t n = align_up(L.segs.size() * sizeof(LinSeg)) + L.states + align_up(L.tree * g->num_groups);
-  if (backward) n += L.states + align_up(L.tree * (size_t)std::max(1, g->num_branches));
+// What a workspace is for: a forward, a backward, a backward that is given the forward's workspace.
+enum Use { kForward = 0, kBackward = 1, kBackwardKept = 2 };
+Use use_of(int backward) { return backward == kBackwardKept ? kBackwardKept : backward ? kBackward : kForward; }
+
+size_t workspace_bytes(const augtree_groups* g, const Layout& L, Use use) {
+  size_t n = align_up(L.segs.size() * sizeof(LinSeg));
+  if (use != kBackwardKept) n += L.states + align_up(L.tree * g->num_groups);
+  if (use != kForward) n += L.states + align_up(L.tree * (size_t)std::max(1, g->num_branches));
   return n;
 }
 
@@ -346,7 +351,7 @@ size_t augtree_linear_workspace_size(const augtree_groups* grp, int backward) {
     if (int st = check_batch(grp, ones.data())) return st;
     Layout L;
     if (int st = make_layout(grp, &L)) return st;
-    n = workspace_bytes(grp, L, backward != 0);
+    n = workspace_bytes(grp, L, use_of(backward));
     return fail_status(AUGTREE_OK, "");
   });
   return n;
@@ -374,7 +379,7 @@ int augtree_linear_fwd(const augtree_groups* grp, const float* decay, const uint
     if ((st = check_apart(ins, 7, outs, 5))) return st;
     Call c;
     c.g = grp;
-    if ((st = make_layout(grp, &c.L)) || (st = check_ws(ws, ws_bytes, workspace_bytes(grp, c.L, false))) ||
+    if ((st = make_layout(grp, &c.L)) || (st = check_ws(ws, ws_bytes, workspace_bytes(grp, c.L, kForward))) ||
         (st = augtree_check_device()))
       return st;
     c.ws = static_cast<char*>(ws);
@@ -422,27 +427,28 @@ int augtree_linear_bwd(const augtree_groups* grp, const float* decay, const uint
     if ((st = check_apart(ins, 10, outs, 7))) return st;
     Call c;
     c.g = grp;
-    if ((st = make_layout(grp, &c.L)) || (st = check_ws(ws, ws_bytes, workspace_bytes(grp, c.L, true))) ||
-        (fwd_ws && (st = check_ws(fwd_ws, fwd_ws_bytes, workspace_bytes(grp, c.L, false)))))
+    if ((st = make_layout(grp, &c.L)) ||
+        (st = check_ws(ws, ws_bytes, workspace_bytes(grp, c.L, fwd_ws ? kBackwardKept : kBackward))) ||
+        (fwd_ws && (st = check_ws(fwd_ws, fwd_ws_bytes, workspace_bytes(grp, c.L, kForward)))))
       return st;
     if ((st = augtree_check_device())) return st;
     c.ws = static_cast<char*>(ws);
     c.stream = static_cast<hipStream_t>(stream);
     if ((st = c.begin(decay))) return st;
-    const float* fwd = nullptr;
-    float* const own = c.take<float>(c.L.states);
-    float* const tree = c.take<float>(c.L.tree * grp->num_groups);
-    float* const rev = c.take<float>(c.L.states);
-    float* const ends = c.take<float>(c.L.tree * std::max(1, grp->num_branches));
     const uint16_t *const q[2] = {q_p, q_r}, *const k[2] = {k_p, k_r}, *const v[2] = {v_p, v_r},
                    *const g[2] = {do_p, do_r};
     uint16_t *const dq[2] = {dq_p, dq_r}, *const dk[2] = {dk_p, dk_r}, *const dv[2] = {dv_p, dv_r};
+    const float* fwd = nullptr;
     if (fwd_ws) {
       fwd = reinterpret_cast<const float*>(static_cast<const char*>(fwd_ws) + align_up(c.L.segs.size() * sizeof(LinSeg)));
     } else {
+      float* const own = c.take<float>(c.L.states);
+      float* const tree = c.take<float>(c.L.tree * grp->num_groups);
       fwd = own;
       if ((st = c.states(false, k, v, state, own, tree, nullptr, nullptr))) return st;
     }
+    float* const rev = c.take<float>(c.L.states);
+    float* const ends = c.take<float>(c.L.tree * std::max(1, grp->num_branches));
     if ((st = c.states(true, q, g, nullptr, rev, ends, nullptr, nullptr))) return st;
     LinGradParams p;
     std::memset(&p, 0, sizeof(p));
