@@ -478,9 +478,9 @@ size_t augtree_head_norm_workspace_size(int64_t rows, int32_t heads, int32_t hea
  * "lse_merge", "dq_prefill", "dkv_prefill", "dq_replay", "dkv_replay", "dq_tree",
  * "dkv_tree", "grad_reduce", "reduce_tree", "linear_table", "linear_state",
  * "linear_state_rev", "linear_scan", "linear_scan_rev", "linear_out", "linear_dq",
- * "linear_dkv", "linear_step", "head_norm", "head_norm_bwd") and the stream the kernel is
- * enqueued on, so that a caller can record HIP events around single
- * kernels. The hook must not call back into the library. NULL removes it.
+ * "linear_dkv", "linear_step", "head_norm", "head_norm_bwd", "head_norm_sum")
+ * and the stream the kernel is enqueued on, so that a caller can record HIP
+ * events around single kernels. The hook must not call back into the library. NULL removes it.
  * Per thread; the library keeps no other state.
  */
 typedef void (*augtree_launch_hook)(const char* role, int phase, void* stream, void* user);

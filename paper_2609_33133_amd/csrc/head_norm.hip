@@ -263,7 +263,13 @@ hipError_t launch_head_norm_fwd(const HeadNormParams& p, hipStream_t stream) {
 }
 
 hipError_t launch_head_norm_bwd(const HeadNormParams& p, hipStream_t stream) {
-  const hipError_t e = with_shape(p.d, [&](auto t, auto nc) {
+  if (p.sum) {
+    const int width = p.heads * p.d;
+    head_norm_sum_kernel<<<(2 * width + 63) / 64, 1024, 0, stream>>>(
+        p.part, head_norm_bwd_grid(p.rows, p.heads, p.d).parts, width, p.dweight, p.dbias);
+    return hipGetLastError();
+  }
+  return with_shape(p.d, [&](auto t, auto nc) {
     constexpr int T = decltype(t)::value, NC = decltype(nc)::value;
     const HeadNormGrid g = head_norm_bwd_grid(p.rows, p.heads, p.d);
     const dim3 grid(g.row_parts, g.head_blocks);
@@ -273,11 +279,6 @@ hipError_t launch_head_norm_bwd(const HeadNormParams& p, hipStream_t stream) {
     else head_norm_bwd_kernel<T, NC, false, false><<<grid, 256, 0, stream>>>(p, g.heads, g.row_parts);
     return hipGetLastError();
   });
-  if (e != hipSuccess || !p.part) return e;
-  const int width = p.heads * p.d;
-  head_norm_sum_kernel<<<(2 * width + 63) / 64, 1024, 0, stream>>>(p.part, head_norm_bwd_grid(p.rows, p.heads, p.d).parts,
-                                                                  width, p.dweight, p.dbias);
-  return hipGetLastError();
 }
 
 }  // namespace augtree

@@ -610,8 +610,15 @@ int augtree_head_norm_bwd(int64_t rows, int32_t heads, int32_t head_dim, int act
   p.silu = activation == AUGTREE_ACT_SILU;
   p.eps = eps;
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  Hook h("head_norm_bwd", s);
-  if ((st = hip_ok(launch_head_norm_bwd(p, s), "head norm backward launch"))) return st;
+  {
+    Hook h("head_norm_bwd", s);
+    if ((st = hip_ok(launch_head_norm_bwd(p, s), "head norm backward launch"))) return st;
+  }
+  if (sums) {
+    p.sum = 1;
+    Hook h("head_norm_sum", s);
+    if ((st = hip_ok(launch_head_norm_bwd(p, s), "head norm sum launch"))) return st;
+  }
   return fail_status(AUGTREE_OK, "");
 }
 

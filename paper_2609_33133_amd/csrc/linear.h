@@ -114,6 +114,7 @@ struct HeadNormParams {
   int64_t rows;
   int32_t heads, d;
   int32_t silu;
+  int32_t sum;                    // backward: 0 the rows' gradients and the parts, 1 the sum of the parts
   float eps;
 };
 // Workgroups: row_parts x head_blocks (about `want` at most) of `heads` heads. In

@@ -12,7 +12,7 @@ HOST = os.path.join(ROOT, "tests", "host")
 
 
 @pytest.mark.timeout(600)
-@pytest.mark.parametrize("name", ["linear_kept_test"])
+@pytest.mark.parametrize("name", ["linear_kept_test", "norm_hook_test"])
 def test_host_logic_under_sanitizers(tmp_path, name):
     gxx = shutil.which("g++")
     if gxx is None or not os.path.isdir(HOST):
