@@ -449,6 +449,7 @@ typedef enum augtree_activation { AUGTREE_ACT_NONE = 0, AUGTREE_ACT_SILU = 1 } a
  * attention: n = (x - mean) / sqrt(var + eps) over the head_dim channels (var
  * with the divisor head_dim), a = n * weight + bias, and
  *   y = act(a),  or with a gate  y = a * act(gate);  act(u) = u / (1 + exp(-u)) (SILU) or u (NONE).
+ * Arithmetic is fp32: squares of values from 2^63 on overflow.
  * In:  x, gate (nullable) [rows,heads,head_dim] bf16; weight, bias (each
  *      nullable: 1 and 0) [heads,head_dim] fp32. head_dim a multiple of 8, at most 1024.
  * Out: y like x (it may be x or gate itself; other overlaps are refused). rows = 0 is a no-op.

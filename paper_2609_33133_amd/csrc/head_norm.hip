@@ -97,7 +97,10 @@ __device__ __forceinline__ float normalise(float* x, int l, int pieces, float in
       sq += x[i] * x[i];
     }
   }
-  const float rstd = __builtin_amdgcn_rsqf(lane_sum<T>(sq) * inv_d + eps);  // 1 ulp
+  // 1 ulp; the instruction takes denormals for zero (both may be one), hence the power of two
+  const float var = lane_sum<T>(sq) * inv_d + eps;
+  const bool tiny = var < 0x1p-126f;
+  const float rstd = __builtin_amdgcn_rsqf(tiny ? var * 0x1p64f : var) * (tiny ? 0x1p32f : 1.f);
 #pragma unroll
   for (int i = 0; i < 8 * NC; ++i) x[i] *= rstd;
   return rstd;

@@ -2,9 +2,11 @@
 import pytest
 import torch
 
+from oracle import linear as L
+from paper_2609_33133_amd import api
 from paper_2609_33133_amd.autograd import group_linear_attention
 
-from linear_helpers import LEAVES, batch, decays, inputs, run
+from linear_helpers import LEAVES, batch, decays, inputs, run, to64
 
 pytestmark = pytest.mark.gpu
 
@@ -25,3 +27,19 @@ def test_a_state_updated_between_forward_and_backward():
     state.zero_()  # the buffer of the next piece
     for n, g in zip(LEAVES, torch.autograd.grad(outs, leaf, (x["do_p"], x["do_r"]))):
         assert torch.equal(g, want["d" + n]), n
+
+
+def test_a_norm_of_tiny_values_with_a_tiny_eps():
+    """var + eps below the least normal number: a constant row gives the bias, others their n. The squares are denormal,
+    off by 2^-150 each of some 2^-133, which is 2^-18 of n."""
+    gen = torch.Generator().manual_seed(73)
+    sign = torch.randint(0, 2, (20, 2, 64), generator=gen).double() * 2 - 1
+    x = (sign * 1e-20).to(torch.bfloat16)
+    x[3], x[4, 1] = 1e-20, 0.0
+    eps = 1e-40
+    w, bias = 1 + 0.1 * torch.randn(2, 64, generator=gen), 0.1 * torch.randn(2, 64, generator=gen)
+    ref = L.norm(x.double().numpy(), weight=w.double().numpy(), bias=bias.double().numpy(), eps=eps)
+    y = api.head_norm_fwd(x.cuda(), w.cuda(), bias.cuda(), eps=eps)
+    mag = 1.5 * abs(w.double().numpy()) + abs(bias.double().numpy())
+    assert (abs(to64(y) - ref["y"]) <= 2.0 ** -8 * abs(ref["y"]) + 2.0 ** -16 * mag).all()
+    assert torch.equal(y[3].cpu(), bias.to(torch.bfloat16)) and torch.equal(y[4, 1].cpu(), bias[1].to(torch.bfloat16))
