@@ -6,7 +6,7 @@ from oracle import linear as L
 from paper_2609_33133_amd import api
 from paper_2609_33133_amd.autograd import group_linear_attention
 
-from linear_helpers import LEAVES, batch, decays, inputs, run, to64
+from linear_helpers import LEAVES, batch, check, decays, inputs, oracle, run, to64
 
 pytestmark = pytest.mark.gpu
 
@@ -43,3 +43,11 @@ def test_a_norm_of_tiny_values_with_a_tiny_eps():
     mag = 1.5 * abs(w.double().numpy()) + abs(bias.double().numpy())
     assert (abs(to64(y) - ref["y"]) <= 2.0 ** -8 * abs(ref["y"]) + 2.0 ** -16 * mag).all()
     assert torch.equal(y[3].cpu(), bias.to(torch.bfloat16)) and torch.equal(y[4, 1].cpu(), bias[1].to(torch.bfloat16))
+
+
+@pytest.mark.parametrize("hq,hkv,d", [(256, 256, 64), (96, 1, 128)])
+def test_as_many_heads_as_there_may_be(hq, hkv, d):
+    """KV heads up to the limit (their decays fill the kernel arguments), and a long loop over the heads of one."""
+    b, dec = batch([(70, [3, 66])], hq, hkv, d), decays(hkv)
+    x = inputs(b, 74)
+    check(run(b, dec, x), oracle(b, dec, x), f"{hq} / {hkv}")
