@@ -22,6 +22,10 @@ The first computes a prompt's state once and goes on from it in every branch
 (augtree_linear_fwd/bwd); the second is the norm over each head that follows
 such a layer (augtree_head_norm_fwd/bwd). At decode, api.linear_step takes one
 token of every sequence at a time.
+
+A step, forward and backward, may be captured into a graph while no eager graph
+of the same leaves is alive (torch's engine would join the two in the capture
+and end the process).
 """
 from __future__ import annotations
 

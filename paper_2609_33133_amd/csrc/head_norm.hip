@@ -14,8 +14,8 @@
 // weight and bias are read once and their gradients are summed in registers.
 // What else costs here is the vector ALU: the exact expf and division of the
 // activation alone kept the forward at 3.2 of the 4.9 TB/s that a copy reaches.
-// 49152 rows of 32 heads of 128 with a gate: forward 240 us (5.0 TB/s), backward
-// 420 us (4.8 TB/s).
+// 49152 rows of 32 heads of 128 with a gate: forward 245 us (4.9 TB/s), backward
+// 417 us (4.8 TB/s).
 #include <type_traits>
 
 #include "common.h"
@@ -212,7 +212,7 @@ __global__ __launch_bounds__(256) void head_norm_bwd_kernel(HeadNormParams p, in
 
 // dweight, dbias: the partial sums. 64 channels a workgroup, 16 wavefronts with
 // every 16th part each (4 wavefronts took 54 us for 512 parts of 2 x 4096
-// where these take 5), then the 16 in order.
+// where these take 6), then the 16 in order.
 __global__ __launch_bounds__(1024) void head_norm_sum_kernel(const float* part, int parts, int width, float* dweight,
                                                              float* dbias) {
   __shared__ float s[16][64];

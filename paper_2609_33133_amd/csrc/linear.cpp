@@ -110,10 +110,12 @@ double rounds(int64_t units, int per_cu) {
 // workgroup of the output kernel takes `row` us a row and 2 d / (1 + group) rows' time for its state; dq and
 // the state kernels come to 1.75 of that; dk and dv take 0.9 a row and twice the state, with workgroups that
 // fill twice the room; each of the two scans moves the states once in and out at 4.7 TB/s, but takes 0.12 us
-// for every block of its longest chain. Measured: over 22 random trees and seven head layouts the rows chosen
-// take 0.5 % longer on average than the best of 64, 128, 192, 256, 384, 512, 768 and 1024, and 4.5 % at most;
-// 32768 rows with eight branches of 2048, 32 / 8 heads, d = 128, take 1110 us with the 832 rows chosen, 1165
-// with 512, 1200 with 1024. The tree alone decides, so that its results do not depend on the batch.
+// for every block of its longest chain. Measured: over 88 random trees of up to 30 k rows and seven head layouts
+// the rows chosen take 0.6 % longer on average than the best of 64, 128, 192, 256, 384, 512, 768 and 1024; with
+// d = 128 4.8 % at most, with d = 64 (17 of them) 1.9 % on average and once 16 % (8 k rows with short branches,
+// 16 / 4 heads). A training step of 32768 rows with eight branches of 2048, 32 / 8 heads, d = 128, takes 1059 us
+// with the 832 rows chosen, 1110 with 512, 1150 with 1024. The tree alone decides, so that its results do not
+// depend on the batch.
 int block_rows(const augtree_groups* g, int tree) {
   const int d = g->head_dim, hkv = g->num_kv_heads, nb = g->num_branches, group = g->num_q_heads / hkv;
   const double row = group * (d == 128 ? 0.033 : 0.025), state = 2.0 * d / (1 + group);
@@ -153,7 +155,7 @@ int make_layout(const augtree_groups* g, Layout* L) {
   L->segs.resize((size_t)ng + nb);
   int64_t blocks = 0;
   // A segment is cut evenly, into the number of blocks that block_rows of a block would make: the branches' blocks, which
-  // start last, are then no longer than they have to be (that batch: 1250 us against 1220 in a steady run).
+  // start last, are then no longer than they have to be (that step: 1076 us against 1081).
   auto add = [&](int i, int row0, int len, int link, int rows) {
     const int64_t n = cdiv(len, rows);
     LinSeg& s = L->segs[i];

@@ -27,11 +27,12 @@
 // rounding; the low terms are 45 % of the matrix instructions and cost about a
 // sixth of the time.
 //
-// What bounds it (49152 rows, 32 / 8 heads, d = 128; a copy reaches 4.9 TB/s
-// here): the output and dq kernels move 1.0 GB each in 234 us, 4.4 TB/s, the state
-// kernels 0.2 GB in 57 us forward and 0.8 GB in 168 us in reverse, 3.6 and 4.8
-// TB/s. The kernel for dk and dv moves 1.2 GB in 330 us, 3.7 TB/s; its matrix
-// cores and its LDS are busy for 40 % of that each, in phases that barriers part.
+// What bounds it (49152 rows, 32 / 8 heads, d = 128, in a steady run; a copy
+// reaches 4.9 TB/s here): the output and dq kernels move 1.0 GB each in 235 and 238
+// us, 4.4 TB/s, the state kernels 0.2 GB in 55 us forward and 0.8 GB in 166 us in
+// reverse, 3.8 and 4.9 TB/s. The kernel for dk and dv moves 1.2 GB in 330 us, 3.7
+// TB/s; its matrix cores are busy for 41 % of that and its LDS for 37 %, in phases
+// that barriers part.
 // The clock is what the chip's power leaves, 1.4 to 2.0 GHz of 2.4. Taken or left
 // within 3 % of the time: P in 32 x 32 tiles, 8 wavefronts of 16 columns, wavefront
 // priorities, tiles fetched half a step earlier, operands of a product with P all
@@ -66,7 +67,7 @@ __device__ __forceinline__ LinSeg load_segment(const LinBatch& b, int i) {
 
 // The segment of a block: the last one that does not begin behind it. All lanes of a wavefront look at once, at 64
 // segments that part the ones in question, so that 4096 take two loads in a row
-// (halving them: 541 us for a training step of 544 segments where this takes 509).
+// (halving them: 541 us for a training step of 32 trees with 16 short branches each, 8 / 2 heads, where this takes 511).
 __device__ __forceinline__ Block find_block(const LinBatch& b, int block) {
   int lo = 0, n = b.num_trees + b.num_branches;
   while (n > 1) {
