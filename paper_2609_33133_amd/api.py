@@ -384,9 +384,9 @@ def _out(t, name, dtype, shape, device):
 def _written(given):
     """Counts a call's writes to the caller's own tensors as torch's in-place operations count theirs, so that a backward
     which saved one of them notices."""
-    given = [t for t in given if t is not None]
-    if given:
-        torch.autograd.graph.increment_version(given)
+    for t in given:
+        if t is not None:
+            torch.autograd.graph.increment_version(t)
 
 
 def _check_batch(b: GroupBatch):
@@ -493,10 +493,11 @@ def linear_step(q, k, v, decay, state, src=None, state_out=None, o=None, scale: 
     itself only without src) and returns (o, state_out). Decode only: tensors that ask for a gradient are refused while
     gradients are enabled."""
     on = _On((("q", q), ("k", k), ("v", v), ("state", state), ("src", src), ("state_out", state_out), ("o", o)), stream)
-    floats = (q, k, v, state, state_out, o)
-    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in floats):
+    if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad or state.requires_grad or
+                                    (state_out is not None and state_out.requires_grad) or
+                                    (o is not None and o.requires_grad)):
         raise ValueError("linear_step forms no gradient: call it under torch.no_grad(), or with detached tensors")
-    if _tangent(floats):
+    if _tangent((q, k, v, state, state_out, o)):
         raise ValueError("linear_step takes no dual tensors: a tangent would get lost")
     if q.dim() != 3 or k.dim() != 3 or state.dim() != 4:
         raise ValueError("q and k must be [rows, heads, head_dim], state [n, heads, head_dim, head_dim]")
