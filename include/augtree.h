@@ -471,6 +471,110 @@ int augtree_head_norm_bwd(int64_t rows, int32_t heads, int32_t head_dim, int act
                           void* ws, size_t ws_bytes, void* stream);
 size_t augtree_head_norm_workspace_size(int64_t rows, int32_t heads, int32_t head_dim);
 
+/* ---------------------------------------------------------------------------
+ * Paged KV cache under replay trees (rollout)
+ *
+ * Attention of new tokens over cached ones, for the sampling that fills the
+ * trees which the calls above train on. Keys and values of one layer lie in a
+ * pool of pages of page_size tokens, [num_pages][Hkv][page_size][d]; a
+ * sequence's tokens are named by its row of the page table. A sequence may have
+ * a parent (a branch its prompt): its tokens then see all tokens of the parent,
+ * whose pages stay where they are and belong to the parent alone, and after
+ * them its own, causally. A parent has no parent itself.
+ *
+ * A step: augtree_page_plan once, for all layers; then per layer
+ * augtree_cache_write and augtree_paged_fwd with that plan. Lengths, tables and
+ * plans stay on the GPU, every call enqueues kernels only and may be captured
+ * into a graph and replayed. Calls that share a plan being written, or a
+ * workspace, must not overlap. Results are bitwise reproducible; how work is cut
+ * (and so the last bits) follows from the batch.
+ * ------------------------------------------------------------------------- */
+
+/* Tables of a cache (DEVICE arrays, owned by the caller), shared by all layers. */
+typedef struct augtree_pages {
+  int32_t num_seqs;    /* rows of the table, at most 2^20 */
+  int32_t max_pages;   /* entries of a row; max_pages * page_size <= 2^30 */
+  int32_t num_pages;   /* pages of the pool; num_pages * page_size <= 2^30 */
+  int32_t page_size;   /* tokens of a page: 16, 32, 64, 128 or 256 */
+  int32_t* table;      /* [num_seqs][max_pages]: page of each page_size tokens of a sequence */
+  int32_t* length;     /* [num_seqs]: cached tokens */
+  int32_t* parent;     /* [num_seqs], < 0: none; NULL: nobody has one */
+  int32_t* free_pages; /* [num_pages]: a ring of free pages */
+  int32_t* free_state; /* [2]: position of the first free page in the ring, number of free pages */
+} augtree_pages;
+
+/* Bits of a plan's status word; 0: the plan is good. A plan with any of them (but
+ * AUGTREE_PAGES_PAGE) has no rows: lengths, the ring and the caches stay as they
+ * were, and the calls that take it do nothing. */
+typedef enum augtree_pages_status {
+  AUGTREE_PAGES_SHORT = 1,  /* fewer free pages than the new tokens need */
+  AUGTREE_PAGES_LONG = 2,   /* a sequence outgrows its row of the table */
+  AUGTREE_PAGES_ROWS = 4,   /* more new tokens than `rows` */
+  AUGTREE_PAGES_LENGTH = 8, /* a length < 0 or past the table; a free_state out of range, or more pages given back than are in use */
+  AUGTREE_PAGES_PARENT = 16, /* a sequence with new tokens whose parent is no sequence, itself, has a parent or ends in this call */
+  AUGTREE_PAGES_PAGE = 32   /* a page of the new tokens is outside the pool: these are not written */
+} augtree_pages_status;
+
+/* Fields of a plan that a caller may read, as offsets in int32 words (augtree_page_plan_offset). */
+typedef enum augtree_plan_field {
+  AUGTREE_PLAN_STATUS = 0,    /* [1] augtree_pages_status */
+  AUGTREE_PLAN_CU_ROWS = 1,   /* [num_seqs + 1] first row of each sequence's new tokens */
+  AUGTREE_PLAN_SLOTS = 2,     /* [rows] page * page_size + place in the page; -1 behind the last row */
+  AUGTREE_PLAN_POSITIONS = 3  /* [rows] tokens before it, its parent's among them; -1 behind the last row */
+} augtree_plan_field;
+
+/* Bytes of a plan for at most `rows` new tokens, 0 on invalid arguments; the offset of a field, -1 on invalid arguments. */
+size_t augtree_page_plan_size(const augtree_pages* pages, int32_t rows, int32_t num_q_heads, int32_t num_kv_heads);
+int64_t augtree_page_plan_offset(const augtree_pages* pages, int32_t rows, int32_t num_q_heads, int32_t num_kv_heads,
+                                 int field);
+
+/*
+ * Plans a step. In: new_rows [num_seqs] DEVICE int32: new tokens of each sequence
+ * (0: none; < 0: the sequence has ended, its pages go back and its length becomes
+ * 0), `pages`. The new tokens are numbered sequence by sequence. Out: the table's
+ * new entries (free pages in ring order, sequence by sequence), the ring's
+ * entries behind its last one (ended sequences' pages, in order; they are free
+ * for the next call), length_out [num_seqs], free_state_out [2] (each may be the
+ * array it follows from), the plan. A parent sees its own new tokens too when its
+ * children's attend to it in the same step.
+ * `rows` may exceed the number of new tokens (a captured graph's room): rows
+ * behind the last one are left as they are by the calls that take the plan.
+ * Neighbouring sequences of one parent share its reading where they have few rows each.
+ */
+int augtree_page_plan(const augtree_pages* pages, const int32_t* new_rows, int32_t rows, int32_t num_q_heads,
+                      int32_t num_kv_heads, int32_t* length_out, int32_t* free_state_out, void* plan,
+                      size_t plan_bytes, void* stream);
+
+/* How a cache holds its values: bf16, or OCP e4m3 bytes that stand for byte * scale, with a scale per KV head. */
+typedef enum augtree_cache_type { AUGTREE_CACHE_BF16 = 0, AUGTREE_CACHE_E4M3 = 1 } augtree_cache_type;
+
+/*
+ * Keys and values of the new tokens, k, v [rows,Hkv,d] bf16, into their slots.
+ * Caches: [num_pages][Hkv][page_size][d], pages k_page_stride (v_page_stride)
+ * BYTES apart (a multiple of 16, at least a page), so that both may be views of
+ * one tensor. e4m3: value / scale, rounded to nearest even, at most 448 in
+ * magnitude (NaN stays NaN); k_scale, v_scale [Hkv] DEVICE fp32, not read for bf16.
+ */
+int augtree_cache_write(const augtree_pages* pages, const void* plan, int32_t rows, int32_t num_q_heads,
+                        int32_t num_kv_heads, int32_t head_dim, const uint16_t* k, const uint16_t* v, int cache_type,
+                        void* k_cache, int64_t k_page_stride, void* v_cache, int64_t v_page_stride,
+                        const float* k_scale, const float* v_scale, void* stream);
+
+/*
+ * Attention of the new tokens, which have been written: o_t = sum_j softmax_j(s
+ * q_t.k_j) v_j over all tokens of the sequence's parent and its own tokens up to
+ * t. In: q [rows,Hq,d] bf16, the caches. Out: o like q; lse [Hq,rows] fp32
+ * (nullable). What stands in a page behind a sequence's last token is not read
+ * into any result; a table entry outside the pool reads as zeros.
+ */
+int augtree_paged_fwd(const augtree_pages* pages, const void* plan, int32_t rows, int32_t num_q_heads,
+                      int32_t num_kv_heads, int32_t head_dim, float softmax_scale, const uint16_t* q, int cache_type,
+                      const void* k_cache, int64_t k_page_stride, const void* v_cache, int64_t v_page_stride,
+                      const float* k_scale, const float* v_scale, uint16_t* o, float* lse, void* ws, size_t ws_bytes,
+                      void* stream);
+size_t augtree_paged_workspace_size(const augtree_pages* pages, int32_t rows, int32_t num_q_heads,
+                                    int32_t num_kv_heads, int32_t head_dim);
+
 /*
  * Launch hook (instrumentation; not part of the method). When set, `hook` is
  * called on the calling thread immediately before (phase 0) and after
@@ -479,7 +583,8 @@ size_t augtree_head_norm_workspace_size(int64_t rows, int32_t heads, int32_t hea
  * "lse_merge", "dq_prefill", "dkv_prefill", "dq_replay", "dkv_replay", "dq_tree",
  * "dkv_tree", "grad_reduce", "reduce_tree", "linear_table", "linear_state",
  * "linear_state_rev", "linear_scan", "linear_scan_rev", "linear_out", "linear_dq",
- * "linear_dkv", "linear_step", "head_norm", "head_norm_bwd", "head_norm_sum")
+ * "linear_dkv", "linear_step", "head_norm", "head_norm_bwd", "head_norm_sum",
+ * "page_plan", "cache_write", "paged_fwd", "paged_merge")
  * and the stream the kernel is enqueued on, so that a caller can record HIP
  * events around single kernels. The hook must not call back into the library. NULL removes it.
  * Per thread; the library keeps no other state.

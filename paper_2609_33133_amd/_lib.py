@@ -35,6 +35,21 @@ OP_TREE_BWD = 5
 ACT_NONE = 0
 ACT_SILU = 1
 
+CACHE_BF16 = 0
+CACHE_E4M3 = 1
+
+PLAN_STATUS = 0
+PLAN_CU_ROWS = 1
+PLAN_SLOTS = 2
+PLAN_POSITIONS = 3
+
+PAGES_SHORT = 1
+PAGES_LONG = 2
+PAGES_ROWS = 4
+PAGES_LENGTH = 8
+PAGES_PARENT = 16
+PAGES_PAGE = 32
+
 EXPORTS = (
     "augtree_workspace_size", "augtree_prefill_fwd", "augtree_replay_fwd", "augtree_lse_merge",
     "augtree_replay_bwd", "augtree_prefill_bwd", "augtree_prompt_grad_reduce", "augtree_status_string",
@@ -43,6 +58,8 @@ EXPORTS = (
     "augtree_noalloc_scratch_bytes", "augtree_set_tree_chunk_blocks", "augtree_tree_chunk_blocks",
     "augtree_linear_workspace_size", "augtree_linear_fwd", "augtree_linear_bwd", "augtree_linear_step",
     "augtree_head_norm_fwd", "augtree_head_norm_bwd", "augtree_head_norm_workspace_size",
+    "augtree_page_plan_size", "augtree_page_plan_offset", "augtree_page_plan", "augtree_cache_write",
+    "augtree_paged_workspace_size", "augtree_paged_fwd",
 )
 
 LAUNCH_HOOK = ctypes.CFUNCTYPE(None, ctypes.c_char_p, ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p)
@@ -63,6 +80,21 @@ class Groups(ctypes.Structure):
     ]
 
 
+class Pages(ctypes.Structure):
+    """struct augtree_pages."""
+    _fields_ = [
+        ("num_seqs", ctypes.c_int32),
+        ("max_pages", ctypes.c_int32),
+        ("num_pages", ctypes.c_int32),
+        ("page_size", ctypes.c_int32),
+        ("table", ctypes.c_void_p),
+        ("length", ctypes.c_void_p),
+        ("parent", ctypes.c_void_p),
+        ("free_pages", ctypes.c_void_p),
+        ("free_state", ctypes.c_void_p),
+    ]
+
+
 class AugtreeError(RuntimeError):
     def __init__(self, status: int, what: str, detail: str):
         super().__init__(f"{what}: status {status}: {detail}")
@@ -77,6 +109,7 @@ _I64 = ctypes.c_int64
 _F32 = ctypes.c_float
 _SZ = ctypes.c_size_t
 _GP = ctypes.POINTER(Groups)
+_PP = ctypes.POINTER(Pages)
 
 
 def _sig(lib):
@@ -107,6 +140,14 @@ def _sig(lib):
         "augtree_head_norm_fwd": (ctypes.c_int, [_I64, _I32, _I32, ctypes.c_int, _F32] + [_P] * 6),
         "augtree_head_norm_bwd": (ctypes.c_int, [_I64, _I32, _I32, ctypes.c_int, _F32] + [_P] * 9 + [_P, _SZ, _P]),
         "augtree_head_norm_workspace_size": (_SZ, [_I64, _I32, _I32]),
+        "augtree_page_plan_size": (_SZ, [_PP, _I32, _I32, _I32]),
+        "augtree_page_plan_offset": (_I64, [_PP, _I32, _I32, _I32, ctypes.c_int]),
+        "augtree_page_plan": (ctypes.c_int, [_PP, _P, _I32, _I32, _I32, _P, _P, _P, _SZ, _P]),
+        "augtree_cache_write": (ctypes.c_int, [_PP, _P, _I32, _I32, _I32, _I32, _P, _P, ctypes.c_int, _P, _I64, _P,
+                                               _I64, _P, _P, _P]),
+        "augtree_paged_workspace_size": (_SZ, [_PP, _I32, _I32, _I32, _I32]),
+        "augtree_paged_fwd": (ctypes.c_int, [_PP, _P, _I32, _I32, _I32, _I32, _F32, _P, ctypes.c_int, _P, _I64, _P,
+                                             _I64, _P, _P, _P, _P, _P, _SZ, _P]),
     }
     for name, (res, args) in sigs.items():
         fn = getattr(lib, name)

@@ -583,3 +583,218 @@ def _head_norm_bwd(x, dy, weight, bias, gate, activation, eps, dx, dgate, dweigh
     _lib.check(lib.augtree_head_norm_bwd(rows, heads, d, activation, eps, _addr(x), _addr(gate), _addr(weight),
                                          _addr(bias), _addr(dy), _addr(dx), _addr(dgate), _addr(dweight), _addr(dbias),
                                          _addr(ws), n, stream), "head_norm_bwd")
+
+
+# ---------------------------------------------------------------------------- paged KV cache
+
+class PageTable:
+    """The tables of a paged KV cache (struct augtree_pages), int32 tensors on one GPU that stay the caller's: `table`
+    [seqs, max_pages], `length` [seqs] cached tokens, `parent` [seqs] (< 0, or no tensor: none), `free_pages` [pages] a
+    ring of free pages, `free_state` [2] its first free entry and their number. One PageTable serves all layers of a
+    model; the caches of a layer are tensors [pages, Hkv, page_size, d]. PageTable.empty makes an unused one."""
+
+    def __init__(self, table, length, parent, free_pages, free_state, page_size: int):
+        on = _On((("table", table), ("length", length), ("parent", parent), ("free_pages", free_pages),
+                  ("free_state", free_state)))
+        if table.dim() != 2 or free_pages.dim() != 1:
+            raise ValueError("table must be [seqs, max_pages], free_pages [pages]")
+        seqs, i32 = table.shape[0], torch.int32
+        _want(table, "table", i32, table.shape)
+        _want(length, "length", i32, (seqs,))
+        if parent is not None:
+            _want(parent, "parent", i32, (seqs,))
+        _want(free_pages, "free_pages", i32, free_pages.shape)
+        _want(free_state, "free_state", i32, (2,))
+        self.device = on.device
+        self.table, self.length, self.parent = table, length, parent
+        self.free_pages, self.free_state = free_pages, free_state
+        self.num_seqs, self.max_pages, self.num_pages = seqs, table.shape[1], free_pages.shape[0]
+        self.page_size = int(page_size)
+        self.struct = _lib.Pages(seqs, self.max_pages, self.num_pages, self.page_size, _addr(table), _addr(length),
+                                 _addr(parent), _addr(free_pages), _addr(free_state))
+        self.ref = ctypes.byref(self.struct)
+
+    @classmethod
+    def empty(cls, num_seqs: int, max_pages: int, num_pages: int, page_size: int, device="cuda") -> "PageTable":
+        """Tables of `num_seqs` sequences without tokens or parents, all pages free."""
+        i32 = dict(dtype=torch.int32, device=device)
+        return cls(torch.zeros(num_seqs, max_pages, **i32), torch.zeros(num_seqs, **i32),
+                   torch.full((num_seqs,), -1, **i32), torch.arange(num_pages, **i32),
+                   torch.tensor([0, num_pages], **i32), page_size)
+
+
+class PagePlan:
+    """A step's plan (page_plan): `cu_rows` [seqs + 1], `slots` and `positions` [rows] and `status` [1] are views of it
+    on the GPU."""
+
+    def __init__(self, pages: PageTable, rows: int, num_q_heads: int, num_kv_heads: int):
+        lib = _lib.load()
+        self.pages, self.rows, self.hq, self.hkv = pages, int(rows), int(num_q_heads), int(num_kv_heads)
+        n = lib.augtree_page_plan_size(pages.ref, self.rows, self.hq, self.hkv)
+        if n == 0:
+            raise _lib.AugtreeError(_lib.AUGTREE_ERR_INVALID_ARGUMENT, "page_plan_size",
+                                    lib.augtree_last_error().decode())
+        self.data = torch.empty(n // 4, dtype=torch.int32, device=pages.device)
+        self._ws_bytes = {}
+
+    def _field(self, field: int, count: int) -> torch.Tensor:
+        at = _lib.load().augtree_page_plan_offset(self.pages.ref, self.rows, self.hq, self.hkv, field)
+        return self.data[at:at + count]
+
+    @property
+    def status(self) -> torch.Tensor:
+        return self._field(_lib.PLAN_STATUS, 1)
+
+    @property
+    def cu_rows(self) -> torch.Tensor:
+        return self._field(_lib.PLAN_CU_ROWS, self.pages.num_seqs + 1)
+
+    @property
+    def slots(self) -> torch.Tensor:
+        return self._field(_lib.PLAN_SLOTS, self.rows)
+
+    @property
+    def positions(self) -> torch.Tensor:
+        return self._field(_lib.PLAN_POSITIONS, self.rows)
+
+    def check(self) -> None:
+        """Raises if the tables could not take the step (waits for the GPU)."""
+        bits = int(self.status)
+        if bits:
+            raise RuntimeError("page_plan: " + "; ".join(text for bit, text in PAGES_STATUS.items() if bits & bit))
+
+    def workspace_size(self, head_dim: int) -> int:
+        """Bytes of workspace of paged_fwd with this plan."""
+        n = self._ws_bytes.get(head_dim)
+        if n is None:
+            lib = _lib.load()
+            n = int(lib.augtree_paged_workspace_size(self.pages.ref, self.rows, self.hq, self.hkv, head_dim))
+            if n == 0:
+                raise _lib.AugtreeError(_lib.AUGTREE_ERR_UNSUPPORTED, "paged_workspace_size",
+                                        lib.augtree_last_error().decode())
+            self._ws_bytes[head_dim] = n
+        return n
+
+
+PAGES_STATUS = {
+    _lib.PAGES_SHORT: "fewer free pages than the new tokens need",
+    _lib.PAGES_LONG: "a sequence outgrows its row of the table",
+    _lib.PAGES_ROWS: "more new tokens than the plan has rows",
+    _lib.PAGES_LENGTH: "a length or the free list's state is out of range",
+    _lib.PAGES_PARENT: "a parent is no sequence, the sequence itself, has a parent or ends in this step",
+    _lib.PAGES_PAGE: "a page of the new tokens is outside the pool",
+}
+
+
+def page_plan(pages: PageTable, new_rows, rows: int, num_q_heads: int, num_kv_heads: int, length_out=None,
+              free_state_out=None, plan: Optional[PagePlan] = None, stream=None) -> PagePlan:
+    """Plans a step of a paged cache (augtree_page_plan): `new_rows` [seqs] int32 on the GPU are the new tokens of every
+    sequence (< 0: it has ended and gives its pages back), `rows` at least their sum. Takes pages from the ring into the
+    tables, advances the lengths and the ring's state (in place, unless length_out and free_state_out are given) and
+    returns the plan that cache_write and paged_fwd of all layers take; `plan`: one of an earlier step of the same sizes,
+    written over. What does not fit leaves everything as it was: PagePlan.check tells."""
+    on = _On((("table", pages.table), ("new_rows", new_rows), ("length_out", length_out),
+              ("free_state_out", free_state_out)), stream)
+    _want(new_rows, "new_rows", torch.int32, (pages.num_seqs,))
+    length = pages.length if length_out is None else length_out
+    state = pages.free_state if free_state_out is None else free_state_out
+    _want(length, "length_out", torch.int32, (pages.num_seqs,))
+    _want(state, "free_state_out", torch.int32, (2,))
+    with on as st:
+        if plan is None:
+            plan = PagePlan(pages, rows, num_q_heads, num_kv_heads)
+        elif plan.pages is not pages or (plan.rows, plan.hq, plan.hkv) != (rows, num_q_heads, num_kv_heads):
+            raise ValueError("the plan was made for other tables, rows or heads")
+        _lib.check(_lib.load().augtree_page_plan(pages.ref, _addr(new_rows), plan.rows, plan.hq, plan.hkv, _addr(length),
+                                                 _addr(state), _addr(plan.data), 4 * plan.data.numel(), st), "page_plan")
+    _written((pages.table, pages.free_pages, length, state, plan.data))
+    return plan
+
+
+def _no_grad(what: str, tensors):
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
+        raise ValueError(f"{what} forms no gradient: call it under torch.no_grad(), or with detached tensors")
+    if _tangent(tensors):
+        raise ValueError(f"{what} takes no dual tensors: a tangent would get lost")
+
+
+def _cache(t, name: str, plan: PagePlan, d: int):
+    """A cache's type and the bytes between its pages: [pages, Hkv, page_size, d], dense but for the first dimension."""
+    pages = plan.pages
+    if t.dtype is torch.bfloat16:
+        kind, size = _lib.CACHE_BF16, 2
+    elif t.dtype is torch.float8_e4m3fn:
+        kind, size = _lib.CACHE_E4M3, 1
+    else:
+        raise TypeError(f"{name}: dtype {t.dtype}, expected torch.bfloat16 or torch.float8_e4m3fn")
+    shape = (pages.num_pages, plan.hkv, pages.page_size, d)
+    if t.shape != shape:
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {shape}")
+    stride, page = t.stride(), pages.page_size * d
+    if stride[3] != 1 or stride[2] != d or (stride[1] != page and plan.hkv > 1):
+        raise ValueError(f"{name} must be contiguous but for its first dimension")
+    return kind, (stride[0] if pages.num_pages > 1 else plan.hkv * page) * size
+
+
+def _caches(k_cache, v_cache, k_scale, v_scale, plan: PagePlan, d: int):
+    kind, k_stride = _cache(k_cache, "k_cache", plan, d)
+    v_kind, v_stride = _cache(v_cache, "v_cache", plan, d)
+    if kind != v_kind:
+        raise TypeError(f"k_cache is {k_cache.dtype}, v_cache {v_cache.dtype}")
+    for n, t in (("k_scale", k_scale), ("v_scale", v_scale)):
+        if (t is not None) != (kind == _lib.CACHE_E4M3):
+            raise ValueError(f"{n} goes with a cache in 8 bits" + (", which needs it" if t is None else ""))
+        if t is not None:
+            _want(t, n, torch.float32, (plan.hkv,))
+    return kind, k_stride, v_stride
+
+
+def cache_write(k, v, k_cache, v_cache, plan: PagePlan, k_scale=None, v_scale=None, stream=None) -> None:
+    """Writes the keys and values of a step's new tokens, k, v [rows, Hkv, d] bf16, into their slots of the caches
+    [pages, Hkv, page_size, d] (augtree_cache_write): bf16, or float8_e4m3fn holding value / scale with fp32 scales [Hkv]
+    on the GPU. The caches may be views with any stride between pages (two halves of one tensor)."""
+    on = _On((("plan", plan.data), ("k", k), ("v", v), ("k_cache", k_cache), ("v_cache", v_cache), ("k_scale", k_scale),
+              ("v_scale", v_scale)), stream)
+    _no_grad("cache_write", (k, v, k_cache, v_cache))
+    if k.dim() != 3:
+        raise ValueError("k must be [rows, heads, head_dim]")
+    d = k.shape[2]
+    _want(k, "k", torch.bfloat16, (plan.rows, plan.hkv, d))
+    _want(v, "v", torch.bfloat16, (plan.rows, plan.hkv, d))
+    kind, k_stride, v_stride = _caches(k_cache, v_cache, k_scale, v_scale, plan, d)
+    with on as st:
+        _lib.check(_lib.load().augtree_cache_write(plan.pages.ref, _addr(plan.data), plan.rows, plan.hq, plan.hkv, d,
+                                                   _addr(k), _addr(v), kind, _addr(k_cache), k_stride, _addr(v_cache),
+                                                   v_stride, _addr(k_scale), _addr(v_scale), st), "cache_write")
+    _written((k_cache, v_cache))
+
+
+def paged_fwd(q, k_cache, v_cache, plan: PagePlan, k_scale=None, v_scale=None, o=None, lse=None,
+              scale: Optional[float] = None, want_lse: bool = False, ws=None, stream=None):
+    """Attention of a step's new tokens, q [rows, Hq, d] bf16, over the cached tokens of their sequences' parents and
+    their own up to themselves (augtree_paged_fwd). Returns (o, lse): o like q, lse [Hq, rows] fp32 or None unless asked
+    for; rows behind the plan's last one are not written. Decode only: tensors that ask for a gradient are refused while
+    gradients are enabled."""
+    on = _On((("plan", plan.data), ("q", q), ("k_cache", k_cache), ("v_cache", v_cache), ("k_scale", k_scale),
+              ("v_scale", v_scale), ("o", o), ("lse", lse), ("ws", ws)), stream)
+    _no_grad("paged_fwd", (q, k_cache, v_cache, o))
+    if q.dim() != 3:
+        raise ValueError("q must be [rows, heads, head_dim]")
+    d = q.shape[2]
+    _want(q, "q", torch.bfloat16, (plan.rows, plan.hq, d))
+    kind, k_stride, v_stride = _caches(k_cache, v_cache, k_scale, v_scale, plan, d)
+    given = (o, lse, ws)
+    _want_ws(ws, "ws")
+    with on as st:
+        o = _out(o, "o", torch.bfloat16, q.shape, on.device)
+        if want_lse or lse is not None:
+            lse = _out(lse, "lse", torch.float32, (plan.hq, plan.rows), on.device)
+        if ws is None:
+            ws = torch.empty(plan.workspace_size(d), dtype=torch.uint8, device=on.device)
+        _lib.check(_lib.load().augtree_paged_fwd(
+            plan.pages.ref, _addr(plan.data), plan.rows, plan.hq, plan.hkv, d,
+            1.0 / math.sqrt(d) if scale is None else float(scale), _addr(q), kind, _addr(k_cache), k_stride,
+            _addr(v_cache), v_stride, _addr(k_scale), _addr(v_scale), _addr(o), _addr(lse), _addr(ws), ws.numel(), st),
+            "paged_fwd")
+    _written(given)
+    return o, lse

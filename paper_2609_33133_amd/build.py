@@ -28,7 +28,7 @@ HIP_FLAGS = ["--offload-arch=" + ARCH, "-Xclang", "-target-feature", "-Xclang", 
 # The linear-attention layer states how far a NaN or an infinity reaches, so its
 # kernels are compiled with NaN honoured (the same instructions but for ten of
 # the 25000 lines of its largest source, and the same times).
-NAN_SOURCES = ("linear", "head_norm")
+NAN_SOURCES = ("linear", "head_norm", "paged")
 # The attention kernels are scheduled by the backend's instruction-level
 # parallelism strategy (the dK/dV kernel runs ~1 % faster than with the
 # default occupancy-driven one, the other two slightly faster; no spills);

@@ -9,21 +9,13 @@
 // partial states done in registers; a tile with only one segment produces one
 // partial state (split mode).
 //
-// Per 64-key block and wavefront: 16 MFMAs for S^T = K Q^T (K rows from LDS,
-// Q^T held in registers), the online-softmax update in fp32 with exp2 (the
-// output is rescaled only when a row maximum grows), and 16 MFMAs for
-// O^T += V^T P^T (V^T by transpose reads of the row-major V tile, P^T straight
-// from the S^T accumulators rounded to bf16). The loop is software-pipelined:
-// the S MFMAs of block b + 1 are interleaved one by one with the exponentials
-// of block b (explicit scheduling groups), so one wavefront keeps the matrix
-// cores and the vector ALUs busy together. LDS addresses come from per-lane
-// offset tables computed once, and operand reads run a few MFMAs ahead of
-// their MFMA. K and V tiles are double-buffered in LDS (separate arrays, loop
+// The step of a 64-key block is FwdCore's (fwd_core.h). K and V tiles are double-buffered in LDS (separate arrays, loop
 // unrolled by two, so the compiler can tell the buffer being filled from the
 // one being read) and copied there directly from global memory
 // (buffer_load ... lds), so no registers hold staged data. Two workgroups
 // share a CU (two wavefronts per SIMD).
 #include "common.h"
+#include "fwd_core.h"
 #include "kernels.h"
 
 namespace augtree {
@@ -31,14 +23,6 @@ namespace augtree {
 namespace {
 
 constexpr int BN = kFwdBlockN;  // keys per block
-constexpr int FWD_DEPTH = 4;  // LDS operand reads run this many MFMAs ahead
-constexpr int PV_DEPTH = 3;   // the same for the P V MFMAs (two reads each)
-constexpr int FWD_VALU_PER_MFMA = 7;  // softmax instructions placed after each S MFMA
-// The exponent reference of a row (its running maximum) moves only when a
-// block's maximum exceeds it by more than this many powers of two. Exact: the
-// reference cancels between numerator and denominator; P stays <= 2^8, far
-// inside the fp32 and bf16 ranges.
-constexpr float RESCALE_MARGIN_LOG2 = 8.f;
 
 template <int D, bool OUT32>
 __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(FwdParams p) {
@@ -112,28 +96,10 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(FwdParams p) {
     if (nblk > 1) load_k(k_buf1);
   }
 
-  // Q^T operand (B of S^T = K Q^T): lane holds query qi, d = 16*ks + 8*hf .. +7
-  bf16x8 qreg[D / 16];
-  {
-    const uint16_t* qp = qsrc + qbase + qoff + hf * 8;
-#pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks)
-      qreg[ks] = as_bf16x8(ldg16(qp + ks * 16));
-  }
-
-  const float c = p.scale_log2;
-  float m_run = -INFINITY;  // running max of raw q.k over this lane's query
-  float l_run = 0.f;        // this half-wave's share of the running sum
-  f32x16 oacc[D / 32];
-#pragma unroll
-  for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) oacc[db][i] = 0.f;
-
-  RowOffsets<D> k_off;  // K row l32; row 32 + l32 has the same swizzle, 32 rows further
-  k_off.init(l32, hf);
-  TrOffsets<D> vtr_off;  // V^T operands
-  vtr_off.init(0, lane);
+  FwdCore<D> core;
+  core.hf = hf;
+  core.load_q(qsrc + qbase + qoff);
+  core.init(p.scale_log2, lane);
   const int qpos_lo = t.b_qpos + rows.wlo;  // causal: the wavefront's first query position
 
   // a causal block whose keys all follow the wavefront's queries (and every
@@ -142,114 +108,20 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(FwdParams p) {
   const int nlive = !rows.wave_any ? 0 : t.b_len > 0 ? nA + (t.b_qpos + rows.whi) / BN + 1 : nA;
   auto skipped = [&](int b) { return b >= nlive; };
 
-  // S^T of one 64-key block (two 32-key halves), raw scores
-  auto s_mfma = [&](const __bf16* kl, f32x16& s0, f32x16& s1) {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) { s0[i] = 0.f; s1[i] = 0.f; }
-#pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks) {
-      s0 = mfma32(lds_row8_at<D>(kl, k_off.o[ks]), qreg[ks], s0);
-      s1 = mfma32(lds_row8_at<D>(kl + 32 * D, k_off.o[ks]), qreg[ks], s1);
-    }
-  };
-
-  // mask, running max and (when it grew) rescale for block b; returns the
-  // exponent offset of the block
-  auto stats = [&](int b, f32x16& s0, f32x16& s1) -> float {
+  auto step = [&](int b, f32x16& s0, f32x16& s1, const __bf16* kn, const __bf16* vl, f32x16& n0, f32x16& n1) {
     const bool isB = b >= nA;
     const int kb0 = (isB ? b - nA : b) * BN;
     const int len = isB ? t.b_len : t.a_len;
-    if ((kb0 + BN > len) || (isB && (kb0 + BN - 1 > qpos_lo))) {
-      const int lim = min(len - 1, isB ? t.b_qpos + qi : len - 1) - kb0;  // last visible key of the block
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        if (acc_row(i, hf) > lim) s0[i] = -INFINITY;
-        if (acc_row(i, hf) + 32 > lim) s1[i] = -INFINITY;
-      }
-    }
-    // four independent chains of three-input maxima (v_max3_f32, written
-    // out: left to itself the compiler pairs the values with two-input maxima
-    // first and needs about a third more instructions), and the half-wave
-    // exchange without LDS
-    auto max3 = [](float a, float b, float c) {
-      float r;
-      asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-      return r;
-    };
-    float m4[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      float m = max3(s0[j], s1[j], s0[j + 4]);
-      m = max3(m, s1[j + 4], s0[j + 8]);
-      m = max3(m, s1[j + 8], s0[j + 12]);
-      m4[j] = fmaxf(m, s1[j + 12]);
-    }
-    const float mx = pair_max(fmaxf(max3(m4[0], m4[1], m4[2]), m4[3]));
-    const float mnew = fmaxf(m_run, mx);
-    // rescale only when some row maximum of this wavefront passed its
-    // reference by more than the margin (always on a row's first visible key:
-    // the reference starts at -inf)
-    if (__any(mx * c > m_run * c + RESCALE_MARGIN_LOG2)) {
-      const float alpha = (mnew == -INFINITY) ? 1.f : __builtin_amdgcn_exp2f((m_run - mnew) * c);
-      l_run *= alpha;
-#pragma unroll
-      for (int db = 0; db < D / 32; ++db)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) oacc[db][i] *= alpha;
-      m_run = mnew;
-    }
-    return (m_run == -INFINITY) ? 0.f : m_run * c;
-  };
-
-  // One block step. Scores S(b) arrive in s0/s1 (computed one step earlier);
-  // the S MFMAs of block b + 1 (from kn, into n0/n1) are interleaved one by
-  // one with the exponentials, row sums and bf16 conversion of block b, so the
-  // matrix cores and the vector ALUs of the wavefront work at the same time;
-  // then O += V(b)^T P(b)^T. On the last block the extra S is computed from a
-  // stale buffer and never used.
-  auto step = [&](int b, f32x16& s0, f32x16& s1, const __bf16* kn, const __bf16* vl, f32x16& n0, f32x16& n1) {
-    const float ms = stats(b, s0, s1);
-    __builtin_amdgcn_sched_barrier(0);
-    s_mfma(kn, n0, n1);
-    float l4[4];  // four independent partial sums
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      s0[i] = __builtin_amdgcn_exp2f(s0[i] * c - ms);
-      s1[i] = __builtin_amdgcn_exp2f(s1[i] * c - ms);
-      l4[i & 3] = i < 4 ? s0[i] + s1[i] : l4[i & 3] + (s0[i] + s1[i]);
-    }
-    l_run += (l4[0] + l4[1]) + (l4[2] + l4[3]);
-    const bf16x8 pb0 = to_bf16x8(s0, 0), pb1 = to_bf16x8(s0, 8);
-    const bf16x8 pb2 = to_bf16x8(s1, 0), pb3 = to_bf16x8(s1, 8);
-    // 16 MFMAs with one K read each (reads run FWD_DEPTH ahead), the ~112
-    // vector instructions of the softmax spread over them
-    __builtin_amdgcn_sched_group_barrier(0x100, FWD_DEPTH, 0);
-#pragma unroll
-    for (int i = 0; i < D / 8; ++i) {
-      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-      if (i < D / 8 - FWD_DEPTH) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x402, FWD_VALU_PER_MFMA, 0);
-    }
-    set_wave_priority<1>();
-    // k-step outer, output column block inner: consecutive MFMAs go to
-    // different accumulators (each still sums its four k-steps in order)
-#pragma unroll
-    for (int db = 0; db < D / 32; ++db) oacc[db] = mfma32(vtr_off.read(vl, 0, db), pb0, oacc[db]);
-#pragma unroll
-    for (int db = 0; db < D / 32; ++db) oacc[db] = mfma32(vtr_off.read(vl, 1, db), pb1, oacc[db]);
-#pragma unroll
-    for (int db = 0; db < D / 32; ++db) oacc[db] = mfma32(vtr_off.read(vl, 2, db), pb2, oacc[db]);
-#pragma unroll
-    for (int db = 0; db < D / 32; ++db) oacc[db] = mfma32(vtr_off.read(vl, 3, db), pb3, oacc[db]);
-    pace_lds_mfma<D / 8, 2, PV_DEPTH>();
-    set_wave_priority<0>();
+    const bool masked = (kb0 + BN > len) || (isB && (kb0 + BN - 1 > qpos_lo));
+    const int lim = min(len - 1, isB ? t.b_qpos + qi : len - 1) - kb0;  // last visible key of the block
+    core.step(masked, lim, s0, s1, kn, vl, n0, n1);
   };
 
   // iteration b loads K(b + 2) over K(b) and V(b + 1) over V(b - 1)
   f32x16 sa0, sa1, sb0, sb1;
   wait_vmem();
   __syncthreads();
-  s_mfma(k_buf0, sa0, sa1);
+  core.s_mfma(k_buf0, sa0, sa1);
   pace_lds_mfma<D / 8, 1, FWD_DEPTH>();
   __syncthreads();
   for (int b = 0; b < nblk; b += 2) {
@@ -267,7 +139,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(FwdParams p) {
     }
   }
 
-  const float l_tot = pair_sum(l_run);
+  const float l_tot = pair_sum(core.l_run);
   const bool part1 = (t.flags & QT_PART1) != 0;
   // (the lane's row again, instead of registers held over the sweep)
   const QRows er(t, p.group, p.group_magic, hh, wave, (int)opaque(l32));
@@ -281,17 +153,17 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(FwdParams p) {
       lse = prow ? p.lse[1] : p.lse[0];
       lrows = prow ? p.lse_rows[1] : p.lse_rows[0];
     }
-    lse[(int64_t)(kvh * p.group + er.head) * lrows + t.q_row0 + er.row] = (m_run * c + __log2f(l_tot)) * kLn2;
+    lse[(int64_t)(kvh * p.group + er.head) * lrows + t.q_row0 + er.row] = (core.m_run * core.c + __log2f(l_tot)) * kLn2;
   }
   if (!rows.wave_any) return;
   // through this wavefront's own buffer (nothing is in flight any more)
   char* const buf = reinterpret_cast<char*>(wave == 0 ? k_buf0 : wave == 1 ? k_buf1 : wave == 2 ? v_buf0 : v_buf1);
   const float inv = 1.f / l_tot;
   if constexpr (OUT32)
-    store_pairs<D>(buf, oacc, inv, p.o32 + (part1 ? p.o32_part : 0) + qbase, qstride, t, p.group, p.group_magic, hh,
+    store_pairs<D>(buf, core.oacc, inv, p.o32 + (part1 ? p.o32_part : 0) + qbase, qstride, t, p.group, p.group_magic, hh,
                    wave, lane);
   else
-    store_pairs<D>(buf, oacc, inv, reinterpret_cast<__bf16*>(prow ? p.o[1] : p.o[0]) + qbase, qstride, t, p.group, p.group_magic, hh, wave,
+    store_pairs<D>(buf, core.oacc, inv, reinterpret_cast<__bf16*>(prow ? p.o[1] : p.o[0]) + qbase, qstride, t, p.group, p.group_magic, hh, wave,
                    lane);
 }
 

@@ -14,47 +14,12 @@
 #include <vector>
 
 #include "../../include/augtree.h"
+#include "host_checks.h"
 #include "internal.h"
 
 using namespace augtree;
 
 namespace {
-
-template <class... A>
-int fail(int status, const char* fmt, A... a) {
-  char buf[512];
-  std::snprintf(buf, sizeof(buf), fmt, a...);
-  return fail_status(status, buf);
-}
-
-int hip_ok(hipError_t e, const char* what) {
-  return e == hipSuccess ? AUGTREE_OK : fail(AUGTREE_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
-}
-
-// Calls the launch hook around one kernel launch.
-struct Hook {
-  const char* role;
-  hipStream_t stream;
-  Hook(const char* r, hipStream_t s) : role(r), stream(s) { launch_hook(role, 0, stream); }
-  ~Hook() { launch_hook(role, 1, stream); }
-};
-
-// No C++ exception crosses the ABI (the tables are vectors).
-template <class F>
-int guarded(F f) {
-  try {
-    return f();
-  } catch (const std::exception& e) {
-    return fail(AUGTREE_ERR_INVALID_ARGUMENT, "host allocation failed: %s", e.what());
-  }
-}
-
-int check_ptr(const void* p, const char* name, bool required, size_t align = 16) {
-  if (!p) return required ? fail(AUGTREE_ERR_INVALID_ARGUMENT, "null pointer: %s", name) : AUGTREE_OK;
-  if (reinterpret_cast<uintptr_t>(p) % align)
-    return fail(AUGTREE_ERR_MISALIGNED, "pointer %s is not %d-byte aligned", name, (int)align);
-  return AUGTREE_OK;
-}
 
 int check_heads(int hq, int hkv, int d, float scale, const float* decay) {
   if (hq < 1 || hkv < 1) return fail(AUGTREE_ERR_INVALID_ARGUMENT, "head counts must be >= 1");
@@ -96,8 +61,6 @@ int check_batch(const augtree_groups* g, const float* decay) {
   }
   return st ? st : check_heads(g->num_q_heads, g->num_kv_heads, g->head_dim, g->softmax_scale, decay);
 }
-
-int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // Rounds of `units` workgroups with at most `per_cu` on each of 256 CUs; w of them on a CU take sqrt(w) times
 // as long as one (measured: 1.42 for two, 2.0 for four).
@@ -146,8 +109,6 @@ struct Layout {
   int64_t blocks = 0, longest = 0;  // of the batch; of the tree with the most
   size_t states = 0, tree = 0;  // bytes: states of all blocks; one state per tree
 };
-
-size_t align_up(size_t n) { return (n + 255) / 256 * 256; }
 
 // (A launch has fewer than 2^32 threads: the state and the scan kernels' are the most.)
 int make_layout(const augtree_groups* g, Layout* L) {
@@ -281,50 +242,6 @@ struct Call {
     return AUGTREE_OK;
   }
 };
-
-int check_ws(const void* ws, size_t have, size_t need) {
-  if (!ws || have < need)
-    return fail(AUGTREE_ERR_WORKSPACE, "workspace of %zu bytes, %zu needed", ws ? have : (size_t)0, need);
-  return check_ptr(ws, "ws", true, 256);
-}
-
-struct Named {
-  const void* p;
-  const char* name;
-};
-
-int check_all(const Named* v, int n, bool required) {
-  for (int i = 0; i < n; ++i)
-    if (int st = check_ptr(v[i].p, v[i].name, required)) return st;
-  return AUGTREE_OK;
-}
-
-bool overlap(const void* a, size_t na, const void* b, size_t nb) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return a && b && na && nb && x < y + nb && y < x + na;
-}
-
-// A tensor of a call, for the check that outputs are apart from all else. An `in_place` output may be an `in_place`
-// input itself.
-struct Span {
-  const void* p;
-  size_t bytes;
-  const char* name;
-  bool in_place = false;
-};
-
-int check_apart(const Span* in, int n_in, const Span* out, int n_out) {
-  for (int i = 0; i < n_out; ++i) {
-    for (int j = 0; j < n_in; ++j)
-      if (overlap(out[i].p, out[i].bytes, in[j].p, in[j].bytes) &&
-          !(out[i].in_place && in[j].in_place && out[i].p == in[j].p))
-        return fail(AUGTREE_ERR_INVALID_ARGUMENT, "%s overlaps %s", out[i].name, in[j].name);
-    for (int j = 0; j < i; ++j)
-      if (overlap(out[i].p, out[i].bytes, out[j].p, out[j].bytes))
-        return fail(AUGTREE_ERR_INVALID_ARGUMENT, "%s overlaps %s", out[i].name, out[j].name);
-  }
-  return AUGTREE_OK;
-}
 
 // bytes of a batch's tensors: q and k rows of prompts and responses, states of trees and branches
 struct Sizes {

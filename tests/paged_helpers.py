@@ -1,0 +1,106 @@
+"""Steps, caches and error bounds of the paged KV cache's tests.
+
+Bounds (per element, from the kernels' roundings; a bf16 rounding is off by at most 2^-8 of the value):
+  o: 2^-8 |o| (its own rounding) + (2^-8 + 2^-13) sum_j p_j |v_j|: p is rounded to bf16 for the product with V; scores are
+     fp32 sums of d <= 128 products, off by 2^-17 of scale sum |q| |k| (under 100 here, but 2^-14 in p with the spread of
+     one row's), exp2 and the fp32 sums over up to a few thousand keys, in blocks of 64, add 2^-15, the merge 2^-20;
+  lse: 2^-17 of max_j scale sum |q| |k_j| (the scores), 2^-16 (row sum, exp2, log2) and 2^-21 |lse|.
+e4m3 values become bf16 exactly and the scales are applied in fp32, so the bounds are the same.
+"""
+import numpy as np
+import torch
+
+from oracle import paged as P
+from paper_2609_33133_amd import api
+
+FP8 = torch.float8_e4m3fn
+
+
+def random_tables(seqs, page, seed, extra=3):
+    """seqs: [(parent, cached, new)]; numpy tables whose pages lie in random order, in a ring that begins anywhere."""
+    rng = np.random.RandomState(seed)
+    parent, cached, new = (np.array(c, np.int64) for c in zip(*seqs))
+    n = np.maximum(new, 0)
+    have, want = -(-cached // page), -(-(cached + n) // page)
+    pages = int(want.sum()) + extra
+    ids = rng.permutation(pages).astype(np.int32)
+    table = rng.randint(-3, pages + 3, (len(seqs), int(want.max()) + 1)).astype(np.int32)
+    at = 0
+    for i, h in enumerate(have):
+        table[i, :h] = ids[at:at + h]
+        at += h
+    first, spare = int(rng.randint(pages)), pages - at
+    ring = rng.randint(-3, pages + 3, pages).astype(np.int32)
+    ring[(first + np.arange(spare)) % pages] = ids[at:]
+    return dict(table=table, length=cached, parent=parent, ring=ring, state=np.array([first, spare]), new=new)
+
+
+def gpu(a):
+    return torch.from_numpy(np.ascontiguousarray(a).astype(np.int32)).cuda()
+
+
+def to64(t):
+    return t.detach().double().cpu().numpy()
+
+
+class Step:
+    """A step on the GPU: tables, caches whose dead slots hold NaN, queries; and what the oracle says about it."""
+
+    def __init__(self, seqs, heads, page, seed=0, fp8=False, spare_rows=0, parents=True, joint=False, amp=1.0):
+        self.hq, self.hkv, self.d = heads
+        self.page, self.fp8 = page, fp8
+        self.t = t = random_tables(seqs, page, seed)
+        self.live = int(np.maximum(t["new"], 0).sum())
+        self.rows = self.live + spare_rows
+        self.pages = api.PageTable(gpu(t["table"]), gpu(t["length"]), gpu(t["parent"]) if parents else None,
+                                   gpu(t["ring"]), gpu(t["state"]), page)
+        self.want = P.plan(t["table"], t["length"], t["parent"], t["ring"], t["state"], t["new"], page, self.rows)
+        gen = torch.Generator().manual_seed(seed + 1)
+        num, shape = len(t["ring"]), (len(t["ring"]), self.hkv, page, self.d)
+        live = torch.zeros(num * page, dtype=torch.bool)
+        table, total = self.want[0], t["length"] + np.maximum(t["new"], 0)
+        for i, n in enumerate(total):
+            at = np.arange(n)
+            live[torch.from_numpy(table[i, at // page].astype(np.int64) * page + at % page)] = True
+        live = live.view(num, 1, page, 1)
+        self.scales = {}
+        for n in "kv":
+            x = (amp if n == "k" else 1.0) * torch.randn(shape, generator=gen)
+            if fp8:
+                s = 0.02 * (1 + torch.rand(self.hkv, generator=gen))
+                self.scales[n + "_scale"] = s.cuda()
+                x = (x / s[:, None, None]).clamp(-448, 448).to(FP8).view(torch.uint8)
+                x = torch.where(live, x, torch.tensor(0x7F, dtype=torch.uint8)).view(FP8)
+            else:
+                x = torch.where(live, x, torch.tensor(float("nan"))).to(torch.bfloat16)
+            setattr(self, n + "_cache", x.cuda())
+        if joint:  # both caches in one tensor, their pages side by side
+            both = torch.stack([self.k_cache.view(torch.uint8), self.v_cache.view(torch.uint8)], 1).contiguous()
+            self.k_cache, self.v_cache = (both[:, j].view(FP8 if fp8 else torch.bfloat16) for j in range(2))
+        self.q = torch.randn(self.rows, self.hq, self.d, generator=gen).to(torch.bfloat16).cuda()
+        self.q[self.live:] = float("nan")
+        self.new = gpu(t["new"])
+
+    def plan(self, **kw):
+        return api.page_plan(self.pages, self.new, self.rows, self.hq, self.hkv, **kw)
+
+    def attend(self, plan, **kw):
+        return api.paged_fwd(self.q, self.k_cache, self.v_cache, plan, want_lse=True, **self.scales, **kw)
+
+    def tokens(self, which, i):
+        x = to64(getattr(self, which + "_cache").float())
+        if self.fp8:
+            x = x * to64(self.scales[which + "_scale"])[:, None, None]
+        at = np.arange(self.t["length"][i] + max(0, self.t["new"][i]))
+        return x[self.want[0][i, at // self.page], :, at % self.page]
+
+    def check_attention(self, o, lse, scale=None):
+        scale = self.d ** -0.5 if scale is None else scale
+        ref, rlse, mag, size = P.attention(to64(self.q)[:self.live], lambda i: self.tokens("k", i),
+                                           lambda i: self.tokens("v", i), self.t["parent"], self.t["length"],
+                                           self.t["new"], scale, self.hq // self.hkv)
+        got, glse = to64(o)[:self.live], to64(lse)[:, :self.live]
+        err = abs(got - ref) - (2.0 ** -8 * abs(ref) + (2.0 ** -8 + 2.0 ** -13) * mag)
+        assert not np.isnan(got).any() and (err <= 0).all(), (np.isnan(got).sum(), err.max())
+        lerr = abs(glse - rlse) - (2.0 ** -17 * size + 2.0 ** -16 + 2.0 ** -21 * abs(rlse))
+        assert not np.isnan(glse).any() and (lerr <= 0).all(), (np.isnan(glse).sum(), lerr.max())
