@@ -99,7 +99,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(FwdParams p) {
   FwdCore<D> core;
   core.hf = hf;
   core.load_q(qsrc + qbase + qoff);
-  core.init(p.scale_log2, lane);
+  core.init(p.scale_log2, l32, lane);
   const int qpos_lo = t.b_qpos + rows.wlo;  // causal: the wavefront's first query position
 
   // a causal block whose keys all follow the wavefront's queries (and every
@@ -112,9 +112,9 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(FwdParams p) {
     const bool isB = b >= nA;
     const int kb0 = (isB ? b - nA : b) * BN;
     const int len = isB ? t.b_len : t.a_len;
-    const bool masked = (kb0 + BN > len) || (isB && (kb0 + BN - 1 > qpos_lo));
-    const int lim = min(len - 1, isB ? t.b_qpos + qi : len - 1) - kb0;  // last visible key of the block
-    core.step(masked, lim, s0, s1, kn, vl, n0, n1);
+    auto masked = [&] { return (kb0 + BN > len) || (isB && (kb0 + BN - 1 > qpos_lo)); };
+    auto limit = [&] { return min(len - 1, isB ? t.b_qpos + qi : len - 1) - kb0; };  // last visible key of the block
+    core.step(masked, limit, s0, s1, kn, vl, n0, n1);
   };
 
   // iteration b loads K(b + 2) over K(b) and V(b + 1) over V(b - 1)

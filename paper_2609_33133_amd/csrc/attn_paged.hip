@@ -213,7 +213,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedFwdParams p) {
     core.load_q(p.q + qbase + pair_offset<D>(rows.row, rows.head, p.s.hq));
     float scale = p.scale_log2;
     if constexpr (E4M3) scale *= p.k_scale[kvh];
-    core.init(scale, lane);
+    core.init(scale, l32, lane);
 
     const int qpos_lo = it.b_pos + rows.wlo;  // causal: the wavefront's first query position
     const int qi = rows.row;
@@ -225,9 +225,9 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedFwdParams p) {
       const bool isB = b >= nA;
       const int kb0 = (isB ? b - nA : b) * BN;
       const int len = isB ? it.b_len : it.a_len;
-      const bool masked = (kb0 + BN > len) || (isB && (kb0 + BN - 1 > qpos_lo));
-      const int lim = min(len - 1, isB ? it.b_pos + qi : len - 1) - kb0;  // last visible key of the block
-      core.step(masked, lim, s0, s1, kn, vl, n0, n1);
+      auto masked = [&] { return (kb0 + BN > len) || (isB && (kb0 + BN - 1 > qpos_lo)); };
+      auto limit = [&] { return min(len - 1, isB ? it.b_pos + qi : len - 1) - kb0; };  // last visible key of the block
+      core.step(masked, limit, s0, s1, kn, vl, n0, n1);
     };
 
     // iteration b loads K(b + 2) over K(b) and V(b + 1) over V(b - 1)
@@ -266,7 +266,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedFwdParams p) {
       }
     }
   } else {  // a part that ends before the tile's last row begins
-    core.init(p.scale_log2, lane);
+    core.init(p.scale_log2, l32, lane);
   }
 
   if (!rows.wave_any) return;

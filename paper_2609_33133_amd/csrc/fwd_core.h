@@ -44,7 +44,7 @@ struct FwdCore {
     for (int ks = 0; ks < D / 16; ++ks) qreg[ks] = as_bf16x8(ldg16(q + hf * 8 + ks * 16));
   }
 
-  __device__ __forceinline__ void init(float scale_log2, int lane) {
+  __device__ __forceinline__ void init(float scale_log2, int l32, int lane) {
     c = scale_log2;
     m_run = -INFINITY;
     l_run = 0.f;
@@ -52,7 +52,7 @@ struct FwdCore {
     for (int db = 0; db < D / 32; ++db)
 #pragma unroll
       for (int i = 0; i < 16; ++i) oacc[db][i] = 0.f;
-    k_off.init(lane & 31, hf);
+    k_off.init(l32, hf);
     vtr_off.init(0, lane);
   }
 
@@ -67,11 +67,13 @@ struct FwdCore {
     }
   }
 
-  // mask (keys behind `lim` of the block, where `masked`, which is uniform),
+  // mask (keys of the block behind limit(), where masked(), which is uniform),
   // running max and (when it grew) rescale for a block; returns the exponent
   // offset of the block
-  __device__ __forceinline__ float stats(bool masked, int lim, f32x16& s0, f32x16& s1) {
-    if (masked) {
+  template <class Masked, class Limit>
+  __device__ __forceinline__ float stats(Masked masked, Limit limit, f32x16& s0, f32x16& s1) {
+    if (masked()) {
+      const int lim = limit();
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         if (acc_row(i, hf) > lim) s0[i] = -INFINITY;
@@ -118,9 +120,10 @@ struct FwdCore {
   // of this one, so the matrix cores and the vector ALUs of the wavefront work
   // at the same time; then O += V^T P^T. On the last block the extra S is
   // computed from a stale buffer and never used.
-  __device__ __forceinline__ void step(bool masked, int lim, f32x16& s0, f32x16& s1, const __bf16* kn,
+  template <class Masked, class Limit>
+  __device__ __forceinline__ void step(Masked masked, Limit limit, f32x16& s0, f32x16& s1, const __bf16* kn,
                                        const __bf16* vl, f32x16& n0, f32x16& n1) {
-    const float ms = stats(masked, lim, s0, s1);
+    const float ms = stats(masked, limit, s0, s1);
     __builtin_amdgcn_sched_barrier(0);
     s_mfma(kn, n0, n1);
     float l4[4];  // four independent partial sums

@@ -141,6 +141,9 @@ int augtree_page_plan(const augtree_pages* pages, const int32_t* new_rows, int32
   PlanParams p;
   std::memset(&p, 0, sizeof(p));
   p.s = s;
+  p.L = plan_layout(s);
+  p.group = num_q_heads / num_kv_heads;
+  p.shift = paged_shift(s.page);
   p.table = pages->table;
   p.length = pages->length;
   p.parent = pages->parent;

@@ -52,7 +52,7 @@ enum : int32_t {
 // Header words.
 enum {
   PH_SEQS, PH_ROWS, PH_HQ, PH_HKV, PH_PAGE,  // what the plan was made for
-  PH_STATUS, PH_TOTAL_ROWS, PH_ITEMS, PH_MERGE_ROWS, PH_PART, PH_FIRST, PH_SPARE,
+  PH_STATUS, PH_TOTAL_ROWS, PH_ITEMS, PH_MERGE_ROWS, PH_MOST_PARTS, PH_PART, PH_FIRST, PH_SPARE, PH_NEED, PH_BACK, PH_FULL,
 };
 
 struct PagedShape {
@@ -69,17 +69,21 @@ inline __host__ __device__ int paged_shift(int page) {
 // Where a plan's arrays are (in words), and the most items and slots of partial
 // results it can have.
 struct PlanLayout {
-  // [seqs]: offsets of the rows (seqs + 1), tokens before and after, parent, first new page, first page given back,
-  // run (its first sequence, or -1), rows of the run that begins here, first row that is merged
-  int64_t cu, cached, total, parent, need, back, run, run_rows, merge0;
-  int64_t unit;  // [2 seqs][kUnitInts]: own unit, unit of the run that begins here
-  int64_t slots, positions, row_seq, merge_rows;  // [rows]
-  int64_t items;                                  // [max_items][kItemInts]
+  // [seqs]: first row (seqs + 1 of them), tokens before and after, parent and its tokens, pages taken and given back by
+  // the sequences before, run (its first sequence, or -1), rows of the run that begins here, rows merged before
+  int64_t cu, cached, total, parent, a_len, need, back, run, run_rows, merge0;
+  // [2 seqs], own unit and unit of the run that begins here: items with a part of C blocks before the unit's, items with
+  // a tile's last part before the unit's, first slot (-1: none), parts of a tile
+  int64_t full0, last0, slot0, parts;
+  int64_t slots, positions;  // [rows]
+  int64_t merge;             // [rows][kMergeInts]
+  int64_t items;             // [max_items][kItemInts]
   int64_t words;
   int32_t max_items, max_parts, max_slots;
 };
-// A unit: first item with a part of C blocks, first item with a tile's last part, first slot (-1: none), parts of a tile.
-constexpr int kUnitInts = 4;
+// A row that is merged: the row; then for its own unit and for its run's: slot of the row's first pair's group and that
+// pair's place in it (pairs count from there on), slots of a part, parts.
+constexpr int kMergeInts = 12;
 
 inline __host__ __device__ PlanLayout plan_layout(const PagedShape& s) {
   PlanLayout L;
@@ -94,16 +98,19 @@ inline __host__ __device__ PlanLayout plan_layout(const PagedShape& s) {
   L.cached = take(n);
   L.total = take(n);
   L.parent = take(n);
+  L.a_len = take(n);
   L.need = take(n);
   L.back = take(n);
   L.run = take(n);
   L.run_rows = take(n);
   L.merge0 = take(n);
-  L.unit = take(2 * n * kUnitInts);
+  L.full0 = take(2 * n);
+  L.last0 = take(2 * n);
+  L.slot0 = take(2 * n);
+  L.parts = take(2 * n);
   L.slots = take(r);
   L.positions = take(r);
-  L.row_seq = take(r);
-  L.merge_rows = take(r);
+  L.merge = take(r * kMergeInts);
   // Every sequence with rows has one tile that may not be full, every run (two sequences or more) one, and parts of
   // C >= all blocks / max_parts blocks are at most max_parts more items. Slots: one per 32 pairs of the units of runs
   // and of their sequences' own; a unit with parts has at most 2 blocks / C of them, of four slots each.
@@ -134,6 +141,7 @@ static_assert(sizeof(PagedItem) == 4 * kItemInts, "item layout");
 
 struct PlanParams {
   PagedShape s;
+  PlanLayout L;
   int32_t* table;          // [seqs][max_pages]
   const int32_t* length;   // [seqs]
   const int32_t* parent;   // [seqs] or nullptr
@@ -143,6 +151,7 @@ struct PlanParams {
   int32_t* length_out;
   int32_t* state_out;
   int32_t* plan;
+  int32_t group, shift;    // query heads of a KV head, log2 of the page size
 };
 
 // Blocks of the parts that units are cut into, from the blocks of all tiles
@@ -162,150 +171,178 @@ inline __host__ __device__ int part_blocks(int64_t blocks, int64_t tiles, const 
 // What a sequence's units are, from the plan's arrays.
 struct UnitView {
   const PlanParams& p;
-  const PlanLayout& L;
-  int g;
-  __host__ __device__ UnitView(const PlanParams& p_, const PlanLayout& L_) : p(p_), L(L_), g(p_.s.hq / p_.s.hkv) {}
-  __host__ __device__ int rows(int i) const { return p.plan[L.cu + i + 1] - p.plan[L.cu + i]; }
-  __host__ __device__ bool small(int i) const {
-    const int n = rows(i);
-    return n > 0 && p.plan[L.parent + i] >= 0 && (int64_t)n * g <= kSmallPairs;
-  }
-  // the sequence's rows meet its parent's tokens in the run's unit
+  __host__ __device__ explicit UnitView(const PlanParams& p_) : p(p_) {}
+  __host__ __device__ int at(int64_t array, int i) const { return p.plan[array + i]; }
+  __host__ __device__ int rows(int i) const { return at(p.L.cu, i + 1) - at(p.L.cu, i); }
+  // the sequence's rows meet its parent's tokens in the unit of a run
   __host__ __device__ bool in_run(int i) const {
-    const int r = p.plan[L.run + i];
-    return r >= 0 && p.plan[L.run_rows + r] > rows(r);
+    const int r = at(p.L.run, i);
+    return r >= 0 && at(p.L.run_rows, r) > rows(r);
   }
   // which: 0 the sequence's own unit, 1 the unit of the run that begins with it
   __host__ __device__ PagedItem unit(int i, int which) const {
     PagedItem u;
-    u.row0 = p.plan[L.cu + i];
+    u.row0 = at(p.L.cu, i);
     u.pair0 = 0;
     u.a_seq = u.b_seq = -1;
     u.a_len = u.b_len = u.b_pos = 0;
     u.blk0 = u.blk1 = 0;
     u.slot = -1;
-    const int par = p.plan[L.parent + i];
+    const int n = rows(i), r = at(p.L.run, i);
+    const bool run = n > 0 && in_run(i);
     if (which == 0) {
-      u.rows = rows(i);
+      u.rows = n;
       u.b_seq = i;
-      u.b_len = p.plan[L.total + i];
-      u.b_pos = p.plan[L.cached + i];
-      if (par >= 0 && u.rows > 0 && !in_run(i)) u.a_seq = par, u.a_len = p.plan[L.total + par];
+      u.b_len = at(p.L.total, i);
+      u.b_pos = at(p.L.cached, i);
+      if (n > 0 && !run) u.a_seq = at(p.L.parent, i), u.a_len = at(p.L.a_len, i);
     } else {
       u.rows = 0;  // (a parent without tokens: nothing to meet)
-      if (p.plan[L.run + i] == i && in_run(i) && p.plan[L.total + par] > 0)
-        u.rows = p.plan[L.run_rows + i], u.a_seq = par, u.a_len = p.plan[L.total + par];
+      if (run && r == i && at(p.L.a_len, i) > 0)
+        u.rows = at(p.L.run_rows, i), u.a_seq = at(p.L.parent, i), u.a_len = at(p.L.a_len, i);
     }
     return u;
   }
   __host__ __device__ static int blocks(const PagedItem& u) {
     return paged_div(u.a_len, kPagedBlock) + paged_div(u.b_len, kPagedBlock);
   }
-  __host__ __device__ int tiles(const PagedItem& u) const { return paged_div(u.rows * g, kTilePairs); }
-  __host__ __device__ bool partial(const PagedItem& u, int i, int which, int parts) const {
-    return parts > 1 || which == 1 || (u.rows > 0 && in_run(i));
-  }
+  __host__ __device__ int tiles(const PagedItem& u) const { return paged_div(u.rows * p.group, kTilePairs); }
 };
+
+// Sums of counts that stop at kMostCount, so that no sequence of bad lengths overflows them.
+constexpr int32_t kMostCount = 1 << 30;
+inline __host__ __device__ int32_t add_count(int32_t a, int32_t b) { return a + b < kMostCount ? a + b : kMostCount; }
 
 // The plan but for what plan_fill writes, by one team of threads: team.tid of
 // team.size, barriers, exclusive scans over the threads.
 template <class Team>
 __host__ __device__ void plan_scan(Team& team, const PlanParams& p) {
   const PagedShape& s = p.s;
-  const PlanLayout L = plan_layout(s);
+  const PlanLayout& L = p.L;
   int32_t* const plan = p.plan;
-  const int g = s.hq / s.hkv, page = s.page;
+  const int g = p.group, shift = p.shift, page = s.page;
   const int per = paged_div(s.seqs, team.size());
   const int i0 = per * team.tid() < s.seqs ? per * team.tid() : s.seqs;
   const int i1 = i0 + per < s.seqs ? i0 + per : s.seqs;
   const int first = p.state[0], spare = p.state[1];
-  const int64_t most = (int64_t)s.max_pages * page;
+  const int most = s.max_pages << shift;
+  auto pages = [&](int tokens) { return (tokens + page - 1) >> shift; };
+
+  // a sequence's step, its numbers brought into range; bits of what is wrong with it
+  struct One {
+    int len, n, need, back, parent, bad;
+    bool small;  // may be of a run
+  };
+  auto look = [&](int i) {
+    One o;
+    const int len = p.length[i], raw = p.fresh[i], par = p.parent ? p.parent[i] : -1;
+    o.bad = len < 0 || len > most ? PAGES_LENGTH : 0;
+    o.len = o.bad ? 0 : len;
+    o.n = raw <= 0 ? 0 : raw < s.rows + 1 ? raw : s.rows + 1;
+    if (raw > most - o.len) o.bad |= PAGES_LONG;
+    o.need = pages(o.len + o.n) - pages(o.len);
+    o.back = raw < 0 ? pages(o.len) : 0;
+    o.parent = par < 0 || o.n == 0 ? -1 : par;
+    o.small = o.parent >= 0 && (int64_t)o.n * g <= kSmallPairs;
+    return o;
+  };
+  // of the sequences with rows: the last one's number and, where it may be of a run, its parent, for a scan of maxima
+  auto key = [](int i, const One& o) { return (int64_t)(i + 1) << 32 | (uint32_t)(o.small ? o.parent + 1 : 0); };
+  auto is_small = [](int64_t k) { return k > 0 && (uint32_t)k != 0; };
 
   // rows, pages needed and given back; what is wrong
   int bad = first < 0 || first >= s.num_pages || spare < 0 || spare > s.num_pages ? PAGES_LENGTH : 0;
-  int64_t sums[3] = {0, 0, 0}, before[3], all[3];
+  int32_t sums[3] = {0, 0, 0}, before[3], all[3];
+  int64_t last = 0;
   for (int i = i0; i < i1; ++i) {
-    const int64_t len = p.length[i], raw = p.fresh[i], n = raw > 0 ? raw : 0;
-    int par = p.parent ? p.parent[i] : -1;
-    if (len < 0 || len > most) bad |= PAGES_LENGTH;
-    else if (len + n > most) bad |= PAGES_LONG;
-    int64_t total = len + n;
-    if (par >= 0 && n > 0) {
-      const bool ok = par < s.seqs && par != i && p.parent[par] < 0 && p.fresh[par] >= 0;
-      if (!ok) bad |= PAGES_PARENT;
+    const One o = look(i);
+    bad |= o.bad;
+    int a_len = 0;
+    if (o.parent >= 0) {
+      const int par = o.parent;
+      if (par < s.seqs && par != i && p.parent[par] < 0 && p.fresh[par] >= 0) {
+        const One q = look(par);
+        a_len = q.len + q.n;
+      } else {
+        bad |= PAGES_PARENT;
+      }
     }
-    plan[L.parent + i] = par < 0 || n == 0 ? -1 : par;
-    plan[L.cached + i] = (int32_t)len;
-    plan[L.total + i] = (int32_t)(total > INT32_MAX ? INT32_MAX : total);
-    sums[0] += n;
-    sums[1] += (total + page - 1) / page - (len + page - 1) / page;
-    sums[2] += raw < 0 && len > 0 ? (len + page - 1) / page : 0;
+    plan[L.cached + i] = o.len;
+    plan[L.total + i] = o.len + o.n;
+    plan[L.parent + i] = o.parent;
+    plan[L.a_len + i] = a_len;
+    sums[0] = add_count(sums[0], o.n);
+    sums[1] = add_count(sums[1], o.need);
+    sums[2] = add_count(sums[2], o.back);
+    if (o.n > 0) last = key(i, o);
   }
-  team.template scan<3>(sums, before, all);
+  int64_t prev = last;
+  team.scan_step(sums, before, all, prev, bad);  // prev: the last sequence with rows before i0
   if (all[0] > s.rows) bad |= PAGES_ROWS;
   if (all[1] > spare) bad |= PAGES_SHORT;
   if (all[2] > s.num_pages - spare) bad |= PAGES_LENGTH;
-  bad = team.any(bad);
+
+  // first row and pages of each sequence; runs: a small sequence begins one unless the nearest sequence with rows before
+  // it is small and of the same parent
+  int begin = -1;
+  int64_t q = prev;
   for (int i = i0; i < i1; ++i) {
-    const int64_t len = p.length[i], raw = p.fresh[i], n = bad ? 0 : raw > 0 ? raw : 0;
-    plan[L.cu + i] = bad ? 0 : (int32_t)before[0];
-    plan[L.need + i] = bad ? 0 : (int32_t)before[1];
-    plan[L.back + i] = bad ? -1 : (raw < 0 ? (int32_t)before[2] : -1);
-    before[0] += n;
-    before[1] += (len + n + page - 1) / page - (len + page - 1) / page;
-    before[2] += raw < 0 && len > 0 ? (len + page - 1) / page : 0;
+    const One o = look(i);
+    plan[L.cu + i] = bad ? 0 : before[0];
+    plan[L.need + i] = bad ? 0 : before[1];
+    plan[L.back + i] = bad ? 0 : before[2];
     plan[L.run + i] = plan[L.run_rows + i] = -1;
-    if (bad) plan[L.cached + i] = plan[L.total + i] = 0, plan[L.parent + i] = -1;
+    before[0] += o.n;
+    before[1] += o.need;
+    before[2] += o.back;
+    if (o.n > 0) {
+      const int64_t k = key(i, o);
+      if (o.small && (uint32_t)q != (uint32_t)k) begin = i;
+      q = k;
+    }
   }
   if (team.tid() == 0) {
-    plan[L.cu + s.seqs] = bad ? 0 : (int32_t)all[0];
-    plan[PH_SEQS] = s.seqs;
-    plan[PH_ROWS] = s.rows;
-    plan[PH_HQ] = s.hq;
-    plan[PH_HKV] = s.hkv;
-    plan[PH_PAGE] = page;
-    plan[PH_STATUS] = bad;
-    plan[PH_TOTAL_ROWS] = bad ? 0 : (int32_t)all[0];
+    const int rows = bad ? 0 : all[0];
+    const int32_t head[] = {s.seqs, s.rows, s.hq, s.hkv, page, bad, rows};
+    for (int k = 0; k < 7; ++k) plan[PH_SEQS + k] = head[k];
+    plan[L.cu + s.seqs] = rows;
     plan[PH_FIRST] = first;
     plan[PH_SPARE] = spare;
-  }
-  team.sync();  // (lengths and state may be written in place from here on)
-  for (int i = i0; i < i1; ++i)
-    p.length_out[i] = bad ? p.length[i] : p.fresh[i] < 0 ? 0 : plan[L.total + i];
-  if (team.tid() == 0) {
-    p.state_out[0] = bad ? first : (int32_t)((first + all[1]) % s.num_pages);
-    p.state_out[1] = bad ? spare : (int32_t)(spare - all[1] + all[2]);
-  }
-
-  // runs: a small sequence begins one unless the nearest sequence with rows before it is small and of the same parent
-  const UnitView view(p, L);
-  int last = -1;
-  for (int i = i0; i < i1; ++i)
-    if (view.rows(i) > 0) last = i;
-  int prev = team.scan_max(last);  // nearest sequence with rows before i0
-  int begin = -1, q = prev;
-  for (int i = i0; i < i1; ++i) {
-    if (view.rows(i) == 0) continue;
-    if (view.small(i) && !(q >= 0 && view.small(q) && plan[L.parent + q] == plan[L.parent + i])) begin = i;
-    q = i;
+    plan[PH_NEED] = bad ? 0 : all[1];
+    plan[PH_BACK] = bad ? 0 : all[2];
   }
   int start = team.scan_max(begin);  // the last run that begins before i0
-  q = prev;
-  for (int i = i0; i < i1; ++i) {
-    if (view.rows(i) == 0) continue;
-    const bool small = view.small(i), before_small = q >= 0 && view.small(q);
-    const bool joins = small && before_small && plan[L.parent + q] == plan[L.parent + i];
-    if (before_small && !joins) plan[L.run_rows + start] = plan[L.cu + i] - plan[L.cu + start];
-    if (small && !joins) start = i;
-    if (small) plan[L.run + i] = start;
-    q = i;
+  if (!bad) {
+    q = prev;
+    int row = i0 < i1 ? plan[L.cu + i0] : 0;
+    for (int i = i0; i < i1; ++i) {
+      const One o = look(i);
+      if (o.n > 0) {
+        const int64_t k = key(i, o);
+        const bool joins = o.small && (uint32_t)q == (uint32_t)k;
+        if (is_small(q) && !joins) plan[L.run_rows + start] = row - plan[L.cu + start];
+        if (o.small && !joins) start = i;
+        if (o.small) plan[L.run + i] = start;
+        q = k;
+        row += o.n;
+      }
+    }
+    // the run that no sequence with rows follows ends with the rows: the thread of the last sequence closes it
+    if (i1 == s.seqs && i0 < i1 && is_small(q)) plan[L.run_rows + start] = all[0] - plan[L.cu + start];
   }
-  // the run that no sequence with rows follows ends with the rows: the thread of the last sequence closes it
-  if (i1 == s.seqs && i0 < i1 && q >= 0 && view.small(q)) plan[L.run_rows + start] = plan[L.cu + s.seqs] - plan[L.cu + start];
-  team.sync();
+  team.sync();  // (nobody reads lengths and state from here on: they may be written in place)
+  for (int i = i0; i < i1; ++i)
+    if (!bad || p.length_out != p.length)
+      p.length_out[i] = bad ? p.length[i] : p.fresh[i] < 0 ? 0 : plan[L.total + i];
+  if (team.tid() == 0) {
+    int to = first + (bad ? 0 : all[1]);
+    p.state_out[0] = to >= s.num_pages && !bad ? to - s.num_pages : to;
+    p.state_out[1] = bad ? spare : spare - all[1] + all[2];
+  }
 
   // blocks of all tiles, and from them the length of a part
-  int64_t w[2] = {0, 0}, w_before[2], w_all[2];
+  const UnitView view(p);
+  int64_t w[2] = {0, 0};
   for (int i = i0; i < i1; ++i)
     for (int which = 0; which < 2; ++which) {
       const PagedItem u = view.unit(i, which);
@@ -313,118 +350,133 @@ __host__ __device__ void plan_scan(Team& team, const PlanParams& p) {
       w[0] += (int64_t)tiles * view.blocks(u);
       w[1] += tiles;
     }
-  team.template scan<2>(w, w_before, w_all);
-  const int part = part_blocks(w_all[0], w_all[1], s, L.max_parts);
+  team.sum(w);
+  const int part = part_blocks(w[0], w[1], s, L.max_parts);
 
   // items: the parts of full length first, then the tiles' last ones; slots of partial results; merged rows
-  int64_t c[4] = {0, 0, 0, 0}, at[4], sum[4];
+  int32_t c[4] = {0, 0, 0, 0}, at[4], sum[4], most_parts = 0;
   for (int pass = 0; pass < 2; ++pass) {
+    int32_t* const n = pass ? at : c;
     for (int i = i0; i < i1; ++i) {
-      bool merged = false;
       for (int which = 0; which < 2; ++which) {
         const PagedItem u = view.unit(i, which);
         const int tiles = view.tiles(u), parts = tiles ? paged_div(view.blocks(u), part) : 0;
-        const bool partial = tiles && view.partial(u, i, which, parts);
-        int32_t* const to = plan + L.unit + (2 * (int64_t)i + which) * kUnitInts;
+        const bool partial = tiles && (parts > 1 || which == 1 || view.in_run(i));
         if (pass) {
-          to[0] = (int32_t)at[0];
-          to[1] = (int32_t)(sum[0] + at[1]);
-          to[2] = partial ? (int32_t)at[2] : -1;
-          to[3] = parts;
-          if (which == 0) plan[L.merge0 + i] = partial ? (int32_t)at[3] : -1;
+          const int64_t k = 2 * (int64_t)i + which;
+          plan[L.full0 + k] = n[0];
+          plan[L.last0 + k] = n[1];
+          plan[L.slot0 + k] = partial ? n[2] : -1;
+          plan[L.parts + k] = parts;
+          if (which == 0) plan[L.merge0 + i] = partial ? n[3] : -1;
         }
-        int64_t* const n = pass ? at : c;
-        if (tiles) n[0] += (int64_t)tiles * (parts - 1), n[1] += tiles;
-        if (partial) n[2] += (int64_t)parts * paged_div(u.rows * g, kSlotPairs);
-        if (which == 0) merged = partial;
+        if (tiles) n[0] += tiles * (parts - 1), n[1] += tiles;
+        if (partial) n[2] += parts * paged_div(u.rows * g, kSlotPairs);
+        if (partial && which == 0) n[3] += u.rows;
+        if (partial && parts > most_parts) most_parts = parts;
       }
-      if (merged) (pass ? at : c)[3] += view.rows(i);
     }
-    if (!pass) team.template scan<4>(c, at, sum);
+    if (!pass) team.scan(c, at, sum);
   }
+  most_parts = team.max_of(most_parts);
   if (team.tid() == 0) {
     plan[PH_PART] = part;
-    plan[PH_ITEMS] = (int32_t)(sum[0] + sum[1]);
-    plan[PH_MERGE_ROWS] = (int32_t)sum[3];
+    plan[PH_FULL] = sum[0];
+    plan[PH_ITEMS] = sum[0] + sum[1];
+    plan[PH_MERGE_ROWS] = sum[3];
+    plan[PH_MOST_PARTS] = most_parts;
   }
   team.sync();
 }
 
-// The rest of the plan, by `size` threads in wavefronts of `lanes` that need
-// not know of one another.
-template <class Team>
-__host__ __device__ void plan_fill(Team& team, const PlanParams& p, int64_t tid, int64_t size, int lanes) {
-  const PagedShape& s = p.s;
-  const PlanLayout L = plan_layout(s);
-  int32_t* const plan = p.plan;
-  const UnitView view(p, L);
-  const int g = s.hq / s.hkv, page = s.page, shift = paged_shift(page);
-  const int first = plan[PH_FIRST], spare = plan[PH_SPARE], part = plan[PH_PART], rows = plan[PH_TOTAL_ROWS];
-  auto ring = [&](int64_t k) { return (int)(k % s.num_pages); };
+// The last of a[0 .. n - 1], which do not decrease, that is at most x (a[0] is).
+inline __host__ __device__ int last_at_most(const int32_t* a, int n, int x) {
+  int lo = 0, hi = n - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (a[mid] <= x) lo = mid;
+    else hi = mid - 1;
+  }
+  return lo;
+}
 
-  // rows: sequence, slot, position; the list of rows to merge
-  for (int64_t r = tid; r < s.rows; r += size) {
-    int seq = -1, slot = -1, pos = -1;
+// The rest of the plan, by `size` threads that need not know of one another:
+// rows, pages and items, each found among its sequences by bisection.
+template <class Team>
+__host__ __device__ void plan_fill(Team& team, const PlanParams& p, int tid, int size) {
+  const PagedShape& s = p.s;
+  const PlanLayout& L = p.L;
+  int32_t* const plan = p.plan;
+  const UnitView view(p);
+  const int g = p.group, page = s.page, shift = p.shift;
+  const int first = plan[PH_FIRST], spare = plan[PH_SPARE], part = plan[PH_PART], rows = plan[PH_TOTAL_ROWS];
+  const int need = plan[PH_NEED], back = plan[PH_BACK], full = plan[PH_FULL], items = plan[PH_ITEMS];
+  auto ring = [&](int k) { return k < s.num_pages ? k : k - s.num_pages; };
+
+  // rows: slot, position, where the merge finds its parts
+  for (int r = tid; r < s.rows; r += size) {
+    int slot = -1, pos = -1;
     if (r < rows) {
-      int lo = 0, hi = s.seqs - 1;  // the last sequence that begins at or before r: the one with rows
-      while (lo < hi) {
-        const int mid = (lo + hi + 1) / 2;
-        if (plan[L.cu + mid] <= r) lo = mid;
-        else hi = mid - 1;
-      }
-      seq = lo;
-      const int off = (int)r - plan[L.cu + seq], cached = plan[L.cached + seq], at = cached + off;
+      const int seq = last_at_most(plan + L.cu, s.seqs, r);
+      const int off = r - plan[L.cu + seq], cached = plan[L.cached + seq], at = cached + off;
       const int have = (cached + page - 1) >> shift, k = at >> shift;
-      const int id = k < have ? p.table[(int64_t)seq * s.max_pages + k]
-                              : p.free_pages[ring((int64_t)first + plan[L.need + seq] + k - have)];
+      const int id = k < have ? p.table[(int64_t)seq * s.max_pages + k] : p.free_pages[ring(first + plan[L.need + seq] + k - have)];
       if (id >= 0 && id < s.num_pages) slot = (id << shift) + (at & (page - 1));
       else team.flag(plan + PH_STATUS, PAGES_PAGE);
-      const int par = plan[L.parent + seq];
-      pos = at + (par >= 0 ? plan[L.total + par] : 0);
+      pos = at + plan[L.a_len + seq];
       const int m = plan[L.merge0 + seq];
-      if (m >= 0) plan[L.merge_rows + m + off] = (int)r;
+      if (m >= 0) {
+        int32_t* const dst = plan + L.merge + (int64_t)(m + off) * kMergeInts;
+        dst[0] = r;
+        for (int u = 0; u < 2; ++u) {
+          const int q = u == 0 ? seq : plan[L.run + seq];
+          const int slot0 = q < 0 ? -1 : plan[L.slot0 + 2 * (int64_t)q + u];
+          const int row0 = q < 0 ? 0 : plan[L.cu + q];
+          const int pair = (r - row0) * g;
+          dst[1 + 4 * u] = slot0 + pair / kSlotPairs;
+          dst[2 + 4 * u] = pair % kSlotPairs;
+          dst[3 + 4 * u] = slot0 < 0 ? 0 : paged_div((u == 0 ? view.rows(q) : plan[L.run_rows + q]) * g, kSlotPairs);
+          dst[4 + 4 * u] = slot0 < 0 ? 0 : plan[L.parts + 2 * (int64_t)q + u];
+        }
+      }
     }
     plan[L.slots + r] = slot;
     plan[L.positions + r] = pos;
-    plan[L.row_seq + r] = seq;
   }
 
-  // sequences, a wavefront each: new pages into the table, ended ones' back to the ring, items
-  const int lane = (int)(tid % lanes);
-  for (int64_t i = tid / lanes; i < s.seqs; i += size / lanes) {
-    const int cached = plan[L.cached + i], have = (cached + page - 1) >> shift;
-    int32_t* const row = p.table + i * s.max_pages;
-    if (view.rows((int)i) > 0) {
-      const int want = (plan[L.total + i] + page - 1) >> shift, need = plan[L.need + i];
-      for (int k = have + lane; k < want; k += lanes) row[k] = p.free_pages[ring((int64_t)first + need + k - have)];
+  // new pages into the table, ended sequences' back to the ring
+  for (int k = tid; k < need; k += size) {
+    const int i = last_at_most(plan + L.need, s.seqs, k);
+    const int have = (plan[L.cached + i] + page - 1) >> shift;
+    p.table[(int64_t)i * s.max_pages + have + k - plan[L.need + i]] = p.free_pages[ring(first + k)];
+  }
+  for (int k = tid; k < back; k += size) {
+    const int i = last_at_most(plan + L.back, s.seqs, k);
+    p.free_pages[ring(ring(first + spare) + k)] = p.table[(int64_t)i * s.max_pages + k - plan[L.back + i]];
+  }
+
+  for (int x = tid; x < items; x += size) {
+    const bool whole = x < full;  // a part of `part` blocks, not a tile's last
+    const int k = whole ? x : x - full;
+    const int unit = last_at_most(plan + (whole ? L.full0 : L.last0), 2 * s.seqs, k);
+    PagedItem it = view.unit(unit >> 1, unit & 1);
+    const int parts = plan[L.parts + unit], slot0 = plan[L.slot0 + unit];
+    const int of_tile = whole ? parts - 1 : 1, j = k - plan[(whole ? L.full0 : L.last0) + unit];
+    // a causal unit's last tiles have the most blocks: they come first
+    const int t = view.tiles(it) - 1 - j / of_tile, c = whole ? j % of_tile : parts - 1;
+    it.pair0 = t * kTilePairs;
+    int end = view.blocks(it);
+    if (it.b_len > 0) {  // up to what the tile's last row sees
+      const int pairs = it.rows * g, lastpair = it.pair0 + kTilePairs - 1 < pairs - 1 ? it.pair0 + kTilePairs - 1 : pairs - 1;
+      end = paged_div(it.a_len, kPagedBlock) + (it.b_pos + lastpair / g) / kPagedBlock + 1;
     }
-    const int back = plan[L.back + i];
-    if (back >= 0)
-      for (int k = lane; k < have; k += lanes) p.free_pages[ring((int64_t)first + spare + back + k)] = row[k];
-    for (int which = 0; which < 2; ++which) {
-      const int32_t* const at = plan + L.unit + (2 * i + which) * kUnitInts;
-      const PagedItem u = view.unit((int)i, which);
-      const int tiles = view.tiles(u), parts = at[3], slots = paged_div(u.rows * g, kSlotPairs);
-      for (int k = lane; k < tiles * parts; k += lanes) {
-        // a causal unit's last tiles have the most blocks: they come first
-        const int t = tiles - 1 - k / parts, c = k % parts;
-        PagedItem it = u;
-        it.pair0 = t * kTilePairs;
-        int end = view.blocks(u);
-        if (u.b_len > 0) {  // up to what the tile's last row sees
-          const int pairs = u.rows * g, lastpair = it.pair0 + kTilePairs - 1 < pairs - 1 ? it.pair0 + kTilePairs - 1 : pairs - 1;
-          end = paged_div(u.a_len, kPagedBlock) + (u.b_pos + lastpair / g) / kPagedBlock + 1;
-        }
-        it.blk0 = (int)((int64_t)c * part < end ? (int64_t)c * part : end);
-        it.blk1 = (int)((int64_t)(c + 1) * part < end ? (int64_t)(c + 1) * part : end);
-        if (at[2] >= 0) it.slot = at[2] + c * slots + t * (kTilePairs / kSlotPairs);
-        const int to = c < parts - 1 ? at[0] + (k / parts) * (parts - 1) + c : at[1] + k / parts;
-        int32_t* const dst = plan + L.items + (int64_t)to * kItemInts;
-        const int32_t w[kItemInts] = {it.row0, it.rows, it.pair0, it.a_seq, it.a_len, it.b_seq, it.b_len, it.b_pos,
-                                      it.blk0, it.blk1, it.slot, 0, 0, 0, 0, 0};
-        for (int j = 0; j < kItemInts; ++j) dst[j] = w[j];
-      }
-    }
+    it.blk0 = (int)((int64_t)c * part < end ? (int64_t)c * part : end);
+    it.blk1 = (int)((int64_t)(c + 1) * part < end ? (int64_t)(c + 1) * part : end);
+    if (slot0 >= 0) it.slot = slot0 + c * paged_div(it.rows * g, kSlotPairs) + t * (kTilePairs / kSlotPairs);
+    int32_t* const dst = plan + L.items + (int64_t)x * kItemInts;
+    const int32_t w[kItemInts] = {it.row0, it.rows, it.pair0, it.a_seq, it.a_len, it.b_seq, it.b_len, it.b_pos,
+                                  it.blk0, it.blk1, it.slot, 0, 0, 0, 0, 0};
+    for (int y = 0; y < kItemInts; ++y) dst[y] = w[y];
   }
 }
 

@@ -7,69 +7,123 @@ namespace augtree {
 namespace {
 
 constexpr int kPlanThreads = 1024;
+constexpr int kMergeAlone = 16;  // parts of a row up to which one group of lanes joins them
 
-// The threads of one workgroup, for plan_scan.
+// The threads of one workgroup, for plan_scan. Each reduction puts one value
+// per wavefront into LDS of its own turn's half, so that two barriers apart no
+// wavefront still reads what the next turn writes.
 struct GroupTeam {
-  int64_t* sums;   // [wavefronts][4] of LDS
-  int* maxs;       // [wavefronts]
+  struct Wave {
+    int64_t key;
+    int32_t v[4], bits;
+  };
+  Wave (*lds)[kPlanThreads / 64];  // [2]
+  int turn = 0;
   __device__ int tid() const { return threadIdx.x; }
-  __device__ int size() const { return blockDim.x; }
+  __device__ int size() const { return kPlanThreads; }
   __device__ void sync() const { __syncthreads(); }
-  __device__ int any(int bits) const {
-    int r = 0;
-#pragma unroll
-    for (int b = 0; b < 6; ++b)
-      if (__syncthreads_or(bits & (1 << b))) r |= 1 << b;
-    return r;
-  }
   __device__ void flag(int32_t* to, int32_t bits) const { atomicOr(to, bits); }
+  __device__ Wave* next() { return lds[turn ^= 1]; }
+
+  template <int K>
+  __device__ static void wave_scan(int32_t (&x)[K]) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        const int32_t y = __shfl_up(x[k], d);
+        if (lane >= d) x[k] = add_count(x[k], y);
+      }
+    }
+  }
   // sums over the threads before this one, and over all
   template <int K>
-  __device__ void scan(const int64_t (&v)[K], int64_t (&before)[K], int64_t (&all)[K]) const {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-    int64_t x[K];
+  __device__ void scan(const int32_t (&v)[K], int32_t (&before)[K], int32_t (&all)[K]) {
+    int64_t none = 0;
+    int bits = 0;
+    scan_step(v, before, all, none, bits);
+  }
+  // the same, the largest key of the threads before this one (0 at least), and the bits of all
+  template <int K>
+  __device__ void scan_step(const int32_t (&v)[K], int32_t (&before)[K], int32_t (&all)[K], int64_t& key, int& bits) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    Wave* const to = next();
+    int32_t x[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) x[k] = v[k];
+    wave_scan(x);
+    int64_t m = key;
+#pragma unroll
     for (int d = 1; d < 64; d *= 2) {
-#pragma unroll
-      for (int k = 0; k < K; ++k) {
-        const int64_t y = __shfl_up((long long)x[k], d);
-        if (lane >= d) x[k] += y;
-      }
+      const int64_t y = __shfl_up((long long)m, d);
+      if (lane >= d && y > m) m = y;
     }
-    __syncthreads();  // the last scan's sums have been read
-    if (lane == 63)
 #pragma unroll
-      for (int k = 0; k < K; ++k) sums[wave * 4 + k] = x[k];
+    for (int b = 1; b <= PAGES_PAGE; b *= 2)
+      if (__any(bits & b)) bits |= b;
+    if (lane == 63) {
+#pragma unroll
+      for (int k = 0; k < K; ++k) to[wave].v[k] = x[k];
+      to[wave].key = m;
+      to[wave].bits = bits;
+    }
     __syncthreads();
+    const int64_t up = __shfl_up((long long)m, 1);
+    key = lane == 0 ? 0 : up;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      before[k] = x[k] - v[k];
+      before[k] = x[k] - v[k];  // (exact where the sum has not stopped: a step whose sums stop is refused)
       all[k] = 0;
     }
-    for (int w = 0; w < waves; ++w)
+    for (int w = 0; w < kPlanThreads / 64; ++w) {
 #pragma unroll
       for (int k = 0; k < K; ++k) {
-        const int64_t y = sums[w * 4 + k];
-        if (w < wave) before[k] += y;
-        all[k] += y;
+        const int32_t y = to[w].v[k];
+        if (w < wave) before[k] = add_count(before[k], y);
+        all[k] = add_count(all[k], y);
       }
+      if (w < wave && to[w].key > key) key = to[w].key;
+      bits |= to[w].bits;
+    }
   }
   // the largest value of the threads before this one, -1 at least
-  __device__ int scan_max(int v) const {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int x = v;
-    for (int d = 1; d < 64; d *= 2) {
-      const int y = __shfl_up(x, d);
-      if (lane >= d) x = max(x, y);
+  __device__ int scan_max(int v) {
+    const int32_t none[1] = {0};
+    int32_t a[1], b[1];
+    int64_t key = v + 1;
+    int bits = 0;
+    scan_step(none, a, b, key, bits);
+    return (int)key - 1;
+  }
+  __device__ void sum(int64_t (&v)[2]) {
+    Wave* const to = next();
+#pragma unroll
+    for (int d = 32; d > 0; d /= 2) {
+      v[0] += __shfl_xor((long long)v[0], d);
+      v[1] += __shfl_xor((long long)v[1], d);
+    }
+    if ((threadIdx.x & 63) == 0) {
+      to[threadIdx.x >> 6].key = v[0];
+      __builtin_memcpy(to[threadIdx.x >> 6].v, &v[1], 8);
     }
     __syncthreads();
-    if (lane == 63) maxs[wave] = x;
+    v[0] = v[1] = 0;
+    for (int w = 0; w < kPlanThreads / 64; ++w) {
+      int64_t y;
+      __builtin_memcpy(&y, to[w].v, 8);
+      v[0] += to[w].key;
+      v[1] += y;
+    }
+  }
+  __device__ int max_of(int v) {
+    Wave* const to = next();
+#pragma unroll
+    for (int d = 32; d > 0; d /= 2) v = max(v, __shfl_xor(v, d));
+    if ((threadIdx.x & 63) == 0) to[threadIdx.x >> 6].v[0] = v;
     __syncthreads();
-    int r = __shfl_up(x, 1);
-    if (lane == 0) r = -1;
-    for (int w = 0; w < wave; ++w) r = max(r, maxs[w]);
-    return r;
+    for (int w = 0; w < kPlanThreads / 64; ++w) v = max(v, to[w].v[0]);
+    return v;
   }
 };
 
@@ -78,16 +132,15 @@ struct GroupTeam {
 // trips between them.
 template <bool FILL>
 __global__ __launch_bounds__(kPlanThreads) void page_plan_kernel(PlanParams p) {
-  __shared__ int64_t sums[kPlanThreads / 64 * 4];
-  __shared__ int maxs[kPlanThreads / 64];
-  GroupTeam team{sums, maxs};
+  __shared__ GroupTeam::Wave lds[2][kPlanThreads / 64];
+  GroupTeam team{lds};
   plan_scan(team, p);
-  if constexpr (FILL) plan_fill(team, p, threadIdx.x, kPlanThreads, 64);
+  if constexpr (FILL) plan_fill(team, p, threadIdx.x, kPlanThreads);
 }
 
 __global__ __launch_bounds__(256) void page_fill_kernel(PlanParams p) {
-  GroupTeam team{nullptr, nullptr};
-  plan_fill(team, p, (int64_t)blockIdx.x * 256 + threadIdx.x, (int64_t)gridDim.x * 256, 64);
+  GroupTeam team{nullptr};
+  plan_fill(team, p, blockIdx.x * 256 + threadIdx.x, gridDim.x * 256);
 }
 
 __device__ __forceinline__ bool plan_is_for(const int32_t* plan, const PagedShape& s) {
@@ -138,52 +191,84 @@ __global__ __launch_bounds__(256) void cache_write_kernel(CacheWriteParams p, Pl
 
 // Joins the partial results of a row: o = sum_p w_p o_p / sum_p w_p, w_p =
 // exp(lse_p - max lse), lse = max + log sum_p w_p, over the parts of its
-// sequence's own unit and of its run's. D / 4 lanes take a (row, head) pair.
+// sequence's own unit and of its run's. D / 4 lanes take a (row, head) pair and,
+// of its parts, every `share`-th: one group of lanes all of them where the plan
+// has few parts a row, else the workgroup's groups together.
 template <int D>
-__global__ __launch_bounds__(256) void paged_merge_kernel(PagedFwdParams p, PlanLayout L) {
-  constexpr int LANES = D / 4;
-  if (!plan_is_for(p.plan, p.s)) return;
+__global__ __launch_bounds__(256) void paged_merge_kernel(PagedFwdParams p, int64_t merge_at) {
+  constexpr int LANES = D / 4, GROUPS = 256 / LANES;
+  __shared__ f32x4 part_acc[GROUPS][LANES];
+  __shared__ float part_top[GROUPS], part_sum[GROUPS];
   const int32_t* const plan = p.plan;
+  if (!plan_is_for(plan, p.s)) return;
   const int64_t pairs = (int64_t)plan[PH_MERGE_ROWS] * p.s.hq;
-  const int lane = threadIdx.x % LANES, g = p.group;
-  for (int64_t i = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES; i < pairs;
-       i += (int64_t)gridDim.x * (256 / LANES)) {
-    const int64_t m = i / p.s.hq;
-    const int head = (int)(i - m * p.s.hq), kvh = head / g;
-    const int row = plan[L.merge_rows + m], seq = plan[L.row_seq + row], run = plan[L.run + seq];
-    // the two units: first slot of the pair's group of 32, slots of a part, parts
-    int64_t slot[2] = {0, 0};
-    int step[2] = {0, 0}, parts[2] = {0, 0}, at[2] = {0, 0};
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int s = u == 0 ? seq : run;
-      if (s < 0) continue;
-      const int32_t* const unit = plan + L.unit + (2 * (int64_t)s + u) * kUnitInts;
-      const int row0 = plan[L.cu + s], rows = u == 0 ? plan[L.cu + s + 1] - row0 : plan[L.run_rows + s];
-      const int pair = (row - row0) * g + head % g;
-      if (unit[2] < 0) continue;
-      step[u] = paged_div(rows * g, kSlotPairs);
-      slot[u] = unit[2] + pair / kSlotPairs;
-      at[u] = pair % kSlotPairs;
-      parts[u] = unit[3];
-    }
-    float top = -INFINITY;
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-      for (int k = 0; k < parts[u]; ++k)
-        top = fmaxf(top, p.part_lse[((slot[u] + (int64_t)k * step[u]) * p.s.hkv + kvh) * kSlotPairs + at[u]]);
+  const int lane = threadIdx.x % LANES, grp = threadIdx.x / LANES, g = p.group;
+  const int share = plan[PH_MOST_PARTS] > kMergeAlone ? GROUPS : 1;
+  const int per = GROUPS / share, mine = share > 1 ? 0 : grp, phase = share > 1 ? grp : 0;
+  for (int64_t i0 = (int64_t)blockIdx.x * per; i0 < pairs; i0 += (int64_t)gridDim.x * per) {
+    const int64_t i = i0 + mine;
+    const bool any = i < pairs;
+    const int64_t m = any ? i / p.s.hq : 0;
+    const int head = any ? (int)(i - m * p.s.hq) : 0, kvh = head / g;
+    const int32_t* const d = plan + merge_at + m * kMergeInts;
+    const int row = d[0];
+    float top = -INFINITY, sum = 0.f;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    float sum = 0.f;
+    if (any)
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
-      for (int k = 0; k < parts[u]; ++k) {
-        const int64_t at32 = ((slot[u] + (int64_t)k * step[u]) * p.s.hkv + kvh) * kSlotPairs + at[u];
-        const float l = p.part_lse[at32];
-        if (l == -INFINITY) continue;  // a part that the row sees nothing of
-        const float w = __expf(l - top);
-        acc += *reinterpret_cast<const f32x4*>(p.part_o + at32 * D + lane * 4) * w;
-        sum += w;
+      for (int u = 0; u < 2; ++u) {
+        const int pair = d[2 + 4 * u] + head - kvh * g, parts = d[4 + 4 * u];
+        // the pair's place in slots of 32 pairs, per KV head; from part to part
+        const int64_t first = ((int64_t)(d[1 + 4 * u] + pair / kSlotPairs) * p.s.hkv + kvh) * kSlotPairs + pair % kSlotPairs;
+        const int64_t step = (int64_t)d[3 + 4 * u] * p.s.hkv * kSlotPairs;
+        // four parts at a time, so that their loads are on their way together
+        for (int k = phase; k < parts; k += 4 * share) {
+          float l[4];
+          f32x4 o[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int kk = k + j * share;
+            const int64_t at = first + (kk < parts ? kk : k) * step;
+            l[j] = p.part_lse[at];
+            o[j] = *reinterpret_cast<const f32x4*>(p.part_o + at * D + lane * 4);
+            if (kk >= parts) l[j] = -INFINITY;
+          }
+          const float t = fmaxf(fmaxf(fmaxf(l[0], l[1]), fmaxf(l[2], l[3])), top);
+          if (t == -INFINITY) continue;  // parts that the row sees nothing of
+          const float back = __expf(top - t);
+          acc = acc * back;
+          sum *= back;
+          top = t;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float w = __expf(l[j] - t);
+            acc += o[j] * w;
+            sum += w;
+          }
+        }
       }
+    if (share > 1) {
+      part_acc[grp][lane] = acc;
+      if (lane == 0) {
+        part_top[grp] = top;
+        part_sum[grp] = sum;
+      }
+      __syncthreads();
+      if (grp == 0) {
+        for (int k = 1; k < GROUPS; ++k) top = fmaxf(top, part_top[k]);
+        const float w0 = __expf(part_top[0] - top);
+        acc = acc * w0;
+        sum *= w0;
+        for (int k = 1; k < GROUPS; ++k) {
+          const float w = __expf(part_top[k] - top);
+          acc += part_acc[k][lane] * w;
+          sum += part_sum[k] * w;
+        }
+      }
+      __syncthreads();
+      if (grp != 0) continue;
+    }
+    if (!any) continue;
     const float inv = 1.f / sum;
     typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
     bf16x4 y;
@@ -203,9 +288,8 @@ hipError_t launch_page_plan(const PlanParams& p, bool apart, hipStream_t stream)
   }
   page_plan_kernel<false><<<1, kPlanThreads, 0, stream>>>(p);
   if (hipError_t e = hipGetLastError()) return e;
-  const int64_t rows = (p.s.rows + 255) / 256, seqs = ((int64_t)p.s.seqs + 3) / 4;
-  const int64_t want = rows > seqs ? rows : seqs;
-  page_fill_kernel<<<(unsigned)(want < 1024 ? want : 1024), 256, 0, stream>>>(p);
+  const int most = p.s.rows > p.L.max_items ? p.s.rows : p.L.max_items;
+  page_fill_kernel<<<most < 1024 * 256 ? (most + 255) / 256 : 1024, 256, 0, stream>>>(p);
   return hipGetLastError();
 }
 
@@ -219,12 +303,10 @@ hipError_t launch_cache_write(const CacheWriteParams& p, hipStream_t stream) {
 }
 
 hipError_t launch_paged_merge(const PagedFwdParams& p, hipStream_t stream) {
-  const PlanLayout L = plan_layout(p.s);
-  const int64_t pairs = (int64_t)p.s.rows * p.s.hq, per = 256 / (p.d / 4);
-  const int64_t want = (pairs + per - 1) / per;
-  const unsigned grid = (unsigned)(want < 2048 ? want : 2048);
-  if (p.d == 128) paged_merge_kernel<128><<<grid, 256, 0, stream>>>(p, L);
-  else paged_merge_kernel<64><<<grid, 256, 0, stream>>>(p, L);
+  const int64_t merge_at = plan_layout(p.s).merge, pairs = (int64_t)p.s.rows * p.s.hq;
+  const unsigned grid = (unsigned)(pairs < 2048 ? pairs : 2048);
+  if (p.d == 128) paged_merge_kernel<128><<<grid, 256, 0, stream>>>(p, merge_at);
+  else paged_merge_kernel<64><<<grid, 256, 0, stream>>>(p, merge_at);
   return hipGetLastError();
 }
 

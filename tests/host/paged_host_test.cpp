@@ -41,13 +41,15 @@ void check(bool ok, const char* what) {
 }
 
 struct Shared {
-  explicit Shared(int n_) : n(n_), sums(n_), maxs(n_), bits(n_) {}
+  explicit Shared(int n_) : n(n_), sums(n_), wide(n_), keys(n_), bits(n_) {}
   const int n;
   std::mutex m;
   std::condition_variable cv;
   int waiting = 0, turn = 0;
-  std::vector<std::vector<int64_t>> sums;
-  std::vector<int> maxs, bits;
+  std::vector<std::vector<int32_t>> sums;
+  std::vector<std::vector<int64_t>> wide;
+  std::vector<int64_t> keys;
+  std::vector<int> bits;
   void barrier() {
     std::unique_lock<std::mutex> l(m);
     const int t = turn;
@@ -67,38 +69,57 @@ struct ThreadTeam {
   int tid() const { return id; }
   int size() const { return s.n; }
   void sync() const { s.barrier(); }
-  int any(int b) const {
-    s.bits[id] = b;
-    s.barrier();
-    int r = 0;
-    for (int x : s.bits) r |= x;
-    s.barrier();
-    return r;
-  }
   void flag(int32_t* to, int32_t b) const {
     std::lock_guard<std::mutex> l(g_lock);
     *to |= b;
   }
   template <int K>
-  void scan(const int64_t (&v)[K], int64_t (&before)[K], int64_t (&all)[K]) const {
+  void scan(const int32_t (&v)[K], int32_t (&before)[K], int32_t (&all)[K]) const {
+    int64_t key = 0;
+    int b = 0;
+    scan_step(v, before, all, key, b);
+  }
+  template <int K>
+  void scan_step(const int32_t (&v)[K], int32_t (&before)[K], int32_t (&all)[K], int64_t& key, int& bits) const {
     s.sums[id].assign(v, v + K);
+    s.keys[id] = key;
+    s.bits[id] = bits;
     s.barrier();
+    key = 0;
+    for (int t = 0; t < s.n; ++t) {
+      if (t < id) key = std::max(key, s.keys[t]);
+      bits |= s.bits[t];
+    }
     for (int k = 0; k < K; ++k) {
       before[k] = all[k] = 0;
       for (int t = 0; t < s.n; ++t) {
-        if (t < id) before[k] += s.sums[t][k];
-        all[k] += s.sums[t][k];
+        if (t < id) before[k] = add_count(before[k], s.sums[t][k]);
+        all[k] = add_count(all[k], s.sums[t][k]);
       }
     }
     s.barrier();
   }
   int scan_max(int v) const {
-    s.maxs[id] = v;
+    const int32_t none[1] = {0};
+    int32_t a[1], b[1];
+    int64_t key = v + 1;
+    int bits = 0;
+    scan_step(none, a, b, key, bits);
+    return (int)key - 1;
+  }
+  void sum(int64_t (&v)[2]) const {
+    s.wide[id].assign(v, v + 2);
     s.barrier();
-    int r = -1;
-    for (int t = 0; t < id; ++t) r = s.maxs[t] > r ? s.maxs[t] : r;
+    v[0] = v[1] = 0;
+    for (auto& w : s.wide) v[0] += w[0], v[1] += w[1];
     s.barrier();
-    return r;
+  }
+  int max_of(int v) const {
+    s.keys[id] = v;
+    s.barrier();
+    for (int64_t k : s.keys) v = std::max(v, (int)k);
+    s.barrier();
+    return v;
   }
 };
 
@@ -120,6 +141,9 @@ Result run(const Step& st, int threads, bool in_place) {
   PlanParams p;
   std::memset(&p, 0, sizeof(p));
   p.s = st.s;
+  p.L = L;
+  p.group = st.s.hq / st.s.hkv;
+  p.shift = paged_shift(st.s.page);
   p.table = r.table.data();
   p.length = in_place ? r.length.data() : length.data();
   p.parent = st.parents ? st.parent.data() : nullptr;
@@ -137,11 +161,10 @@ Result run(const Step& st, int threads, bool in_place) {
       plan_scan(team, p);
     });
   for (auto& t : pool) t.join();
-  // the rest by threads one after the other, in wavefronts of three
-  const int size = 3 * (1 + threads % 4);
-  for (int t = 0; t < size; ++t) {
+  // the rest by threads one after the other
+  for (int t = threads; t-- > 0;) {
     ThreadTeam team{sh, 0};
-    plan_fill(team, p, t, size, 3);
+    plan_fill(team, p, t, threads);
   }
   return r;
 }
@@ -175,7 +198,6 @@ void check_good(const Step& st, const Result& r, const char* label) {
       check(plan[L.slots + row] == table[(int64_t)i * s.max_pages + at / s.page] * s.page + at % s.page, "slot");
       const int par = st.parents ? st.parent[i] : -1;
       check(plan[L.positions + row] == at + (par >= 0 ? st.length[par] + (st.fresh[par] > 0 ? st.fresh[par] : 0) : 0), "position");
-      check(plan[L.row_seq + row] == i, "row's sequence");
       seq_of.push_back(i);
       pos_of.push_back(at);
       ++row;
@@ -199,6 +221,7 @@ void check_good(const Step& st, const Result& r, const char* label) {
   // (pair, segment, block) -> times met; pair -> items, slots
   std::map<std::pair<int, std::pair<int, int>>, int> met;
   std::map<int, std::vector<int>> slots_of;
+  std::map<int, int> place[2];  // pair in the sequence's own unit, in the run's
   std::map<int, int> direct;
   std::vector<char> used(L.max_slots, 0);
   for (int k = 0; k < items; ++k) {
@@ -224,6 +247,7 @@ void check_good(const Step& st, const Result& r, const char* label) {
           if (slot < L.max_slots) used[slot] = 1;
         }
         slots_of[id].push_back(slot);
+        place[it.b_seq < 0][id] = x;
       } else {
         ++direct[id];
       }
@@ -247,32 +271,33 @@ void check_good(const Step& st, const Result& r, const char* label) {
     }
   }
   check((int64_t)met.size() == pairs_seen, "nothing else is met");
-  // the merge's view (launch_paged_merge): the rows it lists, and the slots it finds for them
+  // the merge's view: the rows it lists, and the slots it finds for them
   std::vector<char> merged(row, 0);
+  size_t most = 0;
   check(plan[PH_MERGE_ROWS] <= s.rows, "merged rows");
   for (int m = 0; m < plan[PH_MERGE_ROWS]; ++m) {
-    const int rr = plan[L.merge_rows + m];
+    const int32_t* d = plan + L.merge + (int64_t)m * kMergeInts;
+    const int rr = d[0];
     const bool fine = rr >= 0 && rr < row;
     check(fine && !merged[rr], "merged rows");
     if (!fine) continue;
     merged[rr] = 1;
-    const int seq = plan[L.row_seq + rr], run = plan[L.run + seq];
     for (int h = 0; h < g; ++h) {
       std::vector<int> want = slots_of[rr * g + h], got;
       for (int u = 0; u < 2; ++u) {
-        const int q = u ? run : seq;
-        if (q < 0) continue;
-        const int32_t* unit = plan + L.unit + (2 * (int64_t)q + u) * kUnitInts;
-        const int row0 = plan[L.cu + q], rows = u ? plan[L.run_rows + q] : plan[L.cu + q + 1] - row0;
-        if (unit[2] < 0) continue;
-        const int pair = (rr - row0) * g + h;
-        for (int k = 0; k < unit[3]; ++k) got.push_back(unit[2] + k * cdiv(rows * g, kSlotPairs) + pair / kSlotPairs);
+        const int pair = d[2 + 4 * u] + h;
+        for (int k = 0; k < d[4 + 4 * u]; ++k) got.push_back(d[1 + 4 * u] + pair / kSlotPairs + k * d[3 + 4 * u]);
+        most = std::max(most, (size_t)d[4 + 4 * u]);
       }
       std::sort(want.begin(), want.end());
       std::sort(got.begin(), got.end());
       check(want == got, "the merge finds the parts");
+      // and in them the pair's place
+      for (int u = 0; u < 2; ++u)
+        if (d[4 + 4 * u] > 0) check((d[2 + 4 * u] + h) % kSlotPairs == place[u][rr * g + h] % kSlotPairs, "place in a slot");
     }
   }
+  check((int)most == plan[PH_MOST_PARTS], "most parts");
   for (int rr = 0; rr < row; ++rr) check(merged[rr] == (direct[rr * g] ? 0 : 1), "rows to merge");
 }
 
@@ -353,6 +378,7 @@ hipError_t launched(const char* what) {
 namespace augtree {
 
 hipError_t launch_page_plan(const PlanParams& p, bool apart, hipStream_t) {
+  check(p.L.words == plan_layout(p.s).words && p.group * p.s.hkv == p.s.hq && 1 << p.shift == p.s.page, "layout");
   check(apart == (p.s.rows > 2048 || p.s.seqs > 1024), "one launch or two");
   return launched("plan");
 }
@@ -443,7 +469,7 @@ int main() {
     const PlanLayout L = plan_layout(st.s);
     bool any = false;
     for (int j = 0; j < w.plan[PH_TOTAL_ROWS]; ++j) {
-      const int seq = w.plan[L.row_seq + j], pos = st.length[seq] + j - w.plan[L.cu + seq];
+      const int seq = last_at_most(w.plan.data() + L.cu, st.s.seqs, j), pos = st.length[seq] + j - w.plan[L.cu + seq];
       const bool fresh_page = pos / st.s.page >= cdiv(st.length[seq], st.s.page);
       check(fresh_page ? w.plan[L.slots + j] == -1 : w.plan[L.slots + j] >= 0, "slots outside the pool");
       any = any || fresh_page;
