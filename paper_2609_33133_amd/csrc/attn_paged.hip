@@ -10,9 +10,13 @@
 // rows behind a segment's last token are zeros by the copies' range check, so
 // what stands there is never read.
 //
-// e4m3 caches: the copies bring the bytes into a staging area, each lane then
-// turns its own 16 into bf16 (exactly) and puts them into the tile. The scales
-// of K and V multiply the softmax scale and the result.
+// e4m3 caches: the bytes of the rows that a copy instruction brings land in the
+// upper half of where these rows stand in the bf16 tile; once there, the
+// wavefront that fetched them reads them and writes the rows as bf16 (exactly)
+// over both halves. The scales of K and V multiply the softmax scale and the
+// result.
+#include <type_traits>
+
 #include "common.h"
 #include "fwd_core.h"
 #include "paged.h"
@@ -25,6 +29,21 @@ constexpr int BN = kFwdBlockN;
 static_assert(BN == kPagedBlock && kTilePairs == kPairsPerWorkgroup, "the plan's items are cut to the kernel's tiles");
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+
+// Eight e4m3 values as bf16, exactly.
+__device__ __forceinline__ bf16x8 widen8(int lo, int hi) {
+  bf16x8 y;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(k ? hi : lo, 1.f, false);
+    const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(k ? hi : lo, 1.f, true);
+    y[4 * k] = a[0];
+    y[4 * k + 1] = a[1];
+    y[4 * k + 2] = b[0];
+    y[4 * k + 3] = b[1];
+  }
+  return y;
+}
 
 // A position in a sequence's keys: the next block that is copied.
 struct PageCursor {
@@ -61,7 +80,7 @@ struct PageCopy {
 #pragma unroll
     for (int k = 0; k < PER_WAVE; ++k) {
       const int r = (wave + 4 * k) * RPI + lane / CH;
-      // bf16: straight into the swizzled tile (TileCopy); e4m3: as it lies
+      // bf16: straight into the swizzled tile (TileCopy); e4m3: as it lies, for widen()
       voff[k] = r * ROWB + ((E4M3 ? lane % CH : (lane % CH) ^ swz<D>(r)) << 4);
     }
   }
@@ -71,7 +90,10 @@ struct PageCopy {
     c.ids = c.win + lane < max_pages ? c.row[c.win + lane] : -1;
   }
 
-  __device__ __forceinline__ PageCursor at(const PagedItem& it, int nA) const {
+  // where the bytes of the wavefront's k-th copy instruction land in a tile
+  __device__ __forceinline__ int at(int k) const { return (wave + 4 * k) * (E4M3 ? 2048 : 1024) + (E4M3 ? 1024 : 0); }
+
+  __device__ __forceinline__ PageCursor begin(const PagedItem& it, int nA) const {
     PageCursor c;
     c.isB = it.blk0 >= nA;
     c.row = table + (int64_t)(c.isB ? b_seq : it.a_seq) * max_pages;
@@ -89,12 +111,12 @@ struct PageCopy {
       const int id = __builtin_amdgcn_readlane(c.ids, (c.key >> shift) - c.win);
       const bool ok = (uint32_t)id < (uint32_t)num_pages;
       const char* const base = cache + (ok ? id : 0) * stride + head_off + (c.key & (page - 1)) * ROWB;
-      const int n = ok ? min(BN, c.len - c.key) * ROWB : 0;
+      const int n = __builtin_amdgcn_readfirstlane(ok ? min(BN, c.len - c.key) * ROWB : 0);
       const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, n, 0x00020000);
 #pragma unroll
       for (int k = 0; k < PER_WAVE; ++k)
         __builtin_amdgcn_raw_ptr_buffer_load_lds(
-            rsrc, (__attribute__((address_space(3))) void*)(lds + (wave + 4 * k) * 1024), 16, voff[k], 0, 0, 0);
+            rsrc, (__attribute__((address_space(3))) void*)(lds + at(k)), 16, voff[k], 0, 0, 0);
     } else {
 #pragma unroll
       for (int k = 0; k < PER_WAVE; ++k) {
@@ -103,10 +125,10 @@ struct PageCopy {
         const bool ok = (uint32_t)id < (uint32_t)num_pages;
         // the address that the block's first row would have in this page; only the instruction's rows are read
         const char* const base = cache + (ok ? id : 0) * stride + head_off + ((key & (page - 1)) - r0) * ROWB;
-        const int n = ok && c.len > key ? (r0 + min(RPI, c.len - key)) * ROWB : 0;
+        const int n = __builtin_amdgcn_readfirstlane(ok && c.len > key ? (r0 + min(RPI, c.len - key)) * ROWB : 0);
         const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, n, 0x00020000);
         __builtin_amdgcn_raw_ptr_buffer_load_lds(
-            rsrc, (__attribute__((address_space(3))) void*)(lds + (wave + 4 * k) * 1024), 16, voff[k], 0, 0, 0);
+            rsrc, (__attribute__((address_space(3))) void*)(lds + at(k)), 16, voff[k], 0, 0, 0);
       }
     }
 #endif
@@ -122,38 +144,360 @@ struct PageCopy {
     }
   }
 
-  // e4m3: this wavefront's staged rows as bf16 into the swizzled tile
-  __device__ __forceinline__ void widen(const char* staged, __bf16* tile) const {
+  // e4m3: the rows that this wavefront's copies have brought, as bf16 into the swizzled tile
+  __device__ __forceinline__ void widen(__bf16* tile) const {
     if constexpr (E4M3) {
       constexpr int CH = ROWB / 16;
+      raw16 x[PER_WAVE];
+#pragma unroll
+      for (int k = 0; k < PER_WAVE; ++k)
+        x[k] = *reinterpret_cast<const raw16*>(reinterpret_cast<const char*>(tile) + at(k) + lane * 16);
+      wave_lds_fence();  // the rows are read before any is written
 #pragma unroll
       for (int k = 0; k < PER_WAVE; ++k) {
-        const raw16 x = *reinterpret_cast<const raw16*>(staged + (wave + 4 * k) * 1024 + lane * 16);
         const int r = (wave + 4 * k) * RPI + lane / CH, col = (lane % CH) * 16;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          bf16x8 y;
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[2 * h + j], 1.f, false);
-            const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[2 * h + j], 1.f, true);
-            y[4 * j] = a[0];
-            y[4 * j + 1] = a[1];
-            y[4 * j + 2] = b[0];
-            y[4 * j + 3] = b[1];
-          }
-          *reinterpret_cast<bf16x8*>(tile + toff<D>(r, col + 8 * h)) = y;
-        }
+        for (int h = 0; h < 2; ++h)
+          *reinterpret_cast<bf16x8*>(tile + toff<D>(r, col + 8 * h)) = widen8(x[k][2 * h], x[k][2 * h + 1]);
       }
     }
   }
 };
 
+// ---------------------------------------------------------------------------- items of few pairs
+
+// An item of at most 32 pairs (single tokens: a few heads of one row, or of the
+// rows of a run) is bound by the reading of its keys, so its wavefronts share
+// them instead of the pairs: each takes every fourth block of KEYS keys, 8 KB of
+// K and of V, for all pairs, on its own and without barriers. K of its next
+// block is fetched as soon as the scores of this one are formed, V as soon as
+// they are applied, so that one of the two is always on its way: with two
+// workgroups on a CU at least 64 KB. The page ids of the block after the next
+// one are read a step ahead. The wavefronts' states are joined in LDS at the
+// end.
+//
+// Tiles: per wavefront 4 KB in each of the kernel's four arrays (in arrays of
+// their own K and V can be told apart by the compiler, which would otherwise
+// wait for the one on its way before it reads the other): bf16, d = 128: 64
+// columns each; else half of the keys each. bf16 tiles are [32][64], swizzled
+// as such. e4m3 tiles stay bytes: their operands become bf16 (exactly) as they
+// are read, V^T with the 8-bit transpose read (inside a 16-lane group, lane j
+// addresses 8 bytes of row j / 2 and receives one column of the 8 rows).
+template <int D, bool E4M3>
+struct FewTiles {
+  static constexpr int ROWB = E4M3 ? D : 2 * D;        // bytes of a row in the cache
+  static constexpr int KEYS = 8192 / ROWB;             // keys of a block
+  static constexpr bool BY_COLS = !E4M3 && D == 128;   // the halves of a tile: columns, or keys
+  static constexpr int RB = BY_COLS ? ROWB / 2 : ROWB; // bytes of a row of a half
+  static constexpr int RPI = 1024 / RB;                // rows of one copy instruction
+  static constexpr int GROUPS = KEYS / RPI;            // groups of keys that are looked up on their own
+  static constexpr int SUB = KEYS / 32;                // 32-key tiles
+  static_assert(GROUPS <= 8 && RPI <= 16, "a copy instruction stays inside a page");
+
+  int voff[2];     // this lane's byte offset from an instruction's first row, even and odd instructions
+  int koff[8];     // K operand of 16 columns (bytes inside a half)
+  int voff_tr[4][2];  // V^T operand of 32 columns
+
+  __device__ static __forceinline__ int swz8(int row) { return RB == 128 ? (row >> 1) & 7 : (row >> 2) & 3; }
+
+  __device__ __forceinline__ void init(int lane) {
+    const int l32 = lane & 31, hf = lane >> 5, grp = lane >> 4, j = lane & 15;
+    constexpr int CH = RB / 16;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int r = lane / CH, row = k * RPI + r;
+      voff[k] = r * ROWB + (((lane % CH) ^ (E4M3 ? swz8(row) : swz<64>(row))) << 4);
+    }
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks) {
+      if constexpr (!E4M3) koff[ks] = ks < 4 ? 2 * toff<64>(l32, ks * 16 + hf * 8) : 0;
+      else koff[ks] = ks < D / 16 ? l32 * RB + ((ks ^ swz8(l32)) << 4) + 8 * hf : 0;
+    }
+    if constexpr (!E4M3) {
+      TrOffsets<64> t;
+      t.init(0, lane);
+#pragma unroll
+      for (int db = 0; db < 2; ++db) voff_tr[db][0] = t.o[db][0], voff_tr[db][1] = t.o[db][1];
+    } else {
+      const int r8 = j >> 1, row = 4 * (grp >> 1) + (r8 & 3) + 8 * (r8 >> 2);
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db)
+        voff_tr[db][0] = row * RB + (((2 * db + (grp & 1)) ^ swz8(row)) << 4) + 8 * (j & 1);
+    }
+  }
+
+  // K rows 32 t + l32, columns 16 ks + 8 hf .. +7; h0, h1: the tile's halves
+  __device__ __forceinline__ bf16x8 k_operand(const char* h0, const char* h1, int t, int ks) const {
+    if constexpr (!E4M3) {
+      const bool second = BY_COLS ? ks >= 4 : t >= 1;
+      return *reinterpret_cast<const bf16x8*>((second ? h1 : h0) + koff[BY_COLS ? ks % 4 : ks]);
+    } else {
+      const int row0 = RB == 128 ? 0 : (t & 1) * 32;
+      const int2 x = *reinterpret_cast<const int2*>(((RB == 128 ? t : t >> 1) ? h1 : h0) + row0 * RB + koff[ks]);
+      return widen8(x.x, x.y);
+    }
+  }
+  // V^T: columns 32 db + l32, keys 32 t + 16 m + the ones that accumulator registers 8 m .. 8 m + 7 hold
+  __device__ __forceinline__ bf16x8 v_operand(const char* h0, const char* h1, int t, int m, int db) const {
+    if constexpr (!E4M3) {
+      const bool second = BY_COLS ? db >= 2 : t >= 1;
+      const char* const at = (second ? h1 : h0) + m * 16 * 128;
+      const int k = BY_COLS ? db % 2 : db;
+      const s16x4 a = lds_tr16(reinterpret_cast<const __bf16*>(at + voff_tr[k][0]));
+      const s16x4 b = lds_tr16(reinterpret_cast<const __bf16*>(at + voff_tr[k][1]));
+      bf16x8 r;
+      __builtin_memcpy(&r, &a, 8);
+      __builtin_memcpy(reinterpret_cast<char*>(&r) + 8, &b, 8);
+      return r;
+    } else {
+      typedef int v2i __attribute__((ext_vector_type(2)));
+      const int row0 = (RB == 128 ? 0 : (t & 1) * 32) + 16 * m;
+      const char* const at = ((RB == 128 ? t : t >> 1) ? h1 : h0) + row0 * RB + voff_tr[db][0];
+      const v2i x = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) v2i*)(at));
+      return widen8(x[0], x[1]);
+    }
+  }
+
+  // copies keys key .. key + KEYS - 1 (those from `lim` on: zeros); ids: lane g has the page of key + g * RPI
+  __device__ __forceinline__ void copy(char* h0, char* h1, const char* cache, int64_t stride, int head_off, int ids, int key,
+                                       int lim, int shift, int num_pages) const {
+#if defined(__HIP_DEVICE_COMPILE__)
+#pragma unroll
+    for (int gr = 0; gr < GROUPS; ++gr) {
+      const int id = __builtin_amdgcn_readlane(ids, gr), k = key + gr * RPI;
+      const bool ok = (uint32_t)id < (uint32_t)num_pages;
+      const char* const base = cache + (ok ? id : 0) * stride + (head_off + (k & ((1 << shift) - 1)) * ROWB);
+      // (readfirstlane: clamped on the vector ALU, the range would make the compiler loop over the lanes)
+      const int n = __builtin_amdgcn_readfirstlane(ok ? max(0, min(RPI, lim - k)) * ROWB : 0);
+      const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, n, 0x00020000);
+      if constexpr (BY_COLS) {
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)(h0 + gr * 1024), 16,
+                                                 voff[gr & 1], 0, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)(h1 + gr * 1024), 16,
+                                                 voff[gr & 1] + RB, 0, 0, 0);
+      } else {
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(
+            rsrc, (__attribute__((address_space(3))) void*)((gr < GROUPS / 2 ? h0 : h1) + (gr % (GROUPS / 2)) * 1024), 16,
+            voff[gr & 1], 0, 0, 0);
+      }
+    }
+#endif
+  }
+};
+
+// s_waitcnt vmcnt(N): all but the last N vector-memory accesses of this wavefront have completed
+template <int N>
+__device__ __forceinline__ void wait_vmem_but() {
+  __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | ((N >> 4) << 14));
+}
+// what this wavefront read from LDS has arrived: a copy may overwrite it
+__device__ __forceinline__ void wait_lds() {
+  wave_lds_fence();
+  __builtin_amdgcn_s_waitcnt(0xC07F);
+  wave_lds_fence();
+}
+
+template <int D, bool E4M3>
+__device__ __forceinline__ void attend_few(const PagedFwdParams& p, const PagedItem& it, int kvh, __bf16* k0, __bf16* k1,
+                                           __bf16* v0, __bf16* v1, float (*stat)[4][kSlotPairs]) {
+  typedef FewTiles<D, E4M3> Tiles;
+  constexpr int KEYS = Tiles::KEYS, SUB = Tiles::SUB;
+  const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hf = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int g = p.group, pairs = it.rows * g, shift = __builtin_ctz(p.s.page);
+  const int64_t qbase = ((int64_t)it.row0 * p.s.hq + kvh * g) * D;
+  // this wavefront's 4 KB of each array
+  char* const ka = reinterpret_cast<char*>(k0) + wave * 4096;
+  char* const kb = reinterpret_cast<char*>(k1) + wave * 4096;
+  char* const va = reinterpret_cast<char*>(v0) + wave * 4096;
+  char* const vb = reinterpret_cast<char*>(v1) + wave * 4096;
+  // keys of the item: a0 .. a1 - 1 of segment A, b0 .. b1 - 1 of segment B
+  const int nA64 = (it.a_len + BN - 1) / BN;
+  const int a0 = min(it.blk0, nA64) * BN, a1 = min(min(it.blk1, nA64) * BN, it.a_len);
+  const int b0 = max(it.blk0 - nA64, 0) * BN, b1 = min(max(it.blk1 - nA64, 0) * BN, it.b_len);
+  const int nA = max(0, a1 - a0 + KEYS - 1) / KEYS, n = nA + max(0, b1 - b0 + KEYS - 1) / KEYS;
+  const int32_t* const row_a = p.table + (int64_t)max(it.a_seq, 0) * p.s.max_pages;
+  const int32_t* const row_b = p.table + (int64_t)max(it.b_seq, 0) * p.s.max_pages;
+  auto first_key = [&](int j) { return j < nA ? a0 + j * KEYS : b0 + (j - nA) * KEYS; };
+  auto last_key = [&](int j) { return j < nA ? a1 : b1; };
+  // (behind the last block: entries that nobody uses, so that the count of loads on their way stays the same)
+  auto page_ids = [&](int j) {
+    const int k = first_key(min(j, n - 1)) + (lane & 7) * Tiles::RPI;
+    return (j < nA ? row_a : row_b)[min(k >> shift, p.s.max_pages - 1)];
+  };
+  const char* const kc = static_cast<const char*>(p.k_cache);
+  const char* const vc = static_cast<const char*>(p.v_cache);
+  const int head_off = kvh * (p.s.page * Tiles::ROWB);
+
+  Tiles tiles;
+  tiles.init(lane);
+  int j = wave;
+  int ids = 0, ids_next = 0;
+  if (j < n) {
+    ids = page_ids(j);
+    ids_next = page_ids(j + 4);
+    tiles.copy(ka, kb, kc, p.k_stride, head_off, ids, first_key(j), last_key(j), shift, p.s.num_pages);
+    tiles.copy(va, vb, vc, p.v_stride, head_off, ids, first_key(j), last_key(j), shift, p.s.num_pages);
+  }
+  const int pair = min(l32, pairs - 1), qrow = fast_div(pair, g, p.group_magic);
+  bf16x8 qreg[D / 16];
+  {
+    const uint16_t* const q = p.q + qbase + pair_offset<D>(qrow, pair - qrow * g, p.s.hq) + hf * 8;
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) qreg[ks] = as_bf16x8(ldg16(q + ks * 16));
+  }
+  float c = p.scale_log2;
+  if constexpr (E4M3) c *= p.k_scale[kvh];
+  float m_run = -INFINITY, l_run = 0.f;
+  f32x16 oacc[D / 32];
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) oacc[db][i] = 0.f;
+
+  wait_vmem();  // (before the steps: the compiler would wait for Q in every one)
+  // One block; MORE: another one of this wavefront follows, whose copies go out.
+  auto step = [&](auto more) {
+    constexpr bool MORE = decltype(more)::value;
+    const int key = first_key(j), lim = last_key(j);
+    const bool isB = j >= nA;
+    wait_vmem_but<8>();  // all but V of this block
+    wave_lds_fence();
+    f32x16 s[SUB];
+#pragma unroll
+    for (int t = 0; t < SUB; ++t) {
+      f32x16 s1;  // two chains of MFMAs
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[t][i] = s1[i] = 0.f;
+#pragma unroll
+      for (int ks = 0; ks < D / 16; ks += 2) {
+        s[t] = mfma32(tiles.k_operand(ka, kb, t, ks), qreg[ks], s[t]);
+        s1 = mfma32(tiles.k_operand(ka, kb, t, ks + 1), qreg[ks + 1], s1);
+      }
+      if constexpr (!E4M3) pace_lds_mfma<D / 16, 1, 4>();
+      s[t] += s1;
+      __builtin_amdgcn_sched_barrier(0);  // (the operands of one tile at a time: two workgroups a CU)
+    }
+    wait_lds();
+    const int ids_now = ids_next;
+    if constexpr (MORE) {
+      ids_next = page_ids(j + 8);
+      tiles.copy(ka, kb, kc, p.k_stride, head_off, ids_now, first_key(j + 4), last_key(j + 4), shift, p.s.num_pages);
+    }
+    if (key + KEYS > lim || (isB && key + KEYS - 1 > it.b_pos)) {
+      const int seen = min(lim - 1, isB ? it.b_pos + qrow : lim - 1) - key;  // last visible key of the block
+#pragma unroll
+      for (int t = 0; t < SUB; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (32 * t + acc_row(i, hf) > seen) s[t][i] = -INFINITY;
+    }
+    float mx = s[0][0];
+#pragma unroll
+    for (int t = 0; t < SUB; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[t][i]);
+    mx = pair_max(mx);
+    if (__any(mx * c > m_run * c + RESCALE_MARGIN_LOG2)) {
+      const float mnew = fmaxf(m_run, mx);
+      const float alpha = (mnew == -INFINITY) ? 1.f : __builtin_amdgcn_exp2f((m_run - mnew) * c);
+      l_run *= alpha;
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) oacc[db][i] *= alpha;
+      m_run = mnew;
+    }
+    const float ms = (m_run == -INFINITY) ? 0.f : m_run * c;
+    bf16x8 pb[SUB][2];
+#pragma unroll
+    for (int t = 0; t < SUB; ++t) {
+      float l4[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        s[t][i] = __builtin_amdgcn_exp2f(s[t][i] * c - ms);
+        l4[i & 3] += s[t][i];
+      }
+      l_run += (l4[0] + l4[1]) + (l4[2] + l4[3]);
+      pb[t][0] = to_bf16x8(s[t], 0);
+      pb[t][1] = to_bf16x8(s[t], 8);
+    }
+    __builtin_amdgcn_sched_barrier(0);  // (the softmax runs while V is on its way)
+    if constexpr (MORE) wait_vmem_but<9>();  // all but K of the next block and the page ids after it
+    else wait_vmem();
+    wave_lds_fence();
+#pragma unroll
+    for (int t = 0; t < SUB; ++t) {
+#pragma unroll
+      for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db) oacc[db] = mfma32(tiles.v_operand(va, vb, t, m, db), pb[t][m], oacc[db]);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    if constexpr (MORE) {
+      wait_lds();
+      tiles.copy(va, vb, vc, p.v_stride, head_off, ids_now, first_key(j + 4), last_key(j + 4), shift, p.s.num_pages);
+    }
+  };
+  for (; j + 4 < n; j += 4) step(std::true_type());
+  if (j < n) step(std::false_type());
+
+  // the four states of each pair, joined: wavefront w writes its outputs to array w
+  const float l_tot = pair_sum(l_run);
+  __syncthreads();
+  char* const mine = reinterpret_cast<char*>(wave == 0 ? k0 : wave == 1 ? k1 : wave == 2 ? v0 : v1);
+  constexpr int CPR = D / 4;  // 16-byte chunks of a pair's output
+#pragma unroll
+  for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+    for (int g4 = 0; g4 < 4; ++g4) {
+      const f32x4 v = {oacc[db][g4 * 4], oacc[db][g4 * 4 + 1], oacc[db][g4 * 4 + 2], oacc[db][g4 * 4 + 3]};
+      const int ch = db * 8 + g4 * 2 + hf;
+      *reinterpret_cast<f32x4*>(mine + l32 * (D * 4) + ((ch ^ (l32 & (CPR - 1))) << 4)) = v;
+    }
+  if (hf == 0) {
+    stat[0][wave][l32] = l_tot > 0.f ? m_run : -INFINITY;
+    stat[1][wave][l32] = l_tot;
+  }
+  __syncthreads();
+  const int ch = lane % CPR;
+  float vscale = 1.f;
+  if constexpr (E4M3) vscale = p.v_scale[kvh];
+  for (int x = wave * (64 / CPR) + lane / CPR; x < pairs; x += 4 * (64 / CPR)) {
+    float top = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) top = fmaxf(top, stat[0][w][x]);
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const char* const o = reinterpret_cast<const char*>(w == 0 ? k0 : w == 1 ? k1 : w == 2 ? v0 : v1);
+      const float m = stat[0][w][x], wt = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - top) * c);
+      acc += *reinterpret_cast<const f32x4*>(o + x * (D * 4) + ((ch ^ (x & (CPR - 1))) << 4)) * wt;
+      sum += stat[1][w][x] * wt;
+    }
+    const float inv = sum > 0.f ? vscale / sum : 0.f;
+    const float lse = sum > 0.f ? (top * c + __log2f(sum)) * kLn2 : -INFINITY;
+    if (it.slot < 0) {
+      typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+      bf16x4 y;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) y[k] = (__bf16)(acc[k] * inv);
+      const int r = fast_div(x, g, p.group_magic);
+      *reinterpret_cast<bf16x4*>(p.o + qbase + pair_offset<D>(r, x - r * g, p.s.hq) + ch * 4) = y;
+      if (p.lse && ch == 0) p.lse[(int64_t)(kvh * g + x - r * g) * p.s.rows + it.row0 + r] = lse;
+    } else if (it.slot < p.max_slots) {
+      const int64_t at = ((int64_t)it.slot * p.s.hkv + kvh) * kSlotPairs + x;
+      *reinterpret_cast<f32x4*>(p.part_o + at * D + ch * 4) = acc * inv;
+      if (ch == 0) p.part_lse[at] = lse;
+    }
+  }
+}
+
 template <int D, bool E4M3>
 __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedFwdParams p) {
-  __shared__ __bf16 k_buf0[BN * D], k_buf1[BN * D], v_buf0[BN * D], v_buf1[BN * D];
-  // bytes of an e4m3 cache on their way (K, V)
-  __shared__ char stage_k[E4M3 ? BN * D : 16], stage_v[E4M3 ? BN * D : 16];
+  // (16 KB each: tiles of 64 keys, or of items of few pairs)
+  __shared__ __bf16 k_buf0[BN * 128], k_buf1[BN * 128], v_buf0[BN * 128], v_buf1[BN * 128];
+  __shared__ float stat[2][4][kSlotPairs];
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hf = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);  // uniform: scalar branches below
   const int unit = blockIdx.x;
@@ -171,6 +515,10 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedFwdParams p) {
   if (item >= plan[PH_ITEMS] || plan[PH_SEQS] != p.s.seqs || plan[PH_ROWS] != p.s.rows || plan[PH_HQ] != p.s.hq ||
       plan[PH_HKV] != p.s.hkv || plan[PH_PAGE] != p.s.page)
     return;
+  if (it.rows * p.group <= kSlotPairs) {
+    attend_few<D, E4M3>(p, it, kvh, k_buf0, k_buf1, v_buf0, v_buf1, stat);
+    return;
+  }
   QTile t;
   t.q_row0 = it.row0;
   t.q_len = it.rows;
@@ -191,23 +539,14 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedFwdParams p) {
   FwdCore<D> core;
   core.hf = hf;
   if (b0 < nblk) {
-    PageCursor kcur = cp.at(it, nA), vcur = kcur;
-    // e4m3: through the staging areas, `dst` is filled by land_k / land_v
-    auto load_k = [&](__bf16* dst) { cp.next(kcur, kc, p.k_stride, head_off, E4M3 ? stage_k : reinterpret_cast<char*>(dst)); };
-    auto load_v = [&](__bf16* dst) { cp.next(vcur, vc, p.v_stride, head_off, E4M3 ? stage_v : reinterpret_cast<char*>(dst)); };
-    auto land_k = [&](__bf16* dst) { cp.widen(stage_k, dst); };
-    auto land_v = [&](__bf16* dst) { cp.widen(stage_v, dst); };
+    PageCursor kcur = cp.begin(it, nA), vcur = kcur;
+    auto load_k = [&](__bf16* dst) { cp.next(kcur, kc, p.k_stride, head_off, reinterpret_cast<char*>(dst)); };
+    auto load_v = [&](__bf16* dst) { cp.next(vcur, vc, p.v_stride, head_off, reinterpret_cast<char*>(dst)); };
 
     // the first blocks' copies go out before anything else is computed: K(b + 1)
     // and V(b) are resident while block b is processed
     load_k(k_buf0);
     load_v(v_buf0);
-    if constexpr (E4M3) {
-      wait_vmem();
-      land_k(k_buf0);
-      land_v(v_buf0);
-      wave_lds_fence();
-    }
     if (b0 + 1 < nblk) load_k(k_buf1);
 
     core.load_q(p.q + qbase + pair_offset<D>(rows.row, rows.head, p.s.hq));
@@ -234,8 +573,10 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedFwdParams p) {
     f32x16 sa0, sa1, sb0, sb1;
     wait_vmem();
     if constexpr (E4M3) {
-      if (b0 + 1 < nblk) land_k(k_buf1);
       wave_lds_fence();
+      cp.widen(k_buf0);
+      cp.widen(v_buf0);
+      if (b0 + 1 < nblk) cp.widen(k_buf1);
     }
     __syncthreads();
     core.s_mfma(k_buf0, sa0, sa1);
@@ -247,9 +588,9 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedFwdParams p) {
       if (b < nlive) step(b, sa0, sa1, k_buf1, v_buf0, sb0, sb1);
       wait_vmem();
       if constexpr (E4M3) {
-        if (b + 2 < nblk) land_k(k_buf0);
-        if (b + 1 < nblk) land_v(v_buf1);
         wave_lds_fence();
+        if (b + 2 < nblk) cp.widen(k_buf0);
+        if (b + 1 < nblk) cp.widen(v_buf1);
       }
       __syncthreads();
       if (b + 1 < nblk) {
@@ -258,9 +599,9 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedFwdParams p) {
         if (b + 1 < nlive) step(b + 1, sb0, sb1, k_buf0, v_buf1, sa0, sa1);
         wait_vmem();
         if constexpr (E4M3) {
-          if (b + 3 < nblk) land_k(k_buf1);
-          if (b + 2 < nblk) land_v(v_buf0);
           wave_lds_fence();
+          if (b + 3 < nblk) cp.widen(k_buf1);
+          if (b + 2 < nblk) cp.widen(v_buf0);
         }
         __syncthreads();
       }
