@@ -45,104 +45,88 @@ __device__ __forceinline__ bf16x8 widen8(int lo, int hi) {
   return y;
 }
 
-// A position in a sequence's keys: the next block that is copied.
-struct PageCursor {
-  const int32_t* row;  // the segment's page table
-  int key, len;        // the block's first key; the segment's tokens
-  bool isB;
-  int win;             // first page of the window of 64 table entries
-  int ids;             // this lane's entry of the window
-};
-
 // Copies of 64-key blocks of one KV head from a cache into LDS, by four
-// wavefronts.
-template <int D, bool E4M3>
+// wavefronts. BIG: a page holds a block or more; else a quarter of one or more.
+//
+// Where a block (a quarter) lies is computed lane by lane, for a window of 64 of
+// them at a time: its byte offset in either cache and its valid bytes. A copy
+// then costs three lane reads and an addition on the scalar unit, which eight
+// wavefronts share. (With the offsets formed on the scalar unit, block by block
+// and for both page sizes, a step of a wavefront had 493 scalar instructions
+// instead of the packed forward's 127, and a chunk of 7777 tokens took 1900 us;
+// TODO_FIGURE.)
+template <int D, bool E4M3, bool BIG>
 struct PageCopy {
   static constexpr int ROWB = E4M3 ? D : 2 * D;    // bytes of a row
   static constexpr int RPI = 1024 / ROWB;          // rows of one copy instruction
   static constexpr int PER_WAVE = BN / RPI / 4;    // instructions of a block and wavefront
-  const int32_t* table;
-  int max_pages, num_pages, shift;
-  int b_seq, b_len;
-  int wave, lane;
-  int voff[PER_WAVE];  // this lane's byte offset from the block's first row
+  static constexpr int EPB = BIG ? 1 : 4;          // entries of a block
+  const PagedFwdParams& p;
+  const PagedItem& it;
+  int nA, wave, lane, head_off;
+  int voff[BIG ? PER_WAVE : 1];  // this lane's byte offset from the entry's first row
+  int win;                       // first block of the window
+  int k_lo, k_hi, v_lo, v_hi;    // this lane's entry: its offsets
+  int bytes;                     // and its valid bytes
 
-  __device__ __forceinline__ void init(const PagedFwdParams& p, int b_seq_, int b_len_, int wave_, int lane_) {
-    table = p.table;
-    max_pages = p.s.max_pages;
-    num_pages = p.s.num_pages;
-    shift = __builtin_ctz(p.s.page);
-    b_seq = b_seq_;
-    b_len = b_len_;
-    wave = wave_;
-    lane = lane_;
+  __device__ __forceinline__ PageCopy(const PagedFwdParams& p_, const PagedItem& it_, int nA_, int kvh, int wave_, int lane_)
+      : p(p_), it(it_), nA(nA_), wave(wave_), lane(lane_), head_off(kvh * (p_.s.page * ROWB)) {
     constexpr int CH = ROWB / 16;
 #pragma unroll
-    for (int k = 0; k < PER_WAVE; ++k) {
+    for (int k = 0; k < (BIG ? PER_WAVE : 1); ++k) {
       const int r = (wave + 4 * k) * RPI + lane / CH;
       // bf16: straight into the swizzled tile (TileCopy); e4m3: as it lies, for widen()
-      voff[k] = r * ROWB + ((E4M3 ? lane % CH : (lane % CH) ^ swz<D>(r)) << 4);
+      voff[k] = (BIG ? r : r & 15) * ROWB + ((E4M3 ? lane % CH : (lane % CH) ^ swz<D>(r)) << 4);
     }
+    window(it.blk0);
   }
 
-  __device__ __forceinline__ void window(PageCursor& c) const {
-    c.win = c.key >> shift;
-    c.ids = c.win + lane < max_pages ? c.row[c.win + lane] : -1;
+  __device__ __forceinline__ void window(int blk0) {
+    win = blk0;
+    const int blk = blk0 + lane / EPB, shift = __builtin_ctz(p.s.page);
+    const bool isB = blk >= nA;
+    const int key = (isB ? blk - nA : blk) * BN + (lane % EPB) * (BN / EPB), len = isB ? it.b_len : it.a_len;
+    const int seq = max(isB ? it.b_seq : it.a_seq, 0);
+    const int left = len - key;  // keys from the entry's first one on (none behind the item)
+    int id = -1;
+    if (left > 0) id = p.table[(int64_t)seq * p.s.max_pages + (key >> shift)];
+    const bool ok = (uint32_t)id < (uint32_t)p.s.num_pages;
+    bytes = ok ? min(BN / EPB, left) * ROWB : 0;
+    const int64_t at = head_off + (key & (p.s.page - 1)) * ROWB;
+    const int64_t k = ok ? id * p.k_stride + at : 0, v = ok ? id * p.v_stride + at : 0;
+    k_lo = (int)k;
+    k_hi = (int)(k >> 32);
+    v_lo = (int)v;
+    v_hi = (int)(v >> 32);
+  }
+
+  // the window holds block blk and the one before it
+  __device__ __forceinline__ void ensure(int blk) {
+    if (blk - win >= 64 / EPB) window(blk - 1);
   }
 
   // where the bytes of the wavefront's k-th copy instruction land in a tile
   __device__ __forceinline__ int at(int k) const { return (wave + 4 * k) * (E4M3 ? 2048 : 1024) + (E4M3 ? 1024 : 0); }
 
-  __device__ __forceinline__ PageCursor begin(const PagedItem& it, int nA) const {
-    PageCursor c;
-    c.isB = it.blk0 >= nA;
-    c.row = table + (int64_t)(c.isB ? b_seq : it.a_seq) * max_pages;
-    c.key = (c.isB ? it.blk0 - nA : it.blk0) * BN;
-    c.len = c.isB ? b_len : it.a_len;
-    window(c);
-    return c;
-  }
-
-  // copies the cursor's block and steps the cursor
-  __device__ __forceinline__ void next(PageCursor& c, const char* cache, int64_t stride, int head_off, char* lds) const {
+  __device__ __forceinline__ void copy(const void* cache, int lo, int hi, int blk, __bf16* tile) const {
 #if defined(__HIP_DEVICE_COMPILE__)
-    const int page = 1 << shift;
-    if (shift >= 6) {  // one page holds the block
-      const int id = __builtin_amdgcn_readlane(c.ids, (c.key >> shift) - c.win);
-      const bool ok = (uint32_t)id < (uint32_t)num_pages;
-      const char* const base = cache + (ok ? id : 0) * stride + head_off + (c.key & (page - 1)) * ROWB;
-      const int n = __builtin_amdgcn_readfirstlane(ok ? min(BN, c.len - c.key) * ROWB : 0);
-      const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, n, 0x00020000);
+    char* const lds = reinterpret_cast<char*>(tile);
+    __amdgpu_buffer_rsrc_t rsrc;
 #pragma unroll
-      for (int k = 0; k < PER_WAVE; ++k)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(
-            rsrc, (__attribute__((address_space(3))) void*)(lds + at(k)), 16, voff[k], 0, 0, 0);
-    } else {
-#pragma unroll
-      for (int k = 0; k < PER_WAVE; ++k) {
-        const int r0 = (wave + 4 * k) * RPI, key = c.key + r0;  // the instruction's first row
-        const int id = __builtin_amdgcn_readlane(c.ids, (key >> shift) - c.win);
-        const bool ok = (uint32_t)id < (uint32_t)num_pages;
-        // the address that the block's first row would have in this page; only the instruction's rows are read
-        const char* const base = cache + (ok ? id : 0) * stride + head_off + ((key & (page - 1)) - r0) * ROWB;
-        const int n = __builtin_amdgcn_readfirstlane(ok && c.len > key ? (r0 + min(RPI, c.len - key)) * ROWB : 0);
-        const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, n, 0x00020000);
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(
-            rsrc, (__attribute__((address_space(3))) void*)(lds + at(k)), 16, voff[k], 0, 0, 0);
+    for (int k = 0; k < PER_WAVE; ++k) {
+      if (!BIG || k == 0) {
+        const int e = (blk - win) * EPB + (BIG ? 0 : (wave + 4 * k) * RPI / 16);
+        const uint32_t l = __builtin_amdgcn_readlane(lo, e), h = __builtin_amdgcn_readlane(hi, e);
+        const char* const base = static_cast<const char*>(cache) + (int64_t)((uint64_t)h << 32 | l);
+        rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, __builtin_amdgcn_readlane(bytes, e), 0x00020000);
       }
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)(lds + at(k)), 16,
+                                               voff[BIG ? k : 0], 0, 0, 0);
     }
 #endif
-    c.key += BN;
-    if (c.key >= c.len && !c.isB && b_len > 0) {
-      c.isB = true;
-      c.key = 0;
-      c.len = b_len;
-      c.row = table + (int64_t)b_seq * max_pages;
-      window(c);
-    } else if (((c.key + BN - 1) >> shift) - c.win >= 64) {
-      window(c);
-    }
   }
+  __device__ __forceinline__ void copy_k(int blk, __bf16* tile) const { copy(p.k_cache, k_lo, k_hi, blk, tile); }
+  __device__ __forceinline__ void copy_v(int blk, __bf16* tile) const { copy(p.v_cache, v_lo, v_hi, blk, tile); }
 
   // e4m3: the rows that this wavefront's copies have brought, as bf16 into the swizzled tile
   __device__ __forceinline__ void widen(__bf16* tile) const {
@@ -493,7 +477,7 @@ __device__ __forceinline__ void attend_few(const PagedFwdParams& p, const PagedI
   }
 }
 
-template <int D, bool E4M3>
+template <int D, bool E4M3, bool BIG>
 __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedFwdParams p) {
   // (16 KB each: tiles of 64 keys, or of items of few pairs)
   __shared__ __bf16 k_buf0[BN * 128], k_buf1[BN * 128], v_buf0[BN * 128], v_buf1[BN * 128];
@@ -530,24 +514,16 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedFwdParams p) {
   const int nA = (it.a_len + BN - 1) / BN;
   const int nblk = it.blk1;  // blocks blk0 .. blk1 - 1 of A and then B
 
-  PageCopy<D, E4M3> cp;
-  cp.init(p, it.b_seq, it.b_len, wave, lane);
-  const char* const kc = static_cast<const char*>(p.k_cache);
-  const char* const vc = static_cast<const char*>(p.v_cache);
-  const int head_off = kvh * (p.s.page * PageCopy<D, E4M3>::ROWB);
   const int b0 = it.blk0;
   FwdCore<D> core;
   core.hf = hf;
   if (b0 < nblk) {
-    PageCursor kcur = cp.begin(it, nA), vcur = kcur;
-    auto load_k = [&](__bf16* dst) { cp.next(kcur, kc, p.k_stride, head_off, reinterpret_cast<char*>(dst)); };
-    auto load_v = [&](__bf16* dst) { cp.next(vcur, vc, p.v_stride, head_off, reinterpret_cast<char*>(dst)); };
-
+    PageCopy<D, E4M3, BIG> cp(p, it, nA, kvh, wave, lane);
     // the first blocks' copies go out before anything else is computed: K(b + 1)
     // and V(b) are resident while block b is processed
-    load_k(k_buf0);
-    load_v(v_buf0);
-    if (b0 + 1 < nblk) load_k(k_buf1);
+    cp.copy_k(b0, k_buf0);
+    cp.copy_v(b0, v_buf0);
+    if (b0 + 1 < nblk) cp.copy_k(b0 + 1, k_buf1);
 
     core.load_q(p.q + qbase + pair_offset<D>(rows.row, rows.head, p.s.hq));
     float scale = p.scale_log2;
@@ -583,8 +559,9 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedFwdParams p) {
     pace_lds_mfma<D / 8, 1, FWD_DEPTH>();
     __syncthreads();
     for (int b = b0; b < nblk; b += 2) {
-      if (b + 2 < nblk) load_k(k_buf0);
-      if (b + 1 < nblk) load_v(v_buf1);
+      cp.ensure(b + 2);
+      if (b + 2 < nblk) cp.copy_k(b + 2, k_buf0);
+      if (b + 1 < nblk) cp.copy_v(b + 1, v_buf1);
       if (b < nlive) step(b, sa0, sa1, k_buf1, v_buf0, sb0, sb1);
       wait_vmem();
       if constexpr (E4M3) {
@@ -594,8 +571,9 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedFwdParams p) {
       }
       __syncthreads();
       if (b + 1 < nblk) {
-        if (b + 3 < nblk) load_k(k_buf1);
-        if (b + 2 < nblk) load_v(v_buf0);
+        cp.ensure(b + 3);
+        if (b + 3 < nblk) cp.copy_k(b + 3, k_buf1);
+        if (b + 2 < nblk) cp.copy_v(b + 2, v_buf0);
         if (b + 1 < nlive) step(b + 1, sb0, sb1, k_buf0, v_buf1, sa0, sa1);
         wait_vmem();
         if constexpr (E4M3) {
@@ -633,16 +611,22 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedFwdParams p) {
   }
 }
 
+template <int D, bool E4M3, bool BIG>
+void launch(dim3 grid, const PagedFwdParams& p, hipStream_t stream) {
+  attn_paged_kernel<D, E4M3, BIG><<<grid, 256, 0, stream>>>(p);
+}
+
 }  // namespace
 
 hipError_t launch_paged_fwd(const PagedFwdParams& p, hipStream_t stream) {
-  const dim3 grid((unsigned)((int64_t)p.max_items * p.s.hkv)), block(256);
+  const dim3 grid((unsigned)((int64_t)p.max_items * p.s.hkv));
+  const bool big = p.s.page >= kPagedBlock, e4m3 = p.type == CACHE_E4M3;
   if (p.d == 128) {
-    if (p.type == CACHE_E4M3) attn_paged_kernel<128, true><<<grid, block, 0, stream>>>(p);
-    else attn_paged_kernel<128, false><<<grid, block, 0, stream>>>(p);
+    if (big) e4m3 ? launch<128, true, true>(grid, p, stream) : launch<128, false, true>(grid, p, stream);
+    else e4m3 ? launch<128, true, false>(grid, p, stream) : launch<128, false, false>(grid, p, stream);
   } else {
-    if (p.type == CACHE_E4M3) attn_paged_kernel<64, true><<<grid, block, 0, stream>>>(p);
-    else attn_paged_kernel<64, false><<<grid, block, 0, stream>>>(p);
+    if (big) e4m3 ? launch<64, true, true>(grid, p, stream) : launch<64, false, true>(grid, p, stream);
+    else e4m3 ? launch<64, true, false>(grid, p, stream) : launch<64, false, false>(grid, p, stream);
   }
   return hipGetLastError();
 }

@@ -87,17 +87,19 @@ class Step:
     def attend(self, plan, **kw):
         return api.paged_fwd(self.q, self.k_cache, self.v_cache, plan, want_lse=True, **self.scales, **kw)
 
-    def tokens(self, which, i):
+    def held(self, which):
         x = to64(getattr(self, which + "_cache").float())
-        if self.fp8:
-            x = x * to64(self.scales[which + "_scale"])[:, None, None]
+        return x * to64(self.scales[which + "_scale"])[:, None, None] if self.fp8 else x
+
+    def tokens(self, x, i):
         at = np.arange(self.t["length"][i] + max(0, self.t["new"][i]))
         return x[self.want[0][i, at // self.page], :, at % self.page]
 
     def check_attention(self, o, lse, scale=None):
         scale = self.d ** -0.5 if scale is None else scale
-        ref, rlse, mag, size = P.attention(to64(self.q)[:self.live], lambda i: self.tokens("k", i),
-                                           lambda i: self.tokens("v", i), self.t["parent"], self.t["length"],
+        k, v = self.held("k"), self.held("v")
+        ref, rlse, mag, size = P.attention(to64(self.q)[:self.live], lambda i: self.tokens(k, i),
+                                           lambda i: self.tokens(v, i), self.t["parent"], self.t["length"],
                                            self.t["new"], scale, self.hq // self.hkv)
         got, glse = to64(o)[:self.live], to64(lse)[:, :self.live]
         err = abs(got - ref) - (2.0 ** -8 * abs(ref) + (2.0 ** -8 + 2.0 ** -13) * mag)
