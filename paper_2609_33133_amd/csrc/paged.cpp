@@ -154,7 +154,7 @@ int augtree_page_plan(const augtree_pages* pages, const int32_t* new_rows, int32
   p.state_out = free_state_out;
   p.plan = static_cast<int32_t*>(plan);
   // little to write: by the one workgroup that scans, else by a second launch
-  const bool apart = rows > 2048 || s.seqs > 1024;
+  const bool apart = rows > 2048 || s.seqs > kFillSeqs;
   const hipStream_t str = static_cast<hipStream_t>(stream);
   Hook h("page_plan", str);
   if ((st = hip_ok(launch_page_plan(p, apart, str), "page plan launch"))) return st;

@@ -69,12 +69,12 @@ inline __host__ __device__ int paged_shift(int page) {
 // Where a plan's arrays are (in words), and the most items and slots of partial
 // results it can have.
 struct PlanLayout {
-  // [seqs]: first row (seqs + 1 of them), tokens before and after, parent and its tokens, pages taken and given back by
-  // the sequences before, run (its first sequence, or -1), rows of the run that begins here, rows merged before
-  int64_t cu, cached, total, parent, a_len, need, back, run, run_rows, merge0;
-  // [2 seqs], own unit and unit of the run that begins here: items with a part of C blocks before the unit's, items with
-  // a tile's last part before the unit's, first slot (-1: none), parts of a tile
-  int64_t full0, last0, slot0, parts;
+  int64_t cu;                // [seqs + 1] first row
+  // work: what the construction keeps (PlanArrays). Of each sequence: first row, tokens before and after, parent and its
+  // tokens, pages taken and given back by the sequences before, run (its first sequence, or -1), rows of the run that
+  // begins here, rows merged before. Of its own unit and of the unit of the run that begins here: items with a part of C
+  // blocks before the unit's, items with a tile's last part before the unit's, first slot (-1: none), parts of a tile.
+  int64_t work;
   int64_t slots, positions;  // [rows]
   int64_t merge;             // [rows][kMergeInts]
   int64_t items;             // [max_items][kItemInts]
@@ -95,19 +95,7 @@ inline __host__ __device__ PlanLayout plan_layout(const PagedShape& s) {
     return a;
   };
   L.cu = take(n + 1);
-  L.cached = take(n);
-  L.total = take(n);
-  L.parent = take(n);
-  L.a_len = take(n);
-  L.need = take(n);
-  L.back = take(n);
-  L.run = take(n);
-  L.run_rows = take(n);
-  L.merge0 = take(n);
-  L.full0 = take(2 * n);
-  L.last0 = take(2 * n);
-  L.slot0 = take(2 * n);
-  L.parts = take(2 * n);
+  L.work = take(18 * n + 1);
   L.slots = take(r);
   L.positions = take(r);
   L.merge = take(r * kMergeInts);
@@ -168,57 +156,93 @@ inline __host__ __device__ int part_blocks(int64_t blocks, int64_t tiles, const 
   return c < 1 ? 1 : c > INT32_MAX ? INT32_MAX : (int)c;
 }
 
-// What a sequence's units are, from the plan's arrays.
+// The arrays that the construction works on: the plan's, or copies in faster
+// memory where the same workgroup writes all of the plan.
+struct PlanArrays {
+  int32_t *cu, *cached, *total, *parent, *a_len, *need, *back, *run, *run_rows, *merge0, *full0, *last0, *slot0, *parts;
+  __host__ __device__ static int64_t words(int64_t seqs) { return 18 * seqs + 1; }
+  // one after the other, in `words` words
+  __host__ __device__ static PlanArrays packed(int32_t* at, int n) {
+    PlanArrays a;
+    a.cu = at;
+    a.cached = a.cu + n + 1;
+    a.total = a.cached + n;
+    a.parent = a.total + n;
+    a.a_len = a.parent + n;
+    a.need = a.a_len + n;
+    a.back = a.need + n;
+    a.run = a.back + n;
+    a.run_rows = a.run + n;
+    a.merge0 = a.run_rows + n;
+    a.full0 = a.merge0 + n;
+    a.last0 = a.full0 + 2 * n;
+    a.slot0 = a.last0 + 2 * n;
+    a.parts = a.slot0 + 2 * n;
+    return a;
+  }
+};
+
+// What a sequence's units are.
 struct UnitView {
-  const PlanParams& p;
-  __host__ __device__ explicit UnitView(const PlanParams& p_) : p(p_) {}
-  __host__ __device__ int at(int64_t array, int i) const { return p.plan[array + i]; }
-  __host__ __device__ int rows(int i) const { return at(p.L.cu, i + 1) - at(p.L.cu, i); }
+  const PlanArrays& a;
+  const int group;
+  __host__ __device__ UnitView(const PlanArrays& a_, int group_) : a(a_), group(group_) {}
   // the sequence's rows meet its parent's tokens in the unit of a run
   __host__ __device__ bool in_run(int i) const {
-    const int r = at(p.L.run, i);
-    return r >= 0 && at(p.L.run_rows, r) > rows(r);
+    const int r = a.run[i];
+    return r >= 0 && a.run_rows[r] > a.cu[i + 1] - a.cu[i];
   }
   // which: 0 the sequence's own unit, 1 the unit of the run that begins with it
   __host__ __device__ PagedItem unit(int i, int which) const {
     PagedItem u;
-    u.row0 = at(p.L.cu, i);
+    u.row0 = a.cu[i];
     u.pair0 = 0;
     u.a_seq = u.b_seq = -1;
     u.a_len = u.b_len = u.b_pos = 0;
     u.blk0 = u.blk1 = 0;
     u.slot = -1;
-    const int n = rows(i), r = at(p.L.run, i);
+    const int n = a.cu[i + 1] - u.row0;
     const bool run = n > 0 && in_run(i);
     if (which == 0) {
       u.rows = n;
       u.b_seq = i;
-      u.b_len = at(p.L.total, i);
-      u.b_pos = at(p.L.cached, i);
-      if (n > 0 && !run) u.a_seq = at(p.L.parent, i), u.a_len = at(p.L.a_len, i);
+      u.b_len = a.total[i];
+      u.b_pos = a.cached[i];
+      if (n > 0 && !run) u.a_seq = a.parent[i], u.a_len = a.a_len[i];
     } else {
       u.rows = 0;  // (a parent without tokens: nothing to meet)
-      if (run && r == i && at(p.L.a_len, i) > 0)
-        u.rows = at(p.L.run_rows, i), u.a_seq = at(p.L.parent, i), u.a_len = at(p.L.a_len, i);
+      if (run && a.run[i] == i && a.a_len[i] > 0) u.rows = a.run_rows[i], u.a_seq = a.parent[i], u.a_len = a.a_len[i];
     }
     return u;
   }
   __host__ __device__ static int blocks(const PagedItem& u) {
     return paged_div(u.a_len, kPagedBlock) + paged_div(u.b_len, kPagedBlock);
   }
-  __host__ __device__ int tiles(const PagedItem& u) const { return paged_div(u.rows * p.group, kTilePairs); }
+  __host__ __device__ int tiles(const PagedItem& u) const { return paged_div(u.rows * group, kTilePairs); }
 };
 
 // Sums of counts that stop at kMostCount, so that no sequence of bad lengths overflows them.
 constexpr int32_t kMostCount = 1 << 30;
 inline __host__ __device__ int32_t add_count(int32_t a, int32_t b) { return a + b < kMostCount ? a + b : kMostCount; }
 
+// use(i, load(i)) for i0 <= i < i1 in order, the loads of four at a time ahead of their uses (which may write).
+template <class Load, class Use>
+__host__ __device__ inline void in_batches(int i0, int i1, Load load, Use use) {
+  for (int i = i0; i < i1; i += 4) {
+    decltype(load(0)) v[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = load(i + k < i1 ? i + k : i1 - 1);
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (i + k < i1) use(i + k, v[k]);
+  }
+}
+
 // The plan but for what plan_fill writes, by one team of threads: team.tid of
 // team.size, barriers, exclusive scans over the threads.
 template <class Team>
-__host__ __device__ void plan_scan(Team& team, const PlanParams& p) {
+__host__ __device__ void plan_scan(Team& team, const PlanParams& p, const PlanArrays& a) {
   const PagedShape& s = p.s;
-  const PlanLayout& L = p.L;
   int32_t* const plan = p.plan;
   const int g = p.group, shift = p.shift, page = s.page;
   const int per = paged_div(s.seqs, team.size());
@@ -254,28 +278,36 @@ __host__ __device__ void plan_scan(Team& team, const PlanParams& p) {
   int bad = first < 0 || first >= s.num_pages || spare < 0 || spare > s.num_pages ? PAGES_LENGTH : 0;
   int32_t sums[3] = {0, 0, 0}, before[3], all[3];
   int64_t last = 0;
-  for (int i = i0; i < i1; ++i) {
-    const One o = look(i);
-    bad |= o.bad;
-    int a_len = 0;
-    if (o.parent >= 0) {
-      const int par = o.parent;
+  struct Two {
+    One o;
+    int a_len;  // the parent's tokens
+  };
+  in_batches(i0, i1, [&](int i) {
+    Two t;
+    t.o = look(i);
+    t.a_len = 0;
+    const int par = t.o.parent;
+    if (par >= 0) {
       if (par < s.seqs && par != i && p.parent[par] < 0 && p.fresh[par] >= 0) {
         const One q = look(par);
-        a_len = q.len + q.n;
+        t.a_len = q.len + q.n;
       } else {
-        bad |= PAGES_PARENT;
+        t.o.bad |= PAGES_PARENT;
       }
     }
-    plan[L.cached + i] = o.len;
-    plan[L.total + i] = o.len + o.n;
-    plan[L.parent + i] = o.parent;
-    plan[L.a_len + i] = a_len;
+    return t;
+  }, [&](int i, const Two& t) {
+    const One& o = t.o;
+    bad |= o.bad;
+    a.cached[i] = o.len;
+    a.total[i] = o.len + o.n;
+    a.parent[i] = o.parent;
+    a.a_len[i] = t.a_len;
     sums[0] = add_count(sums[0], o.n);
     sums[1] = add_count(sums[1], o.need);
     sums[2] = add_count(sums[2], o.back);
     if (o.n > 0) last = key(i, o);
-  }
+  });
   int64_t prev = last;
   team.scan_step(sums, before, all, prev, bad);  // prev: the last sequence with rows before i0
   if (all[0] > s.rows) bad |= PAGES_ROWS;
@@ -284,14 +316,14 @@ __host__ __device__ void plan_scan(Team& team, const PlanParams& p) {
 
   // first row and pages of each sequence; runs: a small sequence begins one unless the nearest sequence with rows before
   // it is small and of the same parent
+  const int row0 = bad ? 0 : before[0];
   int begin = -1;
   int64_t q = prev;
-  for (int i = i0; i < i1; ++i) {
-    const One o = look(i);
-    plan[L.cu + i] = bad ? 0 : before[0];
-    plan[L.need + i] = bad ? 0 : before[1];
-    plan[L.back + i] = bad ? 0 : before[2];
-    plan[L.run + i] = plan[L.run_rows + i] = -1;
+  in_batches(i0, i1, look, [&](int i, const One& o) {
+    a.cu[i] = plan[p.L.cu + i] = bad ? 0 : before[0];
+    a.need[i] = bad ? 0 : before[1];
+    a.back[i] = bad ? 0 : before[2];
+    a.run[i] = a.run_rows[i] = -1;
     before[0] += o.n;
     before[1] += o.need;
     before[2] += o.back;
@@ -300,82 +332,104 @@ __host__ __device__ void plan_scan(Team& team, const PlanParams& p) {
       if (o.small && (uint32_t)q != (uint32_t)k) begin = i;
       q = k;
     }
-  }
+  });
   if (team.tid() == 0) {
     const int rows = bad ? 0 : all[0];
     const int32_t head[] = {s.seqs, s.rows, s.hq, s.hkv, page, bad, rows};
     for (int k = 0; k < 7; ++k) plan[PH_SEQS + k] = head[k];
-    plan[L.cu + s.seqs] = rows;
+    a.cu[s.seqs] = plan[p.L.cu + s.seqs] = rows;
     plan[PH_FIRST] = first;
     plan[PH_SPARE] = spare;
     plan[PH_NEED] = bad ? 0 : all[1];
     plan[PH_BACK] = bad ? 0 : all[2];
   }
   int start = team.scan_max(begin);  // the last run that begins before i0
-  if (!bad) {
-    q = prev;
-    int row = i0 < i1 ? plan[L.cu + i0] : 0;
-    for (int i = i0; i < i1; ++i) {
-      const One o = look(i);
-      if (o.n > 0) {
-        const int64_t k = key(i, o);
-        const bool joins = o.small && (uint32_t)q == (uint32_t)k;
-        if (is_small(q) && !joins) plan[L.run_rows + start] = row - plan[L.cu + start];
-        if (o.small && !joins) start = i;
-        if (o.small) plan[L.run + i] = start;
-        q = k;
-        row += o.n;
-      }
-    }
-    // the run that no sequence with rows follows ends with the rows: the thread of the last sequence closes it
-    if (i1 == s.seqs && i0 < i1 && is_small(q)) plan[L.run_rows + start] = all[0] - plan[L.cu + start];
-  }
+  q = prev;
+  int row = row0;
+  in_batches(i0, i1, look, [&](int i, const One& o) {
+    if (bad || o.n == 0) return;
+    const int64_t k = key(i, o);
+    const bool joins = o.small && (uint32_t)q == (uint32_t)k;
+    if (is_small(q) && !joins) a.run_rows[start] = row - a.cu[start];
+    if (o.small && !joins) start = i;
+    if (o.small) a.run[i] = start;
+    q = k;
+    row += o.n;
+  });
+  // the run that no sequence with rows follows ends with the rows: the thread of the last sequence closes it
+  if (!bad && i1 == s.seqs && i0 < i1 && is_small(q)) a.run_rows[start] = all[0] - a.cu[start];
   team.sync();  // (nobody reads lengths and state from here on: they may be written in place)
-  for (int i = i0; i < i1; ++i)
-    if (!bad || p.length_out != p.length)
-      p.length_out[i] = bad ? p.length[i] : p.fresh[i] < 0 ? 0 : plan[L.total + i];
+  in_batches(i0, i1, look, [&](int i, const One& o) {
+    if (!bad) p.length_out[i] = p.fresh[i] < 0 ? 0 : o.len + o.n;
+    else if (p.length_out != p.length) p.length_out[i] = p.length[i];
+    if (bad) a.cached[i] = a.total[i] = a.a_len[i] = 0, a.parent[i] = -1;
+  });
   if (team.tid() == 0) {
-    int to = first + (bad ? 0 : all[1]);
+    const int to = first + (bad ? 0 : all[1]);
     p.state_out[0] = to >= s.num_pages && !bad ? to - s.num_pages : to;
     p.state_out[1] = bad ? spare : spare - all[1] + all[2];
   }
 
   // blocks of all tiles, and from them the length of a part
-  const UnitView view(p);
+  const UnitView view(a, g);
+  struct Units {
+    int rows[2], blocks[2];
+    bool run;
+  };
   int64_t w[2] = {0, 0};
-  for (int i = i0; i < i1; ++i)
+  in_batches(i0, i1, [&](int i) {
+    Units x;
     for (int which = 0; which < 2; ++which) {
       const PagedItem u = view.unit(i, which);
-      const int tiles = view.tiles(u);
-      w[0] += (int64_t)tiles * view.blocks(u);
-      w[1] += tiles;
+      x.rows[which] = u.rows;
+      x.blocks[which] = view.blocks(u);
     }
+    x.run = view.in_run(i);
+    return x;
+  }, [&](int i, const Units& x) {
+    for (int which = 0; which < 2; ++which) {
+      const int tiles = paged_div(x.rows[which] * g, kTilePairs);
+      w[0] += (int64_t)tiles * x.blocks[which];
+      w[1] += tiles;
+      // for the two passes below, which write what belongs here
+      a.full0[2 * (int64_t)i + which] = x.rows[which];
+      a.last0[2 * (int64_t)i + which] = x.blocks[which];
+    }
+    a.merge0[i] = x.run;
+  });
   team.sum(w);
-  const int part = part_blocks(w[0], w[1], s, L.max_parts);
+  const int part = part_blocks(w[0], w[1], s, p.L.max_parts);
 
   // items: the parts of full length first, then the tiles' last ones; slots of partial results; merged rows
   int32_t c[4] = {0, 0, 0, 0}, at[4], sum[4], most_parts = 0;
   for (int pass = 0; pass < 2; ++pass) {
     int32_t* const n = pass ? at : c;
-    for (int i = i0; i < i1; ++i) {
+    in_batches(i0, i1, [&](int i) {
+      Units x;
       for (int which = 0; which < 2; ++which) {
-        const PagedItem u = view.unit(i, which);
-        const int tiles = view.tiles(u), parts = tiles ? paged_div(view.blocks(u), part) : 0;
-        const bool partial = tiles && (parts > 1 || which == 1 || view.in_run(i));
+        x.rows[which] = a.full0[2 * (int64_t)i + which];
+        x.blocks[which] = a.last0[2 * (int64_t)i + which];
+      }
+      x.run = a.merge0[i] != 0;
+      return x;
+    }, [&](int i, const Units& x) {
+      for (int which = 0; which < 2; ++which) {
+        const int tiles = paged_div(x.rows[which] * g, kTilePairs), parts = tiles ? paged_div(x.blocks[which], part) : 0;
+        const bool partial = tiles && (parts > 1 || which == 1 || x.run);
         if (pass) {
           const int64_t k = 2 * (int64_t)i + which;
-          plan[L.full0 + k] = n[0];
-          plan[L.last0 + k] = n[1];
-          plan[L.slot0 + k] = partial ? n[2] : -1;
-          plan[L.parts + k] = parts;
-          if (which == 0) plan[L.merge0 + i] = partial ? n[3] : -1;
+          a.full0[k] = n[0];
+          a.last0[k] = n[1];
+          a.slot0[k] = partial ? n[2] : -1;
+          a.parts[k] = parts;
+          if (which == 0) a.merge0[i] = partial ? n[3] : -1;
         }
         if (tiles) n[0] += tiles * (parts - 1), n[1] += tiles;
-        if (partial) n[2] += parts * paged_div(u.rows * g, kSlotPairs);
-        if (partial && which == 0) n[3] += u.rows;
+        if (partial) n[2] += parts * paged_div(x.rows[which] * g, kSlotPairs);
+        if (partial && which == 0) n[3] += x.rows[which];
         if (partial && parts > most_parts) most_parts = parts;
       }
-    }
+    });
     if (!pass) team.scan(c, at, sum);
   }
   most_parts = team.max_of(most_parts);
@@ -403,65 +457,63 @@ inline __host__ __device__ int last_at_most(const int32_t* a, int n, int x) {
 // The rest of the plan, by `size` threads that need not know of one another:
 // rows, pages and items, each found among its sequences by bisection.
 template <class Team>
-__host__ __device__ void plan_fill(Team& team, const PlanParams& p, int tid, int size) {
+__host__ __device__ void plan_fill(Team& team, const PlanParams& p, const PlanArrays& a, int tid, int size) {
   const PagedShape& s = p.s;
-  const PlanLayout& L = p.L;
   int32_t* const plan = p.plan;
-  const UnitView view(p);
+  const UnitView view(a, p.group);
   const int g = p.group, page = s.page, shift = p.shift;
   const int first = plan[PH_FIRST], spare = plan[PH_SPARE], part = plan[PH_PART], rows = plan[PH_TOTAL_ROWS];
   const int need = plan[PH_NEED], back = plan[PH_BACK], full = plan[PH_FULL], items = plan[PH_ITEMS];
   auto ring = [&](int k) { return k < s.num_pages ? k : k - s.num_pages; };
 
-  // rows: slot, position, where the merge finds its parts
-  for (int r = tid; r < s.rows; r += size) {
+  // a row: slot, position, where the merge finds its parts
+  auto fill_row = [&](int r) {
     int slot = -1, pos = -1;
     if (r < rows) {
-      const int seq = last_at_most(plan + L.cu, s.seqs, r);
-      const int off = r - plan[L.cu + seq], cached = plan[L.cached + seq], at = cached + off;
+      const int seq = last_at_most(a.cu, s.seqs, r);
+      const int off = r - a.cu[seq], cached = a.cached[seq], at = cached + off;
       const int have = (cached + page - 1) >> shift, k = at >> shift;
-      const int id = k < have ? p.table[(int64_t)seq * s.max_pages + k] : p.free_pages[ring(first + plan[L.need + seq] + k - have)];
-      if (id >= 0 && id < s.num_pages) slot = (id << shift) + (at & (page - 1));
-      else team.flag(plan + PH_STATUS, PAGES_PAGE);
-      pos = at + plan[L.a_len + seq];
-      const int m = plan[L.merge0 + seq];
+      const int id = k < have ? p.table[(int64_t)seq * s.max_pages + k] : p.free_pages[ring(first + a.need[seq] + k - have)];
+      const int m = a.merge0[seq];
       if (m >= 0) {
-        int32_t* const dst = plan + L.merge + (int64_t)(m + off) * kMergeInts;
+        int32_t* const dst = plan + p.L.merge + (int64_t)(m + off) * kMergeInts;
         dst[0] = r;
         for (int u = 0; u < 2; ++u) {
-          const int q = u == 0 ? seq : plan[L.run + seq];
-          const int slot0 = q < 0 ? -1 : plan[L.slot0 + 2 * (int64_t)q + u];
-          const int row0 = q < 0 ? 0 : plan[L.cu + q];
+          const int q = u == 0 ? seq : a.run[seq];
+          const int slot0 = q < 0 ? -1 : a.slot0[2 * q + u];
+          const int row0 = q < 0 ? 0 : a.cu[q];
           const int pair = (r - row0) * g;
           dst[1 + 4 * u] = slot0 + pair / kSlotPairs;
           dst[2 + 4 * u] = pair % kSlotPairs;
-          dst[3 + 4 * u] = slot0 < 0 ? 0 : paged_div((u == 0 ? view.rows(q) : plan[L.run_rows + q]) * g, kSlotPairs);
-          dst[4 + 4 * u] = slot0 < 0 ? 0 : plan[L.parts + 2 * (int64_t)q + u];
+          dst[3 + 4 * u] = slot0 < 0 ? 0 : paged_div((u == 0 ? a.cu[q + 1] - row0 : a.run_rows[q]) * g, kSlotPairs);
+          dst[4 + 4 * u] = slot0 < 0 ? 0 : a.parts[2 * q + u];
         }
       }
+      if (id >= 0 && id < s.num_pages) slot = (id << shift) + (at & (page - 1));
+      else team.flag(plan + PH_STATUS, PAGES_PAGE);
+      pos = at + a.a_len[seq];
     }
-    plan[L.slots + r] = slot;
-    plan[L.positions + r] = pos;
-  }
-
-  // new pages into the table, ended sequences' back to the ring
-  for (int k = tid; k < need; k += size) {
-    const int i = last_at_most(plan + L.need, s.seqs, k);
-    const int have = (plan[L.cached + i] + page - 1) >> shift;
-    p.table[(int64_t)i * s.max_pages + have + k - plan[L.need + i]] = p.free_pages[ring(first + k)];
-  }
-  for (int k = tid; k < back; k += size) {
-    const int i = last_at_most(plan + L.back, s.seqs, k);
-    p.free_pages[ring(ring(first + spare) + k)] = p.table[(int64_t)i * s.max_pages + k - plan[L.back + i]];
-  }
-
-  for (int x = tid; x < items; x += size) {
+    plan[p.L.slots + r] = slot;
+    plan[p.L.positions + r] = pos;
+  };
+  // a new page into the table; an ended sequence's page back to the ring
+  auto fill_need = [&](int k) {
+    const int i = last_at_most(a.need, s.seqs, k);
+    const int have = (a.cached[i] + page - 1) >> shift;
+    p.table[(int64_t)i * s.max_pages + have + k - a.need[i]] = p.free_pages[ring(first + k)];
+  };
+  auto fill_back = [&](int k) {
+    const int i = last_at_most(a.back, s.seqs, k);
+    p.free_pages[ring(ring(first + spare) + k)] = p.table[(int64_t)i * s.max_pages + k - a.back[i]];
+  };
+  auto fill_item = [&](int x) {
     const bool whole = x < full;  // a part of `part` blocks, not a tile's last
     const int k = whole ? x : x - full;
-    const int unit = last_at_most(plan + (whole ? L.full0 : L.last0), 2 * s.seqs, k);
+    const int32_t* const of = whole ? a.full0 : a.last0;
+    const int unit = last_at_most(of, 2 * s.seqs, k);
     PagedItem it = view.unit(unit >> 1, unit & 1);
-    const int parts = plan[L.parts + unit], slot0 = plan[L.slot0 + unit];
-    const int of_tile = whole ? parts - 1 : 1, j = k - plan[(whole ? L.full0 : L.last0) + unit];
+    const int parts = a.parts[unit], slot0 = a.slot0[unit];
+    const int of_tile = whole ? parts - 1 : 1, j = k - of[unit];
     // a causal unit's last tiles have the most blocks: they come first
     const int t = view.tiles(it) - 1 - j / of_tile, c = whole ? j % of_tile : parts - 1;
     it.pair0 = t * kTilePairs;
@@ -473,18 +525,31 @@ __host__ __device__ void plan_fill(Team& team, const PlanParams& p, int tid, int
     it.blk0 = (int)((int64_t)c * part < end ? (int64_t)c * part : end);
     it.blk1 = (int)((int64_t)(c + 1) * part < end ? (int64_t)(c + 1) * part : end);
     if (slot0 >= 0) it.slot = slot0 + c * paged_div(it.rows * g, kSlotPairs) + t * (kTilePairs / kSlotPairs);
-    int32_t* const dst = plan + L.items + (int64_t)x * kItemInts;
+    int32_t* const dst = plan + p.L.items + (int64_t)x * kItemInts;
     const int32_t w[kItemInts] = {it.row0, it.rows, it.pair0, it.a_seq, it.a_len, it.b_seq, it.b_len, it.b_pos,
                                   it.blk0, it.blk1, it.slot, 0, 0, 0, 0, 0};
     for (int y = 0; y < kItemInts; ++y) dst[y] = w[y];
+  };
+  // one after the other through all of it, so that every thread has its share of the kinds
+  const int at_back = s.rows + need, at_item = at_back + back, end = at_item + items;
+  for (int x = tid; x < end; x += size) {
+    if (x < s.rows) fill_row(x);
+    else if (x < at_back) fill_need(x - s.rows);
+    else if (x < at_item) fill_back(x - at_back);
+    else fill_item(x - at_item);
   }
 }
+
+// The arrays in the plan itself.
+inline __host__ __device__ PlanArrays plan_arrays(const PlanParams& p) { return PlanArrays::packed(p.plan + p.L.work, p.s.seqs); }
 
 // ---------------------------------------------------------------------------- launchers
 
 // How a cache holds its values.
 enum : int { CACHE_BF16 = 0, CACHE_E4M3 = 1 };
 
+// apart: the plan's arrays by a second launch, with more than one workgroup; else at most kFillSeqs sequences
+constexpr int kFillSeqs = 1024;
 hipError_t launch_page_plan(const PlanParams& p, bool apart, hipStream_t stream);
 
 struct CacheWriteParams {

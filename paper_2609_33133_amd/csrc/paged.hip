@@ -128,19 +128,25 @@ struct GroupTeam {
 };
 
 // One workgroup: the scans over the sequences and, where the rest is little
-// (FILL), that too. Bound by latency: a dozen barriers and the memory round
-// trips between them.
+// (FILL: at most kFillSeqs sequences), that too, with all arrays in LDS. Bound
+// by latency: a dozen barriers and the memory round trips between them. TODO_FIGURE
 template <bool FILL>
 __global__ __launch_bounds__(kPlanThreads) void page_plan_kernel(PlanParams p) {
   __shared__ GroupTeam::Wave lds[2][kPlanThreads / 64];
   GroupTeam team{lds};
-  plan_scan(team, p);
-  if constexpr (FILL) plan_fill(team, p, threadIdx.x, kPlanThreads);
+  if constexpr (FILL) {
+    __shared__ int32_t work[18 * kFillSeqs + 1];
+    const PlanArrays a = PlanArrays::packed(work, p.s.seqs);
+    plan_scan(team, p, a);
+    plan_fill(team, p, a, threadIdx.x, kPlanThreads);
+  } else {
+    plan_scan(team, p, plan_arrays(p));
+  }
 }
 
 __global__ __launch_bounds__(256) void page_fill_kernel(PlanParams p) {
   GroupTeam team{nullptr};
-  plan_fill(team, p, blockIdx.x * 256 + threadIdx.x, gridDim.x * 256);
+  plan_fill(team, p, plan_arrays(p), blockIdx.x * 256 + threadIdx.x, gridDim.x * 256);
 }
 
 __device__ __forceinline__ bool plan_is_for(const int32_t* plan, const PagedShape& s) {
