@@ -147,13 +147,20 @@ struct PlanParams {
 // Few tiles: as many parts as run at once. More of them: parts of half of what
 // a slot of the chip has to do, so that items of different lengths fill it.
 inline __host__ __device__ int part_blocks(int64_t blocks, int64_t tiles, const PagedShape& s, int max_parts) {
-  const int64_t slots = kChipSlots / s.hkv > 1 ? kChipSlots / s.hkv : 1;
-  int64_t c;
-  if (tiles * 4 < slots) c = (blocks + slots - tiles - 1) / (slots - tiles);
-  else c = (blocks + 2 * slots - 1) / (2 * slots) > 8 ? (blocks + 2 * slots - 1) / (2 * slots) : 8;
-  const int64_t least = (blocks + max_parts - 1) / max_parts;
+  const int slots = kChipSlots / s.hkv > 1 ? kChipSlots / s.hkv : 1;
+  // (the GPU has no 64-bit division: of more than 2^31 blocks in thousands, rounded up)
+  auto ceil_div = [](int64_t n, int d) {
+    if (n <= INT32_MAX - 4096) return (int)(((uint32_t)n + (uint32_t)d - 1) / (uint32_t)d);
+    const int64_t k = (n >> 10) + 1;
+    const uint32_t q = ((uint32_t)(k < INT32_MAX ? k : INT32_MAX) + (uint32_t)d - 1) / (uint32_t)d;
+    return q < INT32_MAX >> 10 ? (int)(q << 10) : (int)INT32_MAX;
+  };
+  int c;
+  if (tiles * 4 < slots) c = ceil_div(blocks, slots - (int)tiles);
+  else c = ceil_div(blocks, 2 * slots) > 8 ? ceil_div(blocks, 2 * slots) : 8;
+  const int least = ceil_div(blocks, max_parts);
   if (c < least) c = least;
-  return c < 1 ? 1 : c > INT32_MAX ? INT32_MAX : (int)c;
+  return c < 1 ? 1 : c;
 }
 
 // The arrays that the construction works on: the plan's, or copies in faster
@@ -225,40 +232,42 @@ struct UnitView {
 constexpr int32_t kMostCount = 1 << 30;
 inline __host__ __device__ int32_t add_count(int32_t a, int32_t b) { return a + b < kMostCount ? a + b : kMostCount; }
 
-// use(i, load(i)) for i0 <= i < i1 in order, the loads of four at a time ahead of their uses (which may write).
-template <class Load, class Use>
-__host__ __device__ inline void in_batches(int i0, int i1, Load load, Use use) {
-  for (int i = i0; i < i1; i += 4) {
-    decltype(load(0)) v[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] = load(i + k < i1 ? i + k : i1 - 1);
-#pragma unroll
-    for (int k = 0; k < 4; ++k)
-      if (i + k < i1) use(i + k, v[k]);
+// n / d rounded up, for many n >= 0 by one d >= 1 with n + d < 2^31.
+struct CeilDiv {
+  int32_t d;
+  uint32_t magic;  // 2^32 / d, rounded up: the quotient is right or one too large
+  __host__ __device__ explicit CeilDiv(int32_t d_) : d(d_), magic(d_ == 1 ? 0 : (uint32_t)(0xFFFFFFFFu / (uint32_t)d_) + 1) {}
+  __host__ __device__ int operator()(int n) const {
+    const uint32_t x = (uint32_t)n + d - 1;
+    const uint32_t q = d == 1 ? x : (uint32_t)((uint64_t)x * magic >> 32);
+    return (int)(q * (uint32_t)d > x ? q - 1 : q);
   }
-}
+};
 
-// The plan but for what plan_fill writes, by one team of threads: team.tid of
-// team.size, barriers, exclusive scans over the threads.
-template <class Team>
+// The plan but for what plan_fill writes, by one team of wavefronts. Each takes
+// a range of the sequences, `lanes` neighbours at a time, and knows of the ones
+// before by scans over its lanes, a carry from step to step and a scan over the
+// wavefronts. ONE: the team has a thread for every sequence, which then looks
+// at it once.
+template <bool ONE, class Team>
 __host__ __device__ void plan_scan(Team& team, const PlanParams& p, const PlanArrays& a) {
   const PagedShape& s = p.s;
   int32_t* const plan = p.plan;
   const int g = p.group, shift = p.shift, page = s.page;
-  const int per = paged_div(s.seqs, team.size());
-  const int i0 = per * team.tid() < s.seqs ? per * team.tid() : s.seqs;
-  const int i1 = i0 + per < s.seqs ? i0 + per : s.seqs;
+  const int lanes = team.lanes(), steps = ONE ? 1 : paged_div(s.seqs, team.waves() * lanes);
+  const int base = team.wave() * steps * lanes + team.lane();
   const int first = p.state[0], spare = p.state[1];
   const int most = s.max_pages << shift;
   auto pages = [&](int tokens) { return (tokens + page - 1) >> shift; };
 
-  // a sequence's step, its numbers brought into range; bits of what is wrong with it
+  // a sequence's step, its numbers brought into range (nothing behind the last sequence); bits of what is wrong with it
   struct One {
     int len, n, need, back, parent, bad;
     bool small;  // may be of a run
   };
   auto look = [&](int i) {
-    One o;
+    One o{0, 0, 0, 0, -1, 0, false};
+    if (i >= s.seqs) return o;
     const int len = p.length[i], raw = p.fresh[i], par = p.parent ? p.parent[i] : -1;
     o.bad = len < 0 || len > most ? PAGES_LENGTH : 0;
     o.len = o.bad ? 0 : len;
@@ -270,69 +279,72 @@ __host__ __device__ void plan_scan(Team& team, const PlanParams& p, const PlanAr
     o.small = o.parent >= 0 && (int64_t)o.n * g <= kSmallPairs;
     return o;
   };
-  // of the sequences with rows: the last one's number and, where it may be of a run, its parent, for a scan of maxima
-  auto key = [](int i, const One& o) { return (int64_t)(i + 1) << 32 | (uint32_t)(o.small ? o.parent + 1 : 0); };
-  auto is_small = [](int64_t k) { return k > 0 && (uint32_t)k != 0; };
+  One mine{};
+  auto again = [&](int i) { return ONE ? mine : look(i); };
+  // of the sequences with rows: the last one's number and, where it may be of a run, its parent, for scans of maxima
+  auto key = [](int i, const One& o) {
+    return o.n > 0 ? (int64_t)(i + 1) << 32 | (uint32_t)(o.small ? o.parent + 1 : 0) : 0;
+  };
+  auto is_small = [](int64_t k) { return (uint32_t)k != 0; };
+  auto larger = [](int64_t x, int64_t y) { return x > y ? x : y; };
 
   // rows, pages needed and given back; what is wrong
   int bad = first < 0 || first >= s.num_pages || spare < 0 || spare > s.num_pages ? PAGES_LENGTH : 0;
   int32_t sums[3] = {0, 0, 0}, before[3], all[3];
-  int64_t last = 0;
-  struct Two {
-    One o;
-    int a_len;  // the parent's tokens
-  };
-  in_batches(i0, i1, [&](int i) {
-    Two t;
-    t.o = look(i);
-    t.a_len = 0;
-    const int par = t.o.parent;
-    if (par >= 0) {
+  int64_t prev = 0;
+  for (int j = 0; j < steps; ++j) {
+    const int i = base + j * lanes;
+    One o = look(i);
+    int a_len = 0;
+    if (o.parent >= 0) {
+      const int par = o.parent;
       if (par < s.seqs && par != i && p.parent[par] < 0 && p.fresh[par] >= 0) {
         const One q = look(par);
-        t.a_len = q.len + q.n;
+        a_len = q.len + q.n;
       } else {
-        t.o.bad |= PAGES_PARENT;
+        o.bad |= PAGES_PARENT;
       }
     }
-    return t;
-  }, [&](int i, const Two& t) {
-    const One& o = t.o;
+    mine = o;
     bad |= o.bad;
-    a.cached[i] = o.len;
-    a.total[i] = o.len + o.n;
-    a.parent[i] = o.parent;
-    a.a_len[i] = t.a_len;
+    if (i < s.seqs) {
+      a.cached[i] = o.len;
+      a.total[i] = o.len + o.n;
+      a.parent[i] = o.parent;
+      a.a_len[i] = a_len;
+    }
     sums[0] = add_count(sums[0], o.n);
     sums[1] = add_count(sums[1], o.need);
     sums[2] = add_count(sums[2], o.back);
-    if (o.n > 0) last = key(i, o);
-  });
-  int64_t prev = last;
-  team.scan_step(sums, before, all, prev, bad);  // prev: the last sequence with rows before i0
+    prev = larger(prev, key(i, o));
+  }
+  team.scan_waves(sums, before, all, prev, bad);  // prev: the last sequence with rows before this wavefront's
   if (all[0] > s.rows) bad |= PAGES_ROWS;
   if (all[1] > spare) bad |= PAGES_SHORT;
   if (all[2] > s.num_pages - spare) bad |= PAGES_LENGTH;
 
   // first row and pages of each sequence; runs: a small sequence begins one unless the nearest sequence with rows before
   // it is small and of the same parent
-  const int row0 = bad ? 0 : before[0];
-  int begin = -1;
+  int start = -1;
   int64_t q = prev;
-  in_batches(i0, i1, look, [&](int i, const One& o) {
-    a.cu[i] = plan[p.L.cu + i] = bad ? 0 : before[0];
-    a.need[i] = bad ? 0 : before[1];
-    a.back[i] = bad ? 0 : before[2];
-    a.run[i] = a.run_rows[i] = -1;
-    before[0] += o.n;
-    before[1] += o.need;
-    before[2] += o.back;
-    if (o.n > 0) {
-      const int64_t k = key(i, o);
-      if (o.small && (uint32_t)q != (uint32_t)k) begin = i;
-      q = k;
+  for (int j = 0; j < steps; ++j) {
+    const int i = base + j * lanes;
+    const One o = again(i);
+    const int64_t k = key(i, o);
+    int32_t v[3] = {o.n, o.need, o.back}, total[3];
+    int64_t ahead = k;
+    team.scan_lanes(v, total);
+    const int64_t k_all = team.max_lanes(ahead);
+    if (i < s.seqs) {
+      a.cu[i] = plan[p.L.cu + i] = bad ? 0 : before[0] + v[0];
+      a.need[i] = bad ? 0 : before[1] + v[1];
+      a.back[i] = bad ? 0 : before[2] + v[2];
+      a.run[i] = a.run_rows[i] = -1;
+      if (o.small && (uint32_t)larger(q, ahead) != (uint32_t)k) start = i;
     }
-  });
+    for (int c = 0; c < 3; ++c) before[c] += total[c];
+    q = larger(q, k_all);
+  }
   if (team.tid() == 0) {
     const int rows = bad ? 0 : all[0];
     const int32_t head[] = {s.seqs, s.rows, s.hq, s.hkv, page, bad, rows};
@@ -343,94 +355,130 @@ __host__ __device__ void plan_scan(Team& team, const PlanParams& p, const PlanAr
     plan[PH_NEED] = bad ? 0 : all[1];
     plan[PH_BACK] = bad ? 0 : all[2];
   }
-  int start = team.scan_max(begin);  // the last run that begins before i0
+  start = team.max_waves(start);  // the last run that begins before this wavefront's sequences
   q = prev;
-  int row = row0;
-  in_batches(i0, i1, look, [&](int i, const One& o) {
-    if (bad || o.n == 0) return;
+  for (int j = 0; j < steps; ++j) {
+    const int i = base + j * lanes;
+    const One o = again(i);
     const int64_t k = key(i, o);
-    const bool joins = o.small && (uint32_t)q == (uint32_t)k;
-    if (is_small(q) && !joins) a.run_rows[start] = row - a.cu[start];
-    if (o.small && !joins) start = i;
-    if (o.small) a.run[i] = start;
-    q = k;
-    row += o.n;
-  });
-  // the run that no sequence with rows follows ends with the rows: the thread of the last sequence closes it
-  if (!bad && i1 == s.seqs && i0 < i1 && is_small(q)) a.run_rows[start] = all[0] - a.cu[start];
+    int64_t ahead = k;
+    const int64_t k_all = team.max_lanes(ahead);
+    const int64_t near = larger(q, ahead);
+    const bool joins = o.small && (uint32_t)near == (uint32_t)k;
+    int64_t begin = o.small && !joins ? i + 1 : 0;
+    const int64_t begin_all = team.max_lanes(begin);
+    const int run = begin > 0 ? (int)begin - 1 : start;  // the last that begins before this sequence
+    if (!bad && o.n > 0) {
+      if (is_small(near) && !joins) a.run_rows[run] = a.cu[i] - a.cu[run];
+      if (o.small) a.run[i] = joins ? run : i;
+    }
+    // the run that no sequence with rows follows ends with the rows
+    if (!bad && i == s.seqs - 1 && is_small(larger(near, k))) {
+      const int r = o.small && !joins ? i : run;
+      a.run_rows[r] = all[0] - a.cu[r];
+    }
+    q = larger(q, k_all);
+    if (begin_all > 0) start = (int)begin_all - 1;
+  }
   team.sync();  // (nobody reads lengths and state from here on: they may be written in place)
-  in_batches(i0, i1, look, [&](int i, const One& o) {
-    if (!bad) p.length_out[i] = p.fresh[i] < 0 ? 0 : o.len + o.n;
+  for (int j = 0; j < steps; ++j) {
+    const int i = base + j * lanes;
+    if (i >= s.seqs) break;
+    if (!bad) p.length_out[i] = p.fresh[i] < 0 ? 0 : a.total[i];
     else if (p.length_out != p.length) p.length_out[i] = p.length[i];
     if (bad) a.cached[i] = a.total[i] = a.a_len[i] = 0, a.parent[i] = -1;
-  });
+  }
   if (team.tid() == 0) {
     const int to = first + (bad ? 0 : all[1]);
     p.state_out[0] = to >= s.num_pages && !bad ? to - s.num_pages : to;
     p.state_out[1] = bad ? spare : spare - all[1] + all[2];
   }
 
-  // blocks of all tiles, and from them the length of a part
-  const UnitView view(a, g);
+  // blocks of all tiles (of the units that UnitView describes), and from them the length of a part
   struct Units {
     int rows[2], blocks[2];
     bool run;
   };
+  Units kept{};
   int64_t w[2] = {0, 0};
-  in_batches(i0, i1, [&](int i) {
-    Units x;
-    for (int which = 0; which < 2; ++which) {
-      const PagedItem u = view.unit(i, which);
-      x.rows[which] = u.rows;
-      x.blocks[which] = view.blocks(u);
+  for (int j = 0; j < steps; ++j) {
+    const int i = base + j * lanes;
+    Units x{};
+    if (i < s.seqs) {
+      const int total = a.total[i], n = total - a.cached[i];
+      const int r = a.run[i], run_rows = r >= 0 ? a.run_rows[r] : 0, of_parent = paged_div(a.a_len[i], kPagedBlock);
+      x.run = n > 0 && run_rows > n;
+      x.rows[0] = n;
+      x.blocks[0] = (x.run ? 0 : of_parent) + paged_div(total, kPagedBlock);
+      x.rows[1] = x.run && r == i && of_parent > 0 ? run_rows : 0;
+      x.blocks[1] = of_parent;
+      if (!ONE) {  // for the two passes below, which write what belongs here
+        a.full0[2 * i] = x.rows[0];
+        a.full0[2 * i + 1] = x.rows[1];
+        a.last0[2 * i] = x.blocks[0];
+        a.last0[2 * i + 1] = x.blocks[1];
+        a.merge0[i] = x.run;
+      }
     }
-    x.run = view.in_run(i);
-    return x;
-  }, [&](int i, const Units& x) {
+    kept = x;
     for (int which = 0; which < 2; ++which) {
       const int tiles = paged_div(x.rows[which] * g, kTilePairs);
       w[0] += (int64_t)tiles * x.blocks[which];
       w[1] += tiles;
-      // for the two passes below, which write what belongs here
-      a.full0[2 * (int64_t)i + which] = x.rows[which];
-      a.last0[2 * (int64_t)i + which] = x.blocks[which];
     }
-    a.merge0[i] = x.run;
-  });
+  }
   team.sum(w);
   const int part = part_blocks(w[0], w[1], s, p.L.max_parts);
+  const CeilDiv by_part(part);
 
   // items: the parts of full length first, then the tiles' last ones; slots of partial results; merged rows
   int32_t c[4] = {0, 0, 0, 0}, at[4], sum[4], most_parts = 0;
   for (int pass = 0; pass < 2; ++pass) {
-    int32_t* const n = pass ? at : c;
-    in_batches(i0, i1, [&](int i) {
-      Units x;
-      for (int which = 0; which < 2; ++which) {
-        x.rows[which] = a.full0[2 * (int64_t)i + which];
-        x.blocks[which] = a.last0[2 * (int64_t)i + which];
-      }
-      x.run = a.merge0[i] != 0;
-      return x;
-    }, [&](int i, const Units& x) {
-      for (int which = 0; which < 2; ++which) {
-        const int tiles = paged_div(x.rows[which] * g, kTilePairs), parts = tiles ? paged_div(x.blocks[which], part) : 0;
-        const bool partial = tiles && (parts > 1 || which == 1 || x.run);
-        if (pass) {
-          const int64_t k = 2 * (int64_t)i + which;
-          a.full0[k] = n[0];
-          a.last0[k] = n[1];
-          a.slot0[k] = partial ? n[2] : -1;
-          a.parts[k] = parts;
-          if (which == 0) a.merge0[i] = partial ? n[3] : -1;
+    for (int j = 0; j < steps; ++j) {
+      const int i = base + j * lanes;
+      Units x = kept;
+      if (!ONE) {
+        x = Units{};
+        if (i < s.seqs) {
+          x.rows[0] = a.full0[2 * i];
+          x.rows[1] = a.full0[2 * i + 1];
+          x.blocks[0] = a.last0[2 * i];
+          x.blocks[1] = a.last0[2 * i + 1];
+          x.run = a.merge0[i] != 0;
         }
-        if (tiles) n[0] += tiles * (parts - 1), n[1] += tiles;
-        if (partial) n[2] += parts * paged_div(x.rows[which] * g, kSlotPairs);
-        if (partial && which == 0) n[3] += x.rows[which];
-        if (partial && parts > most_parts) most_parts = parts;
       }
-    });
-    if (!pass) team.scan(c, at, sum);
+      int32_t n[2][4], v[4] = {0, 0, 0, 0}, parts[2];
+      for (int which = 0; which < 2; ++which) {
+        const int tiles = paged_div(x.rows[which] * g, kTilePairs);
+        parts[which] = tiles ? by_part(x.blocks[which]) : 0;
+        const bool partial = tiles && (parts[which] > 1 || which == 1 || x.run);
+        n[which][0] = tiles ? tiles * (parts[which] - 1) : 0;
+        n[which][1] = tiles;
+        n[which][2] = partial ? parts[which] * paged_div(x.rows[which] * g, kSlotPairs) : 0;
+        n[which][3] = partial && which == 0 ? x.rows[which] : 0;
+        for (int k = 0; k < 4; ++k) v[k] += n[which][k];
+        if (partial && parts[which] > most_parts) most_parts = parts[which];
+      }
+      if (!pass) {
+        for (int k = 0; k < 4; ++k) c[k] += v[k];
+        continue;
+      }
+      int32_t total[4];
+      team.scan_lanes(v, total);
+      if (i < s.seqs)
+        for (int which = 0; which < 2; ++which) {
+          const int k = 2 * i + which;
+          for (int y = 0; y < 4; ++y)
+            if (which) v[y] += n[0][y];
+          a.full0[k] = at[0] + v[0];
+          a.last0[k] = at[1] + v[1];
+          a.slot0[k] = n[which][2] ? at[2] + v[2] : -1;
+          a.parts[k] = parts[which];
+          if (which == 0) a.merge0[i] = n[0][3] ? at[3] + v[3] : -1;
+        }
+      for (int k = 0; k < 4; ++k) at[k] += total[k];
+    }
+    if (!pass) team.scan_waves(c, at, sum);
   }
   most_parts = team.max_of(most_parts);
   if (team.tid() == 0) {

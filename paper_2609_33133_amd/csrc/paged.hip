@@ -1,5 +1,7 @@
 // The paged KV cache's plan and write kernels, and the merge of partial results
 // of its attention.
+#include <type_traits>
+
 #include "common.h"
 #include "paged.h"
 
@@ -9,121 +11,162 @@ namespace {
 constexpr int kPlanThreads = 1024;
 constexpr int kMergeAlone = 16;  // parts of a row up to which one group of lanes joins them
 
-// The threads of one workgroup, for plan_scan. Each reduction puts one value
+// x of the lane that a DPP control names, 0 where it names none.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int32_t dpp(int32_t x) {
+  return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false);
+}
+// f(x, value of an earlier lane) for an inclusive scan over the wavefront (N = 64) or each 16 lanes: rows of 16 by
+// shifts, then the rows' last lanes to the rows behind
+template <int N, class F>
+__device__ __forceinline__ void scan_by_dpp(F f) {
+  f(std::integral_constant<int, 0x111>(), std::integral_constant<int, 0xf>());
+  f(std::integral_constant<int, 0x112>(), std::integral_constant<int, 0xf>());
+  f(std::integral_constant<int, 0x114>(), std::integral_constant<int, 0xf>());
+  f(std::integral_constant<int, 0x118>(), std::integral_constant<int, 0xf>());
+  if constexpr (N == 64) {
+    f(std::integral_constant<int, 0x142>(), std::integral_constant<int, 0xa>());
+    f(std::integral_constant<int, 0x143>(), std::integral_constant<int, 0xc>());
+  }
+}
+template <int N>
+__device__ __forceinline__ int32_t sums(int32_t x) {
+  scan_by_dpp<N>([&](auto ctrl, auto rows) { x = add_count(x, dpp<decltype(ctrl)::value, decltype(rows)::value>(x)); });
+  return x;
+}
+template <int N>
+__device__ __forceinline__ int64_t sums64(int64_t x) {
+  scan_by_dpp<N>([&](auto ctrl, auto rows) {
+    const uint32_t lo = dpp<decltype(ctrl)::value, decltype(rows)::value>((int32_t)x);
+    const uint32_t hi = dpp<decltype(ctrl)::value, decltype(rows)::value>((int32_t)(x >> 32));
+    x += (int64_t)((uint64_t)hi << 32 | lo);
+  });
+  return x;
+}
+template <int N>
+__device__ __forceinline__ int64_t maxima(int64_t x) {  // of x >= 0
+  scan_by_dpp<N>([&](auto ctrl, auto rows) {
+    const uint32_t lo = dpp<decltype(ctrl)::value, decltype(rows)::value>((int32_t)x);
+    const uint32_t hi = dpp<decltype(ctrl)::value, decltype(rows)::value>((int32_t)(x >> 32));
+    const int64_t y = (int64_t)((uint64_t)hi << 32 | lo);
+    x = y > x ? y : x;
+  });
+  return x;
+}
+__device__ __forceinline__ int64_t lane64(int64_t x, int lane) {
+  const uint32_t lo = __builtin_amdgcn_readlane((int32_t)x, lane), hi = __builtin_amdgcn_readlane((int32_t)(x >> 32), lane);
+  return (int64_t)((uint64_t)hi << 32 | lo);
+}
+
+// The wavefronts of one workgroup, for plan_scan. Each reduction puts one value
 // per wavefront into LDS of its own turn's half, so that two barriers apart no
-// wavefront still reads what the next turn writes.
+// wavefront still reads what the next turn writes; every wavefront then scans
+// these values, one per lane. All instructions run on one CU, so they count:
+// scans by LDS shuffles, and totals added up by every thread in a loop, took
+// 11 of 29 us for 576 sequences.
 struct GroupTeam {
-  struct Wave {
-    int64_t key;
-    int32_t v[4], bits;
+  static constexpr int kWaves = kPlanThreads / 64;
+  struct Turn {
+    int64_t key[kWaves];
+    int32_t v[4][kWaves], bits[kWaves];
   };
-  Wave (*lds)[kPlanThreads / 64];  // [2]
+  Turn* lds;  // [2]
   int turn = 0;
   __device__ int tid() const { return threadIdx.x; }
-  __device__ int size() const { return kPlanThreads; }
+  __device__ int lane() const { return threadIdx.x & 63; }
+  __device__ int wave() const { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
+  __device__ int lanes() const { return 64; }
+  __device__ int waves() const { return kWaves; }
   __device__ void sync() const { __syncthreads(); }
   __device__ void flag(int32_t* to, int32_t bits) const { atomicOr(to, bits); }
-  __device__ Wave* next() { return lds[turn ^= 1]; }
+  __device__ Turn* next() { return lds + (turn ^= 1); }
 
+  // v: of the lanes before this one; total: of all lanes
   template <int K>
-  __device__ static void wave_scan(int32_t (&x)[K]) {
-    const int lane = threadIdx.x & 63;
+  __device__ void scan_lanes(int32_t (&v)[K], int32_t (&total)[K]) const {
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-#pragma unroll
-      for (int k = 0; k < K; ++k) {
-        const int32_t y = __shfl_up(x[k], d);
-        if (lane >= d) x[k] = add_count(x[k], y);
-      }
+    for (int k = 0; k < K; ++k) {
+      const int32_t x = sums<64>(v[k]);
+      v[k] = x - v[k];  // (exact where the sum has not stopped: a step whose sums stop is refused)
+      total[k] = __builtin_amdgcn_readlane(x, 63);
     }
   }
-  // sums over the threads before this one, and over all
-  template <int K>
-  __device__ void scan(const int32_t (&v)[K], int32_t (&before)[K], int32_t (&all)[K]) {
-    int64_t none = 0;
-    int bits = 0;
-    scan_step(v, before, all, none, bits);
+  // x >= 0: the largest of the lanes before this one, 0 at least; returns the largest of all lanes
+  __device__ int64_t max_lanes(int64_t& x) const {
+    const int64_t m = maxima<64>(x);
+    // (the lane before: shifted by one)
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int32_t)m, 0x138, 0xf, 0xf, false);
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int32_t)(m >> 32), 0x138, 0xf, 0xf, false);
+    x = (int64_t)((uint64_t)hi << 32 | lo);
+    return lane64(m, 63);
   }
-  // the same, the largest key of the threads before this one (0 at least), and the bits of all
+  // sums over the threads: of the wavefronts before this one, of all
   template <int K>
-  __device__ void scan_step(const int32_t (&v)[K], int32_t (&before)[K], int32_t (&all)[K], int64_t& key, int& bits) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    Wave* const to = next();
-    int32_t x[K];
+  __device__ void scan_waves(const int32_t (&v)[K], int32_t (&before)[K], int32_t (&all)[K]) {
+    Turn* const t = next();
+    const int w = wave();
 #pragma unroll
-    for (int k = 0; k < K; ++k) x[k] = v[k];
-    wave_scan(x);
-    int64_t m = key;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const int64_t y = __shfl_up((long long)m, d);
-      if (lane >= d && y > m) m = y;
+    for (int k = 0; k < K; ++k) {
+      const int32_t x = sums<64>(v[k]);
+      if (lane() == 63) t->v[k][w] = x;
     }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int32_t y = sums<kWaves>(lane() < kWaves ? t->v[k][lane()] : 0);
+      before[k] = w > 0 ? __builtin_amdgcn_readlane(y, w - 1) : 0;
+      all[k] = __builtin_amdgcn_readlane(y, kWaves - 1);
+    }
+  }
+  // the same, the largest key (>= 0) of the wavefronts before this one, and the bits of all
+  template <int K>
+  __device__ void scan_waves(const int32_t (&v)[K], int32_t (&before)[K], int32_t (&all)[K], int64_t& key, int& bits) {
+    const int64_t m = maxima<64>(key);
 #pragma unroll
     for (int b = 1; b <= PAGES_PAGE; b *= 2)
       if (__any(bits & b)) bits |= b;
-    if (lane == 63) {
-#pragma unroll
-      for (int k = 0; k < K; ++k) to[wave].v[k] = x[k];
-      to[wave].key = m;
-      to[wave].bits = bits;
+    Turn* const t = lds + (turn ^ 1);
+    const int w = wave();
+    if (lane() == 63) {
+      t->key[w] = m;
+      t->bits[w] = bits;
     }
-    __syncthreads();
-    const int64_t up = __shfl_up((long long)m, 1);
-    key = lane == 0 ? 0 : up;
+    scan_waves(v, before, all);
+    const int64_t y = maxima<kWaves>(lane() < kWaves ? t->key[lane()] : 0);
+    key = w > 0 ? lane64(y, w - 1) : 0;
+    const int other = lane() < kWaves ? t->bits[lane()] : 0;
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      before[k] = x[k] - v[k];  // (exact where the sum has not stopped: a step whose sums stop is refused)
-      all[k] = 0;
-    }
-    for (int w = 0; w < kPlanThreads / 64; ++w) {
-#pragma unroll
-      for (int k = 0; k < K; ++k) {
-        const int32_t y = to[w].v[k];
-        if (w < wave) before[k] = add_count(before[k], y);
-        all[k] = add_count(all[k], y);
-      }
-      if (w < wave && to[w].key > key) key = to[w].key;
-      bits |= to[w].bits;
-    }
+    for (int b = 1; b <= PAGES_PAGE; b *= 2)
+      if (__any(other & b)) bits |= b;
   }
-  // the largest value of the threads before this one, -1 at least
-  __device__ int scan_max(int v) {
-    const int32_t none[1] = {0};
-    int32_t a[1], b[1];
-    int64_t key = v + 1;
-    int bits = 0;
-    scan_step(none, a, b, key, bits);
-    return (int)key - 1;
+  // the largest value of the wavefronts before this one, -1 at least
+  __device__ int max_waves(int v) {
+    Turn* const t = next();
+    const int w = wave();
+    const int64_t x = maxima<64>((int64_t)v + 1);
+    if (lane() == 63) t->key[w] = x;
+    __syncthreads();
+    const int64_t y = maxima<kWaves>(lane() < kWaves ? t->key[lane()] : 0);
+    return w > 0 ? (int)lane64(y, w - 1) - 1 : -1;
+  }
+  __device__ int max_of(int v) {  // of v >= 0
+    Turn* const t = next();
+    const int64_t x = maxima<64>(v);
+    if (lane() == 63) t->key[wave()] = x;
+    __syncthreads();
+    return (int)lane64(maxima<kWaves>(lane() < kWaves ? t->key[lane()] : 0), kWaves - 1);
   }
   __device__ void sum(int64_t (&v)[2]) {
-    Wave* const to = next();
-#pragma unroll
-    for (int d = 32; d > 0; d /= 2) {
-      v[0] += __shfl_xor((long long)v[0], d);
-      v[1] += __shfl_xor((long long)v[1], d);
-    }
-    if ((threadIdx.x & 63) == 0) {
-      to[threadIdx.x >> 6].key = v[0];
-      __builtin_memcpy(to[threadIdx.x >> 6].v, &v[1], 8);
+    Turn* const t = next();
+    int64_t* const second = reinterpret_cast<int64_t*>(t->v);
+    const int64_t x = sums64<64>(v[0]), y = sums64<64>(v[1]);
+    if (lane() == 63) {
+      t->key[wave()] = x;
+      second[wave()] = y;
     }
     __syncthreads();
-    v[0] = v[1] = 0;
-    for (int w = 0; w < kPlanThreads / 64; ++w) {
-      int64_t y;
-      __builtin_memcpy(&y, to[w].v, 8);
-      v[0] += to[w].key;
-      v[1] += y;
-    }
-  }
-  __device__ int max_of(int v) {
-    Wave* const to = next();
-#pragma unroll
-    for (int d = 32; d > 0; d /= 2) v = max(v, __shfl_xor(v, d));
-    if ((threadIdx.x & 63) == 0) to[threadIdx.x >> 6].v[0] = v;
-    __syncthreads();
-    for (int w = 0; w < kPlanThreads / 64; ++w) v = max(v, to[w].v[0]);
-    return v;
+    v[0] = lane64(sums64<kWaves>(lane() < kWaves ? t->key[lane()] : 0), kWaves - 1);
+    v[1] = lane64(sums64<kWaves>(lane() < kWaves ? second[lane()] : 0), kWaves - 1);
   }
 };
 
@@ -132,15 +175,15 @@ struct GroupTeam {
 // by latency: a dozen barriers and the memory round trips between them. TODO_FIGURE
 template <bool FILL>
 __global__ __launch_bounds__(kPlanThreads) void page_plan_kernel(PlanParams p) {
-  __shared__ GroupTeam::Wave lds[2][kPlanThreads / 64];
+  __shared__ GroupTeam::Turn lds[2];
   GroupTeam team{lds};
   if constexpr (FILL) {
     __shared__ int32_t work[18 * kFillSeqs + 1];
     const PlanArrays a = PlanArrays::packed(work, p.s.seqs);
-    plan_scan(team, p, a);
+    plan_scan<true>(team, p, a);
     plan_fill(team, p, a, threadIdx.x, kPlanThreads);
   } else {
-    plan_scan(team, p, plan_arrays(p));
+    plan_scan<false>(team, p, plan_arrays(p));
   }
 }
 

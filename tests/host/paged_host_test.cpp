@@ -63,24 +63,37 @@ struct Shared {
   }
 };
 
+// Threads in place of the kernel's wavefronts, one lane each.
 struct ThreadTeam {
   Shared& s;
   int id;
   int tid() const { return id; }
-  int size() const { return s.n; }
+  int lane() const { return 0; }
+  int wave() const { return id; }
+  int lanes() const { return 1; }
+  int waves() const { return s.n; }
   void sync() const { s.barrier(); }
   void flag(int32_t* to, int32_t b) const {
     std::lock_guard<std::mutex> l(g_lock);
     *to |= b;
   }
   template <int K>
-  void scan(const int32_t (&v)[K], int32_t (&before)[K], int32_t (&all)[K]) const {
-    int64_t key = 0;
-    int b = 0;
-    scan_step(v, before, all, key, b);
+  void scan_lanes(int32_t (&v)[K], int32_t (&total)[K]) const {
+    for (int k = 0; k < K; ++k) total[k] = v[k], v[k] = 0;
+  }
+  int64_t max_lanes(int64_t& x) const {
+    const int64_t all = x;
+    x = 0;
+    return all;
   }
   template <int K>
-  void scan_step(const int32_t (&v)[K], int32_t (&before)[K], int32_t (&all)[K], int64_t& key, int& bits) const {
+  void scan_waves(const int32_t (&v)[K], int32_t (&before)[K], int32_t (&all)[K]) const {
+    int64_t key = 0;
+    int b = 0;
+    scan_waves(v, before, all, key, b);
+  }
+  template <int K>
+  void scan_waves(const int32_t (&v)[K], int32_t (&before)[K], int32_t (&all)[K], int64_t& key, int& bits) const {
     s.sums[id].assign(v, v + K);
     s.keys[id] = key;
     s.bits[id] = bits;
@@ -99,12 +112,12 @@ struct ThreadTeam {
     }
     s.barrier();
   }
-  int scan_max(int v) const {
+  int max_waves(int v) const {
     const int32_t none[1] = {0};
     int32_t a[1], b[1];
     int64_t key = v + 1;
     int bits = 0;
-    scan_step(none, a, b, key, bits);
+    scan_waves(none, a, b, key, bits);
     return (int)key - 1;
   }
   void sum(int64_t (&v)[2]) const {
@@ -161,7 +174,8 @@ Result run(const Step& st, int threads, bool in_place) {
   for (int t = 0; t < threads; ++t)
     pool.emplace_back([&, t] {
       ThreadTeam team{sh, t};
-      plan_scan(team, p, arrays);
+      if (threads >= st.s.seqs) plan_scan<true>(team, p, arrays);
+      else plan_scan<false>(team, p, arrays);
     });
   for (auto& t : pool) t.join();
   // the rest by threads one after the other
