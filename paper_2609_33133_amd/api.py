@@ -304,6 +304,12 @@ def tree_bwd(b: GroupBatch, q_p, k_p, v_p, o_p, lse_p, do_p, q_r, k_r, v_r, o_r,
 
 # ---------------------------------------------------------------------------- linear attention layer
 
+# What torch.cuda.current_device() and current_stream().cuda_stream end in, without their 3 us (the tensors are on a GPU:
+# torch.cuda is initialised).
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
 class _On:
     """The device of a call's tensors made current, with the stream it runs on there. Every tensor has to be on that
     device (a stream given by the caller too)."""
@@ -329,11 +335,11 @@ class _On:
     def __enter__(self):
         if self.stream is not None:  # what is allocated inside belongs to that stream
             self.guard = torch.cuda.stream(self.stream)
-        elif self.device.index != torch.cuda.current_device():
+        elif self.device.index != _current_device():
             self.guard = torch.cuda.device(self.device)
         if self.guard is not None:
             self.guard.__enter__()
-        return torch.cuda.current_stream().cuda_stream
+        return _raw_stream(self.device.index)
 
     def __exit__(self, *exc):
         if self.guard is not None:
@@ -613,6 +619,23 @@ class PageTable:
         self.struct = _lib.Pages(seqs, self.max_pages, self.num_pages, self.page_size, _addr(table), _addr(length),
                                  _addr(parent), _addr(free_pages), _addr(free_state))
         self.ref = ctypes.byref(self.struct)
+        self._sizes = {}
+
+    def _plan_sizes(self, rows: int, hq: int, hkv: int):
+        """Words of a plan, offsets of its fields, and a dict of the workspaces of its attention; kept for the last few
+        sizes."""
+        found = self._sizes.get((rows, hq, hkv))
+        if found is None:
+            lib = _lib.load()
+            n = lib.augtree_page_plan_size(self.ref, rows, hq, hkv)
+            if n == 0:
+                raise _lib.AugtreeError(_lib.AUGTREE_ERR_INVALID_ARGUMENT, "page_plan_size",
+                                        lib.augtree_last_error().decode())
+            if len(self._sizes) >= 64:
+                self._sizes.clear()
+            at = tuple(lib.augtree_page_plan_offset(self.ref, rows, hq, hkv, f) for f in range(4))
+            found = self._sizes[rows, hq, hkv] = n // 4, at, {}
+        return found
 
     @classmethod
     def empty(cls, num_seqs: int, max_pages: int, num_pages: int, page_size: int, device="cuda") -> "PageTable":
@@ -628,18 +651,12 @@ class PagePlan:
     on the GPU."""
 
     def __init__(self, pages: PageTable, rows: int, num_q_heads: int, num_kv_heads: int):
-        lib = _lib.load()
         self.pages, self.rows, self.hq, self.hkv = pages, int(rows), int(num_q_heads), int(num_kv_heads)
-        n = lib.augtree_page_plan_size(pages.ref, self.rows, self.hq, self.hkv)
-        if n == 0:
-            raise _lib.AugtreeError(_lib.AUGTREE_ERR_INVALID_ARGUMENT, "page_plan_size",
-                                    lib.augtree_last_error().decode())
-        self.data = torch.empty(n // 4, dtype=torch.int32, device=pages.device)
-        self._ws_bytes = {}
+        self._words, self._at, self._ws_bytes = pages._plan_sizes(self.rows, self.hq, self.hkv)
+        self.data = torch.empty(self._words, dtype=torch.int32, device=pages.device)
 
     def _field(self, field: int, count: int) -> torch.Tensor:
-        at = _lib.load().augtree_page_plan_offset(self.pages.ref, self.rows, self.hq, self.hkv, field)
-        return self.data[at:at + count]
+        return self.data[self._at[field]:self._at[field] + count]
 
     @property
     def status(self) -> torch.Tensor:
@@ -730,6 +747,8 @@ def _cache(t, name: str, plan: PagePlan, d: int):
     shape = (pages.num_pages, plan.hkv, pages.page_size, d)
     if t.shape != shape:
         raise ValueError(f"{name}: shape {tuple(t.shape)}, expected {shape}")
+    if t.is_contiguous():
+        return kind, plan.hkv * pages.page_size * d * size
     stride, page = t.stride(), pages.page_size * d
     if stride[3] != 1 or stride[2] != d or (stride[1] != page and plan.hkv > 1):
         raise ValueError(f"{name} must be contiguous but for its first dimension")
