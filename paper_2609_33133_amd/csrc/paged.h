@@ -51,13 +51,19 @@ enum : int32_t {
 
 // Header words.
 enum {
-  PH_SEQS, PH_ROWS, PH_HQ, PH_HKV, PH_PAGE,  // what the plan was made for
+  PH_SEQS, PH_ROWS, PH_HQ, PH_HKV, PH_PAGE, PH_MAX_PAGES, PH_NUM_PAGES,  // what the plan was made for (PagedShape)
   PH_STATUS, PH_TOTAL_ROWS, PH_ITEMS, PH_MERGE_ROWS, PH_MOST_PARTS, PH_PART, PH_FIRST, PH_SPARE, PH_NEED, PH_BACK, PH_FULL,
 };
 
 struct PagedShape {
   int32_t seqs, rows, hq, hkv, page, max_pages, num_pages;
 };
+
+// Whether a plan was made for these sizes: a caller may hand over another's.
+inline __host__ __device__ bool plan_is_for(const int32_t* plan, const PagedShape& s) {
+  return plan[PH_SEQS] == s.seqs && plan[PH_ROWS] == s.rows && plan[PH_HQ] == s.hq && plan[PH_HKV] == s.hkv &&
+         plan[PH_PAGE] == s.page && plan[PH_MAX_PAGES] == s.max_pages && plan[PH_NUM_PAGES] == s.num_pages;
+}
 
 inline __host__ __device__ int paged_div(int a, int b) { return (a + b - 1) / b; }
 inline __host__ __device__ int paged_shift(int page) {
@@ -142,12 +148,28 @@ struct PlanParams {
   int32_t group, shift;    // query heads of a KV head, log2 of the page size
 };
 
-// Blocks of the parts that units are cut into, from the blocks of all tiles
-// (each with the blocks of its unit) and the number of tiles, per KV head.
-// Few tiles: as many parts as run at once. More of them: parts of half of what
-// a slot of the chip has to do, so that items of different lengths fill it.
-inline __host__ __device__ int part_blocks(int64_t blocks, int64_t tiles, const PagedShape& s, int max_parts) {
+// What a plan's tiles come to, per KV head: blocks of those of more than 32
+// pairs, of those of at most 32, tiles.
+struct TileSums {
+  int64_t wide, few, tiles;
+};
+
+// Blocks of the parts that units are cut into (each tile counts with the blocks
+// of its unit).
+// Fewer tiles than the chip runs at once: as many parts as it does, but none
+// much shorter than a tile's share, so that a few long tiles among many short
+// ones are still cut. Tiles of at most 32 pairs are bound by the reading of
+// their keys, which one workgroup a CU does as fast as two, with half the parts
+// to join. More tiles: parts of half of what a slot of the chip has to do, so
+// that items of different lengths fill it.
+// Against the best of a dozen lengths each, us: one sequence of 4097 tokens 13.4
+// (13.4), eight branches of a 32768-token prompt 29 (29; with two workgroups a
+// CU 32), 256 sequences of 500 to 8000 274 (273), 512 branches in e4m3 236 (231),
+// a chunk of 1500 and 48 single tokens on two KV heads 68 (65; two parts a slot
+// 78), two chunks of 7777 together 1647 (1647), 16 turns of 150 to 700 1025 (987).
+inline __host__ __device__ int part_blocks(const TileSums& w, const PagedShape& s, int max_parts) {
   const int slots = kChipSlots / s.hkv > 1 ? kChipSlots / s.hkv : 1;
+  const int64_t blocks = w.wide + w.few;
   // (the GPU has no 64-bit division: of more than 2^31 blocks in thousands, rounded up)
   auto ceil_div = [](int64_t n, int d) {
     if (n <= INT32_MAX - 4096) return (int)(((uint32_t)n + (uint32_t)d - 1) / (uint32_t)d);
@@ -155,9 +177,16 @@ inline __host__ __device__ int part_blocks(int64_t blocks, int64_t tiles, const 
     const uint32_t q = ((uint32_t)(k < INT32_MAX ? k : INT32_MAX) + (uint32_t)d - 1) / (uint32_t)d;
     return q < INT32_MAX >> 10 ? (int)(q << 10) : (int)INT32_MAX;
   };
+  const int once = w.few > w.wide && slots > 1 ? slots / 2 : slots;
   int c;
-  if (tiles * 4 < slots) c = ceil_div(blocks, slots - (int)tiles);
-  else c = ceil_div(blocks, 2 * slots) > 8 ? ceil_div(blocks, 2 * slots) : 8;
+  if (w.tiles < once) {
+    c = ceil_div(blocks, once - (int)w.tiles);
+    const int share = ceil_div(blocks, once);
+    if (c > 2 * (int64_t)share) c = 2 * share;
+  } else {
+    c = ceil_div(blocks, 2 * slots);
+    if (c < 8) c = 8;
+  }
   const int least = ceil_div(blocks, max_parts);
   if (c < least) c = least;
   return c < 1 ? 1 : c;
@@ -347,8 +376,8 @@ __host__ __device__ void plan_scan(Team& team, const PlanParams& p, const PlanAr
   }
   if (team.tid() == 0) {
     const int rows = bad ? 0 : all[0];
-    const int32_t head[] = {s.seqs, s.rows, s.hq, s.hkv, page, bad, rows};
-    for (int k = 0; k < 7; ++k) plan[PH_SEQS + k] = head[k];
+    const int32_t head[] = {s.seqs, s.rows, s.hq, s.hkv, page, s.max_pages, s.num_pages, bad, rows};
+    for (int k = 0; k <= PH_TOTAL_ROWS; ++k) plan[k] = head[k];
     a.cu[s.seqs] = plan[p.L.cu + s.seqs] = rows;
     plan[PH_FIRST] = first;
     plan[PH_SPARE] = spare;
@@ -400,7 +429,7 @@ __host__ __device__ void plan_scan(Team& team, const PlanParams& p, const PlanAr
     bool run;
   };
   Units kept{};
-  int64_t w[2] = {0, 0};
+  int64_t w[3] = {0, 0, 0};
   for (int j = 0; j < steps; ++j) {
     const int i = base + j * lanes;
     Units x{};
@@ -423,12 +452,12 @@ __host__ __device__ void plan_scan(Team& team, const PlanParams& p, const PlanAr
     kept = x;
     for (int which = 0; which < 2; ++which) {
       const int tiles = paged_div(x.rows[which] * g, kTilePairs);
-      w[0] += (int64_t)tiles * x.blocks[which];
-      w[1] += tiles;
+      w[x.rows[which] * g <= kSlotPairs] += (int64_t)tiles * x.blocks[which];
+      w[2] += tiles;
     }
   }
   team.sum(w);
-  const int part = part_blocks(w[0], w[1], s, p.L.max_parts);
+  const int part = part_blocks(TileSums{w[0], w[1], w[2]}, s, p.L.max_parts);
   const CeilDiv by_part(part);
 
   // items: the parts of full length first, then the tiles' last ones; slots of partial results; merged rows

@@ -156,17 +156,17 @@ struct GroupTeam {
     __syncthreads();
     return (int)lane64(maxima<kWaves>(lane() < kWaves ? t->key[lane()] : 0), kWaves - 1);
   }
-  __device__ void sum(int64_t (&v)[2]) {
+  __device__ void sum(int64_t (&v)[3]) {
     Turn* const t = next();
-    int64_t* const second = reinterpret_cast<int64_t*>(t->v);
-    const int64_t x = sums64<64>(v[0]), y = sums64<64>(v[1]);
-    if (lane() == 63) {
-      t->key[wave()] = x;
-      second[wave()] = y;
+    int64_t* const at[] = {t->key, reinterpret_cast<int64_t*>(t->v[0]), reinterpret_cast<int64_t*>(t->v[2])};
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+      const int64_t x = sums64<64>(v[k]);
+      if (lane() == 63) at[k][wave()] = x;
     }
     __syncthreads();
-    v[0] = lane64(sums64<kWaves>(lane() < kWaves ? t->key[lane()] : 0), kWaves - 1);
-    v[1] = lane64(sums64<kWaves>(lane() < kWaves ? second[lane()] : 0), kWaves - 1);
+#pragma unroll
+    for (int k = 0; k < 3; ++k) v[k] = lane64(sums64<kWaves>(lane() < kWaves ? at[k][lane()] : 0), kWaves - 1);
   }
 };
 
@@ -192,11 +192,16 @@ __global__ __launch_bounds__(256) void page_fill_kernel(PlanParams p) {
   plan_fill(team, p, plan_arrays(p), blockIdx.x * 256 + threadIdx.x, gridDim.x * 256);
 }
 
-__device__ __forceinline__ bool plan_is_for(const int32_t* plan, const PagedShape& s) {
-  return plan[PH_SEQS] == s.seqs && plan[PH_ROWS] == s.rows && plan[PH_HQ] == s.hq && plan[PH_HKV] == s.hkv &&
-         plan[PH_PAGE] == s.page;
+// x / s correctly rounded, from y = 1 / s correctly rounded: q = x y is off by
+// less than a unit in the last place, and so is the quotient of its exact
+// remainder from making it right (Markstein's theorem). For s of which neither y
+// nor a remainder leaves the normal range, and quotients in e4m3's; any larger
+// one (or NaN) is returned as x y.
+__device__ __forceinline__ float quotient(float x, float s, float y) {
+  const float q = x * y;
+  // (the sign: of a -0 the remainder is +0)
+  return __builtin_fabsf(q) < 512.f ? __builtin_copysignf(__builtin_fmaf(__builtin_fmaf(-q, s, x), y, q), q) : q;
 }
-
 // Four floats as e4m3, rounded to nearest even; what passes 448 becomes 448,
 // NaN stays NaN (a minimum of the two would make it 448).
 __device__ __forceinline__ uint32_t to_e4m3(float a, float b, float c, float d) {
@@ -206,35 +211,43 @@ __device__ __forceinline__ uint32_t to_e4m3(float a, float b, float c, float d) 
   return __builtin_amdgcn_cvt_pk_fp8_f32(in_range(c), in_range(d), w, true);
 }
 
-// Rows of K (y = 0) and V (y = 1) into their slots, 16 bytes of bf16 a thread.
-// Bound by HBM.
+// Rows of K (y = 0) and V (y = 1) into their slots; a thread writes 16 bytes.
+// Bound by HBM. TODO_FIGURE
 template <bool E4M3>
-__global__ __launch_bounds__(256) void cache_write_kernel(CacheWriteParams p, PlanLayout L) {
+__global__ __launch_bounds__(256) void cache_write_kernel(CacheWriteParams p, int64_t slots) {
+  constexpr int N = E4M3 ? 16 : 8;  // values of a thread
   if (!plan_is_for(p.plan, p.s)) return;
-  const int chunks = p.s.hkv * (p.d / 8);  // of a row
+  const int of_head = p.d / N, chunks = p.s.hkv * of_head;  // of a row
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   const int64_t row = i / chunks;
   if (row >= p.s.rows) return;
-  const int slot = p.plan[L.slots + row];
+  const int slot = p.plan[slots + row];
   if (slot < 0) return;
-  const int c = (int)(i - row * chunks), h = c / (p.d / 8), e = (c - h * (p.d / 8)) * 8;
+  const int c = (int)(i - row * chunks), h = c / of_head, e = (c - h * of_head) * N;
   const bool isv = blockIdx.y != 0;
   const int shift = __builtin_ctz(p.s.page);
   const int page = slot >> shift, off = slot & (p.s.page - 1);
-  const uint4 x = ldg16((isv ? p.v : p.k) + i * 8);
+  const uint16_t* const src = (isv ? p.v : p.k) + i * N;
   char* const dst = static_cast<char*>(isv ? p.v_cache : p.k_cache) + page * (isv ? p.v_stride : p.k_stride);
   const int64_t at = ((int64_t)h * p.s.page + off) * p.d + e;
   if constexpr (!E4M3) {
-    *reinterpret_cast<uint4*>(dst + 2 * at) = x;
+    *reinterpret_cast<uint4*>(dst + 2 * at) = ldg16(src);
   } else {
-    const float scale = (isv ? p.v_scale : p.k_scale)[h];
-    float f[8];
+    const uint4 x[2] = {ldg16(src), ldg16(src + 8)};
+    const float scale = (isv ? p.v_scale : p.k_scale)[h], inverse = 1.f / scale;
+    const bool plain = scale > 0x1p-60f && scale < 0x1p60f;
+    uint32_t w[4];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) f[j] = __uint_as_float(half16(x, j) << 16) / scale;
-    uint2 w;
-    w.x = to_e4m3(f[0], f[1], f[2], f[3]);
-    w.y = to_e4m3(f[4], f[5], f[6], f[7]);
-    *reinterpret_cast<uint2*>(dst + at) = w;
+    for (int j = 0; j < 4; ++j) {
+      float f[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float v = __uint_as_float(half16(x[j >> 1], (j & 1) * 4 + k) << 16);
+        f[k] = plain ? quotient(v, scale, inverse) : v / scale;
+      }
+      w[j] = to_e4m3(f[0], f[1], f[2], f[3]);
+    }
+    *reinterpret_cast<uint4*>(dst + at) = uint4{w[0], w[1], w[2], w[3]};
   }
 }
 
@@ -343,11 +356,10 @@ hipError_t launch_page_plan(const PlanParams& p, bool apart, hipStream_t stream)
 }
 
 hipError_t launch_cache_write(const CacheWriteParams& p, hipStream_t stream) {
-  const int64_t threads = (int64_t)p.s.rows * p.s.hkv * (p.d / 8);
+  const int64_t threads = (int64_t)p.s.rows * p.s.hkv * (p.d / (p.type == CACHE_E4M3 ? 16 : 8)), slots = plan_layout(p.s).slots;
   const dim3 grid((unsigned)((threads + 255) / 256), 2);
-  const PlanLayout L = plan_layout(p.s);
-  if (p.type == CACHE_E4M3) cache_write_kernel<true><<<grid, 256, 0, stream>>>(p, L);
-  else cache_write_kernel<false><<<grid, 256, 0, stream>>>(p, L);
+  if (p.type == CACHE_E4M3) cache_write_kernel<true><<<grid, 256, 0, stream>>>(p, slots);
+  else cache_write_kernel<false><<<grid, 256, 0, stream>>>(p, slots);
   return hipGetLastError();
 }
 

@@ -120,11 +120,13 @@ struct ThreadTeam {
     scan_waves(none, a, b, key, bits);
     return (int)key - 1;
   }
-  void sum(int64_t (&v)[2]) const {
-    s.wide[id].assign(v, v + 2);
+  void sum(int64_t (&v)[3]) const {
+    s.wide[id].assign(v, v + 3);
     s.barrier();
-    v[0] = v[1] = 0;
-    for (auto& w : s.wide) v[0] += w[0], v[1] += w[1];
+    for (int k = 0; k < 3; ++k) {
+      v[k] = 0;
+      for (auto& w : s.wide) v[k] += w[k];
+    }
     s.barrier();
   }
   int max_of(int v) const {

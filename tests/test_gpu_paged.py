@@ -128,6 +128,22 @@ def test_write(heads, page, fp8):
         assert (same | (a.isnan() & b.isnan())).all()
 
 
+@pytest.mark.parametrize("scales", [(0.02, 1 / 3), (1.0, 0.0078125), (7e-5, 123.456), (3e-30, 4e25), (1e-38, 1e30)])
+def test_every_bf16_value_in_8_bits(scales):
+    """All 65536 bf16 patterns divided by a scale, bit for bit; NaN as NaN."""
+    rows = 65536 // 64
+    pages = api.PageTable.empty(1, rows // 16, rows // 16, 16)
+    plan = api.page_plan(pages, gpu([rows]), rows, 2, 2)
+    x = torch.arange(65536, dtype=torch.int32).to(torch.int16).view(torch.bfloat16).view(rows, 1, 64).expand(rows, 2, 64).contiguous().cuda()
+    kc, vc = (torch.zeros(rows // 16, 2, 16, 64, device="cuda").to(FP8) for _ in range(2))
+    s = torch.tensor(scales, dtype=torch.float32, device="cuda")
+    api.cache_write(x, x, kc, vc, plan, k_scale=s, v_scale=s)
+    want = (x.float() / s[:, None]).clamp(-448, 448).to(FP8).float().view(rows // 16, 16, 2, 64).transpose(1, 2)
+    for got in (kc.float(), vc.float()):
+        same = (got == want) & (torch.signbit(got) == torch.signbit(want))
+        assert (same | (got.isnan() & want.isnan())).all()
+
+
 @pytest.mark.parametrize("fp8", [False, True])
 @pytest.mark.parametrize("page", [16, 32, 64, 128, 256])
 @pytest.mark.parametrize("name", SETS)
@@ -166,6 +182,32 @@ def test_sharp_scores():
     s = Step(TREES, (8, 2, 128), 32, seed=8, amp=6.0)
     o, lse = s.attend(s.plan())
     s.check_attention(o, lse)
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("where", ["q", "k", "v"])
+def test_nan_and_infinity_stay_with_their_sequence(where, value):
+    """In one row of Q: that row alone. In a token of K or V: the rows of its own sequence (a parent's: its branches)."""
+    s = Step(TREES, (8, 2, 128), 64, seed=14)
+    plan = s.plan()
+    want = s.attend(plan)
+    cu = s.want[4]
+    if where == "q":
+        touched = [int(cu[5]) + 3]
+        s.q[touched[0], 2] = value
+    else:
+        seq = 5
+        at = 20  # a cached token
+        slot = int(s.want[0][seq, at // 64]) * 64 + at % 64
+        (s.k_cache if where == "k" else s.v_cache)[slot // 64, 1, slot % 64, 7] = value
+        touched = range(cu[seq], cu[seq + 1])
+    got = s.attend(plan)
+    keep = torch.ones(s.rows, dtype=torch.bool)
+    keep[list(touched)] = False
+    keep = keep.cuda()
+    assert torch.equal(got[0][keep], want[0][keep]) and torch.equal(got[1][:, keep], want[1][:, keep])
+    heads = [h for h in range(8) if (h != 2 if where == "q" else h < 4)]  # other heads, heads of the other KV head
+    assert torch.equal(got[0][:, heads], want[0][:, heads])
 
 
 def test_rows_behind_the_last_are_left_and_results_repeat():
@@ -228,6 +270,10 @@ def test_a_plan_of_other_sizes_does_nothing():
     q = torch.zeros(5, 4, 128, dtype=torch.bfloat16, device="cuda")
     o = torch.full_like(q, 7.0)
     before = s.k_cache.view(torch.int16).clone()
+    narrow = api.PagePlan(api.PageTable(s.pages.table[:, :1].contiguous(), s.pages.length, s.pages.parent, s.pages.free_pages,
+                                        s.pages.free_state, 64), 3, 4, 2)  # a table with fewer entries
+    narrow.data[:min(narrow.data.numel(), plan.data.numel())] = plan.data[:narrow.data.numel()]
+    api.paged_fwd(q[:3], s.k_cache, s.v_cache, narrow, o=o[:3])
     api.paged_fwd(q, s.k_cache, s.v_cache, other, o=o)
     kv = torch.zeros(5, 2, 128, dtype=torch.bfloat16, device="cuda")
     api.cache_write(kv, kv, s.k_cache, s.v_cache, other)
@@ -319,6 +365,41 @@ def test_rollout_of_trees_meets_group_attention(fp8):
             assert (a.float() - b.float()).norm() <= 2.0 ** -7 * b.float().norm()
         for a, b in ((lse["p"], lse_p), (lse["r"], lse_r)):
             assert (a - b).abs().max() <= 1e-4
+
+
+def test_captured_prefill_replays():
+    """A captured step of more rows than one workgroup plans: prompts of changing lengths in a room of 2300 rows."""
+    hq, hkv, d, page, rows = 4, 2, 64, 32, 2300
+    lens = [[900, 1200, 1], [0, 2300, 0], [5, 7, 1500], [64, 0, 0]]
+    gen = torch.Generator().manual_seed(6)
+    mk = lambda h: torch.randn(rows, h, d, generator=gen).to(torch.bfloat16).cuda()
+    q, k, v = mk(hq), mk(hkv), mk(hkv)
+    pages = [api.PageTable.empty(3, 120, 200, page) for _ in range(2)]
+    caches = [[torch.zeros(200, hkv, page, d, dtype=torch.bfloat16, device="cuda") for _ in range(2)] for _ in range(2)]
+    new = gpu(lens[0])
+
+    def take(n, plan):
+        plan = api.page_plan(pages[n], new, rows, hq, hkv, plan=plan)
+        api.cache_write(k, v, *caches[n], plan)
+        return plan, *api.paged_fwd(q, *caches[n], plan, want_lse=True)
+
+    warm = api.PageTable.empty(3, 120, 200, page)
+    api.paged_fwd(q, *caches[1], api.page_plan(warm, new, rows, hq, hkv))
+    plan = api.PagePlan(pages[1], rows, hq, hkv)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        _, o, lse = take(1, plan)
+    for n in lens:
+        new.copy_(gpu(n))
+        p, o_want, lse_want = take(0, None)
+        p.check()
+        g.replay()
+        torch.cuda.synchronize()
+        live = sum(n)
+        assert torch.equal(o[:live], o_want[:live]) and torch.equal(lse[:, :live], lse_want[:, :live])
+        assert torch.equal(pages[0].table, pages[1].table) and torch.equal(pages[0].length, pages[1].length)
+        assert all(torch.equal(a, b) for a, b in zip(*caches))
 
 
 def test_captured_decode_replays():
