@@ -390,9 +390,9 @@ def _out(t, name, dtype, shape, device):
 def _written(given):
     """Counts a call's writes to the caller's own tensors as torch's in-place operations count theirs, so that a backward
     which saved one of them notices."""
-    for t in given:
-        if t is not None:
-            torch.autograd.graph.increment_version(t)
+    given = [t for t in given if t is not None]
+    if given:
+        torch.autograd.graph.increment_version(given)
 
 
 def _check_batch(b: GroupBatch):
@@ -805,15 +805,18 @@ def paged_fwd(q, k_cache, v_cache, plan: PagePlan, k_scale=None, v_scale=None, o
     given = (o, lse, ws)
     _want_ws(ws, "ws")
     with on as st:
-        o = _out(o, "o", torch.bfloat16, q.shape, on.device)
+        if o is None:
+            o = torch.empty_like(q)
+        else:
+            _want(o, "o", torch.bfloat16, q.shape)
         if want_lse or lse is not None:
             lse = _out(lse, "lse", torch.float32, (plan.hq, plan.rows), on.device)
+        n = plan.workspace_size(d) if ws is None else ws.numel()
         if ws is None:
-            ws = torch.empty(plan.workspace_size(d), dtype=torch.uint8, device=on.device)
+            ws = plan.data.new_empty(n // 4)
         _lib.check(_lib.load().augtree_paged_fwd(
             plan.pages.ref, _addr(plan.data), plan.rows, plan.hq, plan.hkv, d,
             1.0 / math.sqrt(d) if scale is None else float(scale), _addr(q), kind, _addr(k_cache), k_stride,
-            _addr(v_cache), v_stride, _addr(k_scale), _addr(v_scale), _addr(o), _addr(lse), _addr(ws), ws.numel(), st),
-            "paged_fwd")
+            _addr(v_cache), v_stride, _addr(k_scale), _addr(v_scale), _addr(o), _addr(lse), _addr(ws), n, st), "paged_fwd")
     _written(given)
     return o, lse
