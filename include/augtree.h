@@ -488,6 +488,11 @@ size_t augtree_head_norm_workspace_size(int64_t rows, int32_t heads, int32_t hea
  * into a graph and replayed. Calls that share a plan being written, or a
  * workspace, must not overlap. Results are bitwise reproducible; how work is cut
  * (and so the last bits) follows from the batch.
+ * A NaN or infinity in a row of q stays in that row and head. In a token of K or V
+ * it reaches the rows that see the token, in the query heads of its KV head, and
+ * perhaps (in V) earlier new rows of the same sequence within the token's 64 keys;
+ * never another sequence but a parent's branches. (A result that it reaches need
+ * not be NaN.)
  * ------------------------------------------------------------------------- */
 
 /* Tables of a cache (DEVICE arrays, owned by the caller), shared by all layers. */
