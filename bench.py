@@ -132,10 +132,12 @@ def kernel_source_hash() -> str:
     """Hash of the code (comments and whitespace removed) of every native
     source the attention kernels and their schedules are built from, and of
     the compile flags: HBM counters recorded under one hash do not describe
-    another. (The linear-attention layer's sources are not part of a step.)"""
+    another. (The sources of the linear-attention layer and of the paged
+    cache are not part of a step.)"""
     h = hashlib.sha256()
     for path in sorted(glob.glob(os.path.join(ROOT, "paper_2609_33133_amd", "csrc", "*"))):
-        if path.endswith((".hip", ".h", ".cpp")) and not os.path.basename(path).startswith(("linear", "head_norm")):
+        if path.endswith((".hip", ".h", ".cpp")) and not os.path.basename(path).startswith(
+                ("linear", "head_norm", "host_checks", "paged", "attn_paged")):
             with open(path) as f:
                 code = f.read()
             code = re.sub(r"/\*.*?\*/", " ", code, flags=re.S)
