@@ -597,7 +597,16 @@ class PageTable:
     """The tables of a paged KV cache (struct augtree_pages), int32 tensors on one GPU that stay the caller's: `table`
     [seqs, max_pages], `length` [seqs] cached tokens, `parent` [seqs] (< 0, or no tensor: none), `free_pages` [pages] a
     ring of free pages, `free_state` [2] its first free entry and their number. One PageTable serves all layers of a
-    model; the caches of a layer are tensors [pages, Hkv, page_size, d]. PageTable.empty makes an unused one."""
+    model; the caches of a layer are tensors [pages, Hkv, page_size, d]. PageTable.empty makes an unused one. The tensors
+    are written to, not exchanged for others."""
+
+    __slots__ = ("device", "table", "length", "parent", "free_pages", "free_state", "num_seqs", "max_pages", "num_pages",
+                 "page_size", "struct", "ref", "_sizes")
+
+    def __setattr__(self, name, value):
+        if hasattr(self, "_sizes"):  # the library has the tensors' addresses
+            raise AttributeError(f"PageTable.{name} stays what it was made with: write into it")
+        object.__setattr__(self, name, value)
 
     def __init__(self, table, length, parent, free_pages, free_state, page_size: int):
         on = _On((("table", table), ("length", length), ("parent", parent), ("free_pages", free_pages),
@@ -675,7 +684,8 @@ class PagePlan:
         return self._field(_lib.PLAN_POSITIONS, self.rows)
 
     def check(self) -> None:
-        """Raises if the tables could not take the step (waits for the GPU)."""
+        """Raises if the tables could not take the step (waits for the GPU, all of its streams)."""
+        torch.cuda.synchronize(self.pages.device)
         bits = int(self.status)
         if bits:
             raise RuntimeError("page_plan: " + "; ".join(text for bit, text in PAGES_STATUS.items() if bits & bit))

@@ -81,8 +81,9 @@ int check_caches(const PagedShape& s, int d, int type, const void* k, int64_t k_
   c->v_all = (size_t)v_stride * (s.num_pages - 1) + page;
   // apart, or pages of one stride that lie between one another (views of one tensor)
   if (overlap(k, c->k_all, v, c->v_all)) {
-    const int64_t off = (int64_t)((reinterpret_cast<uintptr_t>(v) - reinterpret_cast<uintptr_t>(k)) % (uint64_t)k_stride);
-    if (k_stride != v_stride || k > v || off < page || off > k_stride - page)
+    const uintptr_t a = reinterpret_cast<uintptr_t>(k), b = reinterpret_cast<uintptr_t>(v);
+    const int64_t off = (int64_t)((a < b ? b - a : a - b) % (uint64_t)k_stride);
+    if (k_stride != v_stride || off < page || off > k_stride - page)
       return fail(AUGTREE_ERR_INVALID_ARGUMENT, "k_cache overlaps v_cache");
   }
   return AUGTREE_OK;

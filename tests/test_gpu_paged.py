@@ -170,6 +170,8 @@ def test_attention_heads(heads, fp8):
     [(-1, 3000, 0), (0, 50, 120), (0, 2000, 45)],                          # long rows behind a parent, with parts
     [(-1, 0, 0), (0, 10, 1), (0, 20, 1), (-1, 33, 1)],                     # a parent without tokens
     [(-1, i * 37 % 900, 1) for i in range(300)],
+    [(-1, 3000, 70), (-1, 17000, 1), (-1, 900, 40)],                       # rows of few parts beside one of many
+    [(-1, 12000, 0), (0, 9000, 1), (0, 100, 1), (-1, 30, 1)],              # many parts in both units
 ])
 def test_attention_in_parts(seqs):
     for heads, page in (((8, 2, 128), 64), ((4, 4, 64), 16)):
@@ -218,6 +220,14 @@ def test_rows_behind_the_last_are_left_and_results_repeat():
     assert (o[s.live:] == 3).all() and (lse[:, s.live:] == 3).all()
     o2, lse2 = s.attend(plan, ws=torch.full((plan.workspace_size(s.d),), 0xFF, dtype=torch.uint8, device="cuda"))
     assert torch.equal(o[:s.live], o2[:s.live]) and torch.equal(lse[:, :s.live], lse2[:, :s.live])
+
+
+def test_tables_are_written_not_exchanged():
+    pages = api.PageTable.empty(2, 3, 8, 16)
+    for name in ("length", "table", "parent", "free_state", "page_size"):
+        with pytest.raises(AttributeError, match=name):
+            setattr(pages, name, None)
+    assert api.page_plan(pages, gpu([1, 0]), 1, 1, 1).positions.tolist() == [0]
 
 
 def test_no_parents_tensor_and_other_stream():

@@ -60,6 +60,8 @@ def test_valid_calls_reach_the_device_check(C):
     assert plan(C, pages(parent=None)) == DEVICE
     both = dict(kc=at(11), vc=at(11, PAGE), ks=2 * PAGE, vs=2 * PAGE)  # two halves of one tensor
     assert write(C, **both) == DEVICE and attend(C, **both) == DEVICE
+    both.update(kc=both["vc"], vc=both["kc"])
+    assert write(C, **both) == DEVICE and attend(C, **both) == DEVICE
     assert write(C, kind=1, k_scale=at(16), v_scale=at(17)) == DEVICE
     assert attend(C, lse=None) == DEVICE
 
