@@ -501,8 +501,8 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedFwdParams p) {
     for (int k = 0; k < kItemInts; ++k) w[k] = __builtin_amdgcn_readfirstlane(src[k]);
     __builtin_memcpy(&it, w, sizeof(it));
   }
-  if (item >= plan[PH_ITEMS] || !plan_is_for(plan, p.s))
-    return;
+  const bool fits = plan_is_for(plan, p.s);
+  if (!fits | (item >= plan[PH_ITEMS])) return;
   if (it.rows * p.group <= kSlotPairs) {
     attend_few<D, E4M3>(p, it, kvh, k_buf0, k_buf1, v_buf0, v_buf1, stat);
     return;

@@ -60,9 +60,10 @@ struct PagedShape {
 };
 
 // Whether a plan was made for these sizes: a caller may hand over another's.
+// (Without branches: the words come by one load, not one after the other.)
 inline __host__ __device__ bool plan_is_for(const int32_t* plan, const PagedShape& s) {
-  return plan[PH_SEQS] == s.seqs && plan[PH_ROWS] == s.rows && plan[PH_HQ] == s.hq && plan[PH_HKV] == s.hkv &&
-         plan[PH_PAGE] == s.page && plan[PH_MAX_PAGES] == s.max_pages && plan[PH_NUM_PAGES] == s.num_pages;
+  return ((plan[PH_SEQS] ^ s.seqs) | (plan[PH_ROWS] ^ s.rows) | (plan[PH_HQ] ^ s.hq) | (plan[PH_HKV] ^ s.hkv) |
+          (plan[PH_PAGE] ^ s.page) | (plan[PH_MAX_PAGES] ^ s.max_pages) | (plan[PH_NUM_PAGES] ^ s.num_pages)) == 0;
 }
 
 inline __host__ __device__ int paged_div(int a, int b) { return (a + b - 1) / b; }

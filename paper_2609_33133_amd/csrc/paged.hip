@@ -255,11 +255,83 @@ __global__ __launch_bounds__(256) void cache_write_kernel(CacheWriteParams p, in
   }
 }
 
+// One pair of a merge: where its parts lie, and what they come to so far.
+template <int D>
+struct MergePair {
+  const PagedFwdParams& p;
+  int32_t d[kMergeInts];  // the row's entry of the plan
+  int head, kvh, lane;
+  float top = -INFINITY, sum = 0.f;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+
+  __device__ __forceinline__ MergePair(const PagedFwdParams& p_, const int32_t* merge, int64_t i, int lane_)
+      : p(p_), lane(lane_) {
+    const int64_t m = i / p.s.hq;
+    head = (int)(i - m * p.s.hq);
+    kvh = head / p.group;
+    const int4* const src = reinterpret_cast<const int4*>(merge + m * kMergeInts);  // (arrays of a plan are 16-byte aligned)
+#pragma unroll
+    for (int k = 0; k < kMergeInts / 4; ++k) {
+      const int4 w = src[k];
+      d[4 * k] = w.x;
+      d[4 * k + 1] = w.y;
+      d[4 * k + 2] = w.z;
+      d[4 * k + 3] = w.w;
+    }
+  }
+  __device__ __forceinline__ int parts() const { return d[4] + d[8]; }
+  // the parts phase, phase + share, .. of both units
+  __device__ __forceinline__ void add(int phase, int share) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int pair = d[2 + 4 * u] + head - kvh * p.group, parts = d[4 + 4 * u];
+      // the pair's place in slots of 32 pairs, per KV head; from part to part
+      const int64_t first = ((int64_t)(d[1 + 4 * u] + pair / kSlotPairs) * p.s.hkv + kvh) * kSlotPairs + pair % kSlotPairs;
+      const int64_t step = (int64_t)d[3 + 4 * u] * p.s.hkv * kSlotPairs;
+      // four parts at a time, so that their loads are on their way together
+      for (int k = phase; k < parts; k += 4 * share) {
+        float l[4];
+        f32x4 o[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int kk = k + j * share;
+          const int64_t at = first + (kk < parts ? kk : k) * step;
+          l[j] = p.part_lse[at];
+          o[j] = *reinterpret_cast<const f32x4*>(p.part_o + at * D + lane * 4);
+          if (kk >= parts) l[j] = -INFINITY;
+        }
+        const float t = fmaxf(fmaxf(fmaxf(l[0], l[1]), fmaxf(l[2], l[3])), top);
+        if (t == -INFINITY) continue;  // parts that the row sees nothing of
+        const float back = __expf(top - t);
+        acc = acc * back;
+        sum *= back;
+        top = t;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float w = __expf(l[j] - t);
+          acc += o[j] * w;
+          sum += w;
+        }
+      }
+    }
+  }
+  __device__ __forceinline__ void store() const {
+    const float inv = 1.f / sum;
+    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+    bf16x4 y;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) y[j] = (__bf16)(acc[j] * inv);
+    const int row = d[0];
+    *reinterpret_cast<bf16x4*>(p.o + ((int64_t)row * p.s.hq + head) * D + lane * 4) = y;
+    if (p.lse && lane == 0) p.lse[(int64_t)head * p.s.rows + row] = top + __logf(sum);
+  }
+};
+
 // Joins the partial results of a row: o = sum_p w_p o_p / sum_p w_p, w_p =
 // exp(lse_p - max lse), lse = max + log sum_p w_p, over the parts of its
-// sequence's own unit and of its run's. D / 4 lanes take a (row, head) pair and,
-// of its parts, every `share`-th: one group of lanes all of them where the plan
-// has few parts a row, else the workgroup's groups together. The loads of four
+// sequence's own unit and of its run's. D / 4 lanes take a (row, head) pair;
+// pairs of more than kMergeAlone parts are taken by a workgroup, each of whose
+// groups of lanes joins every eighth (d = 64: sixteenth) part. The loads of four
 // parts are on their way together: 32 pairs of 22 parts take 4 us, 256 of 24 4.4
 // us, 16384 of two 13 us. (By one group, one part after the other, 32 pairs of 33
 // parts took 25 us.)
@@ -270,81 +342,40 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedFwdParams p, int6
   __shared__ float part_top[GROUPS], part_sum[GROUPS];
   const int32_t* const plan = p.plan;
   if (!plan_is_for(plan, p.s)) return;
+  const int32_t* const merge = plan + merge_at;
   const int64_t pairs = (int64_t)plan[PH_MERGE_ROWS] * p.s.hq;
-  const int lane = threadIdx.x % LANES, grp = threadIdx.x / LANES, g = p.group;
-  const int share = plan[PH_MOST_PARTS] > kMergeAlone ? GROUPS : 1;
-  const int per = GROUPS / share, mine = share > 1 ? 0 : grp, phase = share > 1 ? grp : 0;
-  for (int64_t i0 = (int64_t)blockIdx.x * per; i0 < pairs; i0 += (int64_t)gridDim.x * per) {
-    const int64_t i = i0 + mine;
-    const bool any = i < pairs;
-    const int64_t m = any ? i / p.s.hq : 0;
-    const int head = any ? (int)(i - m * p.s.hq) : 0, kvh = head / g;
-    const int32_t* const d = plan + merge_at + m * kMergeInts;
-    const int row = d[0];
-    float top = -INFINITY, sum = 0.f;
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    if (any)
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const int pair = d[2 + 4 * u] + head - kvh * g, parts = d[4 + 4 * u];
-        // the pair's place in slots of 32 pairs, per KV head; from part to part
-        const int64_t first = ((int64_t)(d[1 + 4 * u] + pair / kSlotPairs) * p.s.hkv + kvh) * kSlotPairs + pair % kSlotPairs;
-        const int64_t step = (int64_t)d[3 + 4 * u] * p.s.hkv * kSlotPairs;
-        // four parts at a time, so that their loads are on their way together
-        for (int k = phase; k < parts; k += 4 * share) {
-          float l[4];
-          f32x4 o[4];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const int kk = k + j * share;
-            const int64_t at = first + (kk < parts ? kk : k) * step;
-            l[j] = p.part_lse[at];
-            o[j] = *reinterpret_cast<const f32x4*>(p.part_o + at * D + lane * 4);
-            if (kk >= parts) l[j] = -INFINITY;
-          }
-          const float t = fmaxf(fmaxf(fmaxf(l[0], l[1]), fmaxf(l[2], l[3])), top);
-          if (t == -INFINITY) continue;  // parts that the row sees nothing of
-          const float back = __expf(top - t);
-          acc = acc * back;
-          sum *= back;
-          top = t;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float w = __expf(l[j] - t);
-            acc += o[j] * w;
-            sum += w;
-          }
-        }
-      }
-    if (share > 1) {
-      part_acc[grp][lane] = acc;
-      if (lane == 0) {
-        part_top[grp] = top;
-        part_sum[grp] = sum;
-      }
-      __syncthreads();
-      if (grp == 0) {
-        for (int k = 1; k < GROUPS; ++k) top = fmaxf(top, part_top[k]);
-        const float w0 = __expf(part_top[0] - top);
-        acc = acc * w0;
-        sum *= w0;
-        for (int k = 1; k < GROUPS; ++k) {
-          const float w = __expf(part_top[k] - top);
-          acc += part_acc[k][lane] * w;
-          sum += part_sum[k] * w;
-        }
-      }
-      __syncthreads();
-      if (grp != 0) continue;
+  const int lane = threadIdx.x % LANES, grp = threadIdx.x / LANES;
+  const bool some_together = plan[PH_MOST_PARTS] * 2 > kMergeAlone;  // (of one unit, of which a row has two)
+  for (int64_t i = (int64_t)blockIdx.x * GROUPS + grp; i < pairs; i += (int64_t)gridDim.x * GROUPS) {
+    MergePair<D> x(p, merge, i, lane);
+    if (some_together && x.parts() > kMergeAlone) continue;
+    x.add(0, 1);
+    x.store();
+  }
+  if (!some_together) return;
+  for (int64_t i = blockIdx.x; i < pairs; i += gridDim.x) {
+    MergePair<D> x(p, merge, i, lane);
+    if (x.parts() <= kMergeAlone) continue;  // (the same for the whole workgroup)
+    x.add(grp, GROUPS);
+    part_acc[grp][lane] = x.acc;
+    if (lane == 0) {
+      part_top[grp] = x.top;
+      part_sum[grp] = x.sum;
     }
-    if (!any) continue;
-    const float inv = 1.f / sum;
-    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-    bf16x4 y;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) y[j] = (__bf16)(acc[j] * inv);
-    *reinterpret_cast<bf16x4*>(p.o + ((int64_t)row * p.s.hq + head) * D + lane * 4) = y;
-    if (p.lse && lane == 0) p.lse[(int64_t)head * p.s.rows + row] = top + __logf(sum);
+    __syncthreads();
+    if (grp == 0) {
+      for (int k = 1; k < GROUPS; ++k) x.top = fmaxf(x.top, part_top[k]);
+      const float w0 = __expf(part_top[0] - x.top);
+      x.acc = x.acc * w0;
+      x.sum *= w0;
+      for (int k = 1; k < GROUPS; ++k) {
+        const float w = __expf(part_top[k] - x.top);
+        x.acc += part_acc[k][lane] * w;
+        x.sum += part_sum[k] * w;
+      }
+      x.store();
+    }
+    __syncthreads();
   }
 }
 
@@ -372,7 +403,7 @@ hipError_t launch_cache_write(const CacheWriteParams& p, hipStream_t stream) {
 
 hipError_t launch_paged_merge(const PagedFwdParams& p, hipStream_t stream) {
   const int64_t merge_at = plan_layout(p.s).merge, pairs = (int64_t)p.s.rows * p.s.hq;
-  const unsigned grid = (unsigned)(pairs < 2048 ? pairs : 2048);
+  const unsigned grid = (unsigned)(pairs < 4096 ? pairs : 4096);
   if (p.d == 128) paged_merge_kernel<128><<<grid, 256, 0, stream>>>(p, merge_at);
   else paged_merge_kernel<64><<<grid, 256, 0, stream>>>(p, merge_at);
   return hipGetLastError();
