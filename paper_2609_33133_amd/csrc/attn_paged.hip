@@ -12,14 +12,12 @@
 // forward is: two chunks of 7777 tokens together, over 7.7k and 23k tokens (32 / 8
 // heads, d = 128), in 1.60 to 1.86 ms on different boxes, 1.0 to 1.17 PFLOP/s.
 //
-// e4m3 caches: the bytes of the rows that a copy instruction brings land in the
-// upper half of where these rows stand in the bf16 tile; once there, the
-// wavefront that fetched them reads them and writes the rows as bf16 (exactly)
-// over both halves. The scales of K and V multiply the softmax scale and the
-// result. That costs 17 % of the rate of a bf16 cache on long chunks (16384 tokens:
-// 2205 us, 1880 in bf16), in the wait between the copies and the barrier of a step.
-// (Reading all rows of a step before the first is written, or lanes that write
-// rows of opposite parity together: no faster.)
+// e4m3 caches: tiles stay bytes and every wavefront makes its operands bf16 (exactly) as it reads them, K by 16-byte
+// reads that serve two MFMAs, V^T by 8-bit transpose reads. The scales of K and V multiply the softmax scale and the
+// result. The four wavefronts convert the same tile four times over, but LDS bandwidth is what a step is short of: in
+// clocks of 128 bytes a step of a workgroup takes 1280 in bf16, 640 this way, and 1536 with tiles that the wavefront which
+// fetched them widens in LDS. 16384 tokens 1975 us (bf16 1915, widened in LDS 2250), 16 turns of 150 to 700 tokens 820
+// (843, 1017). Widened in LDS a step ahead, beside the second product: 2270; V alone from bytes: 2155.
 #include <type_traits>
 
 #include "common.h"
@@ -48,6 +46,52 @@ __device__ __forceinline__ bf16x8 widen8(int lo, int hi) {
     y[4 * k + 3] = b[1];
   }
   return y;
+}
+
+// Swizzle of 16-byte chunks in a tile of byte rows.
+template <int RB>
+__device__ __forceinline__ int swz8(int row) {
+  return RB == 128 ? (row >> 1) & 7 : (row >> 2) & 3;
+}
+// The 8-bit transpose read of V^T from such a tile (inside a 16-lane group, lane j addresses 8 bytes of row j / 2 and
+// receives one column of the 8 rows): this lane's offset for columns 32 db .. + 31, keys in the order of the accumulators
+template <int RB>
+__device__ __forceinline__ int tr8_offset(int lane, int db) {
+  const int grp = lane >> 4, j = lane & 15, r8 = j >> 1, row = 4 * (grp >> 1) + (r8 & 3) + 8 * (r8 >> 2);
+  return row * RB + (((2 * db + (grp & 1)) ^ swz8<RB>(row)) << 4) + 8 * (j & 1);
+}
+// The first of the 8 columns that half-wave hf holds of step ks of a product with byte rows: 16 bytes of a row serve two
+// steps, so that they come by one read.
+__device__ __forceinline__ int byte_column(int ks, int hf) { return ks / 2 * 32 + hf * 16 + ks % 2 * 8; }
+__device__ __forceinline__ bf16x8 read_tr8(const char* at) {
+  typedef int v2i __attribute__((ext_vector_type(2)));
+  const v2i x = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) v2i*)(at));
+  return widen8(x[0], x[1]);
+}
+
+// s_waitcnt vmcnt(N): all but the last N vector-memory accesses of this wavefront have completed
+template <int N>
+__device__ __forceinline__ void wait_vmem_but() {
+  __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | ((N >> 4) << 14));
+}
+// what this wavefront read from LDS has arrived: a copy may overwrite it
+__device__ __forceinline__ void wait_lds() {
+  wave_lds_fence();
+  __builtin_amdgcn_s_waitcnt(0xC07F);
+  wave_lds_fence();
+}
+// Scheduling of N MFMAs that take operands from bytes: a read for every PER of them, DEPTH reads ahead, and the four
+// conversions of each.
+template <int N, int PER, int DEPTH>
+__device__ __forceinline__ void pace_bytes() {
+  __builtin_amdgcn_sched_group_barrier(0x100, DEPTH, 0);
+  __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    if (i % PER == 0 && i / PER < N / PER - DEPTH) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
+  }
 }
 
 // Copies of 64-key blocks of one KV head from a cache into LDS, by four
@@ -80,8 +124,8 @@ struct PageCopy {
 #pragma unroll
     for (int k = 0; k < (BIG ? PER_WAVE : 1); ++k) {
       const int r = (wave + 4 * k) * RPI + lane / CH;
-      // bf16: straight into the swizzled tile (TileCopy); e4m3: as it lies, for widen()
-      voff[k] = (BIG ? r : r & 15) * ROWB + ((E4M3 ? lane % CH : (lane % CH) ^ swz<D>(r)) << 4);
+      // straight into the swizzled tile (bf16: TileCopy's)
+      voff[k] = (BIG ? r : r & 15) * ROWB + (((lane % CH) ^ (E4M3 ? swz8<ROWB>(r) : swz<D>(r))) << 4);
     }
     window(it.blk0);
   }
@@ -110,12 +154,9 @@ struct PageCopy {
     if (blk - win >= 64 / EPB) window(blk - 1);
   }
 
-  // where the bytes of the wavefront's k-th copy instruction land in a tile
-  __device__ __forceinline__ int at(int k) const { return (wave + 4 * k) * (E4M3 ? 2048 : 1024) + (E4M3 ? 1024 : 0); }
-
-  __device__ __forceinline__ void copy(const void* cache, int lo, int hi, int blk, __bf16* tile) const {
+  __device__ __forceinline__ void copy(const void* cache, int lo, int hi, int blk, void* tile) const {
 #if defined(__HIP_DEVICE_COMPILE__)
-    char* const lds = reinterpret_cast<char*>(tile);
+    char* const lds = static_cast<char*>(tile);
     __amdgpu_buffer_rsrc_t rsrc;
 #pragma unroll
     for (int k = 0; k < PER_WAVE; ++k) {
@@ -125,32 +166,13 @@ struct PageCopy {
         const char* const base = static_cast<const char*>(cache) + (int64_t)((uint64_t)h << 32 | l);
         rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, __builtin_amdgcn_readlane(bytes, e), 0x00020000);
       }
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)(lds + at(k)), 16,
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)(lds + (wave + 4 * k) * 1024), 16,
                                                voff[BIG ? k : 0], 0, 0, 0);
     }
 #endif
   }
-  __device__ __forceinline__ void copy_k(int blk, __bf16* tile) const { copy(p.k_cache, k_lo, k_hi, blk, tile); }
-  __device__ __forceinline__ void copy_v(int blk, __bf16* tile) const { copy(p.v_cache, v_lo, v_hi, blk, tile); }
-
-  // e4m3: the rows that this wavefront's copies have brought, as bf16 into the swizzled tile
-  __device__ __forceinline__ void widen(__bf16* tile) const {
-    if constexpr (E4M3) {
-      constexpr int CH = ROWB / 16;
-      raw16 x[PER_WAVE];
-#pragma unroll
-      for (int k = 0; k < PER_WAVE; ++k)
-        x[k] = *reinterpret_cast<const raw16*>(reinterpret_cast<const char*>(tile) + at(k) + lane * 16);
-      wave_lds_fence();  // the rows are read before any is written
-#pragma unroll
-      for (int k = 0; k < PER_WAVE; ++k) {
-        const int r = (wave + 4 * k) * RPI + lane / CH, col = (lane % CH) * 16;
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-          *reinterpret_cast<bf16x8*>(tile + toff<D>(r, col + 8 * h)) = widen8(x[k][2 * h], x[k][2 * h + 1]);
-      }
-    }
-  }
+  __device__ __forceinline__ void copy_k(int blk, void* tile) const { copy(p.k_cache, k_lo, k_hi, blk, tile); }
+  __device__ __forceinline__ void copy_v(int blk, void* tile) const { copy(p.v_cache, v_lo, v_hi, blk, tile); }
 };
 
 // ---------------------------------------------------------------------------- items of few pairs
@@ -184,23 +206,21 @@ struct FewTiles {
   static_assert(GROUPS <= 8 && RPI <= 16, "a copy instruction stays inside a page");
 
   int voff[2];     // this lane's byte offset from an instruction's first row, even and odd instructions
-  int koff[8];     // K operand of 16 columns (bytes inside a half)
+  int koff[8];     // K operand of 16 columns, e4m3: of 32 (bytes inside a half)
   int voff_tr[4][2];  // V^T operand of 32 columns
 
-  __device__ static __forceinline__ int swz8(int row) { return RB == 128 ? (row >> 1) & 7 : (row >> 2) & 3; }
-
   __device__ __forceinline__ void init(int lane) {
-    const int l32 = lane & 31, hf = lane >> 5, grp = lane >> 4, j = lane & 15;
+    const int l32 = lane & 31, hf = lane >> 5;
     constexpr int CH = RB / 16;
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       const int r = lane / CH, row = k * RPI + r;
-      voff[k] = r * ROWB + (((lane % CH) ^ (E4M3 ? swz8(row) : swz<64>(row))) << 4);
+      voff[k] = r * ROWB + (((lane % CH) ^ (E4M3 ? swz8<RB>(row) : swz<64>(row))) << 4);
     }
 #pragma unroll
     for (int ks = 0; ks < 8; ++ks) {
       if constexpr (!E4M3) koff[ks] = ks < 4 ? 2 * toff<64>(l32, ks * 16 + hf * 8) : 0;
-      else koff[ks] = ks < D / 16 ? l32 * RB + ((ks ^ swz8(l32)) << 4) + 8 * hf : 0;
+      else koff[ks] = ks < D / 32 ? l32 * RB + (((2 * ks + hf) ^ swz8<RB>(l32)) << 4) : 0;
     }
     if constexpr (!E4M3) {
       TrOffsets<64> t;
@@ -208,22 +228,23 @@ struct FewTiles {
 #pragma unroll
       for (int db = 0; db < 2; ++db) voff_tr[db][0] = t.o[db][0], voff_tr[db][1] = t.o[db][1];
     } else {
-      const int r8 = j >> 1, row = 4 * (grp >> 1) + (r8 & 3) + 8 * (r8 >> 2);
 #pragma unroll
-      for (int db = 0; db < D / 32; ++db)
-        voff_tr[db][0] = row * RB + (((2 * db + (grp & 1)) ^ swz8(row)) << 4) + 8 * (j & 1);
+      for (int db = 0; db < D / 32; ++db) voff_tr[db][0] = tr8_offset<RB>(lane, db);
     }
   }
 
-  // K rows 32 t + l32, columns 16 ks + 8 hf .. +7; h0, h1: the tile's halves
-  __device__ __forceinline__ bf16x8 k_operand(const char* h0, const char* h1, int t, int ks) const {
+  // K rows 32 t + l32, columns of steps ks and ks + 1 (ks is even); h0, h1: the tile's halves
+  __device__ __forceinline__ void k_operands(const char* h0, const char* h1, int t, int ks, bf16x8& x0, bf16x8& x1) const {
     if constexpr (!E4M3) {
       const bool second = BY_COLS ? ks >= 4 : t >= 1;
-      return *reinterpret_cast<const bf16x8*>((second ? h1 : h0) + koff[BY_COLS ? ks % 4 : ks]);
+      const char* const at = second ? h1 : h0;
+      x0 = *reinterpret_cast<const bf16x8*>(at + koff[BY_COLS ? ks % 4 : ks]);
+      x1 = *reinterpret_cast<const bf16x8*>(at + koff[BY_COLS ? ks % 4 + 1 : ks + 1]);
     } else {
       const int row0 = RB == 128 ? 0 : (t & 1) * 32;
-      const int2 x = *reinterpret_cast<const int2*>(((RB == 128 ? t : t >> 1) ? h1 : h0) + row0 * RB + koff[ks]);
-      return widen8(x.x, x.y);
+      const raw16 x = *reinterpret_cast<const raw16*>(((RB == 128 ? t : t >> 1) ? h1 : h0) + row0 * RB + koff[ks / 2]);
+      x0 = widen8(x[0], x[1]);
+      x1 = widen8(x[2], x[3]);
     }
   }
   // V^T: columns 32 db + l32, keys 32 t + 16 m + the ones that accumulator registers 8 m .. 8 m + 7 hold
@@ -239,11 +260,8 @@ struct FewTiles {
       __builtin_memcpy(reinterpret_cast<char*>(&r) + 8, &b, 8);
       return r;
     } else {
-      typedef int v2i __attribute__((ext_vector_type(2)));
       const int row0 = (RB == 128 ? 0 : (t & 1) * 32) + 16 * m;
-      const char* const at = ((RB == 128 ? t : t >> 1) ? h1 : h0) + row0 * RB + voff_tr[db][0];
-      const v2i x = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) v2i*)(at));
-      return widen8(x[0], x[1]);
+      return read_tr8(((RB == 128 ? t : t >> 1) ? h1 : h0) + row0 * RB + voff_tr[db][0]);
     }
   }
 
@@ -273,18 +291,6 @@ struct FewTiles {
 #endif
   }
 };
-
-// s_waitcnt vmcnt(N): all but the last N vector-memory accesses of this wavefront have completed
-template <int N>
-__device__ __forceinline__ void wait_vmem_but() {
-  __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | ((N >> 4) << 14));
-}
-// what this wavefront read from LDS has arrived: a copy may overwrite it
-__device__ __forceinline__ void wait_lds() {
-  wave_lds_fence();
-  __builtin_amdgcn_s_waitcnt(0xC07F);
-  wave_lds_fence();
-}
 
 template <int D, bool E4M3>
 __device__ __forceinline__ void attend_few(const PagedFwdParams& p, const PagedItem& it, int kvh, __bf16* k0, __bf16* k1,
@@ -331,9 +337,9 @@ __device__ __forceinline__ void attend_few(const PagedFwdParams& p, const PagedI
   const int pair = min(l32, pairs - 1), qrow = fast_div(pair, g, p.group_magic);
   bf16x8 qreg[D / 16];
   {
-    const uint16_t* const q = p.q + qbase + pair_offset<D>(qrow, pair - qrow * g, p.s.hq) + hf * 8;
+    const uint16_t* const q = p.q + qbase + pair_offset<D>(qrow, pair - qrow * g, p.s.hq);
 #pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks) qreg[ks] = as_bf16x8(ldg16(q + ks * 16));
+    for (int ks = 0; ks < D / 16; ++ks) qreg[ks] = as_bf16x8(ldg16(q + (E4M3 ? byte_column(ks, hf) : ks * 16 + hf * 8)));
   }
   float c = p.scale_log2;
   if constexpr (E4M3) c *= p.k_scale[kvh];
@@ -360,8 +366,10 @@ __device__ __forceinline__ void attend_few(const PagedFwdParams& p, const PagedI
       for (int i = 0; i < 16; ++i) s[t][i] = s1[i] = 0.f;
 #pragma unroll
       for (int ks = 0; ks < D / 16; ks += 2) {
-        s[t] = mfma32(tiles.k_operand(ka, kb, t, ks), qreg[ks], s[t]);
-        s1 = mfma32(tiles.k_operand(ka, kb, t, ks + 1), qreg[ks + 1], s1);
+        bf16x8 x0, x1;
+        tiles.k_operands(ka, kb, t, ks, x0, x1);
+        s[t] = mfma32(x0, qreg[ks], s[t]);
+        s1 = mfma32(x1, qreg[ks + 1], s1);
       }
       if constexpr (!E4M3) pace_lds_mfma<D / 16, 1, 4>();
       s[t] += s1;
@@ -529,7 +537,13 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedFwdParams p) {
     cp.copy_v(b0, v_buf0);
     if (b0 + 1 < nblk) cp.copy_k(b0 + 1, k_buf1);
 
-    core.load_q(p.q + qbase + pair_offset<D>(rows.row, rows.head, p.s.hq));
+    const uint16_t* const q = p.q + qbase + pair_offset<D>(rows.row, rows.head, p.s.hq);
+    if constexpr (E4M3) {
+#pragma unroll
+      for (int ks = 0; ks < D / 16; ++ks) core.qreg[ks] = as_bf16x8(ldg16(q + byte_column(ks, hf)));
+    } else {
+      core.load_q(q);
+    }
     float scale = p.scale_log2;
     if constexpr (E4M3) scale *= p.k_scale[kvh];
     core.init(scale, l32, lane);
@@ -540,39 +554,72 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedFwdParams p) {
     // later block) contributes nothing; neither does any block to a wavefront
     // without rows
     const int nlive = !rows.wave_any ? 0 : it.b_len > 0 ? nA + (it.b_pos + rows.whi) / BN + 1 : nA;
-    auto step = [&](int b, f32x16& s0, f32x16& s1, const __bf16* kn, const __bf16* vl, f32x16& n0, f32x16& n1) {
-      const bool isB = b >= nA;
-      const int kb0 = (isB ? b - nA : b) * BN;
-      const int len = isB ? it.b_len : it.a_len;
-      auto masked = [&] { return (kb0 + BN > len) || (isB && (kb0 + BN - 1 > qpos_lo)); };
-      auto limit = [&] { return min(len - 1, isB ? it.b_pos + qi : len - 1) - kb0; };  // last visible key of the block
-      core.step(masked, limit, s0, s1, kn, vl, n0, n1);
+    // the block needs a mask; the last visible key in it
+    auto first_of = [&](int b) { return (b >= nA ? b - nA : b) * BN; };
+    auto masked_in = [&](int b) {
+      const int kb0 = first_of(b);
+      return (kb0 + BN > (b >= nA ? it.b_len : it.a_len)) || (b >= nA && (kb0 + BN - 1 > qpos_lo));
+    };
+    auto limit_in = [&](int b) {
+      return (b >= nA ? min(it.b_len - 1, it.b_pos + qi) : it.a_len - 1) - first_of(b);
     };
 
-    // iteration b loads K(b + 2) over K(b) and V(b + 1) over V(b - 1)
     f32x16 sa0, sa1, sb0, sb1;
     wait_vmem();
+    __syncthreads();
+    int k8[D / 32], tr8[D / 32];  // e4m3: operands from byte tiles
     if constexpr (E4M3) {
-      wave_lds_fence();
-      cp.widen(k_buf0);
-      cp.widen(v_buf0);
-      if (b0 + 1 < nblk) cp.widen(k_buf1);
+#pragma unroll
+      for (int ks = 0; ks < D / 32; ++ks) k8[ks] = l32 * D + (((2 * ks + hf) ^ swz8<D>(l32)) << 4);
+#pragma unroll
+      for (int db = 0; db < D / 32; ++db) tr8[db] = tr8_offset<D>(lane, db);
     }
+    auto scores = [&](const __bf16* kl, f32x16& s0, f32x16& s1) {
+      if constexpr (!E4M3) {
+        core.s_mfma(kl, s0, s1);
+      } else {
+        const char* const kb = reinterpret_cast<const char*>(kl);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) { s0[i] = 0.f; s1[i] = 0.f; }
+#pragma unroll
+        for (int ks = 0; ks < D / 32; ++ks) {
+          const raw16 x = *reinterpret_cast<const raw16*>(kb + k8[ks]), y = *reinterpret_cast<const raw16*>(kb + 32 * D + k8[ks]);
+          s0 = mfma32(widen8(x[0], x[1]), core.qreg[2 * ks], s0);
+          s1 = mfma32(widen8(y[0], y[1]), core.qreg[2 * ks], s1);
+          s0 = mfma32(widen8(x[2], x[3]), core.qreg[2 * ks + 1], s0);
+          s1 = mfma32(widen8(y[2], y[3]), core.qreg[2 * ks + 1], s1);
+        }
+      }
+    };
+    scores(k_buf0, sa0, sa1);
+    if constexpr (!E4M3) pace_lds_mfma<D / 8, 1, FWD_DEPTH>();
     __syncthreads();
-    core.s_mfma(k_buf0, sa0, sa1);
-    pace_lds_mfma<D / 8, 1, FWD_DEPTH>();
-    __syncthreads();
+    // iteration b loads K(b + 2) over K(b) and V(b + 1) over V(b - 1)
+    auto step = [&](int b, f32x16& s0, f32x16& s1, const __bf16* kn, const __bf16* vl, f32x16& n0, f32x16& n1) {
+      auto masked = [&] { return masked_in(b); };
+      auto limit = [&] { return limit_in(b); };
+      if constexpr (!E4M3) {
+        core.step(masked, limit, s0, s1, kn, vl, n0, n1);
+      } else {
+        bf16x8 pb[4];
+        core.softmax(masked, limit, s0, s1, [&] { scores(kn, n0, n1); }, pb);
+        set_wave_priority<1>();
+        const char* const vb = reinterpret_cast<const char*>(vl);
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+          for (int db = 0; db < D / 32; ++db)
+            core.oacc[db] = mfma32(read_tr8(vb + ks * 16 * D + tr8[db]), pb[ks], core.oacc[db]);
+        pace_bytes<D / 8, 1, PV_DEPTH>();
+        set_wave_priority<0>();
+      }
+    };
     for (int b = b0; b < nblk; b += 2) {
       cp.ensure(b + 2);
       if (b + 2 < nblk) cp.copy_k(b + 2, k_buf0);
       if (b + 1 < nblk) cp.copy_v(b + 1, v_buf1);
       if (b < nlive) step(b, sa0, sa1, k_buf1, v_buf0, sb0, sb1);
       wait_vmem();
-      if constexpr (E4M3) {
-        wave_lds_fence();
-        if (b + 2 < nblk) cp.widen(k_buf0);
-        if (b + 1 < nblk) cp.widen(v_buf1);
-      }
       __syncthreads();
       if (b + 1 < nblk) {
         cp.ensure(b + 3);
@@ -580,11 +627,6 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedFwdParams p) {
         if (b + 2 < nblk) cp.copy_v(b + 2, v_buf0);
         if (b + 1 < nlive) step(b + 1, sb0, sb1, k_buf0, v_buf1, sa0, sa1);
         wait_vmem();
-        if constexpr (E4M3) {
-          wave_lds_fence();
-          if (b + 3 < nblk) cp.widen(k_buf1);
-          if (b + 2 < nblk) cp.widen(v_buf0);
-        }
         __syncthreads();
       }
     }

@@ -114,18 +114,17 @@ struct FwdCore {
     return (m_run == -INFINITY) ? 0.f : m_run * c;
   }
 
-  // One block step. Scores of the block arrive in s0/s1 (computed one step
-  // earlier); the S MFMAs of the next block (from kn, into n0/n1) are
-  // interleaved one by one with the exponentials, row sums and bf16 conversion
-  // of this one, so the matrix cores and the vector ALUs of the wavefront work
-  // at the same time; then O += V^T P^T. On the last block the extra S is
+  // One block step, first half: the softmax. Scores of the block arrive in s0/s1
+  // (computed one step earlier); the S MFMAs of the next block (next(), s_mfma or
+  // the like) are interleaved one by one with the exponentials, row sums and bf16
+  // conversion (to pb) of this one, so the matrix cores and the vector ALUs of
+  // the wavefront work at the same time. On the last block the extra S is
   // computed from a stale buffer and never used.
-  template <class Masked, class Limit>
-  __device__ __forceinline__ void step(Masked masked, Limit limit, f32x16& s0, f32x16& s1, const __bf16* kn,
-                                       const __bf16* vl, f32x16& n0, f32x16& n1) {
+  template <class Masked, class Limit, class Next>
+  __device__ __forceinline__ void softmax(Masked masked, Limit limit, f32x16& s0, f32x16& s1, Next next, bf16x8 (&pb)[4]) {
     const float ms = stats(masked, limit, s0, s1);
     __builtin_amdgcn_sched_barrier(0);
-    s_mfma(kn, n0, n1);
+    next();
     float l4[4];  // four independent partial sums
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
@@ -134,8 +133,10 @@ struct FwdCore {
       l4[i & 3] = i < 4 ? s0[i] + s1[i] : l4[i & 3] + (s0[i] + s1[i]);
     }
     l_run += (l4[0] + l4[1]) + (l4[2] + l4[3]);
-    const bf16x8 pb0 = to_bf16x8(s0, 0), pb1 = to_bf16x8(s0, 8);
-    const bf16x8 pb2 = to_bf16x8(s1, 0), pb3 = to_bf16x8(s1, 8);
+    pb[0] = to_bf16x8(s0, 0);
+    pb[1] = to_bf16x8(s0, 8);
+    pb[2] = to_bf16x8(s1, 0);
+    pb[3] = to_bf16x8(s1, 8);
     // 16 MFMAs with one K read each (reads run FWD_DEPTH ahead), the ~112
     // vector instructions of the softmax spread over them
     __builtin_amdgcn_sched_group_barrier(0x100, FWD_DEPTH, 0);
@@ -145,17 +146,21 @@ struct FwdCore {
       if (i < D / 8 - FWD_DEPTH) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
       __builtin_amdgcn_sched_group_barrier(0x402, FWD_VALU_PER_MFMA, 0);
     }
+  }
+
+  // All of it: the softmax, then O += V^T P^T.
+  template <class Masked, class Limit>
+  __device__ __forceinline__ void step(Masked masked, Limit limit, f32x16& s0, f32x16& s1, const __bf16* kn,
+                                       const __bf16* vl, f32x16& n0, f32x16& n1) {
+    bf16x8 pb[4];
+    softmax(masked, limit, s0, s1, [&] { s_mfma(kn, n0, n1); }, pb);
     set_wave_priority<1>();
     // k-step outer, output column block inner: consecutive MFMAs go to
     // different accumulators (each still sums its four k-steps in order)
 #pragma unroll
-    for (int db = 0; db < D / 32; ++db) oacc[db] = mfma32(vtr_off.read(vl, 0, db), pb0, oacc[db]);
+    for (int ks = 0; ks < 4; ++ks)
 #pragma unroll
-    for (int db = 0; db < D / 32; ++db) oacc[db] = mfma32(vtr_off.read(vl, 1, db), pb1, oacc[db]);
-#pragma unroll
-    for (int db = 0; db < D / 32; ++db) oacc[db] = mfma32(vtr_off.read(vl, 2, db), pb2, oacc[db]);
-#pragma unroll
-    for (int db = 0; db < D / 32; ++db) oacc[db] = mfma32(vtr_off.read(vl, 3, db), pb3, oacc[db]);
+      for (int db = 0; db < D / 32; ++db) oacc[db] = mfma32(vtr_off.read(vl, ks, db), pb[ks], oacc[db]);
     pace_lds_mfma<D / 8, 2, PV_DEPTH>();
     set_wave_priority<0>();
   }
