@@ -13,8 +13,10 @@
 // with few rows each (kSmallPairs) form a run: their rows together are one
 // more unit against the parent's tokens, which are then read once for all of
 // them. A unit's (row, head) pairs of one KV head are cut into tiles of
-// kTilePairs, its keys (in blocks of kPagedBlock) into parts of C blocks, and
-// an item is one part of one tile. Rows of units with several parts, and of
+// kTilePairs, its keys (in blocks of kPagedBlock) into as few equal parts as
+// none of them passes C blocks, and an item is one part of one tile. (Parts of
+// C blocks and a shorter last one: a chunk of 1500 and 48 single tokens on two
+// KV heads 75 us, with equal ones 72.) Rows of units with several parts, and of
 // runs, leave partial results that a merge kernel joins.
 #pragma once
 
@@ -52,7 +54,7 @@ enum : int32_t {
 // Header words.
 enum {
   PH_SEQS, PH_ROWS, PH_HQ, PH_HKV, PH_PAGE, PH_MAX_PAGES, PH_NUM_PAGES,  // what the plan was made for (PagedShape)
-  PH_STATUS, PH_TOTAL_ROWS, PH_ITEMS, PH_MERGE_ROWS, PH_MOST_PARTS, PH_PART, PH_FIRST, PH_SPARE, PH_NEED, PH_BACK, PH_FULL,
+  PH_STATUS, PH_TOTAL_ROWS, PH_ITEMS, PH_MERGE_ROWS, PH_MOST_PARTS, PH_FIRST, PH_SPARE, PH_NEED, PH_BACK, PH_FULL,
 };
 
 struct PagedShape {
@@ -155,7 +157,7 @@ struct TileSums {
   int64_t wide, few, tiles;
 };
 
-// Blocks of the parts that units are cut into (each tile counts with the blocks
+// The most blocks of the parts that units are cut into (each tile counts with the blocks
 // of its unit).
 // Fewer tiles than the chip runs at once: as many parts as it does, but none
 // much shorter than a tile's share, so that a few long tiles among many short
@@ -463,7 +465,7 @@ __host__ __device__ void plan_scan(Team& team, const PlanParams& p, const PlanAr
   const int part = part_blocks(TileSums{w[0], w[1], w[2]}, s, p.L.max_parts);
   const CeilDiv by_part(part);
 
-  // items: the parts of full length first, then the tiles' last ones; slots of partial results; merged rows
+  // items: the tiles' last parts, which causality shortens, behind all others; slots of partial results; merged rows
   int32_t c[4] = {0, 0, 0, 0}, at[4], sum[4], most_parts = 0;
   for (int pass = 0; pass < 2; ++pass) {
     for (int j = 0; j < steps; ++j) {
@@ -514,7 +516,6 @@ __host__ __device__ void plan_scan(Team& team, const PlanParams& p, const PlanAr
   }
   most_parts = team.max_of(most_parts);
   if (team.tid() == 0) {
-    plan[PH_PART] = part;
     plan[PH_FULL] = sum[0];
     plan[PH_ITEMS] = sum[0] + sum[1];
     plan[PH_MERGE_ROWS] = sum[3];
@@ -542,7 +543,7 @@ __host__ __device__ void plan_fill(Team& team, const PlanParams& p, const PlanAr
   int32_t* const plan = p.plan;
   const UnitView view(a, p.group);
   const int g = p.group, page = s.page, shift = p.shift;
-  const int first = plan[PH_FIRST], spare = plan[PH_SPARE], part = plan[PH_PART], rows = plan[PH_TOTAL_ROWS];
+  const int first = plan[PH_FIRST], spare = plan[PH_SPARE], rows = plan[PH_TOTAL_ROWS];
   const int need = plan[PH_NEED], back = plan[PH_BACK], full = plan[PH_FULL], items = plan[PH_ITEMS];
   auto ring = [&](int k) { return k < s.num_pages ? k : k - s.num_pages; };
 
@@ -587,12 +588,13 @@ __host__ __device__ void plan_fill(Team& team, const PlanParams& p, const PlanAr
     p.free_pages[ring(ring(first + spare) + k)] = p.table[(int64_t)i * s.max_pages + k - a.back[i]];
   };
   auto fill_item = [&](int x) {
-    const bool whole = x < full;  // a part of `part` blocks, not a tile's last
+    const bool whole = x < full;  // not a tile's last part
     const int k = whole ? x : x - full;
     const int32_t* const of = whole ? a.full0 : a.last0;
     const int unit = last_at_most(of, 2 * s.seqs, k);
     PagedItem it = view.unit(unit >> 1, unit & 1);
     const int parts = a.parts[unit], slot0 = a.slot0[unit];
+    const int part = paged_div(view.blocks(it), parts);
     const int of_tile = whole ? parts - 1 : 1, j = k - of[unit];
     // a causal unit's last tiles have the most blocks: they come first
     const int t = view.tiles(it) - 1 - j / of_tile, c = whole ? j % of_tile : parts - 1;
