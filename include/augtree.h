@@ -539,9 +539,10 @@ int64_t augtree_page_plan_offset(const augtree_pages* pages, int32_t rows, int32
  * 0), `pages`. The new tokens are numbered sequence by sequence. Out: the table's
  * new entries (free pages in ring order, sequence by sequence), the ring's
  * entries behind its last one (ended sequences' pages, in order; they are free
- * for the next call; a parent's go with it, so its children end before or with it), length_out [num_seqs], free_state_out [2] (each may be the
- * array it follows from), the plan. A parent sees its own new tokens too when its
- * children's attend to it in the same step.
+ * for the next call; a parent's go with it, so its children end before or with
+ * it), length_out [num_seqs], free_state_out [2] (each may be the array it
+ * follows from), the plan. A parent's new tokens of the same step are among those
+ * that its children's see.
  * `rows` may exceed the number of new tokens (a captured graph's room): rows
  * behind the last one are left as they are by the calls that take the plan.
  * Neighbouring sequences of one parent share its reading where they have few rows each.
@@ -558,7 +559,8 @@ typedef enum augtree_cache_type { AUGTREE_CACHE_BF16 = 0, AUGTREE_CACHE_E4M3 = 1
  * Caches: [num_pages][Hkv][page_size][d], pages k_page_stride (v_page_stride)
  * BYTES apart (a multiple of 16, at least a page), so that both may be views of
  * one tensor. e4m3: value / scale, rounded to nearest even, at most 448 in
- * magnitude (NaN stays NaN); k_scale, v_scale [Hkv] DEVICE fp32, > 0 and finite, not read for bf16.
+ * magnitude (NaN stays NaN); k_scale, v_scale [Hkv] DEVICE fp32, > 0 and finite,
+ * not read for bf16.
  */
 int augtree_cache_write(const augtree_pages* pages, const void* plan, int32_t rows, int32_t num_q_heads,
                         int32_t num_kv_heads, int32_t head_dim, const uint16_t* k, const uint16_t* v, int cache_type,

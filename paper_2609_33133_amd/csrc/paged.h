@@ -54,7 +54,7 @@ enum : int32_t {
 // Header words.
 enum {
   PH_SEQS, PH_ROWS, PH_HQ, PH_HKV, PH_PAGE, PH_MAX_PAGES, PH_NUM_PAGES,  // what the plan was made for (PagedShape)
-  PH_STATUS, PH_TOTAL_ROWS, PH_ITEMS, PH_MERGE_ROWS, PH_MOST_PARTS, PH_FIRST, PH_SPARE, PH_NEED, PH_BACK, PH_FULL,
+  PH_STATUS, PH_TOTAL_ROWS, PH_ITEMS, PH_MERGE_ROWS, PH_MOST_PARTS, PH_FIRST, PH_SPARE, PH_NEED, PH_BACK, PH_BIG,
 };
 
 struct PagedShape {
@@ -167,12 +167,20 @@ struct TileSums {
 // that items of different lengths fill it. (As many parts as make the rounds of the
 // chip shortest, counting 3 blocks' time for a part and 6 for its results in memory,
 // gained nothing on chunks of 1024 to 6000 tokens, 820 to 1180 TFLOP/s either way.)
-// Against the best of a dozen lengths each, us: one sequence of 4097 tokens 13.4
-// (13.4), eight branches of a 32768-token prompt 29 (29; with two workgroups a
-// CU 32), 256 sequences of 500 to 8000 274 (273), 512 branches in e4m3 236 (231),
-// a chunk of 1500 and 48 single tokens on two KV heads 68 (65; two parts a slot
-// 78), two chunks of 7777 together 1647 (1647), 16 turns of 150 to 700 1025 (987).
-inline __host__ __device__ int part_blocks(const TileSums& w, const PagedShape& s, int max_parts) {
+// Against the best of half a dozen lengths each, with items in the order of their
+// sequences, us: one sequence of 4097 tokens
+// 13.4 (13.4), eight branches of a 32768-token prompt 29 (29; with two workgroups
+// a CU 32), 256 sequences of 500 to 8000 274 (273), 512 branches in e4m3 236 (231),
+// a chunk of 1500 and 48 single tokens on two KV heads 75 (70), two chunks of 7777
+// together 1647 (1647).
+// Items of at least `big` blocks, the mean, are launched before the others, so
+// that the last round of the chip is made of short ones: 256 sequences of 500 to
+// 8000 tokens 274 -> 268 us, 512 branches in e4m3 236 -> 225, 16 turns of 150 to
+// 700 805 -> 790.
+struct Cut {
+  int part, big;
+};
+inline __host__ __device__ Cut part_blocks(const TileSums& w, const PagedShape& s, int max_parts) {
   const int slots = kChipSlots / s.hkv > 1 ? kChipSlots / s.hkv : 1;
   const int64_t blocks = w.wide + w.few;
   // (the GPU has no 64-bit division: of more than 2^31 blocks in thousands, rounded up)
@@ -194,13 +202,15 @@ inline __host__ __device__ int part_blocks(const TileSums& w, const PagedShape& 
   }
   const int least = ceil_div(blocks, max_parts);
   if (c < least) c = least;
-  return c < 1 ? 1 : c;
+  if (c < 1) c = 1;
+  const int mean = w.tiles > 0 && w.tiles <= INT32_MAX ? ceil_div(blocks, (int)w.tiles) : 1;
+  return Cut{c, mean <= c ? mean : (c + 1) / 2};
 }
 
 // The arrays that the construction works on: the plan's, or copies in faster
 // memory where the same workgroup writes all of the plan.
 struct PlanArrays {
-  int32_t *cu, *cached, *total, *parent, *a_len, *need, *back, *run, *run_rows, *merge0, *full0, *last0, *slot0, *parts;
+  int32_t *cu, *cached, *total, *parent, *a_len, *need, *back, *run, *run_rows, *merge0, *big0, *rest0, *slot0, *parts;
   __host__ __device__ static int64_t words(int64_t seqs) { return 18 * seqs + 1; }
   // one after the other, in `words` words
   __host__ __device__ static PlanArrays packed(int32_t* at, int n) {
@@ -215,9 +225,9 @@ struct PlanArrays {
     a.run = a.back + n;
     a.run_rows = a.run + n;
     a.merge0 = a.run_rows + n;
-    a.full0 = a.merge0 + n;
-    a.last0 = a.full0 + 2 * n;
-    a.slot0 = a.last0 + 2 * n;
+    a.big0 = a.merge0 + n;
+    a.rest0 = a.big0 + 2 * n;
+    a.slot0 = a.rest0 + 2 * n;
     a.parts = a.slot0 + 2 * n;
     return a;
   }
@@ -447,10 +457,10 @@ __host__ __device__ void plan_scan(Team& team, const PlanParams& p, const PlanAr
       x.rows[1] = x.run && r == i && of_parent > 0 ? run_rows : 0;
       x.blocks[1] = of_parent;
       if (!ONE) {  // for the two passes below, which write what belongs here
-        a.full0[2 * i] = x.rows[0];
-        a.full0[2 * i + 1] = x.rows[1];
-        a.last0[2 * i] = x.blocks[0];
-        a.last0[2 * i + 1] = x.blocks[1];
+        a.big0[2 * i] = x.rows[0];
+        a.big0[2 * i + 1] = x.rows[1];
+        a.rest0[2 * i] = x.blocks[0];
+        a.rest0[2 * i + 1] = x.blocks[1];
         a.merge0[i] = x.run;
       }
     }
@@ -462,10 +472,10 @@ __host__ __device__ void plan_scan(Team& team, const PlanParams& p, const PlanAr
     }
   }
   team.sum(w);
-  const int part = part_blocks(TileSums{w[0], w[1], w[2]}, s, p.L.max_parts);
-  const CeilDiv by_part(part);
+  const Cut cut = part_blocks(TileSums{w[0], w[1], w[2]}, s, p.L.max_parts);
+  const CeilDiv by_part(cut.part);
 
-  // items: the tiles' last parts, which causality shortens, behind all others; slots of partial results; merged rows
+  // items: of units with long parts first, then the others; slots of partial results; merged rows
   int32_t c[4] = {0, 0, 0, 0}, at[4], sum[4], most_parts = 0;
   for (int pass = 0; pass < 2; ++pass) {
     for (int j = 0; j < steps; ++j) {
@@ -474,10 +484,10 @@ __host__ __device__ void plan_scan(Team& team, const PlanParams& p, const PlanAr
       if (!ONE) {
         x = Units{};
         if (i < s.seqs) {
-          x.rows[0] = a.full0[2 * i];
-          x.rows[1] = a.full0[2 * i + 1];
-          x.blocks[0] = a.last0[2 * i];
-          x.blocks[1] = a.last0[2 * i + 1];
+          x.rows[0] = a.big0[2 * i];
+          x.rows[1] = a.big0[2 * i + 1];
+          x.blocks[0] = a.rest0[2 * i];
+          x.blocks[1] = a.rest0[2 * i + 1];
           x.run = a.merge0[i] != 0;
         }
       }
@@ -486,8 +496,9 @@ __host__ __device__ void plan_scan(Team& team, const PlanParams& p, const PlanAr
         const int tiles = paged_div(x.rows[which] * g, kTilePairs);
         parts[which] = tiles ? by_part(x.blocks[which]) : 0;
         const bool partial = tiles && (parts[which] > 1 || which == 1 || x.run);
-        n[which][0] = tiles ? tiles * (parts[which] - 1) : 0;
-        n[which][1] = tiles;
+        const bool big = x.blocks[which] >= parts[which] * cut.big;
+        n[which][0] = big ? tiles * parts[which] : 0;
+        n[which][1] = big ? 0 : tiles * parts[which];
         n[which][2] = partial ? parts[which] * paged_div(x.rows[which] * g, kSlotPairs) : 0;
         n[which][3] = partial && which == 0 ? x.rows[which] : 0;
         for (int k = 0; k < 4; ++k) v[k] += n[which][k];
@@ -504,8 +515,8 @@ __host__ __device__ void plan_scan(Team& team, const PlanParams& p, const PlanAr
           const int k = 2 * i + which;
           for (int y = 0; y < 4; ++y)
             if (which) v[y] += n[0][y];
-          a.full0[k] = at[0] + v[0];
-          a.last0[k] = at[1] + v[1];
+          a.big0[k] = at[0] + v[0];
+          a.rest0[k] = at[1] + v[1];
           a.slot0[k] = n[which][2] ? at[2] + v[2] : -1;
           a.parts[k] = parts[which];
           if (which == 0) a.merge0[i] = n[0][3] ? at[3] + v[3] : -1;
@@ -516,7 +527,7 @@ __host__ __device__ void plan_scan(Team& team, const PlanParams& p, const PlanAr
   }
   most_parts = team.max_of(most_parts);
   if (team.tid() == 0) {
-    plan[PH_FULL] = sum[0];
+    plan[PH_BIG] = sum[0];
     plan[PH_ITEMS] = sum[0] + sum[1];
     plan[PH_MERGE_ROWS] = sum[3];
     plan[PH_MOST_PARTS] = most_parts;
@@ -544,7 +555,7 @@ __host__ __device__ void plan_fill(Team& team, const PlanParams& p, const PlanAr
   const UnitView view(a, p.group);
   const int g = p.group, page = s.page, shift = p.shift;
   const int first = plan[PH_FIRST], spare = plan[PH_SPARE], rows = plan[PH_TOTAL_ROWS];
-  const int need = plan[PH_NEED], back = plan[PH_BACK], full = plan[PH_FULL], items = plan[PH_ITEMS];
+  const int need = plan[PH_NEED], back = plan[PH_BACK], bigs = plan[PH_BIG], items = plan[PH_ITEMS];
   auto ring = [&](int k) { return k < s.num_pages ? k : k - s.num_pages; };
 
   // a row: slot, position, where the merge finds its parts
@@ -588,16 +599,15 @@ __host__ __device__ void plan_fill(Team& team, const PlanParams& p, const PlanAr
     p.free_pages[ring(ring(first + spare) + k)] = p.table[(int64_t)i * s.max_pages + k - a.back[i]];
   };
   auto fill_item = [&](int x) {
-    const bool whole = x < full;  // not a tile's last part
-    const int k = whole ? x : x - full;
-    const int32_t* const of = whole ? a.full0 : a.last0;
+    const bool big = x < bigs;
+    const int k = big ? x : x - bigs;
+    const int32_t* const of = big ? a.big0 : a.rest0;
     const int unit = last_at_most(of, 2 * s.seqs, k);
     PagedItem it = view.unit(unit >> 1, unit & 1);
     const int parts = a.parts[unit], slot0 = a.slot0[unit];
-    const int part = paged_div(view.blocks(it), parts);
-    const int of_tile = whole ? parts - 1 : 1, j = k - of[unit];
-    // a causal unit's last tiles have the most blocks: they come first
-    const int t = view.tiles(it) - 1 - j / of_tile, c = whole ? j % of_tile : parts - 1;
+    const int part = paged_div(view.blocks(it), parts), j = k - of[unit];
+    // a causal unit's last tiles have the most blocks: they come first; its last parts, which causality shortens, last
+    const int tiles = view.tiles(it), c = j / tiles, t = tiles - 1 - (j - c * tiles);
     it.pair0 = t * kTilePairs;
     int end = view.blocks(it);
     if (it.b_len > 0) {  // up to what the tile's last row sees

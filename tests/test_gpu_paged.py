@@ -212,6 +212,43 @@ def test_nan_and_infinity_stay_with_their_sequence(where, value):
     assert torch.equal(got[0][:, heads], want[0][:, heads])
 
 
+@pytest.mark.parametrize("where", ["k", "v"])
+@pytest.mark.parametrize("seqs,seq", [(TREES, 5), (CHUNKS, 1)])
+def test_nan_in_8_bits_stays_with_its_sequence(where, seqs, seq):
+    s = Step(seqs, (8, 2, 128), 64, seed=15, fp8=True)
+    plan = s.plan()
+    want = s.attend(plan)
+    cu, at = s.want[4], 20  # a cached token
+    slot = int(s.want[0][seq, at // 64]) * 64 + at % 64
+    (s.k_cache if where == "k" else s.v_cache).view(torch.uint8)[slot // 64, 1, slot % 64, 7] = 0xFF
+    got = s.attend(plan)
+    mine = slice(int(cu[seq]), int(cu[seq + 1]))
+    if where == "v":
+        assert got[0][mine, 4:, 7].isnan().all()
+    for x, y in zip(got, want):  # the other rows, and the other KV head's heads
+        rows = 1 if x.dim() == 2 else 0
+        heads = 1 - rows
+        assert torch.equal(x.narrow(heads, 0, 4), y.narrow(heads, 0, 4))
+        for part in (slice(0, mine.start), slice(mine.stop, s.live)):
+            assert torch.equal(x[:, part] if rows else x[part], y[:, part] if rows else y[part])
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+def test_two_layers_at_once_share_a_plan(fp8):
+    """On two streams, each with a workspace and outputs of its own."""
+    a, b = (Step(TREES + CHUNKS, (8, 2, 128), 64, seed=21, fp8=fp8) for _ in range(2))
+    b.q, b.k_cache, b.v_cache = b.q.flip(2), b.v_cache, b.k_cache
+    plan = a.plan()
+    want = [x.attend(plan) for x in (a, b)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = [[x.attend(plan, stream=st) for _ in range(4)] for x, st in zip((a, b), streams)]
+    torch.cuda.synchronize()
+    for tries, w in zip(got, want):
+        for o, lse in tries:
+            assert torch.equal(o[:a.live], w[0][:a.live]) and torch.equal(lse[:, :a.live], w[1][:, :a.live])
+
+
 def test_rows_behind_the_last_are_left_and_results_repeat():
     s = Step(TREES, (8, 2, 128), 64, seed=2, spare_rows=40)
     plan = s.plan()
