@@ -378,7 +378,7 @@ __host__ __device__ void plan_scan(Team& team, const PlanParams& p, const PlanAr
     int32_t v[3] = {o.n, o.need, o.back}, total[3];
     int64_t ahead = k;
     team.scan_lanes(v, total);
-    const int64_t k_all = team.max_lanes(ahead);
+    const int64_t k_all = team.last_lanes(ahead);
     if (i < s.seqs) {
       a.cu[i] = plan[p.L.cu + i] = bad ? 0 : before[0] + v[0];
       a.need[i] = bad ? 0 : before[1] + v[1];
@@ -406,11 +406,11 @@ __host__ __device__ void plan_scan(Team& team, const PlanParams& p, const PlanAr
     const One o = again(i);
     const int64_t k = key(i, o);
     int64_t ahead = k;
-    const int64_t k_all = team.max_lanes(ahead);
+    const int64_t k_all = team.last_lanes(ahead);
     const int64_t near = larger(q, ahead);
     const bool joins = o.small && (uint32_t)near == (uint32_t)k;
     int64_t begin = o.small && !joins ? i + 1 : 0;
-    const int64_t begin_all = team.max_lanes(begin);
+    const int64_t begin_all = team.last_lanes(begin);
     const int run = begin > 0 ? (int)begin - 1 : start;  // the last that begins before this sequence
     if (!bad && o.n > 0) {
       if (is_small(near) && !joins) a.run_rows[run] = a.cu[i] - a.cu[run];

@@ -63,7 +63,8 @@ __device__ __forceinline__ int64_t lane64(int64_t x, int lane) {
 // wavefront still reads what the next turn writes; every wavefront then scans
 // these values, one per lane. All instructions run on one CU, so they count:
 // scans by LDS shuffles, and totals added up by every thread in a loop, took
-// 11 of 29 us for 576 sequences.
+// 11 of 29 us for 576 sequences, sums that stop and 64-bit maxima inside a
+// wavefront 3 of 35 for 4352.
 struct GroupTeam {
   static constexpr int kWaves = kPlanThreads / 64;
   struct Turn {
@@ -86,19 +87,20 @@ struct GroupTeam {
   __device__ void scan_lanes(int32_t (&v)[K], int32_t (&total)[K]) const {
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      const int32_t x = sums<64>(v[k]);
-      v[k] = x - v[k];  // (exact where the sum has not stopped: a step whose sums stop is refused)
+      uint32_t x = v[k];  // (a step whose sums pass kMostCount is refused: these may wrap)
+      scan_by_dpp<64>([&](auto ctrl, auto rows) { x += dpp<decltype(ctrl)::value, decltype(rows)::value>(x); });
+      v[k] = x - v[k];
       total[k] = __builtin_amdgcn_readlane(x, 63);
     }
   }
-  // x >= 0: the largest of the lanes before this one, 0 at least; returns the largest of all lanes
-  __device__ int64_t max_lanes(int64_t& x) const {
-    const int64_t m = maxima<64>(x);
-    // (the lane before: shifted by one)
-    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int32_t)m, 0x138, 0xf, 0xf, false);
-    const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int32_t)(m >> 32), 0x138, 0xf, 0xf, false);
-    x = (int64_t)((uint64_t)hi << 32 | lo);
-    return lane64(m, 63);
+  // x: 0 or larger than in all lanes before; the last of the lanes before that is not 0, or 0; returns that of all lanes
+  __device__ int64_t last_lanes(int64_t& x) const {
+    const uint64_t set = __ballot(x != 0), mine = set & ((uint64_t(1) << lane()) - 1);
+    const int64_t all = set ? lane64(x, 63 - __builtin_clzll(set)) : 0;
+    const int at = 4 * (63 - __builtin_clzll(mine | 1));
+    const uint32_t lo = __builtin_amdgcn_ds_bpermute(at, (int32_t)x), hi = __builtin_amdgcn_ds_bpermute(at, (int32_t)(x >> 32));
+    x = mine ? (int64_t)((uint64_t)hi << 32 | lo) : 0;
+    return all;
   }
   // sums over the threads: of the wavefronts before this one, of all
   template <int K>
@@ -173,7 +175,7 @@ struct GroupTeam {
 // One workgroup: the scans over the sequences and, where the rest is little
 // (FILL: at most kFillSeqs sequences), that too, with all arrays in LDS. Bound
 // by latency: a dozen barriers and the memory round trips between them. 576
-// sequences with 496 rows and 585 items 13.5 us, 4352 sequences 35 us and 11 us
+// sequences with 496 rows and 585 items 13.3 us, 4352 sequences 33 us and 11 us
 // for the second launch.
 template <bool FILL>
 __global__ __launch_bounds__(kPlanThreads) void page_plan_kernel(PlanParams p) {

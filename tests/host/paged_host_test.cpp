@@ -81,7 +81,7 @@ struct ThreadTeam {
   void scan_lanes(int32_t (&v)[K], int32_t (&total)[K]) const {
     for (int k = 0; k < K; ++k) total[k] = v[k], v[k] = 0;
   }
-  int64_t max_lanes(int64_t& x) const {
+  int64_t last_lanes(int64_t& x) const {
     const int64_t all = x;
     x = 0;
     return all;
