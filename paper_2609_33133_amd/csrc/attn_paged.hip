@@ -8,16 +8,18 @@
 // page table, at most 64 of whose entries a wavefront holds at a time, one per
 // lane. A block's copies go page by page where pages are shorter than it, and
 // rows behind a segment's last token are zeros by the copies' range check, so
-// what stands there is never read. Bound by the matrix cores as the packed
-// forward is: two chunks of 7777 tokens together, over 7.7k and 23k tokens (32 / 8
-// heads, d = 128), in 1.60 to 1.86 ms on different boxes, 1.0 to 1.17 PFLOP/s.
+// what stands there is never read. Bound by LDS bandwidth and the matrix cores
+// together: two chunks of 7777 tokens together, over 7.7k and 23k tokens (32 / 8
+// heads, d = 128), in 1.60 to 1.86 ms on different cards, 1.0 to 1.17 PFLOP/s.
 //
-// e4m3 caches: tiles stay bytes and every wavefront makes its operands bf16 (exactly) as it reads them, K by 16-byte
-// reads that serve two MFMAs, V^T by 8-bit transpose reads. The scales of K and V multiply the softmax scale and the
-// result. The four wavefronts convert the same tile four times over, but LDS bandwidth is what a step is short of: in
-// clocks of 128 bytes a step of a workgroup takes 1280 in bf16, 640 this way, and 1536 with tiles that the wavefront which
-// fetched them widens in LDS. 16384 tokens 1975 us (bf16 1915, widened in LDS 2250), 16 turns of 150 to 700 tokens 820
-// (843, 1017). Widened in LDS a step ahead, beside the second product: 2270; V alone from bytes: 2155.
+// e4m3 caches: tiles stay bytes and every wavefront makes its operands bf16
+// (exactly) as it reads them, K by 16-byte reads that serve two MFMAs, V^T by 8-bit
+// transpose reads. The scales of K and V multiply the softmax scale and the result.
+// The four wavefronts convert the same tile four times over, but LDS bandwidth is
+// what a step is short of: in clocks of 128 bytes a step of a workgroup takes 1280
+// in bf16, 640 this way, and 1536 with tiles that the wavefront which fetched them
+// widens in LDS. 16384 tokens 1975 us (bf16 1915, widened in LDS 2250, there a step
+// ahead beside the second product 2270, V alone from bytes 2155).
 #include <type_traits>
 
 #include "common.h"
