@@ -81,8 +81,8 @@ struct PlanLayout {
   int64_t cu;                // [seqs + 1] first row
   // work: what the construction keeps (PlanArrays). Of each sequence: first row, tokens before and after, parent and its
   // tokens, pages taken and given back by the sequences before, run (its first sequence, or -1), rows of the run that
-  // begins here, rows merged before. Of its own unit and of the unit of the run that begins here: items with a part of C
-  // blocks before the unit's, items with a tile's last part before the unit's, first slot (-1: none), parts of a tile.
+  // begins here, rows merged before. Of its own unit and of the unit of the run that begins here: items of units with
+  // long parts before the unit's, items of the others before the unit's, first slot (-1: none), parts of a tile.
   int64_t work;
   int64_t slots, positions;  // [rows]
   int64_t merge;             // [rows][kMergeInts]

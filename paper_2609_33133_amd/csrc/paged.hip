@@ -266,12 +266,12 @@ struct MergePair {
   float top = -INFINITY, sum = 0.f;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 
-  __device__ __forceinline__ MergePair(const PagedFwdParams& p_, const int32_t* merge, int64_t i, int lane_)
+  __device__ __forceinline__ MergePair(const PagedFwdParams& p_, const int32_t* merge, uint32_t i, int lane_)
       : p(p_), lane(lane_) {
-    const int64_t m = i / p.s.hq;
+    const uint32_t m = i / (uint32_t)p.s.hq;  // (fewer than 2^30 pairs)
     head = (int)(i - m * p.s.hq);
-    kvh = head / p.group;
-    const int4* const src = reinterpret_cast<const int4*>(merge + m * kMergeInts);  // (arrays of a plan are 16-byte aligned)
+    kvh = fast_div(head, p.group, p.group_magic);
+    const int4* const src = reinterpret_cast<const int4*>(merge + (int64_t)m * kMergeInts);  // (arrays of a plan are 16-byte aligned)
 #pragma unroll
     for (int k = 0; k < kMergeInts / 4; ++k) {
       const int4 w = src[k];
@@ -345,17 +345,17 @@ __global__ __launch_bounds__(256) void paged_merge_kernel(PagedFwdParams p, int6
   const int32_t* const plan = p.plan;
   if (!plan_is_for(plan, p.s)) return;
   const int32_t* const merge = plan + merge_at;
-  const int64_t pairs = (int64_t)plan[PH_MERGE_ROWS] * p.s.hq;
+  const uint32_t pairs = (uint32_t)plan[PH_MERGE_ROWS] * p.s.hq;
   const int lane = threadIdx.x % LANES, grp = threadIdx.x / LANES;
   const bool some_together = plan[PH_MOST_PARTS] * 2 > kMergeAlone;  // (of one unit, of which a row has two)
-  for (int64_t i = (int64_t)blockIdx.x * GROUPS + grp; i < pairs; i += (int64_t)gridDim.x * GROUPS) {
+  for (uint32_t i = blockIdx.x * GROUPS + grp; i < pairs; i += gridDim.x * GROUPS) {
     MergePair<D> x(p, merge, i, lane);
     if (some_together && x.parts() > kMergeAlone) continue;
     x.add(0, 1);
     x.store();
   }
   if (!some_together) return;
-  for (int64_t i = blockIdx.x; i < pairs; i += gridDim.x) {
+  for (uint32_t i = blockIdx.x; i < pairs; i += gridDim.x) {
     MergePair<D> x(p, merge, i, lane);
     if (x.parts() <= kMergeAlone) continue;  // (the same for the whole workgroup)
     x.add(grp, GROUPS);
