@@ -333,30 +333,32 @@ __device__ __forceinline__ void attend_few(const PagedFwdParams& p, const PagedI
   Tiles tiles;
   tiles.init(lane);
   int j = wave;
-  int ids = 0, ids_next = 0;
-  if (j < n) {
-    ids = page_ids(j);
-    ids_next = page_ids(j + 4);
-    tiles.copy(ka, kb, kc, p.k_stride, head_off, ids, first_key(j), last_key(j), p.s.page, p.s.num_pages, lane);
-    tiles.copy(va, vb, vc, p.v_stride, head_off, ids, first_key(j), last_key(j), p.s.page, p.s.num_pages, lane);
-  }
-  const int pair = min(l32, pairs - 1), qrow = fast_div(pair, g, p.group_magic);
-  bf16x8 qreg[D / 16];
-  {
-    const uint16_t* const q = p.q + qbase + pair_offset<D>(qrow, pair - qrow * g, p.s.hq);
-#pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks) qreg[ks] = as_bf16x8(ldg16(q + (E4M3 ? byte_column(ks, hf) : ks * 16 + hf * 8)));
-  }
-  float c = p.scale_log2;
-  if constexpr (E4M3) c *= p.k_scale[kvh];
+  float c = p.scale_log2;  // (e4m3: the scale follows)
   float m_run = -INFINITY, l_run = 0.f;
   f32x16 oacc[D / 32];
 #pragma unroll
   for (int db = 0; db < D / 32; ++db)
 #pragma unroll
     for (int i = 0; i < 16; ++i) oacc[db][i] = 0.f;
-
-  wait_vmem();  // (before the steps: the compiler would wait for Q in every one)
+  const int pair = min(l32, pairs - 1), qrow = fast_div(pair, g, p.group_magic);
+  bf16x8 qreg[D / 16];
+  int ids_next = 0;
+  if (j < n) {
+    const int ids = page_ids(j);
+    ids_next = page_ids(j + 4);
+    const uint16_t* const q = p.q + qbase + pair_offset<D>(qrow, pair - qrow * g, p.s.hq);
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) qreg[ks] = as_bf16x8(ldg16(q + (E4M3 ? byte_column(ks, hf) : ks * 16 + hf * 8)));
+    float k_scale = 1.f;
+    if constexpr (E4M3) k_scale = p.k_scale[kvh];
+    tiles.copy(ka, kb, kc, p.k_stride, head_off, ids, first_key(j), last_key(j), p.s.page, p.s.num_pages, lane);
+    tiles.copy(va, vb, vc, p.v_stride, head_off, ids, first_key(j), last_key(j), p.s.page, p.s.num_pages, lane);
+    wait_vmem_but<16>();  // all but the copies (else the compiler would wait for Q and the scale in every step)
+    if constexpr (E4M3) {
+      asm volatile("" : "+v"(k_scale));
+      c *= k_scale;
+    }
+  }
   // One block; MORE: another one of this wavefront follows, whose copies go out.
   auto step = [&](auto more) {
     constexpr bool MORE = decltype(more)::value;
@@ -446,6 +448,8 @@ __device__ __forceinline__ void attend_few(const PagedFwdParams& p, const PagedI
   if (j < n) step(std::false_type());
 
   // the four states of each pair, joined: wavefront w writes its outputs to array w
+  c = p.scale_log2;  // (a wavefront without blocks joins too)
+  if constexpr (E4M3) c *= p.k_scale[kvh];
   const float l_tot = pair_sum(l_run);
   __syncthreads();
   char* const mine = reinterpret_cast<char*>(wave == 0 ? k0 : wave == 1 ? k1 : wave == 2 ? v0 : v1);
