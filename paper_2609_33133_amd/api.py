@@ -739,8 +739,10 @@ def page_plan(pages: PageTable, new_rows, rows: int, num_q_heads: int, num_kv_he
 
 
 def _no_grad(what: str, tensors):
-    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
-        raise ValueError(f"{what} forms no gradient: call it under torch.no_grad(), or with detached tensors")
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                raise ValueError(f"{what} forms no gradient: call it under torch.no_grad(), or with detached tensors")
     if _tangent(tensors):
         raise ValueError(f"{what} takes no dual tensors: a tangent would get lost")
 
@@ -767,9 +769,12 @@ def _cache(t, name: str, plan: PagePlan, d: int):
 
 def _caches(k_cache, v_cache, k_scale, v_scale, plan: PagePlan, d: int):
     kind, k_stride = _cache(k_cache, "k_cache", plan, d)
-    v_kind, v_stride = _cache(v_cache, "v_cache", plan, d)
-    if kind != v_kind:
+    if v_cache.dtype is not k_cache.dtype:
         raise TypeError(f"k_cache is {k_cache.dtype}, v_cache {v_cache.dtype}")
+    like_k = v_cache.shape == k_cache.shape and v_cache.stride() == k_cache.stride()
+    v_stride = k_stride if like_k else _cache(v_cache, "v_cache", plan, d)[1]
+    if kind == _lib.CACHE_BF16 and k_scale is None and v_scale is None:
+        return kind, k_stride, v_stride
     for n, t in (("k_scale", k_scale), ("v_scale", v_scale)):
         if (t is not None) != (kind == _lib.CACHE_E4M3):
             raise ValueError(f"{n} goes with a cache in 8 bits" + (", which needs it" if t is None else ""))
