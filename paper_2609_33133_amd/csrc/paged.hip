@@ -175,8 +175,8 @@ struct GroupTeam {
 // One workgroup: the scans over the sequences and, where the rest is little
 // (FILL: at most kFillSeqs sequences), that too, with all arrays in LDS. Bound
 // by latency: a dozen barriers and the memory round trips between them. 576
-// sequences with 496 rows and 585 items 13.3 us, 4352 sequences 33 us and 11 us
-// for the second launch.
+// sequences with 496 rows and 585 items 13.3 us, 4352 sequences 33 us and 9 us
+// for the second launch (12 with threads for the rows alone).
 template <bool FILL>
 __global__ __launch_bounds__(kPlanThreads) void page_plan_kernel(PlanParams p) {
   __shared__ GroupTeam::Turn lds[2];
@@ -390,8 +390,9 @@ hipError_t launch_page_plan(const PlanParams& p, bool apart, hipStream_t stream)
   }
   page_plan_kernel<false><<<1, kPlanThreads, 0, stream>>>(p);
   if (hipError_t e = hipGetLastError()) return e;
-  const int most = p.s.rows > p.L.max_items ? p.s.rows : p.L.max_items;
-  page_fill_kernel<<<most < 1024 * 256 ? (most + 255) / 256 : 1024, 256, 0, stream>>>(p);
+  // a thread for every row and item, and for the pages of rows that fill theirs
+  const int64_t most = (int64_t)p.s.rows + p.L.max_items + p.s.rows / p.s.page;
+  page_fill_kernel<<<most < 1024 * 256 ? (unsigned)((most + 255) / 256) : 1024, 256, 0, stream>>>(p);
   return hipGetLastError();
 }
 
