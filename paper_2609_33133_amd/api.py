@@ -786,10 +786,11 @@ def _caches(k_cache, v_cache, k_scale, v_scale, plan: PagePlan, d: int):
 def cache_write(k, v, k_cache, v_cache, plan: PagePlan, k_scale=None, v_scale=None, stream=None) -> None:
     """Writes the keys and values of a step's new tokens, k, v [rows, Hkv, d] bf16, into their slots of the caches
     [pages, Hkv, page_size, d] (augtree_cache_write): bf16, or float8_e4m3fn holding value / scale with fp32 scales [Hkv]
-    on the GPU. The caches may be views with any stride between pages (two halves of one tensor)."""
+    on the GPU. The caches may be views with any stride between pages (two halves of one tensor). Tensors that ask for a
+    gradient, the scales among them, are refused while gradients are enabled, dual tensors always."""
     on = _On((("plan", plan.data), ("k", k), ("v", v), ("k_cache", k_cache), ("v_cache", v_cache), ("k_scale", k_scale),
               ("v_scale", v_scale)), stream)
-    _no_grad("cache_write", (k, v, k_cache, v_cache))
+    _no_grad("cache_write", (k, v, k_cache, v_cache, k_scale, v_scale))
     if k.dim() != 3:
         raise ValueError("k must be [rows, heads, head_dim]")
     d = k.shape[2]
@@ -807,11 +808,11 @@ def paged_fwd(q, k_cache, v_cache, plan: PagePlan, k_scale=None, v_scale=None, o
               scale: Optional[float] = None, want_lse: bool = False, ws=None, stream=None):
     """Attention of a step's new tokens, q [rows, Hq, d] bf16, over the cached tokens of their sequences' parents and
     their own up to themselves (augtree_paged_fwd). Returns (o, lse): o like q, lse [Hq, rows] fp32 or None unless asked
-    for; rows behind the plan's last one are not written. Decode only: tensors that ask for a gradient are refused while
-    gradients are enabled."""
+    for; rows behind the plan's last one are not written. Decode only: tensors that ask for a gradient, the scales and
+    outputs among them, are refused while gradients are enabled, dual tensors always."""
     on = _On((("plan", plan.data), ("q", q), ("k_cache", k_cache), ("v_cache", v_cache), ("k_scale", k_scale),
               ("v_scale", v_scale), ("o", o), ("lse", lse), ("ws", ws)), stream)
-    _no_grad("paged_fwd", (q, k_cache, v_cache, o))
+    _no_grad("paged_fwd", (q, k_cache, v_cache, k_scale, v_scale, o, lse))
     if q.dim() != 3:
         raise ValueError("q must be [rows, heads, head_dim]")
     d = q.shape[2]
