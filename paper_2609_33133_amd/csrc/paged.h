@@ -272,9 +272,13 @@ struct UnitView {
   __host__ __device__ int tiles(const PagedItem& u) const { return paged_div(u.rows * group, kTilePairs); }
 };
 
-// Sums of counts that stop at kMostCount, so that no sequence of bad lengths overflows them.
-constexpr int32_t kMostCount = 1 << 30;
-inline __host__ __device__ int32_t add_count(int32_t a, int32_t b) { return a + b < kMostCount ? a + b : kMostCount; }
+// Sums of counts from 0 to kMostCount that stop there, one above the most rows and pages that there is room for (2^30),
+// so that no numbers of new tokens overflow them or come out as ones that fit.
+constexpr int32_t kMostCount = (1 << 30) + 1;
+inline __host__ __device__ int32_t add_count(int32_t a, int32_t b) {
+  const uint32_t sum = (uint32_t)a + (uint32_t)b;
+  return sum < (uint32_t)kMostCount ? (int32_t)sum : kMostCount;
+}
 
 // n / d rounded up, for many n >= 0 by one d >= 1 with n + d < 2^31.
 struct CeilDiv {
@@ -302,7 +306,9 @@ __host__ __device__ void plan_scan(Team& team, const PlanParams& p, const PlanAr
   const int base = team.wave() * steps * lanes + team.lane();
   const int first = p.state[0], spare = p.state[1];
   const int most = s.max_pages << shift;
-  auto pages = [&](int tokens) { return (tokens + page - 1) >> shift; };
+  // tokens of a sequence after the step, and pages of so many (of one that outgrows its table up to 2^31 + 1)
+  auto after = [](int len, int n) { return (uint32_t)len + (uint32_t)n; };
+  auto pages = [&](uint32_t tokens) { return (int)((tokens + page - 1) >> shift); };
 
   // a sequence's step, its numbers brought into range (nothing behind the last sequence); bits of what is wrong with it
   struct One {
@@ -317,7 +323,7 @@ __host__ __device__ void plan_scan(Team& team, const PlanParams& p, const PlanAr
     o.len = o.bad ? 0 : len;
     o.n = raw <= 0 ? 0 : raw < s.rows + 1 ? raw : s.rows + 1;
     if (raw > most - o.len) o.bad |= PAGES_LONG;
-    o.need = pages(o.len + o.n) - pages(o.len);
+    o.need = pages(after(o.len, o.n)) - pages(o.len);
     o.back = raw < 0 ? pages(o.len) : 0;
     o.parent = par < 0 || o.n == 0 ? -1 : par;
     o.small = o.parent >= 0 && (int64_t)o.n * g <= kSmallPairs;
@@ -344,7 +350,7 @@ __host__ __device__ void plan_scan(Team& team, const PlanParams& p, const PlanAr
       const int par = o.parent;
       if (par < s.seqs && par != i && p.parent[par] < 0 && p.fresh[par] >= 0) {
         const One q = look(par);
-        a_len = q.len + q.n;
+        a_len = (int)after(q.len, q.n);
       } else {
         o.bad |= PAGES_PARENT;
       }
@@ -353,7 +359,7 @@ __host__ __device__ void plan_scan(Team& team, const PlanParams& p, const PlanAr
     bad |= o.bad;
     if (i < s.seqs) {
       a.cached[i] = o.len;
-      a.total[i] = o.len + o.n;
+      a.total[i] = (int)after(o.len, o.n);
       a.parent[i] = o.parent;
       a.a_len[i] = a_len;
     }
@@ -386,7 +392,7 @@ __host__ __device__ void plan_scan(Team& team, const PlanParams& p, const PlanAr
       a.run[i] = a.run_rows[i] = -1;
       if (o.small && (uint32_t)larger(q, ahead) != (uint32_t)k) start = i;
     }
-    for (int c = 0; c < 3; ++c) before[c] += total[c];
+    for (int c = 0; c < 3; ++c) before[c] = (int)((uint32_t)before[c] + (uint32_t)total[c]);  // (a refused step's may wrap)
     q = larger(q, k_all);
   }
   if (team.tid() == 0) {
