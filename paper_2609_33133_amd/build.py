@@ -25,10 +25,11 @@ ARCH = "gfx950"
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-I" + os.path.join(ROOT, "include"), "-I" + CSRC, "-I/opt/rocm/include"]
 HIP_FLAGS = ["--offload-arch=" + ARCH, "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-fno-honor-nans",
              "-ffp-contract=fast"]
-# The linear-attention layer states how far a NaN or an infinity reaches, so its
-# kernels are compiled with NaN honoured (the same instructions but for ten of
-# the 25000 lines of its largest source, and the same times).
-NAN_SOURCES = ("linear", "head_norm", "paged")
+# The linear-attention layer and the paged cache state how far a NaN or an
+# infinity reaches, so their kernels are compiled with NaN honoured (of the
+# linear layer's largest source ten of 25000 instructions differ, of a paged
+# attention kernel 13 of 4200, and the times are the same).
+NAN_SOURCES = ("linear", "head_norm", "paged", "attn_paged")
 # The attention kernels are scheduled by the backend's instruction-level
 # parallelism strategy (the dK/dV kernel runs ~1 % faster than with the
 # default occupancy-driven one, the other two slightly faster; no spills);

@@ -402,9 +402,9 @@ __device__ __forceinline__ void attend_few(const PagedFwdParams& p, const PagedI
     for (int t = 0; t < SUB; ++t)
 #pragma unroll
       for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[t][i]);
-    mx = pair_max(mx);
+    mx = pair_max<MaxWritten>(mx);
     if (__any(mx * c > m_run * c + RESCALE_MARGIN_LOG2)) {
-      const float mnew = fmaxf(m_run, mx);
+      const float mnew = MaxWritten::of(m_run, mx);
       const float alpha = (mnew == -INFINITY) ? 1.f : __builtin_amdgcn_exp2f((m_run - mnew) * c);
       l_run *= alpha;
 #pragma unroll
@@ -537,7 +537,7 @@ __global__ __launch_bounds__(256, 2) void attn_paged_kernel(PagedFwdParams p) {
   const int nblk = it.blk1;  // blocks blk0 .. blk1 - 1 of A and then B
 
   const int b0 = it.blk0;
-  FwdCore<D> core;
+  FwdCore<D, MaxWritten> core;  // (a chunk of 7777 tokens 1630 us; with the compiler's maxima 1670)
   core.hf = hf;
   if (b0 < nblk) {
     PageCopy<D, E4M3, BIG> cp(p, it, nA, kvh, wave, lane);

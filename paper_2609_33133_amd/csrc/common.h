@@ -283,14 +283,30 @@ __device__ __forceinline__ void set_wave_priority() {
   __builtin_amdgcn_sched_barrier(0);
 }
 
+// The larger of two numbers, as the kernels of the packed forward form it: in a
+// source compiled without NaN that is one instruction. (One that honours NaN
+// needs MaxWritten: there the compiler puts an instruction before it for each
+// operand, in case it is a signalling NaN, ten in a step of a block.)
+struct MaxPlain {
+  static __device__ __forceinline__ float of(float a, float b) { return fmaxf(a, b); }
+};
+struct MaxWritten {  // of a NaN and a number: the number
+  static __device__ __forceinline__ float of(float a, float b) {
+    float r;
+    asm("v_max_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
+  }
+};
+
 // max / sum of a value and the one of lane l ^ 32, without LDS: after
 // v_permlane32_swap of (x, x) the two results hold, in every lane, x of the
 // lane and x of its partner (in one order or the other). An LDS shuffle
 // (ds_bpermute) costs an LDS round trip and waits for the wavefront's
 // earlier LDS reads.
+template <class Max>
 __device__ __forceinline__ float pair_max(float x) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  return Max::of(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 __device__ __forceinline__ float pair_sum(float x) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);

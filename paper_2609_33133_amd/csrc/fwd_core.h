@@ -26,7 +26,7 @@ constexpr int FWD_VALU_PER_MFMA = 7;  // softmax instructions placed after each 
 // inside the fp32 and bf16 ranges.
 constexpr float RESCALE_MARGIN_LOG2 = 8.f;
 
-template <int D>
+template <int D, class Max = MaxPlain>
 struct FwdCore {
   static constexpr int BN = kFwdBlockN;  // keys per block
 
@@ -95,10 +95,10 @@ struct FwdCore {
       float m = max3(s0[j], s1[j], s0[j + 4]);
       m = max3(m, s1[j + 4], s0[j + 8]);
       m = max3(m, s1[j + 8], s0[j + 12]);
-      m4[j] = fmaxf(m, s1[j + 12]);
+      m4[j] = Max::of(m, s1[j + 12]);
     }
-    const float mx = pair_max(fmaxf(max3(m4[0], m4[1], m4[2]), m4[3]));
-    const float mnew = fmaxf(m_run, mx);
+    const float mx = pair_max<Max>(Max::of(max3(m4[0], m4[1], m4[2]), m4[3]));
+    const float mnew = Max::of(m_run, mx);
     // rescale only when some row maximum of this wavefront passed its
     // reference by more than the margin (always on a row's first visible key:
     // the reference starts at -inf)
