@@ -486,13 +486,15 @@ size_t augtree_head_norm_workspace_size(int64_t rows, int32_t heads, int32_t hea
  * augtree_cache_write and augtree_paged_fwd with that plan. Lengths, tables and
  * plans stay on the GPU, every call enqueues kernels only and may be captured
  * into a graph and replayed. Calls that share a plan being written, or a
- * workspace, must not overlap. Results are bitwise reproducible; how work is cut
- * (and so the last bits) follows from the batch.
+ * workspace, must not overlap. Results are bitwise reproducible; their last bits
+ * follow from the batch: from how work is cut, and from the scores of rows that are
+ * computed together, which move the reference of their exponents together.
  * A NaN or infinity in a row of q stays in that row and head. In a token of K or V
- * it reaches the rows that see the token, in the query heads of its KV head, and
- * perhaps (in V) earlier new rows of the same sequence within the token's 64 keys;
- * never another sequence but a parent's branches. (A result that it reaches need
- * not be NaN.)
+ * it reaches the rows that see the token, in the query heads of its KV head (in V:
+ * in its channel), and in V perhaps earlier new rows of the same sequence, at most
+ * 94 tokens before it: a wavefront multiplies the 64 keys that its last row is among
+ * with all of its up to 32 rows, and 0 times NaN is NaN. Never another sequence but
+ * a parent's branches. (A result that it reaches need not be NaN.)
  * ------------------------------------------------------------------------- */
 
 /* Tables of a cache (DEVICE arrays, owned by the caller), shared by all layers. */

@@ -26,9 +26,9 @@ COMMON = ["-O3", "-std=c++17", "-fPIC", "-I" + os.path.join(ROOT, "include"), "-
 HIP_FLAGS = ["--offload-arch=" + ARCH, "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-fno-honor-nans",
              "-ffp-contract=fast"]
 # The linear-attention layer and the paged cache state how far a NaN or an
-# infinity reaches, so their kernels are compiled with NaN honoured (of the
-# linear layer's largest source ten of 25000 instructions differ, of a paged
-# attention kernel 13 of 4200, and the times are the same).
+# infinity reaches, so their kernels are compiled with NaN honoured (ten of the
+# 25000 lines of the linear layer's largest source differ, a paged attention
+# kernel has 13 instructions more in 4200, and the times are the same).
 NAN_SOURCES = ("linear", "head_norm", "paged", "attn_paged")
 # The attention kernels are scheduled by the backend's instruction-level
 # parallelism strategy (the dK/dV kernel runs ~1 % faster than with the
