@@ -1,4 +1,5 @@
 """More of the paged KV cache on the GPU."""
+import numpy as np
 import pytest
 import torch
 
@@ -87,3 +88,75 @@ def test_a_bad_new_token(heads, cached, fp8, bad):
                 if where == "v":
                     assert not torch.isfinite(o[first:int(cu[seq + 1]), mine, 7]).any()
     assert all(torch.equal(a, b) for a, b in zip(s.attend(plan), want))
+
+
+def forest(seqs, seed):
+    """Trees one after the other, most of whose branches take a token: runs that cross the 64 lanes of a wavefront, its
+    steps and the wavefronts; some branches rest, end or take more tokens."""
+    rng, rows, root, left = np.random.RandomState(seed), [], -1, 0
+    for i in range(seqs):
+        if left == 0:
+            root, left = i, rng.randint(0, 150)
+            rows.append((-1, rng.randint(0, 200), 0 if rng.rand() < 0.8 else rng.randint(1, 30)))
+        else:
+            left -= 1
+            kind = rng.rand()
+            new = 1 if kind < 0.8 else rng.randint(2, 6) if kind < 0.9 else 0 if kind < 0.94 else -1 if kind < 0.97 else rng.randint(20, 80)
+            rows.append((root, rng.randint(0, 90), new))
+    return rows
+
+
+def check_items(s, plan):
+    """The plan's items lie inside its room and meet, for every (row, head) pair, each block of 64 keys that it sees once."""
+    w, n, r, g = plan.data.cpu().numpy(), s.pages.num_seqs, s.rows, s.hq // s.hkv
+    up = lambda x: -(-x // 4) * 4
+    slots = 32 + up(n + 1) + up(18 * n + 1)
+    np.testing.assert_array_equal(w[slots:slots + r], s.want[5])  # (the layout that is read here)
+    at, items = slots + 2 * up(r) + up(12 * r), int(w[9])
+    assert at + 16 * items <= len(w)
+    cu, new = s.want[4], np.maximum(s.t["new"], 0)
+    total, parent = s.t["length"] + new, s.t["parent"]
+    blocks = lambda t: -(-t // 64)
+    met_a, met_b = (np.zeros((s.live, g), np.int64) for _ in range(2))
+    used = []
+    for row0, rows, pair0, a_seq, a_len, b_seq, b_len, b_pos, blk0, blk1, slot in w[at:at + 16 * items].reshape(-1, 16)[:, :11]:
+        assert 0 <= row0 and rows > 0 and row0 + rows <= s.live and 0 <= pair0 < rows * g and pair0 % 128 == 0
+        assert 0 <= blk0 <= blk1 <= blocks(a_len) + blocks(b_len)
+        assert a_len == (total[a_seq] if a_seq >= 0 else 0) and b_len == (total[b_seq] if b_seq >= 0 else 0)
+        pairs = np.arange(pair0, min(pair0 + 128, rows * g))
+        row, head = row0 + pairs // g, pairs % g
+        seq = np.searchsorted(cu, row, side="right") - 1
+        n_a = blocks(a_len)
+        if a_seq >= 0:
+            assert (parent[seq] == a_seq).all()
+            met_a[row, head] += max(0, min(blk1, n_a) - blk0)
+        if b_seq >= 0:
+            assert (seq == b_seq).all() and b_pos == s.t["length"][b_seq]
+            seen = (b_pos + pairs // g) // 64 + 1  # blocks that the pair sees
+            met_b[row, head] += np.maximum(0, np.minimum(blk1 - n_a, seen) - max(blk0 - n_a, 0))
+        if slot >= 0:
+            used += range(slot, slot + -(-len(pairs) // 32))
+    seq = np.searchsorted(cu, np.arange(s.live), side="right") - 1
+    own = (s.t["length"][seq] + np.arange(s.live) - cu[seq]) // 64 + 1
+    above = np.where(parent[seq] >= 0, blocks(total[parent[seq]]), 0)
+    assert (met_a == above[:, None]).all() and (met_b == own[:, None]).all()
+    assert len(set(used)) == len(used) and (max(used, default=0) + 1) * s.hkv * 32 * (s.d + 1) * 4 <= plan.workspace_size(s.d)
+
+
+@pytest.mark.parametrize("seqs,heads,page,spare,fp8", [
+    (1000, (4, 2, 64), 16, 7, False),     # one launch
+    (1100, (8, 2, 128), 64, 7, False),    # two, of more than 1024 sequences
+    (3000, (4, 4, 64), 32, 0, True),
+    (3000, (7, 1, 128), 16, 50, False),
+    (200, (8, 2, 128), 32, 2100, True),   # two, of more than 2048 rows
+    (900, (6, 1, 64), 64, 2100, False),
+])
+def test_attention_of_many_sequences(seqs, heads, page, spare, fp8):
+    s = Step(forest(seqs, seqs + page), heads, page, seed=seqs, fp8=fp8, spare_rows=spare)
+    plan = s.plan()
+    plan.check()
+    check_items(s, plan)
+    o, lse = s.attend(plan)
+    s.check_attention(o, lse)
+    o2, lse2 = s.attend(plan)
+    assert torch.equal(o[:s.live], o2[:s.live]) and torch.equal(lse[:, :s.live], lse2[:, :s.live])

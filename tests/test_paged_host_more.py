@@ -12,7 +12,7 @@ HOST = os.path.join(ROOT, "tests", "host")
 
 
 @pytest.mark.timeout(600)
-@pytest.mark.parametrize("name", ["paged_sums_test"])
+@pytest.mark.parametrize("name", ["paged_sums_test", "paged_lanes_test"])
 def test_plans_under_sanitizers(tmp_path, name):
     gxx = shutil.which("g++")
     if gxx is None or not os.path.isdir(HOST):
