@@ -581,6 +581,9 @@ int augtree_paged_fwd(const augtree_pages* pages, const void* plan, int32_t rows
                       const void* k_cache, int64_t k_page_stride, const void* v_cache, int64_t v_page_stride,
                       const float* k_scale, const float* v_scale, uint16_t* o, float* lse, void* ws, size_t ws_bytes,
                       void* stream);
+/* Bytes of `ws`, 0 on invalid arguments: room for the most partial results that any plan of these sizes can have, in
+ * slots of 32 (row, head) pairs of every KV head: one at least for each sequence that may have new tokens, and 8192 / Hkv
+ * beside them. One token at 32 / 8 heads, d = 128: 135 MB, of which a token over 4097 writes 0.4. */
 size_t augtree_paged_workspace_size(const augtree_pages* pages, int32_t rows, int32_t num_q_heads,
                                     int32_t num_kv_heads, int32_t head_dim);
 

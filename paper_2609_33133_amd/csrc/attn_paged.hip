@@ -10,7 +10,7 @@
 // rows behind a segment's last token are zeros by the copies' range check, so
 // what stands there is never read. Bound by LDS bandwidth and the matrix cores
 // together: two chunks of 7777 tokens together, over 7.7k and 23k tokens (32 / 8
-// heads, d = 128), in 1.60 to 1.86 ms on different cards, 1.0 to 1.17 PFLOP/s.
+// heads, d = 128), in 1.60 to 1.68 ms, 1.11 to 1.17 PFLOP/s.
 //
 // e4m3 caches: tiles stay bytes and every wavefront makes its operands bf16
 // (exactly) as it reads them, K by 16-byte reads that serve two MFMAs, V^T by 8-bit

@@ -35,7 +35,12 @@ constexpr int kTilePairs = 128;     // (row, head) pairs of a tile
 constexpr int kSlotPairs = 32;      // pairs of a slot of partial results
 // A sequence of a run has at most so many pairs: a tile's worth, from which on
 // its tiles are full and reading the parent's keys once for several sequences
-// saves no matrix work.
+// saves no matrix work. 16 branches of a prompt of 16000, 32 / 8 heads, us: nine
+// tokens each (36 pairs) 60, as units of their own (a limit of 32) 116; 16 tokens
+// 90 and 118; 48 tokens 267, in a run (a limit of 512) 218, but of a prompt of 700
+// 23 and 37. Between 65 and 128 pairs a run does not pay everywhere: 32 tokens 162,
+// with a limit of 64 154; eight trees of four branches of 32 tokens over 3000 90
+// and 68.
 constexpr int kSmallPairs = 128;
 constexpr int kChipSlots = 512;     // workgroups that the chip runs at once (two on each of 256 CUs)
 constexpr int kItemInts = 16;
@@ -159,9 +164,10 @@ struct TileSums {
 
 // The most blocks of the parts that units are cut into (each tile counts with the blocks
 // of its unit).
-// Fewer tiles than the chip runs at once: as many parts as it does, but none
-// much shorter than a tile's share, so that a few long tiles among many short
-// ones are still cut. Tiles of at most 32 pairs are bound by the reading of
+// Fewer tiles than the chip runs at once: as many parts as it does, each tile's
+// last one short; but parts of at most twice an even share, so that a few long
+// tiles among many short ones are still cut. Nothing limits parts from below
+// there. Tiles of at most 32 pairs are bound by the reading of
 // their keys, which one workgroup a CU does as fast as two, with half the parts
 // to join. More tiles: parts of half of what a slot of the chip has to do, so
 // that items of different lengths fill it. (As many parts as make the rounds of the
@@ -172,7 +178,14 @@ struct TileSums {
 // 13.4 (13.4), eight branches of a 32768-token prompt 29 (29; with two workgroups
 // a CU 32), 256 sequences of 500 to 8000 274 (273), 512 branches in e4m3 236 (231),
 // a chunk of 1500 and 48 single tokens on two KV heads 75 (70), two chunks of 7777
-// together 1647 (1647).
+// together 1647 (1647). With many tiles a part has eight blocks at least: 64
+// sequences' nine tokens over 250 to 500, 32 / 8 heads, 29 us, with three 40, with
+// 16 29; over 450 to 900 55, 57 and 45; 16 prompts of 600 to 1200 from nothing 153,
+// 148 and 152.
+// A tile of a causal unit counts with all blocks of its unit, also those behind
+// its last row, and has as many parts: those behind its end are empty, write
+// zeros and are joined with weight 0 (a prompt of 1024 from nothing, 8 / 2 heads:
+// 90 of 192 items of a KV head).
 // Items of at least `big` blocks, the mean, are launched before the others, so
 // that the last round of the chip is made of short ones: 256 sequences of 500 to
 // 8000 tokens 274 -> 268 us, 512 branches in e4m3 236 -> 225, 16 turns of 150 to

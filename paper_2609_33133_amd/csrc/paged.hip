@@ -9,7 +9,12 @@ namespace augtree {
 namespace {
 
 constexpr int kPlanThreads = 1024;
-constexpr int kMergeAlone = 16;  // parts of a row up to which one group of lanes joins them
+// Parts of a row up to which one group of lanes joins them, with more a workgroup.
+// Attention and merge, us, by a workgroup and (a limit of 48) by a group: one
+// sequence of 4096 in 22 parts 11.2 and 14.0, eight branches of 32768 in 23 34.3
+// and 37.1, a chunk of 120 over 9000 in 48 24.4 and 30.4, 64 branches of 9000 in 18
+// 33.2 and 32.2. A limit of six: the same as 16.
+constexpr int kMergeAlone = 16;
 
 // x of the lane that a DPP control names, 0 where it names none.
 template <int CTRL, int ROWS>
@@ -175,7 +180,7 @@ struct GroupTeam {
 // One workgroup: the scans over the sequences and, where the rest is little
 // (FILL: at most kFillSeqs sequences), that too, with all arrays in LDS. Bound
 // by latency: a dozen barriers and the memory round trips between them. 576
-// sequences with 496 rows and 585 items 13.3 us, 4352 sequences 33 us and 9 us
+// sequences with 496 rows and 585 items 13.3 us, 4352 sequences 33 us and 10 us
 // for the second launch (12 with threads for the rows alone).
 template <bool FILL>
 __global__ __launch_bounds__(kPlanThreads) void page_plan_kernel(PlanParams p) {
@@ -216,7 +221,7 @@ __device__ __forceinline__ uint32_t to_e4m3(float a, float b, float c, float d) 
 }
 
 // Rows of K (y = 0) and V (y = 1) into their slots; a thread writes 16 bytes.
-// Bound by HBM: 82660 rows of 4 heads of 128 into e4m3, 254 MB, in 43 us, 5.9 TB/s
+// Bound by HBM: 82660 rows of 4 heads of 128 into e4m3, 254 MB, in 45 us, 5.7 TB/s
 // (eight values a thread and a division each: 62 us); 256 rows of 8 heads in 3 us,
 // the time of a launch.
 template <bool E4M3>
